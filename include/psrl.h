@@ -281,6 +281,79 @@ psrl_status_t psrl_kv_gather(const psrl_plan_t* plan, const void* k_pool, const 
                              int64_t pool_capacity, void* k_tok, void* v_tok, void* stream);
 
 /*
+ * Rotary positions (the step between the projections and the attention).  Pair i of a head's first
+ * `rotary_dim` elements is turned by the angle position * f_i:
+ *   y1 = s (x1 cos - x2 sin),  y2 = s (x2 cos + x1 sin),   the other elements pass through.
+ * A token's position is its place in its own sequence: the tokens of all ancestor segments, then its place in
+ * the segment (seg_anc_tokens + i), so a token shared by many samples is rotated once.
+ *   f_i = base^(-2 i / rotary_dim) radians per position, i < rotary_dim / 2, and with a scaling for contexts
+ *   longer than `original_positions`:
+ *   LINEAR  f_i / factor
+ *   NTK     base replaced by base * factor^(rotary_dim / (rotary_dim - 2))
+ *   YARN    pairs that make more than `high` turns over the original length keep f_i, pairs below `low` turns get
+ *           f_i / factor, a linear ramp over the pair index between them; s = 0.1 ln(factor) + 1
+ *           (Peng et al. 2023; low = 0 means 1, high = 0 means 32)
+ *   BANDED  the same two ends with the ramp linear in the number of turns (low = 0 means 1, high = 0 means 4)
+ * s is 1 unless YARN sets it; attention_scale > 0 replaces it.  Angles are computed exactly modulo a full turn
+ * (64-bit fixed point), so far positions lose nothing.
+ */
+typedef enum { PSRL_ROPE_HALF = 0, PSRL_ROPE_INTERLEAVED = 1 } psrl_rope_layout_t; /* pairs (i, i + rotary_dim/2) | (2i, 2i + 1) */
+typedef enum {
+  PSRL_ROPE_UNSCALED = 0, PSRL_ROPE_LINEAR = 1, PSRL_ROPE_NTK = 2, PSRL_ROPE_YARN = 3, PSRL_ROPE_BANDED = 4
+} psrl_rope_scaling_t;
+typedef struct {
+  int32_t head_dim;           /* multiple of 8, 8..256 */
+  int32_t rotary_dim;         /* even, 2..head_dim */
+  int32_t layout;             /* psrl_rope_layout_t */
+  int32_t scaling;            /* psrl_rope_scaling_t */
+  double base;                /* > 1 */
+  double factor;              /* > 0, finite; read by every scaling but UNSCALED; YARN and BANDED: >= 1 */
+  int32_t original_positions; /* YARN, BANDED: >= 1 */
+  double low, high;           /* YARN, BANDED: turns, 0 <= low < high, 0 = the defaults above */
+  double attention_scale;     /* 0 = as above */
+} psrl_rope_desc_t;
+typedef struct psrl_rope psrl_rope_t;
+
+/* Host only.  Errors: INVALID_ARG, SHAPE (dimensions), HOST_OOM.  On error *out is NULL. */
+psrl_status_t psrl_rope_create(const psrl_rope_desc_t* desc, psrl_rope_t** out);
+/* Borrowed HOST pointer to the rotary_dim / 2 frequencies (radians per position) and the factor s. */
+psrl_status_t psrl_rope_frequencies(const psrl_rope_t* rope, const double** freq, int32_t* n, double* scale);
+void psrl_rope_destroy(psrl_rope_t* rope);
+
+/*
+ * psrl_rope_qkv_fwd - rotates the query rows and puts their keys and values into the pools, in one launch.
+ * Row r is query row r of the plan (the tokens of the HAS_Q segments in canonical order; the K/V of other
+ * segments is in the pools already, rotated, and is left alone).
+ *   q  [T_q, Hq, d], k, v [T_q, Hkv, d]  DEVICE, plan dtype; row r at r * pitch elements, heads contiguous, so the
+ *      three may be slices of one projection output
+ *   q_out [T_q, Hq, d] contiguous: rotated Q (may be q itself when q is contiguous)
+ *   k_pool, v_pool [Hkv, pool_capacity, d]: rotated K and V of row r at the slot of its token; other slots untouched
+ * A source may be NULL (with its destination ignored): skipped.  Pointers 16-byte aligned, pitches a multiple of
+ * 16 bytes and at least a row.  Sources and destinations must not overlap otherwise.
+ * Errors: INVALID_ARG, SHAPE (rope head_dim, pool size, pitches), WORKSPACE (plan not uploaded), CUDA.  Asynchronous.
+ *
+ * psrl_rope_qkv_bwd - the way back: the transposed (inverse) rotation of d_q and of the rows' slots of dk_pool, and the
+ * rows' slots of dv_pool, to row-major dq_out, dk_out, dv_out with pitches (dq_out may be d_q when contiguous).
+ */
+psrl_status_t psrl_rope_qkv_fwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const void* q, int64_t q_pitch,
+                                const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* q_out,
+                                void* k_pool, void* v_pool, int64_t pool_capacity, void* stream);
+psrl_status_t psrl_rope_qkv_bwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const void* d_q, const void* dk_pool,
+                                const void* dv_pool, int64_t pool_capacity, void* dq_out, int64_t dq_pitch,
+                                void* dk_out, int64_t dk_pitch, void* dv_out, int64_t dv_pitch, void* stream);
+
+/*
+ * psrl_rope_rows - the same rotation without a plan, for rows at positions of their own (one new token for each
+ * sequence of a rollout).
+ *   x, y  [n_rows, n_heads, d] DEVICE of `dtype`, rows at pitches as above; y may be x (equal pitches)
+ *   positions [n_rows] DEVICE int32, any value;  inverse != 0: the transposed rotation
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), CUDA.  n_rows = 0 does nothing.  Asynchronous.
+ */
+psrl_status_t psrl_rope_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const void* x, int64_t x_pitch,
+                             const int32_t* positions, int64_t n_rows, int32_t n_heads, void* y, int64_t y_pitch,
+                             int inverse, void* stream);
+
+/*
  * Benchmark aid (no counterpart in the paper): psrl_tree_attn_bwd with a mask
  * of the backward kernels to launch, so that each can be timed on its own
  * with CUDA events.  Bit 0: D = rowsum(dO o O) pre-pass, bit 1: dQ kernel

@@ -2,7 +2,8 @@
  * psrl_cache.h - Dynamic Block Caching for prefix-shared KV (paper Sec. 5.2) over an ordered list of
  * micro-batches (Sec. 4.1 inter-batch and self-sequence sharing, Sec. 4.3 token-wise micro-batching).
  *
- * Host-only bookkeeping, no CUDA call, no data movement.  The caller owns one arena of KV slots per
+ * The manager is host-only bookkeeping: no CUDA call, no data movement (psrl_kv_copy and psrl_kv_move below do
+ * that on the caller's pools).  The caller owns one arena of KV slots per
  * worker (the K/V pools passed to psrl_tree_attn_fwd / _bwd).  Blocks are the segments of the prefix
  * forest (Sec. 5.1: one block per reusable prefix span); a segment occupies one contiguous extent of
  * ceil(len / block) * block slots.  For every micro-batch the manager says which segments take part
@@ -91,6 +92,46 @@ typedef struct {
   int64_t total_slots;      /* sum of all extents: what keeping every block would take */
 } psrl_cache_stats_t;
 psrl_status_t psrl_cache_stats(const psrl_cache_t* cache, psrl_cache_stats_t* out);
+
+/*
+ * Compaction: between end(m) and begin(m + 1) the resident blocks are slid down to the start of the arena, in address
+ * order, so that all free slots are one extent again.  (The paper has no counterpart: its blocks are tensors of their
+ * own, and the allocator below it does this.)  The manager's bookkeeping is updated at once; the caller performs the
+ * listed moves on its pools - K and V, and any other tensor in pool layout that must outlive the call - with
+ * psrl_kv_move before the next micro-batch.  Blocks that follow one another are listed as one extent.
+ *   *moves  HOST, borrowed until the next call, ascending, each destination below its source; may be NULL with *n_moves
+ *   *top    one past the highest resident slot afterwards (may be NULL)
+ * Errors: INVALID_ARG (inside a micro-batch, or the cache is unusable), HOST_OOM.
+ */
+typedef struct {
+  int32_t src_slot, dst_slot, n_slots;
+} psrl_kv_extent_t;
+psrl_status_t psrl_cache_compact(psrl_cache_t* cache, int32_t* n_moves, const psrl_kv_extent_t** moves, int64_t* top);
+
+/*
+ * psrl_kv_copy - copies extents of slots, for all KV heads, from one pair of pools to another (evicted blocks to a
+ * spill buffer, reloaded blocks back, a block to a second arena).
+ *   extents    HOST, read during the call; destinations disjoint; n_slots = 0 does nothing
+ *   row_bytes  head_dim * element size: 128, 256 or 512
+ *   k_src, v_src [n_kv_heads, src_capacity, row_bytes], k_dst, v_dst [n_kv_heads, dst_capacity, row_bytes] DEVICE,
+ *              16-byte aligned; a NULL source is skipped.  A pool may be copied into itself when no written slot is read.
+ * Slots outside the destinations are not touched.
+ * Errors: INVALID_ARG (also overlapping destinations or tensors), SHAPE (extents outside the pools), CUDA, HOST_OOM.
+ * Asynchronous on `stream`; may be captured into a graph (the extents are baked in).
+ *
+ * psrl_kv_move - the same inside one pair of pools, for moves down that may overlap: as if every source were read before
+ * anything is written.
+ *   extents    ascending in source and destination, each disjoint from the next, dst_slot <= src_slot
+ *   workspace  DEVICE, 256 bytes, 256-byte aligned: status word (psrl_device_status) and counters; calls that may overlap
+ *              on the GPU need distinct workspaces
+ * Slots that no destination covers keep what they held.  Errors as above, and WORKSPACE.
+ */
+psrl_status_t psrl_kv_copy(const psrl_kv_extent_t* extents, int32_t n_extents, int32_t n_kv_heads, int32_t row_bytes,
+                           const void* k_src, const void* v_src, int64_t src_capacity, void* k_dst, void* v_dst,
+                           int64_t dst_capacity, void* stream);
+psrl_status_t psrl_kv_move(const psrl_kv_extent_t* extents, int32_t n_extents, int32_t n_kv_heads, int32_t row_bytes,
+                           void* k_pool, void* v_pool, int64_t pool_capacity, void* workspace, size_t workspace_bytes,
+                           void* stream);
 
 /* Current reference count of every segment, [n_segments] (borrowed). */
 psrl_status_t psrl_cache_refcounts(const psrl_cache_t* cache, const int32_t** refcount);

@@ -32,6 +32,9 @@ EXPORTS = [
     "psrl_cache_create", "psrl_cache_begin", "psrl_cache_end", "psrl_cache_stats", "psrl_cache_refcounts",
     "psrl_cache_destroy",
     "psrl_kv_scatter", "psrl_kv_gather",
+    "psrl_rope_create", "psrl_rope_frequencies", "psrl_rope_destroy", "psrl_rope_qkv_fwd", "psrl_rope_qkv_bwd",
+    "psrl_rope_rows",
+    "psrl_cache_compact", "psrl_kv_copy", "psrl_kv_move",
     "psrl_cost_sequence", "psrl_group_workloads", "psrl_place_groups", "psrl_microbatch_tokens",
 ]
 
@@ -72,6 +75,12 @@ class CacheStep(C.Structure):
 class CacheStats(C.Structure):
     _fields_ = [("peak_slots", C.c_int64), ("evicted_slots", C.c_int64), ("reloaded_slots", C.c_int64),
                 ("pool_high_water", C.c_int64), ("total_slots", C.c_int64)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("original_positions", C.c_int32), ("low", C.c_double),
+                ("high", C.c_double), ("attention_scale", C.c_double)]
 
 
 _VIEW_SCALARS32 = ["n_seg", "n_groups", "n_pages", "n_samples", "max_depth", "T", "T_q", "pool_slots"]
@@ -169,6 +178,27 @@ def lib() -> C.CDLL:
     L.psrl_cache_refcounts.restype = C.c_int
     L.psrl_cache_destroy.argtypes = [C.c_void_p]
     L.psrl_cache_destroy.restype = None
+    L.psrl_cache_compact.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(_I32P), C.POINTER(C.c_int64)]
+    L.psrl_cache_compact.restype = C.c_int
+    L.psrl_kv_copy.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64,
+                               C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]
+    L.psrl_kv_copy.restype = C.c_int
+    L.psrl_kv_move.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64,
+                               C.c_void_p, C.c_size_t, C.c_void_p]
+    L.psrl_kv_move.restype = C.c_int
+    L.psrl_rope_create.argtypes = [C.POINTER(RopeDesc), C.POINTER(C.c_void_p)]
+    L.psrl_rope_create.restype = C.c_int
+    L.psrl_rope_frequencies.argtypes = [C.c_void_p, C.POINTER(_F64P), C.POINTER(C.c_int32), C.POINTER(C.c_double)]
+    L.psrl_rope_frequencies.restype = C.c_int
+    L.psrl_rope_destroy.argtypes = [C.c_void_p]
+    L.psrl_rope_destroy.restype = None
+    _VP, _I64 = C.c_void_p, C.c_int64
+    L.psrl_rope_qkv_fwd.argtypes = [_VP, _VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _I64, _VP]
+    L.psrl_rope_qkv_fwd.restype = C.c_int
+    L.psrl_rope_qkv_bwd.argtypes = [_VP, _VP, _VP, _VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP]
+    L.psrl_rope_qkv_bwd.restype = C.c_int
+    L.psrl_rope_rows.argtypes = [_VP, C.c_int, _VP, _I64, _VP, _I64, C.c_int32, _VP, _I64, C.c_int, _VP]
+    L.psrl_rope_rows.restype = C.c_int
     L.psrl_launch_count.argtypes = [C.c_void_p, C.c_int]
     L.psrl_launch_count.restype = C.c_int
     L.psrl_last_cuda_error.restype = C.c_char_p
@@ -425,6 +455,213 @@ def psrl_kv_gather(plan: Plan, k_pool, v_pool, k_tok=None, v_tok=None, stream=No
     return k_tok, v_tok
 
 
+class _on_device_of:
+    """The tensors' device as the current one (the library launches there) and the stream of the call on it: the
+    caller's, or torch's current stream of that device."""
+
+    def __init__(self, stream, *tensors):
+        import torch
+
+        dev = tensors[0].device
+        for t in tensors:
+            if t.device != dev:
+                raise ValueError(f"tensors on {t.device} and {dev}: one call works on one device")
+        if dev.type != "cuda":
+            raise RuntimeError("tensors must live on a CUDA device: this library has no CPU path")
+        if getattr(stream, "device", dev) != dev:
+            raise ValueError(f"stream of {stream.device} for tensors on {dev}")
+        self.other = dev.index != torch.cuda.current_device()
+        self.guard = torch.cuda.device(dev) if self.other else None
+        if stream is None:
+            self.given, self.ptr = None, torch.cuda.current_stream(dev).cuda_stream
+        else:
+            self.given = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=dev)
+            self.ptr = self.given.cuda_stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self
+
+    def __exit__(self, *e):
+        if self.guard is not None:
+            self.guard.__exit__(*e)
+
+    def keep(self, t):
+        """A tensor made for this call: not to be reused before the call's stream has passed it."""
+        if self.given is not None:
+            t.record_stream(self.given)
+        return t
+
+
+_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+_ROPE_SCALINGS = {None: 0, "none": 0, "linear": 1, "ntk": 2, "yarn": 3, "banded": 4}
+
+
+class Rope:
+    """Owner of a psrl_rope_t: a rotary position embedding (include/psrl.h has the formulas).  `freq` holds the radians
+    per position of each pair, `scale` the factor on cos and sin.  low / high / attention_scale 0: the defaults."""
+
+    def __init__(self, head_dim: int, rotary_dim: int = 0, base: float = 10000.0, layout: str = "half",
+                 scaling: Optional[str] = None, factor: float = 1.0, original_positions: int = 0, low: float = 0.0,
+                 high: float = 0.0, attention_scale: float = 0.0):
+        self._h = C.c_void_p()
+        if layout not in _ROPE_LAYOUTS or scaling not in _ROPE_SCALINGS:
+            raise ValueError(f"layout {layout!r} or scaling {scaling!r} unknown")
+        d = RopeDesc(int(head_dim), int(rotary_dim or head_dim), _ROPE_LAYOUTS[layout], _ROPE_SCALINGS[scaling], float(base),
+                     float(factor), int(original_positions), float(low), float(high), float(attention_scale))
+        _check(lib().psrl_rope_create(C.byref(d), C.byref(self._h)), "psrl_rope_create")
+        f, n, sc = C.POINTER(C.c_double)(), C.c_int32(), C.c_double()
+        _check(lib().psrl_rope_frequencies(self._h, C.byref(f), C.byref(n), C.byref(sc)), "psrl_rope_frequencies")
+        self.head_dim, self.rotary_dim = d.head_dim, d.rotary_dim
+        self.freq, self.scale = np.ctypeslib.as_array(f, shape=(n.value,)).copy(), float(sc.value)
+
+    def __del__(self):
+        if getattr(self, "_h", None) and self._h.value:
+            lib().psrl_rope_destroy(self._h)
+            self._h = C.c_void_p()
+
+
+def _rows_pitch(t, rows: int, heads: int, d: int, name: str) -> int:
+    """Row pitch in elements of a [rows, heads, d] tensor whose rows may be slices of a wider matrix."""
+    if t.shape != (rows, heads, d):
+        raise ValueError(f"{name} must be [{rows}, {heads}, {d}], got {tuple(t.shape)}")
+    s = t.stride()
+    if (s[2] != 1 and d > 1) or (s[1] != d and heads > 1):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return s[0] if rows > 1 else heads * d
+
+
+def _rope_pools(plan, *pools):
+    for p in pools:
+        if p.dim() != 3 or p.shape != pools[0].shape or p.shape[0] != plan.n_kv_heads or p.shape[2] != plan.head_dim or not p.is_contiguous():
+            raise ValueError("pools must be contiguous [Hkv, capacity, d]")
+    return int(pools[0].shape[1])
+
+
+def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=None, stream=None):
+    """Rotates the query rows' Q [T_q, Hq, d] into q_out and their K, V [T_q, Hkv, d] into the pools (K rotated), in one
+    launch.  q, k, v may be slices of one projection output (rows at any pitch).  Returns q_out."""
+    import torch
+
+    V, d = plan.view, plan.head_dim
+    _check_dtype(plan, q, k, v, k_pool, v_pool)
+    pq = _rows_pitch(q, V["T_q"], plan.n_q_heads, d, "q")
+    pk, pv = (_rows_pitch(t, V["T_q"], plan.n_kv_heads, d, n) for t, n in ((k, "k"), (v, "v")))
+    cap = _rope_pools(plan, k_pool, v_pool)
+    with _on_device_of(stream, q, k, v, k_pool, v_pool) as on:
+        if q_out is None:
+            q_out = on.keep(torch.empty((V["T_q"], plan.n_q_heads, d), dtype=q.dtype, device=q.device))
+        else:
+            _check_dtype(plan, q_out)
+            if q_out.shape != q.shape or not q_out.is_contiguous() or q_out.device != q.device:
+                raise ValueError("q_out must be contiguous [T_q, Hq, d] on the same device")
+        _check(lib().psrl_rope_qkv_fwd(plan._h, rope._h, q.data_ptr(), pq, k.data_ptr(), pk, v.data_ptr(), pv,
+                                       q_out.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), cap, on.ptr),
+               "psrl_rope_qkv_fwd")
+    return q_out
+
+
+def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None, dk_out=None, dv_out=None, stream=None):
+    """The way back: inverse rotation of d_q and of the query rows' slots of dk_pool, and the rows' slots of dv_pool, to
+    dq_out [T_q, Hq, d], dk_out, dv_out [T_q, Hkv, d] (which may be slices of one gradient matrix).  Returns the three."""
+    import torch
+
+    V, d = plan.view, plan.head_dim
+    _check_dtype(plan, d_q, dk_pool, dv_pool)
+    if d_q.shape != (V["T_q"], plan.n_q_heads, d) or not d_q.is_contiguous():
+        raise ValueError("d_q must be contiguous [T_q, Hq, d]")
+    cap = _rope_pools(plan, dk_pool, dv_pool)
+    with _on_device_of(stream, d_q, dk_pool, dv_pool) as on:
+        outs, pitch = [], []
+        for t, heads, name in ((dq_out, plan.n_q_heads, "dq_out"), (dk_out, plan.n_kv_heads, "dk_out"), (dv_out, plan.n_kv_heads, "dv_out")):
+            if t is None:
+                t = on.keep(torch.empty((V["T_q"], heads, d), dtype=d_q.dtype, device=d_q.device))
+            else:
+                _check_dtype(plan, t)
+                if t.device != d_q.device:
+                    raise ValueError(f"{name} lives on another device")
+            outs.append(t)
+            pitch.append(_rows_pitch(t, V["T_q"], heads, d, name))
+        _check(lib().psrl_rope_qkv_bwd(plan._h, rope._h, d_q.data_ptr(), dk_pool.data_ptr(), dv_pool.data_ptr(), cap,
+                                       outs[0].data_ptr(), pitch[0], outs[1].data_ptr(), pitch[1], outs[2].data_ptr(),
+                                       pitch[2], on.ptr), "psrl_rope_qkv_bwd")
+    return tuple(outs)
+
+
+def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stream=None):
+    """Rotates x [rows, heads, head_dim] (f32 or bf16, rows at any pitch) at int32 `positions` [rows].  Returns y (y may be x)."""
+    import torch
+
+    dt = {torch.float32: PSRL_F32, torch.bfloat16: PSRL_BF16}.get(x.dtype)
+    if dt is None:
+        raise TypeError(f"dtype {x.dtype} is neither float32 nor bfloat16")
+    if x.dim() != 3:
+        raise ValueError("x must be [rows, heads, head_dim]")
+    if positions.dtype != torch.int32 or positions.shape != x.shape[:1] or not positions.is_contiguous():
+        raise ValueError("positions must be contiguous int32 [rows]")
+    rows, heads = x.shape[0], x.shape[1]
+    px = _rows_pitch(x, rows, heads, rope.head_dim, "x")
+    with _on_device_of(stream, x, positions) as on:
+        if y is None:
+            y = on.keep(torch.empty(x.shape, dtype=x.dtype, device=x.device))
+        elif y.dtype != x.dtype or y.device != x.device:
+            raise ValueError("y must have x's type and device")
+        _check(lib().psrl_rope_rows(rope._h, dt, x.data_ptr(), px, positions.data_ptr(), rows, heads, y.data_ptr(),
+                                    _rows_pitch(y, rows, heads, rope.head_dim, "y"), int(bool(inverse)), on.ptr),
+               "psrl_rope_rows")
+    return y
+
+
+def _extents(extents):
+    """[n, 3] int32 (source slot, destination slot, slots), kept alive by the caller, and its address."""
+    e = np.ascontiguousarray(extents, dtype=np.int32)
+    if e.size == 0:
+        return e, 0, None
+    if e.ndim != 2 or e.shape[1] != 3:
+        raise ValueError("extents must be [n, 3]: source slot, destination slot, slots")
+    return e, len(e), e.ctypes.data
+
+
+def _pair_of_pools(k, v, what: str):
+    import torch
+
+    if k.dtype not in (torch.float32, torch.bfloat16) or v.dtype != k.dtype:
+        raise TypeError(f"{what} must both be float32 or both bfloat16")
+    if k.dim() != 3 or k.shape != v.shape or not k.is_contiguous() or not v.is_contiguous():
+        raise ValueError(f"{what} must be contiguous [Hkv, capacity, d] of one shape")
+    return int(k.shape[0]), int(k.shape[1]), int(k.shape[2]) * k.element_size()
+
+
+def psrl_kv_copy(extents, k_src, v_src, k_dst, v_dst, stream=None):
+    """Copies extents [n, 3] (source slot, destination slot, slots) of all heads from the pools k_src, v_src
+    [Hkv, capacity, d] to k_dst, v_dst (another capacity is fine).  Destinations must not overlap one another, nor, inside
+    one pool, any source."""
+    heads, cap, row = _pair_of_pools(k_src, v_src, "source pools")
+    heads2, cap2, row2 = _pair_of_pools(k_dst, v_dst, "destination pools")
+    if heads != heads2 or row != row2 or k_src.dtype != k_dst.dtype:
+        raise ValueError("source and destination pools differ in heads, head dimension or type")
+    e, n, at = _extents(extents)
+    with _on_device_of(stream, k_src, v_src, k_dst, v_dst) as on:
+        _check(lib().psrl_kv_copy(at, n, heads, row, k_src.data_ptr(), v_src.data_ptr(), cap, k_dst.data_ptr(),
+                                  v_dst.data_ptr(), cap2, on.ptr), "psrl_kv_copy")
+
+
+def psrl_kv_move(moves, k_pool, v_pool, stream=None, workspace=None):
+    """Performs the moves of a compaction ([n, 3], ascending, downwards: Cache.compact()) inside the pools, as if every
+    source were read first.  `workspace`: (pointer, bytes) of 256 bytes of device memory; allocated if not given."""
+    import torch
+
+    heads, cap, row = _pair_of_pools(k_pool, v_pool, "pools")
+    e, n, at = _extents(moves)
+    with _on_device_of(stream, k_pool, v_pool) as on:
+        if workspace is None:
+            buf = on.keep(torch.empty(512, dtype=torch.uint8, device=k_pool.device))
+            workspace = ((buf.data_ptr() + 255) // 256 * 256, 256)
+        _check(lib().psrl_kv_move(at, n, heads, row, k_pool.data_ptr(), v_pool.data_ptr(), cap, workspace[0], workspace[1],
+                                  on.ptr), "psrl_kv_move")
+
+
 def _flags_ptr(seg_flags):
     if seg_flags is None:
         return None, None
@@ -518,6 +755,15 @@ class Cache:
         nf, ptr, live = C.c_int32(), _I32P(), C.c_int64()
         _check(lib().psrl_cache_end(self._h, int(m), C.byref(nf), C.byref(ptr), C.byref(live)), "psrl_cache_end")
         return dict(freed=[int(ptr[i]) for i in range(nf.value)], live_slots=int(live.value))
+
+    def compact(self):
+        """Slides the resident blocks together (between end and the next begin).  Returns the moves for psrl_kv_move,
+        [n, 3] int32, and the slot behind the last resident block."""
+        n, ptr, top = C.c_int32(), _I32P(), C.c_int64()
+        _check(lib().psrl_cache_compact(self._h, C.byref(n), C.byref(ptr), C.byref(top)), "psrl_cache_compact")
+        k = n.value
+        moves = np.ctypeslib.as_array(ptr, shape=(k, 3)).copy() if k else np.zeros((0, 3), dtype=np.int32)
+        return moves, int(top.value)
 
     def stats(self) -> dict:
         s = CacheStats()

@@ -27,6 +27,7 @@ struct Cache {
   // buffers behind the borrowed pointers
   std::vector<int32_t> o_seg, o_parent, o_len, o_gbs, o_base, o_new, o_reload, o_evict, o_evict_base, o_freed, local;
   std::vector<uint8_t> o_flags;
+  std::vector<psrl_kv_extent_t> o_moves;
 
   int64_t alloc(int64_t size) {
     for (size_t i = 0; i < free_list.size(); ++i) {
@@ -270,6 +271,48 @@ psrl_status_t psrl_cache_end(psrl_cache_t* h, int32_t m, int32_t* n_freed, const
   if (n_freed) *n_freed = static_cast<int32_t>(c.o_freed.size());
   if (freed_seg) *freed_seg = c.o_freed.data();
   if (live_slots) *live_slots = c.live();
+  return PSRL_OK;
+}
+
+psrl_status_t psrl_cache_compact(psrl_cache_t* h, int32_t* n_moves, const psrl_kv_extent_t** moves, int64_t* top) {
+  if (!h || (moves && !n_moves)) return PSRL_ERR_INVALID_ARG;
+  Cache& c = h->c;
+  if (c.dead || c.in_mb) return PSRL_ERR_INVALID_ARG;
+  try {
+    std::vector<int32_t> order;
+    for (int32_t s = 0; s < c.n; ++s)
+      if (c.base[s] >= 0) order.push_back(s);
+    std::sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return c.base[a] < c.base[b]; });
+    std::vector<psrl_kv_extent_t> out;
+    std::vector<Extent> rest;
+    int64_t at = 0;
+    for (int32_t s : order) {
+      const int64_t from = c.base[s], len = c.extent[s];
+      if (from != at) {
+        if (!out.empty() && out.back().src_slot + int64_t(out.back().n_slots) == from &&
+            out.back().dst_slot + int64_t(out.back().n_slots) == at)
+          out.back().n_slots += static_cast<int32_t>(len);
+        else
+          out.push_back({static_cast<int32_t>(from), static_cast<int32_t>(at), static_cast<int32_t>(len)});
+      }
+      at += len;
+    }
+    const int64_t all = c.capacity ? c.capacity : (int64_t(1) << 40);
+    if (at < all) rest.push_back(Extent{at, all - at});
+    // nothing below allocates: the bookkeeping changes as a whole or not at all
+    c.o_moves.swap(out);
+    c.free_list.swap(rest);
+    int64_t to = 0;
+    for (int32_t s : order) {
+      c.base[s] = to;
+      to += c.extent[s];
+    }
+    if (n_moves) *n_moves = static_cast<int32_t>(c.o_moves.size());
+    if (moves) *moves = c.o_moves.data();
+    if (top) *top = at;
+  } catch (const std::bad_alloc&) {
+    return PSRL_ERR_HOST_OOM;
+  }
   return PSRL_OK;
 }
 

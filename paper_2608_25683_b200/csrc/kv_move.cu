@@ -1,0 +1,359 @@
+// Copying and compacting blocks of the paged K/V pools: the data movement behind the cache manager's decisions
+// (paper Sec. 5.2: blocks are evicted, restored and released as micro-batches come and go).
+//
+// psrl_kv_copy moves extents between pools that do not overlap.  psrl_kv_move slides extents down inside a pool, where
+// an extent's destination may overlap its own source or an earlier extent's: a memmove over a whole arena in one pass.
+//
+// Both are bound by HBM (every byte read once, written once).  The extent list is host data and travels in the kernel's
+// parameters, so a call needs no device copy of it, may be captured into a graph, and leaves nothing behind.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "../../include/psrl_cache.h"
+#include "kernels.h"
+
+namespace psrl {
+namespace {
+
+struct Pools {
+  const uint4 *k_src, *v_src;
+  uint4 *k_dst, *v_dst;
+  int64_t src_cap, dst_cap;
+  int32_t heads;
+  int32_t vecs;  // 16-byte vectors per slot and head
+};
+
+// ------------------------------------------------------------------------------------------------ disjoint copies
+
+constexpr int kCopyThreads = 256, kCopyPiece = 1024;  // vectors of one block: 16 KB, four per thread
+
+template <int kMax>
+struct CopyList {
+  int32_t n;
+  int32_t piece_slots;
+  int32_t src[kMax], dst[kMax], slots[kMax];
+  int32_t first_piece[kMax + 1];
+};
+
+template <int kMax>
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyList<kMax> list, const Pools p) {
+  const int piece = blockIdx.x, head = blockIdx.y;
+  int lo = 0, hi = list.n;  // the last extent whose first piece is <= piece
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (list.first_piece[mid] <= piece) lo = mid; else hi = mid;
+  }
+  const int at = (piece - list.first_piece[lo]) * list.piece_slots;
+  const int n = min(list.piece_slots, list.slots[lo] - at) * p.vecs;
+  const uint4* src = blockIdx.z ? p.v_src : p.k_src;
+  uint4* dst = blockIdx.z ? p.v_dst : p.k_dst;
+  if (!src) return;
+  src += (int64_t(head) * p.src_cap + list.src[lo] + at) * p.vecs;
+  dst += (int64_t(head) * p.dst_cap + list.dst[lo] + at) * p.vecs;
+  uint4 r[kCopyPiece / kCopyThreads];
+#pragma unroll
+  for (int i = 0; i < kCopyPiece / kCopyThreads; ++i)
+    if (threadIdx.x + i * kCopyThreads < n) r[i] = src[threadIdx.x + i * kCopyThreads];
+#pragma unroll
+  for (int i = 0; i < kCopyPiece / kCopyThreads; ++i)
+    if (threadIdx.x + i * kCopyThreads < n) dst[threadIdx.x + i * kCopyThreads] = r[i];
+}
+
+template <int kMax>
+psrl_status_t launch_copies(const psrl_kv_extent_t* ext, int32_t n, const Pools& p, cudaStream_t stream) {
+  CopyList<kMax> list;
+  list.piece_slots = std::max(1, kCopyPiece / p.vecs);
+  for (int32_t at = 0; at < n; at += kMax) {
+    list.n = std::min(kMax, n - at);
+    int64_t pieces = 0;
+    for (int32_t i = 0; i < list.n; ++i) {
+      const psrl_kv_extent_t& e = ext[at + i];
+      list.src[i] = e.src_slot; list.dst[i] = e.dst_slot; list.slots[i] = e.n_slots;
+      list.first_piece[i] = static_cast<int32_t>(pieces);
+      pieces += (int64_t(e.n_slots) + list.piece_slots - 1) / list.piece_slots;
+      if (pieces > INT32_MAX) return PSRL_ERR_SHAPE;
+    }
+    list.first_piece[list.n] = static_cast<int32_t>(pieces);
+    copy_kernel<kMax><<<dim3(unsigned(pieces), unsigned(p.heads), 2), kCopyThreads, 0, stream>>>(list, p);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) { set_last_cuda_error(e); return PSRL_ERR_CUDA; }
+  }
+  return PSRL_OK;
+}
+
+psrl_status_t copy_extents(const psrl_kv_extent_t* ext, int32_t n, const Pools& p, cudaStream_t stream) {
+  // a short list costs a launch less parameter traffic
+  return n <= 64 ? launch_copies<64>(ext, n, p, stream) : launch_copies<1000>(ext, n, p, stream);
+}
+
+// ------------------------------------------------------------------------------------------------ moves in place
+//
+// The slots of all extents, in ascending order, of every (pool, head) are one long sequence of 16-byte vectors, cut into
+// chunks of one load per thread slot of the whole grid.  Vectors only move down, and a chunk's sources lie above every
+// destination of the chunks before it, so
+//   - a chunk may be loaded while earlier chunks are still being stored, and
+//   - a chunk may be stored once it and the chunks before it have been loaded by EVERY block,
+// which is the only synchronisation: one counter per chunk parity.  The next chunk's loads are in flight while a block
+// waits.  All blocks are resident (cooperative launch), and the wait is bounded.
+
+constexpr int kMoveThreads = 512, kMoveRegs = 8;           // 64 KB per block and chunk
+constexpr int kWarpVecs = 32 * kMoveRegs;                  // a warp's part of a chunk: 4 KB of consecutive vectors
+constexpr int kMoveMax = 1000;
+
+struct MoveList {
+  int32_t n;
+  int32_t slots;              // sum of the extents
+  int32_t src[kMoveMax], dst[kMoveMax];
+  int32_t first[kMoveMax + 1];  // slots before the extent
+};
+
+struct Held {
+  uint4 v[kMoveRegs];
+  uint4* to[kMoveRegs];  // nullptr past the end
+};
+
+__device__ __forceinline__ void load_part(const MoveList& list, const Pools& p, uint32_t warp_part, uint32_t total_rows, Held& h) {
+  const int lane = threadIdx.x & 31;
+  // the rows (slot of one pool and head) of this warp's part; lane i looks up row i
+  const uint32_t rows = kWarpVecs / p.vecs;
+  const uint64_t row0 = uint64_t(warp_part) * rows;
+  int64_t src_at = -1, dst_at = 0;
+  int pool = 0;
+  if (lane < int(rows) && row0 + lane < total_rows) {
+    const uint32_t row = uint32_t(row0) + lane;
+    const uint32_t ph = row / uint32_t(list.slots);
+    const int s = int(row - ph * uint32_t(list.slots));
+    pool = ph >= uint32_t(p.heads);
+    const int head = int(ph) - pool * p.heads;
+    int lo = 0, hi = list.n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (list.first[mid] <= s) lo = mid; else hi = mid;
+    }
+    const int in = s - list.first[lo];
+    src_at = (int64_t(head) * p.src_cap + list.src[lo] + in) * p.vecs;
+    dst_at = (int64_t(head) * p.src_cap + list.dst[lo] + in) * p.vecs;
+  }
+#pragma unroll
+  for (int j = 0; j < kMoveRegs; ++j) {
+    const int vec = j * 32 + lane, r = vec / p.vecs, x = vec % p.vecs;
+    const int64_t s = __shfl_sync(0xffffffffu, src_at, r), d = __shfl_sync(0xffffffffu, dst_at, r);
+    const int z = __shfl_sync(0xffffffffu, pool, r);
+    h.to[j] = nullptr;
+    if (s >= 0) {
+      h.v[j] = __ldcg((z ? p.v_src : p.k_src) + s + x);
+      h.to[j] = (z ? p.v_dst : p.k_dst) + d + x;
+    }
+  }
+}
+
+// True once every thread of the block holds its loads: the barrier's predicate depends on their values.
+__device__ __forceinline__ void settle(const Held& h) {
+  uint32_t x = 0;
+#pragma unroll
+  for (int j = 0; j < kMoveRegs; ++j)
+    if (h.to[j]) x |= h.v[j].x ^ h.v[j].y ^ h.v[j].z ^ h.v[j].w;
+  __threadfence();
+  __syncthreads_or(x != 0);
+}
+
+__device__ __forceinline__ void store_part(const Held& h) {
+#pragma unroll
+  for (int j = 0; j < kMoveRegs; ++j)
+    if (h.to[j]) *h.to[j] = h.v[j];
+}
+
+// ws[0] status, ws[16], ws[32] blocks that have loaded their part of the even / odd chunks
+__global__ void __launch_bounds__(kMoveThreads, 1) move_kernel(const __grid_constant__ MoveList list, const Pools p,
+                                                               int* ws, uint32_t n_chunks, uint32_t total_rows) {
+  const uint32_t warps = gridDim.x * (kMoveThreads / 32);
+  const uint32_t mine = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5);
+  __shared__ int s_go;
+  Held h[2];
+  load_part(list, p, mine, total_rows, h[0]);
+  auto step = [&](uint32_t c, Held& now, Held& next) -> bool {
+    settle(now);
+    if (threadIdx.x == 0) {
+      __threadfence();
+      atomicAdd(ws + 16 + 16 * (c & 1), 1);
+    }
+    if (c + 1 < n_chunks) load_part(list, p, (c + 1) * warps + mine, total_rows, next);
+    if (threadIdx.x == 0) {
+      const int want = int((c / 2 + 1) * gridDim.x);
+      int ok = 0;
+      for (uint32_t it = 0; it < (1u << 22) && !ok; ++it) {
+        int seen;
+        asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(ws + 16 + 16 * (c & 1)) : "memory");
+        ok = seen >= want;
+        if (it > 256) __nanosleep(64);
+      }
+      if (!ok) atomicExch(ws, int(PSRL_ERR_TIMEOUT));
+      __threadfence();
+      s_go = ok;
+    }
+    __syncthreads();
+    if (!s_go) return false;  // block-uniform: nothing more is written by this block
+    store_part(now);
+    return true;
+  };
+  for (uint32_t c = 0; c < n_chunks; c += 2) {
+    if (!step(c, h[0], h[1])) return;
+    if (c + 1 >= n_chunks) return;
+    if (!step(c + 1, h[1], h[0])) return;
+  }
+}
+
+psrl_status_t move_extents(const psrl_kv_extent_t* ext, int32_t n, Pools p, int* ws, cudaStream_t stream) {
+  MoveList list;
+  list.n = n;
+  int64_t slots = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    list.src[i] = ext[i].src_slot; list.dst[i] = ext[i].dst_slot; list.first[i] = static_cast<int32_t>(slots);
+    slots += ext[i].n_slots;
+  }
+  list.first[n] = static_cast<int32_t>(slots);
+  list.slots = static_cast<int32_t>(slots);
+  if (!p.k_src) { p.k_src = p.v_src; p.k_dst = p.v_dst; p.v_src = nullptr; }
+  const int64_t rows = slots * p.heads * (p.v_src ? 2 : 1);
+  if (rows > INT32_MAX) return PSRL_ERR_SHAPE;
+  const int64_t block_rows = int64_t(kMoveThreads) * kMoveRegs / p.vecs;
+  const int64_t grid = std::min<int64_t>(resident_ctas(), (rows + block_rows - 1) / block_rows);
+  uint32_t n_chunks = static_cast<uint32_t>((rows + grid * block_rows - 1) / (grid * block_rows));
+  uint32_t total = static_cast<uint32_t>(rows);
+  void* args[] = {&list, &p, &ws, &n_chunks, &total};
+  cudaError_t e = cudaMemsetAsync(ws, 0, kWsHeaderBytes, stream);
+  if (e == cudaSuccess)
+    e = cudaLaunchCooperativeKernel(reinterpret_cast<void*>(move_kernel), dim3(unsigned(grid)), dim3(kMoveThreads), args, 0, stream);
+  if (e != cudaSuccess) { set_last_cuda_error(e); return PSRL_ERR_CUDA; }
+  return PSRL_OK;
+}
+
+// ------------------------------------------------------------------------------------------------ argument checks
+
+bool ok16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+bool in_range(const psrl_kv_extent_t& e, int64_t src_cap, int64_t dst_cap) {
+  return e.n_slots >= 0 && e.src_slot >= 0 && e.dst_slot >= 0 && int64_t(e.src_slot) + e.n_slots <= src_cap &&
+         int64_t(e.dst_slot) + e.n_slots <= dst_cap;
+}
+
+bool row_ok(int32_t row_bytes) { return row_bytes == 128 || row_bytes == 256 || row_bytes == 512; }
+
+// bytes of the two tensors overlap
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + uintptr_t(b_bytes) && y < x + uintptr_t(a_bytes);
+}
+
+struct Range {
+  int64_t at, end;
+};
+bool disjoint(std::vector<Range>& r) {
+  std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.at < b.at; });
+  for (size_t i = 1; i < r.size(); ++i)
+    if (r[i].at < r[i - 1].end) return false;
+  return true;
+}
+
+}  // namespace
+}  // namespace psrl
+
+extern "C" {
+
+psrl_status_t psrl_kv_copy(const psrl_kv_extent_t* extents, int32_t n_extents, int32_t n_kv_heads, int32_t row_bytes,
+                           const void* k_src, const void* v_src, int64_t src_capacity, void* k_dst, void* v_dst,
+                           int64_t dst_capacity, void* stream) {
+  using namespace psrl;
+  if (n_extents < 0 || (n_extents && !extents) || (k_src && !k_dst) || (v_src && !v_dst) || !ok16(k_src) ||
+      !ok16(v_src) || !ok16(k_dst) || !ok16(v_dst))
+    return PSRL_ERR_INVALID_ARG;
+  if (n_kv_heads < 1 || n_kv_heads > 65535 || !row_ok(row_bytes) || src_capacity < 0 || dst_capacity < 0 ||
+      src_capacity > INT32_MAX || dst_capacity > INT32_MAX)
+    return PSRL_ERR_SHAPE;
+  const int64_t src_bytes = src_capacity * n_kv_heads * row_bytes, dst_bytes = dst_capacity * n_kv_heads * row_bytes;
+  if (!k_src) k_dst = nullptr;
+  if (!v_src) v_dst = nullptr;
+  // a pool copied onto itself is fine as long as no extent is written that another (or itself) reads
+  const bool same = (k_src && k_src == k_dst) || (v_src && v_src == v_dst);
+  if ((k_src != k_dst && overlap(k_src, src_bytes, k_dst, dst_bytes)) ||
+      (v_src != v_dst && overlap(v_src, src_bytes, v_dst, dst_bytes)) || overlap(k_src, src_bytes, v_dst, dst_bytes) ||
+      overlap(v_src, src_bytes, k_dst, dst_bytes) || overlap(k_dst, dst_bytes, v_dst, dst_bytes) ||
+      (same && src_capacity != dst_capacity))
+    return PSRL_ERR_INVALID_ARG;
+  try {
+    std::vector<psrl_kv_extent_t> list;
+    std::vector<Range> written, all;
+    list.reserve(n_extents);
+    for (int32_t i = 0; i < n_extents; ++i) {
+      const psrl_kv_extent_t& e = extents[i];
+      if (!in_range(e, src_capacity, dst_capacity)) return PSRL_ERR_SHAPE;
+      if (e.n_slots == 0) continue;
+      list.push_back(e);
+      written.push_back({e.dst_slot, int64_t(e.dst_slot) + e.n_slots});
+    }
+    if (!disjoint(written)) return PSRL_ERR_INVALID_ARG;
+    if (same) {
+      for (const psrl_kv_extent_t& e : list) {
+        // written ranges are sorted and disjoint: the first one that ends behind the source's start decides
+        auto it = std::lower_bound(written.begin(), written.end(), int64_t(e.src_slot),
+                                   [](const Range& r, int64_t at) { return r.end <= at; });
+        if (it != written.end() && it->at < int64_t(e.src_slot) + e.n_slots) return PSRL_ERR_INVALID_ARG;
+      }
+    }
+    if (list.empty() || (!k_src && !v_src)) return PSRL_OK;
+    const Pools p{static_cast<const uint4*>(k_src), static_cast<const uint4*>(v_src), static_cast<uint4*>(k_dst),
+                  static_cast<uint4*>(v_dst), src_capacity, dst_capacity, n_kv_heads, row_bytes / 16};
+    return copy_extents(list.data(), static_cast<int32_t>(list.size()), p, static_cast<cudaStream_t>(stream));
+  } catch (const std::bad_alloc&) {
+    return PSRL_ERR_HOST_OOM;
+  }
+}
+
+psrl_status_t psrl_kv_move(const psrl_kv_extent_t* extents, int32_t n_extents, int32_t n_kv_heads, int32_t row_bytes,
+                           void* k_pool, void* v_pool, int64_t pool_capacity, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  using namespace psrl;
+  if (n_extents < 0 || (n_extents && !extents) || !ok16(k_pool) || !ok16(v_pool) || !ptr_aligned(workspace, 256))
+    return PSRL_ERR_INVALID_ARG;
+  if (n_kv_heads < 1 || n_kv_heads > 65535 || !row_ok(row_bytes) || pool_capacity < 0 || pool_capacity > INT32_MAX)
+    return PSRL_ERR_SHAPE;
+  if (workspace_bytes < kWsHeaderBytes) return PSRL_ERR_WORKSPACE;
+  const int64_t bytes = pool_capacity * n_kv_heads * row_bytes;
+  if (overlap(k_pool, bytes, v_pool, bytes)) return PSRL_ERR_INVALID_ARG;
+  try {
+    std::vector<psrl_kv_extent_t> list;
+    int64_t src_end = 0, dst_end = 0;
+    for (int32_t i = 0; i < n_extents; ++i) {
+      const psrl_kv_extent_t& e = extents[i];
+      if (!in_range(e, pool_capacity, pool_capacity)) return PSRL_ERR_SHAPE;
+      if (e.dst_slot > e.src_slot || e.src_slot < src_end || e.dst_slot < dst_end) return PSRL_ERR_INVALID_ARG;
+      if (e.n_slots == 0) continue;
+      src_end = int64_t(e.src_slot) + e.n_slots;
+      dst_end = int64_t(e.dst_slot) + e.n_slots;
+      if (e.dst_slot != e.src_slot) list.push_back(e);
+    }
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (list.empty() || (!k_pool && !v_pool)) {
+      const cudaError_t e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+      if (e == cudaSuccess) return PSRL_OK;
+      set_last_cuda_error(e);
+      return PSRL_ERR_CUDA;
+    }
+    const Pools p{static_cast<const uint4*>(k_pool), static_cast<const uint4*>(v_pool), static_cast<uint4*>(k_pool),
+                  static_cast<uint4*>(v_pool), pool_capacity, pool_capacity, n_kv_heads, row_bytes / 16};
+    for (size_t at = 0; at < list.size(); at += kMoveMax) {
+      const psrl_status_t st = move_extents(list.data() + at, static_cast<int32_t>(std::min(list.size() - at, size_t(kMoveMax))), p,
+                                            static_cast<int*>(workspace), s);
+      if (st != PSRL_OK) return st;
+    }
+  } catch (const std::bad_alloc&) {
+    return PSRL_ERR_HOST_OOM;
+  }
+  return PSRL_OK;
+}
+
+}  // extern "C"

@@ -373,10 +373,16 @@ psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out) {
     }
     // own items
     P.qrow_seg.resize(P.T_q);
+    P.qrow_pos.resize(P.T_q);
+    P.qrow_slot.resize(P.T_q);
     std::vector<int32_t> own_part_base(n, -1);
     for (int32_t c = 0; c < n; ++c) {
       if (P.seg_q_off[c] < 0) continue;
-      for (int32_t i = 0; i < P.seg_len[c]; ++i) P.qrow_seg[P.seg_q_off[c] + i] = c;
+      for (int32_t i = 0; i < P.seg_len[c]; ++i) {
+        P.qrow_seg[P.seg_q_off[c] + i] = c;
+        P.qrow_pos[P.seg_q_off[c] + i] = P.seg_anc_tokens[c] + i;
+        P.qrow_slot[P.seg_q_off[c] + i] = P.tok_slot[P.seg_tok_off[c] + i];
+      }
       if (has_casc_anc[c]) { own_part_base[c] = P.n_part_rows; P.n_part_rows += P.seg_len[c]; }
       const int32_t anc_tiles = (P.path_off[c + 1] - P.path_off[c]) - P.seg_n_kvt[c];
       for (int32_t t = 0; t < P.seg_n_kvt[c]; ++t) {
@@ -528,6 +534,8 @@ psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out) {
     H.off_bt_pages = append_array(B, P.bt_pages);
     H.off_qrow_seg = append_array(B, P.qrow_seg);
     H.off_tok_slot = append_array(B, P.tok_slot);
+    H.off_qrow_pos = append_array(B, P.qrow_pos);
+    H.off_qrow_slot = append_array(B, P.qrow_slot);
     H.off_kvt = append_array(B, P.kv_tiles);
     H.off_qt = append_array(B, P.q_tiles);
     H.off_kvi = append_array(B, P.kv_items);

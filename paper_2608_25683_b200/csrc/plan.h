@@ -99,6 +99,7 @@ struct DeviceHeader {
   // query row merge_row[i]; its parts are merge_parts[merge_off[i] .. merge_off[i+1]) (partial-row ids)
   int32_t n_part_rows, n_merge_rows, off_merge_row, off_merge_off, off_merge_parts;
   int32_t off_tok_slot;     // [T] pool slot of every token
+  int32_t off_qrow_pos, off_qrow_slot;  // [T_q] position in the sequence and pool slot of every query row's token
 };
 
 struct Plan {
@@ -123,7 +124,7 @@ struct Plan {
   int32_t n_part_rows = 0;
   std::vector<int32_t> merge_row, merge_off, merge_parts;
   std::vector<TileLoad> path_loads;
-  std::vector<int32_t> seg_first_kvt, seg_n_kvt, seg_desc_q_begin, seg_desc_q_end, path_off, path_tiles, path_nvalid, qrow_seg;
+  std::vector<int32_t> seg_first_kvt, seg_n_kvt, seg_desc_q_begin, seg_desc_q_end, path_off, path_tiles, path_nvalid, qrow_seg, qrow_pos, qrow_slot;
   // device blob
   std::vector<int32_t> blob;
   DeviceHeader hdr{};

@@ -1,0 +1,332 @@
+// Rotary positions of the tree's query rows, fused with the way of K and V into the paged pools and back.
+//
+// Pair i of a row's head is turned by the angle pos * f_i.  The angle is only needed modulo a full turn, so f_i is
+// kept as a 64-bit fixed-point fraction of a turn: pos * f_i wraps around exactly in integer arithmetic, and an angle
+// at position 10^6 is as good as one at position 1 (a product in fp32 would be off by 0.06 radians there).
+//
+// Memory bound: every element is read once and written once.  A block takes a few rows; its threads first compute the
+// rows' cos / sin (each used by all Hq + Hkv heads of the row) into shared memory, then stream the heads, two 16-byte
+// vectors per thread and step: in the half layout the two vectors that rotate into each other, so each element is
+// loaded and stored once by the same thread and the rotation may run in place.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "../../include/psrl.h"
+#include "kernels.h"
+#include "plan.h"
+
+struct psrl_rope {
+  psrl_rope_desc_t desc;
+  std::vector<double> freq;      // radians per position
+  std::vector<uint64_t> turns;   // the same as a fraction of a turn, in units of 2^-64
+  double scale = 1.0;
+};
+
+namespace psrl {
+namespace {
+
+constexpr int kMaxPairs = 128;
+constexpr int kThreadsMax = 256;
+constexpr int kRowsMax = 8;  // rows per block at most (shared memory: kRowsMax * kMaxPairs * 8 bytes = 8 KB)
+
+struct Frequencies {
+  uint64_t turns[kMaxPairs];
+};
+
+// One operand of the launch: heads [head0, head0 + heads) of the block's work.  Row r of the source is at
+// (by_slot ? slot[r] : r) * src_row, head h at h * src_head, in elements; the destination likewise.
+struct Part {
+  const void* src;
+  void* dst;
+  int64_t src_row, src_head, dst_row, dst_head;
+  int32_t src_by_slot, dst_by_slot, heads, rotate;
+};
+
+struct RopeParams {
+  Part part[3];
+  const int32_t* pos;
+  const int32_t* slot;
+  int64_t rows;
+  int32_t heads;        // sum over the parts
+  int32_t rows_per_block;
+  int32_t pairs;        // rotary_dim / 2
+  int32_t units;        // two-vector units per head: d / (2 * kElems)
+  int32_t interleaved;
+  float scale, sign;
+};
+
+template <class T, int kElems> struct alignas(sizeof(T) * kElems) Vec { T v[kElems]; };
+
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void from_f(float& y, float x) { y = x; }
+__device__ __forceinline__ void from_f(__nv_bfloat16& y, float x) { y = __float2bfloat16_rn(x); }  // the only rounding below fp32
+
+// kElems = elements per vector: 16 bytes' worth, or 1 when rotary_dim does not divide into pairs of vectors.
+template <class T, int kElems>
+__global__ void __launch_bounds__(kThreadsMax) rope_kernel(const __grid_constant__ RopeParams p,
+                                                           const __grid_constant__ Frequencies f) {
+  __shared__ float2 cs[kRowsMax * kMaxPairs];
+  const int64_t row0 = int64_t(blockIdx.x) * p.rows_per_block;
+  const int n_rows = int(min(int64_t(p.rows_per_block), p.rows - row0));
+  for (int i = threadIdx.x; i < n_rows * p.pairs; i += blockDim.x) {
+    const int r = i / p.pairs, x = i - r * p.pairs;
+    const uint64_t turn = uint64_t(int64_t(p.pos[row0 + r])) * f.turns[x];
+    // signed fraction of a turn in [-1/2, 1/2); sincospi takes half turns
+    const float half_turns = float(int32_t(turn >> 32)) * 0x1p-31f;
+    float s, c;
+    sincospif(half_turns, &s, &c);
+    cs[i] = make_float2(c * p.scale, s * p.scale * p.sign);
+  }
+  __syncthreads();
+  using V = Vec<T, kElems>;
+  const int u = threadIdx.x % p.units;
+  const int rot_units = p.pairs / kElems;
+  // element offsets of the unit's two vectors inside a head
+  int a, b;
+  if (p.interleaved || u >= rot_units) { a = 2 * u * kElems; b = a + kElems; }
+  else { a = u * kElems; b = a + p.pairs; }
+  const int step = blockDim.x / p.units;
+  for (int w = threadIdx.x / p.units; w < n_rows * p.heads; w += step) {
+    const int r = w / p.heads;
+    int h = w - r * p.heads, k = 0;
+    while (h >= p.part[k].heads) { h -= p.part[k].heads; ++k; }
+    const Part& q = p.part[k];
+    const int64_t row = row0 + r;
+    const int64_t slot = (q.src_by_slot || q.dst_by_slot) ? int64_t(p.slot[row]) : 0;
+    const T* src = static_cast<const T*>(q.src) + (q.src_by_slot ? slot : row) * q.src_row + h * q.src_head;
+    T* dst = static_cast<T*>(q.dst) + (q.dst_by_slot ? slot : row) * q.dst_row + h * q.dst_head;
+    V x = *reinterpret_cast<const V*>(src + a), y = *reinterpret_cast<const V*>(src + b);
+    if (q.rotate && u < rot_units) {
+      const float2* t = cs + r * p.pairs + u * kElems;
+      if (!p.interleaved) {
+#pragma unroll
+        for (int e = 0; e < kElems; ++e) {
+          const float c = t[e].x, s = t[e].y, x1 = to_f(x.v[e]), x2 = to_f(y.v[e]);
+          from_f(x.v[e], x1 * c - x2 * s);
+          from_f(y.v[e], x2 * c + x1 * s);
+        }
+      } else if constexpr (kElems == 1) {
+        const float c = t[0].x, s = t[0].y, x1 = to_f(x.v[0]), x2 = to_f(y.v[0]);
+        from_f(x.v[0], x1 * c - x2 * s);
+        from_f(y.v[0], x2 * c + x1 * s);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kElems; e += 2) {
+          const float c0 = t[e / 2].x, s0 = t[e / 2].y, c1 = t[(kElems + e) / 2].x, s1 = t[(kElems + e) / 2].y;
+          const float x1 = to_f(x.v[e]), x2 = to_f(x.v[e + 1]), y1 = to_f(y.v[e]), y2 = to_f(y.v[e + 1]);
+          from_f(x.v[e], x1 * c0 - x2 * s0);
+          from_f(x.v[e + 1], x2 * c0 + x1 * s0);
+          from_f(y.v[e], y1 * c1 - y2 * s1);
+          from_f(y.v[e + 1], y2 * c1 + y1 * s1);
+        }
+      }
+    }
+    *reinterpret_cast<V*>(dst + a) = x;
+    *reinterpret_cast<V*>(dst + b) = y;
+  }
+}
+
+psrl_status_t launch(const psrl_rope& rope, RopeParams& p, psrl_dtype_t dtype, bool inverse, cudaStream_t stream) {
+  const int d = rope.desc.head_dim, rot = rope.desc.rotary_dim;
+  const int full = dtype == PSRL_BF16 ? 8 : 4;
+  p.heads = 0;
+  int n_parts = 0;
+  for (const Part& q : p.part)
+    if (q.src && q.heads) p.part[n_parts++] = q;
+  for (int i = 0; i < n_parts; ++i) p.heads += p.part[i].heads;
+  if (p.rows == 0 || p.heads == 0) return PSRL_OK;
+  // Whole vectors need both halves of the rotated part, and the rest of the head, to be pairs of 16-byte vectors.
+  const bool wide = rot % (2 * full) == 0 && d % (2 * full) == 0;
+  const int elems = wide ? full : 1;
+  p.pairs = rot / 2;
+  p.units = d / (2 * elems);
+  p.interleaved = rope.desc.layout == PSRL_ROPE_INTERLEAVED;
+  p.scale = float(rope.scale);
+  p.sign = inverse ? -1.f : 1.f;
+  const int threads = kThreadsMax / p.units * p.units;
+  // Rows per block: the cos / sin of a row are shared by its heads, so few rows already amortise them.
+  p.rows_per_block = 4;
+  const int64_t grid = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
+  if (grid > INT32_MAX) return PSRL_ERR_SHAPE;
+  Frequencies f{};
+  for (size_t i = 0; i < rope.turns.size(); ++i) f.turns[i] = rope.turns[i];
+  if (dtype == PSRL_BF16) {
+    if (wide) rope_kernel<__nv_bfloat16, 8><<<unsigned(grid), threads, 0, stream>>>(p, f);
+    else rope_kernel<__nv_bfloat16, 1><<<unsigned(grid), threads, 0, stream>>>(p, f);
+  } else {
+    if (wide) rope_kernel<float, 4><<<unsigned(grid), threads, 0, stream>>>(p, f);
+    else rope_kernel<float, 1><<<unsigned(grid), threads, 0, stream>>>(p, f);
+  }
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) { set_last_cuda_error(e); return PSRL_ERR_CUDA; }
+  return PSRL_OK;
+}
+
+bool finite_pos(double x) { return std::isfinite(x) && x > 0.0; }
+
+// NULL is "skip"; else aligned, and the pitch at least a row and a whole number of 16-byte vectors
+bool ok16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool pitch_ok(int64_t pitch, int64_t heads, int d, psrl_dtype_t t) {
+  const int64_t es = t == PSRL_BF16 ? 2 : 4;
+  return pitch >= heads * d && pitch <= (int64_t(1) << 40) && (pitch * es) % 16 == 0;
+}
+
+// The pairs' frequencies; false if the description's scaling arguments make no sense.
+bool frequencies(const psrl_rope_desc_t& d, std::vector<double>& freq, double& scale) {
+  const double r = d.rotary_dim, two_pi = 6.283185307179586476925286766559;
+  const int n = d.rotary_dim / 2;
+  if (!std::isfinite(d.base) || d.base <= 1.0) return false;
+  if (d.scaling != PSRL_ROPE_UNSCALED && !finite_pos(d.factor)) return false;
+  if (!std::isfinite(d.attention_scale) || d.attention_scale < 0.0) return false;
+  double base = d.base;
+  if (d.scaling == PSRL_ROPE_NTK) {
+    if (d.rotary_dim == 2) return false;
+    base *= std::pow(d.factor, r / (r - 2.0));
+    if (!std::isfinite(base) || base <= 0.0) return false;
+  }
+  freq.resize(n);
+  for (int i = 0; i < n; ++i) freq[i] = std::pow(base, -2.0 * i / r);
+  scale = 1.0;
+  if (d.scaling == PSRL_ROPE_LINEAR)
+    for (double& x : freq) x /= d.factor;
+  if (d.scaling == PSRL_ROPE_YARN || d.scaling == PSRL_ROPE_BANDED) {
+    const double low = d.low == 0.0 ? 1.0 : d.low;
+    const double high = d.high == 0.0 ? (d.scaling == PSRL_ROPE_YARN ? 32.0 : 4.0) : d.high;
+    if (d.factor < 1.0 || d.original_positions < 1 || !finite_pos(low) || !finite_pos(high) || low >= high) return false;
+    const double orig = d.original_positions;
+    auto edge = [&](double turns) { return r * std::log(orig / (turns * two_pi)) / (2.0 * std::log(base)); };
+    const double first = std::fmax(std::floor(edge(high)), 0.0), last = std::fmin(std::ceil(edge(low)), r - 1.0);
+    for (int i = 0; i < n; ++i) {
+      double keep;
+      if (d.scaling == PSRL_ROPE_YARN) keep = 1.0 - (i - first) / std::fmax(last - first, 0.001);
+      else keep = (orig * freq[i] / two_pi - low) / (high - low);
+      keep = std::fmin(std::fmax(keep, 0.0), 1.0);
+      freq[i] = freq[i] * keep + freq[i] / d.factor * (1.0 - keep);
+    }
+    if (d.scaling == PSRL_ROPE_YARN) scale = 0.1 * std::log(d.factor) + 1.0;
+  }
+  if (d.attention_scale > 0.0) scale = d.attention_scale;
+  for (double x : freq)
+    if (!std::isfinite(x) || x < 0.0 || x > 1e6) return false;
+  return true;
+}
+
+}  // namespace
+}  // namespace psrl
+
+extern "C" {
+
+psrl_status_t psrl_rope_create(const psrl_rope_desc_t* desc, psrl_rope_t** out) {
+  if (out) *out = nullptr;
+  if (!desc || !out) return PSRL_ERR_INVALID_ARG;
+  if (desc->head_dim < 8 || desc->head_dim > 2 * psrl::kMaxPairs || desc->head_dim % 8 || desc->rotary_dim < 2 ||
+      desc->rotary_dim > desc->head_dim || desc->rotary_dim % 2)
+    return PSRL_ERR_SHAPE;
+  if (desc->layout < PSRL_ROPE_HALF || desc->layout > PSRL_ROPE_INTERLEAVED || desc->scaling < PSRL_ROPE_UNSCALED ||
+      desc->scaling > PSRL_ROPE_BANDED)
+    return PSRL_ERR_INVALID_ARG;
+  psrl_rope* r = new (std::nothrow) psrl_rope;
+  if (!r) return PSRL_ERR_HOST_OOM;
+  try {
+    r->desc = *desc;
+    if (!psrl::frequencies(*desc, r->freq, r->scale)) {
+      delete r;
+      return PSRL_ERR_INVALID_ARG;
+    }
+    for (double f : r->freq) {
+      const long double turn = static_cast<long double>(f) / 6.283185307179586476925286766559L;
+      const long double frac = turn - std::floor(turn);
+      r->turns.push_back(static_cast<uint64_t>(frac * 18446744073709551616.0L));
+    }
+  } catch (const std::bad_alloc&) {
+    delete r;
+    return PSRL_ERR_HOST_OOM;
+  }
+  *out = r;
+  return PSRL_OK;
+}
+
+psrl_status_t psrl_rope_frequencies(const psrl_rope_t* rope, const double** freq, int32_t* n, double* scale) {
+  if (!rope || !freq || !n || !scale) return PSRL_ERR_INVALID_ARG;
+  *freq = rope->freq.data();
+  *n = static_cast<int32_t>(rope->freq.size());
+  *scale = rope->scale;
+  return PSRL_OK;
+}
+
+void psrl_rope_destroy(psrl_rope_t* rope) { delete rope; }
+
+psrl_status_t psrl_rope_qkv_fwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const void* q, int64_t q_pitch,
+                                const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* q_out,
+                                void* k_pool, void* v_pool, int64_t pool_capacity, void* stream) {
+  using namespace psrl;
+  if (!plan || !plan->p || !rope) return PSRL_ERR_INVALID_ARG;
+  const Plan& P = *plan->p;
+  if ((q && !q_out) || (k && !k_pool) || (v && !v_pool) || !ok16(q) || !ok16(k) || !ok16(v) || !ok16(q_out) ||
+      !ok16(k_pool) || !ok16(v_pool))
+    return PSRL_ERR_INVALID_ARG;
+  if (rope->desc.head_dim != P.d || (q && !pitch_ok(q_pitch, P.Hq, P.d, P.dtype)) ||
+      (k && !pitch_ok(k_pitch, P.Hkv, P.d, P.dtype)) || (v && !pitch_ok(v_pitch, P.Hkv, P.d, P.dtype)) ||
+      ((k || v) && pool_capacity < P.pool_slots))
+    return PSRL_ERR_SHAPE;
+  if (!P.dev) return PSRL_ERR_WORKSPACE;
+  RopeParams p{};
+  const int64_t d = P.d;
+  p.part[0] = {q, q_out, q_pitch, d, P.Hq * d, d, 0, 0, P.Hq, 1};
+  p.part[1] = {k, k_pool, k_pitch, d, d, pool_capacity * d, 0, 1, P.Hkv, 1};
+  p.part[2] = {v, v_pool, v_pitch, d, d, pool_capacity * d, 0, 1, P.Hkv, 0};
+  p.pos = P.dev + P.hdr.off_qrow_pos;
+  p.slot = P.dev + P.hdr.off_qrow_slot;
+  p.rows = P.T_q;
+  return launch(*rope, p, P.dtype, false, static_cast<cudaStream_t>(stream));
+}
+
+psrl_status_t psrl_rope_qkv_bwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const void* d_q, const void* dk_pool,
+                                const void* dv_pool, int64_t pool_capacity, void* dq_out, int64_t dq_pitch,
+                                void* dk_out, int64_t dk_pitch, void* dv_out, int64_t dv_pitch, void* stream) {
+  using namespace psrl;
+  if (!plan || !plan->p || !rope) return PSRL_ERR_INVALID_ARG;
+  const Plan& P = *plan->p;
+  if ((d_q && !dq_out) || (dk_pool && !dk_out) || (dv_pool && !dv_out) || !ok16(d_q) || !ok16(dk_pool) ||
+      !ok16(dv_pool) || !ok16(dq_out) || !ok16(dk_out) || !ok16(dv_out))
+    return PSRL_ERR_INVALID_ARG;
+  if (rope->desc.head_dim != P.d || (d_q && !pitch_ok(dq_pitch, P.Hq, P.d, P.dtype)) ||
+      (dk_pool && !pitch_ok(dk_pitch, P.Hkv, P.d, P.dtype)) || (dv_pool && !pitch_ok(dv_pitch, P.Hkv, P.d, P.dtype)) ||
+      ((dk_pool || dv_pool) && pool_capacity < P.pool_slots))
+    return PSRL_ERR_SHAPE;
+  if (!P.dev) return PSRL_ERR_WORKSPACE;
+  RopeParams p{};
+  const int64_t d = P.d;
+  p.part[0] = {d_q, dq_out, P.Hq * d, d, dq_pitch, d, 0, 0, P.Hq, 1};
+  p.part[1] = {dk_pool, dk_out, d, pool_capacity * d, dk_pitch, d, 1, 0, P.Hkv, 1};
+  p.part[2] = {dv_pool, dv_out, d, pool_capacity * d, dv_pitch, d, 1, 0, P.Hkv, 0};
+  p.pos = P.dev + P.hdr.off_qrow_pos;
+  p.slot = P.dev + P.hdr.off_qrow_slot;
+  p.rows = P.T_q;
+  return launch(*rope, p, P.dtype, true, static_cast<cudaStream_t>(stream));
+}
+
+psrl_status_t psrl_rope_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const void* x, int64_t x_pitch,
+                             const int32_t* positions, int64_t n_rows, int32_t n_heads, void* y, int64_t y_pitch,
+                             int inverse, void* stream) {
+  using namespace psrl;
+  if (!rope || n_rows < 0 || n_heads < 1) return PSRL_ERR_INVALID_ARG;
+  if (dtype != PSRL_F32 && dtype != PSRL_BF16) return PSRL_ERR_UNSUPPORTED;
+  const int64_t d = rope->desc.head_dim;
+  if (!pitch_ok(x_pitch, n_heads, int(d), dtype) || !pitch_ok(y_pitch, n_heads, int(d), dtype)) return PSRL_ERR_SHAPE;
+  if (n_rows == 0) return PSRL_OK;
+  if (!ptr_aligned(x, 16) || !ptr_aligned(y, 16) || !ptr_aligned(positions, 4) || (x == y && x_pitch != y_pitch))
+    return PSRL_ERR_INVALID_ARG;
+  RopeParams p{};
+  p.part[0] = {x, y, x_pitch, d, y_pitch, d, 0, 0, n_heads, 1};
+  p.pos = positions;
+  p.rows = n_rows;
+  return launch(*rope, p, dtype, inverse != 0, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
