@@ -354,6 +354,53 @@ psrl_status_t psrl_rope_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const 
                              int inverse, void* stream);
 
 /*
+ * psrl_plan_next_tokens - the targets of the tree's language-model loss.  A query row predicts the next token of its own
+ * segment; the last row of a segment predicts the first token of every child (none at the end of a sample).  Row r's
+ * targets are tokens next[off[r] .. off[r + 1]) - indices into the tree's tokens in canonical order (look their ids up to
+ * get psrl_token_logprob_fwd's targets).  Only tokens of this plan are listed: where a later micro-batch continues a
+ * segment, its first token is that plan's affair, and the caller's to add.
+ *   off [T_q + 1], next [off[T_q]]  HOST, borrowed until psrl_plan_destroy
+ */
+psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off, const int32_t** next);
+
+/*
+ * psrl_token_logprob_fwd / _bwd - the last step of the policy's forward pass and the first of its backward, over the
+ * shared rows of the tree (each row once, however many samples run through it; paper Sec. 2.5, advantage masking: what
+ * the samples' losses want of a shared token arrives as d_logprob of its targets).
+ *   z = scale * hidden[r] . weight[v],   lse[r] = ln sum_v exp(z[r, v]),   logprob[t] = z[r, targets[t]] - lse[r]
+ * for the targets t of row r: target_off[r] <= t < target_off[r + 1], or t = r when target_off is NULL (n_targets ==
+ * n_rows).  Targets outside [0, vocab) are ignored: logprob 0, no gradient.  The logits are never stored.
+ * Backward: G_r = the sum of d_logprob over row r's targets,
+ *   dz[r, v] = scale * (sum of d_logprob over r's targets equal to v  -  G_r exp(z[r, v] - lse[r]))
+ *   d_hidden = dz weight,  d_weight = dz^T hidden
+ * sums in fp32, dz rounded to bf16 as the tensor cores' operand, results rounded once.  Bitwise reproducible.  A row
+ * without a target, or whose d_logprob are all zero, contributes nothing (d_hidden row zero), whatever it holds, and costs
+ * nothing but its place in the workspace.
+ *   hidden   [n_rows, hidden_dim] DEVICE bf16, row pitch in elements;  weight [vocab, hidden_dim] DEVICE bf16
+ *   targets  [n_targets] DEVICE int32;  target_off [n_rows + 1] DEVICE int32, not descending from 0 to n_targets, or NULL
+ *   scale    finite, not 0 (1 / temperature)
+ *   logprob, d_logprob [n_targets], lse [n_rows] DEVICE fp32 (backward: as produced by the forward)
+ *   d_hidden, d_weight  DEVICE bf16 as their tensors, fully overwritten; NULL: not wanted
+ *   workspace  DEVICE, >= psrl_token_logprob_workspace_bytes, 256-byte aligned; holds the device status word.  Forward:
+ *              a few floats per row; backward: about the size of six times `hidden`, whatever the vocabulary.
+ * hidden_dim and the pitches are multiples of 8, tensors 16-byte aligned, tensors must not overlap outputs.
+ * n_rows = 0 does nothing (backward: zeroes d_weight).
+ * Errors: INVALID_ARG, SHAPE, WORKSPACE, CUDA.  Asynchronous; calls that may overlap on the GPU need distinct workspaces.
+ */
+size_t psrl_token_logprob_workspace_bytes(int64_t n_rows, int32_t hidden_dim, int32_t vocab, int64_t n_targets,
+                                          int backward);
+psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
+                                     int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
+                                     const int32_t* targets, int64_t n_targets, const int32_t* target_off, float scale,
+                                     float* logprob, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
+                                     int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
+                                     const int32_t* targets, int64_t n_targets, const int32_t* target_off, float scale,
+                                     const float* logprob, const float* lse, const float* d_logprob, void* d_hidden,
+                                     int64_t d_hidden_pitch, void* d_weight, int64_t d_weight_pitch, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/*
  * Benchmark aid (no counterpart in the paper): psrl_tree_attn_bwd with a mask
  * of the backward kernels to launch, so that each can be timed on its own
  * with CUDA events.  Bit 0: D = rowsum(dO o O) pre-pass, bit 1: dQ kernel

@@ -34,6 +34,7 @@ EXPORTS = [
     "psrl_kv_scatter", "psrl_kv_gather",
     "psrl_rope_create", "psrl_rope_frequencies", "psrl_rope_destroy", "psrl_rope_qkv_fwd", "psrl_rope_qkv_bwd",
     "psrl_rope_rows",
+    "psrl_plan_next_tokens", "psrl_token_logprob_workspace_bytes", "psrl_token_logprob_fwd", "psrl_token_logprob_bwd",
     "psrl_cache_compact", "psrl_kv_copy", "psrl_kv_move",
     "psrl_cost_sequence", "psrl_group_workloads", "psrl_place_groups", "psrl_microbatch_tokens",
 ]
@@ -199,6 +200,15 @@ def lib() -> C.CDLL:
     L.psrl_rope_qkv_bwd.restype = C.c_int
     L.psrl_rope_rows.argtypes = [_VP, C.c_int, _VP, _I64, _VP, _I64, C.c_int32, _VP, _I64, C.c_int, _VP]
     L.psrl_rope_rows.restype = C.c_int
+    L.psrl_plan_next_tokens.argtypes = [_VP, C.POINTER(_I32P), C.POINTER(_I32P)]
+    L.psrl_plan_next_tokens.restype = C.c_int
+    L.psrl_token_logprob_workspace_bytes.argtypes = [_I64, C.c_int32, C.c_int32, _I64, C.c_int]
+    L.psrl_token_logprob_workspace_bytes.restype = C.c_size_t
+    lp = [_I64, C.c_int32, C.c_int32, _VP, _I64, _VP, _I64, _VP, _I64, _VP, C.c_float, _VP, _VP]
+    L.psrl_token_logprob_fwd.argtypes = lp + [_VP, C.c_size_t, _VP]
+    L.psrl_token_logprob_fwd.restype = C.c_int
+    L.psrl_token_logprob_bwd.argtypes = lp + [_VP, _VP, _I64, _VP, _I64, _VP, C.c_size_t, _VP]
+    L.psrl_token_logprob_bwd.restype = C.c_int
     L.psrl_launch_count.argtypes = [C.c_void_p, C.c_int]
     L.psrl_launch_count.restype = C.c_int
     L.psrl_last_cuda_error.restype = C.c_char_p
@@ -286,6 +296,13 @@ class Plan:
         words, n = _I32P(), C.c_size_t()
         _check(lib().psrl_plan_schedule(self._h, C.byref(words), C.byref(n)), "psrl_plan_schedule")
         return np.ctypeslib.as_array(words, shape=(n.value,)).copy()
+
+    def next_tokens(self):
+        """What every query row predicts: (off [T_q + 1], tokens), indices into the tree's tokens in canonical order."""
+        off, nxt = _I32P(), _I32P()
+        _check(lib().psrl_plan_next_tokens(self._h, C.byref(off), C.byref(nxt)), "psrl_plan_next_tokens")
+        o = np.ctypeslib.as_array(off, shape=(self.view["T_q"] + 1,)).copy()
+        return o, np.ctypeslib.as_array(nxt, shape=(int(o[-1]),)).copy() if o[-1] else np.zeros(0, dtype=np.int32)
 
     def device_bytes(self) -> int:
         return int(lib().psrl_plan_device_bytes(self._h))
@@ -660,6 +677,98 @@ def psrl_kv_move(moves, k_pool, v_pool, stream=None, workspace=None):
             workspace = ((buf.data_ptr() + 255) // 256 * 256, 256)
         _check(lib().psrl_kv_move(at, n, heads, row, k_pool.data_ptr(), v_pool.data_ptr(), cap, workspace[0], workspace[1],
                                   on.ptr), "psrl_kv_move")
+
+
+def psrl_token_logprob_workspace_bytes(n_rows: int, hidden_dim: int, vocab: int, n_targets: int, backward: bool) -> int:
+    return int(lib().psrl_token_logprob_workspace_bytes(int(n_rows), int(hidden_dim), int(vocab), int(n_targets),
+                                                        int(bool(backward))))
+
+
+def _logprob_args(hidden, weight, targets, target_off, floats):
+    """Checks shared by the two directions; the shape arguments of the C call."""
+    import torch
+
+    if hidden.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
+        raise TypeError("hidden and weight must be bfloat16")
+    if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
+        raise ValueError("hidden must be [rows, hidden_dim], weight [vocab, hidden_dim]")
+    n, h = hidden.shape
+    for name, t, count in [("targets", targets, None), ("target_off", target_off, n + 1)]:
+        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (count and t.shape[0] != count)):
+            raise ValueError(f"{name} must be a contiguous int32 vector" + (f" of {count}" if count else ""))
+    for name, t, count in floats:
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (count,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 vector of {count}")
+    return n, h, weight.shape[0], targets.shape[0]
+
+
+def _matrix_pitch(t, name: str) -> int:
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
+
+
+def _logprob_workspace(workspace, on, n, h, v, m, backward, device):
+    import torch
+
+    if workspace is not None:
+        return workspace
+    need = psrl_token_logprob_workspace_bytes(n, h, v, m, backward)
+    buf = on.keep(torch.empty(need + 256, dtype=torch.uint8, device=device))
+    return (buf.data_ptr() + 255) // 256 * 256, need
+
+
+def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: float = 1.0, logprob=None, lse=None, stream=None,
+                           workspace=None):
+    """Log-probabilities of `targets` (int32) under softmax(scale * hidden weight^T), without storing the logits.  hidden
+    [rows, H], weight [vocab, H] bf16; row r's targets are targets[target_off[r] : target_off[r + 1]], or targets[r] without
+    target_off.  Returns (logprob [targets], lse [rows]), fp32."""
+    import torch
+
+    n, h, v, m = _logprob_args(hidden, weight, targets, target_off, [])
+    _logprob_args(hidden, weight, targets, target_off, [("logprob", logprob, m), ("lse", lse, n)])
+    given = [t for t in (target_off, logprob, lse) if t is not None]
+    with _on_device_of(stream, hidden, weight, targets, *given) as on:
+        if logprob is None:
+            logprob = on.keep(torch.empty(m, dtype=torch.float32, device=hidden.device))
+        if lse is None:
+            lse = on.keep(torch.empty(n, dtype=torch.float32, device=hidden.device))
+        ws, wsb = _logprob_workspace(workspace, on, n, h, v, m, False, hidden.device)
+        _check(lib().psrl_token_logprob_fwd(n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
+                                            _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
+                                            None if target_off is None else target_off.data_ptr(), scale, logprob.data_ptr(),
+                                            lse.data_ptr(), ws, wsb, on.ptr), "psrl_token_logprob_fwd")
+    return logprob, lse
+
+
+def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, target_off=None, scale: float = 1.0, d_hidden=None,
+                           d_weight=None, want_hidden: bool = True, want_weight: bool = True, stream=None, workspace=None):
+    """Gradients of the above: (d_hidden, d_weight), bf16, given d_logprob [targets] and the forward's logprob and lse.
+    want_hidden / want_weight False: that one is None and not computed."""
+    import torch
+
+    m = targets.shape[0]
+    n, h, v, m = _logprob_args(hidden, weight, targets, target_off,
+                               [("logprob", logprob, m), ("lse", lse, hidden.shape[0]), ("d_logprob", d_logprob, m)])
+    for name, t, like in (("d_hidden", d_hidden, hidden), ("d_weight", d_weight, weight)):
+        if t is not None and (t.dtype != torch.bfloat16 or t.shape != like.shape):
+            raise ValueError(f"{name} must be bfloat16 {tuple(like.shape)}")
+    given = [t for t in (target_off, d_hidden, d_weight) if t is not None]
+    with _on_device_of(stream, hidden, weight, targets, logprob, lse, d_logprob, *given) as on:
+        if d_hidden is None and want_hidden:
+            d_hidden = on.keep(torch.empty((n, h), dtype=torch.bfloat16, device=hidden.device))
+        if d_weight is None and want_weight:
+            d_weight = on.keep(torch.empty((v, h), dtype=torch.bfloat16, device=hidden.device))
+        out = [t if w else None for t, w in ((d_hidden, want_hidden), (d_weight, want_weight))]
+        ws, wsb = _logprob_workspace(workspace, on, n, h, v, m, True, hidden.device)
+        args = [x for t, name in zip(out, ("d_hidden", "d_weight"))
+                for x in ((None, 0) if t is None else (t.data_ptr(), _matrix_pitch(t, name)))]
+        _check(lib().psrl_token_logprob_bwd(n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
+                                            _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
+                                            None if target_off is None else target_off.data_ptr(), scale, logprob.data_ptr(),
+                                            lse.data_ptr(), d_logprob.data_ptr(), *args, ws, wsb, on.ptr),
+               "psrl_token_logprob_bwd")
+    return tuple(out)
 
 
 def _flags_ptr(seg_flags):

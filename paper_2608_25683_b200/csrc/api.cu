@@ -87,6 +87,13 @@ psrl_status_t psrl_plan_schedule(const psrl_plan_t* plan, const int32_t** words,
   return PSRL_OK;
 }
 
+psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off, const int32_t** next) {
+  if (!plan || !plan->p || !off || !next) return PSRL_ERR_INVALID_ARG;
+  *off = plan->p->next_off.data();
+  *next = plan->p->next_tok.data();
+  return PSRL_OK;
+}
+
 size_t psrl_plan_device_bytes(const psrl_plan_t* plan) {
   if (!plan || !plan->p) return 0;
   return plan->p->blob.size() * sizeof(int32_t);

@@ -1,0 +1,781 @@
+// Log-probabilities of target tokens under softmax(scale * hidden * weight^T) over a large vocabulary, and their
+// gradients, without ever holding the logits: the last step of a policy's forward pass and the first of its backward.
+//
+// All four contractions (logits, logits again in the backward, d_hidden, d_weight) run on one matrix kernel:
+//   tile 256 x 256 of a CTA pair (cta_group::2: each CTA holds 128 rows of A and 128 of the 256 columns of B, so a
+//   64-deep step brings 32 KB into each SM for 512 tensor cycles; a lone CTA with a 128 x 256 tile would need 48 KB),
+//   six 32 KB stages filled by TMA, two 256-column accumulators in tensor memory so that the epilogue of one tile
+//   runs under the products of the next, persistent CTAs.
+// What differs is how the operands lie (K-major or MN-major in shared memory) and the epilogue:
+//   kLse   running maximum and sum of exponentials of a row over a run of vocabulary tiles   -> partial (max, sum)
+//   kDz    dz = -scale G softmax, with the entries of the row's targets put in afterwards    -> bf16, one piece of the
+//          vocabulary at a time in the workspace (the softmax part is rounded to bf16 as the tensor cores need it)
+//   kDh    d_hidden += dz W over the pieces, summed in fp32, rounded once at the end
+//   kDw    d_weight = dz^T hidden, the whole sum in tensor memory, rounded once
+// The pieces make dz as large as the caller's hidden states, not as the logits.
+//
+// The backward works on the rows that matter alone: a row without a target, or whose d_logprob are all zero (prompts,
+// padding, samples without advantage), has dz = 0 whatever its hidden state holds.  The other rows are gathered first -
+// one copy of their hidden states, against three products of the vocabulary's depth saved for every row left out - and
+// their number stays on the device, where the products read it.
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include <algorithm>
+
+#include "../../include/psrl.h"
+#include "attn_bf16_common.cuh"
+#include "kernels.h"
+#include "tma.h"
+
+namespace psrl {
+namespace {
+using namespace sm100;
+
+constexpr int kBK = 64;                      // K per stage
+constexpr int kStages = 6;
+constexpr int kOperandBytes = 128 * kBK * 2; // one CTA's share of A or B in a stage
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kGemmThreads = 6 * 32;         // warps 0-3 epilogue, 4 TMA, 5 MMA
+constexpr size_t kGemmSmem = size_t(kStages) * kStageBytes + 1024;
+constexpr int kMaxRun = 8;                   // vocabulary tiles whose maximum and sum stay in registers
+
+enum Kind { kLse, kDz, kDh, kDw };
+
+struct GemmMaps {
+  CUtensorMap a, b;
+};
+
+struct GemmParams {
+  int32_t M, N;                 // valid rows and columns of the product
+  int32_t n_tiles, k_blocks;
+  const int32_t* count;         // rows that matter, on the device: M of kDz and kDh, K of kDw; NULL: as M and k_blocks say
+  const int32_t* row_of;        // kDz, kDh: the caller's row of a gathered row
+  int32_t run;                  // kLse: consecutive column tiles of one work unit
+  float scale_log2;             // logits in powers of two: scale * log2(e)
+  float2* part;                 // kLse: [unit column][M] (max, sum), powers of two
+  const float2* row_info;       // kDz: per row (lse * log2(e), -scale * G)
+  const int32_t* targets;       // kDz
+  const int32_t* target_off;    // kDz: may be NULL (one target per row)
+  const float* entry;           // kDz: value of dz at every target
+  int32_t n_targets, col0;      // kDz: col0 = first vocabulary entry of the piece
+  __nv_bfloat16* out;           // kDz, kDh (last piece), kDw
+  int64_t out_pitch;
+  float* acc;                   // kDh: fp32 sums over the pieces, [M][acc_pitch]
+  int64_t acc_pitch;
+  int32_t first, last;          // kDh: first / last piece
+  int* status;
+};
+
+// ------------------------------------------------------------------------------------------- pair-of-CTAs wrappers
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// shared::cluster address of the first CTA's copy of a shared-memory variable
+__device__ __forceinline__ uint32_t in_leader(const void* p) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
+  return a;
+}
+__device__ __forceinline__ void arrive_leader(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void tma_load_pair(void* dst, const CUtensorMap* m, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], "
+      "[%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(kDescHi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// arrives on the barrier of both CTAs when the products issued so far are done
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+      "h"(uint16_t(3))
+      : "memory");
+}
+__device__ __forceinline__ void st_global_32B(void* p, const uint32_t (&r)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void ld_global_32B(const void* p, float (&r)[8]) {
+  asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
+               : "l"(p)
+               : "memory");
+}
+
+// Work unit -> row tile and first column tile: groups of kGroupM row tiles, inside a group the row tile moves fastest, so
+// that the CTAs at work share column tiles and a group's rows stay in the L2.
+constexpr int kGroupM = 32;
+__device__ __forceinline__ void unit_tile(int m_tiles, int unit, int n_units, int& mt, int& nu) {
+  const int per = kGroupM * n_units;
+  const int g = unit / per, r = unit - g * per;
+  const int gm = min(kGroupM, m_tiles - g * kGroupM);
+  nu = r / gm;
+  mt = g * kGroupM + r - nu * gm;
+}
+
+// The targets of a row, kept inside the array whatever the offsets say.
+__device__ __forceinline__ void target_range(const int32_t* off, int64_t row, int n_targets, int& b, int& e) {
+  b = off ? min(max(off[row], 0), n_targets) : int(row);
+  e = off ? min(max(off[row + 1], b), n_targets) : int(row) + 1;
+}
+
+struct __align__(8) PairBarriers {
+  uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
+};
+
+// Sixteen fp32 results to bf16, 32 bytes.
+__device__ __forceinline__ void store_bf16x16(__nv_bfloat16* dst, const float* v) {
+  uint32_t o[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+  st_global_32B(dst, o);
+}
+
+template <Kind kKind>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
+gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
+  // which operand lies with its M or N side contiguous: W in dz W; both in dz^T hidden
+  constexpr bool kAmn = kKind == kDw, kBmn = kKind == kDh || kKind == kDw;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  __shared__ PairBarriers bar;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_rank();
+  const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+  const int n_units = (p.n_tiles + p.run - 1) / p.run;
+  const int count = p.count ? *p.count : 0;
+  const int M = p.count && kKind != kDw ? count : p.M;
+  const int k_blocks = p.count && kKind == kDw ? (count + kBK - 1) / kBK : p.k_blocks;
+  const int m_tiles = (M + 255) / 256, units = m_tiles * n_units;
+
+  if (tid == 0) {
+    s_abort = 0;
+    for (int i = 0; i < kStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar.acc_full[i], 1); mbar_init(&bar.acc_empty[i], 8); }
+    fence_mbar_init();
+  }
+  if (warp == 5) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();   // the peer's barriers exist before anything arrives on them
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  volatile int* abortp = &s_abort;
+
+  if (warp == 4) {
+    // ======================= TMA producer (both CTAs) =======================
+    if (lane == 0) {
+      tma_prefetch_desc(&maps.a);
+      tma_prefetch_desc(&maps.b);
+      uint32_t it = 0;
+      bool ok = true;
+      for (int unit = cluster; unit < units && ok; unit += n_clusters) {
+        int mt, nu;
+        unit_tile(m_tiles, unit, n_units, mt, nu);
+        const int nt_end = min((nu + 1) * p.run, p.n_tiles);
+        for (int nt = nu * p.run; nt < nt_end && ok; ++nt) {
+          const int m0 = mt * 256 + int(rank) * 128, n0 = nt * 256 + int(rank) * 128;
+          for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+            const uint32_t s = it % kStages, round = it / kStages;
+            if (round > 0 && !mbar_wait(&bar.empty[s], (round + 1) & 1, abortp, p.status)) { ok = false; break; }
+            // the second CTA's copies count on the first one's barrier as well
+            if (rank == 0) mbar_expect_tx(&bar.full[s], 2 * kStageBytes);
+            const uint32_t full = in_leader(&bar.full[s]);
+            uint8_t* sa = smem + s * kStageBytes;
+            uint8_t* sb = sa + kOperandBytes;
+            if (kAmn) {
+              tma_load_pair(sa, &maps.a, full, m0, kb * kBK);
+              tma_load_pair(sa + kOperandBytes / 2, &maps.a, full, m0 + 64, kb * kBK);
+            } else {
+              tma_load_pair(sa, &maps.a, full, kb * kBK, m0);
+            }
+            if (kBmn) {
+              tma_load_pair(sb, &maps.b, full, n0, kb * kBK);
+              tma_load_pair(sb + kOperandBytes / 2, &maps.b, full, n0 + 64, kb * kBK);
+            } else {
+              tma_load_pair(sb, &maps.b, full, kb * kBK, n0);
+            }
+          }
+        }
+      }
+      // the last arrivals on the stages' barriers come from the pair's products: this CTA stays until they are here
+      for (uint32_t i = 0; i < kStages && ok; ++i) {
+        const uint32_t uses = it / kStages + (i < it % kStages ? 1 : 0);
+        if (uses > 0) ok = mbar_wait(&bar.empty[i], (uses + 1) & 1, abortp, p.status);
+      }
+    }
+  } else if (warp == 5) {
+    // ======================= MMA issuer (first CTA of the pair) =======================
+    if (rank == 0) {
+      constexpr uint32_t idesc = make_idesc(256, 256, kAmn ? 1 : 0, kBmn ? 1 : 0);
+      // bytes from one 64-wide block of an MN-major operand to the next; per 16-deep step: 32 bytes, or 16 rows
+      constexpr uint32_t kLbo = kOperandBytes / 2;
+      constexpr uint32_t kStepA = kAmn ? 2048 >> 4 : 32 >> 4, kStepB = kBmn ? 2048 >> 4 : 32 >> 4;
+      const bool elected = elect_one();
+      uint32_t it = 0, tile = 0;
+      bool ok = true;
+      for (int unit = cluster; unit < units && ok; unit += n_clusters) {
+        int mt, nu;
+        unit_tile(m_tiles, unit, n_units, mt, nu);
+        const int nt_end = min((nu + 1) * p.run, p.n_tiles);
+        for (int nt = nu * p.run; nt < nt_end && ok; ++nt, ++tile) {
+          const uint32_t a = tile & 1, use = tile >> 1;
+          if (use > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bar.acc_empty[a], (use + 1) & 1, abortp, p.status));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t d = tmem + a * 256;
+          for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+            const uint32_t s = it % kStages;
+            if (!mbar_wait_all1(&bar.full[s], (it / kStages) & 1, abortp, p.status)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sa = smem_u32(smem) + s * kStageBytes, sb = sa + kOperandBytes;
+            const uint32_t da = desc_lo(sa, kAmn ? kLbo : 0), db = desc_lo(sb, kBmn ? kLbo : 0);
+            if (elected) {
+#pragma unroll
+              for (uint32_t k = 0; k < kBK / 16; ++k)
+                mma_pair(d, da + k * kStepA, db + k * kStepB, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+              commit_pair(&bar.empty[s]);
+            }
+            __syncwarp();
+          }
+          if (ok && elected) commit_pair(&bar.acc_full[a]);
+          __syncwarp();
+        }
+      }
+    }
+  } else {
+    // ======================= epilogue: one thread per row =======================
+    const uint32_t lane_addr = tmem + (uint32_t(warp) << 21);   // lane 32 * warp
+    const uint32_t empty0 = in_leader(&bar.acc_empty[0]), empty1 = in_leader(&bar.acc_empty[1]);
+    uint32_t tile = 0;
+    bool ok = true;
+    for (int unit = cluster; unit < units && ok; unit += n_clusters) {
+      int mt, nu;
+      unit_tile(m_tiles, unit, n_units, mt, nu);
+      const int row = mt * 256 + int(rank) * 128 + warp * 32 + lane;
+      const bool live = row < M;
+      float best = -CUDART_INF_F, sum = 0.f;                       // kLse
+      float lse2 = 0.f, coef = 0.f;                                // kDz
+      int t_begin = 0, t_end = 0;
+      // dz is read in steps of kBK rows by the product for d_weight: the rows behind the last one of a step are zero
+      const bool pad = kKind == kDz && !live && row < (M + kBK - 1) / kBK * kBK;
+      const int64_t user_row = (kKind == kDz || kKind == kDh) && live ? p.row_of[row] : row;
+      if (kKind == kDz && live) {
+        const float2 ri = p.row_info[user_row];
+        lse2 = ri.x; coef = ri.y;
+        target_range(p.target_off, user_row, p.n_targets, t_begin, t_end);
+      }
+      const int nt_end = min((nu + 1) * p.run, p.n_tiles);
+      for (int nt = nu * p.run; nt < nt_end; ++nt, ++tile) {
+        const uint32_t a = tile & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(&bar.acc_full[a], (tile >> 1) & 1, abortp, p.status));
+        if (!ok) break;
+        tc_fence_after();
+        const int n0 = nt * 256;
+#pragma unroll 1
+        for (int c = 0; c < 8; ++c) {
+          const int col = n0 + c * 32;
+          if (col >= p.N) break;   // warp-uniform
+          uint32_t r[32];
+          tmem_ld32(lane_addr + a * 256 + c * 32, r);
+          tmem_wait_ld();
+          if constexpr (kKind == kLse) {
+            float top = -CUDART_INF_F;
+            if (col + 32 > p.N) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (col + i >= p.N) r[i] = __float_as_uint(p.scale_log2 > 0.f ? -CUDART_INF_F : CUDART_INF_F);
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float z = __uint_as_float(r[i]) * p.scale_log2;
+              r[i] = __float_as_uint(z);
+              top = fmaxf(top, z);
+            }
+            if (top > best) { sum *= ex2(best - top); best = top; }
+            const float ref = best == -CUDART_INF_F ? 0.f : best;   // nothing finite yet: every term is zero
+            float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              s0 += ex2(__uint_as_float(r[i]) - ref);
+              s1 += ex2(__uint_as_float(r[i + 1]) - ref);
+            }
+            sum += s0 + s1;
+          } else if constexpr (kKind == kDz) {
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = coef * ex2(fmaf(__uint_as_float(r[i]), p.scale_log2, -lse2));
+            if (col + 32 > p.N) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (col + i >= p.N) v[i] = 0.f;
+            }
+            if (pad) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = 0.f;
+            }
+            if (live || pad) {
+              __nv_bfloat16* o = p.out + int64_t(row) * p.out_pitch + col;
+              store_bf16x16(o, v);
+              store_bf16x16(o + 16, v + 16);
+            }
+          } else {
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = k_blocks ? __uint_as_float(r[i]) : 0.f;   // an empty sum writes no accumulator
+            if (live) {
+              if (kKind == kDh && !p.first) {
+                const float* q = p.acc + int64_t(row) * p.acc_pitch + col;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  float old[8];
+                  ld_global_32B(q + 8 * j, old);
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) v[8 * j + i] += old[i];
+                }
+              }
+              if (kKind == kDh && !p.last) {
+                float* q = p.acc + int64_t(row) * p.acc_pitch + col;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  uint32_t o[8];
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(v[8 * j + i]);
+                  st_global_32B(q + 8 * j, o);
+                }
+              } else {
+                // rows of the caller's tensor: 16-byte aligned, and the last columns may be fewer than 32
+                __nv_bfloat16* o = p.out + user_row * p.out_pitch + col;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  if (col + 8 * j < p.N) {
+                    uint4 w;
+                    w.x = pack_bf16(v[8 * j], v[8 * j + 1]);
+                    w.y = pack_bf16(v[8 * j + 2], v[8 * j + 3]);
+                    w.z = pack_bf16(v[8 * j + 4], v[8 * j + 5]);
+                    w.w = pack_bf16(v[8 * j + 6], v[8 * j + 7]);
+                    *reinterpret_cast<uint4*>(o + 8 * j) = w;
+                  }
+                }
+              }
+            }
+          }
+        }
+        // the accumulator may be overwritten
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_leader(a ? empty1 : empty0);
+        if (kKind == kDz) {
+          // the row's targets inside this tile, over what this thread has just stored there
+          for (int t = t_begin; t < t_end; ++t) {
+            const int x = p.targets[t] - p.col0;
+            if (x >= n0 && x < min(n0 + 256, p.N)) p.out[int64_t(row) * p.out_pitch + x] = __float2bfloat16_rn(p.entry[t]);
+          }
+        }
+      }
+      if (kKind == kLse && ok && live) p.part[int64_t(nu) * M + row] = make_float2(best, sum);
+    }
+  }
+  // ---- teardown ----
+  __syncthreads();
+  if (s_abort) {
+    // a wait gave up: let copies and products in flight come to rest before the memory they use is given back
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  }
+  tc_fence_before();
+  cluster_sync();
+  if (warp == 5) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------- small kernels
+
+// lse of 32 rows from their partial (max, sum), then the log-probabilities of the rows' targets: the target's logit is a
+// dot product of its own (two rows read per target, against a whole pass over the weights for the lse).
+constexpr int kFinalWarps = 8;
+__global__ void __launch_bounds__(kFinalWarps * 32) final_kernel(const float2* __restrict__ part, int n_parts, int M, int hidden_dim,
+                                                                 int vocab, const __nv_bfloat16* __restrict__ hidden, int64_t h_pitch,
+                                                                 const __nv_bfloat16* __restrict__ weight, int64_t w_pitch,
+                                                                 const int32_t* __restrict__ targets, const int32_t* __restrict__ off,
+                                                                 int n_targets, float scale, float* __restrict__ logprob,
+                                                                 float* __restrict__ lse) {
+  __shared__ float2 s_part[kFinalWarps][32];
+  __shared__ float s_lse[32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row0 = blockIdx.x * 32, row = row0 + lane;
+  float m = -CUDART_INF_F, s = 0.f;
+  if (row < M) {
+    for (int i = warp; i < n_parts; i += kFinalWarps) {
+      const float2 x = part[int64_t(i) * M + row];
+      const float top = fmaxf(m, x.x);
+      const float ref = top == -CUDART_INF_F ? 0.f : top;
+      s = s * exp2f(m - ref) + x.y * exp2f(x.x - ref);
+      m = top;
+    }
+  }
+  s_part[warp][lane] = make_float2(m, s);
+  __syncthreads();
+  if (warp == 0) {
+    float top = -CUDART_INF_F, sum = 0.f;
+    for (int w = 0; w < kFinalWarps; ++w) top = fmaxf(top, s_part[w][lane].x);
+    const float ref = top == -CUDART_INF_F ? 0.f : top;
+    for (int w = 0; w < kFinalWarps; ++w) sum += s_part[w][lane].y * exp2f(s_part[w][lane].x - ref);
+    const float l = (ref + log2f(sum)) * kLn2;
+    s_lse[lane] = l;
+    if (row < M) lse[row] = l;
+  }
+  __syncthreads();
+  const int vecs = hidden_dim / 8;
+  int at = 0;   // targets of the rows before, for the distribution over the warps
+  for (int r = 0; r < 32 && row0 + r < M; ++r) {
+    int b, e;
+    target_range(off, row0 + r, n_targets, b, e);
+    for (int t = b; t < e; ++t, ++at) {
+      if (at % kFinalWarps != warp) continue;
+      const int y = targets[t];
+      if (y < 0 || y >= vocab) {
+        if (lane == 0) logprob[t] = 0.f;
+        continue;
+      }
+      const uint4* hv = reinterpret_cast<const uint4*>(hidden + int64_t(row0 + r) * h_pitch);
+      const uint4* wv = reinterpret_cast<const uint4*>(weight + int64_t(y) * w_pitch);
+      float acc = 0.f;
+#pragma unroll 4
+      for (int i = lane; i < vecs; i += 32) {
+        const uint4 x = hv[i], w = wv[i];
+        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          acc = fmaf(__uint_as_float(xs[j] << 16), __uint_as_float(ws[j] << 16), acc);
+          acc = fmaf(__uint_as_float(xs[j] & 0xffff0000u), __uint_as_float(ws[j] & 0xffff0000u), acc);
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+      // a log-probability is not positive; the two sums are rounded apart
+      if (lane == 0) logprob[t] = fminf(scale * acc - s_lse[r], 0.f);
+    }
+  }
+}
+
+// Per row the sum G of its targets' gradients, and dz at every target: scale (g_t - G p_t), g_t = the sum over the row's
+// targets with the same token.  Written as (g_t - G) - G (e^lp - 1): for a row with one token the first difference is
+// zero and nothing cancels as its probability nears one.  A warp per row; one bit per row says whether any gradient is not
+// zero.
+constexpr int kRowsPerByte = 8;
+__global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int vocab, const int32_t* __restrict__ targets,
+                                                                 const int32_t* __restrict__ off, int n_targets,
+                                                                 const float* __restrict__ logprob, const float* __restrict__ lse,
+                                                                 const float* __restrict__ d_logprob, float scale,
+                                                                 float2* __restrict__ row_info, float* __restrict__ entry,
+                                                                 uint8_t* __restrict__ matters) {
+  __shared__ uint32_t s_bits;
+  if (threadIdx.x == 0) s_bits = 0;
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * kRowsPerByte + warp;
+  if (row < M) {
+    int b, e;
+    target_range(off, row, n_targets, b, e);
+    float total = 0.f;
+    bool any = false;
+    for (int t = b + lane; t < e; t += 32) {
+      const int y = targets[t];
+      if (y < 0 || y >= vocab) continue;
+      const float g = d_logprob[t];
+      total += g;
+      any |= g != 0.f;   // NaN counts
+    }
+    any = __any_sync(0xffffffffu, any);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    if (any) {
+      for (int t = b + lane; t < e; t += 32) {
+        const int y = targets[t];
+        if (y < 0 || y >= vocab) continue;   // no entry of dz belongs to it
+        float same = 0.f;
+        for (int u = b; u < e; ++u)
+          if (targets[u] == y) same += d_logprob[u];
+        entry[t] = scale * ((same - total) - total * expm1f(logprob[t]));
+      }
+    }
+    if (lane == 0) {
+      row_info[row] = make_float2(lse[row] * kLog2e, -scale * total);
+      if (any) atomicOr(&s_bits, 1u << warp);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) matters[blockIdx.x] = uint8_t(s_bits);
+}
+
+// Gathers the hidden states of the rows that matter, in order, and zeroes the others' d_hidden.  A block takes 32 rows and
+// counts the rows before them itself: one bit per row is little to read.
+constexpr int kGatherRows = 32;
+__global__ void __launch_bounds__(256) gather_kernel(int M, const uint8_t* __restrict__ matters, const uint4* __restrict__ hidden,
+                                                     int64_t h_pitch_vecs, int vecs, uint4* __restrict__ gathered,
+                                                     int32_t* __restrict__ row_of, int32_t* __restrict__ count,
+                                                     uint4* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
+  __shared__ int s_before;
+  if (threadIdx.x == 0) s_before = 0;
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int byte0 = blockIdx.x * (kGatherRows / 8), n_bytes = (M + 7) / 8;
+  int before = 0;
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(matters);
+  for (int i = threadIdx.x; i < byte0 / 4; i += 256) before += __popc(words[i]);
+  before = __reduce_add_sync(0xffffffffu, before);
+  if (lane == 0 && before) atomicAdd(&s_before, before);
+  __syncthreads();
+  uint32_t bits = 0;
+  for (int i = 0; i < kGatherRows / 8; ++i)
+    if (byte0 + i < n_bytes) bits |= uint32_t(matters[byte0 + i]) << (8 * i);
+  const int at0 = s_before;
+  for (int r = warp; r < kGatherRows; r += 8) {
+    const int row = blockIdx.x * kGatherRows + r;
+    if (row >= M) break;
+    if (bits >> r & 1) {
+      const int at = at0 + __popc(bits & ((1u << r) - 1));
+      if (lane == 0) row_of[at] = row;
+      for (int i = lane; i < vecs; i += 32) gathered[int64_t(at) * vecs + i] = hidden[row * h_pitch_vecs + i];
+    } else if (d_hidden) {
+      for (int i = lane; i < vecs; i += 32) d_hidden[row * dh_pitch_vecs + i] = make_uint4(0, 0, 0, 0);
+    }
+  }
+  if (blockIdx.x == gridDim.x - 1) {
+    const int n = at0 + __popc(bits);
+    if (threadIdx.x == 0) *count = n;
+    // the rows behind the last one, up to a whole step of the product that sums over rows
+    const int64_t end = int64_t((n + kBK - 1) / kBK * kBK) * vecs;
+    for (int64_t i = int64_t(n) * vecs + threadIdx.x; i < end; i += 256) gathered[i] = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------- host side
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+struct Layout {
+  int32_t n_tiles, run, n_parts, m_tiles;
+  int64_t piece;                 // vocabulary entries of one piece of the backward
+  int64_t rows;                  // rows that the backward's gathered buffers hold
+  size_t part, row_info, entry, matters, row_of, count, gathered, dz, acc, total;
+};
+
+Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward) {
+  Layout L{};
+  L.m_tiles = static_cast<int32_t>((n + 255) / 256);
+  L.n_tiles = static_cast<int32_t>((v + 255) / 256);
+  size_t at = kWsHeaderBytes;
+  auto take = [&](size_t bytes) { const size_t a = at; at += (bytes + 255) / 256 * 256; return a; };
+  if (!backward) {
+    // short runs while there are few tiles (they balance the pairs of CTAs), long ones to keep the partials small
+    const int64_t tiles = int64_t(L.m_tiles) * L.n_tiles;
+    L.run = static_cast<int32_t>(std::min<int64_t>(kMaxRun, std::max<int64_t>(1, tiles / (74 * 16))));
+    L.n_parts = (L.n_tiles + L.run - 1) / L.run;
+    L.part = take(size_t(L.n_parts) * n * sizeof(float2));
+  } else {
+    // a piece of dz is about 128 MB (it then partly stays in the L2 for the two products that read it) but at least
+    // 8192 entries wide: below that the fp32 sums of d_hidden cost more traffic than the products hide
+    L.piece = std::min(round_up(v, 256), std::max<int64_t>(8192, (int64_t(64) << 20) / n / 256 * 256));
+    L.row_info = take(size_t(n) * sizeof(float2));
+    L.entry = take(size_t(n_targets) * sizeof(float));
+    L.rows = round_up(n, kBK);
+    L.matters = take(size_t(n + 7) / 8);
+    L.row_of = take(size_t(n) * sizeof(int32_t));
+    L.count = take(sizeof(int32_t));
+    L.gathered = take(size_t(L.rows) * h * 2);
+    L.dz = take(size_t(L.rows) * L.piece * 2);
+    L.acc = take(L.piece < v ? size_t(n) * round_up(h, 32) * sizeof(float) : 0);
+  }
+  L.total = at;
+  return L;
+}
+
+template <Kind kKind>
+cudaError_t launch_gemm(const GemmMaps& maps, GemmParams& p, cudaStream_t stream) {
+  static bool done[64] = {};
+  cudaError_t e = ensure_dynamic_smem(gemm_kernel<kKind>, kGemmSmem, done);
+  if (e != cudaSuccess) return e;
+  p.n_tiles = (p.N + 255) / 256;
+  if (p.run < 1) p.run = 1;
+  const int64_t units = (int64_t(p.M) + 255) / 256 * ((p.n_tiles + p.run - 1) / p.run);
+  if (units > INT32_MAX / 2) return cudaErrorInvalidValue;
+  const int clusters = static_cast<int>(std::min<int64_t>(units, resident_ctas() / 2));
+  gemm_kernel<kKind><<<2 * clusters, kGemmThreads, kGemmSmem, stream>>>(maps, p);
+  return cudaGetLastError();
+}
+
+psrl_status_t cuda_failed(cudaError_t e) {
+  set_last_cuda_error(e);
+  return PSRL_ERR_CUDA;
+}
+
+bool al16(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool al4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+bool pitch16(int64_t pitch, int64_t cols) { return pitch >= cols && pitch % 8 == 0 && pitch <= (int64_t(1) << 36); }
+
+// Shared checks of both directions; PSRL_OK with n_rows == 0 means there is nothing to do.
+psrl_status_t check(int64_t n, int32_t h, int32_t v, const void* hidden, int64_t hp, const void* weight, int64_t wp,
+                    const int32_t* targets, int64_t n_targets, const int32_t* off, float scale) {
+  if (n < 0 || n_targets < 0 || n > INT32_MAX - 512 || n_targets > INT32_MAX - 512) return PSRL_ERR_INVALID_ARG;
+  if (h < 8 || h % 8 || v < 1 || v > INT32_MAX - 512 || !pitch16(hp, h) || !pitch16(wp, h)) return PSRL_ERR_SHAPE;
+  if (!off && n_targets != n) return PSRL_ERR_SHAPE;
+  if (!(scale == scale) || scale == 0.f || scale > 1e30f || scale < -1e30f) return PSRL_ERR_INVALID_ARG;
+  if (n == 0) return PSRL_OK;
+  if (!al16(hidden) || !al16(weight) || (n_targets && !al4(targets)) || (off && !al4(off))) return PSRL_ERR_INVALID_ARG;
+  return PSRL_OK;
+}
+
+}  // namespace
+}  // namespace psrl
+
+extern "C" {
+
+size_t psrl_token_logprob_workspace_bytes(int64_t n_rows, int32_t hidden_dim, int32_t vocab, int64_t n_targets, int backward) {
+  if (n_rows < 0 || hidden_dim < 1 || vocab < 1 || n_targets < 0) return 0;
+  if (n_rows == 0) return psrl::kWsHeaderBytes;
+  return psrl::layout(n_rows, hidden_dim, vocab, n_targets, backward != 0).total;
+}
+
+psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
+                                     int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
+                                     const int32_t* targets, int64_t n_targets, const int32_t* target_off, float scale,
+                                     float* logprob, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace psrl;
+  psrl_status_t st = check(n_rows, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, targets, n_targets, target_off, scale);
+  if (st != PSRL_OK) return st;
+  if (!ptr_aligned(workspace, 256)) return PSRL_ERR_INVALID_ARG;
+  if (workspace_bytes < psrl_token_logprob_workspace_bytes(n_rows, hidden_dim, vocab, n_targets, 0)) return PSRL_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+  if (e != cudaSuccess) return cuda_failed(e);
+  if (n_rows == 0) return PSRL_OK;
+  if (!al4(lse) || (n_targets && !al4(logprob))) return PSRL_ERR_INVALID_ARG;
+  const Layout L = layout(n_rows, hidden_dim, vocab, n_targets, false);
+  char* ws = static_cast<char*>(workspace);
+  GemmMaps maps;
+  if (!make_map_bf16_2d(&maps.a, hidden, hidden_dim, n_rows, hidden_pitch * 2, 128) ||
+      !make_map_bf16_2d(&maps.b, weight, hidden_dim, vocab, weight_pitch * 2, 128))
+    return PSRL_ERR_CUDA;
+  GemmParams p{};
+  p.M = static_cast<int32_t>(n_rows);
+  p.N = vocab;
+  p.k_blocks = (hidden_dim + kBK - 1) / kBK;
+  p.run = L.run;
+  p.scale_log2 = scale * kLog2e;
+  p.part = reinterpret_cast<float2*>(ws + L.part);
+  p.status = reinterpret_cast<int*>(ws);
+  e = launch_gemm<kLse>(maps, p, s);
+  if (e != cudaSuccess) return cuda_failed(e);
+  final_kernel<<<unsigned((n_rows + 31) / 32), kFinalWarps * 32, 0, s>>>(
+      p.part, L.n_parts, p.M, hidden_dim, vocab, static_cast<const __nv_bfloat16*>(hidden), hidden_pitch,
+      static_cast<const __nv_bfloat16*>(weight), weight_pitch, targets, target_off, static_cast<int>(n_targets), scale, logprob, lse);
+  e = cudaGetLastError();
+  return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+}
+
+psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
+                                     int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
+                                     const int32_t* targets, int64_t n_targets, const int32_t* target_off, float scale,
+                                     const float* logprob, const float* lse, const float* d_logprob, void* d_hidden,
+                                     int64_t d_hidden_pitch, void* d_weight, int64_t d_weight_pitch, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  using namespace psrl;
+  psrl_status_t st = check(n_rows, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, targets, n_targets, target_off, scale);
+  if (st != PSRL_OK) return st;
+  if (!ptr_aligned(workspace, 256) || (d_hidden && !al16(d_hidden)) || (d_weight && !al16(d_weight))) return PSRL_ERR_INVALID_ARG;
+  if ((d_hidden && !pitch16(d_hidden_pitch, hidden_dim)) || (d_weight && !pitch16(d_weight_pitch, hidden_dim))) return PSRL_ERR_SHAPE;
+  if (workspace_bytes < psrl_token_logprob_workspace_bytes(n_rows, hidden_dim, vocab, n_targets, 1)) return PSRL_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+  if (e != cudaSuccess) return cuda_failed(e);
+  if (n_rows == 0) {
+    if (d_weight) e = cudaMemset2DAsync(d_weight, size_t(d_weight_pitch) * 2, 0, size_t(hidden_dim) * 2, vocab, s);
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
+  if (!al4(lse) || (n_targets && (!al4(logprob) || !al4(d_logprob)))) return PSRL_ERR_INVALID_ARG;
+  if (!d_hidden && !d_weight) return PSRL_OK;
+  const Layout L = layout(n_rows, hidden_dim, vocab, n_targets, true);
+  char* ws = static_cast<char*>(workspace);
+  GemmParams base{};
+  base.status = reinterpret_cast<int*>(ws);
+  base.scale_log2 = scale * kLog2e;
+  float2* row_info = reinterpret_cast<float2*>(ws + L.row_info);
+  float* entry = reinterpret_cast<float*>(ws + L.entry);
+  __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + L.dz);
+  const int32_t M = static_cast<int32_t>(n_rows);
+  rows_kernel<<<unsigned((n_rows + 7) / 8), 256, 0, s>>>(M, vocab, targets, target_off, static_cast<int>(n_targets), logprob, lse,
+                                                         d_logprob, scale, row_info, entry, reinterpret_cast<uint8_t*>(ws + L.matters));
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return cuda_failed(e);
+  __nv_bfloat16* gathered = reinterpret_cast<__nv_bfloat16*>(ws + L.gathered);
+  base.count = reinterpret_cast<int32_t*>(ws + L.count);
+  base.row_of = reinterpret_cast<int32_t*>(ws + L.row_of);
+  gather_kernel<<<unsigned((n_rows + kGatherRows - 1) / kGatherRows), 256, 0, s>>>(
+      M, reinterpret_cast<uint8_t*>(ws + L.matters), static_cast<const uint4*>(hidden), hidden_pitch / 8, hidden_dim / 8,
+      reinterpret_cast<uint4*>(gathered), reinterpret_cast<int32_t*>(ws + L.row_of), reinterpret_cast<int32_t*>(ws + L.count),
+      static_cast<uint4*>(d_hidden), d_hidden_pitch / 8);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return cuda_failed(e);
+  const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(weight);
+  for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
+    const int64_t nv = std::min<int64_t>(L.piece, vocab - v0);
+    const __nv_bfloat16* wv = w + v0 * weight_pitch;
+    GemmMaps mz, mh, mw;
+    if (!make_map_bf16_2d(&mz.a, gathered, hidden_dim, L.rows, int64_t(hidden_dim) * 2, 128) ||
+        !make_map_bf16_2d(&mz.b, wv, hidden_dim, nv, weight_pitch * 2, 128) ||
+        !make_map_bf16_2d(&mh.a, dz, nv, L.rows, L.piece * 2, 128) ||
+        !make_map_bf16_2d(&mh.b, wv, hidden_dim, nv, weight_pitch * 2, 64) ||
+        !make_map_bf16_2d(&mw.a, dz, nv, L.rows, L.piece * 2, 64) ||
+        !make_map_bf16_2d(&mw.b, gathered, hidden_dim, L.rows, int64_t(hidden_dim) * 2, 64))
+      return PSRL_ERR_CUDA;
+    GemmParams z = base;
+    z.M = M; z.N = static_cast<int32_t>(nv); z.k_blocks = (hidden_dim + kBK - 1) / kBK;
+    z.row_info = row_info; z.targets = targets; z.target_off = target_off; z.entry = entry;
+    z.n_targets = static_cast<int32_t>(n_targets); z.col0 = static_cast<int32_t>(v0);
+    z.out = dz; z.out_pitch = L.piece;
+    e = launch_gemm<kDz>(mz, z, s);
+    if (e == cudaSuccess && d_hidden) {
+      GemmParams g = base;
+      g.M = M; g.N = hidden_dim; g.k_blocks = static_cast<int32_t>((nv + kBK - 1) / kBK);
+      g.out = static_cast<__nv_bfloat16*>(d_hidden); g.out_pitch = d_hidden_pitch;
+      g.acc = reinterpret_cast<float*>(ws + L.acc); g.acc_pitch = round_up(hidden_dim, 32);
+      g.first = v0 == 0; g.last = v0 + nv >= vocab;
+      e = launch_gemm<kDh>(mh, g, s);
+    }
+    if (e == cudaSuccess && d_weight) {
+      GemmParams g = base;
+      g.M = static_cast<int32_t>(nv); g.N = hidden_dim; g.k_blocks = static_cast<int32_t>((n_rows + kBK - 1) / kBK);
+      g.out = static_cast<__nv_bfloat16*>(d_weight) + v0 * d_weight_pitch; g.out_pitch = d_weight_pitch;
+      e = launch_gemm<kDw>(mw, g, s);
+    }
+    if (e != cudaSuccess) return cuda_failed(e);
+  }
+  return PSRL_OK;
+}
+
+}  // extern "C"

@@ -350,6 +350,20 @@ psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out) {
         P.seg_cascaded[c] = (fewer || starved) ? 1 : 0;
       }
     }
+    // what every query row predicts: the next token of its segment, or the first token of every child
+    P.next_off.assign(1, 0);
+    std::vector<std::vector<int32_t>> children(n);
+    for (int32_t c = 0; c < n; ++c)
+      if (P.seg_parent[c] >= 0) children[P.seg_parent[c]].push_back(c);
+    for (int32_t c = 0; c < n; ++c) {
+      if (P.seg_q_off[c] < 0) continue;
+      for (int32_t i = 0; i + 1 < P.seg_len[c]; ++i) {
+        P.next_tok.push_back(P.seg_tok_off[c] + i + 1);
+        P.next_off.push_back(static_cast<int32_t>(P.next_tok.size()));
+      }
+      for (int32_t x : children[c]) P.next_tok.push_back(P.seg_tok_off[x]);
+      P.next_off.push_back(static_cast<int32_t>(P.next_tok.size()));
+    }
     // per-segment list of KV tiles for the own items: non-cascaded ancestors root->parent, then own
     P.path_off.assign(n + 1, 0);
     std::vector<uint8_t> has_casc_anc(n, 0);

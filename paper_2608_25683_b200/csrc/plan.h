@@ -125,6 +125,7 @@ struct Plan {
   std::vector<int32_t> merge_row, merge_off, merge_parts;
   std::vector<TileLoad> path_loads;
   std::vector<int32_t> seg_first_kvt, seg_n_kvt, seg_desc_q_begin, seg_desc_q_end, path_off, path_tiles, path_nvalid, qrow_seg, qrow_pos, qrow_slot;
+  std::vector<int32_t> next_off, next_tok;  // [T_q + 1], the tokens that every query row predicts
   // device blob
   std::vector<int32_t> blob;
   DeviceHeader hdr{};
