@@ -97,12 +97,14 @@ psrl_status_t copy_extents(const psrl_kv_extent_t* ext, int32_t n, const Pools& 
 // destination of the chunks before it, so
 //   - a chunk may be loaded while earlier chunks are still being stored, and
 //   - a chunk may be stored once it and the chunks before it have been loaded by EVERY block,
-// which is the only synchronisation: one counter per chunk parity.  The next chunk's loads are in flight while a block
-// waits.  All blocks are resident (cooperative launch), and the wait is bounded.
+// which is the only synchronisation.  The next chunk's loads are in flight while a block waits.
+//   large moves   one block per SM (cooperative launch, all resident), one counter per chunk parity, a bounded wait
+//   small moves   one cluster of up to eight blocks and its hardware barrier: an ordinary launch, nothing to zero first
 
 constexpr int kMoveThreads = 512, kMoveRegs = 8;           // 64 KB per block and chunk
 constexpr int kWarpVecs = 32 * kMoveRegs;                  // a warp's part of a chunk: 4 KB of consecutive vectors
 constexpr int kMoveMax = 1000;
+constexpr int kClusterMax = 8;
 
 struct MoveList {
   int32_t n;
@@ -111,24 +113,26 @@ struct MoveList {
   int32_t first[kMoveMax + 1];  // slots before the extent
 };
 
+// A warp's part of a chunk: its vectors, and in lane i where its row i (slot of one pool and head) goes.
 struct Held {
   uint4 v[kMoveRegs];
-  uint4* to[kMoveRegs];  // nullptr past the end
+  int64_t dst_at;   // in vectors from the pool's start, -1 past the end
+  int32_t pool;
 };
 
 __device__ __forceinline__ void load_part(const MoveList& list, const Pools& p, uint32_t warp_part, uint32_t total_rows, Held& h) {
   const int lane = threadIdx.x & 31;
-  // the rows (slot of one pool and head) of this warp's part; lane i looks up row i
   const uint32_t rows = kWarpVecs / p.vecs;
   const uint64_t row0 = uint64_t(warp_part) * rows;
-  int64_t src_at = -1, dst_at = 0;
-  int pool = 0;
+  int64_t src_at = -1;
+  h.dst_at = -1;
+  h.pool = 0;
   if (lane < int(rows) && row0 + lane < total_rows) {
     const uint32_t row = uint32_t(row0) + lane;
     const uint32_t ph = row / uint32_t(list.slots);
     const int s = int(row - ph * uint32_t(list.slots));
-    pool = ph >= uint32_t(p.heads);
-    const int head = int(ph) - pool * p.heads;
+    h.pool = ph >= uint32_t(p.heads);
+    const int head = int(ph) - h.pool * p.heads;
     int lo = 0, hi = list.n;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -136,68 +140,75 @@ __device__ __forceinline__ void load_part(const MoveList& list, const Pools& p, 
     }
     const int in = s - list.first[lo];
     src_at = (int64_t(head) * p.src_cap + list.src[lo] + in) * p.vecs;
-    dst_at = (int64_t(head) * p.src_cap + list.dst[lo] + in) * p.vecs;
+    h.dst_at = (int64_t(head) * p.src_cap + list.dst[lo] + in) * p.vecs;
   }
+  const int shift = 31 - __clz(p.vecs);
 #pragma unroll
   for (int j = 0; j < kMoveRegs; ++j) {
-    const int vec = j * 32 + lane, r = vec / p.vecs, x = vec % p.vecs;
-    const int64_t s = __shfl_sync(0xffffffffu, src_at, r), d = __shfl_sync(0xffffffffu, dst_at, r);
-    const int z = __shfl_sync(0xffffffffu, pool, r);
-    h.to[j] = nullptr;
-    if (s >= 0) {
-      h.v[j] = __ldcg((z ? p.v_src : p.k_src) + s + x);
-      h.to[j] = (z ? p.v_dst : p.k_dst) + d + x;
-    }
+    const int vec = j * 32 + lane, r = vec >> shift, x = vec & (p.vecs - 1);
+    const int64_t at = __shfl_sync(0xffffffffu, src_at, r);
+    const int z = __shfl_sync(0xffffffffu, h.pool, r);
+    h.v[j] = make_uint4(0, 0, 0, 0);
+    if (at >= 0) h.v[j] = __ldcg((z ? p.v_src : p.k_src) + at + x);
   }
 }
 
-// True once every thread of the block holds its loads: the barrier's predicate depends on their values.
+// True once every thread of the block HOLDS its loads: the barrier's predicate is computed from their values, so no later
+// store, of this or another block, can be seen by them.  (A fence would order them too, but also wait for the stores of
+// the chunk before.)
 __device__ __forceinline__ void settle(const Held& h) {
   uint32_t x = 0;
 #pragma unroll
-  for (int j = 0; j < kMoveRegs; ++j)
-    if (h.to[j]) x |= h.v[j].x ^ h.v[j].y ^ h.v[j].z ^ h.v[j].w;
-  __threadfence();
+  for (int j = 0; j < kMoveRegs; ++j) x |= h.v[j].x ^ h.v[j].y ^ h.v[j].z ^ h.v[j].w;
   __syncthreads_or(x != 0);
 }
 
-__device__ __forceinline__ void store_part(const Held& h) {
+__device__ __forceinline__ void store_part(const Pools& p, const Held& h) {
+  const int lane = threadIdx.x & 31;
+  const int shift = 31 - __clz(p.vecs);
 #pragma unroll
-  for (int j = 0; j < kMoveRegs; ++j)
-    if (h.to[j]) *h.to[j] = h.v[j];
+  for (int j = 0; j < kMoveRegs; ++j) {
+    const int vec = j * 32 + lane, r = vec >> shift, x = vec & (p.vecs - 1);
+    const int64_t at = __shfl_sync(0xffffffffu, h.dst_at, r);
+    const int z = __shfl_sync(0xffffffffu, h.pool, r);
+    if (at >= 0) (z ? p.v_dst : p.k_dst)[at + x] = h.v[j];
+  }
 }
 
 // ws[0] status, ws[16], ws[32] blocks that have loaded their part of the even / odd chunks
+template <bool kCluster>
 __global__ void __launch_bounds__(kMoveThreads, 1) move_kernel(const __grid_constant__ MoveList list, const Pools p,
-                                                               int* ws, uint32_t n_chunks, uint32_t total_rows) {
+                                                               int* ws, uint32_t n_chunks, uint32_t total_rows, bool first) {
   const uint32_t warps = gridDim.x * (kMoveThreads / 32);
   const uint32_t mine = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5);
   __shared__ int s_go;
   Held h[2];
   load_part(list, p, mine, total_rows, h[0]);
+  if (kCluster && first && blockIdx.x == 0 && threadIdx.x == 0) ws[0] = int(PSRL_OK);
   auto step = [&](uint32_t c, Held& now, Held& next) -> bool {
     settle(now);
-    if (threadIdx.x == 0) {
-      __threadfence();
-      atomicAdd(ws + 16 + 16 * (c & 1), 1);
-    }
+    if (kCluster) asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    else if (threadIdx.x == 0) atomicAdd(ws + 16 + 16 * (c & 1), 1);
     if (c + 1 < n_chunks) load_part(list, p, (c + 1) * warps + mine, total_rows, next);
-    if (threadIdx.x == 0) {
-      const int want = int((c / 2 + 1) * gridDim.x);
-      int ok = 0;
-      for (uint32_t it = 0; it < (1u << 22) && !ok; ++it) {
-        int seen;
-        asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(ws + 16 + 16 * (c & 1)) : "memory");
-        ok = seen >= want;
-        if (it > 256) __nanosleep(64);
+    if (kCluster) {
+      asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    } else {
+      if (threadIdx.x == 0) {
+        const int want = int((c / 2 + 1) * gridDim.x);
+        int ok = 0;
+        for (uint32_t it = 0; it < (1u << 22) && !ok; ++it) {
+          int seen;
+          asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(seen) : "l"(ws + 16 + 16 * (c & 1)) : "memory");
+          ok = seen >= want;
+          if (it > 1024) __nanosleep(64);
+        }
+        if (!ok) atomicExch(ws, int(PSRL_ERR_TIMEOUT));
+        s_go = ok;
       }
-      if (!ok) atomicExch(ws, int(PSRL_ERR_TIMEOUT));
-      __threadfence();
-      s_go = ok;
+      __syncthreads();
+      if (!s_go) return false;  // block-uniform: nothing more is written by this block
     }
-    __syncthreads();
-    if (!s_go) return false;  // block-uniform: nothing more is written by this block
-    store_part(now);
+    store_part(p, now);
     return true;
   };
   for (uint32_t c = 0; c < n_chunks; c += 2) {
@@ -207,7 +218,7 @@ __global__ void __launch_bounds__(kMoveThreads, 1) move_kernel(const __grid_cons
   }
 }
 
-psrl_status_t move_extents(const psrl_kv_extent_t* ext, int32_t n, Pools p, int* ws, cudaStream_t stream) {
+psrl_status_t move_extents(const psrl_kv_extent_t* ext, int32_t n, Pools p, int* ws, bool first, cudaStream_t stream) {
   MoveList list;
   list.n = n;
   int64_t slots = 0;
@@ -221,13 +232,36 @@ psrl_status_t move_extents(const psrl_kv_extent_t* ext, int32_t n, Pools p, int*
   const int64_t rows = slots * p.heads * (p.v_src ? 2 : 1);
   if (rows > INT32_MAX) return PSRL_ERR_SHAPE;
   const int64_t block_rows = int64_t(kMoveThreads) * kMoveRegs / p.vecs;
-  const int64_t grid = std::min<int64_t>(resident_ctas(), (rows + block_rows - 1) / block_rows);
+  const int64_t blocks = (rows + block_rows - 1) / block_rows;
+  // A cluster moves 0.5 MB a chunk; past kClusterChunks of them the whole GPU is quicker in spite of its dearer launch.
+  constexpr int64_t kClusterChunks = 4;
+  const bool small = blocks <= kClusterMax * kClusterChunks;
+  int64_t grid = std::min<int64_t>(resident_ctas(), blocks);
+  if (small)
+    for (grid = 1; grid < std::min<int64_t>(blocks, kClusterMax);) grid *= 2;
   uint32_t n_chunks = static_cast<uint32_t>((rows + grid * block_rows - 1) / (grid * block_rows));
   uint32_t total = static_cast<uint32_t>(rows);
-  void* args[] = {&list, &p, &ws, &n_chunks, &total};
-  cudaError_t e = cudaMemsetAsync(ws, 0, kWsHeaderBytes, stream);
-  if (e == cudaSuccess)
-    e = cudaLaunchCooperativeKernel(reinterpret_cast<void*>(move_kernel), dim3(unsigned(grid)), dim3(kMoveThreads), args, 0, stream);
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(grid));
+  cfg.blockDim = dim3(kMoveThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cudaError_t e = cudaSuccess;
+  if (small) {
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(grid);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    e = cudaLaunchKernelEx(&cfg, move_kernel<true>, list, p, ws, n_chunks, total, first);
+  } else {
+    attr.id = cudaLaunchAttributeCooperative;
+    attr.val.cooperative = 1;
+    // a later part of a long list keeps the status of the parts before
+    const size_t keep = first ? 0 : 16 * sizeof(int);
+    e = cudaMemsetAsync(reinterpret_cast<char*>(ws) + keep, 0, kWsHeaderBytes - keep, stream);
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, move_kernel<false>, list, p, ws, n_chunks, total, first);
+  }
   if (e != cudaSuccess) { set_last_cuda_error(e); return PSRL_ERR_CUDA; }
   return PSRL_OK;
 }
@@ -347,7 +381,7 @@ psrl_status_t psrl_kv_move(const psrl_kv_extent_t* extents, int32_t n_extents, i
                   static_cast<uint4*>(v_pool), pool_capacity, pool_capacity, n_kv_heads, row_bytes / 16};
     for (size_t at = 0; at < list.size(); at += kMoveMax) {
       const psrl_status_t st = move_extents(list.data() + at, static_cast<int32_t>(std::min(list.size() - at, size_t(kMoveMax))), p,
-                                            static_cast<int*>(workspace), s);
+                                            static_cast<int*>(workspace), at == 0, s);
       if (st != PSRL_OK) return st;
     }
   } catch (const std::bad_alloc&) {
