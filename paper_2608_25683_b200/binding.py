@@ -472,43 +472,50 @@ def psrl_kv_gather(plan: Plan, k_pool, v_pool, k_tok=None, v_tok=None, stream=No
     return k_tok, v_tok
 
 
-class _on_device_of:
-    """The tensors' device as the current one (the library launches there) and the stream of the call on it: the
-    caller's, or torch's current stream of that device."""
+def _device_of(*tensors) -> int:
+    """The CUDA device that all the tensors of a call live on."""
+    dev = tensors[0].get_device()
+    if dev < 0:
+        raise RuntimeError("tensors must live on a CUDA device: this library has no CPU path")
+    for t in tensors:
+        if t.get_device() != dev:
+            raise ValueError(f"tensors on {t.device} and {tensors[0].device}: one call works on one device")
+    return dev
 
-    def __init__(self, stream, *tensors):
-        import torch
 
-        dev = tensors[0].device
-        for t in tensors:
-            if t.device != dev:
-                raise ValueError(f"tensors on {t.device} and {dev}: one call works on one device")
-        if dev.type != "cuda":
-            raise RuntimeError("tensors must live on a CUDA device: this library has no CPU path")
-        if getattr(stream, "device", dev) != dev:
-            raise ValueError(f"stream of {stream.device} for tensors on {dev}")
-        self.other = dev.index != torch.cuda.current_device()
-        self.guard = torch.cuda.device(dev) if self.other else None
-        if stream is None:
-            self.given, self.ptr = None, torch.cuda.current_stream(dev).cuda_stream
-        else:
-            self.given = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=dev)
-            self.ptr = self.given.cuda_stream
+def _stream_on(stream, dev: int):
+    """(raw stream handle of a call on device `dev`, torch stream to keep temporaries for or None).  Without a stream it is
+    torch's current one of that device; the raw handle skips a Stream object, a third of a small call's host time."""
+    import torch
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev), None
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=dev)
+    elif stream.device.index != dev:
+        raise ValueError(f"stream of {stream.device} for tensors on cuda:{dev}")
+    return stream.cuda_stream, stream
 
-    def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
 
-    def keep(self, t):
-        """A tensor made for this call: not to be reused before the call's stream has passed it."""
-        if self.given is not None:
-            t.record_stream(self.given)
-        return t
+def _kept(t, stream):
+    """A tensor made for this call: not to be reused before the call's stream has passed it."""
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _launch(name: str, dev: int, *args):
+    """One C call with the tensors' device as the current one: the library launches there."""
+    import torch
+
+    fn = getattr(lib(), name)
+    if dev == torch._C._cuda_getDevice():
+        st = fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args)
+    if st != PSRL_OK:
+        _check(st, name)
 
 
 _ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
@@ -549,6 +556,11 @@ def _rows_pitch(t, rows: int, heads: int, d: int, name: str) -> int:
     return s[0] if rows > 1 else heads * d
 
 
+def _plan_device(plan, dev: int):
+    if plan._dev is not None and plan._dev.get_device() != dev:
+        raise ValueError(f"the plan was uploaded to {plan._dev.device}, the tensors live on cuda:{dev}")
+
+
 def _rope_pools(plan, *pools):
     for p in pools:
         if p.dim() != 3 or p.shape != pools[0].shape or p.shape[0] != plan.n_kv_heads or p.shape[2] != plan.head_dim or not p.is_contiguous():
@@ -566,16 +578,17 @@ def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=Non
     pq = _rows_pitch(q, V["T_q"], plan.n_q_heads, d, "q")
     pk, pv = (_rows_pitch(t, V["T_q"], plan.n_kv_heads, d, n) for t, n in ((k, "k"), (v, "v")))
     cap = _rope_pools(plan, k_pool, v_pool)
-    with _on_device_of(stream, q, k, v, k_pool, v_pool) as on:
-        if q_out is None:
-            q_out = on.keep(torch.empty((V["T_q"], plan.n_q_heads, d), dtype=q.dtype, device=q.device))
-        else:
-            _check_dtype(plan, q_out)
-            if q_out.shape != q.shape or not q_out.is_contiguous() or q_out.device != q.device:
-                raise ValueError("q_out must be contiguous [T_q, Hq, d] on the same device")
-        _check(lib().psrl_rope_qkv_fwd(plan._h, rope._h, q.data_ptr(), pq, k.data_ptr(), pk, v.data_ptr(), pv,
-                                       q_out.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), cap, on.ptr),
-               "psrl_rope_qkv_fwd")
+    dev = _device_of(q, k, v, k_pool, v_pool)
+    _plan_device(plan, dev)
+    raw, keep = _stream_on(stream, dev)
+    if q_out is None:
+        q_out = _kept(torch.empty((V["T_q"], plan.n_q_heads, d), dtype=q.dtype, device=q.device), keep)
+    else:
+        _check_dtype(plan, q_out)
+        if q_out.shape != q.shape or not q_out.is_contiguous() or q_out.device != q.device:
+            raise ValueError("q_out must be contiguous [T_q, Hq, d] on the same device")
+    _launch("psrl_rope_qkv_fwd", dev, plan._h, rope._h, q.data_ptr(), pq, k.data_ptr(), pk, v.data_ptr(), pv,
+            q_out.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), cap, raw)
     return q_out
 
 
@@ -589,20 +602,22 @@ def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None
     if d_q.shape != (V["T_q"], plan.n_q_heads, d) or not d_q.is_contiguous():
         raise ValueError("d_q must be contiguous [T_q, Hq, d]")
     cap = _rope_pools(plan, dk_pool, dv_pool)
-    with _on_device_of(stream, d_q, dk_pool, dv_pool) as on:
-        outs, pitch = [], []
-        for t, heads, name in ((dq_out, plan.n_q_heads, "dq_out"), (dk_out, plan.n_kv_heads, "dk_out"), (dv_out, plan.n_kv_heads, "dv_out")):
-            if t is None:
-                t = on.keep(torch.empty((V["T_q"], heads, d), dtype=d_q.dtype, device=d_q.device))
-            else:
-                _check_dtype(plan, t)
-                if t.device != d_q.device:
-                    raise ValueError(f"{name} lives on another device")
-            outs.append(t)
-            pitch.append(_rows_pitch(t, V["T_q"], heads, d, name))
-        _check(lib().psrl_rope_qkv_bwd(plan._h, rope._h, d_q.data_ptr(), dk_pool.data_ptr(), dv_pool.data_ptr(), cap,
-                                       outs[0].data_ptr(), pitch[0], outs[1].data_ptr(), pitch[1], outs[2].data_ptr(),
-                                       pitch[2], on.ptr), "psrl_rope_qkv_bwd")
+    dev = _device_of(d_q, dk_pool, dv_pool)
+    _plan_device(plan, dev)
+    raw, keep = _stream_on(stream, dev)
+    outs, pitch = [], []
+    for t, heads, name in ((dq_out, plan.n_q_heads, "dq_out"), (dk_out, plan.n_kv_heads, "dk_out"), (dv_out, plan.n_kv_heads, "dv_out")):
+        if t is None:
+            t = _kept(torch.empty((V["T_q"], heads, d), dtype=d_q.dtype, device=d_q.device), keep)
+        else:
+            _check_dtype(plan, t)
+            if t.device != d_q.device:
+                raise ValueError(f"{name} lives on another device")
+        outs.append(t)
+        pitch.append(_rows_pitch(t, V["T_q"], heads, d, name))
+    _launch("psrl_rope_qkv_bwd", dev, plan._h, rope._h, d_q.data_ptr(), dk_pool.data_ptr(), dv_pool.data_ptr(), cap,
+            outs[0].data_ptr(), pitch[0], outs[1].data_ptr(), pitch[1], outs[2].data_ptr(),
+            pitch[2], raw)
     return tuple(outs)
 
 
@@ -619,25 +634,30 @@ def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stre
         raise ValueError("positions must be contiguous int32 [rows]")
     rows, heads = x.shape[0], x.shape[1]
     px = _rows_pitch(x, rows, heads, rope.head_dim, "x")
-    with _on_device_of(stream, x, positions) as on:
-        if y is None:
-            y = on.keep(torch.empty(x.shape, dtype=x.dtype, device=x.device))
-        elif y.dtype != x.dtype or y.device != x.device:
-            raise ValueError("y must have x's type and device")
-        _check(lib().psrl_rope_rows(rope._h, dt, x.data_ptr(), px, positions.data_ptr(), rows, heads, y.data_ptr(),
-                                    _rows_pitch(y, rows, heads, rope.head_dim, "y"), int(bool(inverse)), on.ptr),
-               "psrl_rope_rows")
+    dev = _device_of(x, positions)
+    raw, keep = _stream_on(stream, dev)
+    if y is None:
+        y = _kept(torch.empty(x.shape, dtype=x.dtype, device=x.device), keep)
+    elif y.dtype != x.dtype or y.device != x.device:
+        raise ValueError("y must have x's type and device")
+    _launch("psrl_rope_rows", dev, rope._h, dt, x.data_ptr(), px, positions.data_ptr(), rows, heads, y.data_ptr(),
+            _rows_pitch(y, rows, heads, rope.head_dim, "y"), int(bool(inverse)), raw)
     return y
 
 
 def _extents(extents):
     """[n, 3] int32 (source slot, destination slot, slots), kept alive by the caller, and its address."""
-    e = np.ascontiguousarray(extents, dtype=np.int32)
+    e = np.asarray(extents)
+    if e.dtype != np.int32:
+        if e.size and (e.dtype.kind not in "iu" or int(e.min()) < -2 ** 31 or int(e.max()) >= 2 ** 31):
+            raise ValueError("extents must be 32-bit integers")
+        e = e.astype(np.int32)
+    e = np.ascontiguousarray(e)
     if e.size == 0:
         return e, 0, None
     if e.ndim != 2 or e.shape[1] != 3:
         raise ValueError("extents must be [n, 3]: source slot, destination slot, slots")
-    return e, len(e), e.ctypes.data
+    return e, len(e), e.__array_interface__["data"][0]
 
 
 def _pair_of_pools(k, v, what: str):
@@ -659,9 +679,10 @@ def psrl_kv_copy(extents, k_src, v_src, k_dst, v_dst, stream=None):
     if heads != heads2 or row != row2 or k_src.dtype != k_dst.dtype:
         raise ValueError("source and destination pools differ in heads, head dimension or type")
     e, n, at = _extents(extents)
-    with _on_device_of(stream, k_src, v_src, k_dst, v_dst) as on:
-        _check(lib().psrl_kv_copy(at, n, heads, row, k_src.data_ptr(), v_src.data_ptr(), cap, k_dst.data_ptr(),
-                                  v_dst.data_ptr(), cap2, on.ptr), "psrl_kv_copy")
+    dev = _device_of(k_src, v_src, k_dst, v_dst)
+    raw, keep = _stream_on(stream, dev)
+    _launch("psrl_kv_copy", dev, at, n, heads, row, k_src.data_ptr(), v_src.data_ptr(), cap, k_dst.data_ptr(),
+            v_dst.data_ptr(), cap2, raw)
 
 
 def psrl_kv_move(moves, k_pool, v_pool, stream=None, workspace=None):
@@ -671,12 +692,13 @@ def psrl_kv_move(moves, k_pool, v_pool, stream=None, workspace=None):
 
     heads, cap, row = _pair_of_pools(k_pool, v_pool, "pools")
     e, n, at = _extents(moves)
-    with _on_device_of(stream, k_pool, v_pool) as on:
-        if workspace is None:
-            buf = on.keep(torch.empty(512, dtype=torch.uint8, device=k_pool.device))
-            workspace = ((buf.data_ptr() + 255) // 256 * 256, 256)
-        _check(lib().psrl_kv_move(at, n, heads, row, k_pool.data_ptr(), v_pool.data_ptr(), cap, workspace[0], workspace[1],
-                                  on.ptr), "psrl_kv_move")
+    dev = _device_of(k_pool, v_pool)
+    raw, keep = _stream_on(stream, dev)
+    if workspace is None:
+        buf = _kept(torch.empty(512, dtype=torch.uint8, device=k_pool.device), keep)
+        workspace = ((buf.data_ptr() + 255) // 256 * 256, 256)
+    _launch("psrl_kv_move", dev, at, n, heads, row, k_pool.data_ptr(), v_pool.data_ptr(), cap, workspace[0], workspace[1],
+            raw)
 
 
 def psrl_token_logprob_workspace_bytes(n_rows: int, hidden_dim: int, vocab: int, n_targets: int, backward: bool) -> int:
@@ -708,13 +730,13 @@ def _matrix_pitch(t, name: str) -> int:
     return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
 
 
-def _logprob_workspace(workspace, on, n, h, v, m, backward, device):
+def _logprob_workspace(workspace, keep, n, h, v, m, backward, device):
     import torch
 
     if workspace is not None:
         return workspace
     need = psrl_token_logprob_workspace_bytes(n, h, v, m, backward)
-    buf = on.keep(torch.empty(need + 256, dtype=torch.uint8, device=device))
+    buf = _kept(torch.empty(need + 256, dtype=torch.uint8, device=device), keep)
     return (buf.data_ptr() + 255) // 256 * 256, need
 
 
@@ -728,16 +750,17 @@ def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: floa
     n, h, v, m = _logprob_args(hidden, weight, targets, target_off, [])
     _logprob_args(hidden, weight, targets, target_off, [("logprob", logprob, m), ("lse", lse, n)])
     given = [t for t in (target_off, logprob, lse) if t is not None]
-    with _on_device_of(stream, hidden, weight, targets, *given) as on:
-        if logprob is None:
-            logprob = on.keep(torch.empty(m, dtype=torch.float32, device=hidden.device))
-        if lse is None:
-            lse = on.keep(torch.empty(n, dtype=torch.float32, device=hidden.device))
-        ws, wsb = _logprob_workspace(workspace, on, n, h, v, m, False, hidden.device)
-        _check(lib().psrl_token_logprob_fwd(n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
-                                            _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
-                                            None if target_off is None else target_off.data_ptr(), scale, logprob.data_ptr(),
-                                            lse.data_ptr(), ws, wsb, on.ptr), "psrl_token_logprob_fwd")
+    dev = _device_of(hidden, weight, targets, *given)
+    raw, keep = _stream_on(stream, dev)
+    if logprob is None:
+        logprob = _kept(torch.empty(m, dtype=torch.float32, device=hidden.device), keep)
+    if lse is None:
+        lse = _kept(torch.empty(n, dtype=torch.float32, device=hidden.device), keep)
+    ws, wsb = _logprob_workspace(workspace, keep, n, h, v, m, False, hidden.device)
+    _launch("psrl_token_logprob_fwd", dev, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
+            _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
+            None if target_off is None else target_off.data_ptr(), scale, logprob.data_ptr(),
+            lse.data_ptr(), ws, wsb, raw)
     return logprob, lse
 
 
@@ -754,20 +777,20 @@ def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, tar
         if t is not None and (t.dtype != torch.bfloat16 or t.shape != like.shape):
             raise ValueError(f"{name} must be bfloat16 {tuple(like.shape)}")
     given = [t for t in (target_off, d_hidden, d_weight) if t is not None]
-    with _on_device_of(stream, hidden, weight, targets, logprob, lse, d_logprob, *given) as on:
-        if d_hidden is None and want_hidden:
-            d_hidden = on.keep(torch.empty((n, h), dtype=torch.bfloat16, device=hidden.device))
-        if d_weight is None and want_weight:
-            d_weight = on.keep(torch.empty((v, h), dtype=torch.bfloat16, device=hidden.device))
-        out = [t if w else None for t, w in ((d_hidden, want_hidden), (d_weight, want_weight))]
-        ws, wsb = _logprob_workspace(workspace, on, n, h, v, m, True, hidden.device)
-        args = [x for t, name in zip(out, ("d_hidden", "d_weight"))
-                for x in ((None, 0) if t is None else (t.data_ptr(), _matrix_pitch(t, name)))]
-        _check(lib().psrl_token_logprob_bwd(n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
-                                            _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
-                                            None if target_off is None else target_off.data_ptr(), scale, logprob.data_ptr(),
-                                            lse.data_ptr(), d_logprob.data_ptr(), *args, ws, wsb, on.ptr),
-               "psrl_token_logprob_bwd")
+    dev = _device_of(hidden, weight, targets, logprob, lse, d_logprob, *given)
+    raw, keep = _stream_on(stream, dev)
+    if d_hidden is None and want_hidden:
+        d_hidden = _kept(torch.empty((n, h), dtype=torch.bfloat16, device=hidden.device), keep)
+    if d_weight is None and want_weight:
+        d_weight = _kept(torch.empty((v, h), dtype=torch.bfloat16, device=hidden.device), keep)
+    out = [t if w else None for t, w in ((d_hidden, want_hidden), (d_weight, want_weight))]
+    ws, wsb = _logprob_workspace(workspace, keep, n, h, v, m, True, hidden.device)
+    args = [x for t, name in zip(out, ("d_hidden", "d_weight"))
+            for x in ((None, 0) if t is None else (t.data_ptr(), _matrix_pitch(t, name)))]
+    _launch("psrl_token_logprob_bwd", dev, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
+            _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
+            None if target_off is None else target_off.data_ptr(), scale, logprob.data_ptr(),
+            lse.data_ptr(), d_logprob.data_ptr(), *args, ws, wsb, raw)
     return tuple(out)
 
 

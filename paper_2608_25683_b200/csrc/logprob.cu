@@ -415,22 +415,110 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
 
 // ------------------------------------------------------------------------------------------------- small kernels
 
-// lse of 32 rows from their partial (max, sum), then the log-probabilities of the rows' targets: the target's logit is a
-// dot product of its own (two rows read per target, against a whole pass over the weights for the lse).
-constexpr int kFinalWarps = 8;
-__global__ void __launch_bounds__(kFinalWarps * 32) final_kernel(const float2* __restrict__ part, int n_parts, int M, int hidden_dim,
-                                                                 int vocab, const __nv_bfloat16* __restrict__ hidden, int64_t h_pitch,
-                                                                 const __nv_bfloat16* __restrict__ weight, int64_t w_pitch,
-                                                                 const int32_t* __restrict__ targets, const int32_t* __restrict__ off,
-                                                                 int n_targets, float scale, float* __restrict__ logprob,
-                                                                 float* __restrict__ lse) {
-  __shared__ float2 s_part[kFinalWarps][32];
-  __shared__ float s_lse[32];
+// Few rows (the next tokens of a rollout): the weights are read once whatever the rows, so the products are bound by HBM
+// and ordinary fp32 arithmetic keeps up, two multiply-adds an instruction.  A warp takes four vocabulary entries at a time
+// and holds their products with all kRows hidden rows, which lie in shared memory; running maximum and sum per row.
+constexpr int kFewThreads = 256, kFewV = 4;
+constexpr size_t kFewSmem = 128 * 1024;   // hidden rows at most
+
+// eight bf16 as four pairs of fp32
+__device__ __forceinline__ void widen(const uint4& x, f32x2 (&o)[4]) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = make_f32x2(w[j] << 16, w[j] & 0xffff0000u);
+}
+
+template <int kRows>
+__global__ void __launch_bounds__(kFewThreads) few_rows_kernel(int M, int vecs, int vocab, const uint4* __restrict__ hidden,
+                                                               int64_t h_pitch_vecs, const uint4* __restrict__ weight,
+                                                               int64_t w_pitch_vecs, float scale_log2, float2* __restrict__ part) {
+  extern __shared__ uint4 s_h[];   // [kRows][vecs]
+  __shared__ float2 s_best[kFewThreads / 32][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int row0 = blockIdx.x * 32, row = row0 + lane;
+  for (int i = threadIdx.x; i < kRows * vecs; i += kFewThreads) {
+    const int r = i / vecs;
+    s_h[i] = r < M ? hidden[r * h_pitch_vecs + (i - r * vecs)] : make_uint4(0, 0, 0, 0);
+  }
+  __syncthreads();
+  float best[kRows], sum[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) { best[r] = -CUDART_INF_F; sum[r] = 0.f; }
+  const int stride = gridDim.x * (kFewThreads / 32) * kFewV;
+  for (int v0 = (blockIdx.x * (kFewThreads / 32) + warp) * kFewV; v0 < vocab; v0 += stride) {
+    f32x2 acc[kRows][kFewV];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int k = 0; k < kFewV; ++k) acc[r][k] = make_f32x2(0.f, 0.f);
+    const uint4* wp[kFewV];
+#pragma unroll
+    for (int k = 0; k < kFewV; ++k) wp[k] = weight + int64_t(min(v0 + k, vocab - 1)) * w_pitch_vecs;
+#pragma unroll 2
+    for (int i = lane; i < vecs; i += 32) {
+      f32x2 w[kFewV][4];
+#pragma unroll
+      for (int k = 0; k < kFewV; ++k) widen(__ldcs(wp[k] + i), w[k]);
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        f32x2 h[4];
+        widen(s_h[r * vecs + i], h);
+#pragma unroll
+        for (int k = 0; k < kFewV; ++k)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[r][k] = fma2(h[j], w[k][j], acc[r][k]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      float z[kFewV], top = best[r];
+#pragma unroll
+      for (int k = 0; k < kFewV; ++k) {
+        float x, y;
+        split_f32x2(acc[r][k], x, y);
+        x += y;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        z[k] = v0 + k < vocab ? x * scale_log2 : -CUDART_INF_F;
+        top = fmaxf(top, z[k]);
+      }
+      const float ref = top == -CUDART_INF_F ? 0.f : top;
+      sum[r] *= ex2(best[r] - ref);
+#pragma unroll
+      for (int k = 0; k < kFewV; ++k) sum[r] += ex2(z[k] - ref);
+      best[r] = top;
+    }
+  }
+  if (lane == 0)
+    for (int r = 0; r < kRows; ++r) s_best[warp][r] = make_float2(best[r], sum[r]);
+  __syncthreads();
+  if (threadIdx.x < kRows && threadIdx.x < M) {
+    const int r = threadIdx.x;
+    float top = -CUDART_INF_F, s = 0.f;
+    for (int i = 0; i < kFewThreads / 32; ++i) top = fmaxf(top, s_best[i][r].x);
+    const float ref = top == -CUDART_INF_F ? 0.f : top;
+    for (int i = 0; i < kFewThreads / 32; ++i) s += s_best[i][r].y * ex2(s_best[i][r].x - ref);
+    part[int64_t(blockIdx.x) * M + r] = make_float2(top, s);
+  }
+}
+
+// lse of kRows rows from their partial (max, sum), then the log-probabilities of the rows' targets: the target's logit is a
+// dot product of its own (two rows read per target, against a whole pass over the weights for the lse).
+constexpr int kFinalThreads = 256;
+template <int kRows>
+__global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __restrict__ part, int n_parts, int M, int hidden_dim,
+                                                              int vocab, const __nv_bfloat16* __restrict__ hidden, int64_t h_pitch,
+                                                              const __nv_bfloat16* __restrict__ weight, int64_t w_pitch,
+                                                              const int32_t* __restrict__ targets, const int32_t* __restrict__ off,
+                                                              int n_targets, float scale, float* __restrict__ logprob,
+                                                              float* __restrict__ lse) {
+  constexpr int kSlices = kFinalThreads / kRows;
+  __shared__ float2 s_part[kSlices][kRows];
+  __shared__ float s_lse[kRows];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row0 = blockIdx.x * kRows, mine = threadIdx.x % kRows, slice = threadIdx.x / kRows, row = row0 + mine;
   float m = -CUDART_INF_F, s = 0.f;
   if (row < M) {
-    for (int i = warp; i < n_parts; i += kFinalWarps) {
+    for (int i = slice; i < n_parts; i += kSlices) {
       const float2 x = part[int64_t(i) * M + row];
       const float top = fmaxf(m, x.x);
       const float ref = top == -CUDART_INF_F ? 0.f : top;
@@ -438,25 +526,30 @@ __global__ void __launch_bounds__(kFinalWarps * 32) final_kernel(const float2* _
       m = top;
     }
   }
-  s_part[warp][lane] = make_float2(m, s);
+  s_part[slice][mine] = make_float2(m, s);
+  for (int half = kSlices / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (slice < half) {
+      const float2 x = s_part[slice][mine], y = s_part[slice + half][mine];
+      const float top = fmaxf(x.x, y.x), ref = top == -CUDART_INF_F ? 0.f : top;
+      s_part[slice][mine] = make_float2(top, x.y * exp2f(x.x - ref) + y.y * exp2f(y.x - ref));
+    }
+  }
   __syncthreads();
-  if (warp == 0) {
-    float top = -CUDART_INF_F, sum = 0.f;
-    for (int w = 0; w < kFinalWarps; ++w) top = fmaxf(top, s_part[w][lane].x);
-    const float ref = top == -CUDART_INF_F ? 0.f : top;
-    for (int w = 0; w < kFinalWarps; ++w) sum += s_part[w][lane].y * exp2f(s_part[w][lane].x - ref);
-    const float l = (ref + log2f(sum)) * kLn2;
-    s_lse[lane] = l;
+  if (slice == 0) {
+    const float2 x = s_part[0][mine];
+    const float l = ((x.x == -CUDART_INF_F ? 0.f : x.x) + log2f(x.y)) * kLn2;
+    s_lse[mine] = l;
     if (row < M) lse[row] = l;
   }
   __syncthreads();
   const int vecs = hidden_dim / 8;
   int at = 0;   // targets of the rows before, for the distribution over the warps
-  for (int r = 0; r < 32 && row0 + r < M; ++r) {
+  for (int r = 0; r < kRows && row0 + r < M; ++r) {
     int b, e;
     target_range(off, row0 + r, n_targets, b, e);
     for (int t = b; t < e; ++t, ++at) {
-      if (at % kFinalWarps != warp) continue;
+      if (at % (kFinalThreads / 32) != warp) continue;
       const int y = targets[t];
       if (y < 0 || y >= vocab) {
         if (lane == 0) logprob[t] = 0.f;
@@ -464,21 +557,22 @@ __global__ void __launch_bounds__(kFinalWarps * 32) final_kernel(const float2* _
       }
       const uint4* hv = reinterpret_cast<const uint4*>(hidden + int64_t(row0 + r) * h_pitch);
       const uint4* wv = reinterpret_cast<const uint4*>(weight + int64_t(y) * w_pitch);
-      float acc = 0.f;
+      f32x2 acc = make_f32x2(0.f, 0.f);
 #pragma unroll 4
       for (int i = lane; i < vecs; i += 32) {
-        const uint4 x = hv[i], w = wv[i];
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
+        f32x2 x[4], w[4];
+        widen(hv[i], x);
+        widen(wv[i], w);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          acc = fmaf(__uint_as_float(xs[j] << 16), __uint_as_float(ws[j] << 16), acc);
-          acc = fmaf(__uint_as_float(xs[j] & 0xffff0000u), __uint_as_float(ws[j] & 0xffff0000u), acc);
-        }
+        for (int j = 0; j < 4; ++j) acc = fma2(x[j], w[j], acc);
       }
+      float z, z1;
+      split_f32x2(acc, z, z1);
+      z += z1;
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+      for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
       // a log-probability is not positive; the two sums are rounded apart
-      if (lane == 0) logprob[t] = fminf(scale * acc - s_lse[r], 0.f);
+      if (lane == 0) logprob[t] = fminf(scale * z - s_lse[r], 0.f);
     }
   }
 }
@@ -578,8 +672,12 @@ __global__ void __launch_bounds__(256) gather_kernel(int M, const uint8_t* __res
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
+constexpr int kFewRows = 8;       // up to here the forward takes few_rows_kernel
+constexpr int kFewBlocks = 1184;  // its blocks at most: eight per SM
+
 struct Layout {
-  int32_t n_tiles, run, n_parts, m_tiles;
+  int32_t n_tiles, run, n_parts;
+  int32_t few;                   // rows that few_rows_kernel is built for, 0: the matrix kernel
   int64_t piece;                 // vocabulary entries of one piece of the backward
   int64_t rows;                  // rows that the backward's gathered buffers hold
   size_t part, row_info, entry, matters, row_of, count, gathered, dz, acc, total;
@@ -587,15 +685,20 @@ struct Layout {
 
 Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward) {
   Layout L{};
-  L.m_tiles = static_cast<int32_t>((n + 255) / 256);
+  const int64_t m_tiles = (n + 255) / 256;
   L.n_tiles = static_cast<int32_t>((v + 255) / 256);
   size_t at = kWsHeaderBytes;
   auto take = [&](size_t bytes) { const size_t a = at; at += (bytes + 255) / 256 * 256; return a; };
   if (!backward) {
     // short runs while there are few tiles (they balance the pairs of CTAs), long ones to keep the partials small
-    const int64_t tiles = int64_t(L.m_tiles) * L.n_tiles;
+    const int64_t tiles = m_tiles * L.n_tiles;
     L.run = static_cast<int32_t>(std::min<int64_t>(kMaxRun, std::max<int64_t>(1, tiles / (74 * 16))));
     L.n_parts = (L.n_tiles + L.run - 1) / L.run;
+    if (n <= kFewRows) {
+      for (L.few = 1; L.few < n;) L.few *= 2;
+      if (size_t(L.few) * h * 2 > kFewSmem) L.few = 0;
+      else L.n_parts = static_cast<int32_t>(std::min<int64_t>(kFewBlocks, (v + kFewThreads / 32 * kFewV - 1) / (kFewThreads / 32 * kFewV)));
+    }
     L.part = take(size_t(L.n_parts) * n * sizeof(float2));
   } else {
     // a piece of dz is about 128 MB (it then partly stays in the L2 for the two products that read it) but at least
@@ -626,6 +729,18 @@ cudaError_t launch_gemm(const GemmMaps& maps, GemmParams& p, cudaStream_t stream
   if (units > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int clusters = static_cast<int>(std::min<int64_t>(units, resident_ctas() / 2));
   gemm_kernel<kKind><<<2 * clusters, kGemmThreads, kGemmSmem, stream>>>(maps, p);
+  return cudaGetLastError();
+}
+
+template <int kRows>
+cudaError_t launch_few(const Layout& L, int32_t M, int32_t h, int32_t v, const void* hidden, int64_t hp, const void* weight, int64_t wp,
+                       float scale, float2* part, cudaStream_t stream) {
+  static bool done[64] = {};
+  const size_t smem = size_t(kRows) * h * 2;
+  cudaError_t e = ensure_dynamic_smem(few_rows_kernel<kRows>, kFewSmem, done);
+  if (e != cudaSuccess) return e;
+  few_rows_kernel<kRows><<<unsigned(L.n_parts), kFewThreads, smem, stream>>>(M, h / 8, v, static_cast<const uint4*>(hidden), hp / 8,
+                                                                           static_cast<const uint4*>(weight), wp / 8, scale * kLog2e, part);
   return cudaGetLastError();
 }
 
@@ -677,22 +792,34 @@ psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t
   if (!al4(lse) || (n_targets && !al4(logprob))) return PSRL_ERR_INVALID_ARG;
   const Layout L = layout(n_rows, hidden_dim, vocab, n_targets, false);
   char* ws = static_cast<char*>(workspace);
-  GemmMaps maps;
-  if (!make_map_bf16_2d(&maps.a, hidden, hidden_dim, n_rows, hidden_pitch * 2, 128) ||
-      !make_map_bf16_2d(&maps.b, weight, hidden_dim, vocab, weight_pitch * 2, 128))
-    return PSRL_ERR_CUDA;
-  GemmParams p{};
-  p.M = static_cast<int32_t>(n_rows);
-  p.N = vocab;
-  p.k_blocks = (hidden_dim + kBK - 1) / kBK;
-  p.run = L.run;
-  p.scale_log2 = scale * kLog2e;
-  p.part = reinterpret_cast<float2*>(ws + L.part);
-  p.status = reinterpret_cast<int*>(ws);
-  e = launch_gemm<kLse>(maps, p, s);
+  float2* part = reinterpret_cast<float2*>(ws + L.part);
+  const int32_t M = static_cast<int32_t>(n_rows);
+  if (L.few) {
+    e = L.few == 1 ? launch_few<1>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s)
+      : L.few == 2 ? launch_few<2>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s)
+      : L.few == 4 ? launch_few<4>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s)
+                   : launch_few<8>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s);
+  } else {
+    GemmMaps maps;
+    if (!make_map_bf16_2d(&maps.a, hidden, hidden_dim, n_rows, hidden_pitch * 2, 128) ||
+        !make_map_bf16_2d(&maps.b, weight, hidden_dim, vocab, weight_pitch * 2, 128))
+      return PSRL_ERR_CUDA;
+    GemmParams p{};
+    p.M = M;
+    p.N = vocab;
+    p.k_blocks = (hidden_dim + kBK - 1) / kBK;
+    p.run = L.run;
+    p.scale_log2 = scale * kLog2e;
+    p.part = part;
+    p.status = reinterpret_cast<int*>(ws);
+    e = launch_gemm<kLse>(maps, p, s);
+  }
   if (e != cudaSuccess) return cuda_failed(e);
-  final_kernel<<<unsigned((n_rows + 31) / 32), kFinalWarps * 32, 0, s>>>(
-      p.part, L.n_parts, p.M, hidden_dim, vocab, static_cast<const __nv_bfloat16*>(hidden), hidden_pitch,
+  // rows of a block: 32 read the partials in whole lines; with few rows more threads to each of them finish sooner
+  const int rows = M >= 4096 ? 32 : M >= 256 ? 4 : 1;
+  auto final = rows == 32 ? final_kernel<32> : rows == 4 ? final_kernel<4> : final_kernel<1>;
+  final<<<unsigned((M + rows - 1) / rows), kFinalThreads, 0, s>>>(
+      part, L.n_parts, M, hidden_dim, vocab, static_cast<const __nv_bfloat16*>(hidden), hidden_pitch,
       static_cast<const __nv_bfloat16*>(weight), weight_pitch, targets, target_off, static_cast<int>(n_targets), scale, logprob, lse);
   e = cudaGetLastError();
   return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
