@@ -10,8 +10,10 @@
 //   kLse   running maximum and sum of exponentials of a row over a run of vocabulary tiles   -> partial (max, sum)
 //   kDz    dz = -scale G softmax, with the entries of the row's targets put in afterwards    -> bf16, one piece of the
 //          vocabulary at a time in the workspace (the softmax part is rounded to bf16 as the tensor cores need it)
-//   kDh    d_hidden += dz W over the pieces, summed in fp32, rounded once at the end
-//   kDw    d_weight = dz^T hidden, the whole sum in tensor memory, rounded once
+//   kGrad  both gradients of a piece in one launch: d_hidden += dz W, summed over the pieces in fp32 and rounded once at
+//          the end, and d_weight = dz^T hidden, the whole sum in tensor memory, rounded once.  The few deep tiles of
+//          d_hidden come first, the many shallow ones of d_weight even out what they leave (grad_work); with few rows the
+//          depth of d_hidden is split as well, into partial sums that a last kernel adds in order.
 // The pieces make dz as large as the caller's hidden states, not as the logits.
 //
 // The backward works on the rows that matter alone: a row without a target, or whose d_logprob are all zero (prompts,
@@ -40,17 +42,18 @@ constexpr int kGemmThreads = 6 * 32;         // warps 0-3 epilogue, 4 TMA, 5 MMA
 constexpr size_t kGemmSmem = size_t(kStages) * kStageBytes + 1024;
 constexpr int kMaxRun = 8;                   // vocabulary tiles whose maximum and sum stay in registers
 
-enum Kind { kLse, kDz, kDh, kDw };
+enum Kind { kLse, kDz, kGrad };
 
 struct GemmMaps {
-  CUtensorMap a, b;
+  CUtensorMap a, b;     // kGrad: of d_hidden
+  CUtensorMap a2, b2;   // kGrad: of d_weight
 };
 
 struct GemmParams {
   int32_t M, N;                 // valid rows and columns of the product
   int32_t n_tiles, k_blocks;
-  const int32_t* count;         // rows that matter, on the device: M of kDz and kDh, K of kDw; NULL: as M and k_blocks say
-  const int32_t* row_of;        // kDz, kDh: the caller's row of a gathered row
+  const int32_t* count;         // kDz, kGrad: rows that matter, on the device (kLse: NULL, all M)
+  const int32_t* row_of;        // kDz, kGrad: the caller's row of a gathered row
   int32_t run;                  // kLse: consecutive column tiles of one work unit
   float scale_log2;             // logits in powers of two: scale * log2(e)
   float2* part;                 // kLse: [unit column][M] (max, sum), powers of two
@@ -59,11 +62,15 @@ struct GemmParams {
   const int32_t* target_off;    // kDz: may be NULL (one target per row)
   const float* entry;           // kDz: value of dz at every target
   int32_t n_targets, col0;      // kDz: col0 = first vocabulary entry of the piece
-  __nv_bfloat16* out;           // kDz, kDh (last piece), kDw
+  __nv_bfloat16* out;           // kDz: dz; kGrad: d_hidden, or NULL
   int64_t out_pitch;
-  float* acc;                   // kDh: fp32 sums over the pieces, [M][acc_pitch]
-  int64_t acc_pitch;
-  int32_t first, last;          // kDh: first / last piece
+  __nv_bfloat16* out2;          // kGrad: the piece's rows of d_weight, or NULL
+  int64_t out2_pitch;
+  int32_t vocab;                // kGrad: entries of the piece
+  int32_t splits;               // kGrad: parts of d_hidden's sum over them
+  float* acc;                   // kGrad: fp32 sums of d_hidden over the pieces, [splits][acc_rows][acc_pitch]
+  int64_t acc_pitch, acc_rows;
+  int32_t first, last;          // kGrad: first / last piece
   int* status;
 };
 
@@ -137,6 +144,45 @@ __device__ __forceinline__ void target_range(const int32_t* off, int64_t row, in
   e = off ? min(max(off[row + 1], b), n_targets) : int(row) + 1;
 }
 
+// What a pair of CTAs does next in kGrad: a tile of d_hidden (over part of its depth) or of d_weight.
+struct GradWork {
+  int weight;       // 1: d_weight
+  int mt, nt;
+  int kb0, kb1;     // steps of its sum
+  int split;
+};
+// Pair c of C takes the units c, c + C, ... of d_hidden.  The first r pairs then have one more than the others, who make up
+// for it with the first tiles of d_weight; the rest of those go round.  No counter, no order that could vary.
+__device__ __forceinline__ bool grad_work(const GemmParams& p, int rows, int c, int C, int i, GradWork& w) {
+  const int m_tiles = p.out ? (rows + 255) / 256 : 0, v_tiles = p.out2 ? (p.vocab + 255) / 256 : 0;
+  const int per = m_tiles * p.n_tiles, n_hidden = per * p.splits;
+  const int steps = (p.vocab + kBK - 1) / kBK, row_steps = (rows + kBK - 1) / kBK;
+  const int u = c + i * C;
+  if (u < n_hidden) {
+    w.weight = 0;
+    w.split = u / per;
+    unit_tile(m_tiles, u - w.split * per, p.n_tiles, w.mt, w.nt);
+    w.kb0 = int(int64_t(steps) * w.split / p.splits);
+    w.kb1 = int(int64_t(steps) * (w.split + 1) / p.splits);
+    return true;
+  }
+  const int q = n_hidden / C, r = n_hidden - q * C, n_weight = v_tiles * p.n_tiles;
+  const int j = i - q - (c < r ? 1 : 0), light = C - r;
+  int ahead = 0;
+  // cost of a unit in steps; a tile of few steps is bound by its epilogue, worth about eight
+  if (r > 0) ahead = min((steps / p.splits + 8) / max(row_steps, 8), n_weight / light);
+  int at = ahead * light;
+  if (c >= r && j < ahead) at = j * light + c - r;
+  else at += (c >= r ? j - ahead : j) * C + c;
+  if (at >= n_weight) return false;
+  w.weight = 1;
+  w.split = 0;
+  w.kb0 = 0;
+  w.kb1 = row_steps;
+  unit_tile(v_tiles, at, p.n_tiles, w.mt, w.nt);
+  return true;
+}
+
 struct __align__(8) PairBarriers {
   uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
 };
@@ -152,8 +198,6 @@ __device__ __forceinline__ void store_bf16x16(__nv_bfloat16* dst, const float* v
 template <Kind kKind>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
-  // which operand lies with its M or N side contiguous: W in dz W; both in dz^T hidden
-  constexpr bool kAmn = kKind == kDw, kBmn = kKind == kDh || kKind == kDw;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   __shared__ PairBarriers bar;
@@ -163,10 +207,28 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   const uint32_t rank = cluster_rank();
   const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
   const int n_units = (p.n_tiles + p.run - 1) / p.run;
-  const int count = p.count ? *p.count : 0;
-  const int M = p.count && kKind != kDw ? count : p.M;
-  const int k_blocks = p.count && kKind == kDw ? (count + kBK - 1) / kBK : p.k_blocks;
-  const int m_tiles = (M + 255) / 256, units = m_tiles * n_units;
+  const int rows = kKind == kLse ? p.M : *p.count;
+  const int m_tiles = (rows + 255) / 256;
+
+  // The i-th work unit of this pair: a row tile and consecutive column tiles, all over steps kb0 .. kb1.
+  auto work = [&](int i, GradWork& w, int& nt_end) -> bool {
+    if constexpr (kKind == kGrad) {
+      if (!grad_work(p, rows, cluster, n_clusters, i, w)) return false;
+      nt_end = w.nt + 1;
+    } else {
+      const int unit = cluster + i * n_clusters;
+      if (unit >= m_tiles * n_units) return false;
+      int nu;
+      unit_tile(m_tiles, unit, n_units, w.mt, nu);
+      w.weight = 0;
+      w.kb0 = 0;
+      w.kb1 = p.k_blocks;
+      w.split = nu;
+      w.nt = nu * p.run;
+      nt_end = min(w.nt + p.run, p.n_tiles);
+    }
+    return true;
+  };
 
   if (tid == 0) {
     s_abort = 0;
@@ -184,6 +246,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   volatile int* abortp = &s_abort;
+  GradWork w;
+  int nt_end;
 
   if (warp == 4) {
     // ======================= TMA producer (both CTAs) =======================
@@ -192,13 +256,14 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
       tma_prefetch_desc(&maps.b);
       uint32_t it = 0;
       bool ok = true;
-      for (int unit = cluster; unit < units && ok; unit += n_clusters) {
-        int mt, nu;
-        unit_tile(m_tiles, unit, n_units, mt, nu);
-        const int nt_end = min((nu + 1) * p.run, p.n_tiles);
-        for (int nt = nu * p.run; nt < nt_end && ok; ++nt) {
-          const int m0 = mt * 256 + int(rank) * 128, n0 = nt * 256 + int(rank) * 128;
-          for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+      for (int i = 0; ok && work(i, w, nt_end); ++i) {
+        const bool a_mn = kKind == kGrad && w.weight;
+        const CUtensorMap* ma = a_mn ? &maps.a2 : &maps.a;
+        const CUtensorMap* mb = a_mn ? &maps.b2 : &maps.b;
+        const int m0 = w.mt * 256 + int(rank) * 128;
+        for (int nt = w.nt; nt < nt_end && ok; ++nt) {
+          const int n0 = nt * 256 + int(rank) * 128;
+          for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
             const uint32_t s = it % kStages, round = it / kStages;
             if (round > 0 && !mbar_wait(&bar.empty[s], (round + 1) & 1, abortp, p.status)) { ok = false; break; }
             // the second CTA's copies count on the first one's barrier as well
@@ -206,17 +271,17 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
             const uint32_t full = in_leader(&bar.full[s]);
             uint8_t* sa = smem + s * kStageBytes;
             uint8_t* sb = sa + kOperandBytes;
-            if (kAmn) {
-              tma_load_pair(sa, &maps.a, full, m0, kb * kBK);
-              tma_load_pair(sa + kOperandBytes / 2, &maps.a, full, m0 + 64, kb * kBK);
+            if (a_mn) {
+              tma_load_pair(sa, ma, full, m0, kb * kBK);
+              tma_load_pair(sa + kOperandBytes / 2, ma, full, m0 + 64, kb * kBK);
             } else {
-              tma_load_pair(sa, &maps.a, full, kb * kBK, m0);
+              tma_load_pair(sa, ma, full, kb * kBK, m0);
             }
-            if (kBmn) {
-              tma_load_pair(sb, &maps.b, full, n0, kb * kBK);
-              tma_load_pair(sb + kOperandBytes / 2, &maps.b, full, n0 + 64, kb * kBK);
+            if (kKind == kGrad) {
+              tma_load_pair(sb, mb, full, n0, kb * kBK);
+              tma_load_pair(sb + kOperandBytes / 2, mb, full, n0 + 64, kb * kBK);
             } else {
-              tma_load_pair(sb, &maps.b, full, kb * kBK, n0);
+              tma_load_pair(sb, mb, full, kb * kBK, n0);
             }
           }
         }
@@ -230,33 +295,34 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   } else if (warp == 5) {
     // ======================= MMA issuer (first CTA of the pair) =======================
     if (rank == 0) {
-      constexpr uint32_t idesc = make_idesc(256, 256, kAmn ? 1 : 0, kBmn ? 1 : 0);
-      // bytes from one 64-wide block of an MN-major operand to the next; per 16-deep step: 32 bytes, or 16 rows
-      constexpr uint32_t kLbo = kOperandBytes / 2;
-      constexpr uint32_t kStepA = kAmn ? 2048 >> 4 : 32 >> 4, kStepB = kBmn ? 2048 >> 4 : 32 >> 4;
+      // Operands: hidden, weight and dz with the depth contiguous (K-major) in the logits; in the gradients both lie with
+      // the other side contiguous (MN-major), but for dz in d_hidden.  An MN-major operand's 64-wide blocks are kLbo bytes
+      // apart and a 16-deep step is 16 rows of 128 bytes; K-major, a step is 32 bytes.
+      constexpr uint32_t kLbo = kOperandBytes / 2, kStepK = 32 >> 4, kStepMn = 2048 >> 4;
+      constexpr uint32_t kStepB = kKind == kGrad ? kStepMn : kStepK;
       const bool elected = elect_one();
       uint32_t it = 0, tile = 0;
       bool ok = true;
-      for (int unit = cluster; unit < units && ok; unit += n_clusters) {
-        int mt, nu;
-        unit_tile(m_tiles, unit, n_units, mt, nu);
-        const int nt_end = min((nu + 1) * p.run, p.n_tiles);
-        for (int nt = nu * p.run; nt < nt_end && ok; ++nt, ++tile) {
+      for (int i = 0; ok && work(i, w, nt_end); ++i) {
+        const bool a_mn = kKind == kGrad && w.weight;
+        const uint32_t idesc = make_idesc(256, 256, a_mn ? 1 : 0, kKind == kGrad ? 1 : 0);
+        const uint32_t step_a = a_mn ? kStepMn : kStepK, lbo_a = a_mn ? kLbo : 0;
+        for (int nt = w.nt; nt < nt_end && ok; ++nt, ++tile) {
           const uint32_t a = tile & 1, use = tile >> 1;
           if (use > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bar.acc_empty[a], (use + 1) & 1, abortp, p.status));
           if (!ok) break;
           tc_fence_after();
           const uint32_t d = tmem + a * 256;
-          for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+          for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
             const uint32_t s = it % kStages;
             if (!mbar_wait_all1(&bar.full[s], (it / kStages) & 1, abortp, p.status)) { ok = false; break; }
             tc_fence_after();
             const uint32_t sa = smem_u32(smem) + s * kStageBytes, sb = sa + kOperandBytes;
-            const uint32_t da = desc_lo(sa, kAmn ? kLbo : 0), db = desc_lo(sb, kBmn ? kLbo : 0);
+            const uint32_t da = desc_lo(sa, lbo_a), db = desc_lo(sb, kKind == kGrad ? kLbo : 0);
             if (elected) {
 #pragma unroll
               for (uint32_t k = 0; k < kBK / 16; ++k)
-                mma_pair(d, da + k * kStepA, db + k * kStepB, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                mma_pair(d, da + k * step_a, db + k * kStepB, idesc, (kb > w.kb0 || k > 0) ? 1u : 0u);
               commit_pair(&bar.empty[s]);
             }
             __syncwarp();
@@ -272,24 +338,31 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
     const uint32_t empty0 = in_leader(&bar.acc_empty[0]), empty1 = in_leader(&bar.acc_empty[1]);
     uint32_t tile = 0;
     bool ok = true;
-    for (int unit = cluster; unit < units && ok; unit += n_clusters) {
-      int mt, nu;
-      unit_tile(m_tiles, unit, n_units, mt, nu);
-      const int row = mt * 256 + int(rank) * 128 + warp * 32 + lane;
-      const bool live = row < M;
+    for (int i = 0; ok && work(i, w, nt_end); ++i) {
+      const int row = w.mt * 256 + int(rank) * 128 + warp * 32 + lane;
+      const bool live = row < (kKind == kGrad && w.weight ? p.vocab : rows);
       float best = -CUDART_INF_F, sum = 0.f;                       // kLse
       float lse2 = 0.f, coef = 0.f;                                // kDz
       int t_begin = 0, t_end = 0;
       // dz is read in steps of kBK rows by the product for d_weight: the rows behind the last one of a step are zero
-      const bool pad = kKind == kDz && !live && row < (M + kBK - 1) / kBK * kBK;
-      const int64_t user_row = (kKind == kDz || kKind == kDh) && live ? p.row_of[row] : row;
+      const bool pad = kKind == kDz && !live && row < (rows + kBK - 1) / kBK * kBK;
       if (kKind == kDz && live) {
+        const int user_row = p.row_of[row];
         const float2 ri = p.row_info[user_row];
         lse2 = ri.x; coef = ri.y;
         target_range(p.target_off, user_row, p.n_targets, t_begin, t_end);
       }
-      const int nt_end = min((nu + 1) * p.run, p.n_tiles);
-      for (int nt = nu * p.run; nt < nt_end; ++nt, ++tile) {
+      // kGrad: where the row goes as bf16, or the fp32 sums that it is added to
+      __nv_bfloat16* out_row = nullptr;
+      float* acc_row = nullptr;
+      if (kKind == kGrad && live) {
+        if (w.weight) out_row = p.out2 + int64_t(row) * p.out2_pitch;
+        else {
+          if (p.last && p.splits == 1) out_row = p.out + int64_t(p.row_of[row]) * p.out_pitch;
+          if (!out_row || !p.first) acc_row = p.acc + (int64_t(w.split) * p.acc_rows + row) * p.acc_pitch;
+        }
+      }
+      for (int nt = w.nt; nt < nt_end; ++nt, ++tile) {
         const uint32_t a = tile & 1;
         ok = __all_sync(0xffffffffu, mbar_wait(&bar.acc_full[a], (tile >> 1) & 1, abortp, p.status));
         if (!ok) break;
@@ -345,41 +418,36 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
           } else {
             float v[32];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = k_blocks ? __uint_as_float(r[i]) : 0.f;   // an empty sum writes no accumulator
-            if (live) {
-              if (kKind == kDh && !p.first) {
-                const float* q = p.acc + int64_t(row) * p.acc_pitch + col;
+            for (int i = 0; i < 32; ++i) v[i] = w.kb1 > w.kb0 ? __uint_as_float(r[i]) : 0.f;   // an empty sum writes no accumulator
+            if (acc_row && !p.first) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  float old[8];
-                  ld_global_32B(q + 8 * j, old);
+              for (int j = 0; j < 4; ++j) {
+                float old[8];
+                ld_global_32B(acc_row + col + 8 * j, old);
 #pragma unroll
-                  for (int i = 0; i < 8; ++i) v[8 * j + i] += old[i];
-                }
+                for (int i = 0; i < 8; ++i) v[8 * j + i] += old[i];
               }
-              if (kKind == kDh && !p.last) {
-                float* q = p.acc + int64_t(row) * p.acc_pitch + col;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  uint32_t o[8];
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(v[8 * j + i]);
-                  st_global_32B(q + 8 * j, o);
-                }
+            }
+            if (out_row) {
+              // the caller's rows are 16-byte aligned, and the last columns may be fewer than 32
+              if (col + 32 <= p.N && (reinterpret_cast<uintptr_t>(out_row) & 31) == 0) {
+                store_bf16x16(out_row + col, v);
+                store_bf16x16(out_row + col + 16, v + 16);
               } else {
-                // rows of the caller's tensor: 16-byte aligned, and the last columns may be fewer than 32
-                __nv_bfloat16* o = p.out + user_row * p.out_pitch + col;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                  if (col + 8 * j < p.N) {
-                    uint4 w;
-                    w.x = pack_bf16(v[8 * j], v[8 * j + 1]);
-                    w.y = pack_bf16(v[8 * j + 2], v[8 * j + 3]);
-                    w.z = pack_bf16(v[8 * j + 4], v[8 * j + 5]);
-                    w.w = pack_bf16(v[8 * j + 6], v[8 * j + 7]);
-                    *reinterpret_cast<uint4*>(o + 8 * j) = w;
-                  }
-                }
+                for (int j = 0; j < 4; ++j)
+                  if (col + 8 * j < p.N)
+                    *reinterpret_cast<uint4*>(out_row + col + 8 * j) =
+                        make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
+                                   pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+              }
+            } else if (acc_row) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                uint32_t o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(v[8 * j + i]);
+                st_global_32B(acc_row + col + 8 * j, o);
               }
             }
           }
@@ -396,7 +464,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
           }
         }
       }
-      if (kKind == kLse && ok && live) p.part[int64_t(nu) * M + row] = make_float2(best, sum);
+      if (kKind == kLse && ok && live) p.part[int64_t(w.split) * rows + row] = make_float2(best, sum);
     }
   }
   // ---- teardown ----
@@ -626,6 +694,23 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int voca
   if (threadIdx.x == 0) matters[blockIdx.x] = uint8_t(s_bits);
 }
 
+// d_hidden from the parts of its sum, in order.
+__global__ void __launch_bounds__(256) sum_kernel(const float4* __restrict__ acc, int splits, int64_t split_vecs, int pitch_vecs, int vecs,
+                                                  const int32_t* __restrict__ count, const int32_t* __restrict__ row_of,
+                                                  uint2* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
+  const int row = blockIdx.x;
+  if (row >= *count) return;
+  const int64_t to = row_of[row] * dh_pitch_vecs;
+  for (int i = threadIdx.x; i < vecs; i += 256) {
+    float4 s = acc[int64_t(row) * pitch_vecs + i];
+    for (int k = 1; k < splits; ++k) {
+      const float4 x = acc[k * split_vecs + int64_t(row) * pitch_vecs + i];
+      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+    d_hidden[to + i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+  }
+}
+
 // Gathers the hidden states of the rows that matter, in order, and zeroes the others' d_hidden.  A block takes 32 rows and
 // counts the rows before them itself: one bit per row is little to read.
 constexpr int kGatherRows = 32;
@@ -680,6 +765,7 @@ struct Layout {
   int32_t few;                   // rows that few_rows_kernel is built for, 0: the matrix kernel
   int64_t piece;                 // vocabulary entries of one piece of the backward
   int64_t rows;                  // rows that the backward's gathered buffers hold
+  int32_t splits;                // parts of d_hidden's sums
   size_t part, row_info, entry, matters, row_of, count, gathered, dz, acc, total;
 };
 
@@ -712,7 +798,11 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
     L.count = take(sizeof(int32_t));
     L.gathered = take(size_t(L.rows) * h * 2);
     L.dz = take(size_t(L.rows) * L.piece * 2);
-    L.acc = take(L.piece < v ? size_t(n) * round_up(h, 32) * sizeof(float) : 0);
+    // Parts of d_hidden's sum: with few rows there are fewer of its tiles than pairs of CTAs, and each is as deep as the
+    // piece; four units for every pair, of at least 16 steps, share that out.
+    const int64_t tiles = m_tiles * ((h + 255) / 256), most = std::min<int64_t>(16, L.piece / kBK / 16);
+    L.splits = tiles >= 148 ? 1 : static_cast<int32_t>(std::max<int64_t>(1, std::min(most, (296 + tiles - 1) / tiles)));
+    L.acc = take(L.piece < v || L.splits > 1 ? size_t(L.splits) * n * round_up(h, 32) * sizeof(float) : 0);
   }
   L.total = at;
   return L;
@@ -725,7 +815,8 @@ cudaError_t launch_gemm(const GemmMaps& maps, GemmParams& p, cudaStream_t stream
   if (e != cudaSuccess) return e;
   p.n_tiles = (p.N + 255) / 256;
   if (p.run < 1) p.run = 1;
-  const int64_t units = (int64_t(p.M) + 255) / 256 * ((p.n_tiles + p.run - 1) / p.run);
+  int64_t units = (int64_t(p.M) + 255) / 256 * ((p.n_tiles + p.run - 1) / p.run);
+  if (kKind == kGrad) units = units * p.splits + (int64_t(p.vocab) + 255) / 256 * p.n_tiles;
   if (units > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int clusters = static_cast<int>(std::min<int64_t>(units, resident_ctas() / 2));
   gemm_kernel<kKind><<<2 * clusters, kGemmThreads, kGemmSmem, stream>>>(maps, p);
@@ -854,6 +945,8 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   float2* row_info = reinterpret_cast<float2*>(ws + L.row_info);
   float* entry = reinterpret_cast<float*>(ws + L.entry);
   __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + L.dz);
+  float* acc = reinterpret_cast<float*>(ws + L.acc);
+  const int64_t acc_pitch = round_up(hidden_dim, 32);
   const int32_t M = static_cast<int32_t>(n_rows);
   rows_kernel<<<unsigned((n_rows + 7) / 8), 256, 0, s>>>(M, vocab, targets, target_off, static_cast<int>(n_targets), logprob, lse,
                                                          d_logprob, scale, row_info, entry, reinterpret_cast<uint8_t*>(ws + L.matters));
@@ -872,13 +965,13 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
     const int64_t nv = std::min<int64_t>(L.piece, vocab - v0);
     const __nv_bfloat16* wv = w + v0 * weight_pitch;
-    GemmMaps mz, mh, mw;
+    GemmMaps mz, mg;
     if (!make_map_bf16_2d(&mz.a, gathered, hidden_dim, L.rows, int64_t(hidden_dim) * 2, 128) ||
         !make_map_bf16_2d(&mz.b, wv, hidden_dim, nv, weight_pitch * 2, 128) ||
-        !make_map_bf16_2d(&mh.a, dz, nv, L.rows, L.piece * 2, 128) ||
-        !make_map_bf16_2d(&mh.b, wv, hidden_dim, nv, weight_pitch * 2, 64) ||
-        !make_map_bf16_2d(&mw.a, dz, nv, L.rows, L.piece * 2, 64) ||
-        !make_map_bf16_2d(&mw.b, gathered, hidden_dim, L.rows, int64_t(hidden_dim) * 2, 64))
+        !make_map_bf16_2d(&mg.a, dz, nv, L.rows, L.piece * 2, 128) ||
+        !make_map_bf16_2d(&mg.b, wv, hidden_dim, nv, weight_pitch * 2, 64) ||
+        !make_map_bf16_2d(&mg.a2, dz, nv, L.rows, L.piece * 2, 64) ||
+        !make_map_bf16_2d(&mg.b2, gathered, hidden_dim, L.rows, int64_t(hidden_dim) * 2, 64))
       return PSRL_ERR_CUDA;
     GemmParams z = base;
     z.M = M; z.N = static_cast<int32_t>(nv); z.k_blocks = (hidden_dim + kBK - 1) / kBK;
@@ -886,20 +979,23 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
     z.n_targets = static_cast<int32_t>(n_targets); z.col0 = static_cast<int32_t>(v0);
     z.out = dz; z.out_pitch = L.piece;
     e = launch_gemm<kDz>(mz, z, s);
-    if (e == cudaSuccess && d_hidden) {
-      GemmParams g = base;
-      g.M = M; g.N = hidden_dim; g.k_blocks = static_cast<int32_t>((nv + kBK - 1) / kBK);
-      g.out = static_cast<__nv_bfloat16*>(d_hidden); g.out_pitch = d_hidden_pitch;
-      g.acc = reinterpret_cast<float*>(ws + L.acc); g.acc_pitch = round_up(hidden_dim, 32);
-      g.first = v0 == 0; g.last = v0 + nv >= vocab;
-      e = launch_gemm<kDh>(mh, g, s);
-    }
-    if (e == cudaSuccess && d_weight) {
-      GemmParams g = base;
-      g.M = static_cast<int32_t>(nv); g.N = hidden_dim; g.k_blocks = static_cast<int32_t>((n_rows + kBK - 1) / kBK);
-      g.out = static_cast<__nv_bfloat16*>(d_weight) + v0 * d_weight_pitch; g.out_pitch = d_weight_pitch;
-      e = launch_gemm<kDw>(mw, g, s);
-    }
+    if (e != cudaSuccess) return cuda_failed(e);
+    GemmParams g = base;
+    g.M = M; g.N = hidden_dim; g.vocab = static_cast<int32_t>(nv);
+    g.out = static_cast<__nv_bfloat16*>(d_hidden); g.out_pitch = d_hidden_pitch;
+    if (d_weight) g.out2 = static_cast<__nv_bfloat16*>(d_weight) + v0 * d_weight_pitch;
+    g.out2_pitch = d_weight_pitch;
+    g.splits = L.splits;
+    g.acc = acc; g.acc_pitch = acc_pitch; g.acc_rows = n_rows;
+    g.first = v0 == 0; g.last = v0 + nv >= vocab;
+    e = launch_gemm<kGrad>(mg, g, s);
+    if (e != cudaSuccess) return cuda_failed(e);
+  }
+  if (d_hidden && L.splits > 1) {
+    sum_kernel<<<unsigned(n_rows), 256, 0, s>>>(reinterpret_cast<const float4*>(acc), L.splits, n_rows * acc_pitch / 4,
+                                                static_cast<int>(acc_pitch / 4), hidden_dim / 4, base.count, base.row_of,
+                                                static_cast<uint2*>(d_hidden), d_hidden_pitch / 4);
+    e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_failed(e);
   }
   return PSRL_OK;
