@@ -4,14 +4,14 @@
 // All four contractions (logits, logits again in the backward, d_hidden, d_weight) run on one matrix kernel:
 //   tile 256 x 256 of a CTA pair (cta_group::2: each CTA holds 128 rows of A and 128 of the 256 columns of B, so a
 //   64-deep step brings 32 KB into each SM for 512 tensor cycles; a lone CTA with a 128 x 256 tile would need 48 KB),
-//   six 32 KB stages filled by TMA, two 256-column accumulators in tensor memory so that the epilogue of one tile
+//   five or six 32 KB stages filled by TMA, two 256-column accumulators in tensor memory so that the epilogue of one tile
 //   runs under the products of the next, persistent CTAs.
 // What differs is how the operands lie (K-major or MN-major in shared memory) and the epilogue:
 //   kLse   running maximum and sum of exponentials of a row over a run of vocabulary tiles   -> partial (max, sum)
 //   kDz    dz = -scale G softmax, with the entries of the row's targets put in afterwards    -> bf16, one piece of the
 //          vocabulary at a time in the workspace (the softmax part is rounded to bf16 as the tensor cores need it)
-//   kGrad  both gradients of a piece in one launch: d_hidden += dz W, summed over the pieces in fp32 and rounded once at
-//          the end, and d_weight = dz^T hidden, the whole sum in tensor memory, rounded once.  The few deep tiles of
+//   kGrad  both gradients of a piece in one launch: d_hidden += dz W, added to fp32 sums over the pieces by the TMA unit and
+//          rounded once at the end, and d_weight = dz^T hidden, the whole sum in tensor memory, rounded once.  The few deep tiles of
 //          d_hidden come first, the many shallow ones of d_weight even out what they leave (grad_work); with few rows the
 //          depth of d_hidden is split as well, into partial sums that a last kernel adds in order.
 // The pieces make dz as large as the caller's hidden states, not as the logits.
@@ -35,42 +35,46 @@ namespace {
 using namespace sm100;
 
 constexpr int kBK = 64;                      // K per stage
-constexpr int kStages = 6;
 constexpr int kOperandBytes = 128 * kBK * 2; // one CTA's share of A or B in a stage
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kGemmThreads = 6 * 32;         // warps 0-3 epilogue, 4 TMA, 5 MMA
-constexpr size_t kGemmSmem = size_t(kStages) * kStageBytes + 1024;
+constexpr int kOutBytes = 128 * 128;         // what an epilogue group stores at a time: 128 rows of 128 bytes
+// Two epilogue groups of four warps, each with one half of a tile's columns (a single group is one warp per scheduler, bound
+// by the latency of its instructions where tiles are shallow), a TMA warp, an MMA warp.
+constexpr int kGroups = 2, kEpilogueWarps = 4 * kGroups, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + 1;
+constexpr int kGemmThreads = (kEpilogueWarps + 2) * 32;
 constexpr int kMaxRun = 8;                   // vocabulary tiles whose maximum and sum stay in registers
 
 enum Kind { kLse, kDz, kGrad };
 
+// 32 KB stages of operands; the kinds that store tiles give one of them to their output buffers, two per group
+constexpr int stages(Kind k) { return k == kLse ? 6 : 5; }
+constexpr size_t gemm_smem(Kind k) { return size_t(stages(k)) * kStageBytes + (k == kLse ? 0 : size_t(kGroups) * 2 * kOutBytes) + 1024; }
+
 struct GemmMaps {
   CUtensorMap a, b;     // kGrad: of d_hidden
   CUtensorMap a2, b2;   // kGrad: of d_weight
+  CUtensorMap out;      // kDz: dz; kGrad: the fp32 sums of d_hidden.  Boxes of 128 rows
+  CUtensorMap out2;     // kGrad: the piece's rows of d_weight
 };
 
 struct GemmParams {
   int32_t M, N;                 // valid rows and columns of the product
   int32_t n_tiles, k_blocks;
   const int32_t* count;         // kDz, kGrad: rows that matter, on the device (kLse: NULL, all M)
-  const int32_t* row_of;        // kDz, kGrad: the caller's row of a gathered row
+  const int32_t* row_of;        // kDz: the caller's row of a gathered row
   int32_t run;                  // kLse: consecutive column tiles of one work unit
   float scale_log2;             // logits in powers of two: scale * log2(e)
-  float2* part;                 // kLse: [unit column][M] (max, sum), powers of two
+  float2* part;                 // kLse: [unit column][group][M] (max, sum), powers of two
   const float2* row_info;       // kDz: per row (lse * log2(e), -scale * G)
   const int32_t* targets;       // kDz
   const int32_t* target_off;    // kDz: may be NULL (one target per row)
   const float* entry;           // kDz: value of dz at every target
   int32_t n_targets, col0;      // kDz: col0 = first vocabulary entry of the piece
-  __nv_bfloat16* out;           // kDz: dz; kGrad: d_hidden, or NULL
-  int64_t out_pitch;
-  __nv_bfloat16* out2;          // kGrad: the piece's rows of d_weight, or NULL
-  int64_t out2_pitch;
   int32_t vocab;                // kGrad: entries of the piece
   int32_t splits;               // kGrad: parts of d_hidden's sum over them
-  float* acc;                   // kGrad: fp32 sums of d_hidden over the pieces, [splits][acc_rows][acc_pitch]
-  int64_t acc_pitch, acc_rows;
-  int32_t first, last;          // kGrad: first / last piece
+  int32_t acc_rows;             // kGrad: rows of one part's sums
+  int32_t want_hidden, want_weight;   // kGrad
+  int32_t first;                // kGrad: the first piece: the sums are stored, later they are added to
   int* status;
 };
 
@@ -115,15 +119,16 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
       "h"(uint16_t(3))
       : "memory");
 }
-__device__ __forceinline__ void st_global_32B(void* p, const uint32_t (&r)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
-               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+// A box from shared memory to a tiled tensor map, or added to what is there (fp32).  Parts outside the tensor are dropped.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* smem_src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(reinterpret_cast<uint64_t>(m)),
+               "r"(smem_u32(smem_src)), "r"(x), "r"(y)
                : "memory");
 }
-__device__ __forceinline__ void ld_global_32B(const void* p, float (&r)[8]) {
-  asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7])
-               : "l"(p)
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap* m, const void* smem_src, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                   reinterpret_cast<uint64_t>(m)),
+               "r"(smem_u32(smem_src)), "r"(x), "r"(y)
                : "memory");
 }
 
@@ -153,56 +158,101 @@ struct GradWork {
 };
 // Pair c of C takes the units c, c + C, ... of d_hidden.  The first r pairs then have one more than the others, who make up
 // for it with the first tiles of d_weight; the rest of those go round.  No counter, no order that could vary.
-__device__ __forceinline__ bool grad_work(const GemmParams& p, int rows, int c, int C, int i, GradWork& w) {
-  const int m_tiles = p.out ? (rows + 255) / 256 : 0, v_tiles = p.out2 ? (p.vocab + 255) / 256 : 0;
-  const int per = m_tiles * p.n_tiles, n_hidden = per * p.splits;
-  const int steps = (p.vocab + kBK - 1) / kBK, row_steps = (rows + kBK - 1) / kBK;
-  const int u = c + i * C;
-  if (u < n_hidden) {
-    w.weight = 0;
-    w.split = u / per;
-    unit_tile(m_tiles, u - w.split * per, p.n_tiles, w.mt, w.nt);
-    w.kb0 = int(int64_t(steps) * w.split / p.splits);
-    w.kb1 = int(int64_t(steps) * (w.split + 1) / p.splits);
+struct GradPlan {
+  int m_tiles, v_tiles, per, n_hidden, mine, n_weight, ahead, light, steps, row_steps;
+  bool lighter;
+
+  __device__ __forceinline__ GradPlan(const GemmParams& p, int rows, int c, int C) {
+    m_tiles = p.want_hidden ? (rows + 255) / 256 : 0;
+    v_tiles = p.want_weight ? (p.vocab + 255) / 256 : 0;
+    per = m_tiles * p.n_tiles;
+    n_hidden = per * p.splits;
+    steps = (p.vocab + kBK - 1) / kBK;
+    row_steps = (rows + kBK - 1) / kBK;
+    const int q = n_hidden / C, r = n_hidden - q * C;
+    mine = q + (c < r ? 1 : 0);
+    n_weight = v_tiles * p.n_tiles;
+    light = C - r;
+    lighter = c >= r;
+    // cost of a unit in steps; a tile of few steps is bound by its epilogue, worth about six
+    ahead = r > 0 ? min((steps / p.splits + 6) / max(row_steps, 6), n_weight / light) : 0;
+  }
+  __device__ __forceinline__ bool get(const GemmParams& p, int c, int C, int i, GradWork& w) const {
+    if (i < mine) {
+      const int u = c + i * C;
+      w.weight = 0;
+      w.split = u / per;
+      unit_tile(m_tiles, u - w.split * per, p.n_tiles, w.mt, w.nt);
+      w.kb0 = part_of(steps, w.split, p.splits);
+      w.kb1 = part_of(steps, w.split + 1, p.splits);
+      return true;
+    }
+    const int j = i - mine;
+    int at = ahead * light;
+    if (lighter && j < ahead) at = j * light + c - (C - light);
+    else at += (lighter ? j - ahead : j) * C + c;
+    if (at >= n_weight) return false;
+    w.weight = 1;
+    w.split = 0;
+    w.kb0 = 0;
+    w.kb1 = row_steps;
+    unit_tile(v_tiles, at, p.n_tiles, w.mt, w.nt);
     return true;
   }
-  const int q = n_hidden / C, r = n_hidden - q * C, n_weight = v_tiles * p.n_tiles;
-  const int j = i - q - (c < r ? 1 : 0), light = C - r;
-  int ahead = 0;
-  // cost of a unit in steps; a tile of few steps is bound by its epilogue, worth about eight
-  if (r > 0) ahead = min((steps / p.splits + 8) / max(row_steps, 8), n_weight / light);
-  int at = ahead * light;
-  if (c >= r && j < ahead) at = j * light + c - r;
-  else at += (c >= r ? j - ahead : j) * C + c;
-  if (at >= n_weight) return false;
-  w.weight = 1;
-  w.split = 0;
-  w.kb0 = 0;
-  w.kb1 = row_steps;
-  unit_tile(v_tiles, at, p.n_tiles, w.mt, w.nt);
-  return true;
-}
+  // where part k of n begins; n <= 16 parts of fewer than 2^25 steps
+  __device__ __forceinline__ static int part_of(int steps, int k, int n) { return int(unsigned(steps) * unsigned(k) / unsigned(n)); }
+};
 
+template <int kStages>
 struct __align__(8) PairBarriers {
   uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
 };
 
-// Sixteen fp32 results to bf16, 32 bytes.
-__device__ __forceinline__ void store_bf16x16(__nv_bfloat16* dst, const float* v) {
-  uint32_t o[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) o[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-  st_global_32B(dst, o);
-}
+// How results leave: the CTA's 128 rows, 128 bytes of each at a time, through two buffers in shared memory (the 128-byte
+// swizzle of the tensor map makes the row-per-thread writes free of bank conflicts) and one TMA store per buffer.  With 32
+// bytes per thread and row straight to global memory, or a store for each warp's 32 rows, d_weight of 64 rows (1.07 GB) took
+// 335 us: the first is bound by scattered sectors, the second by the TMA unit's time per box.
+// The four warps of a group take every step together; the named barrier is theirs.
+constexpr uint32_t kBarOut = 1, kOutThreads = 128;   // barrier 1 + group
+struct TileOut {
+  uint8_t* buf;      // two times kOutBytes
+  uint32_t bar;
+  int row;           // the thread's row of the tile
+  uint32_t n = 0;    // stores so far
+
+  // the buffer to write to next: once the store before last has been read out
+  __device__ __forceinline__ uint8_t* next() {
+    if (n >= 2 && row == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    named_sync(bar, kOutThreads);
+    return buf + (n & 1) * kOutBytes;
+  }
+  __device__ __forceinline__ void put(uint8_t* b, int chunk, uint4 v) const {
+    *reinterpret_cast<uint4*>(b + row * 128 + ((chunk ^ (row & 7)) << 4)) = v;
+  }
+  __device__ __forceinline__ void send(const CUtensorMap* m, int x, int y, bool add) {
+    fence_proxy_async();
+    named_sync(bar, kOutThreads);
+    if (row == 0) {
+      if (add) tma_add_2d(m, buf + (n & 1) * kOutBytes, x, y);
+      else tma_store_2d(m, buf + (n & 1) * kOutBytes, x, y);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    ++n;
+  }
+  __device__ __forceinline__ void finish() {
+    if (row == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+};
 
 template <Kind kKind>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  __shared__ PairBarriers bar;
+  constexpr int kStages = stages(kKind);
+  __shared__ PairBarriers<kStages> bar;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort;
+  __shared__ int s_abort, s_go[kGroups][2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank();
   const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
@@ -210,10 +260,12 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   const int rows = kKind == kLse ? p.M : *p.count;
   const int m_tiles = (rows + 255) / 256;
 
+  const GradPlan plan(p, rows, cluster, n_clusters);   // kGrad
+
   // The i-th work unit of this pair: a row tile and consecutive column tiles, all over steps kb0 .. kb1.
   auto work = [&](int i, GradWork& w, int& nt_end) -> bool {
     if constexpr (kKind == kGrad) {
-      if (!grad_work(p, rows, cluster, n_clusters, i, w)) return false;
+      if (!plan.get(p, cluster, n_clusters, i, w)) return false;
       nt_end = w.nt + 1;
     } else {
       const int unit = cluster + i * n_clusters;
@@ -233,10 +285,10 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   if (tid == 0) {
     s_abort = 0;
     for (int i = 0; i < kStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&bar.acc_full[i], 1); mbar_init(&bar.acc_empty[i], 8); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar.acc_full[i], 1); mbar_init(&bar.acc_empty[i], 2 * kEpilogueWarps); }
     fence_mbar_init();
   }
-  if (warp == 5) {
+  if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
@@ -249,7 +301,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   GradWork w;
   int nt_end;
 
-  if (warp == 4) {
+  if (warp == kTmaWarp) {
     // ======================= TMA producer (both CTAs) =======================
     if (lane == 0) {
       tma_prefetch_desc(&maps.a);
@@ -292,7 +344,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
         if (uses > 0) ok = mbar_wait(&bar.empty[i], (uses + 1) & 1, abortp, p.status);
       }
     }
-  } else if (warp == 5) {
+  } else if (warp == kMmaWarp) {
     // ======================= MMA issuer (first CTA of the pair) =======================
     if (rank == 0) {
       // Operands: hidden, weight and dz with the depth contiguous (K-major) in the logits; in the gradients both lie with
@@ -333,139 +385,125 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
       }
     }
   } else {
-    // ======================= epilogue: one thread per row =======================
-    const uint32_t lane_addr = tmem + (uint32_t(warp) << 21);   // lane 32 * warp
+    // ======================= epilogue: one thread per row and half of the columns =======================
+    const int group = warp >> 2, gt = tid & 127;
+    const uint32_t bar_id = kBarOut + group;
+    const uint32_t lane_addr = tmem + (uint32_t(warp & 3) << 21) + group * 128;   // lane 32 * (warp % 4)
     const uint32_t empty0 = in_leader(&bar.acc_empty[0]), empty1 = in_leader(&bar.acc_empty[1]);
+    TileOut out;
+    out.buf = smem + kStages * kStageBytes + group * 2 * kOutBytes;
+    out.bar = bar_id;
+    out.row = gt;
     uint32_t tile = 0;
     bool ok = true;
     for (int i = 0; ok && work(i, w, nt_end); ++i) {
-      const int row = w.mt * 256 + int(rank) * 128 + warp * 32 + lane;
-      const bool live = row < (kKind == kGrad && w.weight ? p.vocab : rows);
+      const int row0 = w.mt * 256 + int(rank) * 128, row = row0 + gt;
+      const bool live = row < rows;
       float best = -CUDART_INF_F, sum = 0.f;                       // kLse
       float lse2 = 0.f, coef = 0.f;                                // kDz
-      int t_begin = 0, t_end = 0;
-      // dz is read in steps of kBK rows by the product for d_weight: the rows behind the last one of a step are zero
-      const bool pad = kKind == kDz && !live && row < (rows + kBK - 1) / kBK * kBK;
+      int t_begin = 0, t_end = 0, first_target = -1;
       if (kKind == kDz && live) {
         const int user_row = p.row_of[row];
         const float2 ri = p.row_info[user_row];
         lse2 = ri.x; coef = ri.y;
         target_range(p.target_off, user_row, p.n_targets, t_begin, t_end);
-      }
-      // kGrad: where the row goes as bf16, or the fp32 sums that it is added to
-      __nv_bfloat16* out_row = nullptr;
-      float* acc_row = nullptr;
-      if (kKind == kGrad && live) {
-        if (w.weight) out_row = p.out2 + int64_t(row) * p.out2_pitch;
-        else {
-          if (p.last && p.splits == 1) out_row = p.out + int64_t(p.row_of[row]) * p.out_pitch;
-          if (!out_row || !p.first) acc_row = p.acc + (int64_t(w.split) * p.acc_rows + row) * p.acc_pitch;
-        }
+        if (t_begin < t_end) first_target = p.targets[t_begin];
       }
       for (int nt = w.nt; nt < nt_end; ++nt, ++tile) {
         const uint32_t a = tile & 1;
-        ok = __all_sync(0xffffffffu, mbar_wait(&bar.acc_full[a], (tile >> 1) & 1, abortp, p.status));
+        // one warp waits for its group: the four leave together if the wait gives up, so none is missed at their barrier
+        if ((warp & 3) == 0) {
+          ok = mbar_wait(&bar.acc_full[a], (tile >> 1) & 1, abortp, p.status);
+          if (lane == 0) s_go[group][a] = ok;
+        }
+        named_sync(bar_id, kOutThreads);
+        ok = s_go[group][a];
         if (!ok) break;
         tc_fence_after();
-        const int n0 = nt * 256;
+        const int n0 = nt * 256 + group * 128;
 #pragma unroll 1
-        for (int c = 0; c < 8; ++c) {
-          const int col = n0 + c * 32;
-          if (col >= p.N) break;   // warp-uniform
-          uint32_t r[32];
-          tmem_ld32(lane_addr + a * 256 + c * 32, r);
+        for (int c = 0; c < 2; ++c) {
+          const int col = n0 + c * 64;
+          if (col >= p.N) break;   // uniform in the group
+          uint32_t r[2][32];
+          tmem_ld32(lane_addr + a * 256 + c * 64, r[0]);
+          tmem_ld32(lane_addr + a * 256 + c * 64 + 32, r[1]);
           tmem_wait_ld();
           if constexpr (kKind == kLse) {
-            float top = -CUDART_INF_F;
-            if (col + 32 > p.N) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (col + i >= p.N) r[i] = __float_as_uint(p.scale_log2 > 0.f ? -CUDART_INF_F : CUDART_INF_F);
+            for (int h = 0; h < 2; ++h) {
+              if (col + 32 * h + 32 > p.N) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (col + 32 * h + i >= p.N) r[h][i] = __float_as_uint(p.scale_log2 > 0.f ? -CUDART_INF_F : CUDART_INF_F);
+              }
+              float top = -CUDART_INF_F;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float z = __uint_as_float(r[h][i]) * p.scale_log2;
+                r[h][i] = __float_as_uint(z);
+                top = fmaxf(top, z);
+              }
+              if (top > best) { sum *= ex2(best - top); best = top; }
+              const float ref = best == -CUDART_INF_F ? 0.f : best;   // nothing finite yet: every term is zero
+              float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+              for (int i = 0; i < 32; i += 2) {
+                s0 += ex2(__uint_as_float(r[h][i]) - ref);
+                s1 += ex2(__uint_as_float(r[h][i + 1]) - ref);
+              }
+              sum += s0 + s1;
             }
+          } else if (kKind == kGrad && !w.weight) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float z = __uint_as_float(r[i]) * p.scale_log2;
-              r[i] = __float_as_uint(z);
-              top = fmaxf(top, z);
-            }
-            if (top > best) { sum *= ex2(best - top); best = top; }
-            const float ref = best == -CUDART_INF_F ? 0.f : best;   // nothing finite yet: every term is zero
-            float s0 = 0.f, s1 = 0.f;
+            for (int h = 0; h < 2; ++h) {
+              if (col + 32 * h >= p.N) break;
+              uint8_t* b = out.next();
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              s0 += ex2(__uint_as_float(r[i]) - ref);
-              s1 += ex2(__uint_as_float(r[i + 1]) - ref);
-            }
-            sum += s0 + s1;
-          } else if constexpr (kKind == kDz) {
-            float v[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = coef * ex2(fmaf(__uint_as_float(r[i]), p.scale_log2, -lse2));
-            if (col + 32 > p.N) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (col + i >= p.N) v[i] = 0.f;
-            }
-            if (pad) {
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = 0.f;
-            }
-            if (live || pad) {
-              __nv_bfloat16* o = p.out + int64_t(row) * p.out_pitch + col;
-              store_bf16x16(o, v);
-              store_bf16x16(o + 16, v + 16);
+              for (int j = 0; j < 8; ++j)
+                out.put(b, j, w.kb1 > w.kb0 ? make_uint4(r[h][4 * j], r[h][4 * j + 1], r[h][4 * j + 2], r[h][4 * j + 3])
+                                            : make_uint4(0, 0, 0, 0));   // an empty sum writes no accumulator
+              // the parts' sums follow one another; rows behind the last one are sums nobody reads, but not another part's
+              if (row0 < p.acc_rows) out.send(&maps.out, col + 32 * h, w.split * p.acc_rows + row0, !p.first);
             }
           } else {
-            float v[32];
+            uint8_t* b = out.next();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = w.kb1 > w.kb0 ? __uint_as_float(r[i]) : 0.f;   // an empty sum writes no accumulator
-            if (acc_row && !p.first) {
+            for (int j = 0; j < 8; ++j) {
+              uint32_t o[4];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                float old[8];
-                ld_global_32B(acc_row + col + 8 * j, old);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[8 * j + i] += old[i];
+              for (int i = 0; i < 4; ++i) {
+                float lo = __uint_as_float(r[j / 4][j % 4 * 8 + 2 * i]), hi = __uint_as_float(r[j / 4][j % 4 * 8 + 2 * i + 1]);
+                if constexpr (kKind == kDz) {
+                  lo = coef * ex2(fmaf(lo, p.scale_log2, -lse2));
+                  hi = coef * ex2(fmaf(hi, p.scale_log2, -lse2));
+                }
+                o[i] = pack_bf16(lo, hi);
+              }
+              // kDz: rows behind the last one are zero, as the product for d_weight reads dz in steps of kBK rows
+              const bool any = kKind == kDz ? live : w.kb1 > w.kb0;
+              out.put(b, j, any ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(0, 0, 0, 0));
+            }
+            if constexpr (kKind == kDz) {
+              // the row's targets inside these columns, over what this thread has just written
+              for (int t = t_begin; t < t_end; ++t) {
+                const uint32_t x = uint32_t(t == t_begin ? first_target : p.targets[t]) - uint32_t(p.col0 + col);
+                if (x < uint32_t(min(64, p.N - col)))
+                  *reinterpret_cast<__nv_bfloat16*>(b + gt * 128 + (((x >> 3) ^ (gt & 7)) << 4) + (x & 7) * 2) =
+                      __float2bfloat16_rn(p.entry[t]);
               }
             }
-            if (out_row) {
-              // the caller's rows are 16-byte aligned, and the last columns may be fewer than 32
-              if (col + 32 <= p.N && (reinterpret_cast<uintptr_t>(out_row) & 31) == 0) {
-                store_bf16x16(out_row + col, v);
-                store_bf16x16(out_row + col + 16, v + 16);
-              } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                  if (col + 8 * j < p.N)
-                    *reinterpret_cast<uint4*>(out_row + col + 8 * j) =
-                        make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
-                                   pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
-              }
-            } else if (acc_row) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                uint32_t o[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(v[8 * j + i]);
-                st_global_32B(acc_row + col + 8 * j, o);
-              }
-            }
+            out.send(kKind == kGrad ? &maps.out2 : &maps.out, col, row0, false);
           }
         }
         // the accumulator may be overwritten
         tc_fence_before();
         __syncwarp();
         if (lane == 0) arrive_leader(a ? empty1 : empty0);
-        if (kKind == kDz) {
-          // the row's targets inside this tile, over what this thread has just stored there
-          for (int t = t_begin; t < t_end; ++t) {
-            const int x = p.targets[t] - p.col0;
-            if (x >= n0 && x < min(n0 + 256, p.N)) p.out[int64_t(row) * p.out_pitch + x] = __float2bfloat16_rn(p.entry[t]);
-          }
-        }
       }
-      if (kKind == kLse && ok && live) p.part[int64_t(w.split) * rows + row] = make_float2(best, sum);
+      if (kKind == kLse && ok && live) p.part[(int64_t(w.split) * kGroups + group) * rows + row] = make_float2(best, sum);
     }
+    if (kKind != kLse) out.finish();
   }
   // ---- teardown ----
   __syncthreads();
@@ -475,7 +513,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   }
   tc_fence_before();
   cluster_sync();
-  if (warp == 5) {
+  if (warp == kMmaWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
@@ -698,47 +736,42 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int voca
 __global__ void __launch_bounds__(256) sum_kernel(const float4* __restrict__ acc, int splits, int64_t split_vecs, int pitch_vecs, int vecs,
                                                   const int32_t* __restrict__ count, const int32_t* __restrict__ row_of,
                                                   uint2* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
-  const int row = blockIdx.x;
-  if (row >= *count) return;
-  const int64_t to = row_of[row] * dh_pitch_vecs;
-  for (int i = threadIdx.x; i < vecs; i += 256) {
-    float4 s = acc[int64_t(row) * pitch_vecs + i];
-    for (int k = 1; k < splits; ++k) {
-      const float4 x = acc[k * split_vecs + int64_t(row) * pitch_vecs + i];
-      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
-    }
-    d_hidden[to + i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+  const int row = blockIdx.x, i = blockIdx.y * 256 + threadIdx.x;
+  if (row >= *count || i >= vecs) return;
+  acc += int64_t(row) * pitch_vecs + i;
+  float4 s = acc[0];
+#pragma unroll 4
+  for (int k = 1; k < splits; ++k) {
+    const float4 x = acc[k * split_vecs];
+    s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
   }
+  d_hidden[row_of[row] * dh_pitch_vecs + i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
 }
 
-// Gathers the hidden states of the rows that matter, in order, and zeroes the others' d_hidden.  A block takes 32 rows and
-// counts the rows before them itself: one bit per row is little to read.
-constexpr int kGatherRows = 32;
-__global__ void __launch_bounds__(256) gather_kernel(int M, const uint8_t* __restrict__ matters, const uint4* __restrict__ hidden,
-                                                     int64_t h_pitch_vecs, int vecs, uint4* __restrict__ gathered,
-                                                     int32_t* __restrict__ row_of, int32_t* __restrict__ count,
-                                                     uint4* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
+// Gathers the hidden states of the rows that matter, in order, and zeroes the others' d_hidden.  A warp per row; a block
+// counts the rows before its own itself: one bit per row is little to read.
+__global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, const uint8_t* __restrict__ matters, const uint4* __restrict__ hidden,
+                                                                   int64_t h_pitch_vecs, int vecs, uint4* __restrict__ gathered,
+                                                                   int32_t* __restrict__ row_of, int32_t* __restrict__ count,
+                                                                   uint4* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
   __shared__ int s_before;
   if (threadIdx.x == 0) s_before = 0;
   __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int byte0 = blockIdx.x * (kGatherRows / 8), n_bytes = (M + 7) / 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, byte = blockIdx.x;
   int before = 0;
   const uint32_t* words = reinterpret_cast<const uint32_t*>(matters);
-  for (int i = threadIdx.x; i < byte0 / 4; i += 256) before += __popc(words[i]);
+  for (int i = threadIdx.x; i <= byte / 4; i += kRowsPerByte * 32)
+    before += __popc(words[i] & (i < byte / 4 ? ~0u : (1u << byte % 4 * 8) - 1));
   before = __reduce_add_sync(0xffffffffu, before);
   if (lane == 0 && before) atomicAdd(&s_before, before);
   __syncthreads();
-  uint32_t bits = 0;
-  for (int i = 0; i < kGatherRows / 8; ++i)
-    if (byte0 + i < n_bytes) bits |= uint32_t(matters[byte0 + i]) << (8 * i);
-  const int at0 = s_before;
-  for (int r = warp; r < kGatherRows; r += 8) {
-    const int row = blockIdx.x * kGatherRows + r;
-    if (row >= M) break;
-    if (bits >> r & 1) {
-      const int at = at0 + __popc(bits & ((1u << r) - 1));
+  const uint32_t bits = matters[byte];
+  const int at0 = s_before, row = byte * kRowsPerByte + warp;
+  if (row < M) {
+    if (bits >> warp & 1) {
+      const int at = at0 + __popc(bits & ((1u << warp) - 1));
       if (lane == 0) row_of[at] = row;
+#pragma unroll 8
       for (int i = lane; i < vecs; i += 32) gathered[int64_t(at) * vecs + i] = hidden[row * h_pitch_vecs + i];
     } else if (d_hidden) {
       for (int i = lane; i < vecs; i += 32) d_hidden[row * dh_pitch_vecs + i] = make_uint4(0, 0, 0, 0);
@@ -749,7 +782,7 @@ __global__ void __launch_bounds__(256) gather_kernel(int M, const uint8_t* __res
     if (threadIdx.x == 0) *count = n;
     // the rows behind the last one, up to a whole step of the product that sums over rows
     const int64_t end = int64_t((n + kBK - 1) / kBK * kBK) * vecs;
-    for (int64_t i = int64_t(n) * vecs + threadIdx.x; i < end; i += 256) gathered[i] = make_uint4(0, 0, 0, 0);
+    for (int64_t i = int64_t(n) * vecs + threadIdx.x; i < end; i += kRowsPerByte * 32) gathered[i] = make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -757,14 +790,16 @@ __global__ void __launch_bounds__(256) gather_kernel(int M, const uint8_t* __res
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-constexpr int kFewRows = 8;       // up to here the forward takes few_rows_kernel
+// Up to kFewRows rows the forward takes few_rows_kernel: 1, 2, 4 rows of 4096 x 131072 weights 191, 221, 203 us, all of
+// them 206 us by the matrix kernel, whose sums are less exact; with 8 rows it is 415 us (fp32 arithmetic) against 206.
+constexpr int kFewRows = 4;
 constexpr int kFewBlocks = 1184;  // its blocks at most: eight per SM
 
 struct Layout {
   int32_t n_tiles, run, n_parts;
   int32_t few;                   // rows that few_rows_kernel is built for, 0: the matrix kernel
   int64_t piece;                 // vocabulary entries of one piece of the backward
-  int64_t rows;                  // rows that the backward's gathered buffers hold
+  int64_t rows, acc_rows;        // rows that the backward's gathered buffers and the sums of d_hidden hold
   int32_t splits;                // parts of d_hidden's sums
   size_t part, row_info, entry, matters, row_of, count, gathered, dz, acc, total;
 };
@@ -779,11 +814,12 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
     // short runs while there are few tiles (they balance the pairs of CTAs), long ones to keep the partials small
     const int64_t tiles = m_tiles * L.n_tiles;
     L.run = static_cast<int32_t>(std::min<int64_t>(kMaxRun, std::max<int64_t>(1, tiles / (74 * 16))));
-    L.n_parts = (L.n_tiles + L.run - 1) / L.run;
+    L.n_parts = (L.n_tiles + L.run - 1) / L.run * kGroups;
     if (n <= kFewRows) {
       for (L.few = 1; L.few < n;) L.few *= 2;
       if (size_t(L.few) * h * 2 > kFewSmem) L.few = 0;
-      else L.n_parts = static_cast<int32_t>(std::min<int64_t>(kFewBlocks, (v + kFewThreads / 32 * kFewV - 1) / (kFewThreads / 32 * kFewV)));
+      const int64_t per_block = kFewThreads / 32 * kFewV;
+      if (L.few) L.n_parts = static_cast<int32_t>(std::min<int64_t>(kFewBlocks, (v + per_block - 1) / per_block));
     }
     L.part = take(size_t(L.n_parts) * n * sizeof(float2));
   } else {
@@ -795,7 +831,8 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
     L.row_info = take(size_t(n) * sizeof(float2));
     L.entry = take(size_t(n_targets) * sizeof(float));
     L.rows = round_up(n, kBK);
-    L.matters = take(size_t(n + 7) / 8);
+    L.acc_rows = round_up(n, 128);
+    L.matters = take(size_t(n + 7) / 8 + 3);
     L.row_of = take(size_t(n) * sizeof(int32_t));
     L.count = take(sizeof(int32_t));
     L.gathered = take(size_t(L.rows) * h * 2);
@@ -804,7 +841,7 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
     // piece; four units for every pair, of at least 16 steps, share that out.
     const int64_t tiles = m_tiles * ((h + 255) / 256), most = std::min<int64_t>(16, L.piece / kBK / 16);
     L.splits = tiles >= 148 ? 1 : static_cast<int32_t>(std::max<int64_t>(1, std::min(most, (296 + tiles - 1) / tiles)));
-    L.acc = take(L.piece < v || L.splits > 1 ? size_t(L.splits) * n * round_up(h, 32) * sizeof(float) : 0);
+    L.acc = take(size_t(L.splits) * L.acc_rows * round_up(h, 32) * sizeof(float));
   }
   L.total = at;
   return L;
@@ -813,7 +850,7 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
 template <Kind kKind>
 cudaError_t launch_gemm(const GemmMaps& maps, GemmParams& p, cudaStream_t stream) {
   static bool done[64] = {};
-  cudaError_t e = ensure_dynamic_smem(gemm_kernel<kKind>, kGemmSmem, done);
+  cudaError_t e = ensure_dynamic_smem(gemm_kernel<kKind>, gemm_smem(kKind), done);
   if (e != cudaSuccess) return e;
   p.n_tiles = (p.N + 255) / 256;
   if (p.run < 1) p.run = 1;
@@ -821,7 +858,7 @@ cudaError_t launch_gemm(const GemmMaps& maps, GemmParams& p, cudaStream_t stream
   if (kKind == kGrad) units = units * p.splits + (int64_t(p.vocab) + 255) / 256 * p.n_tiles;
   if (units > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int clusters = static_cast<int>(std::min<int64_t>(units, resident_ctas() / 2));
-  gemm_kernel<kKind><<<2 * clusters, kGemmThreads, kGemmSmem, stream>>>(maps, p);
+  gemm_kernel<kKind><<<2 * clusters, kGemmThreads, gemm_smem(kKind), stream>>>(maps, p);
   return cudaGetLastError();
 }
 
@@ -890,8 +927,7 @@ psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t
   if (L.few) {
     e = L.few == 1 ? launch_few<1>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s)
       : L.few == 2 ? launch_few<2>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s)
-      : L.few == 4 ? launch_few<4>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s)
-                   : launch_few<8>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s);
+                   : launch_few<4>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s);
   } else {
     GemmMaps maps;
     if (!make_map_bf16_2d(&maps.a, hidden, hidden_dim, n_rows, hidden_pitch * 2, 128) ||
@@ -950,14 +986,14 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   float* acc = reinterpret_cast<float*>(ws + L.acc);
   const int64_t acc_pitch = round_up(hidden_dim, 32);
   const int32_t M = static_cast<int32_t>(n_rows);
-  rows_kernel<<<unsigned((n_rows + 7) / 8), 256, 0, s>>>(M, vocab, targets, target_off, static_cast<int>(n_targets), logprob, lse,
+  rows_kernel<<<unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte), kRowsPerByte * 32, 0, s>>>(M, vocab, targets, target_off, static_cast<int>(n_targets), logprob, lse,
                                                          d_logprob, scale, row_info, entry, reinterpret_cast<uint8_t*>(ws + L.matters));
   e = cudaGetLastError();
   if (e != cudaSuccess) return cuda_failed(e);
   __nv_bfloat16* gathered = reinterpret_cast<__nv_bfloat16*>(ws + L.gathered);
   base.count = reinterpret_cast<int32_t*>(ws + L.count);
   base.row_of = reinterpret_cast<int32_t*>(ws + L.row_of);
-  gather_kernel<<<unsigned((n_rows + kGatherRows - 1) / kGatherRows), 256, 0, s>>>(
+  gather_kernel<<<unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte), kRowsPerByte * 32, 0, s>>>(
       M, reinterpret_cast<uint8_t*>(ws + L.matters), static_cast<const uint4*>(hidden), hidden_pitch / 8, hidden_dim / 8,
       reinterpret_cast<uint4*>(gathered), reinterpret_cast<int32_t*>(ws + L.row_of), reinterpret_cast<int32_t*>(ws + L.count),
       static_cast<uint4*>(d_hidden), d_hidden_pitch / 8);
@@ -973,28 +1009,29 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
         !make_map_bf16_2d(&mg.a, dz, nv, L.rows, L.piece * 2, 128) ||
         !make_map_bf16_2d(&mg.b, wv, hidden_dim, nv, weight_pitch * 2, 64) ||
         !make_map_bf16_2d(&mg.a2, dz, nv, L.rows, L.piece * 2, 64) ||
-        !make_map_bf16_2d(&mg.b2, gathered, hidden_dim, L.rows, int64_t(hidden_dim) * 2, 64))
+        !make_map_bf16_2d(&mg.b2, gathered, hidden_dim, L.rows, int64_t(hidden_dim) * 2, 64) ||
+        !make_map_bf16_2d(&mz.out, dz, nv, L.rows, L.piece * 2, 128) ||
+        !make_map_f32_2d(&mg.out, acc, hidden_dim, L.splits * L.acc_rows, acc_pitch * 4, 128) ||
+        (d_weight && !make_map_bf16_2d(&mg.out2, static_cast<__nv_bfloat16*>(d_weight) + v0 * d_weight_pitch, hidden_dim, nv,
+                                       d_weight_pitch * 2, 128)))
       return PSRL_ERR_CUDA;
     GemmParams z = base;
     z.M = M; z.N = static_cast<int32_t>(nv); z.k_blocks = (hidden_dim + kBK - 1) / kBK;
     z.row_info = row_info; z.targets = targets; z.target_off = target_off; z.entry = entry;
     z.n_targets = static_cast<int32_t>(n_targets); z.col0 = static_cast<int32_t>(v0);
-    z.out = dz; z.out_pitch = L.piece;
     e = launch_gemm<kDz>(mz, z, s);
     if (e != cudaSuccess) return cuda_failed(e);
     GemmParams g = base;
     g.M = M; g.N = hidden_dim; g.vocab = static_cast<int32_t>(nv);
-    g.out = static_cast<__nv_bfloat16*>(d_hidden); g.out_pitch = d_hidden_pitch;
-    if (d_weight) g.out2 = static_cast<__nv_bfloat16*>(d_weight) + v0 * d_weight_pitch;
-    g.out2_pitch = d_weight_pitch;
+    g.want_hidden = d_hidden != nullptr; g.want_weight = d_weight != nullptr;
     g.splits = L.splits;
-    g.acc = acc; g.acc_pitch = acc_pitch; g.acc_rows = n_rows;
-    g.first = v0 == 0; g.last = v0 + nv >= vocab;
+    g.acc_rows = static_cast<int32_t>(L.acc_rows);
+    g.first = v0 == 0;
     e = launch_gemm<kGrad>(mg, g, s);
     if (e != cudaSuccess) return cuda_failed(e);
   }
-  if (d_hidden && L.splits > 1) {
-    sum_kernel<<<unsigned(n_rows), 256, 0, s>>>(reinterpret_cast<const float4*>(acc), L.splits, n_rows * acc_pitch / 4,
+  if (d_hidden) {
+    sum_kernel<<<dim3(unsigned(n_rows), unsigned((hidden_dim / 4 + 255) / 256)), 256, 0, s>>>(reinterpret_cast<const float4*>(acc), L.splits, L.acc_rows * acc_pitch / 4,
                                                 static_cast<int>(acc_pitch / 4), hidden_dim / 4, base.count, base.row_of,
                                                 static_cast<uint2*>(d_hidden), d_hidden_pitch / 4);
     e = cudaGetLastError();

@@ -30,8 +30,10 @@ struct MapKey {
   const void* base;
   uint64_t cols, rows, pitch;
   uint32_t box_rows;
+  CUtensorMapDataType type;
   bool operator==(const MapKey& o) const {
-    return base == o.base && cols == o.cols && rows == o.rows && pitch == o.pitch && box_rows == o.box_rows;
+    return base == o.base && cols == o.cols && rows == o.rows && pitch == o.pitch && box_rows == o.box_rows &&
+           type == o.type;
   }
 };
 struct MapSlot {
@@ -48,13 +50,13 @@ size_t map_hash(const MapKey& k) {
   h ^= (k.cols * 31 + k.pitch * 17 + k.box_rows) * 0x94D049BB133111EBull;
   return size_t((h >> 29) % kMapSlots);
 }
-}  // namespace
 
-bool make_map_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
-                      uint32_t box_rows) {
+// boxes are 128 bytes wide
+bool make_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t box_cols, const void* base, uint64_t cols, uint64_t rows,
+              uint64_t pitch_bytes, uint32_t box_rows) {
   std::call_once(g_once, resolve);
   if (!g_encode) return false;
-  const MapKey key{base, cols, rows, pitch_bytes, box_rows};
+  const MapKey key{base, cols, rows, pitch_bytes, box_rows, type};
   const size_t slot = map_hash(key);
   {
     std::lock_guard<std::mutex> lock(g_maps_mu);
@@ -65,9 +67,9 @@ bool make_map_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_
   }
   cuuint64_t dims[2] = {cols, rows};
   cuuint64_t strides[1] = {pitch_bytes};
-  cuuint32_t box[2] = {64, box_rows};
+  cuuint32_t box[2] = {box_cols, box_rows};
   cuuint32_t es[2] = {1, 1};
-  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, es,
+  CUresult r = g_encode(map, type, 2, const_cast<void*>(base), dims, strides, box, es,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
@@ -81,6 +83,16 @@ bool make_map_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_
     g_maps[slot].map = *map;
   }
   return true;
+}
+}  // namespace
+
+bool make_map_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
+                      uint32_t box_rows) {
+  return make_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 64, base, cols, rows, pitch_bytes, box_rows);
+}
+bool make_map_f32_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
+                     uint32_t box_rows) {
+  return make_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 32, base, cols, rows, pitch_bytes, box_rows);
 }
 
 }  // namespace psrl

@@ -13,4 +13,8 @@ namespace psrl {
 bool make_map_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
                       uint32_t box_rows);
 
+// The same for fp32, boxes of box_rows x 32 columns.
+bool make_map_f32_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
+                     uint32_t box_rows);
+
 }  // namespace psrl
