@@ -38,8 +38,9 @@ constexpr int kBK = 64;                      // K per stage
 constexpr int kOperandBytes = 128 * kBK * 2; // one CTA's share of A or B in a stage
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kOutBytes = 128 * 128;         // what an epilogue group stores at a time: 128 rows of 128 bytes
-// Two epilogue groups of four warps, each with one half of a tile's columns (a single group is one warp per scheduler, bound
-// by the latency of its instructions where tiles are shallow), a TMA warp, an MMA warp.
+// Two epilogue groups of four warps, one for each accumulator, so that where tiles are shallow the latencies of one tile's
+// way out (products, hand-over, stores) pass under the other's; a TMA warp, an MMA warp.  d_weight of 64 rows, 1.07 GB:
+// one group 335 us, two with half of every tile each 298, with every other tile each 218.
 constexpr int kGroups = 2, kEpilogueWarps = 4 * kGroups, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + 1;
 constexpr int kGemmThreads = (kEpilogueWarps + 2) * 32;
 constexpr int kMaxRun = 8;                   // vocabulary tiles whose maximum and sum stay in registers
@@ -285,7 +286,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   if (tid == 0) {
     s_abort = 0;
     for (int i = 0; i < kStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&bar.acc_full[i], 1); mbar_init(&bar.acc_empty[i], 2 * kEpilogueWarps); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar.acc_full[i], 1); mbar_init(&bar.acc_empty[i], 8); }   // four warps in either CTA
     fence_mbar_init();
   }
   if (warp == kMmaWarp) {
@@ -385,11 +386,11 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
       }
     }
   } else {
-    // ======================= epilogue: one thread per row and half of the columns =======================
+    // ======================= epilogue: one thread per row, a group for every other tile =======================
     const int group = warp >> 2, gt = tid & 127;
     const uint32_t bar_id = kBarOut + group;
-    const uint32_t lane_addr = tmem + (uint32_t(warp & 3) << 21) + group * 128;   // lane 32 * (warp % 4)
-    const uint32_t empty0 = in_leader(&bar.acc_empty[0]), empty1 = in_leader(&bar.acc_empty[1]);
+    const uint32_t lane_addr = tmem + (uint32_t(warp & 3) << 21) + group * 256;   // lane 32 * (warp % 4)
+    const uint32_t acc_empty = in_leader(&bar.acc_empty[group]);
     TileOut out;
     out.buf = smem + kStages * kStageBytes + group * 2 * kOutBytes;
     out.bar = bar_id;
@@ -410,24 +411,24 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
         if (t_begin < t_end) first_target = p.targets[t_begin];
       }
       for (int nt = w.nt; nt < nt_end; ++nt, ++tile) {
-        const uint32_t a = tile & 1;
+        if ((tile & 1) != uint32_t(group)) continue;
         // one warp waits for its group: the four leave together if the wait gives up, so none is missed at their barrier
         if ((warp & 3) == 0) {
-          ok = mbar_wait(&bar.acc_full[a], (tile >> 1) & 1, abortp, p.status);
-          if (lane == 0) s_go[group][a] = ok;
+          ok = mbar_wait(&bar.acc_full[group], (tile >> 1) & 1, abortp, p.status);
+          if (lane == 0) s_go[group][(tile >> 1) & 1] = ok;
         }
         named_sync(bar_id, kOutThreads);
-        ok = s_go[group][a];
+        ok = s_go[group][(tile >> 1) & 1];
         if (!ok) break;
         tc_fence_after();
-        const int n0 = nt * 256 + group * 128;
+        const int n0 = nt * 256;
 #pragma unroll 1
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < 4; ++c) {
           const int col = n0 + c * 64;
           if (col >= p.N) break;   // uniform in the group
           uint32_t r[2][32];
-          tmem_ld32(lane_addr + a * 256 + c * 64, r[0]);
-          tmem_ld32(lane_addr + a * 256 + c * 64 + 32, r[1]);
+          tmem_ld32(lane_addr + c * 64, r[0]);
+          tmem_ld32(lane_addr + c * 64 + 32, r[1]);
           tmem_wait_ld();
           if constexpr (kKind == kLse) {
 #pragma unroll
@@ -499,7 +500,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
         // the accumulator may be overwritten
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) arrive_leader(a ? empty1 : empty0);
+        if (lane == 0) arrive_leader(acc_empty);
       }
       if (kKind == kLse && ok && live) p.part[(int64_t(w.split) * kGroups + group) * rows + row] = make_float2(best, sum);
     }
