@@ -63,6 +63,7 @@ struct GemmParams {
   int32_t n_tiles, k_blocks;
   const int32_t* count;         // kDz, kGrad: rows that matter, on the device (kLse: NULL, all M)
   const int32_t* row_of;        // kDz: the caller's row of a gathered row
+  int32_t tile_n;               // columns of a tile: 256, or fewer in the logits (a multiple of 64)
   int32_t run;                  // kLse: consecutive column tiles of one work unit
   float scale_log2;             // logits in powers of two: scale * log2(e)
   float2* part;                 // kLse: [unit column][group][M] (max, sum), powers of two
@@ -78,6 +79,11 @@ struct GemmParams {
   int32_t first;                // kGrad: the first piece: the sums are stored, later they are added to
   int* status;
 };
+
+// The kernels of a call are launched so that each may start while the one before it runs out: what a kernel needs of the
+// call's earlier kernels it reads after previous_kernel_done().
+__device__ __forceinline__ void previous_kernel_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void next_kernel_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ------------------------------------------------------------------------------------------- pair-of-CTAs wrappers
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -258,6 +264,28 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   const uint32_t rank = cluster_rank();
   const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
   const int n_units = (p.n_tiles + p.run - 1) / p.run;
+  const int tile_n = kKind == kGrad ? 256 : p.tile_n;
+
+  if (tid == 0) {
+    s_abort = 0;
+    for (int i = 0; i < kStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar.acc_full[i], 1); mbar_init(&bar.acc_empty[i], 8); }   // four warps in either CTA
+    fence_mbar_init();
+    tma_prefetch_desc(&maps.a);
+    tma_prefetch_desc(&maps.b);
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();   // the peer's barriers exist before anything arrives on them
+  tc_fence_after();
+  previous_kernel_done();
+  next_kernel_may_start();
+  if (kKind == kLse && blockIdx.x == 0 && tid == 0) *p.status = int(PSRL_OK);
+
   const int rows = kKind == kLse ? p.M : *p.count;
   const int m_tiles = (rows + 255) / 256;
 
@@ -283,20 +311,6 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
     return true;
   };
 
-  if (tid == 0) {
-    s_abort = 0;
-    for (int i = 0; i < kStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(&bar.acc_full[i], 1); mbar_init(&bar.acc_empty[i], 8); }   // four warps in either CTA
-    fence_mbar_init();
-  }
-  if (warp == kMmaWarp) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-  }
-  tc_fence_before();
-  __syncthreads();
-  cluster_sync();   // the peer's barriers exist before anything arrives on them
-  tc_fence_after();
   const uint32_t tmem = s_tmem;
   volatile int* abortp = &s_abort;
   GradWork w;
@@ -305,8 +319,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
   if (warp == kTmaWarp) {
     // ======================= TMA producer (both CTAs) =======================
     if (lane == 0) {
-      tma_prefetch_desc(&maps.a);
-      tma_prefetch_desc(&maps.b);
+      const uint32_t stage_tx = 2 * (kOperandBytes + uint32_t(tile_n) * kBK);   // of both CTAs
       uint32_t it = 0;
       bool ok = true;
       for (int i = 0; ok && work(i, w, nt_end); ++i) {
@@ -315,12 +328,12 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
         const CUtensorMap* mb = a_mn ? &maps.b2 : &maps.b;
         const int m0 = w.mt * 256 + int(rank) * 128;
         for (int nt = w.nt; nt < nt_end && ok; ++nt) {
-          const int n0 = nt * 256 + int(rank) * 128;
+          const int n0 = nt * tile_n + int(rank) * (tile_n / 2);
           for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
             const uint32_t s = it % kStages, round = it / kStages;
             if (round > 0 && !mbar_wait(&bar.empty[s], (round + 1) & 1, abortp, p.status)) { ok = false; break; }
             // the second CTA's copies count on the first one's barrier as well
-            if (rank == 0) mbar_expect_tx(&bar.full[s], 2 * kStageBytes);
+            if (rank == 0) mbar_expect_tx(&bar.full[s], stage_tx);
             const uint32_t full = in_leader(&bar.full[s]);
             uint8_t* sa = smem + s * kStageBytes;
             uint8_t* sb = sa + kOperandBytes;
@@ -358,7 +371,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
       bool ok = true;
       for (int i = 0; ok && work(i, w, nt_end); ++i) {
         const bool a_mn = kKind == kGrad && w.weight;
-        const uint32_t idesc = make_idesc(256, 256, a_mn ? 1 : 0, kKind == kGrad ? 1 : 0);
+        const uint32_t idesc = make_idesc(256, tile_n, a_mn ? 1 : 0, kKind == kGrad ? 1 : 0);
         const uint32_t step_a = a_mn ? kStepMn : kStepK, lbo_a = a_mn ? kLbo : 0;
         for (int nt = w.nt; nt < nt_end && ok; ++nt, ++tile) {
           const uint32_t a = tile & 1, use = tile >> 1;
@@ -421,11 +434,11 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
         ok = s_go[group][(tile >> 1) & 1];
         if (!ok) break;
         tc_fence_after();
-        const int n0 = nt * 256;
+        const int n0 = nt * tile_n, n_end = min(n0 + tile_n, p.N);
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
           const int col = n0 + c * 64;
-          if (col >= p.N) break;   // uniform in the group
+          if (col >= n_end) break;   // uniform in the group
           uint32_t r[2][32];
           tmem_ld32(lane_addr + c * 64, r[0]);
           tmem_ld32(lane_addr + c * 64 + 32, r[1]);
@@ -538,7 +551,9 @@ __device__ __forceinline__ void widen(const uint4& x, f32x2 (&o)[4]) {
 template <int kRows>
 __global__ void __launch_bounds__(kFewThreads) few_rows_kernel(int M, int vecs, int vocab, const uint4* __restrict__ hidden,
                                                                int64_t h_pitch_vecs, const uint4* __restrict__ weight,
-                                                               int64_t w_pitch_vecs, float scale_log2, float2* __restrict__ part) {
+                                                               int64_t w_pitch_vecs, float scale_log2, float2* __restrict__ part, int* __restrict__ status) {
+  next_kernel_may_start();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = int(PSRL_OK);
   extern __shared__ uint4 s_h[];   // [kRows][vecs]
   __shared__ float2 s_best[kFewThreads / 32][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -618,11 +633,42 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
                                                               const int32_t* __restrict__ targets, const int32_t* __restrict__ off,
                                                               int n_targets, float scale, float* __restrict__ logprob,
                                                               float* __restrict__ lse) {
-  constexpr int kSlices = kFinalThreads / kRows;
+  constexpr int kSlices = kFinalThreads / kRows, kWarps = kFinalThreads / 32;
   __shared__ float2 s_part[kSlices][kRows];
   __shared__ float s_lse[kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row0 = blockIdx.x * kRows, mine = threadIdx.x % kRows, slice = threadIdx.x / kRows, row = row0 + mine;
+  // The targets' logits need nothing of the kernel before: they are computed while it runs out.  Target number `at` of the
+  // block's rows is warp at % kWarps's.
+  const int vecs = hidden_dim / 8;
+  int at = 0;
+  for (int r = 0; r < kRows && row0 + r < M; ++r) {
+    int b, e;
+    target_range(off, row0 + r, n_targets, b, e);
+    for (int t = b; t < e; ++t, ++at) {
+      if (at % kWarps != warp) continue;
+      const int y = targets[t];
+      if (y < 0 || y >= vocab) continue;
+      const uint4* hv = reinterpret_cast<const uint4*>(hidden + int64_t(row0 + r) * h_pitch);
+      const uint4* wv = reinterpret_cast<const uint4*>(weight + int64_t(y) * w_pitch);
+      f32x2 acc = make_f32x2(0.f, 0.f);
+#pragma unroll 4
+      for (int i = lane; i < vecs; i += 32) {
+        f32x2 x[4], w[4];
+        widen(hv[i], x);
+        widen(wv[i], w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc = fma2(x[j], w[j], acc);
+      }
+      float z, z1;
+      split_f32x2(acc, z, z1);
+      z += z1;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+      if (lane == 0) logprob[t] = scale * z;   // the same thread subtracts the lse below
+    }
+  }
+  previous_kernel_done();
   float m = -CUDART_INF_F, s = 0.f;
   if (row < M) {
     for (int i = slice; i < n_parts; i += kSlices) {
@@ -650,37 +696,18 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
     if (row < M) lse[row] = l;
   }
   __syncthreads();
-  const int vecs = hidden_dim / 8;
-  int at = 0;   // targets of the rows before, for the distribution over the warps
+  at = 0;
   for (int r = 0; r < kRows && row0 + r < M; ++r) {
     int b, e;
     target_range(off, row0 + r, n_targets, b, e);
-    for (int t = b; t < e; ++t, ++at) {
-      if (at % (kFinalThreads / 32) != warp) continue;
-      const int y = targets[t];
-      if (y < 0 || y >= vocab) {
-        if (lane == 0) logprob[t] = 0.f;
-        continue;
+    if (lane == 0) {
+      for (int t = b + (warp - at % kWarps + kWarps) % kWarps; t < e; t += kWarps) {
+        const int y = targets[t];
+        // a log-probability is not positive; the two sums are rounded apart
+        logprob[t] = y >= 0 && y < vocab ? fminf(logprob[t] - s_lse[r], 0.f) : 0.f;
       }
-      const uint4* hv = reinterpret_cast<const uint4*>(hidden + int64_t(row0 + r) * h_pitch);
-      const uint4* wv = reinterpret_cast<const uint4*>(weight + int64_t(y) * w_pitch);
-      f32x2 acc = make_f32x2(0.f, 0.f);
-#pragma unroll 4
-      for (int i = lane; i < vecs; i += 32) {
-        f32x2 x[4], w[4];
-        widen(hv[i], x);
-        widen(wv[i], w);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc = fma2(x[j], w[j], acc);
-      }
-      float z, z1;
-      split_f32x2(acc, z, z1);
-      z += z1;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-      // a log-probability is not positive; the two sums are rounded apart
-      if (lane == 0) logprob[t] = fminf(scale * z - s_lse[r], 0.f);
     }
+    at += e - b;
   }
 }
 
@@ -694,7 +721,9 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int voca
                                                                  const float* __restrict__ logprob, const float* __restrict__ lse,
                                                                  const float* __restrict__ d_logprob, float scale,
                                                                  float2* __restrict__ row_info, float* __restrict__ entry,
-                                                                 uint8_t* __restrict__ matters) {
+                                                                 uint8_t* __restrict__ matters, int* __restrict__ status) {
+  next_kernel_may_start();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *status = int(PSRL_OK);
   __shared__ uint32_t s_bits;
   if (threadIdx.x == 0) s_bits = 0;
   __syncthreads();
@@ -737,6 +766,7 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int voca
 __global__ void __launch_bounds__(256) sum_kernel(const float4* __restrict__ acc, int splits, int64_t split_vecs, int pitch_vecs, int vecs,
                                                   const int32_t* __restrict__ count, const int32_t* __restrict__ row_of,
                                                   uint2* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
+  previous_kernel_done();
   const int row = blockIdx.x, i = blockIdx.y * 256 + threadIdx.x;
   if (row >= *count || i >= vecs) return;
   acc += int64_t(row) * pitch_vecs + i;
@@ -758,6 +788,8 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, const 
   __shared__ int s_before;
   if (threadIdx.x == 0) s_before = 0;
   __syncthreads();
+  previous_kernel_done();
+  next_kernel_may_start();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, byte = blockIdx.x;
   int before = 0;
   const uint32_t* words = reinterpret_cast<const uint32_t*>(matters);
@@ -797,7 +829,7 @@ constexpr int kFewRows = 4;
 constexpr int kFewBlocks = 1184;  // its blocks at most: eight per SM
 
 struct Layout {
-  int32_t n_tiles, run, n_parts;
+  int32_t tile_n, n_tiles, run, n_parts;
   int32_t few;                   // rows that few_rows_kernel is built for, 0: the matrix kernel
   int64_t piece;                 // vocabulary entries of one piece of the backward
   int64_t rows, acc_rows;        // rows that the backward's gathered buffers and the sums of d_hidden hold
@@ -805,16 +837,32 @@ struct Layout {
   size_t part, row_info, entry, matters, row_of, count, gathered, dz, acc, total;
 };
 
+// Columns of a tile of the logits.  Wide tiles use the tensor cores and the L2 best; with few tiles the rounds of the 74 pairs
+// of CTAs come out uneven, and narrower ones even them (79 tiles of 256 columns take two rounds, so do 105 of 192).
+int tile_columns(int64_t m_tiles, int64_t v, int64_t k_blocks, int pairs) {
+  if (m_tiles * ((v + 255) / 256) >= 4 * pairs) return 256;
+  int best = 256;
+  int64_t least = INT64_MAX;
+  for (int w = 256; w >= 64; w -= 64) {
+    const int64_t tiles = m_tiles * ((v + w - 1) / w), cost = (tiles + pairs - 1) / pairs * (2 * w * k_blocks + 1500);
+    if (cost < least) { least = cost; best = w; }
+  }
+  return best;
+}
+
 Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward) {
   Layout L{};
   const int64_t m_tiles = (n + 255) / 256;
-  L.n_tiles = static_cast<int32_t>((v + 255) / 256);
+  // the forward's tiles; the backward's of the logits too while all rows are one tile (how many of them matter is not known here)
+  const int pairs = resident_ctas() / 2;
+  L.tile_n = !backward || m_tiles == 1 ? tile_columns(m_tiles, v, (h + kBK - 1) / kBK, pairs) : 256;
+  L.n_tiles = static_cast<int32_t>((v + L.tile_n - 1) / L.tile_n);
   size_t at = kWsHeaderBytes;
   auto take = [&](size_t bytes) { const size_t a = at; at += (bytes + 255) / 256 * 256; return a; };
   if (!backward) {
     // short runs while there are few tiles (they balance the pairs of CTAs), long ones to keep the partials small
     const int64_t tiles = m_tiles * L.n_tiles;
-    L.run = static_cast<int32_t>(std::min<int64_t>(kMaxRun, std::max<int64_t>(1, tiles / (74 * 16))));
+    L.run = static_cast<int32_t>(std::min<int64_t>(kMaxRun, std::max<int64_t>(1, tiles / (pairs * 16))));
     L.n_parts = (L.n_tiles + L.run - 1) / L.run * kGroups;
     if (n <= kFewRows) {
       for (L.few = 1; L.few < n;) L.few *= 2;
@@ -848,31 +896,46 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
   return L;
 }
 
+// A kernel of a call; all but the first may start before the one before has ended (see previous_kernel_done).
+template <class... P, class... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, bool first, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = first ? 0 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 template <Kind kKind>
-cudaError_t launch_gemm(const GemmMaps& maps, GemmParams& p, cudaStream_t stream) {
+cudaError_t launch_gemm(const GemmMaps& maps, GemmParams& p, bool first, cudaStream_t stream) {
   static bool done[64] = {};
   cudaError_t e = ensure_dynamic_smem(gemm_kernel<kKind>, gemm_smem(kKind), done);
   if (e != cudaSuccess) return e;
-  p.n_tiles = (p.N + 255) / 256;
+  if (p.tile_n == 0) p.tile_n = 256;
+  p.n_tiles = (p.N + p.tile_n - 1) / p.tile_n;
   if (p.run < 1) p.run = 1;
   int64_t units = (int64_t(p.M) + 255) / 256 * ((p.n_tiles + p.run - 1) / p.run);
   if (kKind == kGrad) units = units * p.splits + (int64_t(p.vocab) + 255) / 256 * p.n_tiles;
   if (units > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int clusters = static_cast<int>(std::min<int64_t>(units, resident_ctas() / 2));
-  gemm_kernel<kKind><<<2 * clusters, kGemmThreads, gemm_smem(kKind), stream>>>(maps, p);
-  return cudaGetLastError();
+  return launch(gemm_kernel<kKind>, dim3(2 * clusters), kGemmThreads, gemm_smem(kKind), stream, first, maps, p);
 }
 
 template <int kRows>
 cudaError_t launch_few(const Layout& L, int32_t M, int32_t h, int32_t v, const void* hidden, int64_t hp, const void* weight, int64_t wp,
-                       float scale, float2* part, cudaStream_t stream) {
+                       float scale, float2* part, int* status, cudaStream_t stream) {
   static bool done[64] = {};
   const size_t smem = size_t(kRows) * h * 2;
   cudaError_t e = ensure_dynamic_smem(few_rows_kernel<kRows>, kFewSmem, done);
   if (e != cudaSuccess) return e;
-  few_rows_kernel<kRows><<<unsigned(L.n_parts), kFewThreads, smem, stream>>>(M, h / 8, v, static_cast<const uint4*>(hidden), hp / 8,
-                                                                           static_cast<const uint4*>(weight), wp / 8, scale * kLog2e, part);
-  return cudaGetLastError();
+  return launch(few_rows_kernel<kRows>, dim3(unsigned(L.n_parts)), kFewThreads, smem, stream, true, M, h / 8, v, static_cast<const uint4*>(hidden),
+                hp / 8, static_cast<const uint4*>(weight), wp / 8, scale * kLog2e, part, status);
 }
 
 psrl_status_t cuda_failed(cudaError_t e) {
@@ -916,42 +979,45 @@ psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t
   if (st != PSRL_OK) return st;
   if (!ptr_aligned(workspace, 256)) return PSRL_ERR_INVALID_ARG;
   if (workspace_bytes < psrl_token_logprob_workspace_bytes(n_rows, hidden_dim, vocab, n_targets, 0)) return PSRL_ERR_WORKSPACE;
+  if (n_rows && (!al4(lse) || (n_targets && !al4(logprob)))) return PSRL_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
-  if (e != cudaSuccess) return cuda_failed(e);
-  if (n_rows == 0) return PSRL_OK;
-  if (!al4(lse) || (n_targets && !al4(logprob))) return PSRL_ERR_INVALID_ARG;
+  cudaError_t e = cudaSuccess;
+  if (n_rows == 0) {
+    e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);   // otherwise the first kernel clears the status
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
   const Layout L = layout(n_rows, hidden_dim, vocab, n_targets, false);
   char* ws = static_cast<char*>(workspace);
   float2* part = reinterpret_cast<float2*>(ws + L.part);
+  int* status = reinterpret_cast<int*>(ws);
   const int32_t M = static_cast<int32_t>(n_rows);
   if (L.few) {
-    e = L.few == 1 ? launch_few<1>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s)
-      : L.few == 2 ? launch_few<2>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s)
-                   : launch_few<4>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, s);
+    e = L.few == 1 ? launch_few<1>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, status, s)
+      : L.few == 2 ? launch_few<2>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, status, s)
+                   : launch_few<4>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, status, s);
   } else {
     GemmMaps maps;
     if (!make_map_bf16_2d(&maps.a, hidden, hidden_dim, n_rows, hidden_pitch * 2, 128) ||
-        !make_map_bf16_2d(&maps.b, weight, hidden_dim, vocab, weight_pitch * 2, 128))
+        !make_map_bf16_2d(&maps.b, weight, hidden_dim, vocab, weight_pitch * 2, L.tile_n / 2))
       return PSRL_ERR_CUDA;
     GemmParams p{};
     p.M = M;
     p.N = vocab;
     p.k_blocks = (hidden_dim + kBK - 1) / kBK;
+    p.tile_n = L.tile_n;
     p.run = L.run;
     p.scale_log2 = scale * kLog2e;
     p.part = part;
-    p.status = reinterpret_cast<int*>(ws);
-    e = launch_gemm<kLse>(maps, p, s);
+    p.status = status;
+    e = launch_gemm<kLse>(maps, p, true, s);
   }
   if (e != cudaSuccess) return cuda_failed(e);
   // rows of a block: 32 read the partials in whole lines; with few rows more threads to each of them finish sooner
   const int rows = M >= 4096 ? 32 : M >= 256 ? 4 : 1;
   auto final = rows == 32 ? final_kernel<32> : rows == 4 ? final_kernel<4> : final_kernel<1>;
-  final<<<unsigned((M + rows - 1) / rows), kFinalThreads, 0, s>>>(
-      part, L.n_parts, M, hidden_dim, vocab, static_cast<const __nv_bfloat16*>(hidden), hidden_pitch,
-      static_cast<const __nv_bfloat16*>(weight), weight_pitch, targets, target_off, static_cast<int>(n_targets), scale, logprob, lse);
-  e = cudaGetLastError();
+  e = launch(final, dim3(unsigned((M + rows - 1) / rows)), kFinalThreads, 0, s, false, part, L.n_parts, M, hidden_dim, vocab,
+             static_cast<const __nv_bfloat16*>(hidden), hidden_pitch, static_cast<const __nv_bfloat16*>(weight), weight_pitch, targets,
+             target_off, static_cast<int>(n_targets), scale, logprob, lse);
   return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
 }
 
@@ -967,14 +1033,15 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   if (!ptr_aligned(workspace, 256) || (d_hidden && !al16(d_hidden)) || (d_weight && !al16(d_weight))) return PSRL_ERR_INVALID_ARG;
   if ((d_hidden && !pitch16(d_hidden_pitch, hidden_dim)) || (d_weight && !pitch16(d_weight_pitch, hidden_dim))) return PSRL_ERR_SHAPE;
   if (workspace_bytes < psrl_token_logprob_workspace_bytes(n_rows, hidden_dim, vocab, n_targets, 1)) return PSRL_ERR_WORKSPACE;
+  if (n_rows && (!al4(lse) || (n_targets && (!al4(logprob) || !al4(d_logprob))))) return PSRL_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+  cudaError_t e = cudaSuccess;
+  if (n_rows == 0 || (!d_hidden && !d_weight)) e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);   // otherwise the first kernel clears the status
   if (e != cudaSuccess) return cuda_failed(e);
   if (n_rows == 0) {
     if (d_weight) e = cudaMemset2DAsync(d_weight, size_t(d_weight_pitch) * 2, 0, size_t(hidden_dim) * 2, vocab, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
-  if (!al4(lse) || (n_targets && (!al4(logprob) || !al4(d_logprob)))) return PSRL_ERR_INVALID_ARG;
   if (!d_hidden && !d_weight) return PSRL_OK;
   const Layout L = layout(n_rows, hidden_dim, vocab, n_targets, true);
   char* ws = static_cast<char*>(workspace);
@@ -987,18 +1054,17 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   float* acc = reinterpret_cast<float*>(ws + L.acc);
   const int64_t acc_pitch = round_up(hidden_dim, 32);
   const int32_t M = static_cast<int32_t>(n_rows);
-  rows_kernel<<<unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte), kRowsPerByte * 32, 0, s>>>(M, vocab, targets, target_off, static_cast<int>(n_targets), logprob, lse,
-                                                         d_logprob, scale, row_info, entry, reinterpret_cast<uint8_t*>(ws + L.matters));
-  e = cudaGetLastError();
+  e = launch(rows_kernel, dim3(unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte)), kRowsPerByte * 32, 0, s, true, M, vocab, targets,
+             target_off, static_cast<int>(n_targets), logprob, lse, d_logprob, scale, row_info, entry,
+             reinterpret_cast<uint8_t*>(ws + L.matters), base.status);
   if (e != cudaSuccess) return cuda_failed(e);
   __nv_bfloat16* gathered = reinterpret_cast<__nv_bfloat16*>(ws + L.gathered);
   base.count = reinterpret_cast<int32_t*>(ws + L.count);
   base.row_of = reinterpret_cast<int32_t*>(ws + L.row_of);
-  gather_kernel<<<unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte), kRowsPerByte * 32, 0, s>>>(
-      M, reinterpret_cast<uint8_t*>(ws + L.matters), static_cast<const uint4*>(hidden), hidden_pitch / 8, hidden_dim / 8,
-      reinterpret_cast<uint4*>(gathered), reinterpret_cast<int32_t*>(ws + L.row_of), reinterpret_cast<int32_t*>(ws + L.count),
-      static_cast<uint4*>(d_hidden), d_hidden_pitch / 8);
-  e = cudaGetLastError();
+  e = launch(gather_kernel, dim3(unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte)), kRowsPerByte * 32, 0, s, false, M,
+             reinterpret_cast<uint8_t*>(ws + L.matters), static_cast<const uint4*>(hidden), hidden_pitch / 8, hidden_dim / 8,
+             reinterpret_cast<uint4*>(gathered), reinterpret_cast<int32_t*>(ws + L.row_of), reinterpret_cast<int32_t*>(ws + L.count),
+             static_cast<uint4*>(d_hidden), d_hidden_pitch / 8);
   if (e != cudaSuccess) return cuda_failed(e);
   const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(weight);
   for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
@@ -1006,7 +1072,7 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
     const __nv_bfloat16* wv = w + v0 * weight_pitch;
     GemmMaps mz, mg;
     if (!make_map_bf16_2d(&mz.a, gathered, hidden_dim, L.rows, int64_t(hidden_dim) * 2, 128) ||
-        !make_map_bf16_2d(&mz.b, wv, hidden_dim, nv, weight_pitch * 2, 128) ||
+        !make_map_bf16_2d(&mz.b, wv, hidden_dim, nv, weight_pitch * 2, L.tile_n / 2) ||
         !make_map_bf16_2d(&mg.a, dz, nv, L.rows, L.piece * 2, 128) ||
         !make_map_bf16_2d(&mg.b, wv, hidden_dim, nv, weight_pitch * 2, 64) ||
         !make_map_bf16_2d(&mg.a2, dz, nv, L.rows, L.piece * 2, 64) ||
@@ -1020,7 +1086,8 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
     z.M = M; z.N = static_cast<int32_t>(nv); z.k_blocks = (hidden_dim + kBK - 1) / kBK;
     z.row_info = row_info; z.targets = targets; z.target_off = target_off; z.entry = entry;
     z.n_targets = static_cast<int32_t>(n_targets); z.col0 = static_cast<int32_t>(v0);
-    e = launch_gemm<kDz>(mz, z, s);
+    z.tile_n = L.tile_n;
+    e = launch_gemm<kDz>(mz, z, false, s);
     if (e != cudaSuccess) return cuda_failed(e);
     GemmParams g = base;
     g.M = M; g.N = hidden_dim; g.vocab = static_cast<int32_t>(nv);
@@ -1028,14 +1095,13 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
     g.splits = L.splits;
     g.acc_rows = static_cast<int32_t>(L.acc_rows);
     g.first = v0 == 0;
-    e = launch_gemm<kGrad>(mg, g, s);
+    e = launch_gemm<kGrad>(mg, g, false, s);
     if (e != cudaSuccess) return cuda_failed(e);
   }
   if (d_hidden) {
-    sum_kernel<<<dim3(unsigned(n_rows), unsigned((hidden_dim / 4 + 255) / 256)), 256, 0, s>>>(reinterpret_cast<const float4*>(acc), L.splits, L.acc_rows * acc_pitch / 4,
-                                                static_cast<int>(acc_pitch / 4), hidden_dim / 4, base.count, base.row_of,
-                                                static_cast<uint2*>(d_hidden), d_hidden_pitch / 4);
-    e = cudaGetLastError();
+    e = launch(sum_kernel, dim3(unsigned(n_rows), unsigned((hidden_dim / 4 + 255) / 256)), 256, 0, s, false, reinterpret_cast<const float4*>(acc),
+               L.splits, L.acc_rows * acc_pitch / 4, static_cast<int>(acc_pitch / 4), hidden_dim / 4, base.count, base.row_of,
+               static_cast<uint2*>(d_hidden), d_hidden_pitch / 4);
     if (e != cudaSuccess) return cuda_failed(e);
   }
   return PSRL_OK;
