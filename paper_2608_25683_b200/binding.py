@@ -661,13 +661,13 @@ def _extents(extents):
 
 
 def _pair_of_pools(k, v, what: str):
-    import torch
-
-    if k.dtype not in (torch.float32, torch.bfloat16) or v.dtype != k.dtype:
+    """(heads, capacity, bytes of a slot and head) of two pools of one shape."""
+    shape, size = k.shape, k.element_size()
+    if str(k.dtype) not in ("torch.bfloat16", "torch.float32") or v.dtype != k.dtype:
         raise TypeError(f"{what} must both be float32 or both bfloat16")
-    if k.dim() != 3 or k.shape != v.shape or not k.is_contiguous() or not v.is_contiguous():
+    if len(shape) != 3 or shape != v.shape or not k.is_contiguous() or not v.is_contiguous():
         raise ValueError(f"{what} must be contiguous [Hkv, capacity, d] of one shape")
-    return int(k.shape[0]), int(k.shape[1]), int(k.shape[2]) * k.element_size()
+    return shape[0], shape[1], shape[2] * size
 
 
 def psrl_kv_copy(extents, k_src, v_src, k_dst, v_dst, stream=None):

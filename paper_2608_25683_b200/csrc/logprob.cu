@@ -47,6 +47,11 @@ constexpr int kMaxRun = 8;                   // vocabulary tiles whose maximum a
 
 enum Kind { kLse, kDz, kGrad };
 
+// Up to kTwiceRows rows, half of a tile's rows are free and everything is bound by the weights' bytes.  dz is then kept
+// twice, rounded to bf16 and what that leaves, in rows r and 128 + r: the second CTA of a pair computes the same logits as the
+// first, and both products add the two.  With more rows dz's roundings average out in d_weight's sums.
+constexpr int kTwiceRows = 128;
+
 // 32 KB stages of operands; the kinds that store tiles give one of them to their output buffers, two per group
 constexpr int stages(Kind k) { return k == kLse ? 6 : 5; }
 constexpr size_t gemm_smem(Kind k) { return size_t(stages(k)) * kStageBytes + (k == kLse ? 0 : size_t(kGroups) * 2 * kOutBytes) + 1024; }
@@ -61,12 +66,14 @@ struct GemmMaps {
 struct GemmParams {
   int32_t M, N;                 // valid rows and columns of the product
   int32_t n_tiles, k_blocks;
+  int32_t twice;                // kDz, kGrad: rows 128 ... hold the rest of dz below bf16 (see kTwiceRows)
   const int32_t* count;         // kDz, kGrad: rows that matter, on the device (kLse: NULL, all M)
   const int32_t* row_of;        // kDz: the caller's row of a gathered row
   int32_t tile_n;               // columns of a tile: 256, or fewer in the logits (a multiple of 64)
   int32_t run;                  // kLse: consecutive column tiles of one work unit
   float scale_log2;             // logits in powers of two: scale * log2(e)
   float2* part;                 // kLse: [unit column][group][M] (max, sum), powers of two
+  int32_t* part_at;             // kLse: the vocabulary entry of the maximum
   const float2* row_info;       // kDz: per row (lse * log2(e), -scale * G)
   const int32_t* targets;       // kDz
   const int32_t* target_off;    // kDz: may be NULL (one target per row)
@@ -170,12 +177,12 @@ struct GradPlan {
   bool lighter;
 
   __device__ __forceinline__ GradPlan(const GemmParams& p, int rows, int c, int C) {
-    m_tiles = p.want_hidden ? (rows + 255) / 256 : 0;
+    m_tiles = p.want_hidden ? (rows + 255) / 256 : 0;   // twice: rows <= 128, one tile as well
     v_tiles = p.want_weight ? (p.vocab + 255) / 256 : 0;
     per = m_tiles * p.n_tiles;
     n_hidden = per * p.splits;
     steps = (p.vocab + kBK - 1) / kBK;
-    row_steps = (rows + kBK - 1) / kBK;
+    row_steps = (rows + kBK - 1) / kBK << p.twice;
     const int q = n_hidden / C, r = n_hidden - q * C;
     mine = q + (c < r ? 1 : 0);
     n_weight = v_tiles * p.n_tiles;
@@ -329,7 +336,10 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
         const int m0 = w.mt * 256 + int(rank) * 128;
         for (int nt = w.nt; nt < nt_end && ok; ++nt) {
           const int n0 = nt * tile_n + int(rank) * (tile_n / 2);
-          for (int kb = w.kb0; kb < w.kb1; ++kb, ++it) {
+          // twice: the second half of d_weight's steps are the rows from 128 on
+          const int skip = kKind == kGrad && w.weight && p.twice ? 128 / kBK - w.kb1 / 2 : 0;
+          for (int step = w.kb0; step < w.kb1; ++step, ++it) {
+            const int kb = step + (skip && step >= w.kb1 / 2 ? skip : 0);
             const uint32_t s = it % kStages, round = it / kStages;
             if (round > 0 && !mbar_wait(&bar.empty[s], (round + 1) & 1, abortp, p.status)) { ok = false; break; }
             // the second CTA's copies count on the first one's barrier as well
@@ -412,12 +422,15 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
     bool ok = true;
     for (int i = 0; ok && work(i, w, nt_end); ++i) {
       const int row0 = w.mt * 256 + int(rank) * 128, row = row0 + gt;
-      const bool live = row < rows;
+      const bool rest = kKind == kDz && p.twice && rank == 1;
+      const int of_row = rest ? gt : row;
+      const bool live = of_row < rows;
       float best = -CUDART_INF_F, sum = 0.f;                       // kLse
+      int best_at = 0;
       float lse2 = 0.f, coef = 0.f;                                // kDz
       int t_begin = 0, t_end = 0, first_target = -1;
       if (kKind == kDz && live) {
-        const int user_row = p.row_of[row];
+        const int user_row = p.row_of[of_row];
         const float2 ri = p.row_info[user_row];
         lse2 = ri.x; coef = ri.y;
         target_range(p.target_off, user_row, p.n_targets, t_begin, t_end);
@@ -458,7 +471,13 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
                 r[h][i] = __float_as_uint(z);
                 top = fmaxf(top, z);
               }
-              if (top > best) { sum *= ex2(best - top); best = top; }
+              if (top > best) {   // seldom after the first columns
+                sum *= ex2(best - top);
+                best = top;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (__uint_as_float(r[h][i]) == top) best_at = col + 32 * h + i;
+              }
               const float ref = best == -CUDART_INF_F ? 0.f : best;   // nothing finite yet: every term is zero
               float s0 = 0.f, s1 = 0.f;
 #pragma unroll
@@ -493,6 +512,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
                   hi = coef * ex2(fmaf(hi, p.scale_log2, -lse2));
                 }
                 o[i] = pack_bf16(lo, hi);
+                if (kKind == kDz && rest) o[i] = pack_bf16(lo - __uint_as_float(o[i] << 16), hi - __uint_as_float(o[i] & 0xffff0000u));
               }
               // kDz: rows behind the last one are zero, as the product for d_weight reads dz in steps of kBK rows
               const bool any = kKind == kDz ? live : w.kb1 > w.kb0;
@@ -502,9 +522,12 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
               // the row's targets inside these columns, over what this thread has just written
               for (int t = t_begin; t < t_end; ++t) {
                 const uint32_t x = uint32_t(t == t_begin ? first_target : p.targets[t]) - uint32_t(p.col0 + col);
-                if (x < uint32_t(min(64, p.N - col)))
-                  *reinterpret_cast<__nv_bfloat16*>(b + gt * 128 + (((x >> 3) ^ (gt & 7)) << 4) + (x & 7) * 2) =
-                      __float2bfloat16_rn(p.entry[t]);
+                if (x < uint32_t(min(64, p.N - col))) {
+                  const float v = p.entry[t];
+                  __nv_bfloat16 y = __float2bfloat16_rn(v);
+                  if (rest) y = __float2bfloat16_rn(v - __bfloat162float(y));
+                  *reinterpret_cast<__nv_bfloat16*>(b + gt * 128 + (((x >> 3) ^ (gt & 7)) << 4) + (x & 7) * 2) = y;
+                }
               }
             }
             out.send(kKind == kGrad ? &maps.out2 : &maps.out, col, row0, false);
@@ -515,7 +538,11 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
         __syncwarp();
         if (lane == 0) arrive_leader(acc_empty);
       }
-      if (kKind == kLse && ok && live) p.part[(int64_t(w.split) * kGroups + group) * rows + row] = make_float2(best, sum);
+      if (kKind == kLse && ok && live) {
+        const int64_t at = (int64_t(w.split) * kGroups + group) * rows + row;
+        p.part[at] = make_float2(best, sum);
+        p.part_at[at] = best_at;
+      }
     }
     if (kKind != kLse) out.finish();
   }
@@ -625,9 +652,32 @@ __global__ void __launch_bounds__(kFewThreads) few_rows_kernel(int M, int vecs, 
 
 // lse of kRows rows from their partial (max, sum), then the log-probabilities of the rows' targets: the target's logit is a
 // dot product of its own (two rows read per target, against a whole pass over the weights for the lse).
+// The tensor cores cut off what a step of 16 adds below the sum's last bit, always towards zero: after 256 steps a logit of
+// 20 is about 3e-5 short.  That matters where one entry carries the sum - a confident row, whose log-probability is the
+// small difference of two such numbers - so the largest entry's logit is computed again, in fp32, and its term replaced:
+// lse of 8192 rows of 4096 deep products 3.0e-6 -> 6.3e-7 relative to 64 bits.
+__device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfloat16* y, int vecs) {
+  const uint4 *xv = reinterpret_cast<const uint4*>(x), *yv = reinterpret_cast<const uint4*>(y);
+  f32x2 acc = make_f32x2(0.f, 0.f);
+#pragma unroll 4
+  for (int i = threadIdx.x & 31; i < vecs; i += 32) {
+    f32x2 a[4], b[4];
+    widen(xv[i], a);
+    widen(yv[i], b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = fma2(a[j], b[j], acc);
+  }
+  float z, z1;
+  split_f32x2(acc, z, z1);
+  z += z1;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+  return z;
+}
+
 constexpr int kFinalThreads = 256;
 template <int kRows>
-__global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __restrict__ part, int n_parts, int M, int hidden_dim,
+__global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __restrict__ part, const int32_t* __restrict__ part_at, int n_parts, int M, int hidden_dim,
                                                               int vocab, const __nv_bfloat16* __restrict__ hidden, int64_t h_pitch,
                                                               const __nv_bfloat16* __restrict__ weight, int64_t w_pitch,
                                                               const int32_t* __restrict__ targets, const int32_t* __restrict__ off,
@@ -635,6 +685,7 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
                                                               float* __restrict__ lse) {
   constexpr int kSlices = kFinalThreads / kRows, kWarps = kFinalThreads / 32;
   __shared__ float2 s_part[kSlices][kRows];
+  __shared__ int32_t s_at[kSlices][kRows];
   __shared__ float s_lse[kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row0 = blockIdx.x * kRows, mine = threadIdx.x % kRows, slice = threadIdx.x / kRows, row = row0 + mine;
@@ -649,30 +700,17 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
       if (at % kWarps != warp) continue;
       const int y = targets[t];
       if (y < 0 || y >= vocab) continue;
-      const uint4* hv = reinterpret_cast<const uint4*>(hidden + int64_t(row0 + r) * h_pitch);
-      const uint4* wv = reinterpret_cast<const uint4*>(weight + int64_t(y) * w_pitch);
-      f32x2 acc = make_f32x2(0.f, 0.f);
-#pragma unroll 4
-      for (int i = lane; i < vecs; i += 32) {
-        f32x2 x[4], w[4];
-        widen(hv[i], x);
-        widen(wv[i], w);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc = fma2(x[j], w[j], acc);
-      }
-      float z, z1;
-      split_f32x2(acc, z, z1);
-      z += z1;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+      const float z = warp_dot(hidden + int64_t(row0 + r) * h_pitch, weight + int64_t(y) * w_pitch, vecs);
       if (lane == 0) logprob[t] = scale * z;   // the same thread subtracts the lse below
     }
   }
   previous_kernel_done();
   float m = -CUDART_INF_F, s = 0.f;
+  int m_at = 0;
   if (row < M) {
     for (int i = slice; i < n_parts; i += kSlices) {
       const float2 x = part[int64_t(i) * M + row];
+      if (part_at && x.x > m) m_at = part_at[int64_t(i) * M + row];
       const float top = fmaxf(m, x.x);
       const float ref = top == -CUDART_INF_F ? 0.f : top;
       s = s * exp2f(m - ref) + x.y * exp2f(x.x - ref);
@@ -680,20 +718,28 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
     }
   }
   s_part[slice][mine] = make_float2(m, s);
+  s_at[slice][mine] = m_at;
   for (int half = kSlices / 2; half > 0; half /= 2) {
     __syncthreads();
     if (slice < half) {
       const float2 x = s_part[slice][mine], y = s_part[slice + half][mine];
       const float top = fmaxf(x.x, y.x), ref = top == -CUDART_INF_F ? 0.f : top;
       s_part[slice][mine] = make_float2(top, x.y * exp2f(x.x - ref) + y.y * exp2f(y.x - ref));
+      if (y.x > x.x) s_at[slice][mine] = s_at[slice + half][mine];
     }
   }
   __syncthreads();
-  if (slice == 0) {
-    const float2 x = s_part[0][mine];
-    const float l = ((x.x == -CUDART_INF_F ? 0.f : x.x) + log2f(x.y)) * kLn2;
-    s_lse[mine] = l;
-    if (row < M) lse[row] = l;
+  for (int r = warp; r < kRows && row0 + r < M; r += kWarps) {
+    float2 x = s_part[0][r];
+    if (part_at && fabsf(x.x) <= 1e30f) {   // not for infinities and NaN
+      const float z = warp_dot(hidden + int64_t(row0 + r) * h_pitch, weight + int64_t(s_at[0][r]) * w_pitch, vecs) * (scale * kLog2e);
+      x.y = x.y - 1.f + exp2f(z - x.x);     // the maximum's term of the sum is one
+    }
+    if (lane == 0) {
+      const float l = ((x.x == -CUDART_INF_F ? 0.f : x.x) + log2f(x.y)) * kLn2;
+      s_lse[r] = l;
+      lse[row0 + r] = l;
+    }
   }
   __syncthreads();
   at = 0;
@@ -763,17 +809,17 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int voca
 }
 
 // d_hidden from the parts of its sum, in order.
-__global__ void __launch_bounds__(256) sum_kernel(const float4* __restrict__ acc, int splits, int64_t split_vecs, int pitch_vecs, int vecs,
+__global__ void __launch_bounds__(256) sum_kernel(const float4* __restrict__ acc, int splits, int64_t split_vecs, int twice, int pitch_vecs, int vecs,
                                                   const int32_t* __restrict__ count, const int32_t* __restrict__ row_of,
                                                   uint2* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
   previous_kernel_done();
   const int row = blockIdx.x, i = blockIdx.y * 256 + threadIdx.x;
   if (row >= *count || i >= vecs) return;
   acc += int64_t(row) * pitch_vecs + i;
-  float4 s = acc[0];
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int k = 1; k < splits; ++k) {
-    const float4 x = acc[k * split_vecs];
+  for (int k = 0; k < splits << twice; ++k) {
+    const float4 x = acc[(k >> twice) * split_vecs + (k & twice) * int64_t(128) * pitch_vecs];
     s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
   }
   d_hidden[row_of[row] * dh_pitch_vecs + i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
@@ -781,7 +827,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const float4* __restrict__ acc
 
 // Gathers the hidden states of the rows that matter, in order, and zeroes the others' d_hidden.  A warp per row; a block
 // counts the rows before its own itself: one bit per row is little to read.
-__global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, const uint8_t* __restrict__ matters, const uint4* __restrict__ hidden,
+__global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, int twice, const uint8_t* __restrict__ matters, const uint4* __restrict__ hidden,
                                                                    int64_t h_pitch_vecs, int vecs, uint4* __restrict__ gathered,
                                                                    int32_t* __restrict__ row_of, int32_t* __restrict__ count,
                                                                    uint4* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
@@ -805,7 +851,11 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, const 
       const int at = at0 + __popc(bits & ((1u << warp) - 1));
       if (lane == 0) row_of[at] = row;
 #pragma unroll 8
-      for (int i = lane; i < vecs; i += 32) gathered[int64_t(at) * vecs + i] = hidden[row * h_pitch_vecs + i];
+      for (int i = lane; i < vecs; i += 32) {
+        const uint4 x = hidden[row * h_pitch_vecs + i];
+        gathered[int64_t(at) * vecs + i] = x;
+        if (twice) gathered[int64_t(at + 128) * vecs + i] = x;
+      }
     } else if (d_hidden) {
       for (int i = lane; i < vecs; i += 32) d_hidden[row * dh_pitch_vecs + i] = make_uint4(0, 0, 0, 0);
     }
@@ -815,7 +865,10 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, const 
     if (threadIdx.x == 0) *count = n;
     // the rows behind the last one, up to a whole step of the product that sums over rows
     const int64_t end = int64_t((n + kBK - 1) / kBK * kBK) * vecs;
-    for (int64_t i = int64_t(n) * vecs + threadIdx.x; i < end; i += kRowsPerByte * 32) gathered[i] = make_uint4(0, 0, 0, 0);
+    for (int64_t i = int64_t(n) * vecs + threadIdx.x; i < end; i += kRowsPerByte * 32) {
+      gathered[i] = make_uint4(0, 0, 0, 0);
+      if (twice) gathered[i + int64_t(128) * vecs] = make_uint4(0, 0, 0, 0);
+    }
   }
 }
 
@@ -834,7 +887,8 @@ struct Layout {
   int64_t piece;                 // vocabulary entries of one piece of the backward
   int64_t rows, acc_rows;        // rows that the backward's gathered buffers and the sums of d_hidden hold
   int32_t splits;                // parts of d_hidden's sums
-  size_t part, row_info, entry, matters, row_of, count, gathered, dz, acc, total;
+  int32_t twice;                 // dz in two bf16 parts
+  size_t part, part_at, row_info, entry, matters, row_of, count, gathered, dz, acc, total;
 };
 
 // Columns of a tile of the logits.  Wide tiles use the tensor cores and the L2 best; with few tiles the rounds of the 74 pairs
@@ -871,6 +925,7 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
       if (L.few) L.n_parts = static_cast<int32_t>(std::min<int64_t>(kFewBlocks, (v + per_block - 1) / per_block));
     }
     L.part = take(size_t(L.n_parts) * n * sizeof(float2));
+    if (!L.few) L.part_at = take(size_t(L.n_parts) * n * sizeof(int32_t));
   } else {
     // a piece of dz is about 128 MB (it then partly stays in the L2 for the two products that read it) but at least
     // 8192 entries wide: below that the fp32 sums of d_hidden cost more traffic than the products hide
@@ -879,8 +934,9 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
     L.piece = round_up((v + pieces - 1) / pieces, 256);
     L.row_info = take(size_t(n) * sizeof(float2));
     L.entry = take(size_t(n_targets) * sizeof(float));
-    L.rows = round_up(n, kBK);
-    L.acc_rows = round_up(n, 128);
+    L.twice = n <= kTwiceRows;
+    L.rows = L.twice ? 256 : round_up(n, kBK);
+    L.acc_rows = L.twice ? 256 : round_up(n, 128);
     L.matters = take(size_t(n + 7) / 8 + 3);
     L.row_of = take(size_t(n) * sizeof(int32_t));
     L.count = take(sizeof(int32_t));
@@ -989,6 +1045,7 @@ psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t
   const Layout L = layout(n_rows, hidden_dim, vocab, n_targets, false);
   char* ws = static_cast<char*>(workspace);
   float2* part = reinterpret_cast<float2*>(ws + L.part);
+  int32_t* part_at = reinterpret_cast<int32_t*>(ws + L.part_at);
   int* status = reinterpret_cast<int*>(ws);
   const int32_t M = static_cast<int32_t>(n_rows);
   if (L.few) {
@@ -1008,6 +1065,7 @@ psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t
     p.run = L.run;
     p.scale_log2 = scale * kLog2e;
     p.part = part;
+    p.part_at = part_at;
     p.status = status;
     e = launch_gemm<kLse>(maps, p, true, s);
   }
@@ -1015,7 +1073,7 @@ psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t
   // rows of a block: 32 read the partials in whole lines; with few rows more threads to each of them finish sooner
   const int rows = M >= 4096 ? 32 : M >= 256 ? 4 : 1;
   auto final = rows == 32 ? final_kernel<32> : rows == 4 ? final_kernel<4> : final_kernel<1>;
-  e = launch(final, dim3(unsigned((M + rows - 1) / rows)), kFinalThreads, 0, s, false, part, L.n_parts, M, hidden_dim, vocab,
+  e = launch(final, dim3(unsigned((M + rows - 1) / rows)), kFinalThreads, 0, s, false, part, L.few ? nullptr : part_at, L.n_parts, M, hidden_dim, vocab,
              static_cast<const __nv_bfloat16*>(hidden), hidden_pitch, static_cast<const __nv_bfloat16*>(weight), weight_pitch, targets,
              target_off, static_cast<int>(n_targets), scale, logprob, lse);
   return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
@@ -1048,6 +1106,7 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   GemmParams base{};
   base.status = reinterpret_cast<int*>(ws);
   base.scale_log2 = scale * kLog2e;
+  base.twice = L.twice;
   float2* row_info = reinterpret_cast<float2*>(ws + L.row_info);
   float* entry = reinterpret_cast<float*>(ws + L.entry);
   __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + L.dz);
@@ -1061,7 +1120,7 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   __nv_bfloat16* gathered = reinterpret_cast<__nv_bfloat16*>(ws + L.gathered);
   base.count = reinterpret_cast<int32_t*>(ws + L.count);
   base.row_of = reinterpret_cast<int32_t*>(ws + L.row_of);
-  e = launch(gather_kernel, dim3(unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte)), kRowsPerByte * 32, 0, s, false, M,
+  e = launch(gather_kernel, dim3(unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte)), kRowsPerByte * 32, 0, s, false, M, L.twice,
              reinterpret_cast<uint8_t*>(ws + L.matters), static_cast<const uint4*>(hidden), hidden_pitch / 8, hidden_dim / 8,
              reinterpret_cast<uint4*>(gathered), reinterpret_cast<int32_t*>(ws + L.row_of), reinterpret_cast<int32_t*>(ws + L.count),
              static_cast<uint4*>(d_hidden), d_hidden_pitch / 8);
@@ -1100,7 +1159,7 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   }
   if (d_hidden) {
     e = launch(sum_kernel, dim3(unsigned(n_rows), unsigned((hidden_dim / 4 + 255) / 256)), 256, 0, s, false, reinterpret_cast<const float4*>(acc),
-               L.splits, L.acc_rows * acc_pitch / 4, static_cast<int>(acc_pitch / 4), hidden_dim / 4, base.count, base.row_of,
+               L.splits, L.acc_rows * acc_pitch / 4, L.twice, static_cast<int>(acc_pitch / 4), hidden_dim / 4, base.count, base.row_of,
                static_cast<uint2*>(d_hidden), d_hidden_pitch / 4);
     if (e != cudaSuccess) return cuda_failed(e);
   }
