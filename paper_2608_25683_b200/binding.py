@@ -759,7 +759,7 @@ def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: floa
     ws, wsb = _logprob_workspace(workspace, keep, n, h, v, m, False, hidden.device)
     _launch("psrl_token_logprob_fwd", dev, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
             _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
-            None if target_off is None else target_off.data_ptr(), scale, logprob.data_ptr(),
+            None if target_off is None else target_off.data_ptr(), float(scale), logprob.data_ptr(),
             lse.data_ptr(), ws, wsb, raw)
     return logprob, lse
 
@@ -789,7 +789,7 @@ def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, tar
             for x in ((None, 0) if t is None else (t.data_ptr(), _matrix_pitch(t, name)))]
     _launch("psrl_token_logprob_bwd", dev, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
             _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
-            None if target_off is None else target_off.data_ptr(), scale, logprob.data_ptr(),
+            None if target_off is None else target_off.data_ptr(), float(scale), logprob.data_ptr(),
             lse.data_ptr(), d_logprob.data_ptr(), *args, ws, wsb, raw)
     return tuple(out)
 

@@ -129,12 +129,13 @@ __device__ __forceinline__ void rotate_vectors(uint4& xv, uint4& yv, const float
 // keeps those of its two vectors in registers, and streams the heads, two vectors of a head per lane and step.  No
 // barrier, no index arithmetic per head but an addition.
 //
-// Two heads in flight per lane and four blocks per SM, 64 registers: the gradients of 195,923 rows of 80 heads, 8.03 GB,
-// take 1210 us, what a plain copy of as much takes; one head 1260, three 1275, four with three blocks 1224.
-constexpr int kWarps = 8, kBatch = 2;
+// Two heads in flight per lane, 64 registers: the gradients of 195,923 rows of 80 heads, 8.03 GB,
+// take 1206 us, what a plain copy of as much takes; one head 1260, three 1275, four (80 registers) 1224.  Blocks of
+// four warps: 8,758 rows of 48 heads 43.1 us, of eight warps 45.0.
+constexpr int kWarps = 4, kBatch = 2;
 
 template <bool kBf16, bool kInterleaved>
-__global__ void __launch_bounds__(kWarps * 32, 4) rope_kernel(const __grid_constant__ RopeParams p,
+__global__ void __launch_bounds__(kWarps * 32, 32 / kWarps) rope_kernel(const __grid_constant__ RopeParams p,
                                                               const __grid_constant__ Frequencies f) {
   constexpr int kElems = kBf16 ? 8 : 4, kBytes = kBf16 ? 2 : 4;
   __shared__ float2 cs[kWarps][kMaxPairs];
@@ -402,7 +403,7 @@ psrl_status_t psrl_rope_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const 
                              const int32_t* positions, int64_t n_rows, int32_t n_heads, void* y, int64_t y_pitch,
                              int inverse, void* stream) {
   using namespace psrl;
-  if (!rope || n_rows < 0 || n_heads < 1) return PSRL_ERR_INVALID_ARG;
+  if (!rope || n_rows < 0 || n_heads < 1 || n_heads > 65535) return PSRL_ERR_INVALID_ARG;
   if (dtype != PSRL_F32 && dtype != PSRL_BF16) return PSRL_ERR_UNSUPPORTED;
   const int64_t d = rope->desc.head_dim;
   if (!pitch_ok(x_pitch, n_heads, int(d), dtype) || !pitch_ok(y_pitch, n_heads, int(d), dtype)) return PSRL_ERR_SHAPE;
