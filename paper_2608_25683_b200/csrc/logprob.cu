@@ -75,10 +75,8 @@ struct GemmParams {
   float2* part;                 // kLse: [unit column][group][M] (max, sum), powers of two
   int32_t* part_at;             // kLse: the vocabulary entry of the maximum
   const float2* row_info;       // kDz: per row (lse * log2(e), -scale * G)
-  const int32_t* targets;       // kDz
-  const int32_t* target_off;    // kDz: may be NULL (one target per row)
-  const float* entry;           // kDz: value of dz at every target
-  int32_t n_targets, col0;      // kDz: col0 = first vocabulary entry of the piece
+  const int2* only;             // kDz: per row its target and the bits of dz there, if it has exactly one; else (-1, 0)
+  int32_t col0;                 // kDz: first vocabulary entry of the piece
   int32_t vocab;                // kGrad: entries of the piece
   int32_t splits;               // kGrad: parts of d_hidden's sum over them
   int32_t acc_rows;             // kGrad: rows of one part's sums
@@ -258,6 +256,12 @@ struct TileOut {
   }
 };
 
+// dz rounded to bf16, or the rest below that
+__device__ __forceinline__ __nv_bfloat16 dz_part(float v, bool rest) {
+  const __nv_bfloat16 y = __float2bfloat16_rn(v);
+  return rest ? __float2bfloat16_rn(v - __bfloat162float(y)) : y;
+}
+
 template <Kind kKind>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
@@ -428,13 +432,12 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
       float best = -CUDART_INF_F, sum = 0.f;                       // kLse
       int best_at = 0;
       float lse2 = 0.f, coef = 0.f;                                // kDz
-      int t_begin = 0, t_end = 0, first_target = -1;
+      int2 only = make_int2(-1, 0);
       if (kKind == kDz && live) {
         const int user_row = p.row_of[of_row];
         const float2 ri = p.row_info[user_row];
         lse2 = ri.x; coef = ri.y;
-        target_range(p.target_off, user_row, p.n_targets, t_begin, t_end);
-        if (t_begin < t_end) first_target = p.targets[t_begin];
+        only = p.only[user_row];
       }
       for (int nt = w.nt; nt < nt_end; ++nt, ++tile) {
         if ((tile & 1) != uint32_t(group)) continue;
@@ -519,16 +522,12 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
               out.put(b, j, any ? make_uint4(o[0], o[1], o[2], o[3]) : make_uint4(0, 0, 0, 0));
             }
             if constexpr (kKind == kDz) {
-              // the row's targets inside these columns, over what this thread has just written
-              for (int t = t_begin; t < t_end; ++t) {
-                const uint32_t x = uint32_t(t == t_begin ? first_target : p.targets[t]) - uint32_t(p.col0 + col);
-                if (x < uint32_t(min(64, p.N - col))) {
-                  const float v = p.entry[t];
-                  __nv_bfloat16 y = __float2bfloat16_rn(v);
-                  if (rest) y = __float2bfloat16_rn(v - __bfloat162float(y));
-                  *reinterpret_cast<__nv_bfloat16*>(b + gt * 128 + (((x >> 3) ^ (gt & 7)) << 4) + (x & 7) * 2) = y;
-                }
-              }
+              // the row's target, where it is in these columns, over what this thread has just written (patch_kernel does it for
+              // rows with several: their number has no limit, and a tile would wait for its longest row)
+              const uint32_t x = uint32_t(only.x) - uint32_t(p.col0 + col);
+              if (x < uint32_t(min(64, p.N - col)))
+                *reinterpret_cast<__nv_bfloat16*>(b + gt * 128 + (((x >> 3) ^ (gt & 7)) << 4) + (x & 7) * 2) =
+                    dz_part(__int_as_float(only.y), rest);
             }
             out.send(kKind == kGrad ? &maps.out2 : &maps.out, col, row0, false);
           }
@@ -761,12 +760,30 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
 // targets with the same token.  Written as (g_t - G) - G (e^lp - 1): for a row with one token the first difference is
 // zero and nothing cancels as its probability nears one.  A warp per row; one bit per row says whether any gradient is not
 // zero.
+// Equal tokens: 32 targets at a time are compared across the warp; a row with more than that keeps its tokens' sums in a
+// hash table of twice as many places, and the warp adds one batch after the other, so the order of every sum is fixed.
 constexpr int kRowsPerByte = 8;
+struct TokenSum {
+  int32_t token;
+  float sum;
+};
+// the place of `token` in a table of `places` that has room; -1 is free
+__device__ __forceinline__ int place_of(volatile TokenSum* table, int places, int token, bool insert) {
+  uint32_t at = (uint32_t(token) * 2654435761u) % uint32_t(places);
+  for (int i = 0; i < places; ++i) {
+    const int seen = insert ? atomicCAS(const_cast<int32_t*>(&table[at].token), -1, token) : table[at].token;
+    if (seen == token || seen == -1) break;
+    at = at + 1 == uint32_t(places) ? 0 : at + 1;
+  }
+  return int(at);
+}
+
 __global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int vocab, const int32_t* __restrict__ targets,
                                                                  const int32_t* __restrict__ off, int n_targets,
                                                                  const float* __restrict__ logprob, const float* __restrict__ lse,
                                                                  const float* __restrict__ d_logprob, float scale,
-                                                                 float2* __restrict__ row_info, float* __restrict__ entry,
+                                                                 float2* __restrict__ row_info, int2* __restrict__ only,
+                                                                 float* __restrict__ entry, TokenSum* table,
                                                                  uint8_t* __restrict__ matters, int* __restrict__ status) {
   next_kernel_may_start();
   if (blockIdx.x == 0 && threadIdx.x == 0) *status = int(PSRL_OK);
@@ -789,23 +806,69 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int voca
     any = __any_sync(0xffffffffu, any);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    int2 one = make_int2(-1, 0);
     if (any) {
-      for (int t = b + lane; t < e; t += 32) {
-        const int y = targets[t];
-        if (y < 0 || y >= vocab) continue;   // no entry of dz belongs to it
-        float same = 0.f;
-        for (int u = b; u < e; ++u)
-          if (targets[u] == y) same += d_logprob[u];
-        entry[t] = scale * ((same - total) - total * expm1f(logprob[t]));
+      volatile TokenSum* mine = table + 2 * int64_t(b);   // read past the L1, which atomics do not update
+      const int places = 2 * (e - b);
+      const bool hashed = e - b > 32;
+      if (hashed) {
+        for (int i = lane; i < places; i += 32) { mine[i].token = -1; mine[i].sum = 0.f; }
+        __syncwarp();
+      }
+      for (int t0 = b; t0 < e; t0 += 32) {
+        const int t = t0 + lane;
+        const int y = t < e ? targets[t] : -1;
+        const bool valid = y >= 0 && y < vocab;
+        const float g = valid ? d_logprob[t] : 0.f;
+        const uint32_t same = __match_any_sync(0xffffffffu, valid ? y : -1 - lane);
+        float sum = 0.f;
+        for (int j = 0; j < 32; ++j) {
+          const float x = __shfl_sync(0xffffffffu, g, j);
+          if (same >> j & 1) sum += x;
+        }
+        if (!hashed) {
+          if (valid) {
+            const float v = scale * ((sum - total) - total * expm1f(logprob[t]));
+            entry[t] = v;
+            if (e - b == 1) one = make_int2(y, __float_as_int(v));
+          }
+        } else if (valid && lane == __ffs(same) - 1) {
+          volatile TokenSum& at = mine[place_of(mine, places, y, true)];   // one lane per token
+          at.sum = at.sum + sum;
+        }
+        __syncwarp();
+      }
+      if (hashed) {
+        __threadfence_block();
+        for (int t = b + lane; t < e; t += 32) {
+          const int y = targets[t];
+          if (y >= 0 && y < vocab)
+            entry[t] = scale * ((mine[place_of(mine, places, y, false)].sum - total) - total * expm1f(logprob[t]));
+        }
       }
     }
     if (lane == 0) {
       row_info[row] = make_float2(lse[row] * kLog2e, -scale * total);
+      only[row] = one;
       if (any) atomicOr(&s_bits, 1u << warp);
     }
   }
   __syncthreads();
   if (threadIdx.x == 0) matters[blockIdx.x] = uint8_t(s_bits);
+}
+
+// dz at the targets of the rows that have several, over what the product's epilogue has stored: one thread per target.
+__global__ void __launch_bounds__(256) patch_kernel(int n_targets, const int32_t* __restrict__ targets, const int32_t* __restrict__ row_at,
+                                                    const float* __restrict__ entry, const int32_t* __restrict__ count, int col0, int nv,
+                                                    int twice, __nv_bfloat16* __restrict__ dz, int64_t pitch) {
+  previous_kernel_done();
+  next_kernel_may_start();
+  const int t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= n_targets) return;
+  const uint32_t x = uint32_t(targets[t]) - uint32_t(col0), row = uint32_t(row_at[t]);
+  if (x >= uint32_t(nv) || row >= uint32_t(*count)) return;
+  dz[int64_t(row) * pitch + x] = dz_part(entry[t], false);
+  if (twice) dz[int64_t(row + 128) * pitch + x] = dz_part(entry[t], true);
 }
 
 // d_hidden from the parts of its sum, in order.
@@ -830,6 +893,7 @@ __global__ void __launch_bounds__(256) sum_kernel(const float4* __restrict__ acc
 __global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, int twice, const uint8_t* __restrict__ matters, const uint4* __restrict__ hidden,
                                                                    int64_t h_pitch_vecs, int vecs, uint4* __restrict__ gathered,
                                                                    int32_t* __restrict__ row_of, int32_t* __restrict__ count,
+                                                                   const int32_t* __restrict__ off, int n_targets, int32_t* __restrict__ row_at,
                                                                    uint4* __restrict__ d_hidden, int64_t dh_pitch_vecs) {
   __shared__ int s_before;
   if (threadIdx.x == 0) s_before = 0;
@@ -847,8 +911,15 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, int tw
   const uint32_t bits = matters[byte];
   const int at0 = s_before, row = byte * kRowsPerByte + warp;
   if (row < M) {
-    if (bits >> warp & 1) {
-      const int at = at0 + __popc(bits & ((1u << warp) - 1));
+    const bool mine = bits >> warp & 1;
+    const int at = at0 + __popc(bits & ((1u << warp) - 1));
+    if (off) {
+      // where the targets of a row with several of them are gathered to; -1: nothing for patch_kernel to do
+      int b, e;
+      target_range(off, row, n_targets, b, e);
+      for (int t = b + lane; t < e; t += 32) row_at[t] = mine && e - b > 1 ? at : -1;
+    }
+    if (mine) {
       if (lane == 0) row_of[at] = row;
 #pragma unroll 8
       for (int i = lane; i < vecs; i += 32) {
@@ -888,7 +959,7 @@ struct Layout {
   int64_t rows, acc_rows;        // rows that the backward's gathered buffers and the sums of d_hidden hold
   int32_t splits;                // parts of d_hidden's sums
   int32_t twice;                 // dz in two bf16 parts
-  size_t part, part_at, row_info, entry, matters, row_of, count, gathered, dz, acc, total;
+  size_t part, part_at, row_info, only, entry, table, row_at, matters, row_of, count, gathered, dz, acc, total;
 };
 
 // Columns of a tile of the logits.  Wide tiles use the tensor cores and the L2 best; with few tiles the rounds of the 74 pairs
@@ -933,7 +1004,10 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
     const int64_t pieces = (v + most_wide - 1) / most_wide;
     L.piece = round_up((v + pieces - 1) / pieces, 256);
     L.row_info = take(size_t(n) * sizeof(float2));
+    L.only = take(size_t(n) * sizeof(int2));
     L.entry = take(size_t(n_targets) * sizeof(float));
+    L.table = take(2 * size_t(n_targets) * sizeof(TokenSum));
+    L.row_at = take(size_t(n_targets) * sizeof(int32_t));
     L.twice = n <= kTwiceRows;
     L.rows = L.twice ? 256 : round_up(n, kBK);
     L.acc_rows = L.twice ? 256 : round_up(n, 128);
@@ -1108,14 +1182,16 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   base.scale_log2 = scale * kLog2e;
   base.twice = L.twice;
   float2* row_info = reinterpret_cast<float2*>(ws + L.row_info);
+  int2* only = reinterpret_cast<int2*>(ws + L.only);
   float* entry = reinterpret_cast<float*>(ws + L.entry);
+  int32_t* row_at = reinterpret_cast<int32_t*>(ws + L.row_at);
   __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + L.dz);
   float* acc = reinterpret_cast<float*>(ws + L.acc);
   const int64_t acc_pitch = round_up(hidden_dim, 32);
   const int32_t M = static_cast<int32_t>(n_rows);
   e = launch(rows_kernel, dim3(unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte)), kRowsPerByte * 32, 0, s, true, M, vocab, targets,
-             target_off, static_cast<int>(n_targets), logprob, lse, d_logprob, scale, row_info, entry,
-             reinterpret_cast<uint8_t*>(ws + L.matters), base.status);
+             target_off, static_cast<int>(n_targets), logprob, lse, d_logprob, scale, row_info, only, entry,
+             reinterpret_cast<TokenSum*>(ws + L.table), reinterpret_cast<uint8_t*>(ws + L.matters), base.status);
   if (e != cudaSuccess) return cuda_failed(e);
   __nv_bfloat16* gathered = reinterpret_cast<__nv_bfloat16*>(ws + L.gathered);
   base.count = reinterpret_cast<int32_t*>(ws + L.count);
@@ -1123,7 +1199,7 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   e = launch(gather_kernel, dim3(unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte)), kRowsPerByte * 32, 0, s, false, M, L.twice,
              reinterpret_cast<uint8_t*>(ws + L.matters), static_cast<const uint4*>(hidden), hidden_pitch / 8, hidden_dim / 8,
              reinterpret_cast<uint4*>(gathered), reinterpret_cast<int32_t*>(ws + L.row_of), reinterpret_cast<int32_t*>(ws + L.count),
-             static_cast<uint4*>(d_hidden), d_hidden_pitch / 8);
+             target_off, static_cast<int>(n_targets), row_at, static_cast<uint4*>(d_hidden), d_hidden_pitch / 8);
   if (e != cudaSuccess) return cuda_failed(e);
   const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(weight);
   for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
@@ -1143,11 +1219,15 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
       return PSRL_ERR_CUDA;
     GemmParams z = base;
     z.M = M; z.N = static_cast<int32_t>(nv); z.k_blocks = (hidden_dim + kBK - 1) / kBK;
-    z.row_info = row_info; z.targets = targets; z.target_off = target_off; z.entry = entry;
-    z.n_targets = static_cast<int32_t>(n_targets); z.col0 = static_cast<int32_t>(v0);
+    z.row_info = row_info; z.only = only; z.col0 = static_cast<int32_t>(v0);
     z.tile_n = L.tile_n;
     e = launch_gemm<kDz>(mz, z, false, s);
     if (e != cudaSuccess) return cuda_failed(e);
+    if (target_off && n_targets) {
+      e = launch(patch_kernel, dim3(unsigned((n_targets + 255) / 256)), 256, 0, s, false, static_cast<int>(n_targets), targets, row_at, entry,
+                 base.count, z.col0, static_cast<int>(nv), L.twice, dz, L.piece);
+      if (e != cudaSuccess) return cuda_failed(e);
+    }
     GemmParams g = base;
     g.M = M; g.N = hidden_dim; g.vocab = static_cast<int32_t>(nv);
     g.want_hidden = d_hidden != nullptr; g.want_weight = d_weight != nullptr;

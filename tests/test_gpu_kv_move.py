@@ -90,6 +90,12 @@ def test_offsets_past_32_bits(lib):
     for t, x in ((k, 1.0), (v, 2.0)):
         assert (t[:, cap - 80:cap - 32] == x).all() and (t[:, 5:37] == x).all() and (t[:, cap - 32:] == 0).all()
         assert (t[:, 37:cap - 80] == 0).all() and (t[:, :5] == 0).all()
+    # the same by the kernel for large moves, the whole of the last slots
+    for t in (k, v):
+        t[:, cap - 40000:] = torch.arange(40000, device="cuda")[:, None] % 251
+    lib.psrl_kv_move([[cap - 40000, cap - 40100, 40000]], k, v)
+    for t in (k, v):
+        assert (t[:, cap - 40100:cap - 100] == (torch.arange(40000, device="cuda") % 251).to(torch.bfloat16)[:, None]).all()
 
 
 def test_streams_graphs_and_empty_lists(lib):

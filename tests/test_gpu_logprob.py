@@ -112,6 +112,16 @@ def test_ragged_targets(lib, seed):
     assert empty.any() and (dh[empty] == 0).all()
 
 
+def test_a_row_with_very_many_targets(lib):
+    """300,000 targets in one row, most tokens many times over: the cost grows with their number, not with its square."""
+    n, h, v, k = 40, 64, 5000, 300000
+    hidden, weight, targets, g = make(n, h, v, 21, m=k + n)
+    off = torch.arange(n + 1, device="cuda", dtype=torch.int32)
+    off[8:] += k
+    targets[3000:4000] = -7
+    check(lib, hidden, weight, targets, g / 500, off)
+
+
 def test_no_targets_and_no_rows(lib):
     hidden, weight, targets, g = make(40, 64, 300, 3)
     none = torch.zeros(41, dtype=torch.int32, device="cuda")

@@ -98,7 +98,7 @@ def test_refusals(lib):
     rows = lambda *a: lib.STATUS_NAMES[L.psrl_rope_rows(*a)]
     good = [rope._h, 0, p, 64, p, 3, 1, p, 64, 0, None]
     assert rows(*change(1, 7)) == "PSRL_ERR_UNSUPPORTED"
-    assert rows(*change(2, None)) == rows(*change(4, None)) == rows(*change(5, -1)) == rows(*change(6, 0)) == "PSRL_ERR_INVALID_ARG"
+    assert rows(*change(2, None)) == rows(*change(4, None)) == rows(*change(5, -1)) == rows(*change(6, 0)) == rows(*change(6, 65536)) == "PSRL_ERR_INVALID_ARG"
     assert rows(*change(8, 68)) == "PSRL_ERR_INVALID_ARG"        # in place with two pitches
     assert rows(*change(3, 60)) == "PSRL_ERR_SHAPE"
     assert rows(*change(5, 0)) == "PSRL_OK"                      # no rows, nothing launched
