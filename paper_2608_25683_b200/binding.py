@@ -483,13 +483,39 @@ def _device_of(*tensors) -> int:
     return dev
 
 
+_torch_c = None
+
+
+def _cuda():
+    """torch's C module, looked up once: small calls are bound by the host's time."""
+    global _torch_c
+    if _torch_c is None:
+        import torch
+
+        _torch_c = torch._C
+    return _torch_c
+
+
+_type_codes = None
+
+
+def _type_code(t):
+    """PSRL_F32, PSRL_BF16 or None."""
+    global _type_codes
+    if _type_codes is None:
+        import torch
+
+        _type_codes = {torch.float32: PSRL_F32, torch.bfloat16: PSRL_BF16}
+    return _type_codes.get(t.dtype)
+
+
 def _stream_on(stream, dev: int):
     """(raw stream handle of a call on device `dev`, torch stream to keep temporaries for or None).  Without a stream it is
     torch's current one of that device; the raw handle skips a Stream object, a third of a small call's host time."""
+    if stream is None:
+        return _cuda()._cuda_getCurrentRawStream(dev), None
     import torch
 
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(dev), None
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=dev)
     elif stream.device.index != dev:
@@ -506,12 +532,12 @@ def _kept(t, stream):
 
 def _launch(name: str, dev: int, *args):
     """One C call with the tensors' device as the current one: the library launches there."""
-    import torch
-
-    fn = getattr(lib(), name)
-    if dev == torch._C._cuda_getDevice():
+    fn = getattr(_lib or lib(), name)
+    if dev == _cuda()._cuda_getDevice():
         st = fn(*args)
     else:
+        import torch
+
         with torch.cuda.device(dev):
             st = fn(*args)
     if st != PSRL_OK:
@@ -623,25 +649,26 @@ def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None
 
 def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stream=None):
     """Rotates x [rows, heads, head_dim] (f32 or bf16, rows at any pitch) at int32 `positions` [rows].  Returns y (y may be x)."""
-    import torch
-
-    dt = {torch.float32: PSRL_F32, torch.bfloat16: PSRL_BF16}.get(x.dtype)
+    dt = _type_code(x)
     if dt is None:
         raise TypeError(f"dtype {x.dtype} is neither float32 nor bfloat16")
-    if x.dim() != 3:
+    shape = x.shape
+    if len(shape) != 3:
         raise ValueError("x must be [rows, heads, head_dim]")
-    if positions.dtype != torch.int32 or positions.shape != x.shape[:1] or not positions.is_contiguous():
+    rows, heads, _ = shape
+    if str(positions.dtype) != "torch.int32" or positions.shape != shape[:1] or not positions.is_contiguous():
         raise ValueError("positions must be contiguous int32 [rows]")
-    rows, heads = x.shape[0], x.shape[1]
     px = _rows_pitch(x, rows, heads, rope.head_dim, "x")
     dev = _device_of(x, positions)
     raw, keep = _stream_on(stream, dev)
     if y is None:
-        y = _kept(torch.empty(x.shape, dtype=x.dtype, device=x.device), keep)
-    elif y.dtype != x.dtype or y.device != x.device:
+        import torch
+
+        y = _kept(torch.empty(shape, dtype=x.dtype, device=x.device), keep)
+    elif y.dtype is not x.dtype or y.get_device() != dev:
         raise ValueError("y must have x's type and device")
     _launch("psrl_rope_rows", dev, rope._h, dt, x.data_ptr(), px, positions.data_ptr(), rows, heads, y.data_ptr(),
-            _rows_pitch(y, rows, heads, rope.head_dim, "y"), int(bool(inverse)), raw)
+            px if y is x else _rows_pitch(y, rows, heads, rope.head_dim, "y"), 1 if inverse else 0, raw)
     return y
 
 
@@ -663,7 +690,7 @@ def _extents(extents):
 def _pair_of_pools(k, v, what: str):
     """(heads, capacity, bytes of a slot and head) of two pools of one shape."""
     shape, size = k.shape, k.element_size()
-    if str(k.dtype) not in ("torch.bfloat16", "torch.float32") or v.dtype != k.dtype:
+    if _type_code(k) is None or v.dtype is not k.dtype:
         raise TypeError(f"{what} must both be float32 or both bfloat16")
     if len(shape) != 3 or shape != v.shape or not k.is_contiguous() or not v.is_contiguous():
         raise ValueError(f"{what} must be contiguous [Hkv, capacity, d] of one shape")
@@ -688,13 +715,13 @@ def psrl_kv_copy(extents, k_src, v_src, k_dst, v_dst, stream=None):
 def psrl_kv_move(moves, k_pool, v_pool, stream=None, workspace=None):
     """Performs the moves of a compaction ([n, 3], ascending, downwards: Cache.compact()) inside the pools, as if every
     source were read first.  `workspace`: (pointer, bytes) of 256 bytes of device memory; allocated if not given."""
-    import torch
-
     heads, cap, row = _pair_of_pools(k_pool, v_pool, "pools")
     e, n, at = _extents(moves)
     dev = _device_of(k_pool, v_pool)
     raw, keep = _stream_on(stream, dev)
     if workspace is None:
+        import torch
+
         buf = _kept(torch.empty(512, dtype=torch.uint8, device=k_pool.device), keep)
         workspace = ((buf.data_ptr() + 255) // 256 * 256, 256)
     _launch("psrl_kv_move", dev, at, n, heads, row, k_pool.data_ptr(), v_pool.data_ptr(), cap, workspace[0], workspace[1],

@@ -30,6 +30,7 @@ struct Pools {
 
 // ------------------------------------------------------------------------------------------------ disjoint copies
 
+constexpr int kShortList = 64, kLongList = 1000;   // extents that travel in a launch's parameters
 constexpr int kCopyThreads = 256, kCopyPiece = 1024;  // vectors of one block: 16 KB, four per thread
 
 template <int kMax>
@@ -88,7 +89,7 @@ psrl_status_t launch_copies(const psrl_kv_extent_t* ext, int32_t n, const Pools&
 
 psrl_status_t copy_extents(const psrl_kv_extent_t* ext, int32_t n, const Pools& p, cudaStream_t stream) {
   // a short list costs a launch less parameter traffic
-  return n <= 64 ? launch_copies<64>(ext, n, p, stream) : launch_copies<1000>(ext, n, p, stream);
+  return n <= kShortList ? launch_copies<kShortList>(ext, n, p, stream) : launch_copies<kLongList>(ext, n, p, stream);
 }
 
 // ------------------------------------------------------------------------------------------------ moves in place
@@ -112,14 +113,14 @@ psrl_status_t copy_extents(const psrl_kv_extent_t* ext, int32_t n, const Pools& 
 
 constexpr int kMoveThreads = 512, kMoveRegs = 8;           // small moves: 64 KB per block and chunk
 constexpr int kWarpVecs = 32 * kMoveRegs;                  // a warp's part of a chunk: 4 KB of consecutive vectors
-constexpr int kMoveMax = 1000;
 constexpr int kClusterMax = 8;
 
+template <int kMax>
 struct MoveList {
   int32_t n;
   int32_t slots;              // sum of the extents
-  int32_t src[kMoveMax], dst[kMoveMax];
-  int32_t first[kMoveMax + 1];  // slots before the extent
+  int32_t src[kMax], dst[kMax];
+  int32_t first[kMax + 1];    // slots before the extent
 };
 
 // A warp's part of a chunk: its vectors, and in lane i where its row i (slot of one pool and head) goes.
@@ -129,7 +130,8 @@ struct Held {
   int32_t pool;
 };
 
-__device__ __forceinline__ void load_part(const MoveList& list, const Pools& p, uint32_t warp_part, uint32_t total_rows, Held& h) {
+template <class List>
+__device__ __forceinline__ void load_part(const List& list, const Pools& p, uint32_t warp_part, uint32_t total_rows, Held& h) {
   const int lane = threadIdx.x & 31;
   const uint32_t rows = kWarpVecs / p.vecs;
   const uint64_t row0 = uint64_t(warp_part) * rows;
@@ -184,7 +186,8 @@ __device__ __forceinline__ void store_part(const Pools& p, const Held& h) {
   }
 }
 
-__global__ void __launch_bounds__(kMoveThreads, 1) move_cluster_kernel(const __grid_constant__ MoveList list, const Pools p,
+template <int kMax>
+__global__ void __launch_bounds__(kMoveThreads, 1) move_cluster_kernel(const __grid_constant__ MoveList<kMax> list, const Pools p,
                                                                        int* ws, uint32_t n_chunks, uint32_t total_rows, bool first) {
   const uint32_t warps = gridDim.x * (kMoveThreads / 32);
   const uint32_t mine = blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5);
@@ -223,8 +226,8 @@ __device__ __forceinline__ int extent_of(const int32_t* starts, int n, int at) {
   }
   return lo;
 }
-template <class F>
-__device__ __forceinline__ void for_pieces(const MoveList& list, const Pools& p, uint32_t row, uint32_t end, F f) {
+template <class List, class F>
+__device__ __forceinline__ void for_pieces(const List& list, const Pools& p, uint32_t row, uint32_t end, F f) {
   if (row >= end) return;
   uint32_t ph = row / uint32_t(list.slots);
   int s = int(row - ph * uint32_t(list.slots));
@@ -244,7 +247,8 @@ __device__ __forceinline__ void for_pieces(const MoveList& list, const Pools& p,
 }
 
 // ws[0] status, ws[8] the next part, ws[16 + g % kRing] parts of group g that have been loaded (never reset)
-__global__ void __launch_bounds__(kBulkWarps * 32, 1) move_bulk_kernel(const __grid_constant__ MoveList list, const Pools p, int* ws,
+template <int kMax>
+__global__ void __launch_bounds__(kBulkWarps * 32, 1) move_bulk_kernel(const __grid_constant__ MoveList<kMax> list, const Pools p, int* ws,
                                                                        uint32_t n_parts, uint32_t total_rows) {
   extern __shared__ __align__(128) uint8_t part_mem[];
   __shared__ uint64_t landed[kBulkWarps];
@@ -321,8 +325,9 @@ __global__ void __launch_bounds__(kBulkWarps * 32, 1) move_bulk_kernel(const __g
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // copies in flight come to rest before the block's memory is given back
 }
 
+template <int kMax>
 psrl_status_t move_extents(const psrl_kv_extent_t* ext, int32_t n, Pools p, int* ws, bool first, cudaStream_t stream) {
-  MoveList list;
+  MoveList<kMax> list;
   list.n = n;
   int64_t slots = 0;
   for (int32_t i = 0; i < n; ++i) {
@@ -353,10 +358,10 @@ psrl_status_t move_extents(const psrl_kv_extent_t* ext, int32_t n, Pools p, int*
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = grid;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    e = cudaLaunchKernelEx(&cfg, move_cluster_kernel, list, p, ws, n_chunks, total, first);
+    e = cudaLaunchKernelEx(&cfg, move_cluster_kernel<kMax>, list, p, ws, n_chunks, total, first);
   } else {
     static bool done[64] = {};
-    e = ensure_dynamic_smem(move_bulk_kernel, kBulkSmem, done);
+    e = ensure_dynamic_smem(move_bulk_kernel<kMax>, kBulkSmem, done);
     const int64_t part_rows = kBulkBytes / (int64_t(p.vecs) * 16), parts = (rows + part_rows - 1) / part_rows;
     const int64_t grid = std::min<int64_t>(std::min(resident_ctas(), kSpan * kGroup / kBulkWarps), (parts + kBulkWarps - 1) / kBulkWarps);
     // a group has to be at work as a whole: a device with fewer warps than that would wait for parts that nobody has taken
@@ -369,7 +374,7 @@ psrl_status_t move_extents(const psrl_kv_extent_t* ext, int32_t n, Pools p, int*
     // a later part of a long list keeps the status of the parts before
     const size_t keep = first ? 0 : 8 * sizeof(int);
     if (e == cudaSuccess) e = cudaMemsetAsync(reinterpret_cast<char*>(ws) + keep, 0, kWsHeaderBytes - keep, stream);
-    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, move_bulk_kernel, list, p, ws, static_cast<uint32_t>(parts), total);
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, move_bulk_kernel<kMax>, list, p, ws, static_cast<uint32_t>(parts), total);
   }
   if (e != cudaSuccess) { set_last_cuda_error(e); return PSRL_ERR_CUDA; }
   return PSRL_OK;
@@ -488,9 +493,13 @@ psrl_status_t psrl_kv_move(const psrl_kv_extent_t* extents, int32_t n_extents, i
     }
     const Pools p{static_cast<const uint4*>(k_pool), static_cast<const uint4*>(v_pool), static_cast<uint4*>(k_pool),
                   static_cast<uint4*>(v_pool), pool_capacity, pool_capacity, n_kv_heads, row_bytes / 16};
-    for (size_t at = 0; at < list.size(); at += kMoveMax) {
-      const psrl_status_t st = move_extents(list.data() + at, static_cast<int32_t>(std::min(list.size() - at, size_t(kMoveMax))), p,
-                                            static_cast<int*>(workspace), at == 0, s);
+    // a short list costs a launch less parameter traffic
+    const bool few = list.size() <= kShortList;
+    for (size_t at = 0; at < list.size(); at += kLongList) {
+      const int32_t n = static_cast<int32_t>(std::min(list.size() - at, size_t(kLongList)));
+      int* ws = static_cast<int*>(workspace);
+      const psrl_status_t st = few ? move_extents<kShortList>(list.data() + at, n, p, ws, at == 0, s)
+                                   : move_extents<kLongList>(list.data() + at, n, p, ws, at == 0, s);
       if (st != PSRL_OK) return st;
     }
   } catch (const std::bad_alloc&) {
