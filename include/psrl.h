@@ -382,7 +382,9 @@ psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off
  *   logprob, d_logprob [n_targets], lse [n_rows] DEVICE fp32 (backward: as produced by the forward)
  *   d_hidden, d_weight  DEVICE bf16 as their tensors, fully overwritten; NULL: not wanted
  *   workspace  DEVICE, >= psrl_token_logprob_workspace_bytes, 256-byte aligned; holds the device status word.  Forward:
- *              a few floats per row; backward: about the size of six times `hidden`, whatever the vocabulary.
+ *              at most 12 bytes per row and 128 entries of the vocabulary (1024 where there are thousands of rows);
+ *              backward: 16 KB per row, or 128 MB if that is more, for a piece of dz, three times `hidden`, and 24 bytes
+ *              per target, whatever the vocabulary.
  * hidden_dim and the pitches are multiples of 8, tensors 16-byte aligned, tensors must not overlap outputs.
  * n_rows = 0 does nothing (backward: zeroes d_weight).
  * Errors: INVALID_ARG, SHAPE, WORKSPACE, CUDA.  Asynchronous; calls that may overlap on the GPU need distinct workspaces.

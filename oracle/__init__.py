@@ -11,6 +11,10 @@ shares no code with the CUDA path.
                 sequence and run through naive softmax attention, forward and
                 backward, in fp64; results are scattered back to the shared
                 layout.
+  rope.py       rotary positions as complex rotations, frequencies of the long-
+                context scalings.
+  logprob.py    token log-probabilities and gradients row by row; the tokens a
+                tree's rows predict, from its samples.
 
 Pins (what each function is checked against, other than itself) are listed in
 the header of each module.

@@ -1017,9 +1017,10 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
     L.gathered = take(size_t(L.rows) * h * 2);
     L.dz = take(size_t(L.rows) * L.piece * 2);
     // Parts of d_hidden's sum: with few rows there are fewer of its tiles than pairs of CTAs, and each is as deep as the
-    // piece; four units for every pair, of at least 16 steps, share that out.
+    // piece; two units for every pair, of at least 16 steps, share that out (777 rows, half of them without targets, one unit
+    // for every pair 462 us, two 426, four 432).
     const int64_t tiles = m_tiles * ((h + 255) / 256), most = std::min<int64_t>(16, L.piece / kBK / 16);
-    L.splits = tiles >= 148 ? 1 : static_cast<int32_t>(std::max<int64_t>(1, std::min(most, (296 + tiles - 1) / tiles)));
+    L.splits = tiles >= 74 ? 1 : static_cast<int32_t>(std::max<int64_t>(1, std::min(most, (148 + tiles - 1) / tiles)));
     L.acc = take(size_t(L.splits) * L.acc_rows * round_up(h, 32) * sizeof(float));
   }
   L.total = at;
