@@ -373,30 +373,32 @@ psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off
  * Backward: G_r = the sum of d_logprob over row r's targets,
  *   dz[r, v] = scale * (sum of d_logprob over r's targets equal to v  -  G_r exp(z[r, v] - lse[r]))
  *   d_hidden = dz weight,  d_weight = dz^T hidden
- * sums in fp32, dz rounded to bf16 as the tensor cores' operand, results rounded once.  Bitwise reproducible.  A row
+ * sums in fp32; bf16: dz rounded to bf16 as the tensor cores' operand (up to 128 rows in two parts), results rounded once;
+ * f32: fp32 arithmetic throughout, as in the library's other fp32 paths (for parity; not tuned).  Bitwise reproducible.  A row
  * without a target, or whose d_logprob are all zero, contributes nothing (d_hidden row zero), whatever it holds, and costs
  * nothing but its place in the workspace.
- *   hidden   [n_rows, hidden_dim] DEVICE bf16, row pitch in elements;  weight [vocab, hidden_dim] DEVICE bf16
+ *   hidden   [n_rows, hidden_dim] DEVICE of `dtype`, row pitch in elements;  weight [vocab, hidden_dim] DEVICE of `dtype`
  *   targets  [n_targets] DEVICE int32;  target_off [n_rows + 1] DEVICE int32, not descending from 0 to n_targets, or NULL
  *   scale    finite, not 0 (1 / temperature)
  *   logprob, d_logprob [n_targets], lse [n_rows] DEVICE fp32 (backward: as produced by the forward)
- *   d_hidden, d_weight  DEVICE bf16 as their tensors, fully overwritten; NULL: not wanted
+ *   d_hidden, d_weight  DEVICE of `dtype` as their tensors, fully overwritten; NULL: not wanted
  *   workspace  DEVICE, >= psrl_token_logprob_workspace_bytes, 256-byte aligned; holds the device status word.  Forward:
  *              at most 12 bytes per row and 128 entries of the vocabulary (1024 where there are thousands of rows);
  *              backward: 16 KB per row, or 128 MB if that is more, for a piece of dz, three times `hidden`, and 24 bytes
  *              per target, whatever the vocabulary.
- * hidden_dim and the pitches are multiples of 8, tensors 16-byte aligned, tensors must not overlap outputs.
+ * hidden_dim is a multiple of 8, pitches are multiples of 16 bytes, tensors 16-byte aligned and apart from the outputs.
  * n_rows = 0 does nothing (backward: zeroes d_weight).
- * Errors: INVALID_ARG, SHAPE, WORKSPACE, CUDA.  Asynchronous; calls that may overlap on the GPU need distinct workspaces.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), WORKSPACE, CUDA.  Asynchronous; calls that may overlap on the GPU need
+ * distinct workspaces.
  */
-size_t psrl_token_logprob_workspace_bytes(int64_t n_rows, int32_t hidden_dim, int32_t vocab, int64_t n_targets,
-                                          int backward);
-psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
-                                     int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
+size_t psrl_token_logprob_workspace_bytes(psrl_dtype_t dtype, int64_t n_rows, int32_t hidden_dim, int32_t vocab,
+                                          int64_t n_targets, int backward);
+psrl_status_t psrl_token_logprob_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t hidden_dim, int32_t vocab,
+                                     const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
                                      const int32_t* targets, int64_t n_targets, const int32_t* target_off, float scale,
                                      float* logprob, float* lse, void* workspace, size_t workspace_bytes, void* stream);
-psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
-                                     int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
+psrl_status_t psrl_token_logprob_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t hidden_dim, int32_t vocab,
+                                     const void* hidden, int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
                                      const int32_t* targets, int64_t n_targets, const int32_t* target_off, float scale,
                                      const float* logprob, const float* lse, const float* d_logprob, void* d_hidden,
                                      int64_t d_hidden_pitch, void* d_weight, int64_t d_weight_pitch, void* workspace,

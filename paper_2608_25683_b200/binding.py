@@ -202,9 +202,9 @@ def lib() -> C.CDLL:
     L.psrl_rope_rows.restype = C.c_int
     L.psrl_plan_next_tokens.argtypes = [_VP, C.POINTER(_I32P), C.POINTER(_I32P)]
     L.psrl_plan_next_tokens.restype = C.c_int
-    L.psrl_token_logprob_workspace_bytes.argtypes = [_I64, C.c_int32, C.c_int32, _I64, C.c_int]
+    L.psrl_token_logprob_workspace_bytes.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, _I64, C.c_int]
     L.psrl_token_logprob_workspace_bytes.restype = C.c_size_t
-    lp = [_I64, C.c_int32, C.c_int32, _VP, _I64, _VP, _I64, _VP, _I64, _VP, C.c_float, _VP, _VP]
+    lp = [C.c_int, _I64, C.c_int32, C.c_int32, _VP, _I64, _VP, _I64, _VP, _I64, _VP, C.c_float, _VP, _VP]
     L.psrl_token_logprob_fwd.argtypes = lp + [_VP, C.c_size_t, _VP]
     L.psrl_token_logprob_fwd.restype = C.c_int
     L.psrl_token_logprob_bwd.argtypes = lp + [_VP, _VP, _I64, _VP, _I64, _VP, C.c_size_t, _VP]
@@ -728,8 +728,9 @@ def psrl_kv_move(moves, k_pool, v_pool, stream=None, workspace=None):
             raw)
 
 
-def psrl_token_logprob_workspace_bytes(n_rows: int, hidden_dim: int, vocab: int, n_targets: int, backward: bool) -> int:
-    return int(lib().psrl_token_logprob_workspace_bytes(int(n_rows), int(hidden_dim), int(vocab), int(n_targets),
+def psrl_token_logprob_workspace_bytes(n_rows: int, hidden_dim: int, vocab: int, n_targets: int, backward: bool,
+                                       dtype: str = "bf16") -> int:
+    return int(lib().psrl_token_logprob_workspace_bytes(PSRL_F32 if dtype == "f32" else PSRL_BF16, int(n_rows), int(hidden_dim), int(vocab), int(n_targets),
                                                         int(bool(backward))))
 
 
@@ -737,8 +738,9 @@ def _logprob_args(hidden, weight, targets, target_off, floats):
     """Checks shared by the two directions; the shape arguments of the C call."""
     import torch
 
-    if hidden.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
-        raise TypeError("hidden and weight must be bfloat16")
+    dt = _type_code(hidden)
+    if dt is None or weight.dtype is not hidden.dtype:
+        raise TypeError("hidden and weight must both be bfloat16 or both float32")
     if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
         raise ValueError("hidden must be [rows, hidden_dim], weight [vocab, hidden_dim]")
     n, h = hidden.shape
@@ -748,21 +750,21 @@ def _logprob_args(hidden, weight, targets, target_off, floats):
     for name, t, count in floats:
         if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (count,) or not t.is_contiguous()):
             raise ValueError(f"{name} must be a contiguous float32 vector of {count}")
-    return n, h, weight.shape[0], targets.shape[0]
+    return dt, n, h, weight.shape[0], targets.shape[0]
 
 
 def _matrix_pitch(t, name: str) -> int:
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8   # one row: any pitch will do
 
 
-def _logprob_workspace(workspace, keep, n, h, v, m, backward, device):
+def _logprob_workspace(workspace, keep, dt, n, h, v, m, backward, device):
     import torch
 
     if workspace is not None:
         return workspace
-    need = psrl_token_logprob_workspace_bytes(n, h, v, m, backward)
+    need = int(lib().psrl_token_logprob_workspace_bytes(dt, n, h, v, m, backward))
     buf = _kept(torch.empty(need + 256, dtype=torch.uint8, device=device), keep)
     return (buf.data_ptr() + 255) // 256 * 256, need
 
@@ -770,11 +772,11 @@ def _logprob_workspace(workspace, keep, n, h, v, m, backward, device):
 def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: float = 1.0, logprob=None, lse=None, stream=None,
                            workspace=None):
     """Log-probabilities of `targets` (int32) under softmax(scale * hidden weight^T), without storing the logits.  hidden
-    [rows, H], weight [vocab, H] bf16; row r's targets are targets[target_off[r] : target_off[r + 1]], or targets[r] without
+    [rows, H], weight [vocab, H], both bf16 or both f32; row r's targets are targets[target_off[r] : target_off[r + 1]], or targets[r] without
     target_off.  Returns (logprob [targets], lse [rows]), fp32."""
     import torch
 
-    n, h, v, m = _logprob_args(hidden, weight, targets, target_off, [])
+    dt, n, h, v, m = _logprob_args(hidden, weight, targets, target_off, [])
     _logprob_args(hidden, weight, targets, target_off, [("logprob", logprob, m), ("lse", lse, n)])
     given = [t for t in (target_off, logprob, lse) if t is not None]
     dev = _device_of(hidden, weight, targets, *given)
@@ -783,8 +785,8 @@ def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: floa
         logprob = _kept(torch.empty(m, dtype=torch.float32, device=hidden.device), keep)
     if lse is None:
         lse = _kept(torch.empty(n, dtype=torch.float32, device=hidden.device), keep)
-    ws, wsb = _logprob_workspace(workspace, keep, n, h, v, m, False, hidden.device)
-    _launch("psrl_token_logprob_fwd", dev, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
+    ws, wsb = _logprob_workspace(workspace, keep, dt, n, h, v, m, False, hidden.device)
+    _launch("psrl_token_logprob_fwd", dev, dt, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
             _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
             None if target_off is None else target_off.data_ptr(), float(scale), logprob.data_ptr(),
             lse.data_ptr(), ws, wsb, raw)
@@ -793,28 +795,28 @@ def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: floa
 
 def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, target_off=None, scale: float = 1.0, d_hidden=None,
                            d_weight=None, want_hidden: bool = True, want_weight: bool = True, stream=None, workspace=None):
-    """Gradients of the above: (d_hidden, d_weight), bf16, given d_logprob [targets] and the forward's logprob and lse.
+    """Gradients of the above: (d_hidden, d_weight), of hidden's type, given d_logprob [targets] and the forward's logprob and lse.
     want_hidden / want_weight False: that one is None and not computed."""
     import torch
 
     m = targets.shape[0]
-    n, h, v, m = _logprob_args(hidden, weight, targets, target_off,
-                               [("logprob", logprob, m), ("lse", lse, hidden.shape[0]), ("d_logprob", d_logprob, m)])
+    dt, n, h, v, m = _logprob_args(hidden, weight, targets, target_off,
+                                   [("logprob", logprob, m), ("lse", lse, hidden.shape[0]), ("d_logprob", d_logprob, m)])
     for name, t, like in (("d_hidden", d_hidden, hidden), ("d_weight", d_weight, weight)):
-        if t is not None and (t.dtype != torch.bfloat16 or t.shape != like.shape):
-            raise ValueError(f"{name} must be bfloat16 {tuple(like.shape)}")
+        if t is not None and (t.dtype is not hidden.dtype or t.shape != like.shape):
+            raise ValueError(f"{name} must be {hidden.dtype} {tuple(like.shape)}")
     given = [t for t in (target_off, d_hidden, d_weight) if t is not None]
     dev = _device_of(hidden, weight, targets, logprob, lse, d_logprob, *given)
     raw, keep = _stream_on(stream, dev)
     if d_hidden is None and want_hidden:
-        d_hidden = _kept(torch.empty((n, h), dtype=torch.bfloat16, device=hidden.device), keep)
+        d_hidden = _kept(torch.empty((n, h), dtype=hidden.dtype, device=hidden.device), keep)
     if d_weight is None and want_weight:
-        d_weight = _kept(torch.empty((v, h), dtype=torch.bfloat16, device=hidden.device), keep)
+        d_weight = _kept(torch.empty((v, h), dtype=hidden.dtype, device=hidden.device), keep)
     out = [t if w else None for t, w in ((d_hidden, want_hidden), (d_weight, want_weight))]
-    ws, wsb = _logprob_workspace(workspace, keep, n, h, v, m, True, hidden.device)
+    ws, wsb = _logprob_workspace(workspace, keep, dt, n, h, v, m, True, hidden.device)
     args = [x for t, name in zip(out, ("d_hidden", "d_weight"))
             for x in ((None, 0) if t is None else (t.data_ptr(), _matrix_pitch(t, name)))]
-    _launch("psrl_token_logprob_bwd", dev, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
+    _launch("psrl_token_logprob_bwd", dev, dt, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
             _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
             None if target_off is None else target_off.data_ptr(), float(scale), logprob.data_ptr(),
             lse.data_ptr(), d_logprob.data_ptr(), *args, ws, wsb, raw)

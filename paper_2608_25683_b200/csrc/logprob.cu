@@ -655,6 +655,26 @@ __global__ void __launch_bounds__(kFewThreads) few_rows_kernel(int M, int vecs, 
 // 20 is about 3e-5 short.  That matters where one entry carries the sum - a confident row, whose log-probability is the
 // small difference of two such numbers - so the largest entry's logit is computed again, in fp32, and its term replaced:
 // lse of 8192 rows of 4096 deep products 3.0e-6 -> 6.3e-7 relative to 64 bits.
+__device__ __forceinline__ float warp_sum(f32x2 acc) {
+  float z, z1;
+  split_f32x2(acc, z, z1);
+  z += z1;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+  return z;
+}
+// dot product of two rows of `vecs` 16-byte vectors, for the whole warp
+__device__ __forceinline__ float warp_dot(const float* x, const float* y, int vecs) {
+  const float4 *xv = reinterpret_cast<const float4*>(x), *yv = reinterpret_cast<const float4*>(y);
+  f32x2 acc = make_f32x2(0.f, 0.f);
+#pragma unroll 4
+  for (int i = threadIdx.x & 31; i < vecs; i += 32) {
+    const float4 a = xv[i], b = yv[i];
+    acc = fma2(make_f32x2(a.x, a.y), make_f32x2(b.x, b.y), acc);
+    acc = fma2(make_f32x2(a.z, a.w), make_f32x2(b.z, b.w), acc);
+  }
+  return warp_sum(acc);
+}
 __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfloat16* y, int vecs) {
   const uint4 *xv = reinterpret_cast<const uint4*>(x), *yv = reinterpret_cast<const uint4*>(y);
   f32x2 acc = make_f32x2(0.f, 0.f);
@@ -666,19 +686,14 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* x, const __nv_bfl
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc = fma2(a[j], b[j], acc);
   }
-  float z, z1;
-  split_f32x2(acc, z, z1);
-  z += z1;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-  return z;
+  return warp_sum(acc);
 }
 
 constexpr int kFinalThreads = 256;
-template <int kRows>
+template <int kRows, class T>
 __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __restrict__ part, const int32_t* __restrict__ part_at, int n_parts, int M, int hidden_dim,
-                                                              int vocab, const __nv_bfloat16* __restrict__ hidden, int64_t h_pitch,
-                                                              const __nv_bfloat16* __restrict__ weight, int64_t w_pitch,
+                                                              int vocab, const T* __restrict__ hidden, int64_t h_pitch,
+                                                              const T* __restrict__ weight, int64_t w_pitch,
                                                               const int32_t* __restrict__ targets, const int32_t* __restrict__ off,
                                                               int n_targets, float scale, float* __restrict__ logprob,
                                                               float* __restrict__ lse) {
@@ -690,7 +705,7 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
   const int row0 = blockIdx.x * kRows, mine = threadIdx.x % kRows, slice = threadIdx.x / kRows, row = row0 + mine;
   // The targets' logits need nothing of the kernel before: they are computed while it runs out.  Target number `at` of the
   // block's rows is warp at % kWarps's.
-  const int vecs = hidden_dim / 8;
+  const int vecs = hidden_dim / int(16 / sizeof(T));
   int at = 0;
   for (int r = 0; r < kRows && row0 + r < M; ++r) {
     int b, e;
@@ -858,17 +873,22 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) rows_kernel(int M, int voca
 }
 
 // dz at the targets of the rows that have several, over what the product's epilogue has stored: one thread per target.
+template <class T>
 __global__ void __launch_bounds__(256) patch_kernel(int n_targets, const int32_t* __restrict__ targets, const int32_t* __restrict__ row_at,
                                                     const float* __restrict__ entry, const int32_t* __restrict__ count, int col0, int nv,
-                                                    int twice, __nv_bfloat16* __restrict__ dz, int64_t pitch) {
+                                                    int twice, T* __restrict__ dz, int64_t pitch) {
   previous_kernel_done();
   next_kernel_may_start();
   const int t = blockIdx.x * 256 + threadIdx.x;
   if (t >= n_targets) return;
   const uint32_t x = uint32_t(targets[t]) - uint32_t(col0), row = uint32_t(row_at[t]);
   if (x >= uint32_t(nv) || row >= uint32_t(*count)) return;
-  dz[int64_t(row) * pitch + x] = dz_part(entry[t], false);
-  if (twice) dz[int64_t(row + 128) * pitch + x] = dz_part(entry[t], true);
+  if constexpr (sizeof(T) == 4) {
+    dz[int64_t(row) * pitch + x] = entry[t];
+  } else {
+    dz[int64_t(row) * pitch + x] = dz_part(entry[t], false);
+    if (twice) dz[int64_t(row + 128) * pitch + x] = dz_part(entry[t], true);
+  }
 }
 
 // d_hidden from the parts of its sum, in order.
@@ -943,6 +963,14 @@ __global__ void __launch_bounds__(kRowsPerByte * 32) gather_kernel(int M, int tw
   }
 }
 
+}  // namespace
+}  // namespace psrl
+
+#include "logprob_f32.cuh"
+
+namespace psrl {
+namespace {
+
 // ------------------------------------------------------------------------------------------------- host side
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
@@ -975,7 +1003,8 @@ int tile_columns(int64_t m_tiles, int64_t v, int64_t k_blocks, int pairs) {
   return best;
 }
 
-Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward) {
+Layout layout(psrl_dtype_t dtype, int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward) {
+  const bool f32 = dtype == PSRL_F32;
   Layout L{};
   const int64_t m_tiles = (n + 255) / 256;
   // the forward's tiles; the backward's of the logits too while all rows are one tile (how many of them matter is not known here)
@@ -984,7 +1013,12 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
   L.n_tiles = static_cast<int32_t>((v + L.tile_n - 1) / L.tile_n);
   size_t at = kWsHeaderBytes;
   auto take = [&](size_t bytes) { const size_t a = at; at += (bytes + 255) / 256 * 256; return a; };
-  if (!backward) {
+  if (!backward && f32) {
+    const int64_t blocks = ((n + kF32Tile - 1) / kF32Tile) * ((v + kF32Tile - 1) / kF32Tile);
+    L.run = static_cast<int32_t>(std::min<int64_t>(16, std::max<int64_t>(1, blocks / (8 * resident_ctas()))));
+    L.n_parts = static_cast<int32_t>((v + int64_t(kF32Tile) * L.run - 1) / (int64_t(kF32Tile) * L.run));
+    L.part = take(size_t(L.n_parts) * n * sizeof(float2));
+  } else if (!backward) {
     // short runs while there are few tiles (they balance the pairs of CTAs), long ones to keep the partials small
     const int64_t tiles = m_tiles * L.n_tiles;
     L.run = static_cast<int32_t>(std::min<int64_t>(kMaxRun, std::max<int64_t>(1, tiles / (pairs * 16))));
@@ -1008,20 +1042,21 @@ Layout layout(int64_t n, int64_t h, int64_t v, int64_t n_targets, bool backward)
     L.entry = take(size_t(n_targets) * sizeof(float));
     L.table = take(2 * size_t(n_targets) * sizeof(TokenSum));
     L.row_at = take(size_t(n_targets) * sizeof(int32_t));
-    L.twice = n <= kTwiceRows;
+    L.twice = !f32 && n <= kTwiceRows;
     L.rows = L.twice ? 256 : round_up(n, kBK);
     L.acc_rows = L.twice ? 256 : round_up(n, 128);
     L.matters = take(size_t(n + 7) / 8 + 3);
     L.row_of = take(size_t(n) * sizeof(int32_t));
     L.count = take(sizeof(int32_t));
-    L.gathered = take(size_t(L.rows) * h * 2);
-    L.dz = take(size_t(L.rows) * L.piece * 2);
+    const size_t es = f32 ? 4 : 2;
+    L.gathered = take(size_t(L.rows) * h * es);
+    L.dz = take(size_t(L.rows) * L.piece * es);
     // Parts of d_hidden's sum: with few rows there are fewer of its tiles than pairs of CTAs, and each is as deep as the
     // piece; two units for every pair, of at least 16 steps, share that out (777 rows, half of them without targets, one unit
     // for every pair 462 us, two 426, four 432).
     const int64_t tiles = m_tiles * ((h + 255) / 256), most = std::min<int64_t>(16, L.piece / kBK / 16);
     L.splits = tiles >= 74 ? 1 : static_cast<int32_t>(std::max<int64_t>(1, std::min(most, (148 + tiles - 1) / tiles)));
-    L.acc = take(size_t(L.splits) * L.acc_rows * round_up(h, 32) * sizeof(float));
+    if (!f32) L.acc = take(size_t(L.splits) * L.acc_rows * round_up(h, 32) * sizeof(float));
   }
   L.total = at;
   return L;
@@ -1069,6 +1104,13 @@ cudaError_t launch_few(const Layout& L, int32_t M, int32_t h, int32_t v, const v
                 hp / 8, static_cast<const uint4*>(weight), wp / 8, scale * kLog2e, part, status);
 }
 
+template <F32Kind kKind>
+cudaError_t launch_f32(const F32Params& p, int64_t col_blocks, int64_t rows, bool first, cudaStream_t stream) {
+  const int64_t row_blocks = (rows + kF32Tile - 1) / kF32Tile;
+  if (row_blocks > 65535 || col_blocks > INT32_MAX) return cudaErrorInvalidValue;
+  return launch(f32_kernel<kKind>, dim3(unsigned(col_blocks), unsigned(row_blocks)), 256, 0, stream, first, p);
+}
+
 psrl_status_t cuda_failed(cudaError_t e) {
   set_last_cuda_error(e);
   return PSRL_ERR_CUDA;
@@ -1076,13 +1118,16 @@ psrl_status_t cuda_failed(cudaError_t e) {
 
 bool al16(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool al4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
-bool pitch16(int64_t pitch, int64_t cols) { return pitch >= cols && pitch % 8 == 0 && pitch <= (int64_t(1) << 36); }
+// elements of a 16-byte vector
+int64_t vec_of(psrl_dtype_t t) { return t == PSRL_BF16 ? 8 : 4; }
+bool pitch16(psrl_dtype_t t, int64_t pitch, int64_t cols) { return pitch >= cols && pitch % vec_of(t) == 0 && pitch <= (int64_t(1) << 36); }
 
 // Shared checks of both directions; PSRL_OK with n_rows == 0 means there is nothing to do.
-psrl_status_t check(int64_t n, int32_t h, int32_t v, const void* hidden, int64_t hp, const void* weight, int64_t wp,
+psrl_status_t check(psrl_dtype_t t, int64_t n, int32_t h, int32_t v, const void* hidden, int64_t hp, const void* weight, int64_t wp,
                     const int32_t* targets, int64_t n_targets, const int32_t* off, float scale) {
+  if (t != PSRL_BF16 && t != PSRL_F32) return PSRL_ERR_UNSUPPORTED;
   if (n < 0 || n_targets < 0 || n > INT32_MAX - 512 || n_targets > INT32_MAX - 512) return PSRL_ERR_INVALID_ARG;
-  if (h < 8 || h % 8 || v < 1 || v > INT32_MAX - 512 || !pitch16(hp, h) || !pitch16(wp, h)) return PSRL_ERR_SHAPE;
+  if (h < 8 || h % 8 || v < 1 || v > INT32_MAX - 512 || !pitch16(t, hp, h) || !pitch16(t, wp, h)) return PSRL_ERR_SHAPE;
   if (!off && n_targets != n) return PSRL_ERR_SHAPE;
   if (!(scale == scale) || scale == 0.f || scale > 1e30f || scale < -1e30f) return PSRL_ERR_INVALID_ARG;
   if (n == 0) return PSRL_OK;
@@ -1095,21 +1140,22 @@ psrl_status_t check(int64_t n, int32_t h, int32_t v, const void* hidden, int64_t
 
 extern "C" {
 
-size_t psrl_token_logprob_workspace_bytes(int64_t n_rows, int32_t hidden_dim, int32_t vocab, int64_t n_targets, int backward) {
+size_t psrl_token_logprob_workspace_bytes(psrl_dtype_t dtype, int64_t n_rows, int32_t hidden_dim, int32_t vocab, int64_t n_targets,
+                                          int backward) {
   if (n_rows < 0 || hidden_dim < 1 || vocab < 1 || n_targets < 0) return 0;
   if (n_rows == 0) return psrl::kWsHeaderBytes;
-  return psrl::layout(n_rows, hidden_dim, vocab, n_targets, backward != 0).total;
+  return psrl::layout(dtype, n_rows, hidden_dim, vocab, n_targets, backward != 0).total;
 }
 
-psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
+psrl_status_t psrl_token_logprob_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
                                      int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
                                      const int32_t* targets, int64_t n_targets, const int32_t* target_off, float scale,
                                      float* logprob, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   using namespace psrl;
-  psrl_status_t st = check(n_rows, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, targets, n_targets, target_off, scale);
+  psrl_status_t st = check(dtype, n_rows, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, targets, n_targets, target_off, scale);
   if (st != PSRL_OK) return st;
   if (!ptr_aligned(workspace, 256)) return PSRL_ERR_INVALID_ARG;
-  if (workspace_bytes < psrl_token_logprob_workspace_bytes(n_rows, hidden_dim, vocab, n_targets, 0)) return PSRL_ERR_WORKSPACE;
+  if (workspace_bytes < psrl_token_logprob_workspace_bytes(dtype, n_rows, hidden_dim, vocab, n_targets, 0)) return PSRL_ERR_WORKSPACE;
   if (n_rows && (!al4(lse) || (n_targets && !al4(logprob)))) return PSRL_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
@@ -1117,13 +1163,20 @@ psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t
     e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);   // otherwise the first kernel clears the status
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
-  const Layout L = layout(n_rows, hidden_dim, vocab, n_targets, false);
+  const Layout L = layout(dtype, n_rows, hidden_dim, vocab, n_targets, false);
   char* ws = static_cast<char*>(workspace);
   float2* part = reinterpret_cast<float2*>(ws + L.part);
   int32_t* part_at = reinterpret_cast<int32_t*>(ws + L.part_at);
   int* status = reinterpret_cast<int*>(ws);
   const int32_t M = static_cast<int32_t>(n_rows);
-  if (L.few) {
+  if (dtype == PSRL_F32) {
+    e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+    if (e != cudaSuccess) return cuda_failed(e);
+    F32Params p{};
+    p.a = static_cast<const float*>(hidden); p.a_pitch = hidden_pitch; p.b = static_cast<const float*>(weight); p.b_pitch = weight_pitch;
+    p.M = M; p.N = vocab; p.K = hidden_dim; p.scale_log2 = scale * kLog2e; p.part = part; p.run = L.run;
+    e = launch_f32<kF32Lse>(p, L.n_parts, n_rows, true, s);
+  } else if (L.few) {
     e = L.few == 1 ? launch_few<1>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, status, s)
       : L.few == 2 ? launch_few<2>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, status, s)
                    : launch_few<4>(L, M, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, scale, part, status, s);
@@ -1147,36 +1200,47 @@ psrl_status_t psrl_token_logprob_fwd(int64_t n_rows, int32_t hidden_dim, int32_t
   if (e != cudaSuccess) return cuda_failed(e);
   // rows of a block: 32 read the partials in whole lines; with few rows more threads to each of them finish sooner
   const int rows = M >= 4096 ? 32 : M >= 256 ? 4 : 1;
-  auto final = rows == 32 ? final_kernel<32> : rows == 4 ? final_kernel<4> : final_kernel<1>;
-  e = launch(final, dim3(unsigned((M + rows - 1) / rows)), kFinalThreads, 0, s, false, part, L.few ? nullptr : part_at, L.n_parts, M, hidden_dim, vocab,
+  const dim3 grid(unsigned((M + rows - 1) / rows));
+  if (dtype == PSRL_F32) {
+    auto final = rows == 32 ? final_kernel<32, float> : rows == 4 ? final_kernel<4, float> : final_kernel<1, float>;
+    e = launch(final, grid, kFinalThreads, 0, s, false, part, nullptr, L.n_parts, M, hidden_dim, vocab, static_cast<const float*>(hidden),
+               hidden_pitch, static_cast<const float*>(weight), weight_pitch, targets, target_off, static_cast<int>(n_targets), scale,
+               logprob, lse);
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
+  using Bf = __nv_bfloat16;
+  auto final = rows == 32 ? final_kernel<32, Bf> : rows == 4 ? final_kernel<4, Bf> : final_kernel<1, Bf>;
+  e = launch(final, grid, kFinalThreads, 0, s, false, part, L.few ? nullptr : part_at, L.n_parts, M, hidden_dim, vocab,
              static_cast<const __nv_bfloat16*>(hidden), hidden_pitch, static_cast<const __nv_bfloat16*>(weight), weight_pitch, targets,
              target_off, static_cast<int>(n_targets), scale, logprob, lse);
   return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
 }
 
-psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
+psrl_status_t psrl_token_logprob_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t hidden_dim, int32_t vocab, const void* hidden,
                                      int64_t hidden_pitch, const void* weight, int64_t weight_pitch,
                                      const int32_t* targets, int64_t n_targets, const int32_t* target_off, float scale,
                                      const float* logprob, const float* lse, const float* d_logprob, void* d_hidden,
                                      int64_t d_hidden_pitch, void* d_weight, int64_t d_weight_pitch, void* workspace,
                                      size_t workspace_bytes, void* stream) {
   using namespace psrl;
-  psrl_status_t st = check(n_rows, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, targets, n_targets, target_off, scale);
+  psrl_status_t st = check(dtype, n_rows, hidden_dim, vocab, hidden, hidden_pitch, weight, weight_pitch, targets, n_targets, target_off, scale);
   if (st != PSRL_OK) return st;
   if (!ptr_aligned(workspace, 256) || (d_hidden && !al16(d_hidden)) || (d_weight && !al16(d_weight))) return PSRL_ERR_INVALID_ARG;
-  if ((d_hidden && !pitch16(d_hidden_pitch, hidden_dim)) || (d_weight && !pitch16(d_weight_pitch, hidden_dim))) return PSRL_ERR_SHAPE;
-  if (workspace_bytes < psrl_token_logprob_workspace_bytes(n_rows, hidden_dim, vocab, n_targets, 1)) return PSRL_ERR_WORKSPACE;
+  if ((d_hidden && !pitch16(dtype, d_hidden_pitch, hidden_dim)) || (d_weight && !pitch16(dtype, d_weight_pitch, hidden_dim))) return PSRL_ERR_SHAPE;
+  if (workspace_bytes < psrl_token_logprob_workspace_bytes(dtype, n_rows, hidden_dim, vocab, n_targets, 1)) return PSRL_ERR_WORKSPACE;
   if (n_rows && (!al4(lse) || (n_targets && (!al4(logprob) || !al4(d_logprob))))) return PSRL_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   if (n_rows == 0 || (!d_hidden && !d_weight)) e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);   // otherwise the first kernel clears the status
   if (e != cudaSuccess) return cuda_failed(e);
+  const size_t es = dtype == PSRL_F32 ? 4 : 2;
+  const int64_t vec = vec_of(dtype);
   if (n_rows == 0) {
-    if (d_weight) e = cudaMemset2DAsync(d_weight, size_t(d_weight_pitch) * 2, 0, size_t(hidden_dim) * 2, vocab, s);
+    if (d_weight) e = cudaMemset2DAsync(d_weight, size_t(d_weight_pitch) * es, 0, size_t(hidden_dim) * es, vocab, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
   if (!d_hidden && !d_weight) return PSRL_OK;
-  const Layout L = layout(n_rows, hidden_dim, vocab, n_targets, true);
+  const Layout L = layout(dtype, n_rows, hidden_dim, vocab, n_targets, true);
   char* ws = static_cast<char*>(workspace);
   GemmParams base{};
   base.status = reinterpret_cast<int*>(ws);
@@ -1198,10 +1262,41 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
   base.count = reinterpret_cast<int32_t*>(ws + L.count);
   base.row_of = reinterpret_cast<int32_t*>(ws + L.row_of);
   e = launch(gather_kernel, dim3(unsigned((n_rows + kRowsPerByte - 1) / kRowsPerByte)), kRowsPerByte * 32, 0, s, false, M, L.twice,
-             reinterpret_cast<uint8_t*>(ws + L.matters), static_cast<const uint4*>(hidden), hidden_pitch / 8, hidden_dim / 8,
+             reinterpret_cast<uint8_t*>(ws + L.matters), static_cast<const uint4*>(hidden), hidden_pitch / vec, static_cast<int>(hidden_dim / vec),
              reinterpret_cast<uint4*>(gathered), reinterpret_cast<int32_t*>(ws + L.row_of), reinterpret_cast<int32_t*>(ws + L.count),
-             target_off, static_cast<int>(n_targets), row_at, static_cast<uint4*>(d_hidden), d_hidden_pitch / 8);
+             target_off, static_cast<int>(n_targets), row_at, static_cast<uint4*>(d_hidden), d_hidden_pitch / vec);
   if (e != cudaSuccess) return cuda_failed(e);
+  if (dtype == PSRL_F32) {
+    const float *hf = reinterpret_cast<const float*>(ws + L.gathered), *wf = static_cast<const float*>(weight);
+    float* zf = reinterpret_cast<float*>(ws + L.dz);
+    for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
+      const int32_t nv = static_cast<int32_t>(std::min<int64_t>(L.piece, vocab - v0));
+      F32Params p{};
+      p.count = base.count; p.row_of = base.row_of; p.scale_log2 = base.scale_log2; p.row_info = row_info; p.only = only;
+      p.col0 = static_cast<int32_t>(v0); p.first = v0 == 0;
+      F32Params z = p;
+      z.a = hf; z.a_pitch = hidden_dim; z.b = wf + v0 * weight_pitch; z.b_pitch = weight_pitch;
+      z.M = M; z.N = nv; z.K = hidden_dim; z.out = zf; z.out_pitch = L.piece;
+      e = launch_f32<kF32Dz>(z, (nv + kF32Tile - 1) / kF32Tile, n_rows, false, s);
+      if (e == cudaSuccess && target_off && n_targets)
+        e = launch(patch_kernel<float>, dim3(unsigned((n_targets + 255) / 256)), 256, 0, s, false, static_cast<int>(n_targets), targets, row_at,
+                   entry, base.count, p.col0, static_cast<int>(nv), 0, zf, L.piece);
+      if (e == cudaSuccess && d_hidden) {
+        F32Params g = p;
+        g.a = zf; g.a_pitch = L.piece; g.b = wf + v0 * weight_pitch; g.b_pitch = weight_pitch;
+        g.M = M; g.N = hidden_dim; g.K = nv; g.out = static_cast<float*>(d_hidden); g.out_pitch = d_hidden_pitch;
+        e = launch_f32<kF32Dh>(g, (hidden_dim + kF32Tile - 1) / kF32Tile, n_rows, false, s);
+      }
+      if (e == cudaSuccess && d_weight) {
+        F32Params g = p;
+        g.a = zf; g.a_pitch = L.piece; g.b = hf; g.b_pitch = hidden_dim;
+        g.M = nv; g.N = hidden_dim; g.out = static_cast<float*>(d_weight) + v0 * d_weight_pitch; g.out_pitch = d_weight_pitch;
+        e = launch_f32<kF32Dw>(g, (hidden_dim + kF32Tile - 1) / kF32Tile, nv, false, s);
+      }
+      if (e != cudaSuccess) return cuda_failed(e);
+    }
+    return PSRL_OK;
+  }
   const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(weight);
   for (int64_t v0 = 0; v0 < vocab; v0 += L.piece) {
     const int64_t nv = std::min<int64_t>(L.piece, vocab - v0);
@@ -1225,7 +1320,7 @@ psrl_status_t psrl_token_logprob_bwd(int64_t n_rows, int32_t hidden_dim, int32_t
     e = launch_gemm<kDz>(mz, z, false, s);
     if (e != cudaSuccess) return cuda_failed(e);
     if (target_off && n_targets) {
-      e = launch(patch_kernel, dim3(unsigned((n_targets + 255) / 256)), 256, 0, s, false, static_cast<int>(n_targets), targets, row_at, entry,
+      e = launch(patch_kernel<__nv_bfloat16>, dim3(unsigned((n_targets + 255) / 256)), 256, 0, s, false, static_cast<int>(n_targets), targets, row_at, entry,
                  base.count, z.col0, static_cast<int>(nv), L.twice, dz, L.piece);
       if (e != cudaSuccess) return cuda_failed(e);
     }

@@ -8,6 +8,7 @@ Error bounds, with A = max over v of |scale| sum_i |h_i w_vi| of the row:
             dz = scale (g_t - G p) with p = exp(lp): an error e of lp moves it by |scale G| p e, whatever is left of dz
             itself where p is near 1, so scale |G| e (e as for logprob) times the other operand is added there
   products  sums in fp32 as above over K terms, then half a bf16 step of the result
+  f32       the same with K terms added one by one in fp32 (K 2^-24) and half steps of 2^-24
 Sums of absolute values come from the oracle."""
 import numpy as np
 import pytest
@@ -21,19 +22,23 @@ from util import build_plan, to_np
 pytestmark = pytest.mark.gpu
 
 
-def make(n, h, v, seed, scale=1.0, off=None, m=None, spread=1.0):
+def make(n, h, v, seed, m=None, spread=1.0, dtype=torch.bfloat16):
     g = torch.Generator(device="cuda").manual_seed(seed)
     rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")
-    hidden = rnd(n, h).to(torch.bfloat16)
-    weight = (rnd(v, h) * (spread / np.sqrt(h))).to(torch.bfloat16)
+    hidden = rnd(n, h).to(dtype)
+    weight = (rnd(v, h) * (spread / np.sqrt(h))).to(dtype)
     m = n if m is None else m
     targets = torch.randint(0, v, (m,), generator=g, device="cuda").to(torch.int32)
     return hidden, weight, targets, rnd(m)
 
 
-def bounds(hidden, weight, scale, want):
+def sum_error(k, dtype):
+    return (k / 16 + 8) * 2.0 ** -22 if dtype == torch.bfloat16 else (k + 8) * 2.0 ** -24
+
+
+def bounds(hidden, weight, scale, want, dtype=torch.bfloat16):
     a = np.abs(scale) * (np.abs(hidden) @ np.abs(weight).T).max(1)
-    z = (hidden.shape[1] / 16 + 8) * 2.0 ** -22 * a
+    z = sum_error(hidden.shape[1], dtype) * a
     return z, z + 2.0 ** -20 + 2.0 ** -22 * np.abs(want["lse"])
 
 
@@ -42,7 +47,8 @@ def check(lib, hidden, weight, targets, g, off=None, scale=1.0, **kw):
     on = None if off is None else off.cpu().numpy()
     want = oracle_logprob(hn, wn, tn, on, scale, to_np(g))
     lp, lse = lib.psrl_token_logprob_fwd(hidden, weight, targets, off, scale=scale, **kw)
-    zerr, lerr = bounds(hn, wn, scale, want)
+    half = 2.0 ** -8 if hidden.dtype == torch.bfloat16 else 2.0 ** -24
+    zerr, lerr = bounds(hn, wn, scale, want, hidden.dtype)
     assert (np.abs(to_np(lse) - want["lse"]) <= lerr).all()
     row = np.arange(len(hn)) if on is None else np.repeat(np.arange(len(hn)), np.diff(on))
     size = np.abs(want["logprob"]) + 2 * np.abs(want["lse"][row])
@@ -54,10 +60,11 @@ def check(lib, hidden, weight, targets, g, off=None, scale=1.0, **kw):
     moved = np.zeros((len(hn), len(wn)))           # what lp's error does to dz at the targets
     np.maximum.at(moved, (row[on_target], tn[on_target]), (np.abs(scale * total[row]) * lperr)[on_target])
     dh, dw = lib.psrl_token_logprob_bwd(hidden, weight, targets, lp, lse, g, off, scale=scale, **kw)
-    pe = (lerr + zerr).max() * 2 + 2.0 ** -8 + 2.0 ** -18
+    assert dh.dtype == dw.dtype == hidden.dtype
+    pe = (lerr + zerr).max() * 2 + half + 2.0 ** -18
     for got, d, absd, k, far in ((dh, want["d_hidden"], want["dh_abs"], len(wn), moved @ np.abs(wn)),
                                  (dw, want["d_weight"], want["dw_abs"], len(hn), moved.T @ np.abs(hn))):
-        tol = far + (pe + (k / 16 + 24) * 2.0 ** -22) * absd + 2.0 ** -8 * np.abs(d) * (1 + 2.0 ** -7) + 1e-37
+        tol = far + (pe + sum_error(k, hidden.dtype) + 2.0 ** -18) * absd + half * np.abs(d) * (1 + 2.0 ** -7) + 1e-37
         err = np.abs(to_np(got) - d) - tol
         assert err.max() <= 0, (float(err.max()), float(np.abs(d).max()))
     return lp, lse, dh, dw
@@ -69,6 +76,45 @@ def check(lib, hidden, weight, targets, g, off=None, scale=1.0, **kw):
 def test_one_target_per_row(lib, n, h, v, scale):
     hidden, weight, targets, g = make(n, h, v, n + h + v)
     check(lib, hidden, weight, targets, g, scale=scale)
+
+
+@pytest.mark.parametrize("n,h,v", [(1, 8, 1), (3, 72, 255), (64, 64, 64), (65, 136, 130), (130, 40, 1000), (33, 256, 5000), (700, 16, 3001)])
+@pytest.mark.parametrize("scale", [1.0, -0.4])
+def test_fp32(lib, n, h, v, scale):
+    hidden, weight, targets, g = make(n, h, v, n + h + v, dtype=torch.float32)
+    check(lib, hidden, weight, targets, g, scale=scale)
+
+
+def test_fp32_ragged_and_strided(lib):
+    """Rows with none, one and several targets, slices of wider matrices, several pieces of the vocabulary."""
+    rng = np.random.default_rng(2)
+    n, h, v = 9000, 16, 9001
+    count = rng.choice([0, 1, 1, 2], n)
+    off = torch.as_tensor(np.concatenate([[0], np.cumsum(count)]).astype(np.int32), device="cuda")
+    hidden, weight, targets, g = make(n, h, v, 22, m=int(count.sum()), dtype=torch.float32)
+    targets[::50] = -1
+    wide = torch.full((n, h + 12), float("nan"), device="cuda")
+    wide[:, 4:4 + h] = hidden
+    lp, lse = lib.psrl_token_logprob_fwd(wide[:, 4:4 + h], weight, targets, off)
+    out = torch.full_like(wide, 5.0)
+    dh, dw = lib.psrl_token_logprob_bwd(wide[:, 4:4 + h], weight, targets, lp, lse, g, off, d_hidden=out[:, 4:4 + h])
+    assert (out[:, :4] == 5).all() and (out[:, 4 + h:] == 5).all()
+    hd, wd = hidden.double(), weight.double()
+    z = hd @ wd.T
+    ref = torch.logsumexp(z, 1)
+    assert ((lse.double() - ref).abs() <= 2.0 ** -19 + 2.0 ** -21 * ref.abs()).all()
+    row = torch.repeat_interleave(torch.arange(n, device="cuda"), torch.as_tensor(count, device="cuda"))
+    keep = targets >= 0
+    want = (z[row, targets.long().clamp(min=0)] - ref[row]) * keep
+    assert ((lp.double() - want).abs() <= 2.0 ** -18 + 2.0 ** -21 * want.abs()).all()
+    total = torch.zeros(n, device="cuda", dtype=torch.float64).index_add_(0, row, g.double() * keep)
+    dz = -total[:, None] * torch.exp(z - ref[:, None])
+    dz.index_put_((row, targets.long().clamp(min=0)), g.double() * keep, accumulate=True)
+    # at the targets: |G| times the error of lp (below 2^-18 + 2^-21 x 25 < 2^-16) times the other operand
+    big, t = (total[row].abs() * keep)[:, None] * 2.0 ** -16, targets.long().clamp(min=0)
+    far_h, far_w = (torch.zeros_like(x).index_add_(0, i, big * y[j].abs()) for x, i, y, j in ((hd, row, wd, t), (wd, t, hd, row)))
+    for got, d, absd, k, far in ((dh, dz @ wd, dz.abs() @ wd.abs(), v, far_h), (dw, dz.T @ hd, dz.abs().T @ hd.abs(), n, far_w)):
+        assert ((got.double() - d).abs() <= (sum_error(k, torch.float32) + 2.0 ** -16) * absd + far).all()
 
 
 def test_confident_rows(lib):
@@ -250,8 +296,9 @@ def test_device_status_and_wrapper_refusals(lib):
     lp, lse = lib.psrl_token_logprob_fwd(hidden, weight, targets, workspace=ws)
     lib.psrl_token_logprob_bwd(hidden, weight, targets, lp, lse, g, workspace=ws)
     assert lib.lib().psrl_device_status(ctypes.c_void_p(ws[0]), None) == 0
-    with pytest.raises(TypeError):
-        lib.psrl_token_logprob_fwd(hidden.float(), weight, targets)
+    for x, w in ((hidden.float(), weight), (hidden.half(), weight.half())):
+        with pytest.raises(TypeError):
+            lib.psrl_token_logprob_fwd(x, w, targets)
     for bad in (dict(targets=targets.long()), dict(weight=weight[:, :56]), dict(target_off=targets), dict(lse=lse[:3])):
         with pytest.raises(ValueError):
             lib.psrl_token_logprob_fwd(**{**dict(hidden=hidden, weight=weight, targets=targets), **bad})

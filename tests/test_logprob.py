@@ -61,9 +61,10 @@ def test_refusals(lib):
     buf = ctypes.create_string_buffer(8192)
     p = (ctypes.addressof(buf) + 255) // 256 * 256
     big = 1 << 40
-    good = [4, 64, 100, p, 64, p, 64, p, 4, None, 1.0, p, p, p, big, None]
+    good = [1, 4, 64, 100, p, 64, p, 64, p, 4, None, 1.0, p, p, p, big, None]
     fwd = lambda *a: lib.STATUS_NAMES[L.psrl_token_logprob_fwd(*a)]
-    change = lambda i, v: good[:i] + [v] + good[i + 1:]
+    change = lambda i, v: good[:i + 1] + [v] + good[i + 2:]
+    assert fwd(*change(-1, 2)) == "PSRL_ERR_UNSUPPORTED"
     for i, v in [(0, -1), (3, None), (3, p + 8), (5, p + 2), (7, None), (9, p + 2), (10, 0.0), (10, float("nan")),
                  (10, float("inf")), (13, None), (13, p + 16)]:
         assert fwd(*change(i, v)) == "PSRL_ERR_INVALID_ARG", (i, v)
@@ -71,7 +72,7 @@ def test_refusals(lib):
         assert fwd(*change(i, v)) == "PSRL_ERR_SHAPE", (i, v)
     assert fwd(*change(14, 255)) == "PSRL_ERR_WORKSPACE"
     need = lib.psrl_token_logprob_workspace_bytes(4, 64, 100, 4, True)
-    good = [4, 64, 100, p, 64, p, 64, p, 4, None, 1.0, p, p, p, p, 64, p, 64, p, need, None]
+    good = [1, 4, 64, 100, p, 64, p, 64, p, 4, None, 1.0, p, p, p, p, 64, p, 64, p, need, None]
     bwd = lambda *a: lib.STATUS_NAMES[L.psrl_token_logprob_bwd(*a)]
     assert bwd(*change(19, need - 1)) == "PSRL_ERR_WORKSPACE"
     assert bwd(*change(14, p + 4)) == bwd(*change(16, p + 8)) == bwd(*change(18, p + 8)) == "PSRL_ERR_INVALID_ARG"
