@@ -387,7 +387,7 @@ psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off
  *              backward: 16 KB per row, or 128 MB if that is more, for a piece of dz, three times `hidden`, and 24 bytes
  *              per target, whatever the vocabulary.
  * hidden_dim is a multiple of 8, pitches are multiples of 16 bytes, tensors 16-byte aligned and apart from the outputs.
- * n_rows = 0 does nothing (backward: zeroes d_weight).
+ * n_rows = 0 does nothing (backward: zeroes d_weight).  Rows, targets and vocabulary are at most 2^30.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), WORKSPACE, CUDA.  Asynchronous; calls that may overlap on the GPU need
  * distinct workspaces.
  */

@@ -523,11 +523,15 @@ def _stream_on(stream, dev: int):
     return stream.cuda_stream, stream
 
 
-def _kept(t, stream):
-    """A tensor made for this call: not to be reused before the call's stream has passed it."""
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+def _new(stream, shape, dtype, device):
+    """A tensor made for a call.  With a stream of its own the call's tensors come from that stream's memory: memory that
+    the current stream gave back may still be in use there."""
+    import torch
+
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _launch(name: str, dev: int, *args):
@@ -597,8 +601,6 @@ def _rope_pools(plan, *pools):
 def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=None, stream=None):
     """Rotates the query rows' Q [T_q, Hq, d] into q_out and their K, V [T_q, Hkv, d] into the pools (K rotated), in one
     launch.  q, k, v may be slices of one projection output (rows at any pitch).  Returns q_out."""
-    import torch
-
     V, d = plan.view, plan.head_dim
     _check_dtype(plan, q, k, v, k_pool, v_pool)
     pq = _rows_pitch(q, V["T_q"], plan.n_q_heads, d, "q")
@@ -608,7 +610,7 @@ def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=Non
     _plan_device(plan, dev)
     raw, keep = _stream_on(stream, dev)
     if q_out is None:
-        q_out = _kept(torch.empty((V["T_q"], plan.n_q_heads, d), dtype=q.dtype, device=q.device), keep)
+        q_out = _new(keep, (V["T_q"], plan.n_q_heads, d), q.dtype, q.device)
     else:
         _check_dtype(plan, q_out)
         if q_out.shape != q.shape or not q_out.is_contiguous() or q_out.device != q.device:
@@ -621,8 +623,6 @@ def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=Non
 def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None, dk_out=None, dv_out=None, stream=None):
     """The way back: inverse rotation of d_q and of the query rows' slots of dk_pool, and the rows' slots of dv_pool, to
     dq_out [T_q, Hq, d], dk_out, dv_out [T_q, Hkv, d] (which may be slices of one gradient matrix).  Returns the three."""
-    import torch
-
     V, d = plan.view, plan.head_dim
     _check_dtype(plan, d_q, dk_pool, dv_pool)
     if d_q.shape != (V["T_q"], plan.n_q_heads, d) or not d_q.is_contiguous():
@@ -634,7 +634,7 @@ def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None
     outs, pitch = [], []
     for t, heads, name in ((dq_out, plan.n_q_heads, "dq_out"), (dk_out, plan.n_kv_heads, "dk_out"), (dv_out, plan.n_kv_heads, "dv_out")):
         if t is None:
-            t = _kept(torch.empty((V["T_q"], heads, d), dtype=d_q.dtype, device=d_q.device), keep)
+            t = _new(keep, (V["T_q"], heads, d), d_q.dtype, d_q.device)
         else:
             _check_dtype(plan, t)
             if t.device != d_q.device:
@@ -662,9 +662,7 @@ def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stre
     dev = _device_of(x, positions)
     raw, keep = _stream_on(stream, dev)
     if y is None:
-        import torch
-
-        y = _kept(torch.empty(shape, dtype=x.dtype, device=x.device), keep)
+        y = _new(keep, shape, x.dtype, x.device)
     elif y.dtype is not x.dtype or y.get_device() != dev:
         raise ValueError("y must have x's type and device")
     _launch("psrl_rope_rows", dev, rope._h, dt, x.data_ptr(), px, positions.data_ptr(), rows, heads, y.data_ptr(),
@@ -722,7 +720,7 @@ def psrl_kv_move(moves, k_pool, v_pool, stream=None, workspace=None):
     if workspace is None:
         import torch
 
-        buf = _kept(torch.empty(512, dtype=torch.uint8, device=k_pool.device), keep)
+        buf = _new(keep, 512, torch.uint8, k_pool.device)
         workspace = ((buf.data_ptr() + 255) // 256 * 256, 256)
     _launch("psrl_kv_move", dev, at, n, heads, row, k_pool.data_ptr(), v_pool.data_ptr(), cap, workspace[0], workspace[1],
             raw)
@@ -765,7 +763,7 @@ def _logprob_workspace(workspace, keep, dt, n, h, v, m, backward, device):
     if workspace is not None:
         return workspace
     need = int(lib().psrl_token_logprob_workspace_bytes(dt, n, h, v, m, backward))
-    buf = _kept(torch.empty(need + 256, dtype=torch.uint8, device=device), keep)
+    buf = _new(keep, need + 256, torch.uint8, device)
     return (buf.data_ptr() + 255) // 256 * 256, need
 
 
@@ -782,9 +780,9 @@ def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: floa
     dev = _device_of(hidden, weight, targets, *given)
     raw, keep = _stream_on(stream, dev)
     if logprob is None:
-        logprob = _kept(torch.empty(m, dtype=torch.float32, device=hidden.device), keep)
+        logprob = _new(keep, m, torch.float32, hidden.device)
     if lse is None:
-        lse = _kept(torch.empty(n, dtype=torch.float32, device=hidden.device), keep)
+        lse = _new(keep, n, torch.float32, hidden.device)
     ws, wsb = _logprob_workspace(workspace, keep, dt, n, h, v, m, False, hidden.device)
     _launch("psrl_token_logprob_fwd", dev, dt, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
             _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
@@ -797,8 +795,6 @@ def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, tar
                            d_weight=None, want_hidden: bool = True, want_weight: bool = True, stream=None, workspace=None):
     """Gradients of the above: (d_hidden, d_weight), of hidden's type, given d_logprob [targets] and the forward's logprob and lse.
     want_hidden / want_weight False: that one is None and not computed."""
-    import torch
-
     m = targets.shape[0]
     dt, n, h, v, m = _logprob_args(hidden, weight, targets, target_off,
                                    [("logprob", logprob, m), ("lse", lse, hidden.shape[0]), ("d_logprob", d_logprob, m)])
@@ -809,9 +805,9 @@ def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, tar
     dev = _device_of(hidden, weight, targets, logprob, lse, d_logprob, *given)
     raw, keep = _stream_on(stream, dev)
     if d_hidden is None and want_hidden:
-        d_hidden = _kept(torch.empty((n, h), dtype=hidden.dtype, device=hidden.device), keep)
+        d_hidden = _new(keep, (n, h), hidden.dtype, hidden.device)
     if d_weight is None and want_weight:
-        d_weight = _kept(torch.empty((v, h), dtype=hidden.dtype, device=hidden.device), keep)
+        d_weight = _new(keep, (v, h), hidden.dtype, hidden.device)
     out = [t if w else None for t, w in ((d_hidden, want_hidden), (d_weight, want_weight))]
     ws, wsb = _logprob_workspace(workspace, keep, dt, n, h, v, m, True, hidden.device)
     args = [x for t, name in zip(out, ("d_hidden", "d_weight"))

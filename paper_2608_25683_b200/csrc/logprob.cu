@@ -10,10 +10,10 @@
 //   kLse   running maximum and sum of exponentials of a row over a run of vocabulary tiles   -> partial (max, sum)
 //   kDz    dz = -scale G softmax, with the entries of the row's targets put in afterwards    -> bf16, one piece of the
 //          vocabulary at a time in the workspace (the softmax part is rounded to bf16 as the tensor cores need it)
-//   kGrad  both gradients of a piece in one launch: d_hidden += dz W, added to fp32 sums over the pieces by the TMA unit and
-//          rounded once at the end, and d_weight = dz^T hidden, the whole sum in tensor memory, rounded once.  The few deep tiles of
-//          d_hidden come first, the many shallow ones of d_weight even out what they leave (grad_work); with few rows the
-//          depth of d_hidden is split as well, into partial sums that a last kernel adds in order.
+//   kGrad  both gradients of a piece in one launch: d_hidden += dz W, added to fp32 sums over the pieces by the TMA unit
+//          and rounded once at the end, and d_weight = dz^T hidden, the whole sum in tensor memory, rounded once.
+//          The few deep tiles of d_hidden come first, the many shallow ones of d_weight even out what they leave (GradPlan);
+//          with few rows the depth of d_hidden is split as well, into partial sums that a last kernel adds in order.
 // The pieces make dz as large as the caller's hidden states, not as the logits.
 //
 // The backward works on the rows that matter alone: a row without a target, or whose d_logprob are all zero (prompts,
@@ -1118,6 +1118,7 @@ psrl_status_t cuda_failed(cudaError_t e) {
 
 bool al16(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool al4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+constexpr int64_t kMostEntries = int64_t(1) << 30;   // rows, targets, vocabulary: indices and twice as many stay in 32 bits
 // elements of a 16-byte vector
 int64_t vec_of(psrl_dtype_t t) { return t == PSRL_BF16 ? 8 : 4; }
 bool pitch16(psrl_dtype_t t, int64_t pitch, int64_t cols) { return pitch >= cols && pitch % vec_of(t) == 0 && pitch <= (int64_t(1) << 36); }
@@ -1126,8 +1127,8 @@ bool pitch16(psrl_dtype_t t, int64_t pitch, int64_t cols) { return pitch >= cols
 psrl_status_t check(psrl_dtype_t t, int64_t n, int32_t h, int32_t v, const void* hidden, int64_t hp, const void* weight, int64_t wp,
                     const int32_t* targets, int64_t n_targets, const int32_t* off, float scale) {
   if (t != PSRL_BF16 && t != PSRL_F32) return PSRL_ERR_UNSUPPORTED;
-  if (n < 0 || n_targets < 0 || n > INT32_MAX - 512 || n_targets > INT32_MAX - 512) return PSRL_ERR_INVALID_ARG;
-  if (h < 8 || h % 8 || v < 1 || v > INT32_MAX - 512 || !pitch16(t, hp, h) || !pitch16(t, wp, h)) return PSRL_ERR_SHAPE;
+  if (n < 0 || n_targets < 0 || n > kMostEntries || n_targets > kMostEntries) return PSRL_ERR_INVALID_ARG;
+  if (h < 8 || h % 8 || v < 1 || v > kMostEntries || !pitch16(t, hp, h) || !pitch16(t, wp, h)) return PSRL_ERR_SHAPE;
   if (!off && n_targets != n) return PSRL_ERR_SHAPE;
   if (!(scale == scale) || scale == 0.f || scale > 1e30f || scale < -1e30f) return PSRL_ERR_INVALID_ARG;
   if (n == 0) return PSRL_OK;

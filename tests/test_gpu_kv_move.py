@@ -131,6 +131,28 @@ def test_streams_graphs_and_empty_lists(lib):
     assert torch.equal(bits(k).cpu(), want[0])
 
 
+def test_moves_that_overlap_in_time(lib):
+    """Large and small moves on two streams at once, each with a workspace of its own."""
+    e = [np.array([[700, 650, 30000], [30800, 30650, 9000]], dtype=np.int32), np.array([[90, 60, 500]], dtype=np.int32)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    start = [pools(40 + i, 8, 40000 if i == 0 else 600, 128, "bf16") for i in (0, 1)]
+    want = []
+    for i in (0, 1):
+        k, v = (t.clone() for t in start[i])
+        lib.psrl_kv_move(e[i], k, v)
+        want.append((bits(k).clone(), bits(v).clone()))
+        assert torch.equal(bits(k).cpu(), plain(e[i], start[i][0], start[i][0]))
+    copies = [[tuple(t.clone() for t in start[i]) for _ in range(6)] for i in (0, 1)]
+    torch.cuda.synchronize()
+    for j in range(6):
+        for i in (0, 1):
+            lib.psrl_kv_move(e[i], *copies[i][j], stream=streams[i])
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for k, v in copies[i]:
+            assert torch.equal(bits(k), want[i][0]) and torch.equal(bits(v), want[i][1])
+
+
 def test_wrapper_refusals(lib):
     k, v = pools(6, 2, 32, 128, "bf16")
     k2, v2 = pools(7, 2, 32, 128, "bf16")

@@ -286,6 +286,26 @@ def test_streams_and_graphs(lib):
     assert all(torch.equal(x, y) for x, y in zip(a + b, (lp, lse, dh, dw)))
 
 
+def test_calls_that_overlap(lib):
+    """Two streams, each with inputs and temporaries of its own, many calls in flight at once."""
+    sets = [make(n, 192, 3000, 30 + n) for n in (3, 300)]
+    want = []
+    for hidden, weight, targets, g in sets:
+        lp, lse = lib.psrl_token_logprob_fwd(hidden, weight, targets)
+        want.append((lp, lse) + lib.psrl_token_logprob_bwd(hidden, weight, targets, lp, lse, g))
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, (hidden, weight, targets, g) in enumerate(sets):
+            a = lib.psrl_token_logprob_fwd(hidden, weight, targets, stream=streams[i])
+            got[i].append(a + lib.psrl_token_logprob_bwd(hidden, weight, targets, *a, g, stream=streams[i]))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for x in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(x, want[i]))
+
+
 def test_device_status_and_wrapper_refusals(lib):
     import ctypes
 

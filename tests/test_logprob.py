@@ -65,10 +65,10 @@ def test_refusals(lib):
     fwd = lambda *a: lib.STATUS_NAMES[L.psrl_token_logprob_fwd(*a)]
     change = lambda i, v: good[:i + 1] + [v] + good[i + 2:]
     assert fwd(*change(-1, 2)) == "PSRL_ERR_UNSUPPORTED"
-    for i, v in [(0, -1), (3, None), (3, p + 8), (5, p + 2), (7, None), (9, p + 2), (10, 0.0), (10, float("nan")),
+    for i, v in [(0, -1), (0, 2 ** 30 + 1), (8, 2 ** 30 + 1), (3, None), (3, p + 8), (5, p + 2), (7, None), (9, p + 2), (10, 0.0), (10, float("nan")),
                  (10, float("inf")), (13, None), (13, p + 16)]:
         assert fwd(*change(i, v)) == "PSRL_ERR_INVALID_ARG", (i, v)
-    for i, v in [(1, 60), (1, 0), (2, 0), (4, 56), (4, 68), (6, 63), (8, 5)]:
+    for i, v in [(1, 60), (1, 0), (2, 0), (2, 2 ** 30 + 1), (4, 56), (4, 68), (6, 63), (8, 5)]:
         assert fwd(*change(i, v)) == "PSRL_ERR_SHAPE", (i, v)
     assert fwd(*change(14, 255)) == "PSRL_ERR_WORKSPACE"
     need = lib.psrl_token_logprob_workspace_bytes(4, 64, 100, 4, True)
