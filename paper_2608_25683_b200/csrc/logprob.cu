@@ -565,6 +565,9 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
 // and ordinary fp32 arithmetic keeps up, two multiply-adds an instruction.  A warp takes four vocabulary entries at a time
 // and holds their products with all kRows hidden rows, which lie in shared memory; running maximum and sum per row.
 constexpr int kFewThreads = 256, kFewV = 4;
+// Blocks of an SM, and of the launch for each SM: one wave, as every block gets the same share of the vocabulary (4 rows with
+// twice as many blocks 197 us, with these 190).
+__host__ __device__ constexpr int few_blocks(int rows) { return rows == 1 ? 4 : rows == 2 ? 3 : 2; }
 constexpr size_t kFewSmem = 128 * 1024;   // hidden rows at most
 
 // eight bf16 as four pairs of fp32
@@ -575,7 +578,7 @@ __device__ __forceinline__ void widen(const uint4& x, f32x2 (&o)[4]) {
 }
 
 template <int kRows>
-__global__ void __launch_bounds__(kFewThreads) few_rows_kernel(int M, int vecs, int vocab, const uint4* __restrict__ hidden,
+__global__ void __launch_bounds__(kFewThreads, few_blocks(kRows)) few_rows_kernel(int M, int vecs, int vocab, const uint4* __restrict__ hidden,
                                                                int64_t h_pitch_vecs, const uint4* __restrict__ weight,
                                                                int64_t w_pitch_vecs, float scale_log2, float2* __restrict__ part, int* __restrict__ status) {
   next_kernel_may_start();
@@ -975,10 +978,9 @@ namespace {
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Up to kFewRows rows the forward takes few_rows_kernel: 1, 2, 4 rows of 4096 x 131072 weights 191, 221, 203 us, all of
+// Up to kFewRows rows the forward takes few_rows_kernel: 1, 2, 4 rows of 4096 x 131072 weights 185, 189, 190 us, all of
 // them 206 us by the matrix kernel, whose sums are less exact; with 8 rows it is 415 us (fp32 arithmetic) against 206.
 constexpr int kFewRows = 4;
-constexpr int kFewBlocks = 1184;  // its blocks at most: eight per SM
 
 struct Layout {
   int32_t tile_n, n_tiles, run, n_parts;
@@ -1027,7 +1029,7 @@ Layout layout(psrl_dtype_t dtype, int64_t n, int64_t h, int64_t v, int64_t n_tar
       for (L.few = 1; L.few < n;) L.few *= 2;
       if (size_t(L.few) * h * 2 > kFewSmem) L.few = 0;
       const int64_t per_block = kFewThreads / 32 * kFewV;
-      if (L.few) L.n_parts = static_cast<int32_t>(std::min<int64_t>(kFewBlocks, (v + per_block - 1) / per_block));
+      if (L.few) L.n_parts = static_cast<int32_t>(std::min<int64_t>(few_blocks(L.few) * resident_ctas(), (v + per_block - 1) / per_block));
     }
     L.part = take(size_t(L.n_parts) * n * sizeof(float2));
     if (!L.few) L.part_at = take(size_t(L.n_parts) * n * sizeof(int32_t));
