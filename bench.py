@@ -281,6 +281,48 @@ def flush_l2(device):
     _flush_buf.add_(1)
 
 
+def operators_leg(lib, r, w, V, device, pk, vocab=131072, most_rows=16384):
+    """The steps around the attention on this workload's tree: rotary positions fused with the pools (both directions), a
+    compaction that moves every slot behind the first sixteen, and the log-probabilities of the rows' next tokens with their
+    gradients over a vocabulary of `vocab` (at most `most_rows` rows, hidden width Hq * d)."""
+    import torch
+
+    T, d, dt = V["T_q"], w.head_dim, r.k.dtype
+    rnd = lambda *s: torch.randn(*s, device=device).to(dt)
+    rope = lib.Rope(d, base=1000000.0)
+    q, k, v = rnd(T, w.n_q_heads, d), rnd(T, w.n_kv_heads, d), rnd(T, w.n_kv_heads, d)
+    kp, vp = r.k.clone(), r.v.clone()
+    out = {}
+
+    def hbm(name, nbytes, fn):
+        ms = time_region(fn, 10, 2, device if nbytes < 2 * L2_BYTES else None)
+        gbs = nbytes / (ms * 1e-3) / 1e9
+        out[name] = {"ms": round(ms, 4), "bytes": nbytes, "gbs": round(gbs, 1), "frac_of_hbm": round(gbs / pk["hbm_gbs"], 4)}
+
+    row_bytes = 2 * T * (w.n_q_heads + 2 * w.n_kv_heads) * d * q.element_size()
+    q_out = torch.empty_like(q)
+    hbm("rope_fwd", row_bytes, lambda: lib.psrl_rope_qkv_fwd(r.plan, rope, q, k, v, kp, vp, q_out=q_out))
+    hbm("rope_bwd", row_bytes, lambda: lib.psrl_rope_qkv_bwd(r.plan, rope, q, kp, vp, dq_out=q_out, dk_out=k, dv_out=v))
+    slots = kp.shape[1] - 16
+    hbm("kv_move", 4 * slots * w.n_kv_heads * d * q.element_size(), lambda: lib.psrl_kv_move([[16, 0, slots]], kp, vp))
+    del q, k, v, kp, vp, q_out
+    rows, h = min(T, most_rows), w.n_q_heads * d
+    off, nxt = r.plan.next_tokens()
+    off = torch.as_tensor(off[:rows + 1], device=device)
+    ids = torch.randint(0, vocab, (V["T"],), device=device)
+    targets = ids[torch.as_tensor(nxt[:int(off[-1])], device=device).long()].to(torch.int32)
+    hidden, weight = rnd(rows, h), rnd(vocab, h) * (1.0 / np.sqrt(h))
+    grad = torch.randn(len(targets), device=device)
+    lp, lse = lib.psrl_token_logprob_fwd(hidden, weight, targets, off)
+    for name, n, fn in (("logprob_fwd", 2, lambda: lib.psrl_token_logprob_fwd(hidden, weight, targets, off)),
+                        ("logprob_bwd", 6, lambda: lib.psrl_token_logprob_bwd(hidden, weight, targets, lp, lse, grad, off))):
+        ms = time_region(fn, 5, 2)
+        tf = n * rows * h * vocab / (ms * 1e-3) / 1e12
+        out[name] = {"ms": round(ms, 4), "rows": rows, "hidden": h, "vocab": vocab, "tflops": round(tf, 1),
+                     "frac_of_bf16_peak": {"burst": round(tf / pk["bf16_tflops"], 4), "sustained": round(tf / pk["bf16_tflops_sustained"], 4)}}
+    return out
+
+
 def time_region(fn, iters, warmup=0, flush_device=None):
     """Mean time of fn over `iters` calls, CUDA events on the current stream.  With flush_device
     every call is timed on its own and the L2 is flushed before it (outside the timed part)."""
@@ -844,6 +886,8 @@ def measure_config(args, lib, name, device, rank, world, local, headline):
                 "scatter_gbs": round(nbytes_pack / (t_sc * 1e-3) / 1e9, 1), "gather_gbs": round(nbytes_pack / (t_ga * 1e-3) / 1e9, 1),
                 "hbm_peak_gbs": pk["hbm_gbs"], "scatter_frac": round(nbytes_pack / (t_sc * 1e-3) / 1e9 / pk["hbm_gbs"], 4),
                 "gather_frac": round(nbytes_pack / (t_ga * 1e-3) / 1e9 / pk["hbm_gbs"], 4)}
+        if args.operators and world == 1:
+            extra["operators"] = operators_leg(lib, r, w, V, device, pk)
         if args.schedule and world == 1:
             extra["schedule"] = schedule_leg(lib, device, args.seed + 11)
         if args.microbatch and world == 1:
@@ -876,6 +920,8 @@ def main():
     ap.add_argument("--length-scale", type=float, default=1.0,
                     help="scale every segment length (tree shape and prefix match rate unchanged, cf. Sec. 7.5)")
     ap.add_argument("--pack", action="store_true", help="also time K/V scatter into the pools and the gather back")
+    ap.add_argument("--operators", action="store_true",
+                    help="also time the steps around the attention: rotary positions with the pools, compacting the arena, token log-probabilities")
     ap.add_argument("--schedule", action="store_true",
                     help="also fit Eq. 1 to measured times and compare load-balanced with round-robin group placement")
     ap.add_argument("--microbatch", action="store_true",
@@ -937,7 +983,8 @@ def main():
                 bitwise_reproducible_3_runs=res["bitwise_reproducible_3_runs"], plan=res["plan"],
                 unshared=res["unshared"], cuda_graph=res.get("cuda_graph"), frac_of_bf16_peak=res["frac_of_bf16_peak"],
                 per_config=per_config or None, library_context=extra.get("library_context"),
-                microbatch=extra.get("microbatch"), schedule=extra.get("schedule"), kv_pack=extra.get("kv_pack"))
+                microbatch=extra.get("microbatch"), schedule=extra.get("schedule"), kv_pack=extra.get("kv_pack"),
+                operators=extra.get("operators"))
     print(json.dumps(line), flush=True)
     if world > 1:
         dist.barrier()
