@@ -69,6 +69,7 @@ struct GemmParams {
   int32_t twice;                // kDz, kGrad: rows 128 ... hold the rest of dz below bf16 (see kTwiceRows)
   const int32_t* count;         // kDz, kGrad: rows that matter, on the device (kLse: NULL, all M)
   const int32_t* row_of;        // kDz: the caller's row of a gathered row
+  int32_t group;                // kLse, kDz: row tiles that are walked together
   int32_t tile_n;               // columns of a tile: 256, or fewer in the logits (a multiple of 64)
   int32_t run;                  // kLse: consecutive column tiles of one work unit
   float scale_log2;             // logits in powers of two: scale * log2(e)
@@ -144,15 +145,20 @@ __device__ __forceinline__ void tma_add_2d(const CUtensorMap* m, const void* sme
                : "memory");
 }
 
-// Work unit -> row tile and first column tile: groups of kGroupM row tiles, inside a group the row tile moves fastest, so
-// that the CTAs at work share column tiles and a group's rows stay in the L2.
-constexpr int kGroupM = 16;   // forward of 8192 x 4096 x 131072 rows: 6.1 ms, with 32 or 8 6.7
-__device__ __forceinline__ void unit_tile(int m_tiles, int unit, int n_units, int& mt, int& nu) {
-  const int per = kGroupM * n_units;
+// Work unit -> row tile and first column tile: groups of row tiles, inside a group the row tile moves fastest, so that the
+// CTAs at work share column tiles and a group's rows stay in the L2.  For logits (tiles as deep as the hidden dimension) a
+// group is as many row tiles as fit kGroupBytes: 8192 x 4096 x 131072 forward in 6.2 ms, with 72 MB or 18 MB 6.8 to 7.4;
+// 16384 x 2048 x 131072 5.8 to 6.1, a tenth less than with 16 tiles; at a hidden size of 8192 18 to 144 MB are within the
+// noise.  For gradients, whose tiles are as deep as the rows or the vocabulary and walk it in step, the operands of the CTAs
+// at work count and not the group's: kGradGroup tiles, 8192 x 4096 x 131072 backward in 20.1 ms, with 4 20.5, 16 20.6, 32 21.5.
+constexpr int64_t kGroupBytes = int64_t(36) << 20;
+constexpr int kGradGroup = 8;
+__device__ __forceinline__ void unit_tile(int group, int m_tiles, int unit, int n_units, int& mt, int& nu) {
+  const int per = group * n_units;
   const int g = unit / per, r = unit - g * per;
-  const int gm = min(kGroupM, m_tiles - g * kGroupM);
+  const int gm = min(group, m_tiles - g * group);
   nu = r / gm;
-  mt = g * kGroupM + r - nu * gm;
+  mt = g * group + r - nu * gm;
 }
 
 // The targets of a row, kept inside the array whatever the offsets say.
@@ -194,7 +200,7 @@ struct GradPlan {
       const int u = c + i * C;
       w.weight = 0;
       w.split = u / per;
-      unit_tile(m_tiles, u - w.split * per, p.n_tiles, w.mt, w.nt);
+      unit_tile(kGradGroup, m_tiles, u - w.split * per, p.n_tiles, w.mt, w.nt);
       w.kb0 = part_of(steps, w.split, p.splits);
       w.kb1 = part_of(steps, w.split + 1, p.splits);
       return true;
@@ -208,7 +214,7 @@ struct GradPlan {
     w.split = 0;
     w.kb0 = 0;
     w.kb1 = row_steps;
-    unit_tile(v_tiles, at, p.n_tiles, w.mt, w.nt);
+    unit_tile(kGradGroup, v_tiles, at, p.n_tiles, w.mt, w.nt);
     return true;
   }
   // where part k of n begins; n <= 16 parts of fewer than 2^25 steps
@@ -311,7 +317,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
       const int unit = cluster + i * n_clusters;
       if (unit >= m_tiles * n_units) return false;
       int nu;
-      unit_tile(m_tiles, unit, n_units, w.mt, nu);
+      unit_tile(p.group, m_tiles, unit, n_units, w.mt, nu);
       w.weight = 0;
       w.kb0 = 0;
       w.kb1 = p.k_blocks;
@@ -1086,6 +1092,11 @@ cudaError_t launch_gemm(const GemmMaps& maps, GemmParams& p, bool first, cudaStr
   cudaError_t e = ensure_dynamic_smem(gemm_kernel<kKind>, gemm_smem(kKind), done);
   if (e != cudaSuccess) return e;
   if (p.tile_n == 0) p.tile_n = 256;
+  // even groups of at most kGroupBytes (a row tile is 256 rows of 2 bytes)
+  const int64_t row_tiles = std::max<int64_t>(1, (int64_t(p.M) + 255) / 256);
+  const int64_t most = std::max<int64_t>(1, kGroupBytes / (int64_t(std::max(p.k_blocks, 1)) * kBK * 512));
+  const int64_t groups = (row_tiles + most - 1) / most;
+  p.group = int32_t((row_tiles + groups - 1) / groups);
   p.n_tiles = (p.N + p.tile_n - 1) / p.tile_n;
   if (p.run < 1) p.run = 1;
   int64_t units = (int64_t(p.M) + 255) / 256 * ((p.n_tiles + p.run - 1) / p.run);
