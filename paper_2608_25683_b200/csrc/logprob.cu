@@ -83,6 +83,8 @@ struct GemmParams {
   int32_t acc_rows;             // kGrad: rows of one part's sums
   int32_t want_hidden, want_weight;   // kGrad
   int32_t first;                // kGrad: the first piece: the sums are stored, later they are added to
+  uint32_t* pace;               // kLse: what all pairs have begun, zero at the start (see keep_pace); NULL: each at its own pace
+  uint32_t pace_shift;          // in units of 1 << pace_shift steps
   int* status;
 };
 
@@ -159,6 +161,36 @@ __device__ __forceinline__ void unit_tile(int group, int m_tiles, int unit, int 
   const int gm = min(group, m_tiles - g * group);
   nu = r / gm;
   mt = g * group + r - nu * gm;
+}
+
+// Pace.  The pairs at work share what they read of the rows and of the weights only while they are about as far along the
+// depth: left to themselves they drift apart by whole tiles, and what one of them has fetched has left the L2 when the others
+// come by (8192 x 8192 x 65536: 18.4 GB read from DRAM, 4.4 if each group of rows reads the weights once).  So each pair counts
+// every few steps that it begins, and goes on only when all pairs' sum is that of pairs one such unit behind.  It is
+// a help and no barrier: a pair that has waited in vain (kPaceTries, about 0.2 ms; other work may hold some SMs) waits no more, and
+// one that is through counts kPaceDone, which frees the others.  Forward of 131072 entries, TFLOP/s with a pause between the
+// calls: 16384 x 8192 in units of 8 steps 1480 to 1535, without pace 1236 to 1500; 2048 x 16384 x 65536 1470, 1350; 1024 x 8192
+// 1440, 1270 to 1400; 8192 x 4096 in units of 16 1530 to 1580, 1450 to 1555 (units of 8 cost 3 % there back to back).  At a
+// hidden size of 2048 it loses up to 3 %, with 512 to 700 rows 1 %, with less than four rounds of tiles up to 13 %.  The gradients
+// lose 1 to 2 %: few pairs at work share an operand there.
+constexpr int kPaceTries = 200;
+constexpr size_t kPaceAt = 128;            // in the header of the workspace
+constexpr int kPaceRows = 1024, kPaceDepth = 4096;
+constexpr uint32_t kPaceDone = 1u << 24;   // 74 pairs' stay below 2^31
+__device__ __forceinline__ void count_pace(uint32_t* pace, uint32_t n) {
+  asm volatile("red.relaxed.gpu.global.add.u32 [%0], %1;" ::"l"(pace), "r"(n) : "memory");
+}
+__device__ __forceinline__ uint32_t read_pace(const uint32_t* pace) {
+  uint32_t n;
+  asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(pace) : "memory");
+  return n;
+}
+__device__ __forceinline__ bool keep_pace(const uint32_t* pace, uint32_t want) {
+  for (int i = 0; i < kPaceTries; ++i) {
+    if (int32_t(read_pace(pace) - want) >= 0) return true;
+    __nanosleep(100);
+  }
+  return false;
 }
 
 // The targets of a row, kept inside the array whatever the offsets say.
@@ -338,7 +370,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
     if (lane == 0) {
       const uint32_t stage_tx = 2 * (kOperandBytes + uint32_t(tile_n) * kBK);   // of both CTAs
       uint32_t it = 0;
-      bool ok = true;
+      bool ok = true, wait_pace = true;
+      const bool paced = kKind == kLse && p.pace && rank == 0;   // the second CTA keeps step through the stages
       for (int i = 0; ok && work(i, w, nt_end); ++i) {
         const bool a_mn = kKind == kGrad && w.weight;
         const CUtensorMap* ma = a_mn ? &maps.a2 : &maps.a;
@@ -350,6 +383,11 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
           const int skip = kKind == kGrad && w.weight && p.twice ? 128 / kBK - w.kb1 / 2 : 0;
           for (int step = w.kb0; step < w.kb1; ++step, ++it) {
             const int kb = step + (skip && step >= w.kb1 / 2 ? skip : 0);
+            if (paced && (it & ((1u << p.pace_shift) - 1)) == 0) {
+              count_pace(p.pace, 1);
+              const uint32_t n = it >> p.pace_shift;
+              if (wait_pace && n > 1) wait_pace = keep_pace(p.pace, (n - 1) * uint32_t(n_clusters));
+            }
             const uint32_t s = it % kStages, round = it / kStages;
             if (round > 0 && !mbar_wait(&bar.empty[s], (round + 1) & 1, abortp, p.status)) { ok = false; break; }
             // the second CTA's copies count on the first one's barrier as well
@@ -372,6 +410,7 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
           }
         }
       }
+      if (paced) count_pace(p.pace, kPaceDone);
       // the last arrivals on the stages' barriers come from the pair's products: this CTA stays until they are here
       for (uint32_t i = 0; i < kStages && ok; ++i) {
         const uint32_t uses = it / kStages + (i < it % kStages ? 1 : 0);
@@ -1209,6 +1248,14 @@ psrl_status_t psrl_token_logprob_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t
     p.part = part;
     p.part_at = part_at;
     p.status = status;
+    // where depth and rows are such that the pairs' operands fill the L2, and over several rounds of tiles (see keep_pace)
+    const bool paced = hidden_dim >= kPaceDepth && n_rows >= kPaceRows && (n_rows + 255) / 256 * ((vocab + 255) / 256) >= 4 * (resident_ctas() / 2);
+    if (paced) {
+      e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+      if (e != cudaSuccess) return cuda_failed(e);
+      p.pace = reinterpret_cast<uint32_t*>(ws + kPaceAt);
+      p.pace_shift = p.k_blocks > 64 ? 3 : 4;
+    }
     e = launch_gemm<kLse>(maps, p, true, s);
   }
   if (e != cudaSuccess) return cuda_failed(e);

@@ -329,3 +329,31 @@ def test_device_status_and_wrapper_refusals(lib):
     with pytest.raises(lib.PsrlError) as e:
         lib.psrl_token_logprob_fwd(hidden, weight, targets[:10])
     assert e.value.name == "PSRL_ERR_SHAPE"
+
+
+@pytest.mark.parametrize("h", [4096, 4168])
+def test_pairs_that_keep_pace(lib, h):
+    """Enough rows, depth and vocabulary that the pairs of CTAs wait for one another: four forwards in flight on two streams,
+    more CTAs than the device holds at once, then a captured one replayed; all alike, and right for some of the rows."""
+    n, v = 1030, 16384 - 37
+    hidden, weight, targets, _ = make(n, h, v, 50)
+    lp, lse = lib.psrl_token_logprob_fwd(hidden, weight, targets)
+    rows = torch.tensor([0, 1, 255, 256, 1023, 1024, n - 1], device="cuda")
+    hn, wn = to_np(hidden[rows]), to_np(weight)
+    want = oracle_logprob(hn, wn, targets[rows].cpu().numpy())
+    zerr, lerr = bounds(hn, wn, 1.0, want)
+    assert (np.abs(to_np(lse[rows]) - want["lse"]) <= lerr).all()
+    size = np.abs(want["logprob"]) + 2 * np.abs(want["lse"])
+    assert (np.abs(to_np(lp[rows]) - want["logprob"]) <= lerr + zerr + 2.0 ** -22 * size).all()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [lib.psrl_token_logprob_fwd(hidden, weight, targets, stream=s) for _ in range(2) for s in streams]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got.append(lib.psrl_token_logprob_fwd(hidden, weight, targets))
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for x in got:
+        assert torch.equal(x[0], lp) and torch.equal(x[1], lse)
