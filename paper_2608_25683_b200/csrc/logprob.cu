@@ -165,11 +165,11 @@ __device__ __forceinline__ void unit_tile(int group, int m_tiles, int unit, int 
 
 // Pace.  The pairs at work share what they read of the rows and of the weights only while they are about as far along the
 // depth: left to themselves they drift apart by whole tiles, and what one of them has fetched has left the L2 when the others
-// come by (8192 x 8192 x 65536: 18.4 GB read from DRAM, 4.4 if each group of rows reads the weights once).  So each pair counts
-// every few steps that it begins, and goes on only when all pairs' sum is that of pairs one such unit behind.  It is
-// a help and no barrier: a pair that has waited in vain (kPaceTries, about 0.2 ms; other work may hold some SMs) waits no more, and
-// one that is through counts kPaceDone, which frees the others.  Forward of 131072 entries, TFLOP/s with a pause between the
-// calls: 16384 x 8192 in units of 8 steps 1480 to 1535, without pace 1236 to 1500; 2048 x 16384 x 65536 1470, 1350; 1024 x 8192
+// come by (8192 x 8192 x 65536: 18.4 GB read from DRAM, 10.4 with pace, 4.4 if each group of rows reads the weights once).
+// So each pair counts every few steps that it begins, and goes on only when all pairs' sum is that of pairs one such unit
+// behind.  It is a help and no barrier: a pair that has waited in vain (kPaceTries, about 0.2 ms; other work may hold some
+// SMs) waits no more, and one that is through counts kPaceDone, which frees the others.  Forward, TFLOP/s with a pause
+// between the calls: 16384 x 8192 in units of 8 steps 1480 to 1535, without pace 1236 to 1500; 2048 x 16384 x 65536 1460, 1350; 1024 x 8192
 // 1440, 1270 to 1400; 8192 x 4096 in units of 16 1530 to 1580, 1450 to 1555 (units of 8 cost 3 % there back to back).  At a
 // hidden size of 2048 it loses up to 3 %, with 512 to 700 rows 1 %, with less than four rounds of tiles up to 13 %.  The gradients
 // lose 1 to 2 %: few pairs at work share an operand there.
