@@ -15,6 +15,7 @@
 
 #include "../../include/psrl_cache.h"
 #include "kernels.h"
+#include "move_order.h"
 #include "sm100.cuh"
 
 namespace psrl {
@@ -103,7 +104,8 @@ psrl_status_t copy_extents(const psrl_kv_extent_t* ext, int32_t n, const Pools& 
 //   large moves   one block per SM (cooperative launch, all resident).  The sequence is cut into 64 KB parts, handed out
 //                 in order; a warp takes a part, loads it into its own share of shared memory with bulk copies, counts it
 //                 as loaded, waits until the parts whose sources it overwrites are, and stores it.  Every part handed out
-//                 gets loaded whatever the others do, and the parts waited for are no later ones, so the waits end.
+//                 gets loaded whatever the others do, and the parts waited for are no later ones, so the waits end
+//                 (move_order.h has the arithmetic and why the counts of 32 groups are enough).
 //                 169,632 slots of 4 KB:
 //                 235 us, 5.9 TB/s; the same copied to other pools, where nothing waits, 209 us.  (Chunks of the whole
 //                 grid, stored once every block had loaded its share of them, took 270 us in registers and 296 us through
@@ -210,22 +212,9 @@ __global__ void __launch_bounds__(kMoveThreads, 1) move_cluster_kernel(const __g
 // Three warps with 64 KB each; twelve with 16 KB take 328 us instead of 235: the counters, one line of the L2, bound them.
 constexpr int kBulkWarps = 3, kBulkBytes = 64 * 1024, kBulkLanes = 8;   // a lane's share of a part: 8 KB
 constexpr size_t kBulkSmem = size_t(kBulkWarps) * kBulkBytes;
-constexpr int kGroup = 32;        // parts of a group
-// Groups are told apart modulo kRing.  The parts at work span at most kSpan groups, and no part is stored while a group
-// more than kAhead before its own is incomplete, so the groups whose counts still change span less than the ring.
-constexpr int kRing = 32, kSpan = 15, kAhead = 15;
-static_assert(kRing <= 32 && kSpan + kAhead + 1 < kRing, "a lane polls one group");
 
 // The contiguous pieces of rows [row, end) of the sequence: calls f(pool, first source vector, first destination vector,
 // rows, rows before).
-__device__ __forceinline__ int extent_of(const int32_t* starts, int n, int at) {   // the last one that starts at or before `at`
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (starts[mid] <= at) lo = mid; else hi = mid;
-  }
-  return lo;
-}
 template <class List, class F>
 __device__ __forceinline__ void for_pieces(const List& list, const Pools& p, uint32_t row, uint32_t end, F f) {
   if (row >= end) return;
@@ -281,20 +270,12 @@ __global__ void __launch_bounds__(kBulkWarps * 32, 1) move_bulk_kernel(const __g
     });
     if (!__all_sync(0xffffffffu, sm100::mbar_wait(&landed[warp], phase, abortp, ws))) break;
     phase ^= 1;
-    // What this part overwrites must have been loaded: the sources below its last destination slot.  They are rows of
-    // this part or of parts before it; the last of them decides.
-    const uint32_t last_row = end - 1, ph = last_row / uint32_t(list.slots);
-    const int s_last = int(last_row - ph * uint32_t(list.slots)), e_last = extent_of(list.first, list.n, s_last);
-    const int dst_last = list.dst[e_last] + s_last - list.first[e_last];
-    const int e_src = extent_of(list.src, list.n, dst_last);
-    // (no source at or below it: then nothing of this head is overwritten that anybody reads, and an earlier row is safe too)
-    const int s_src = list.src[e_src] > dst_last ? 0 : min(list.first[e_src] + dst_last - list.src[e_src], list.first[e_src + 1] - 1);
-    const uint32_t group = part / kGroup;
-    const uint32_t until = max((ph * uint32_t(list.slots) + s_src) / part_rows / kGroup, group > kAhead ? group - kAhead : 0);
-    // the copies have landed: nothing reads this part's sources any more
-    if (lane == 0) atomicAdd(ws + 16 + group % kRing, 1);
-    const uint32_t g = next_group + lane;
-    const int want = int(g / kRing * kGroup + min(uint32_t(kGroup), n_parts - min(g * kGroup, n_parts)));
+    const uint32_t group = part / kGroup, until = wait_until(list, part, end, part_rows);
+    // The copies have landed: nothing reads this part's sources any more.  Their values are here, so no store that follows can
+    // change them, and the count needs no release (which waits for the part before to be stored as well: 270 us, not 238).
+    if (lane == 0) asm volatile("red.relaxed.gpu.global.add.s32 [%0], 1;" ::"l"(ws + 16 + group % kRing) : "memory");
+    const uint32_t g = poll_from(next_group, group) + lane;
+    const int want = int(full_count(g, n_parts));
     bool ok = false;
     for (uint32_t it = 0; it < (1u << 22) && !ok; ++it) {
       int seen = want;
@@ -309,6 +290,7 @@ __global__ void __launch_bounds__(kBulkWarps * 32, 1) move_bulk_kernel(const __g
       break;
     }
     next_group = max(next_group, until + 1);
+    __syncwarp();   // what any lane has seen loaded orders every lane's stores
     asm volatile("fence.proxy.async;" ::: "memory");
     for_pieces(list, p, my_row, min(my_row + lane_rows, end), [&](int pool, int64_t, int64_t dst, uint32_t n, uint32_t done) {
       asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"((pool ? p.v_dst : p.k_dst) + dst),
@@ -363,9 +345,9 @@ psrl_status_t move_extents(const psrl_kv_extent_t* ext, int32_t n, Pools p, int*
     static bool done[64] = {};
     e = ensure_dynamic_smem(move_bulk_kernel<kMax>, kBulkSmem, done);
     const int64_t part_rows = kBulkBytes / (int64_t(p.vecs) * 16), parts = (rows + part_rows - 1) / part_rows;
-    const int64_t grid = std::min<int64_t>(std::min(resident_ctas(), kSpan * kGroup / kBulkWarps), (parts + kBulkWarps - 1) / kBulkWarps);
+    const int64_t grid = std::min<int64_t>(std::min(resident_ctas(), int(kSpan * kGroup / kBulkWarps)), (parts + kBulkWarps - 1) / kBulkWarps);
     // a group has to be at work as a whole: a device with fewer warps than that would wait for parts that nobody has taken
-    if (grid * kBulkWarps < std::min<int64_t>(kGroup, parts)) return PSRL_ERR_UNSUPPORTED;
+    if (grid * kBulkWarps < std::min<int64_t>(int64_t(kGroup), parts)) return PSRL_ERR_UNSUPPORTED;
     cfg.gridDim = dim3(unsigned(grid));
     cfg.blockDim = dim3(kBulkWarps * 32);
     cfg.dynamicSmemBytes = kBulkSmem;

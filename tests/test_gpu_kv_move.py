@@ -191,3 +191,42 @@ def test_cached_blocks_survive_compaction(lib):
         moved += len(moves)
         lib.psrl_kv_move(moves, K, V)
     assert moved >= 1
+
+
+@pytest.mark.parametrize("kind", ["half freed", "far then near", "one slot"])
+def test_large_moves_beside_other_work(lib, kind):
+    """Several hundred MB moved on one stream while matrix products keep another busy, so that the move's blocks neither start
+    nor run alike: half of the arena freed; each head's first blocks far down and its last ones hardly at all; one block of
+    nearly the whole arena by one slot.  Byte-exact every time, and the status word is clear."""
+    rng = np.random.default_rng(3)
+    if kind == "half freed":
+        size, gap = 16 * rng.integers(1, 80, 150), 16 * rng.integers(0, 80, 150)
+    elif kind == "far then near":
+        size, gap = 16 * rng.integers(1, 120, 100), np.where(np.arange(100) % 2, 16, 0)
+        gap[0] = 30000
+    else:
+        size, gap = np.array([90001]), np.array([1])
+    src = np.cumsum(size + gap) - size
+    e = np.stack([src, np.cumsum(size) - size, size], 1).astype(np.int32)
+    heads, cap, d = 8, int(src[-1] + size[-1]) + 5, 128
+    k0, v0 = pools(60, heads, cap, d, "bf16")
+    want = []
+    for t in (k0, v0):
+        w = bits(t).clone()
+        for s, to, n in e.tolist():
+            w[:, to:to + n] = bits(t)[:, s:s + n]
+        want.append(w)
+    a = torch.randn(2048, 2048, device="cuda").to(torch.bfloat16)
+    move, other = torch.cuda.Stream(), torch.cuda.Stream()
+    buf = torch.empty(512, dtype=torch.uint8, device="cuda")
+    ws = (buf.data_ptr() + 255) // 256 * 256, 256
+    for _ in range(8):
+        k, v = k0.clone(), v0.clone()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            for _ in range(30):
+                a @ a
+        lib.psrl_kv_move(e, k, v, stream=move, workspace=ws)
+        torch.cuda.synchronize()
+        assert lib.lib().psrl_device_status(ws[0], None) == 0
+        assert torch.equal(bits(k), want[0]) and torch.equal(bits(v), want[1])
