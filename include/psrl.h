@@ -370,6 +370,8 @@ psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off
  *   z = scale * hidden[r] . weight[v],   lse[r] = ln sum_v exp(z[r, v]),   logprob[t] = z[r, targets[t]] - lse[r]
  * for the targets t of row r: target_off[r] <= t < target_off[r + 1], or t = r when target_off is NULL (n_targets ==
  * n_rows).  Targets outside [0, vocab) are ignored: logprob 0, no gradient.  The logits are never stored.
+ * Logits that are not finite: NaN or +inf makes the lse of its row and the logprob of the targets there NaN; -inf is an entry
+ * of probability 0 (a row of nothing else has lse -inf, logprob NaN).  Other rows are not touched.
  * Backward: G_r = the sum of d_logprob over row r's targets,
  *   dz[r, v] = scale * (sum of d_logprob over r's targets equal to v  -  G_r exp(z[r, v] - lse[r]))
  *   d_hidden = dz weight,  d_weight = dz^T hidden

@@ -811,8 +811,9 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
     if (lane == 0) {
       for (int t = b + (warp - at % kWarps + kWarps) % kWarps; t < e; t += kWarps) {
         const int y = targets[t];
-        // a log-probability is not positive; the two sums are rounded apart
-        logprob[t] = y >= 0 && y < vocab ? fminf(logprob[t] - s_lse[r], 0.f) : 0.f;
+        // a log-probability is not positive; the two sums are rounded apart.  (fminf would turn NaN into a certainty.)
+        const float x = logprob[t] - s_lse[r];
+        logprob[t] = y >= 0 && y < vocab ? (x > 0.f ? 0.f : x) : 0.f;
       }
     }
     at += e - b;
