@@ -294,6 +294,14 @@ struct TileOut {
   }
 };
 
+// Exponent of a probability: z - lse, both in powers of two, each with its own rounding.  With logits of 10^8 that alone is some
+// hundred, and the probability infinite, so it is held at one.  NaN stays.
+__device__ __forceinline__ float at_most_one(float exponent) {
+  float y;
+  asm("min.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(exponent));
+  return y;
+}
+
 // dz rounded to bf16, or the rest below that
 __device__ __forceinline__ __nv_bfloat16 dz_part(float v, bool rest) {
   const __nv_bfloat16 y = __float2bfloat16_rn(v);
@@ -556,8 +564,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
               for (int i = 0; i < 4; ++i) {
                 float lo = __uint_as_float(r[j / 4][j % 4 * 8 + 2 * i]), hi = __uint_as_float(r[j / 4][j % 4 * 8 + 2 * i + 1]);
                 if constexpr (kKind == kDz) {
-                  lo = coef * ex2(fmaf(lo, p.scale_log2, -lse2));
-                  hi = coef * ex2(fmaf(hi, p.scale_log2, -lse2));
+                  lo = coef * ex2(at_most_one(fmaf(lo, p.scale_log2, -lse2)));
+                  hi = coef * ex2(at_most_one(fmaf(hi, p.scale_log2, -lse2)));
                 }
                 o[i] = pack_bf16(lo, hi);
                 if (kKind == kDz && rest) o[i] = pack_bf16(lo - __uint_as_float(o[i] << 16), hi - __uint_as_float(o[i] & 0xffff0000u));
@@ -795,7 +803,11 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
     float2 x = s_part[0][r];
     if (part_at && fabsf(x.x) <= 1e30f) {   // not for infinities and NaN
       const float z = warp_dot(hidden + int64_t(row0 + r) * h_pitch, weight + int64_t(s_at[0][r]) * w_pitch, vecs) * (scale * kLog2e);
-      x.y = x.y - 1.f + exp2f(z - x.x);     // the maximum's term of the sum is one
+      const float d = z - x.x, rest = x.y - 1.f;   // the maximum's term of the sum is one
+      if (fabsf(d) < 64.f) x.y = rest + exp2f(d);
+      // logits so large that the two sums are far apart: the smaller of the largest term and the rest does not count
+      else if (d < 0.f && rest > 0.f) x.y = rest;
+      else x = make_float2(z, 1.f);
     }
     if (lane == 0) {
       const float l = ((x.x == -CUDART_INF_F ? 0.f : x.x) + log2f(x.y)) * kLn2;

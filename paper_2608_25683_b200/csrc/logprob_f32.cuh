@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(256) f32_kernel(const F32Params p) {
           float v = acc[i][j];
           float* o = p.out + to * p.out_pitch + n;
           if constexpr (kKind == kF32Dz) {
-            v = info.y * exp2f(fmaf(v, p.scale_log2, -info.x));
+            v = info.y * exp2f(at_most_one(fmaf(v, p.scale_log2, -info.x)));
             if (only.x == p.col0 + n) v = __int_as_float(only.y);
           }
           if constexpr (kKind == kF32Dh) { if (!p.first) v += *o; }
