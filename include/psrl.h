@@ -326,14 +326,14 @@ void psrl_rope_destroy(psrl_rope_t* rope);
  * segments is in the pools already, rotated, and is left alone).
  *   q  [T_q, Hq, d], k, v [T_q, Hkv, d]  DEVICE, plan dtype; row r at r * pitch elements, heads contiguous, so the
  *      three may be slices of one projection output
- *   q_out [T_q, Hq, d] contiguous: rotated Q (may be q itself when q is contiguous)
+ *   q_out [T_q, Hq, d] contiguous: rotated Q (may be q itself when q is contiguous; INVALID_ARG when it is not)
  *   k_pool, v_pool [Hkv, pool_capacity, d]: rotated K and V of row r at the slot of its token; other slots untouched
  * A source may be NULL (with its destination ignored): skipped.  Pointers 16-byte aligned, pitches a multiple of
  * 16 bytes and at least a row.  Sources and destinations must not overlap otherwise.
  * Errors: INVALID_ARG, SHAPE (rope head_dim, pool size, pitches), WORKSPACE (plan not uploaded), CUDA.  Asynchronous.
  *
  * psrl_rope_qkv_bwd - the way back: the transposed (inverse) rotation of d_q and of the rows' slots of dk_pool, and the
- * rows' slots of dv_pool, to row-major dq_out, dk_out, dv_out with pitches (dq_out may be d_q when contiguous).
+ * rows' slots of dv_pool, to row-major dq_out, dk_out, dv_out with pitches (dq_out may be d_q with the pitch of a row).
  */
 psrl_status_t psrl_rope_qkv_fwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const void* q, int64_t q_pitch,
                                 const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* q_out,

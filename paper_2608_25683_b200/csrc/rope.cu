@@ -264,6 +264,11 @@ bool pitch_ok(int64_t pitch, int64_t heads, int d, psrl_dtype_t t) {
   return pitch >= heads * d && pitch <= (int64_t(1) << 40) && (pitch * es) % 16 == 0;
 }
 
+// In place, but with rows at other distances: a row would be written over one that has yet to be read.
+bool two_pitches(const void* x, int64_t x_pitch, const void* y, int64_t y_pitch, int64_t rows) {
+  return x && x == y && x_pitch != y_pitch && rows > 1;
+}
+
 // The pairs' frequencies; false if the description's scaling arguments make no sense.
 bool frequencies(const psrl_rope_desc_t& d, std::vector<double>& freq, double& scale) {
   const double r = d.rotary_dim, two_pi = 6.283185307179586476925286766559;
@@ -362,6 +367,7 @@ psrl_status_t psrl_rope_qkv_fwd(const psrl_plan_t* plan, const psrl_rope_t* rope
       (k && !pitch_ok(k_pitch, P.Hkv, P.d, P.dtype)) || (v && !pitch_ok(v_pitch, P.Hkv, P.d, P.dtype)) ||
       ((k || v) && pool_capacity < P.pool_slots))
     return PSRL_ERR_SHAPE;
+  if (two_pitches(q, q_pitch, q_out, int64_t(P.Hq) * P.d, P.T_q)) return PSRL_ERR_INVALID_ARG;
   if (!P.dev) return PSRL_ERR_WORKSPACE;
   RopeParams p{};
   const int64_t d = P.d;
@@ -387,6 +393,7 @@ psrl_status_t psrl_rope_qkv_bwd(const psrl_plan_t* plan, const psrl_rope_t* rope
       (dk_pool && !pitch_ok(dk_pitch, P.Hkv, P.d, P.dtype)) || (dv_pool && !pitch_ok(dv_pitch, P.Hkv, P.d, P.dtype)) ||
       ((dk_pool || dv_pool) && pool_capacity < P.pool_slots))
     return PSRL_ERR_SHAPE;
+  if (two_pitches(d_q, int64_t(P.Hq) * P.d, dq_out, dq_pitch, P.T_q)) return PSRL_ERR_INVALID_ARG;
   if (!P.dev) return PSRL_ERR_WORKSPACE;
   RopeParams p{};
   const int64_t d = P.d;
@@ -408,7 +415,7 @@ psrl_status_t psrl_rope_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const 
   const int64_t d = rope->desc.head_dim;
   if (!pitch_ok(x_pitch, n_heads, int(d), dtype) || !pitch_ok(y_pitch, n_heads, int(d), dtype)) return PSRL_ERR_SHAPE;
   if (n_rows == 0) return PSRL_OK;
-  if (!ptr_aligned(x, 16) || !ptr_aligned(y, 16) || !ptr_aligned(positions, 4) || (x == y && x_pitch != y_pitch))
+  if (!ptr_aligned(x, 16) || !ptr_aligned(y, 16) || !ptr_aligned(positions, 4) || two_pitches(x, x_pitch, y, y_pitch, n_rows))
     return PSRL_ERR_INVALID_ARG;
   RopeParams p{};
   p.part[0] = {x, y, x_pitch, d, y_pitch, d, 0, 0, n_heads, 1};

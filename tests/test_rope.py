@@ -102,3 +102,21 @@ def test_refusals(lib):
     assert rows(*change(8, 68)) == "PSRL_ERR_INVALID_ARG"        # in place with two pitches
     assert rows(*change(3, 60)) == "PSRL_ERR_SHAPE"
     assert rows(*change(5, 0)) == "PSRL_OK"                      # no rows, nothing launched
+
+
+def test_in_place_only_with_one_pitch(lib):
+    """q_out may be q, and dq_out d_q, where both are contiguous.  With rows further apart on one side a row would be written
+    over one that has yet to be read."""
+    L, plan, rope = lib.lib(), lib.Plan([-1, 0], [20, 5], [16], 2, 1, 64, "f32"), lib.Rope(64)
+    buf = ctypes.create_string_buffer(1 << 16)
+    p = (ctypes.addressof(buf) + 255) // 256 * 256
+    far = p + 32768
+    name = lambda st: lib.STATUS_NAMES[st]
+    fwd = lambda q, pitch, out: name(L.psrl_rope_qkv_fwd(plan.handle, rope._h, q, pitch, far, 64, far, 64, out, far, far, 64, None))
+    bwd = lambda q, out, pitch: name(L.psrl_rope_qkv_bwd(plan.handle, rope._h, q, far, far, 64, out, pitch, far, 64, far, 64, None))
+    assert fwd(p, 128, p) == fwd(p, 256, p + 8192) == "PSRL_ERR_WORKSPACE"      # accepted: only the upload is missing
+    assert bwd(p, p, 128) == bwd(p, p + 8192, 256) == "PSRL_ERR_WORKSPACE"
+    assert fwd(p, 256, p) == fwd(p, 132, p) == "PSRL_ERR_INVALID_ARG"
+    assert bwd(p, p, 256) == bwd(p, p, 132) == "PSRL_ERR_INVALID_ARG"
+    one = lib.Plan([-1], [1], [16], 2, 1, 64, "f32")                             # one row has no next one
+    assert name(L.psrl_rope_qkv_fwd(one.handle, rope._h, p, 256, far, 64, far, 64, p, far, far, 64, None)) == "PSRL_ERR_WORKSPACE"
