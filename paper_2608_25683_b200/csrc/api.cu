@@ -89,6 +89,11 @@ psrl_status_t psrl_plan_schedule(const psrl_plan_t* plan, const int32_t** words,
 
 psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off, const int32_t** next) {
   if (!plan || !plan->p || !off || !next) return PSRL_ERR_INVALID_ARG;
+  try {
+    psrl::next_tokens(*plan->p);
+  } catch (const std::bad_alloc&) {
+    return PSRL_ERR_HOST_OOM;
+  }
   *off = plan->p->next_off.data();
   *next = plan->p->next_tok.data();
   return PSRL_OK;

@@ -350,20 +350,6 @@ psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out) {
         P.seg_cascaded[c] = (fewer || starved) ? 1 : 0;
       }
     }
-    // what every query row predicts: the next token of its segment, or the first token of every child
-    P.next_off.assign(1, 0);
-    std::vector<std::vector<int32_t>> children(n);
-    for (int32_t c = 0; c < n; ++c)
-      if (P.seg_parent[c] >= 0) children[P.seg_parent[c]].push_back(c);
-    for (int32_t c = 0; c < n; ++c) {
-      if (P.seg_q_off[c] < 0) continue;
-      for (int32_t i = 0; i + 1 < P.seg_len[c]; ++i) {
-        P.next_tok.push_back(P.seg_tok_off[c] + i + 1);
-        P.next_off.push_back(static_cast<int32_t>(P.next_tok.size()));
-      }
-      for (int32_t x : children[c]) P.next_tok.push_back(P.seg_tok_off[x]);
-      P.next_off.push_back(static_cast<int32_t>(P.next_tok.size()));
-    }
     // per-segment list of KV tiles for the own items: non-cascaded ancestors root->parent, then own
     P.path_off.assign(n + 1, 0);
     std::vector<uint8_t> has_casc_anc(n, 0);
@@ -388,15 +374,16 @@ psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out) {
     // own items
     P.qrow_seg.resize(P.T_q);
     P.qrow_pos.resize(P.T_q);
-    P.qrow_slot.resize(P.T_q);
+    // with no cached segment the query rows are the tokens, and tok_slot has their slots
+    const bool rows_are_tokens = P.T_q == P.T;
+    if (!rows_are_tokens) P.qrow_slot.resize(P.T_q);
     std::vector<int32_t> own_part_base(n, -1);
     for (int32_t c = 0; c < n; ++c) {
       if (P.seg_q_off[c] < 0) continue;
-      for (int32_t i = 0; i < P.seg_len[c]; ++i) {
-        P.qrow_seg[P.seg_q_off[c] + i] = c;
-        P.qrow_pos[P.seg_q_off[c] + i] = P.seg_anc_tokens[c] + i;
-        P.qrow_slot[P.seg_q_off[c] + i] = P.tok_slot[P.seg_tok_off[c] + i];
-      }
+      const int32_t at = P.seg_q_off[c], len = P.seg_len[c];
+      std::fill_n(P.qrow_seg.begin() + at, len, c);
+      std::iota(P.qrow_pos.begin() + at, P.qrow_pos.begin() + at + len, P.seg_anc_tokens[c]);
+      if (!rows_are_tokens) std::copy_n(P.tok_slot.begin() + P.seg_tok_off[c], len, P.qrow_slot.begin() + at);
       if (has_casc_anc[c]) { own_part_base[c] = P.n_part_rows; P.n_part_rows += P.seg_len[c]; }
       const int32_t anc_tiles = (P.path_off[c + 1] - P.path_off[c]) - P.seg_n_kvt[c];
       for (int32_t t = 0; t < P.seg_n_kvt[c]; ++t) {
@@ -528,6 +515,12 @@ psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out) {
     H.n_qt = static_cast<int32_t>(P.q_tiles.size()); H.T = P.T; H.T_q = P.T_q;
     H.n_bt = static_cast<int32_t>(P.bt_pages.size());
     std::vector<int32_t>& B = P.blob;
+    // nearly all of it is per query row, token or tile; growing step by step would copy it several times over
+    B.reserve(P.qrow_seg.size() + P.tok_slot.size() + P.qrow_pos.size() + P.qrow_slot.size() + 2 * P.path_tiles.size() +
+              P.path_tiles.size() * (sizeof(TileLoad) / sizeof(int32_t)) +
+              P.kv_tiles.size() * (sizeof(KvTile) / sizeof(int32_t)) + P.q_tiles.size() * (sizeof(QTile) / sizeof(int32_t)) +
+              P.kv_items.size() * (sizeof(KvItem) / sizeof(int32_t)) + P.merge_row.size() + P.merge_off.size() + P.merge_parts.size() +
+              4 * P.page_slot.size() + P.bt_pages.size() + 16 * size_t(n) + 1024);
     B.assign(sizeof(DeviceHeader) / sizeof(int32_t), 0);
     H.off_seg_len = append_array(B, P.seg_len);
     H.off_seg_q_off = append_array(B, P.seg_q_off);
@@ -549,7 +542,7 @@ psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out) {
     H.off_qrow_seg = append_array(B, P.qrow_seg);
     H.off_tok_slot = append_array(B, P.tok_slot);
     H.off_qrow_pos = append_array(B, P.qrow_pos);
-    H.off_qrow_slot = append_array(B, P.qrow_slot);
+    H.off_qrow_slot = rows_are_tokens ? H.off_tok_slot : append_array(B, P.qrow_slot);
     H.off_kvt = append_array(B, P.kv_tiles);
     H.off_qt = append_array(B, P.q_tiles);
     H.off_kvi = append_array(B, P.kv_items);
@@ -593,6 +586,34 @@ psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out) {
   guard.p = nullptr;
   out = pl;
   return PSRL_OK;
+}
+
+// The next token of the row's segment, or the first token of every child.  A plan for the attention alone never needs it.
+void next_tokens(const Plan& P) {
+  std::call_once(P.next_once, [&] {
+    const int32_t n = P.n_seg;
+    std::vector<int32_t> first_child(n + 1, 0), child(n), off, tok;
+    for (int32_t c = 0; c < n; ++c)
+      if (P.seg_parent[c] >= 0) ++first_child[P.seg_parent[c] + 1];
+    std::partial_sum(first_child.begin(), first_child.end(), first_child.begin());
+    std::vector<int32_t> at(first_child.begin(), first_child.end() - 1);
+    for (int32_t c = 0; c < n; ++c)
+      if (P.seg_parent[c] >= 0) child[at[P.seg_parent[c]]++] = c;
+    off.reserve(size_t(P.T_q) + 1);
+    tok.reserve(size_t(P.T_q) + n);   // every row but a segment's last has one, every segment is one row's at most
+    off.push_back(0);
+    for (int32_t c = 0; c < n; ++c) {
+      if (P.seg_q_off[c] < 0) continue;
+      for (int32_t i = 0; i + 1 < P.seg_len[c]; ++i) {
+        tok.push_back(P.seg_tok_off[c] + i + 1);
+        off.push_back(static_cast<int32_t>(tok.size()));
+      }
+      for (int32_t k = first_child[c]; k < first_child[c + 1]; ++k) tok.push_back(P.seg_tok_off[child[k]]);
+      off.push_back(static_cast<int32_t>(tok.size()));
+    }
+    P.next_off.swap(off);
+    P.next_tok.swap(tok);
+  });
 }
 
 }  // namespace psrl

@@ -2,6 +2,7 @@
 // through psrl_plan_view_t plus the device work schedule the kernels consume.
 #pragma once
 #include <cstdint>
+#include <mutex>
 #include <vector>
 
 #include "../../include/psrl.h"
@@ -125,7 +126,9 @@ struct Plan {
   std::vector<int32_t> merge_row, merge_off, merge_parts;
   std::vector<TileLoad> path_loads;
   std::vector<int32_t> seg_first_kvt, seg_n_kvt, seg_desc_q_begin, seg_desc_q_end, path_off, path_tiles, path_nvalid, qrow_seg, qrow_pos, qrow_slot;
-  std::vector<int32_t> next_off, next_tok;  // [T_q + 1], the tokens that every query row predicts
+  // [T_q + 1], the tokens that every query row predicts: made by the first next_tokens()
+  mutable std::once_flag next_once;
+  mutable std::vector<int32_t> next_off, next_tok;
   // device blob
   std::vector<int32_t> blob;
   DeviceHeader hdr{};
@@ -133,6 +136,9 @@ struct Plan {
 };
 
 psrl_status_t build_plan(const psrl_tree_desc_t& desc, Plan*& out);
+
+// Fills next_off and next_tok; any number of threads may ask.  Throws std::bad_alloc.
+void next_tokens(const Plan& P);
 
 }  // namespace psrl
 

@@ -77,3 +77,25 @@ def test_refusals(lib):
     assert bwd(*change(19, need - 1)) == "PSRL_ERR_WORKSPACE"
     assert bwd(*change(14, p + 4)) == bwd(*change(16, p + 8)) == bwd(*change(18, p + 8)) == "PSRL_ERR_INVALID_ARG"
     assert bwd(*change(15, 60)) == bwd(*change(17, 72 - 4)) == "PSRL_ERR_SHAPE"
+
+
+def test_next_tokens_are_made_once_for_all_threads(lib):
+    """The plan makes them when they are first asked for, whoever asks: the same arrays for every thread, at the same place."""
+    from concurrent.futures import ThreadPoolExecutor
+
+    rng = np.random.default_rng(4)
+    parent, seg_len, gbs, flags = random_forest(rng, 40, 900, 2, cached_roots=True, step_samples=True)
+    L = lib.lib()
+
+    def ask(plan):
+        off, nxt = ctypes.POINTER(ctypes.c_int32)(), ctypes.POINTER(ctypes.c_int32)()
+        assert L.psrl_plan_next_tokens(plan.handle, ctypes.byref(off), ctypes.byref(nxt)) == 0
+        return ctypes.addressof(off.contents), ctypes.addressof(nxt.contents)
+
+    with ThreadPoolExecutor(8) as pool:
+        for _ in range(20):
+            plan = lib.Plan(parent, seg_len, gbs, 4, 2, 128, "bf16", seg_flags=flags)
+            assert len(set(pool.map(ask, [plan] * 16))) == 1
+    want = oracle_next_tokens(oracle_plan(parent, seg_len, gbs, flags))
+    off, tok = plan.next_tokens()
+    assert {r: sorted(tok[off[r]:off[r + 1]].tolist()) for r in range(len(off) - 1)} == want

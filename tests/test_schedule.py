@@ -229,3 +229,14 @@ def test_random_forests(lib):
             seg_len[0] = 1500
         plan = binding.Plan(parent, seg_len, gbs, 4, 2, 128, "bf16", seg_flags=flags)
         check_schedule(plan)
+
+
+def test_query_rows_share_the_tokens_slots(lib):
+    """Where no segment is cached the query rows are the tokens: the schedule that travels to the device has their slots once."""
+    for flags, shared in ((None, True), ([0, 1 | 2, 1 | 2], False)):
+        plan = lib.Plan([-1, 0, 0], [200, 70, 130], [64], 4, 2, 128, "bf16", seg_flags=flags)
+        H = decode(plan)["H"]
+        assert (H["off_qrow_slot"] == H["off_tok_slot"]) == shared
+        w, V = plan.schedule(), plan.view
+        first = 0 if shared else 200
+        assert np.array_equal(w[H["off_qrow_slot"]:H["off_qrow_slot"] + V["T_q"]], V["tok_slot"][first:])
