@@ -405,7 +405,63 @@ def psrl_tree_attn_bwd(plan: Plan, q, k_pool, v_pool, o, lse, d_o, softmax_scale
     return d_q, dk_pool, dv_pool
 
 
-def psrl_device_status(plan: Plan, kind: str = "fwd", stream=None, device="cuda") -> int:
+class Workspace:
+    """Device memory for a call's temporaries and its status word, for psrl_kv_move and the token log-probabilities
+    (`workspace=`).  status() tells whether a wait inside the kernels gave up; without a workspace of one's own the
+    log-probabilities make one that is gone when the call returns, and its status with it.  Calls that may overlap on the GPU
+    need workspaces of their own."""
+
+    __slots__ = ("ptr", "nbytes", "_buf", "_home", "_raw")
+
+    def __init__(self, nbytes: int, device="cuda", stream=None, _raw=None):
+        """On `stream` of the device (a torch stream), or its current one."""
+        import torch
+
+        self.nbytes = nbytes = nbytes if nbytes > 256 else 256
+        if stream is None:
+            buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+        else:
+            buf = _new(stream, nbytes + 256, torch.uint8, device)
+        self._buf = buf
+        self.ptr = (buf.data_ptr() + 255) // 256 * 256
+        self._raw = _raw     # stream of the last call
+        # the stream that the memory belongs to
+        if _raw is None:
+            _raw = _cuda()._cuda_getCurrentRawStream(buf.get_device()) if stream is None else stream.cuda_stream
+        self._home = _raw
+
+    def __iter__(self):
+        return iter((self.ptr, self.nbytes))
+
+    def status(self) -> int:
+        """PSRL_OK, or PSRL_ERR_TIMEOUT where the last call's results are not to be used (psrl_kv_move: nor its pools).  Waits
+        for the stream of that call."""
+        if self._raw is None:
+            raise RuntimeError("no call has used this workspace")
+        import torch
+
+        with torch.cuda.device(self._buf.device):
+            return int(lib().psrl_device_status(self.ptr, self._raw))
+
+
+def _use_workspace(workspace, raw: int, keep, dev: int):
+    """(pointer, bytes) of what the caller passed, a Workspace or such a pair, for a call on a stream."""
+    if isinstance(workspace, Workspace):
+        if workspace._buf.get_device() != dev:
+            raise ValueError(f"workspace on {workspace._buf.device}, tensors on cuda:{dev}")
+        workspace._raw = raw
+        if raw != workspace._home:   # its memory must outlive this call, too
+            import torch
+
+            workspace._buf.record_stream(keep or torch.cuda.current_stream(dev))
+    ptr, nbytes = workspace
+    return ptr, nbytes
+
+
+def psrl_device_status(plan, kind: str = "fwd", stream=None, device="cuda") -> int:
+    """Status of the last attention call of `plan`, or of the last call with a Workspace."""
+    if isinstance(plan, Workspace):
+        return plan.status()
     ws, _ = plan.workspace(kind, device)
     return int(lib().psrl_device_status(C.c_void_p(ws), _stream_ptr(stream)))
 
@@ -712,18 +768,20 @@ def psrl_kv_copy(extents, k_src, v_src, k_dst, v_dst, stream=None):
 
 def psrl_kv_move(moves, k_pool, v_pool, stream=None, workspace=None):
     """Performs the moves of a compaction ([n, 3], ascending, downwards: Cache.compact()) inside the pools, as if every
-    source were read first.  `workspace`: (pointer, bytes) of 256 bytes of device memory; allocated if not given."""
+    source were read first.  `workspace`: a Workspace, or (pointer, bytes) of 256 bytes of device memory; made if not given.
+    Returns the workspace; its status() tells whether the move came to its end (a wait that gave up leaves the pools half
+    moved)."""
     heads, cap, row = _pair_of_pools(k_pool, v_pool, "pools")
     e, n, at = _extents(moves)
     dev = _device_of(k_pool, v_pool)
     raw, keep = _stream_on(stream, dev)
     if workspace is None:
-        import torch
-
-        buf = _new(keep, 512, torch.uint8, k_pool.device)
-        workspace = ((buf.data_ptr() + 255) // 256 * 256, 256)
-    _launch("psrl_kv_move", dev, at, n, heads, row, k_pool.data_ptr(), v_pool.data_ptr(), cap, workspace[0], workspace[1],
-            raw)
+        workspace = Workspace(256, k_pool.device, keep, raw)
+        ws, wsb = workspace.ptr, 256
+    else:
+        ws, wsb = _use_workspace(workspace, raw, keep, dev)
+    _launch("psrl_kv_move", dev, at, n, heads, row, k_pool.data_ptr(), v_pool.data_ptr(), cap, ws, wsb, raw)
+    return workspace
 
 
 def psrl_token_logprob_workspace_bytes(n_rows: int, hidden_dim: int, vocab: int, n_targets: int, backward: bool,
@@ -757,21 +815,20 @@ def _matrix_pitch(t, name: str) -> int:
     return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8   # one row: any pitch will do
 
 
-def _logprob_workspace(workspace, keep, dt, n, h, v, m, backward, device):
-    import torch
-
-    if workspace is not None:
-        return workspace
-    need = int(lib().psrl_token_logprob_workspace_bytes(dt, n, h, v, m, backward))
-    buf = _new(keep, need + 256, torch.uint8, device)
-    return (buf.data_ptr() + 255) // 256 * 256, need
+def _logprob_workspace(workspace, raw, keep, dt, n, h, v, m, backward, device):
+    """(pointer, bytes, what holds the memory until the call is on its stream)"""
+    if workspace is None:
+        workspace = Workspace(lib().psrl_token_logprob_workspace_bytes(dt, n, h, v, m, backward), device, keep, raw)
+        return workspace.ptr, workspace.nbytes, workspace
+    return (*_use_workspace(workspace, raw, keep, device.index), workspace)
 
 
 def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: float = 1.0, logprob=None, lse=None, stream=None,
                            workspace=None):
     """Log-probabilities of `targets` (int32) under softmax(scale * hidden weight^T), without storing the logits.  hidden
     [rows, H], weight [vocab, H], both bf16 or both f32; row r's targets are targets[target_off[r] : target_off[r + 1]], or targets[r] without
-    target_off.  Returns (logprob [targets], lse [rows]), fp32."""
+    target_off.  `workspace`: a Workspace of psrl_token_logprob_workspace_bytes(), whose status() tells whether a wait inside
+    the kernels gave up; made if not given.  Returns (logprob [targets], lse [rows]), fp32."""
     import torch
 
     dt, n, h, v, m = _logprob_args(hidden, weight, targets, target_off, [])
@@ -783,7 +840,7 @@ def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: floa
         logprob = _new(keep, m, torch.float32, hidden.device)
     if lse is None:
         lse = _new(keep, n, torch.float32, hidden.device)
-    ws, wsb = _logprob_workspace(workspace, keep, dt, n, h, v, m, False, hidden.device)
+    ws, wsb, held = _logprob_workspace(workspace, raw, keep, dt, n, h, v, m, False, hidden.device)
     _launch("psrl_token_logprob_fwd", dev, dt, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
             _matrix_pitch(weight, "weight"), targets.data_ptr(), m,
             None if target_off is None else target_off.data_ptr(), float(scale), logprob.data_ptr(),
@@ -794,7 +851,7 @@ def psrl_token_logprob_fwd(hidden, weight, targets, target_off=None, scale: floa
 def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, target_off=None, scale: float = 1.0, d_hidden=None,
                            d_weight=None, want_hidden: bool = True, want_weight: bool = True, stream=None, workspace=None):
     """Gradients of the above: (d_hidden, d_weight), of hidden's type, given d_logprob [targets] and the forward's logprob and lse.
-    want_hidden / want_weight False: that one is None and not computed."""
+    want_hidden / want_weight False: that one is None and not computed.  `workspace` as above (backward True)."""
     m = targets.shape[0]
     dt, n, h, v, m = _logprob_args(hidden, weight, targets, target_off,
                                    [("logprob", logprob, m), ("lse", lse, hidden.shape[0]), ("d_logprob", d_logprob, m)])
@@ -809,7 +866,7 @@ def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, tar
     if d_weight is None and want_weight:
         d_weight = _new(keep, (v, h), hidden.dtype, hidden.device)
     out = [t if w else None for t, w in ((d_hidden, want_hidden), (d_weight, want_weight))]
-    ws, wsb = _logprob_workspace(workspace, keep, dt, n, h, v, m, True, hidden.device)
+    ws, wsb, held = _logprob_workspace(workspace, raw, keep, dt, n, h, v, m, True, hidden.device)
     args = [x for t, name in zip(out, ("d_hidden", "d_weight"))
             for x in ((None, 0) if t is None else (t.data_ptr(), _matrix_pitch(t, name)))]
     _launch("psrl_token_logprob_bwd", dev, dt, n, h, v, hidden.data_ptr(), _matrix_pitch(hidden, "hidden"), weight.data_ptr(),
