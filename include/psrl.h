@@ -385,9 +385,10 @@ psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off
  *   logprob, d_logprob [n_targets], lse [n_rows] DEVICE fp32 (backward: as produced by the forward)
  *   d_hidden, d_weight  DEVICE of `dtype` as their tensors, fully overwritten; NULL: not wanted
  *   workspace  DEVICE, >= psrl_token_logprob_workspace_bytes, 256-byte aligned; holds the device status word.  Forward:
- *              at most 12 bytes per row and 128 entries of the vocabulary (1024 where there are thousands of rows);
- *              backward: 16 KB per row, or 128 MB if that is more, for a piece of dz, three times `hidden`, and 24 bytes
- *              per target, whatever the vocabulary.
+ *              at most 16 bytes per row and 128 entries of the vocabulary (2 bytes where there are thousands of rows), and 8 MB;
+ *              backward, with R = n_rows in whole 128s, at least 256: a piece of dz, 64 Mi numbers or 8192 per row of R if
+ *              that is more; R rows of `hidden`; sums in fp32, R rows or 64 MB if that is more (bf16); 40 bytes per row and 24
+ *              per target; whatever the vocabulary.  (Numbers and rows of `dtype`.)
  * hidden_dim is a multiple of 8, pitches are multiples of 16 bytes, tensors 16-byte aligned and apart from the outputs.
  * n_rows = 0 does nothing (backward: zeroes d_weight).  Rows, targets and vocabulary are at most 2^30.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), WORKSPACE, CUDA.  Asynchronous; calls that may overlap on the GPU need

@@ -1092,9 +1092,12 @@ Layout layout(psrl_dtype_t dtype, int64_t n, int64_t h, int64_t v, int64_t n_tar
     L.part = take(size_t(L.n_parts) * n * sizeof(float2));
     if (!L.few) L.part_at = take(size_t(L.n_parts) * n * sizeof(int32_t));
   } else {
-    // a piece of dz is about 128 MB (it then partly stays in the L2 for the two products that read it) but at least
+    L.twice = !f32 && n <= kTwiceRows;
+    L.rows = L.twice ? 256 : round_up(n, kBK);
+    L.acc_rows = L.twice ? 256 : round_up(n, 128);
+    // a piece of dz is 64 Mi numbers (in bf16 it then partly stays in the L2 for the two products that read it) but at least
     // 8192 entries wide: below that the fp32 sums of d_hidden cost more traffic than the products hide
-    const int64_t most_wide = std::max<int64_t>(8192, (int64_t(64) << 20) / n);
+    const int64_t most_wide = std::max<int64_t>(8192, (int64_t(64) << 20) / L.rows / 256 * 256);
     const int64_t pieces = (v + most_wide - 1) / most_wide;
     L.piece = round_up((v + pieces - 1) / pieces, 256);
     L.row_info = take(size_t(n) * sizeof(float2));
@@ -1102,9 +1105,6 @@ Layout layout(psrl_dtype_t dtype, int64_t n, int64_t h, int64_t v, int64_t n_tar
     L.entry = take(size_t(n_targets) * sizeof(float));
     L.table = take(2 * size_t(n_targets) * sizeof(TokenSum));
     L.row_at = take(size_t(n_targets) * sizeof(int32_t));
-    L.twice = !f32 && n <= kTwiceRows;
-    L.rows = L.twice ? 256 : round_up(n, kBK);
-    L.acc_rows = L.twice ? 256 : round_up(n, 128);
     L.matters = take(size_t(n + 7) / 8 + 3);
     L.row_of = take(size_t(n) * sizeof(int32_t));
     L.count = take(sizeof(int32_t));

@@ -357,3 +357,39 @@ def test_pairs_that_keep_pace(lib, h):
     torch.cuda.synchronize()
     for x in got:
         assert torch.equal(x[0], lp) and torch.equal(x[1], lse)
+
+
+@pytest.mark.parametrize("n,dtype", [(1, torch.bfloat16), (5, torch.bfloat16), (128, torch.bfloat16), (200, torch.bfloat16), (3, torch.float32)])
+def test_few_rows_over_several_pieces(lib, n, dtype):
+    """A vocabulary of more than one piece for few rows, whose dz is kept in two parts, with several targets a row."""
+    h, v, m = 16, 600011 if n <= 128 else 700001, 3 * n
+    if dtype == torch.float32:
+        v = 1100003
+    hidden, weight, targets, g = make(n, h, v, 70 + n, m=m, dtype=dtype)
+    off = torch.arange(0, m + 1, 3, device="cuda", dtype=torch.int32)
+    targets[1] = targets[0]
+    targets[2] = v - 1
+    lp, lse = lib.psrl_token_logprob_fwd(hidden, weight, targets, off)
+    dh, dw = lib.psrl_token_logprob_bwd(hidden, weight, targets, lp, lse, g, off)
+    hd, wd, gd, t = hidden.double(), weight.double(), g.double(), targets.long()
+    row = torch.arange(n, device="cuda").repeat_interleave(3)
+    z = hd @ wd.T
+    ref = torch.logsumexp(z, 1)
+    a = (hd.abs() @ wd.abs().T).amax(1)
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+    zerr = sum_error(h, dtype) * a
+    lerr = zerr + 2.0 ** -20 + 2.0 ** -22 * ref.abs()
+    assert ((lse.double() - ref).abs() <= lerr).all()
+    want = z[row, t] - ref[row]
+    lperr = lerr[row] + zerr[row] + 2.0 ** -22 * (want.abs() + 2 * ref[row].abs())
+    assert ((lp.double() - want).abs() <= lperr).all()
+    total = torch.zeros(n, device="cuda", dtype=torch.float64).index_add_(0, row, gd)
+    dz = -total[:, None] * torch.exp(z - ref[:, None])
+    dz.index_put_((row, t), gd, accumulate=True)
+    moved = (total[row].abs() * lperr)[:, None]
+    far_h = torch.zeros_like(hd).index_add_(0, row, moved * wd[t].abs())
+    far_w = torch.zeros_like(wd).index_add_(0, t, moved * hd[row].abs())
+    pe = float((lerr + zerr).max()) * 2 + half + 2.0 ** -18
+    for got, d, absd, k, far in ((dh, dz @ wd, dz.abs() @ wd.abs(), v, far_h), (dw, dz.T @ hd, dz.abs().T @ hd.abs(), n, far_w)):
+        tol = far + (pe + sum_error(k, dtype) + 2.0 ** -18) * absd + half * d.abs() * (1 + 2.0 ** -7) + 1e-37
+        assert ((got.double() - d).abs() <= tol).all()

@@ -99,3 +99,26 @@ def test_next_tokens_are_made_once_for_all_threads(lib):
     want = oracle_next_tokens(oracle_plan(parent, seg_len, gbs, flags))
     off, tok = plan.next_tokens()
     assert {r: sorted(tok[off[r]:off[r + 1]].tolist()) for r in range(len(off) - 1)} == want
+
+
+def workspace_bound(dtype, n, h, v, m, backward):
+    """What include/psrl.h says a call may take."""
+    if n == 0:
+        return 256
+    if not backward:
+        return 16 * n * (v // 128 + 2) + (8 << 20)
+    es, rows = (4 if dtype == "f32" else 2), max(256, -(-n // 128) * 128)
+    wide = -(-h // 32) * 32
+    return es * max(64 << 20, 8192 * rows) + es * rows * h + max(4 * rows * wide, 64 << 20) + 40 * n + 24 * m + 4096
+
+
+def test_workspace_keeps_to_its_bounds(lib):
+    """Few rows, many rows, narrow and wide: never more than the header says, whatever the vocabulary."""
+    for dtype in ("bf16", "f32"):
+        for n in (0, 1, 2, 4, 5, 8, 16, 40, 64, 100, 128, 129, 200, 256, 257, 342, 512, 520, 777, 1000, 4096, 8192, 8193, 50000, 200000):
+            for h in (8, 64, 72, 1024, 3584, 4096, 8192, 16384):
+                for v in (1, 7, 100, 1000, 20000, 50257, 131072, 1 << 18, (1 << 18) + 1, 1 << 20, 1 << 24, 1 << 30):
+                    for m in (0, n, 3 * n):
+                        for backward in (False, True):
+                            got = lib.psrl_token_logprob_workspace_bytes(n, h, v, m, backward, dtype)
+                            assert got <= workspace_bound(dtype, n, h, v, m, backward), (dtype, n, h, v, m, backward, got)
