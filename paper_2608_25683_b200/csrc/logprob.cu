@@ -1115,7 +1115,7 @@ Layout layout(psrl_dtype_t dtype, int64_t n, int64_t h, int64_t v, int64_t n_tar
     // piece; two units for every pair, of at least 16 steps, share that out (777 rows, half of them without targets, one unit
     // for every pair 462 us, two 426, four 432).
     const int64_t tiles = m_tiles * ((h + 255) / 256), most = std::min<int64_t>(16, L.piece / kBK / 16);
-    L.splits = tiles >= 74 ? 1 : static_cast<int32_t>(std::max<int64_t>(1, std::min(most, (148 + tiles - 1) / tiles)));
+    L.splits = tiles >= pairs ? 1 : static_cast<int32_t>(std::max<int64_t>(1, std::min(most, (2 * pairs + tiles - 1) / tiles)));
     if (!f32) L.acc = take(size_t(L.splits) * L.acc_rows * round_up(h, 32) * sizeof(float));
   }
   L.total = at;
