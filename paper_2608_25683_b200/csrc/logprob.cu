@@ -1169,11 +1169,18 @@ cudaError_t launch_few(const Layout& L, int32_t M, int32_t h, int32_t v, const v
                 hp / 8, static_cast<const uint4*>(weight), wp / 8, scale * kLog2e, part, status);
 }
 
+// One launch counts 65,535 blocks of rows; further rows take further launches.
 template <F32Kind kKind>
-cudaError_t launch_f32(const F32Params& p, int64_t col_blocks, int64_t rows, bool first, cudaStream_t stream) {
+cudaError_t launch_f32(F32Params p, int64_t col_blocks, int64_t rows, bool first, cudaStream_t stream) {
+  constexpr int64_t kMost = 65535;
   const int64_t row_blocks = (rows + kF32Tile - 1) / kF32Tile;
-  if (row_blocks > 65535 || col_blocks > INT32_MAX) return cudaErrorInvalidValue;
-  return launch(f32_kernel<kKind>, dim3(unsigned(col_blocks), unsigned(row_blocks)), 256, 0, stream, first, p);
+  if (col_blocks > INT32_MAX) return cudaErrorInvalidValue;
+  cudaError_t e = cudaSuccess;
+  for (int64_t at = 0; e == cudaSuccess && at < row_blocks; at += kMost) {
+    p.row0 = static_cast<int32_t>(at * kF32Tile);
+    e = launch(f32_kernel<kKind>, dim3(unsigned(col_blocks), unsigned(std::min(kMost, row_blocks - at))), 256, 0, stream, first && at == 0, p);
+  }
+  return e;
 }
 
 psrl_status_t cuda_failed(cudaError_t e) {

@@ -14,6 +14,7 @@ struct F32Params {
   const float *a, *b;            // operands; where an element (m, k) of A lies depends on the kind (see f32_kernel)
   int64_t a_pitch, b_pitch;
   int32_t M, N, K;
+  int32_t row0;                  // first row of the launch
   const int32_t* count;          // rows that matter: M of kF32Dz, kF32Dh, K of kF32Dw
   const int32_t* row_of;         // the caller's row of a gathered row
   float scale_log2;
@@ -55,7 +56,7 @@ __global__ void __launch_bounds__(256) f32_kernel(const F32Params p) {
   next_kernel_may_start();
   const int rows = kKind == kF32Lse ? p.M : *p.count;
   const int M = kKind == kF32Dw ? p.M : rows, K = kKind == kF32Dw ? rows : p.K;
-  const int m0 = blockIdx.y * kF32Tile, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  const int m0 = p.row0 + int(blockIdx.y) * kF32Tile, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
   if (m0 >= M) return;
   float best[4], sum[4];
 #pragma unroll
