@@ -121,7 +121,7 @@ psrl_status_t psrl_cache_compact(psrl_cache_t* cache, int32_t* n_moves, const ps
  *
  * psrl_kv_move - the same inside one pair of pools, for moves down that may overlap: as if every source were read before
  * anything is written.
- *   extents    ascending in source and destination, each disjoint from the next, dst_slot <= src_slot
+ *   extents    ascending in source and destination, each disjoint from the next, dst_slot <= src_slot; n_slots = 0 does nothing
  *   workspace  DEVICE, 256 bytes, 256-byte aligned: status word (psrl_device_status) and counters; calls that may overlap
  *              on the GPU need distinct workspaces
  * Slots that no destination covers keep what they held.  Errors as above, and WORKSPACE.

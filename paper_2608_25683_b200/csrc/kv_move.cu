@@ -460,8 +460,8 @@ psrl_status_t psrl_kv_move(const psrl_kv_extent_t* extents, int32_t n_extents, i
     for (int32_t i = 0; i < n_extents; ++i) {
       const psrl_kv_extent_t& e = extents[i];
       if (!in_range(e, pool_capacity, pool_capacity)) return PSRL_ERR_SHAPE;
-      if (e.dst_slot > e.src_slot || e.src_slot < src_end || e.dst_slot < dst_end) return PSRL_ERR_INVALID_ARG;
       if (e.n_slots == 0) continue;
+      if (e.dst_slot > e.src_slot || e.src_slot < src_end || e.dst_slot < dst_end) return PSRL_ERR_INVALID_ARG;
       src_end = int64_t(e.src_slot) + e.n_slots;
       dst_end = int64_t(e.dst_slot) + e.n_slots;
       if (e.dst_slot != e.src_slot) list.push_back(e);

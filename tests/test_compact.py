@@ -128,3 +128,19 @@ def test_copy_and_move_refusals(lib):
     assert move(none, wsb=255) == "PSRL_ERR_WORKSPACE"
     with pytest.raises(ValueError):
         binding._extents([[1, 2], [3, 4]])
+
+
+def test_empty_extents_of_a_move_do_nothing(lib):
+    """Wherever they are listed, as in a copy: only the extents with slots have to ascend."""
+    L = lib.lib()
+    buf = ctypes.create_string_buffer(1 << 16)
+    p = (ctypes.addressof(buf) + 255) // 256 * 256
+
+    def move(e):
+        # no pools: a call that passes the checks has nothing to move, and clears the workspace where there is a GPU
+        return lib.STATUS_NAMES[L.psrl_kv_move(e.ctypes.data, len(e), 2, 128, None, None, 32, p, 256, None)]
+
+    for e in (ext([3, 9, 0]), ext([8, 4, 4], [2, 2, 0], [12, 8, 4]), ext([8, 8, 4], [2, 3, 0])):
+        assert move(e) not in ("PSRL_ERR_INVALID_ARG", "PSRL_ERR_SHAPE")
+    assert move(ext([31, 33, 0])) == "PSRL_ERR_SHAPE"                            # out of the pool all the same
+    assert move(ext([3, 9, 1])) == move(ext([8, 4, 4], [2, 2, 1])) == "PSRL_ERR_INVALID_ARG"
