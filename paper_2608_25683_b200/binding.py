@@ -616,6 +616,7 @@ class Rope:
                  scaling: Optional[str] = None, factor: float = 1.0, original_positions: int = 0, low: float = 0.0,
                  high: float = 0.0, attention_scale: float = 0.0):
         self._h = C.c_void_p()
+        self._destroy = lib().psrl_rope_destroy
         if layout not in _ROPE_LAYOUTS or scaling not in _ROPE_SCALINGS:
             raise ValueError(f"layout {layout!r} or scaling {scaling!r} unknown")
         d = RopeDesc(int(head_dim), int(rotary_dim or head_dim), _ROPE_LAYOUTS[layout], _ROPE_SCALINGS[scaling], float(base),
@@ -628,8 +629,8 @@ class Rope:
 
     def __del__(self):
         if getattr(self, "_h", None) and self._h.value:
-            lib().psrl_rope_destroy(self._h)
-            self._h = C.c_void_p()
+            self._destroy(self._h)      # held by the object: at the interpreter's end this module's names may be gone
+            self._h.value = None
 
 
 def _rows_pitch(t, rows: int, heads: int, d: int, name: str) -> int:
@@ -936,6 +937,7 @@ class Cache:
     def __init__(self, parent, seg_len, group_block_size, mb_of_seg, n_microbatches: int, seg_flags=None,
                  capacity_slots: int = 0):
         self._h = C.c_void_p()
+        self._destroy = lib().psrl_cache_destroy
         p, l, g, mb = _i32(parent), _i32(seg_len), _i32(group_block_size), _i32(mb_of_seg)
         d = CacheDesc()
         d.n_segments = len(p)
@@ -991,8 +993,8 @@ class Cache:
 
     def __del__(self):
         if getattr(self, "_h", None) and self._h.value:
-            lib().psrl_cache_destroy(self._h)
-            self._h = C.c_void_p()
+            self._destroy(self._h)      # held by the object: at the interpreter's end this module's names may be gone
+            self._h.value = None
 
 
 def psrl_launch_count(plan: Plan, backward: bool) -> int:

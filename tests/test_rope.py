@@ -1,5 +1,8 @@
 """Rotary positions, host side: frequencies against the oracle's, the plan's positions and slots of the query rows, refusals."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -120,3 +123,13 @@ def test_in_place_only_with_one_pitch(lib):
     assert bwd(p, p, 256) == bwd(p, p, 132) == "PSRL_ERR_INVALID_ARG"
     one = lib.Plan([-1], [1], [16], 2, 1, 64, "f32")                             # one row has no next one
     assert name(L.psrl_rope_qkv_fwd(one.handle, rope._h, p, 256, far, 64, far, 64, p, far, far, 64, None)) == "PSRL_ERR_WORKSPACE"
+
+
+def test_handles_that_outlive_the_interpreter(lib):
+    """Plans, rotary embeddings and caches held in a module's names until the process ends: nothing is complained about."""
+    code = ("import torch\n"
+            "from paper_2608_25683_b200 import binding as b\n"
+            "kept = [b.Rope(64), b.Plan([-1], [20], [16], 2, 1, 64, 'f32'), b.Cache([-1], [16], [16], [0], 1)]\n"
+            "def use(): return b\n")
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert out.returncode == 0 and out.stderr == ""
