@@ -433,15 +433,15 @@ class Workspace:
     def __iter__(self):
         return iter((self.ptr, self.nbytes))
 
-    def status(self) -> int:
+    def status(self, stream=None) -> int:
         """PSRL_OK, or PSRL_ERR_TIMEOUT where the last call's results are not to be used (psrl_kv_move: nor its pools).  Waits
-        for the stream of that call."""
+        for the stream of that call, or for `stream`: the one that a graph with the call was replayed on."""
         if self._raw is None:
             raise RuntimeError("no call has used this workspace")
         import torch
 
         with torch.cuda.device(self._buf.device):
-            return int(lib().psrl_device_status(self.ptr, self._raw))
+            return int(lib().psrl_device_status(self.ptr, self._raw if stream is None else _stream_ptr(stream)))
 
 
 def _use_workspace(workspace, raw: int, keep, dev: int):
@@ -461,7 +461,7 @@ def _use_workspace(workspace, raw: int, keep, dev: int):
 def psrl_device_status(plan, kind: str = "fwd", stream=None, device="cuda") -> int:
     """Status of the last attention call of `plan`, or of the last call with a Workspace."""
     if isinstance(plan, Workspace):
-        return plan.status()
+        return plan.status(stream)
     ws, _ = plan.workspace(kind, device)
     return int(lib().psrl_device_status(C.c_void_p(ws), _stream_ptr(stream)))
 

@@ -57,3 +57,33 @@ def test_log_probabilities_with_a_workspace_of_the_callers(lib, n, dtype):
     assert e.value.name == "PSRL_ERR_WORKSPACE"
     with pytest.raises(ValueError):
         lib.psrl_kv_move([], *pools(1, 1, 4, 128, "bf16"), workspace=(1, 2, 3))
+
+
+def test_captured_calls_with_workspaces_of_their_own(lib):
+    """Two graphs, each with its workspace, replayed on streams of their own; the status of a replay is that stream's."""
+    k0, v0 = pools(3, 4, 9000, 128, "bf16")
+    e = [[100, 20, 8800]]
+    want = plain(e, k0, k0), plain(e, v0, v0)
+    hidden, weight, targets, g = make(300, 64, 1000, 4)
+    lp, lse = lib.psrl_token_logprob_fwd(hidden, weight, targets)
+    grads = lib.psrl_token_logprob_bwd(hidden, weight, targets, lp, lse, g)
+    jobs = []
+    for _ in range(2):
+        k, v = k0.clone(), v0.clone()
+        move, loss = lib.Workspace(256), lib.Workspace(lib.psrl_token_logprob_workspace_bytes(300, 64, 1000, 300, True))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            lib.psrl_kv_move(e, k, v, workspace=move)
+            out = lib.psrl_token_logprob_bwd(hidden, weight, targets, lp, lse, g, workspace=loss)
+        jobs.append((graph, k, v, move, loss, out, torch.cuda.Stream()))
+    for _ in range(3):
+        for graph, k, v, *_ in jobs:
+            k.copy_(k0), v.copy_(v0)
+        torch.cuda.synchronize()
+        for graph, k, v, move, loss, out, stream in jobs:
+            with torch.cuda.stream(stream):
+                graph.replay()
+        for graph, k, v, move, loss, out, stream in jobs:
+            assert move.status(stream) == loss.status(stream) == lib.psrl_device_status(loss, stream=stream) == lib.PSRL_OK
+            assert torch.equal(bits(k).cpu(), want[0]) and torch.equal(bits(v).cpu(), want[1])
+            assert all(torch.equal(a, b) for a, b in zip(out, grads))
