@@ -293,7 +293,8 @@ psrl_status_t psrl_kv_gather(const psrl_plan_t* plan, const void* k_pool, const 
  *   YARN    pairs that make more than `high` turns over the original length keep f_i, pairs below `low` turns get
  *           f_i / factor, a linear ramp over the pair index between them; s = 0.1 ln(factor) + 1
  *           (Peng et al. 2023; low = 0 means 1, high = 0 means 32)
- *   BANDED  the same two ends with the ramp linear in the number of turns (low = 0 means 1, high = 0 means 4)
+ *   BANDED  the same two ends with the ramp linear in the number of turns (low = 0 means 1, high = 0 means 4): the
+ *           scaling by wavelength that open-weight long-context models published with their configurations in 2024
  * s is 1 unless YARN sets it; attention_scale > 0 replaces it.  Angles are computed exactly modulo a full turn
  * (64-bit fixed point), so far positions lose nothing.
  */

@@ -107,7 +107,7 @@ psrl_status_t copy_extents(const psrl_kv_extent_t* ext, int32_t n, const Pools& 
 //                 gets loaded whatever the others do, and the parts waited for are no later ones, so the waits end
 //                 (move_order.h has the arithmetic and why the counts of 32 groups are enough).
 //                 169,632 slots of 4 KB:
-//                 235 us, 5.9 TB/s; the same copied to other pools, where nothing waits, 209 us.  (Chunks of the whole
+//                 239 us, 5.8 TB/s; the same copied to other pools, where nothing waits, 209 us.  (Chunks of the whole
 //                 grid, stored once every block had loaded its share of them, took 270 us in registers and 296 us through
 //                 six stages of shared memory: all blocks ran at the pace of the slowest.)
 //   small moves   one cluster of up to eight blocks and its hardware barrier: an ordinary launch, nothing to zero first;
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kMoveThreads, 1) move_cluster_kernel(const __g
   }
 }
 
-// Three warps with 64 KB each; twelve with 16 KB take 328 us instead of 235: the counters, one line of the L2, bound them.
+// Three warps with 64 KB each; twelve with 16 KB take 328 us instead of 239: the counters, one line of the L2, bound them.
 constexpr int kBulkWarps = 3, kBulkBytes = 64 * 1024, kBulkLanes = 8;   // a lane's share of a part: 8 KB
 constexpr size_t kBulkSmem = size_t(kBulkWarps) * kBulkBytes;
 

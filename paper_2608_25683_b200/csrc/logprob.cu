@@ -171,8 +171,10 @@ __device__ __forceinline__ void unit_tile(int group, int m_tiles, int unit, int 
 // SMs) waits no more, and one that is through counts kPaceDone, which frees the others.  Forward, TFLOP/s with a pause
 // between the calls: 16384 x 8192 in units of 8 steps 1480 to 1535, without pace 1236 to 1500; 2048 x 16384 x 65536 1460, 1350; 1024 x 8192
 // 1440, 1270 to 1400; 8192 x 4096 in units of 16 1530 to 1580, 1450 to 1555 (units of 8 cost 3 % there back to back).  At a
-// hidden size of 2048 it loses up to 3 %, with 512 to 700 rows 1 %, with less than four rounds of tiles up to 13 %.  The gradients
-// lose 1 to 2 %: few pairs at work share an operand there.
+// hidden size of 2048 it loses up to 3 %, with 512 to 700 rows 1 %, with less than four rounds of tiles up to 13 %.  In between:
+// 3584 deep 8192 rows 1600 with pace, 1558 without, 16384 rows 1628, 1565, 2048 rows the same; 2560 deep 8192 rows 1610, 1589, 2048
+// rows 1430, 1470.  So the depth could be a little lower; it is where the gain is beyond doubt at every number of rows.  The
+// gradients lose 1 to 2 %: few pairs at work share an operand there.
 constexpr int kPaceTries = 200;
 constexpr size_t kPaceAt = 128;            // in the header of the workspace
 constexpr int kPaceRows = 1024, kPaceDepth = 4096;
@@ -618,8 +620,8 @@ gemm_kernel(const __grid_constant__ GemmMaps maps, const GemmParams p) {
 // and ordinary fp32 arithmetic keeps up, two multiply-adds an instruction.  A warp takes four vocabulary entries at a time
 // and holds their products with all kRows hidden rows, which lie in shared memory; running maximum and sum per row.
 constexpr int kFewThreads = 256, kFewV = 4;
-// Blocks of an SM, and of the launch for each SM: one wave, as every block gets the same share of the vocabulary (4 rows with
-// twice as many blocks 197 us, with these 190).
+// Blocks of an SM, and of the launch for each SM: one wave, as every block gets the same share of the vocabulary (4096 x 131072,
+// 4 rows: 185 us; twice as many blocks are no quicker and leave twice the partial sums).
 __host__ __device__ constexpr int few_blocks(int rows) { return rows == 1 ? 4 : rows == 2 ? 3 : 2; }
 constexpr size_t kFewSmem = 128 * 1024;   // hidden rows at most
 
@@ -1036,8 +1038,8 @@ namespace {
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Up to kFewRows rows the forward takes few_rows_kernel: 1, 2, 4 rows of 4096 x 131072 weights 185, 189, 190 us, all of
-// them 206 us by the matrix kernel, whose sums are less exact; with 8 rows it is 415 us (fp32 arithmetic) against 206.
+// Up to kFewRows rows the forward takes few_rows_kernel: 1, 2, 4 rows of 4096 x 131072 weights 164, 176, 185 us, by the
+// matrix kernel, whose sums are less exact, 257, 220, 222 (64 rows 205); 8 rows by this kernel were 415 us (fp32 arithmetic).
 constexpr int kFewRows = 4;
 
 struct Layout {
@@ -1113,7 +1115,7 @@ Layout layout(psrl_dtype_t dtype, int64_t n, int64_t h, int64_t v, int64_t n_tar
     L.dz = take(size_t(L.rows) * L.piece * es);
     // Parts of d_hidden's sum: with few rows there are fewer of its tiles than pairs of CTAs, and each is as deep as the
     // piece; two units for every pair, of at least 16 steps, share that out (777 rows, half of them without targets, one unit
-    // for every pair 462 us, two 426, four 432).
+    // for every pair 441 us, two 416, four 425: 30 calls after a pause; in long runs the power cap makes the 416 us 466).
     const int64_t tiles = m_tiles * ((h + 255) / 256), most = std::min<int64_t>(16, L.piece / kBK / 16);
     L.splits = tiles >= pairs ? 1 : static_cast<int32_t>(std::max<int64_t>(1, std::min(most, (2 * pairs + tiles - 1) / tiles)));
     if (!f32) L.acc = take(size_t(L.splits) * L.acc_rows * round_up(h, 32) * sizeof(float));
