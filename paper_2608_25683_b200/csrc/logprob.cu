@@ -809,7 +809,7 @@ __global__ void __launch_bounds__(kFinalThreads) final_kernel(const float2* __re
       if (fabsf(d) < 64.f) x.y = rest + exp2f(d);
       // logits so large that the two sums are far apart: the smaller of the largest term and the rest does not count
       else if (d < 0.f && rest > 0.f) x.y = rest;
-      else x = make_float2(z, 1.f);
+      else x = make_float2(z, rest == rest ? 1.f : rest);   // NaN stays
     }
     if (lane == 0) {
       const float l = ((x.x == -CUDART_INF_F ? 0.f : x.x) + log2f(x.y)) * kLn2;

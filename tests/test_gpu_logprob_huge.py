@@ -35,3 +35,13 @@ def test_finite_logits_of_any_size(lib, n, dtype, size, scale):
     # dz has at most the target and entries whose probabilities the logits' error can make one: every entry, in the worst case
     assert (np.abs(to_np(dh)) <= 1.01 * g_abs[:, None] * (top_w + np.abs(wn).sum(0))[None, :] + 1e-30).all()
     assert (np.abs(to_np(dw)) <= 1.01 * 2 * (g_abs[:, None] * top_h).sum(0)[None, :]).all()
+
+
+@pytest.mark.parametrize("n,dtype", [(3, torch.bfloat16), (40, torch.bfloat16), (300, torch.bfloat16), (40, torch.float32)])
+@pytest.mark.parametrize("size", [1.0, 1e10])
+def test_huge_logits_beside_one_that_is_no_number(lib, n, dtype, size):
+    hidden, weight, targets, g = make(n, 512, 700, n, dtype=dtype)
+    hidden = (hidden.float() * size).to(dtype)
+    weight[650, 3] = float("nan")
+    lp, lse = lib.psrl_token_logprob_fwd(hidden, weight, targets)
+    assert torch.isnan(lse).all() and torch.isnan(lp).all()
