@@ -355,6 +355,37 @@ psrl_status_t psrl_rope_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const 
                              int inverse, void* stream);
 
 /*
+ * Rotary positions with several axes (time, height and width of the tokens of images and video): pair i of a head is turned by
+ * positions[axis(i)] * f_i, with the frequencies and scalings above.  sections[a] pairs go by axis a:
+ *   BLOCKS  the first sections[0] pairs by axis 0, the next sections[1] by axis 1, and so on
+ *   CYCLIC  pair i by axis i % n_axes while i < n_axes * sections[i % n_axes], by axis 0 otherwise
+ * psrl_rope_create is the form with one axis.  The entry points above take a rope of several axes, too: a row's one position is
+ * then its position on every axis, which is what text has.
+ * n_axes 1..4; sections [n_axes] HOST, >= 0, of the sum rotary_dim / 2 and (CYCLIC) such that every axis gets its pairs.
+ * Errors: INVALID_ARG, SHAPE (dimensions, sections), HOST_OOM.  On error *out is NULL.
+ */
+typedef enum { PSRL_ROPE_BLOCKS = 0, PSRL_ROPE_CYCLIC = 1 } psrl_rope_order_t;
+psrl_status_t psrl_rope_create_axes(const psrl_rope_desc_t* desc, int32_t n_axes, const int32_t* sections, psrl_rope_order_t order,
+                                    psrl_rope_t** out);
+
+/*
+ * psrl_rope_axes_qkv_fwd / _bwd, psrl_rope_axes_rows - psrl_rope_qkv_fwd / _bwd and psrl_rope_rows with positions of the
+ * caller's own for each axis, in place of the tree's.
+ *   positions [n_axes, T_q] (axes_rows: [n_axes, n_rows]) DEVICE int32, any value; axis a's from positions + a * axis_pitch,
+ *             axis_pitch >= the number of rows
+ * Errors: as there, SHAPE also for axis_pitch.
+ */
+psrl_status_t psrl_rope_axes_qkv_fwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const int32_t* positions, int64_t axis_pitch,
+                                     const void* q, int64_t q_pitch, const void* k, int64_t k_pitch, const void* v, int64_t v_pitch,
+                                     void* q_out, void* k_pool, void* v_pool, int64_t pool_capacity, void* stream);
+psrl_status_t psrl_rope_axes_qkv_bwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const int32_t* positions, int64_t axis_pitch,
+                                     const void* d_q, const void* dk_pool, const void* dv_pool, int64_t pool_capacity, void* dq_out,
+                                     int64_t dq_pitch, void* dk_out, int64_t dk_pitch, void* dv_out, int64_t dv_pitch, void* stream);
+psrl_status_t psrl_rope_axes_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const void* x, int64_t x_pitch, const int32_t* positions,
+                                  int64_t axis_pitch, int64_t n_rows, int32_t n_heads, void* y, int64_t y_pitch, int inverse,
+                                  void* stream);
+
+/*
  * psrl_plan_next_tokens - the targets of the tree's language-model loss.  A query row predicts the next token of its own
  * segment; the last row of a segment predicts the first token of every child (none at the end of a sample).  Row r's
  * targets are tokens next[off[r] .. off[r + 1]) - indices into the tree's tokens in canonical order (look their ids up to

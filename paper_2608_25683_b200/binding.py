@@ -34,6 +34,7 @@ EXPORTS = [
     "psrl_kv_scatter", "psrl_kv_gather",
     "psrl_rope_create", "psrl_rope_frequencies", "psrl_rope_destroy", "psrl_rope_qkv_fwd", "psrl_rope_qkv_bwd",
     "psrl_rope_rows",
+    "psrl_rope_create_axes", "psrl_rope_axes_qkv_fwd", "psrl_rope_axes_qkv_bwd", "psrl_rope_axes_rows",
     "psrl_plan_next_tokens", "psrl_token_logprob_workspace_bytes", "psrl_token_logprob_fwd", "psrl_token_logprob_bwd",
     "psrl_cache_compact", "psrl_kv_copy", "psrl_kv_move",
     "psrl_cost_sequence", "psrl_group_workloads", "psrl_place_groups", "psrl_microbatch_tokens",
@@ -200,6 +201,14 @@ def lib() -> C.CDLL:
     L.psrl_rope_qkv_bwd.restype = C.c_int
     L.psrl_rope_rows.argtypes = [_VP, C.c_int, _VP, _I64, _VP, _I64, C.c_int32, _VP, _I64, C.c_int, _VP]
     L.psrl_rope_rows.restype = C.c_int
+    L.psrl_rope_create_axes.argtypes = [C.POINTER(RopeDesc), C.c_int32, _I32P, C.c_int, C.POINTER(C.c_void_p)]
+    L.psrl_rope_create_axes.restype = C.c_int
+    L.psrl_rope_axes_qkv_fwd.argtypes = [_VP, _VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _VP, _I64, _VP]
+    L.psrl_rope_axes_qkv_fwd.restype = C.c_int
+    L.psrl_rope_axes_qkv_bwd.argtypes = [_VP, _VP, _VP, _I64, _VP, _VP, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP]
+    L.psrl_rope_axes_qkv_bwd.restype = C.c_int
+    L.psrl_rope_axes_rows.argtypes = [_VP, C.c_int, _VP, _I64, _VP, _I64, _I64, C.c_int32, _VP, _I64, C.c_int, _VP]
+    L.psrl_rope_axes_rows.restype = C.c_int
     L.psrl_plan_next_tokens.argtypes = [_VP, C.POINTER(_I32P), C.POINTER(_I32P)]
     L.psrl_plan_next_tokens.restype = C.c_int
     L.psrl_token_logprob_workspace_bytes.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, _I64, C.c_int]
@@ -605,23 +614,32 @@ def _launch(name: str, dev: int, *args):
 
 
 _ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+_ROPE_ORDERS = {"blocks": 0, "cyclic": 1}
 _ROPE_SCALINGS = {None: 0, "none": 0, "linear": 1, "ntk": 2, "yarn": 3, "banded": 4}
 
 
 class Rope:
     """Owner of a psrl_rope_t: a rotary position embedding (include/psrl.h has the formulas).  `freq` holds the radians
-    per position of each pair, `scale` the factor on cos and sin.  low / high / attention_scale 0: the defaults."""
+    per position of each pair, `scale` the factor on cos and sin.  low / high / attention_scale 0: the defaults.
+    `sections` = [pairs of axis 0, of axis 1, ...]: several axes (time, height, width), with the pairs of an axis in "blocks" or
+    going round them in turn ("cyclic")."""
 
     def __init__(self, head_dim: int, rotary_dim: int = 0, base: float = 10000.0, layout: str = "half",
                  scaling: Optional[str] = None, factor: float = 1.0, original_positions: int = 0, low: float = 0.0,
-                 high: float = 0.0, attention_scale: float = 0.0):
+                 high: float = 0.0, attention_scale: float = 0.0, sections: Optional[Sequence[int]] = None, order: str = "blocks"):
         self._h = C.c_void_p()
         self._destroy = lib().psrl_rope_destroy
-        if layout not in _ROPE_LAYOUTS or scaling not in _ROPE_SCALINGS:
-            raise ValueError(f"layout {layout!r} or scaling {scaling!r} unknown")
+        if layout not in _ROPE_LAYOUTS or scaling not in _ROPE_SCALINGS or order not in _ROPE_ORDERS:
+            raise ValueError(f"layout {layout!r}, scaling {scaling!r} or order {order!r} unknown")
         d = RopeDesc(int(head_dim), int(rotary_dim or head_dim), _ROPE_LAYOUTS[layout], _ROPE_SCALINGS[scaling], float(base),
                      float(factor), int(original_positions), float(low), float(high), float(attention_scale))
-        _check(lib().psrl_rope_create(C.byref(d), C.byref(self._h)), "psrl_rope_create")
+        if sections is None:
+            _check(lib().psrl_rope_create(C.byref(d), C.byref(self._h)), "psrl_rope_create")
+        else:
+            parts = _i32(sections)
+            _check(lib().psrl_rope_create_axes(C.byref(d), len(parts), parts.ctypes.data_as(_I32P), _ROPE_ORDERS[order],
+                                               C.byref(self._h)), "psrl_rope_create_axes")
+        self.n_axes = 1 if sections is None else len(parts)
         f, n, sc = C.POINTER(C.c_double)(), C.c_int32(), C.c_double()
         _check(lib().psrl_rope_frequencies(self._h, C.byref(f), C.byref(n), C.byref(sc)), "psrl_rope_frequencies")
         self.head_dim, self.rotary_dim = d.head_dim, d.rotary_dim
@@ -658,12 +676,40 @@ def _rope_pools(plan, *pools):
 def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=None, stream=None):
     """Rotates the query rows' Q [T_q, Hq, d] into q_out and their K, V [T_q, Hkv, d] into the pools (K rotated), in one
     launch.  q, k, v may be slices of one projection output (rows at any pitch).  Returns q_out."""
+    return _rope_qkv_fwd("psrl_rope_qkv_fwd", plan, rope, None, q, k, v, k_pool, v_pool, q_out, stream)
+
+
+def psrl_rope_axes_qkv_fwd(plan: Plan, rope: Rope, positions, q, k, v, k_pool, v_pool, q_out=None, stream=None):
+    """The same with int32 `positions` [axes, T_q] of the caller's own, a row for each axis of the rope."""
+    return _rope_qkv_fwd("psrl_rope_axes_qkv_fwd", plan, rope, positions, q, k, v, k_pool, v_pool, q_out, stream)
+
+
+def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None, dk_out=None, dv_out=None, stream=None):
+    """The way back: inverse rotation of d_q and of the query rows' slots of dk_pool, and the rows' slots of dv_pool, to
+    dq_out [T_q, Hq, d], dk_out, dv_out [T_q, Hkv, d] (which may be slices of one gradient matrix).  Returns the three."""
+    return _rope_qkv_bwd("psrl_rope_qkv_bwd", plan, rope, None, d_q, dk_pool, dv_pool, dq_out, dk_out, dv_out, stream)
+
+
+def psrl_rope_axes_qkv_bwd(plan: Plan, rope: Rope, positions, d_q, dk_pool, dv_pool, dq_out=None, dk_out=None, dv_out=None, stream=None):
+    """The same with int32 `positions` [axes, T_q], as in the forward."""
+    return _rope_qkv_bwd("psrl_rope_axes_qkv_bwd", plan, rope, positions, d_q, dk_pool, dv_pool, dq_out, dk_out, dv_out, stream)
+
+
+def _axis_pitch(rope: Rope, positions, rows: int) -> int:
+    """Elements between two axes' positions."""
+    if str(positions.dtype) != "torch.int32" or positions.shape != (rope.n_axes, rows) or (rows > 1 and positions.stride(1) != 1):
+        raise ValueError(f"positions must be int32 [{rope.n_axes}, {rows}], the rows of an axis contiguous")
+    return positions.stride(0) if rope.n_axes > 1 else rows
+
+
+def _rope_qkv_fwd(name, plan, rope, positions, q, k, v, k_pool, v_pool, q_out, stream):
     V, d = plan.view, plan.head_dim
     _check_dtype(plan, q, k, v, k_pool, v_pool)
     pq = _rows_pitch(q, V["T_q"], plan.n_q_heads, d, "q")
     pk, pv = (_rows_pitch(t, V["T_q"], plan.n_kv_heads, d, n) for t, n in ((k, "k"), (v, "v")))
     cap = _rope_pools(plan, k_pool, v_pool)
-    dev = _device_of(q, k, v, k_pool, v_pool)
+    at = () if positions is None else (positions.data_ptr(), _axis_pitch(rope, positions, V["T_q"]))
+    dev = _device_of(q, k, v, k_pool, v_pool, *(() if positions is None else (positions,)))
     _plan_device(plan, dev)
     raw, keep = _stream_on(stream, dev)
     if q_out is None:
@@ -672,33 +718,32 @@ def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=Non
         _check_dtype(plan, q_out)
         if q_out.shape != q.shape or not q_out.is_contiguous() or q_out.device != q.device:
             raise ValueError("q_out must be contiguous [T_q, Hq, d] on the same device")
-    _launch("psrl_rope_qkv_fwd", dev, plan._h, rope._h, q.data_ptr(), pq, k.data_ptr(), pk, v.data_ptr(), pv,
+    _launch(name, dev, plan._h, rope._h, *at, q.data_ptr(), pq, k.data_ptr(), pk, v.data_ptr(), pv,
             q_out.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), cap, raw)
     return q_out
 
 
-def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None, dk_out=None, dv_out=None, stream=None):
-    """The way back: inverse rotation of d_q and of the query rows' slots of dk_pool, and the rows' slots of dv_pool, to
-    dq_out [T_q, Hq, d], dk_out, dv_out [T_q, Hkv, d] (which may be slices of one gradient matrix).  Returns the three."""
+def _rope_qkv_bwd(name, plan, rope, positions, d_q, dk_pool, dv_pool, dq_out, dk_out, dv_out, stream):
     V, d = plan.view, plan.head_dim
     _check_dtype(plan, d_q, dk_pool, dv_pool)
     if d_q.shape != (V["T_q"], plan.n_q_heads, d) or not d_q.is_contiguous():
         raise ValueError("d_q must be contiguous [T_q, Hq, d]")
     cap = _rope_pools(plan, dk_pool, dv_pool)
-    dev = _device_of(d_q, dk_pool, dv_pool)
+    at = () if positions is None else (positions.data_ptr(), _axis_pitch(rope, positions, V["T_q"]))
+    dev = _device_of(d_q, dk_pool, dv_pool, *(() if positions is None else (positions,)))
     _plan_device(plan, dev)
     raw, keep = _stream_on(stream, dev)
     outs, pitch = [], []
-    for t, heads, name in ((dq_out, plan.n_q_heads, "dq_out"), (dk_out, plan.n_kv_heads, "dk_out"), (dv_out, plan.n_kv_heads, "dv_out")):
+    for t, heads, which in ((dq_out, plan.n_q_heads, "dq_out"), (dk_out, plan.n_kv_heads, "dk_out"), (dv_out, plan.n_kv_heads, "dv_out")):
         if t is None:
             t = _new(keep, (V["T_q"], heads, d), d_q.dtype, d_q.device)
         else:
             _check_dtype(plan, t)
             if t.device != d_q.device:
-                raise ValueError(f"{name} lives on another device")
+                raise ValueError(f"{which} lives on another device")
         outs.append(t)
-        pitch.append(_rows_pitch(t, V["T_q"], heads, d, name))
-    _launch("psrl_rope_qkv_bwd", dev, plan._h, rope._h, d_q.data_ptr(), dk_pool.data_ptr(), dv_pool.data_ptr(), cap,
+        pitch.append(_rows_pitch(t, V["T_q"], heads, d, which))
+    _launch(name, dev, plan._h, rope._h, *at, d_q.data_ptr(), dk_pool.data_ptr(), dv_pool.data_ptr(), cap,
             outs[0].data_ptr(), pitch[0], outs[1].data_ptr(), pitch[1], outs[2].data_ptr(),
             pitch[2], raw)
     return tuple(outs)
@@ -706,6 +751,17 @@ def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None
 
 def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stream=None):
     """Rotates x [rows, heads, head_dim] (f32 or bf16, rows at any pitch) at int32 `positions` [rows].  Returns y (y may be x)."""
+    if str(positions.dtype) != "torch.int32" or positions.shape != x.shape[:1] or not positions.is_contiguous():
+        raise ValueError("positions must be contiguous int32 [rows]")
+    return _rope_rows("psrl_rope_rows", rope, x, positions, (), y, inverse, stream)
+
+
+def psrl_rope_axes_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stream=None):
+    """The same at `positions` [axes, rows], a row for each axis of the rope."""
+    return _rope_rows("psrl_rope_axes_rows", rope, x, positions, (_axis_pitch(rope, positions, x.shape[0]),), y, inverse, stream)
+
+
+def _rope_rows(name, rope, x, positions, axis_pitch, y, inverse, stream):
     dt = _type_code(x)
     if dt is None:
         raise TypeError(f"dtype {x.dtype} is neither float32 nor bfloat16")
@@ -713,8 +769,6 @@ def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stre
     if len(shape) != 3:
         raise ValueError("x must be [rows, heads, head_dim]")
     rows, heads, _ = shape
-    if str(positions.dtype) != "torch.int32" or positions.shape != shape[:1] or not positions.is_contiguous():
-        raise ValueError("positions must be contiguous int32 [rows]")
     px = _rows_pitch(x, rows, heads, rope.head_dim, "x")
     dev = _device_of(x, positions)
     raw, keep = _stream_on(stream, dev)
@@ -722,7 +776,7 @@ def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stre
         y = _new(keep, shape, x.dtype, x.device)
     elif y.dtype is not x.dtype or y.get_device() != dev:
         raise ValueError("y must have x's type and device")
-    _launch("psrl_rope_rows", dev, rope._h, dt, x.data_ptr(), px, positions.data_ptr(), rows, heads, y.data_ptr(),
+    _launch(name, dev, rope._h, dt, x.data_ptr(), px, positions.data_ptr(), *axis_pitch, rows, heads, y.data_ptr(),
             px if y is x else _rows_pitch(y, rows, heads, rope.head_dim, "y"), 1 if inverse else 0, raw)
     return y
 

@@ -4,6 +4,10 @@
 // kept as a 64-bit fixed-point fraction of a turn: pos * f_i wraps around exactly in integer arithmetic, and an angle
 // at position 10^6 is as good as one at position 1 (a product in fp32 would be off by 0.06 radians there).
 //
+// With several axes (time, height, width of images and video) pair i is turned by pos[axis(i)] * f_i.  The axis travels in the
+// two lowest bits of the fraction: at position 2^31 they are worth less than 2^-31 of a turn, and the angle is rounded to
+// 2^-25 of one all the same.
+//
 // Memory bound: every element is read once and written once.  A warp takes a row: the row's cos / sin serve all its
 // Hq + Hkv heads, which stream by in 16-byte vectors.  A lane handles the two vectors that rotate into each other, so each
 // element is loaded and stored by the same thread and the rotation may run in place.
@@ -24,12 +28,15 @@ struct psrl_rope {
   std::vector<double> freq;      // radians per position
   std::vector<uint64_t> turns;   // the same as a fraction of a turn, in units of 2^-64
   double scale = 1.0;
+  int32_t n_axes = 1;            // more than one: the axis of a pair is in the lowest bits of its fraction of a turn
 };
 
 namespace psrl {
 namespace {
 
 constexpr int kMaxPairs = 128;
+constexpr int kMaxAxes = 4;
+constexpr uint64_t kAxisBits = kMaxAxes - 1;
 
 struct Frequencies {
   uint64_t turns[kMaxPairs];
@@ -46,9 +53,11 @@ struct Part {
 
 struct RopeParams {
   Part part[3];
-  const int32_t* pos;
+  const int32_t* pos;   // [axes], axis_pitch apart
   const int32_t* slot;
   int64_t rows;
+  int64_t axis_pitch;
+  int32_t axes;
   int32_t heads;        // sum over the parts
   int32_t shares;       // warps of a row
   int32_t pairs;        // rotary_dim / 2
@@ -134,7 +143,7 @@ __device__ __forceinline__ void rotate_vectors(uint4& xv, uint4& yv, const float
 // four warps: 8,758 rows of 48 heads 43.1 us, of eight warps 45.0.
 constexpr int kWarps = 4, kBatch = 2;
 
-template <bool kBf16, bool kInterleaved>
+template <bool kBf16, bool kInterleaved, bool kAxes>
 __global__ void __launch_bounds__(kWarps * 32, 32 / kWarps) rope_kernel(const __grid_constant__ RopeParams p,
                                                               const __grid_constant__ Frequencies f) {
   constexpr int kElems = kBf16 ? 8 : 4, kBytes = kBf16 ? 2 : 4;
@@ -145,8 +154,17 @@ __global__ void __launch_bounds__(kWarps * 32, 32 / kWarps) rope_kernel(const __
   const int64_t row = p.shares == 1 ? task : task / p.shares;
   const int share = int(task - row * p.shares);
   const int64_t slot = p.slot ? int64_t(p.slot[row]) : 0;
-  const int32_t pos = p.pos[row];
-  for (int x = lane; x < p.pairs; x += 32) cs[warp][x] = turn_at(p, f, pos, x);
+  if constexpr (kAxes) {   // a lane for each axis loads the row's position, the pairs get theirs from it
+    const int32_t mine = lane < p.axes ? p.pos[lane * p.axis_pitch + row] : 0;
+    for (int x0 = 0; x0 < p.pairs; x0 += 32) {
+      const int x = min(x0 + lane, p.pairs - 1);
+      const int32_t pos = __shfl_sync(0xffffffffu, mine, int(f.turns[x] & kAxisBits));
+      cs[warp][x] = turn_at(p, f, pos, x);   // lanes behind the last pair write what its own lane writes
+    }
+  } else {
+    const int32_t pos = p.pos[row];
+    for (int x = lane; x < p.pairs; x += 32) cs[warp][x] = turn_at(p, f, pos, x);
+  }
   __syncwarp();
   const int u = lane % p.units, at = lane / p.units, step = 32 / p.units;
   if (at >= step) return;
@@ -194,12 +212,13 @@ __global__ void __launch_bounds__(kWarps * 32, 32 / kWarps) rope_kernel(const __
 
 // The same element by element, where rotary_dim does not divide into pairs of 16-byte vectors: one thread per pair of
 // elements, a block per few rows.  Uncommon sizes; bound by instructions, not by HBM.
-template <class T>
+template <class T, bool kAxes>
 __global__ void __launch_bounds__(256) rope_scalar_kernel(const __grid_constant__ RopeParams p, const __grid_constant__ Frequencies f) {
   __shared__ float2 cs[kMaxPairs];
   const int64_t row = blockIdx.x;
   const int64_t slot = p.slot ? int64_t(p.slot[row]) : 0;
-  for (int x = threadIdx.x; x < p.pairs; x += 256) cs[x] = turn_at(p, f, p.pos[row], x);
+  for (int x = threadIdx.x; x < p.pairs; x += 256)
+    cs[x] = turn_at(p, f, kAxes ? p.pos[int64_t(f.turns[x] & kAxisBits) * p.axis_pitch + row] : p.pos[row], x);
   __syncthreads();
   for (int w = threadIdx.x; w < p.heads * p.units; w += 256) {
     const int u = w % p.units;
@@ -242,13 +261,18 @@ psrl_status_t launch(const psrl_rope& rope, RopeParams& p, psrl_dtype_t dtype, b
   if (grid > INT32_MAX) return PSRL_ERR_SHAPE;
   Frequencies f{};
   for (size_t i = 0; i < rope.turns.size(); ++i) f.turns[i] = rope.turns[i];
+  const bool bf16 = dtype == PSRL_BF16;
   if (wide) {
-    auto kernel = dtype == PSRL_BF16 ? (p.interleaved ? rope_kernel<true, true> : rope_kernel<true, false>)
-                                     : (p.interleaved ? rope_kernel<false, true> : rope_kernel<false, false>);
+    auto kernel = bf16 ? (p.interleaved ? rope_kernel<true, true, false> : rope_kernel<true, false, false>)
+                       : (p.interleaved ? rope_kernel<false, true, false> : rope_kernel<false, false, false>);
+    if (p.axes > 1)
+      kernel = bf16 ? (p.interleaved ? rope_kernel<true, true, true> : rope_kernel<true, false, true>)
+                    : (p.interleaved ? rope_kernel<false, true, true> : rope_kernel<false, false, true>);
     kernel<<<unsigned(grid), kWarps * 32, 0, stream>>>(p, f);
   } else {
-    if (dtype == PSRL_BF16) rope_scalar_kernel<__nv_bfloat16><<<unsigned(grid), 256, 0, stream>>>(p, f);
-    else rope_scalar_kernel<float><<<unsigned(grid), 256, 0, stream>>>(p, f);
+    auto kernel = bf16 ? rope_scalar_kernel<__nv_bfloat16, false> : rope_scalar_kernel<float, false>;
+    if (p.axes > 1) kernel = bf16 ? rope_scalar_kernel<__nv_bfloat16, true> : rope_scalar_kernel<float, true>;
+    kernel<<<unsigned(grid), 256, 0, stream>>>(p, f);
   }
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) { set_last_cuda_error(e); return PSRL_ERR_CUDA; }
@@ -267,6 +291,28 @@ bool pitch_ok(int64_t pitch, int64_t heads, int d, psrl_dtype_t t) {
 // In place, but with rows at other distances: a row would be written over one that has yet to be read.
 bool two_pitches(const void* x, int64_t x_pitch, const void* y, int64_t y_pitch, int64_t rows) {
   return x && x == y && x_pitch != y_pitch && rows > 1;
+}
+
+// The axis of every pair; false if the sections do not make up the pairs.
+bool axes_of(int pairs, int n_axes, const int32_t* sections, psrl_rope_order_t order, std::vector<int>& axis) {
+  int64_t sum = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    if (sections[a] < 0) return false;
+    sum += sections[a];
+  }
+  if (sum != pairs) return false;
+  std::vector<int> left(sections, sections + n_axes);
+  for (int i = 0, a = 0; i < pairs; ++i) {
+    if (order == PSRL_ROPE_CYCLIC) {
+      a = i % n_axes;
+      if (i >= int64_t(n_axes) * sections[a]) a = 0;
+    } else {
+      while (left[a] == 0) ++a;
+    }
+    if (--left[a] < 0) return false;
+    axis.push_back(a);
+  }
+  return true;
 }
 
 // The pairs' frequencies; false if the description's scaling arguments make no sense.
@@ -309,14 +355,111 @@ bool frequencies(const psrl_rope_desc_t& d, std::vector<double>& freq, double& s
   return true;
 }
 
+// Positions of the caller's own, one row for each axis.
+struct Positions {
+  const int32_t* pos;
+  int64_t pitch;
+};
+
+// Without positions of its own (the plan's, or one for each row) a rope of several axes reads the same one for all of them.
+void set_axes(RopeParams& p, const psrl_rope& rope, const Positions* at) {
+  p.axes = rope.n_axes;
+  p.axis_pitch = at ? at->pitch : 0;
+}
+
+psrl_status_t qkv_fwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const Positions* at, const void* q, int64_t q_pitch, const void* k,
+                      int64_t k_pitch, const void* v, int64_t v_pitch, void* q_out, void* k_pool, void* v_pool, int64_t pool_capacity,
+                      void* stream) {
+  if (!plan || !plan->p || !rope) return PSRL_ERR_INVALID_ARG;
+  const Plan& P = *plan->p;
+  if ((q && !q_out) || (k && !k_pool) || (v && !v_pool) || !ok16(q) || !ok16(k) || !ok16(v) || !ok16(q_out) ||
+      !ok16(k_pool) || !ok16(v_pool))
+    return PSRL_ERR_INVALID_ARG;
+  if (rope->desc.head_dim != P.d || (q && !pitch_ok(q_pitch, P.Hq, P.d, P.dtype)) ||
+      (k && !pitch_ok(k_pitch, P.Hkv, P.d, P.dtype)) || (v && !pitch_ok(v_pitch, P.Hkv, P.d, P.dtype)) ||
+      ((k || v) && pool_capacity < P.pool_slots))
+    return PSRL_ERR_SHAPE;
+  if (two_pitches(q, q_pitch, q_out, int64_t(P.Hq) * P.d, P.T_q)) return PSRL_ERR_INVALID_ARG;
+  if (at && P.T_q > 0) {
+    if (at->pitch < P.T_q) return PSRL_ERR_SHAPE;
+    if (!ptr_aligned(at->pos, 4)) return PSRL_ERR_INVALID_ARG;
+  }
+  if (!P.dev) return PSRL_ERR_WORKSPACE;
+  RopeParams p{};
+  const int64_t d = P.d;
+  p.part[0] = {q, q_out, q_pitch, d, P.Hq * d, d, 0, 0, P.Hq, 1};
+  p.part[1] = {k, k_pool, k_pitch, d, d, pool_capacity * d, 0, 1, P.Hkv, 1};
+  p.part[2] = {v, v_pool, v_pitch, d, d, pool_capacity * d, 0, 1, P.Hkv, 0};
+  p.pos = at ? at->pos : P.dev + P.hdr.off_qrow_pos;
+  p.slot = P.dev + P.hdr.off_qrow_slot;
+  p.rows = P.T_q;
+  set_axes(p, *rope, at);
+  return launch(*rope, p, P.dtype, false, static_cast<cudaStream_t>(stream));
+}
+
+psrl_status_t qkv_bwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const Positions* at, const void* d_q, const void* dk_pool,
+                      const void* dv_pool, int64_t pool_capacity, void* dq_out, int64_t dq_pitch, void* dk_out, int64_t dk_pitch,
+                      void* dv_out, int64_t dv_pitch, void* stream) {
+  if (!plan || !plan->p || !rope) return PSRL_ERR_INVALID_ARG;
+  const Plan& P = *plan->p;
+  if ((d_q && !dq_out) || (dk_pool && !dk_out) || (dv_pool && !dv_out) || !ok16(d_q) || !ok16(dk_pool) ||
+      !ok16(dv_pool) || !ok16(dq_out) || !ok16(dk_out) || !ok16(dv_out))
+    return PSRL_ERR_INVALID_ARG;
+  if (rope->desc.head_dim != P.d || (d_q && !pitch_ok(dq_pitch, P.Hq, P.d, P.dtype)) ||
+      (dk_pool && !pitch_ok(dk_pitch, P.Hkv, P.d, P.dtype)) || (dv_pool && !pitch_ok(dv_pitch, P.Hkv, P.d, P.dtype)) ||
+      ((dk_pool || dv_pool) && pool_capacity < P.pool_slots))
+    return PSRL_ERR_SHAPE;
+  if (two_pitches(d_q, int64_t(P.Hq) * P.d, dq_out, dq_pitch, P.T_q)) return PSRL_ERR_INVALID_ARG;
+  if (at && P.T_q > 0) {
+    if (at->pitch < P.T_q) return PSRL_ERR_SHAPE;
+    if (!ptr_aligned(at->pos, 4)) return PSRL_ERR_INVALID_ARG;
+  }
+  if (!P.dev) return PSRL_ERR_WORKSPACE;
+  RopeParams p{};
+  const int64_t d = P.d;
+  p.part[0] = {d_q, dq_out, P.Hq * d, d, dq_pitch, d, 0, 0, P.Hq, 1};
+  p.part[1] = {dk_pool, dk_out, d, pool_capacity * d, dk_pitch, d, 1, 0, P.Hkv, 1};
+  p.part[2] = {dv_pool, dv_out, d, pool_capacity * d, dv_pitch, d, 1, 0, P.Hkv, 0};
+  p.pos = at ? at->pos : P.dev + P.hdr.off_qrow_pos;
+  p.slot = P.dev + P.hdr.off_qrow_slot;
+  p.rows = P.T_q;
+  set_axes(p, *rope, at);
+  return launch(*rope, p, P.dtype, true, static_cast<cudaStream_t>(stream));
+}
+
+// pitch 0: the same position on every axis
+psrl_status_t rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const void* x, int64_t x_pitch, Positions at, int64_t n_rows,
+                   int32_t n_heads, void* y, int64_t y_pitch, int inverse, void* stream) {
+  if (!rope || n_rows < 0 || n_heads < 1 || n_heads > 65535) return PSRL_ERR_INVALID_ARG;
+  if (dtype != PSRL_F32 && dtype != PSRL_BF16) return PSRL_ERR_UNSUPPORTED;
+  const int64_t d = rope->desc.head_dim;
+  if (!pitch_ok(x_pitch, n_heads, int(d), dtype) || !pitch_ok(y_pitch, n_heads, int(d), dtype)) return PSRL_ERR_SHAPE;
+  if (n_rows == 0) return PSRL_OK;
+  if (!ptr_aligned(x, 16) || !ptr_aligned(y, 16) || !ptr_aligned(at.pos, 4) || two_pitches(x, x_pitch, y, y_pitch, n_rows))
+    return PSRL_ERR_INVALID_ARG;
+  RopeParams p{};
+  p.part[0] = {x, y, x_pitch, d, y_pitch, d, 0, 0, n_heads, 1};
+  p.pos = at.pos;
+  p.rows = n_rows;
+  set_axes(p, *rope, at.pitch ? &at : nullptr);
+  return launch(*rope, p, dtype, inverse != 0, static_cast<cudaStream_t>(stream));
+}
+
 }  // namespace
 }  // namespace psrl
 
 extern "C" {
 
 psrl_status_t psrl_rope_create(const psrl_rope_desc_t* desc, psrl_rope_t** out) {
+  const int32_t all = desc ? desc->rotary_dim / 2 : 0;
+  return psrl_rope_create_axes(desc, 1, &all, PSRL_ROPE_BLOCKS, out);
+}
+
+psrl_status_t psrl_rope_create_axes(const psrl_rope_desc_t* desc, int32_t n_axes, const int32_t* sections, psrl_rope_order_t order,
+                                    psrl_rope_t** out) {
   if (out) *out = nullptr;
-  if (!desc || !out) return PSRL_ERR_INVALID_ARG;
+  if (!desc || !out || !sections || n_axes < 1 || n_axes > psrl::kMaxAxes || order < PSRL_ROPE_BLOCKS || order > PSRL_ROPE_CYCLIC)
+    return PSRL_ERR_INVALID_ARG;
   if (desc->head_dim < 8 || desc->head_dim > 2 * psrl::kMaxPairs || desc->head_dim % 8 || desc->rotary_dim < 2 ||
       desc->rotary_dim > desc->head_dim || desc->rotary_dim % 2)
     return PSRL_ERR_SHAPE;
@@ -331,11 +474,19 @@ psrl_status_t psrl_rope_create(const psrl_rope_desc_t* desc, psrl_rope_t** out) 
       delete r;
       return PSRL_ERR_INVALID_ARG;
     }
+    std::vector<int> axis;
+    if (!psrl::axes_of(desc->rotary_dim / 2, n_axes, sections, order, axis)) {
+      delete r;
+      return PSRL_ERR_SHAPE;
+    }
+    r->n_axes = n_axes;
     for (double f : r->freq) {
       const long double turn = static_cast<long double>(f) / 6.283185307179586476925286766559L;
       const long double frac = turn - std::floor(turn);
       r->turns.push_back(static_cast<uint64_t>(frac * 18446744073709551616.0L));
     }
+    if (n_axes > 1)
+      for (size_t i = 0; i < axis.size(); ++i) r->turns[i] = (r->turns[i] & ~psrl::kAxisBits) | uint64_t(axis[i]);
   } catch (const std::bad_alloc&) {
     delete r;
     return PSRL_ERR_HOST_OOM;
@@ -357,71 +508,41 @@ void psrl_rope_destroy(psrl_rope_t* rope) { delete rope; }
 psrl_status_t psrl_rope_qkv_fwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const void* q, int64_t q_pitch,
                                 const void* k, int64_t k_pitch, const void* v, int64_t v_pitch, void* q_out,
                                 void* k_pool, void* v_pool, int64_t pool_capacity, void* stream) {
-  using namespace psrl;
-  if (!plan || !plan->p || !rope) return PSRL_ERR_INVALID_ARG;
-  const Plan& P = *plan->p;
-  if ((q && !q_out) || (k && !k_pool) || (v && !v_pool) || !ok16(q) || !ok16(k) || !ok16(v) || !ok16(q_out) ||
-      !ok16(k_pool) || !ok16(v_pool))
-    return PSRL_ERR_INVALID_ARG;
-  if (rope->desc.head_dim != P.d || (q && !pitch_ok(q_pitch, P.Hq, P.d, P.dtype)) ||
-      (k && !pitch_ok(k_pitch, P.Hkv, P.d, P.dtype)) || (v && !pitch_ok(v_pitch, P.Hkv, P.d, P.dtype)) ||
-      ((k || v) && pool_capacity < P.pool_slots))
-    return PSRL_ERR_SHAPE;
-  if (two_pitches(q, q_pitch, q_out, int64_t(P.Hq) * P.d, P.T_q)) return PSRL_ERR_INVALID_ARG;
-  if (!P.dev) return PSRL_ERR_WORKSPACE;
-  RopeParams p{};
-  const int64_t d = P.d;
-  p.part[0] = {q, q_out, q_pitch, d, P.Hq * d, d, 0, 0, P.Hq, 1};
-  p.part[1] = {k, k_pool, k_pitch, d, d, pool_capacity * d, 0, 1, P.Hkv, 1};
-  p.part[2] = {v, v_pool, v_pitch, d, d, pool_capacity * d, 0, 1, P.Hkv, 0};
-  p.pos = P.dev + P.hdr.off_qrow_pos;
-  p.slot = P.dev + P.hdr.off_qrow_slot;
-  p.rows = P.T_q;
-  return launch(*rope, p, P.dtype, false, static_cast<cudaStream_t>(stream));
+  return psrl::qkv_fwd(plan, rope, nullptr, q, q_pitch, k, k_pitch, v, v_pitch, q_out, k_pool, v_pool, pool_capacity, stream);
 }
 
 psrl_status_t psrl_rope_qkv_bwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const void* d_q, const void* dk_pool,
                                 const void* dv_pool, int64_t pool_capacity, void* dq_out, int64_t dq_pitch,
                                 void* dk_out, int64_t dk_pitch, void* dv_out, int64_t dv_pitch, void* stream) {
-  using namespace psrl;
-  if (!plan || !plan->p || !rope) return PSRL_ERR_INVALID_ARG;
-  const Plan& P = *plan->p;
-  if ((d_q && !dq_out) || (dk_pool && !dk_out) || (dv_pool && !dv_out) || !ok16(d_q) || !ok16(dk_pool) ||
-      !ok16(dv_pool) || !ok16(dq_out) || !ok16(dk_out) || !ok16(dv_out))
-    return PSRL_ERR_INVALID_ARG;
-  if (rope->desc.head_dim != P.d || (d_q && !pitch_ok(dq_pitch, P.Hq, P.d, P.dtype)) ||
-      (dk_pool && !pitch_ok(dk_pitch, P.Hkv, P.d, P.dtype)) || (dv_pool && !pitch_ok(dv_pitch, P.Hkv, P.d, P.dtype)) ||
-      ((dk_pool || dv_pool) && pool_capacity < P.pool_slots))
-    return PSRL_ERR_SHAPE;
-  if (two_pitches(d_q, int64_t(P.Hq) * P.d, dq_out, dq_pitch, P.T_q)) return PSRL_ERR_INVALID_ARG;
-  if (!P.dev) return PSRL_ERR_WORKSPACE;
-  RopeParams p{};
-  const int64_t d = P.d;
-  p.part[0] = {d_q, dq_out, P.Hq * d, d, dq_pitch, d, 0, 0, P.Hq, 1};
-  p.part[1] = {dk_pool, dk_out, d, pool_capacity * d, dk_pitch, d, 1, 0, P.Hkv, 1};
-  p.part[2] = {dv_pool, dv_out, d, pool_capacity * d, dv_pitch, d, 1, 0, P.Hkv, 0};
-  p.pos = P.dev + P.hdr.off_qrow_pos;
-  p.slot = P.dev + P.hdr.off_qrow_slot;
-  p.rows = P.T_q;
-  return launch(*rope, p, P.dtype, true, static_cast<cudaStream_t>(stream));
+  return psrl::qkv_bwd(plan, rope, nullptr, d_q, dk_pool, dv_pool, pool_capacity, dq_out, dq_pitch, dk_out, dk_pitch, dv_out, dv_pitch,
+                       stream);
+}
+
+psrl_status_t psrl_rope_axes_qkv_fwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const int32_t* positions, int64_t axis_pitch,
+                                     const void* q, int64_t q_pitch, const void* k, int64_t k_pitch, const void* v, int64_t v_pitch,
+                                     void* q_out, void* k_pool, void* v_pool, int64_t pool_capacity, void* stream) {
+  const psrl::Positions at{positions, axis_pitch};
+  return psrl::qkv_fwd(plan, rope, &at, q, q_pitch, k, k_pitch, v, v_pitch, q_out, k_pool, v_pool, pool_capacity, stream);
+}
+
+psrl_status_t psrl_rope_axes_qkv_bwd(const psrl_plan_t* plan, const psrl_rope_t* rope, const int32_t* positions, int64_t axis_pitch,
+                                     const void* d_q, const void* dk_pool, const void* dv_pool, int64_t pool_capacity, void* dq_out,
+                                     int64_t dq_pitch, void* dk_out, int64_t dk_pitch, void* dv_out, int64_t dv_pitch, void* stream) {
+  const psrl::Positions at{positions, axis_pitch};
+  return psrl::qkv_bwd(plan, rope, &at, d_q, dk_pool, dv_pool, pool_capacity, dq_out, dq_pitch, dk_out, dk_pitch, dv_out, dv_pitch, stream);
 }
 
 psrl_status_t psrl_rope_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const void* x, int64_t x_pitch,
                              const int32_t* positions, int64_t n_rows, int32_t n_heads, void* y, int64_t y_pitch,
                              int inverse, void* stream) {
-  using namespace psrl;
-  if (!rope || n_rows < 0 || n_heads < 1 || n_heads > 65535) return PSRL_ERR_INVALID_ARG;
-  if (dtype != PSRL_F32 && dtype != PSRL_BF16) return PSRL_ERR_UNSUPPORTED;
-  const int64_t d = rope->desc.head_dim;
-  if (!pitch_ok(x_pitch, n_heads, int(d), dtype) || !pitch_ok(y_pitch, n_heads, int(d), dtype)) return PSRL_ERR_SHAPE;
-  if (n_rows == 0) return PSRL_OK;
-  if (!ptr_aligned(x, 16) || !ptr_aligned(y, 16) || !ptr_aligned(positions, 4) || two_pitches(x, x_pitch, y, y_pitch, n_rows))
-    return PSRL_ERR_INVALID_ARG;
-  RopeParams p{};
-  p.part[0] = {x, y, x_pitch, d, y_pitch, d, 0, 0, n_heads, 1};
-  p.pos = positions;
-  p.rows = n_rows;
-  return launch(*rope, p, dtype, inverse != 0, static_cast<cudaStream_t>(stream));
+  return psrl::rows(rope, dtype, x, x_pitch, {positions, 0}, n_rows, n_heads, y, y_pitch, inverse, stream);
+}
+
+psrl_status_t psrl_rope_axes_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, const void* x, int64_t x_pitch, const int32_t* positions,
+                                  int64_t axis_pitch, int64_t n_rows, int32_t n_heads, void* y, int64_t y_pitch, int inverse,
+                                  void* stream) {
+  if (n_rows > 0 && axis_pitch < n_rows) return PSRL_ERR_SHAPE;
+  return psrl::rows(rope, dtype, x, x_pitch, {positions, axis_pitch}, n_rows, n_heads, y, y_pitch, inverse, stream);
 }
 
 }  // extern "C"
