@@ -386,6 +386,42 @@ psrl_status_t psrl_rope_axes_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, c
                                   void* stream);
 
 /*
+ * psrl_rms_norm_fwd / _bwd - the norm between a layer's parts, with the residual stream's addition.
+ *   h = x + residual (rounded to dtype as it is stored in `summed`; h = x without a residual)
+ *   y = h * r * weight,   r = (mean(h^2) + eps)^(-1/2)
+ *   codes = y / scale in 8 bits (e4m3, to the nearest, ties to even),  scale = max(amax |y| / 448, 2^-126) of the row
+ * over the last `dim` elements: of a row, or with n_heads > 1 of each head of a row (norms of q and k: a row's heads are contiguous,
+ * rows may be slices of a projection's).  Squares and sums in fp32; a row whose squares pass fp32's range is scaled first.  A row that
+ * holds NaN or an infinity has NaN there (NaN in all its codes and its scale); other rows are not touched.
+ * Backward, h as stored: g = d_y * weight,
+ *   d_x = d_summed + r * (g - h r^2 mean(g h))   (the gradient of x and of residual alike)
+ *   d_weight = sum over rows (and heads) of d_y h r, in fp32, in a fixed order: bitwise reproducible
+ *   x, residual, summed, y, d_y, d_summed, d_x  [n_rows, n_heads, dim] DEVICE of `dtype`, rows at a pitch in elements; residual,
+ *            d_summed NULL: none; summed (read only with a residual), y, codes, d_x NULL: not wanted
+ *   weight, d_weight [dim] DEVICE of `dtype`; weight NULL: ones (d_weight must be NULL then); d_weight NULL: not wanted
+ *   codes    [n_rows, n_heads, dim] DEVICE e4m3, codes_pitch a multiple of 16;  scales [n_rows * n_heads] DEVICE fp32, with codes
+ *   workspace  DEVICE, 256-byte aligned, >= 256 bytes, with d_weight >= psrl_rms_norm_workspace_bytes; holds the device status word
+ * An output may be one of the call's inputs (equal pitches); otherwise tensors are apart.  dim a multiple of 8, 8..32768;
+ * pointers 16-byte aligned (scales 4), pitches a multiple of 16 bytes and at least a row; eps > 0.
+ * n_rows = 0 does nothing (backward: zeroes d_weight).
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), WORKSPACE, CUDA.  Asynchronous.
+ *
+ * psrl_quantize_rows - the 8-bit output alone, of rows as they are (a weight matrix, laid out once): codes = e4m3(x / scale),
+ * scale = max(amax |x| / 448, 2^-126).
+ */
+psrl_status_t psrl_rms_norm_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim, const void* x, int64_t x_pitch,
+                                const void* residual, int64_t residual_pitch, const void* weight, float eps, void* summed,
+                                int64_t summed_pitch, void* y, int64_t y_pitch, void* codes, int64_t codes_pitch, float* scales,
+                                void* stream);
+size_t psrl_rms_norm_workspace_bytes(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim);
+psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim, const void* summed, int64_t summed_pitch,
+                                const void* weight, float eps, const void* d_y, int64_t d_y_pitch, const void* d_summed,
+                                int64_t d_summed_pitch, void* d_x, int64_t d_x_pitch, void* d_weight, void* workspace,
+                                size_t workspace_bytes, void* stream);
+psrl_status_t psrl_quantize_rows(psrl_dtype_t dtype, int64_t n_rows, int32_t dim, const void* x, int64_t x_pitch, void* codes,
+                                 int64_t codes_pitch, float* scales, void* stream);
+
+/*
  * psrl_plan_next_tokens - the targets of the tree's language-model loss.  A query row predicts the next token of its own
  * segment; the last row of a segment predicts the first token of every child (none at the end of a sample).  Row r's
  * targets are tokens next[off[r] .. off[r + 1]) - indices into the tree's tokens in canonical order (look their ids up to

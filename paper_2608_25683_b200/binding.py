@@ -35,6 +35,7 @@ EXPORTS = [
     "psrl_rope_create", "psrl_rope_frequencies", "psrl_rope_destroy", "psrl_rope_qkv_fwd", "psrl_rope_qkv_bwd",
     "psrl_rope_rows",
     "psrl_rope_create_axes", "psrl_rope_axes_qkv_fwd", "psrl_rope_axes_qkv_bwd", "psrl_rope_axes_rows",
+    "psrl_rms_norm_fwd", "psrl_rms_norm_bwd", "psrl_rms_norm_workspace_bytes", "psrl_quantize_rows",
     "psrl_plan_next_tokens", "psrl_token_logprob_workspace_bytes", "psrl_token_logprob_fwd", "psrl_token_logprob_bwd",
     "psrl_cache_compact", "psrl_kv_copy", "psrl_kv_move",
     "psrl_cost_sequence", "psrl_group_workloads", "psrl_place_groups", "psrl_microbatch_tokens",
@@ -209,6 +210,16 @@ def lib() -> C.CDLL:
     L.psrl_rope_axes_qkv_bwd.restype = C.c_int
     L.psrl_rope_axes_rows.argtypes = [_VP, C.c_int, _VP, _I64, _VP, _I64, _I64, C.c_int32, _VP, _I64, C.c_int, _VP]
     L.psrl_rope_axes_rows.restype = C.c_int
+    L.psrl_rms_norm_fwd.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, _VP, _I64, _VP, _I64, _VP, C.c_float, _VP, _I64, _VP, _I64, _VP,
+                                    _I64, _VP, _VP]
+    L.psrl_rms_norm_fwd.restype = C.c_int
+    L.psrl_rms_norm_workspace_bytes.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32]
+    L.psrl_rms_norm_workspace_bytes.restype = C.c_size_t
+    L.psrl_rms_norm_bwd.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, _VP, _I64, _VP, C.c_float, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _VP,
+                                    C.c_size_t, _VP]
+    L.psrl_rms_norm_bwd.restype = C.c_int
+    L.psrl_quantize_rows.argtypes = [C.c_int, _I64, C.c_int32, _VP, _I64, _VP, _I64, _VP, _VP]
+    L.psrl_quantize_rows.restype = C.c_int
     L.psrl_plan_next_tokens.argtypes = [_VP, C.POINTER(_I32P), C.POINTER(_I32P)]
     L.psrl_plan_next_tokens.restype = C.c_int
     L.psrl_token_logprob_workspace_bytes.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, _I64, C.c_int]
@@ -929,6 +940,159 @@ def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, tar
             None if target_off is None else target_off.data_ptr(), float(scale), logprob.data_ptr(),
             lse.data_ptr(), d_logprob.data_ptr(), *args, ws, wsb, raw)
     return tuple(out)
+
+
+def _stream_rows(t, shape, name: str, like=None) -> int:
+    """Row pitch of a [rows, dim] or [rows, heads, dim] tensor of `shape`, of the type and on the device of `like`."""
+    if t.shape != shape or (like is not None and (t.dtype is not like.dtype or t.get_device() != like.get_device())):
+        raise ValueError(f"{name} must be {tuple(shape)}" + (f" of {like.dtype} on {like.device}" if like is not None else ""))
+    if len(shape) == 2:
+        return _matrix_pitch(t, name)
+    return _rows_pitch(t, shape[0], shape[1], shape[2], name)
+
+
+def _norm_args(x, weight):
+    """(type, rows, heads, dim) of the rows to be normed; weight fits them."""
+    dt, shape = _type_code(x), x.shape
+    if dt is None:
+        raise TypeError(f"dtype {x.dtype} is neither float32 nor bfloat16")
+    if len(shape) not in (2, 3):
+        raise ValueError("rows must be [rows, dim] or [rows, heads, dim]")
+    if weight is not None:
+        if weight.dtype is not x.dtype:
+            raise TypeError(f"weight is {weight.dtype}, the rows are {x.dtype}")
+        if weight.shape != shape[-1:] or not weight.is_contiguous():
+            raise ValueError(f"weight must be a contiguous vector of {shape[-1]}")
+    return dt, shape[0], shape[1] if len(shape) == 3 else 1, shape[-1]
+
+
+_e4m3 = None
+
+
+def _codes_type():
+    global _e4m3
+    if _e4m3 is None:
+        import torch
+
+        _e4m3 = torch.float8_e4m3fn
+    return _e4m3
+
+
+def _codes_rows(codes, shape, keep, device, name="codes"):
+    """(tensor of 8-bit codes of `shape`, row pitch), made if not given: rows 16 bytes or a multiple apart."""
+    rows, least = shape[0], shape[1] if len(shape) == 2 else shape[1] * shape[2]
+    pitch = -(-least // 16) * 16
+    if codes is None:
+        codes = _new(keep, (rows, pitch) if pitch != least else shape, _codes_type(), device)
+        return (codes if pitch == least else codes[:, :least].unflatten(1, shape[1:]) if len(shape) == 3 else codes[:, :least]), pitch
+    if codes.dtype is not _codes_type() or codes.get_device() != device.index:
+        raise ValueError(f"{name} must be float8_e4m3fn on {device}")
+    at = _stream_rows(codes, shape, name)
+    return codes, at if rows > 1 else pitch
+
+
+def _floats(t, shape, keep, device, name):
+    """A contiguous float32 tensor of `shape`, made if not given."""
+    import torch
+
+    if t is None:
+        return _new(keep, shape, torch.float32, device)
+    if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() or t.get_device() != device.index:
+        raise ValueError(f"{name} must be contiguous float32 {tuple(shape)} on {device}")
+    return t
+
+
+def psrl_rms_norm_fwd(x, weight, eps: float = 1e-6, residual=None, y=None, summed=None, codes=None, scales=None, want_y: bool = True,
+                      want_codes: bool = False, stream=None):
+    """Root-mean-square norm of h = x + residual: x [rows, dim], or [rows, heads, dim] with a norm for each head (f32 or bf16, rows
+    at any pitch), weight [dim] or None.  Returns (y, summed, codes, scales): summed = h where there is a residual, codes and scales
+    the rows in 8 bits (float8_e4m3fn, a float32 scale for each) with want_codes; what is not wanted is None.  Outputs may be inputs."""
+    dt, rows, heads, dim = _norm_args(x, weight)
+    shape = x.shape
+    dev = _device_of(x) if weight is None else _device_of(x, weight)
+    raw, keep = _stream_on(stream, dev)
+    px = _stream_rows(x, shape, "x")
+    a_res, p_res, a_sum, p_sum, a_y, p_y, a_c, p_c, a_s = None, 0, None, 0, None, 0, None, 0, None
+    if residual is not None:
+        a_res, p_res = residual.data_ptr(), _stream_rows(residual, shape, "residual", x)
+        if summed is None:
+            summed, p_sum = _new(keep, shape, x.dtype, x.device), heads * dim
+        else:
+            p_sum = _stream_rows(summed, shape, "summed", x)
+        a_sum = summed.data_ptr()
+    elif summed is not None:
+        raise ValueError("summed without a residual: x itself is the stream")
+    if not want_y:
+        y = None
+    elif y is None:
+        y, p_y = _new(keep, shape, x.dtype, x.device), heads * dim
+        a_y = y.data_ptr()
+    else:
+        a_y, p_y = y.data_ptr(), _stream_rows(y, shape, "y", x)
+    if want_codes:
+        codes, p_c = _codes_rows(codes, shape, keep, x.device)
+        scales = _floats(scales, shape[:-1], keep, x.device, "scales")
+        a_c, a_s = codes.data_ptr(), scales.data_ptr()
+    else:
+        codes = scales = None
+    _launch("psrl_rms_norm_fwd", dev, dt, rows, heads, dim, x.data_ptr(), px, a_res, p_res, None if weight is None else weight.data_ptr(),
+            eps, a_sum, p_sum, a_y, p_y, a_c, p_c, a_s, raw)
+    return y, summed, codes, scales
+
+
+def psrl_rms_norm_workspace_bytes(n_rows: int, n_heads: int, dim: int, dtype: str = "bf16") -> int:
+    return int(lib().psrl_rms_norm_workspace_bytes(PSRL_F32 if dtype == "f32" else PSRL_BF16, int(n_rows), int(n_heads), int(dim)))
+
+
+def psrl_rms_norm_bwd(summed, weight, d_y, eps: float = 1e-6, d_summed=None, d_x=None, d_weight=None, want_x: bool = True,
+                      want_weight: bool = True, stream=None, workspace=None):
+    """Gradients of the above: (d_x, d_weight) given the rows h that were normed (the forward's `summed`, or its x), d_y and, with a
+    residual, the gradient d_summed that the stream brings back; d_x is the gradient of x and of residual.  d_x may be d_y or
+    d_summed.  `workspace`: a Workspace of psrl_rms_norm_workspace_bytes(); made if not given."""
+    dt, rows, heads, dim = _norm_args(summed, weight)
+    shape = summed.shape
+    dev = _device_of(summed, d_y) if weight is None else _device_of(summed, d_y, weight)
+    raw, keep = _stream_on(stream, dev)
+    ph, pd = _stream_rows(summed, shape, "summed"), _stream_rows(d_y, shape, "d_y", summed)
+    a_s, p_s, a_x, p_x = None, 0, None, 0
+    if d_summed is not None:
+        a_s, p_s = d_summed.data_ptr(), _stream_rows(d_summed, shape, "d_summed", summed)
+    if not want_x:
+        d_x = None
+    else:
+        if d_x is None:
+            d_x, p_x = _new(keep, shape, summed.dtype, summed.device), heads * dim
+        else:
+            p_x = _stream_rows(d_x, shape, "d_x", summed)
+        a_x = d_x.data_ptr()
+    if not want_weight or weight is None:
+        d_weight = None
+    elif d_weight is None:
+        d_weight = _new(keep, weight.shape, weight.dtype, weight.device)
+    elif d_weight.dtype is not weight.dtype or d_weight.shape != weight.shape or not d_weight.is_contiguous() or d_weight.get_device() != dev:
+        raise ValueError(f"d_weight must be a contiguous vector of {dim}, {weight.dtype} on {weight.device}")
+    if workspace is None:
+        held = Workspace(lib().psrl_rms_norm_workspace_bytes(dt, rows, heads, dim), summed.device, keep, raw)
+        ws, wsb = held.ptr, held.nbytes
+    else:
+        ws, wsb = _use_workspace(workspace, raw, keep, dev)
+    _launch("psrl_rms_norm_bwd", dev, dt, rows, heads, dim, summed.data_ptr(), ph, None if weight is None else weight.data_ptr(), eps,
+            d_y.data_ptr(), pd, a_s, p_s, a_x, p_x, None if d_weight is None else d_weight.data_ptr(), ws, wsb, raw)
+    return d_x, d_weight
+
+
+def psrl_quantize_rows(x, codes=None, scales=None, stream=None):
+    """Rows x [rows, dim] (f32 or bf16) in 8 bits: (codes float8_e4m3fn [rows, dim], scales float32 [rows])."""
+    dt, rows, heads, dim = _norm_args(x, None)
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, dim]")
+    dev = _device_of(x)
+    raw, keep = _stream_on(stream, dev)
+    px = _matrix_pitch(x, "x")
+    codes, pc = _codes_rows(codes, x.shape, keep, x.device)
+    scales = _floats(scales, x.shape[:1], keep, x.device, "scales")
+    _launch("psrl_quantize_rows", dev, dt, rows, dim, x.data_ptr(), px, codes.data_ptr(), pc, scales.data_ptr(), raw)
+    return codes, scales
 
 
 def _flags_ptr(seg_flags):

@@ -1,0 +1,574 @@
+// Root-mean-square norm of the residual stream, its gradients, and rows in 8 bits.
+//
+//   h = x + residual (rounded as it is stored),  y = h r w,  r = (mean(h^2) + eps)^-1/2
+//   8 bits: codes = e4m3(y / s), s = max(amax |y| / 448, 2^-126) for each row
+//   g = d_y w:  d_x = d_summed + r (g - h r^2 mean(g h)),  d_weight = sum over the rows of d_y h r
+//
+// Memory bound: each element is read once and written once.  A row stays in the registers of a group of threads between the
+// loads, the sum over it and the stores, so nothing is read twice; up to 32 lanes the sum is made by shuffles, beyond that with one
+// barrier.  Blocks are persistent, keep the weight in registers and, in the backward, their share of d_weight's sums, which a
+// second kernel adds up in the blocks' order: no atomics, the same bits every time.
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <float.h>
+
+#include <algorithm>
+
+#include "../../include/psrl.h"
+#include "kernels.h"
+
+namespace psrl {
+namespace {
+
+constexpr int kMaxDim = 32768;
+constexpr float kCodeMax = 448.f;          // the largest e4m3 number
+constexpr float kLeastScale = 0x1p-126f;   // a row of zeros, or nearly: its codes are zeros, or nearly
+
+struct FwdParams {
+  const void *x, *residual, *weight;
+  void *summed, *y;
+  uint8_t* codes;
+  float* scales;
+  int64_t x_pitch, residual_pitch, summed_pitch, y_pitch, codes_pitch;
+  int64_t rows;       // times heads
+  int32_t heads, vecs;
+  float inv_dim, eps;
+  int32_t norm;       // 0: only the 8-bit output of x itself
+};
+
+struct BwdParams {
+  const void *h, *weight, *d_y, *d_summed;
+  void* d_x;
+  float* part;        // [blocks][dim], or NULL
+  int* status;
+  int64_t h_pitch, d_y_pitch, d_summed_pitch, d_x_pitch;
+  int64_t rows;
+  int32_t heads, vecs;
+  float inv_dim, eps;
+};
+
+template <class T> constexpr int kElems = 16 / int(sizeof(T));
+
+// a 16-byte vector of bf16 or fp32 numbers
+template <class T>
+__device__ __forceinline__ void widen(const uint4& v, float (&o)[kElems<T>]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      o[i] = __uint_as_float(w[i]);
+    } else {
+      o[2 * i] = __uint_as_float(w[i] << 16);
+      o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ uint4 narrow(const float (&o)[kElems<T>]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      w[i] = __float_as_uint(o[i]);
+    } else {
+      const __nv_bfloat162 p = __floats2bfloat162_rn(o[2 * i], o[2 * i + 1]);   // the only rounding of an output
+      w[i] = *reinterpret_cast<const uint32_t*>(&p);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// max that a NaN survives
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+struct Add {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+struct MaxNan {
+  __device__ __forceinline__ float operator()(float a, float b) const { return max_nan(a, b); }
+};
+
+// The values of a group of kGroup threads joined, for all of them, in a fixed order.  Beyond a warp: `s` holds a value for each warp.
+// Every row has one barrier at least, so a warp that writes for the row after next knows that all have read this row's: two
+// rows in a row use two `s`.
+template <int kGroup, class Op>
+__device__ __forceinline__ float join(float v, Op op, float* s) {
+#pragma unroll
+  for (int o = (kGroup < 32 ? kGroup : 32) / 2; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+  if constexpr (kGroup > 32) {
+    constexpr int kWarps = kGroup / 32;
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = s[threadIdx.x & (kWarps - 1)];
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+  }
+  return v;
+}
+template <int kGroup>
+__device__ __forceinline__ float2 join_sums(float2 v, float2* s) {
+#pragma unroll
+  for (int o = (kGroup < 32 ? kGroup : 32) / 2; o > 0; o >>= 1) {
+    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+  }
+  if constexpr (kGroup > 32) {
+    constexpr int kWarps = kGroup / 32;
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = s[threadIdx.x & (kWarps - 1)];
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) {
+      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+      v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    }
+  }
+  return v;
+}
+
+// Squares of numbers beyond 2^56 may pass fp32's range: the sum is then made again of h 2^-80, whose squares do not, and whose
+// roundings are the same.  (eps is nothing beside such a row.  NaN and infinities come this way, too, and stay.)
+constexpr float kSmall = 0x1p-80f;
+__device__ __forceinline__ bool too_large(float sum) { return !(sum <= FLT_MAX); }
+
+constexpr int threads_of(int group) { return group > 256 ? group : group > 32 ? group : 256; }
+
+// Row i of rows x heads, in vectors of the matrix at `pitch` elements a row.
+template <class T>
+__device__ __forceinline__ int64_t vec_at(int64_t row, int head, int64_t pitch, int vecs) {
+  return row * (pitch / kElems<T>) + int64_t(head) * vecs;
+}
+
+template <class T, int kGroup, int kVecs>
+__global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __grid_constant__ FwdParams p) {
+  constexpr int kE = kElems<T>, kPerBlock = threads_of(kGroup) / kGroup;
+  __shared__ float s_sum[2][3][32];   // two rows in a row use two
+  const int lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup;
+  uint4 w[kVecs];
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    const int v = lane + k * kGroup;
+    w[k] = make_uint4(0, 0, 0, 0);
+    if (p.weight && v < p.vecs) w[k] = static_cast<const uint4*>(p.weight)[v];
+  }
+  int turn = 0;
+  // all threads of a warp take part in its shuffles: a group without a row of its own goes along with the others
+  for (int64_t i0 = int64_t(blockIdx.x) * kPerBlock; i0 < p.rows; i0 += int64_t(gridDim.x) * kPerBlock, turn ^= 1) {
+    const int64_t i = i0 + group;
+    const bool live = i < p.rows;
+    const int64_t row = p.heads == 1 ? i : i / p.heads;
+    const int head = p.heads == 1 ? 0 : int(i - row * p.heads);
+    const uint4* x = static_cast<const uint4*>(p.x) + vec_at<T>(row, head, p.x_pitch, p.vecs);
+    const uint4* res = static_cast<const uint4*>(p.residual) + vec_at<T>(row, head, p.residual_pitch, p.vecs);
+    uint4 xv[kVecs], rv[kVecs];
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const int v = lane + k * kGroup;
+      xv[k] = rv[k] = make_uint4(0, 0, 0, 0);
+      if (live && v < p.vecs) {
+        xv[k] = x[v];
+        if (p.residual) rv[k] = res[v];
+      }
+    }
+    if (p.residual) {
+      uint4* to = static_cast<uint4*>(p.summed) + vec_at<T>(row, head, p.summed_pitch, p.vecs);
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        float a[kE], b[kE];
+        widen<T>(xv[k], a);
+        widen<T>(rv[k], b);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) a[e] += b[e];
+        xv[k] = narrow<T>(a);
+        const int v = lane + k * kGroup;
+        if (p.summed && live && v < p.vecs) to[v] = xv[k];
+      }
+    }
+    float r = 1.f;
+    if (p.norm) {
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        float h[kE];
+        widen<T>(xv[k], h);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) sum = fmaf(h[e], h[e], sum);
+      }
+      sum = join<kGroup>(sum, Add(), s_sum[turn][0]);
+      r = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
+      if (kGroup > 32 ? too_large(sum) : __any_sync(0xffffffffu, too_large(sum))) {   // uniform in a warp, or in the block
+        float small = 0.f;
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+          float h[kE];
+          widen<T>(xv[k], h);
+#pragma unroll
+          for (int e = 0; e < kE; ++e) small = fmaf(h[e] * kSmall, h[e] * kSmall, small);
+        }
+        small = join<kGroup>(small, Add(), s_sum[turn][1]);
+        if (too_large(sum)) r = rsqrtf(small * p.inv_dim) * kSmall;
+      }
+    }
+    uint4* y = static_cast<uint4*>(p.y) + vec_at<T>(row, head, p.y_pitch, p.vecs);
+    float amax = 0.f;
+    float o[kVecs][kE];
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      float g[kE];
+      widen<T>(xv[k], o[k]);
+      widen<T>(w[k], g);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        o[k][e] *= r;
+        if (p.weight) o[k][e] *= g[e];
+      }
+      const int v = lane + k * kGroup;
+      if (v < p.vecs) {
+        if (p.y && live) y[v] = narrow<T>(o[k]);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) amax = max_nan(amax, fabsf(o[k][e]));
+      }
+    }
+    if (p.codes) {
+      amax = join<kGroup>(amax, MaxNan(), s_sum[turn][2]);
+      const float scale = max_nan(amax / kCodeMax, kLeastScale);
+      const float inv = 1.f / scale;
+      uint8_t* c = p.codes + row * p.codes_pitch + int64_t(head) * p.vecs * kE;
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        uint32_t b[kE / 4];
+#pragma unroll
+        for (int e = 0; e < kE; e += 4) {   // rounded to the nearest code, ties to even; what passes the largest by a rounding is held there
+          const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(o[k][e] * inv, o[k][e + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+          const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(o[k][e + 2] * inv, o[k][e + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+          b[e / 4] = lo | hi << 16;
+        }
+        const int v = lane + k * kGroup;
+        if (live && v < p.vecs) {
+          if constexpr (kE == 8) reinterpret_cast<uint2*>(c)[v] = make_uint2(b[0], b[1]);
+          else reinterpret_cast<uint32_t*>(c)[v] = b[0];
+        }
+      }
+      if (live && lane == 0) p.scales[i] = scale;
+    }
+  }
+}
+
+template <class T, int kGroup, int kVecs>
+__global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __grid_constant__ BwdParams p) {
+  constexpr int kE = kElems<T>, kThreads = threads_of(kGroup), kPerBlock = kThreads / kGroup;
+  __shared__ float2 s_sum[2][2][32];
+  __shared__ float s_part[kGroup > 32 ? 1 : kThreads * kVecs * kE];
+  if (p.status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
+  const int lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup;
+  uint4 w[kVecs];
+  float dw[kVecs][kE];
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    const int v = lane + k * kGroup;
+    w[k] = make_uint4(0, 0, 0, 0);
+    if (p.weight && v < p.vecs) w[k] = static_cast<const uint4*>(p.weight)[v];
+#pragma unroll
+    for (int e = 0; e < kE; ++e) dw[k][e] = 0.f;
+  }
+  int turn = 0;
+  for (int64_t i0 = int64_t(blockIdx.x) * kPerBlock; i0 < p.rows; i0 += int64_t(gridDim.x) * kPerBlock, turn ^= 1) {
+    const int64_t i = i0 + group;
+    const bool live = i < p.rows;
+    const int64_t row = p.heads == 1 ? i : i / p.heads;
+    const int head = p.heads == 1 ? 0 : int(i - row * p.heads);
+    const uint4* h = static_cast<const uint4*>(p.h) + vec_at<T>(row, head, p.h_pitch, p.vecs);
+    const uint4* dy = static_cast<const uint4*>(p.d_y) + vec_at<T>(row, head, p.d_y_pitch, p.vecs);
+    const uint4* ds = static_cast<const uint4*>(p.d_summed) + vec_at<T>(row, head, p.d_summed_pitch, p.vecs);
+    uint4 hv[kVecs], gv[kVecs], sv[kVecs];
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const int v = lane + k * kGroup;
+      hv[k] = gv[k] = sv[k] = make_uint4(0, 0, 0, 0);
+      if (live && v < p.vecs) {
+        hv[k] = h[v];
+        gv[k] = dy[v];
+        if (p.d_summed) sv[k] = ds[v];
+      }
+    }
+    auto sums = [&](float small) {
+      float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        float a[kE], g[kE], c[kE];
+        widen<T>(hv[k], a);
+        widen<T>(gv[k], g);
+        widen<T>(w[k], c);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          a[e] *= small;
+          if (p.weight) g[e] *= c[e];
+          s.x = fmaf(a[e], a[e], s.x);
+          s.y = fmaf(a[e], g[e], s.y);
+        }
+      }
+      return s;
+    };
+    float2 s = join_sums<kGroup>(sums(1.f), s_sum[turn][0]);
+    float r = rsqrtf(fmaf(s.x, p.inv_dim, p.eps)), along = s.y * p.inv_dim * r;   // mean of g times the unit row h r
+    if (kGroup > 32 ? too_large(s.x) : __any_sync(0xffffffffu, too_large(s.x))) {
+      const float2 t = join_sums<kGroup>(sums(kSmall), s_sum[turn][1]);
+      if (too_large(s.x)) {
+        r = rsqrtf(t.x * p.inv_dim);
+        along = t.y * p.inv_dim * r;
+        r *= kSmall;
+      }
+    }
+    uint4* dx = static_cast<uint4*>(p.d_x) + vec_at<T>(row, head, p.d_x_pitch, p.vecs);
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      float a[kE], g[kE], c[kE], o[kE];
+      widen<T>(hv[k], a);
+      widen<T>(gv[k], g);
+      widen<T>(w[k], c);
+      widen<T>(sv[k], o);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const float unit = a[e] * r;
+        if (live) dw[k][e] = fmaf(g[e], unit, dw[k][e]);
+        const float gw = p.weight ? g[e] * c[e] : g[e];
+        o[e] = fmaf(r, fmaf(-unit, along, gw), o[e]);
+      }
+      const int v = lane + k * kGroup;
+      if (p.d_x && live && v < p.vecs) dx[v] = narrow<T>(o);
+    }
+  }
+  if (!p.part) return;
+  float* part = p.part + int64_t(blockIdx.x) * p.vecs * kE;
+  if constexpr (kGroup > 32) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const int v = lane + k * kGroup;
+      if (v < p.vecs)
+#pragma unroll
+        for (int e = 0; e < kE; e += 4) *reinterpret_cast<float4*>(part + v * kE + e) = make_float4(dw[k][e], dw[k][e + 1], dw[k][e + 2], dw[k][e + 3]);
+    }
+  } else {
+    constexpr int kRow = kGroup * kVecs * kE;
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k)
+#pragma unroll
+      for (int e = 0; e < kE; ++e) s_part[group * kRow + (lane + k * kGroup) * kE + e] = dw[k][e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.vecs * kE; c += kThreads) {
+      float s = 0.f;
+      for (int g = 0; g < kPerBlock; ++g) s += s_part[g * kRow + c];
+      part[c] = s;
+    }
+  }
+}
+
+// d_weight: the blocks' sums, added in a fixed order.  A block takes 32 columns, 32 threads share the parts of each.
+template <class T>
+__global__ void __launch_bounds__(1024) rms_weight_kernel(const float* __restrict__ part, int parts, int dim, T* __restrict__ d_weight) {
+  __shared__ float s[32][33];
+  const int c = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
+  float sum = 0.f;
+  if (col < dim)
+    for (int i = slice; i < parts; i += 32) sum += part[int64_t(i) * dim + col];
+  s[slice][c] = sum;
+  __syncthreads();
+  sum = s[c][slice];   // thread (slice, c) now has part c of column `slice`
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (c == 0 && blockIdx.x * 32 + slice < dim) {
+    if constexpr (sizeof(T) == 4) d_weight[blockIdx.x * 32 + slice] = sum;
+    else d_weight[blockIdx.x * 32 + slice] = __float2bfloat16_rn(sum);
+  }
+}
+
+// Threads of a row's group and the vectors of each.
+struct Shape {
+  int group, vecs;
+};
+// Few vectors to a thread hide the latency of a row with many threads where rows are few; with many rows more vectors in flight
+// a thread and fewer barriers a byte are better.
+Shape shape_of(int vecs, int64_t rows) {
+  if (vecs <= 8) return {8, 1};
+  if (vecs <= 16) return {16, 1};
+  if (vecs <= 32) return {32, 1};
+  if (rows <= 2 * resident_ctas()) {
+    if (vecs <= 128) return {128, 1};
+    if (vecs <= 256) return {256, 1};
+    if (vecs <= 512) return {512, 1};
+    if (vecs <= 1024) return {1024, 1};
+    if (vecs <= 2048) return {1024, 2};
+    return vecs <= 4096 ? Shape{1024, 4} : Shape{1024, 8};
+  }
+  if (vecs <= 64) return {32, 2};
+  if (vecs <= 128) return {32, 4};
+  if (vecs <= 256) return {128, 2};
+  if (vecs <= 512) return {256, 2};
+  if (vecs <= 768) return {256, 3};
+  if (vecs <= 1024) return {256, 4};
+  if (vecs <= 2048) return {512, 4};
+  return vecs <= 4096 ? Shape{1024, 4} : Shape{1024, 8};
+}
+
+// Blocks of a launch: as many as the SMs hold at about 1024 threads each, and no more than there are rows for.
+int64_t blocks_of(const Shape& s, int64_t rows) {
+  const int threads = threads_of(s.group), per_block = threads / s.group;
+  return std::min<int64_t>(int64_t(resident_ctas()) * std::max(1, 1024 / threads), (rows + per_block - 1) / per_block);
+}
+
+template <class T, int kGroup, int kVecs, class P>
+void launch_one(const P& p, int64_t blocks, cudaStream_t stream) {
+  if constexpr (std::is_same_v<P, FwdParams>) rms_fwd_kernel<T, kGroup, kVecs><<<unsigned(blocks), threads_of(kGroup), 0, stream>>>(p);
+  else rms_bwd_kernel<T, kGroup, kVecs><<<unsigned(blocks), threads_of(kGroup), 0, stream>>>(p);
+}
+
+template <class T, class P>
+cudaError_t launch(const P& p, cudaStream_t stream) {
+  const Shape s = shape_of(p.vecs, p.rows);
+  const int64_t blocks = blocks_of(s, p.rows);
+  switch (s.group * 16 + s.vecs) {
+    case 8 * 16 + 1: launch_one<T, 8, 1>(p, blocks, stream); break;
+    case 16 * 16 + 1: launch_one<T, 16, 1>(p, blocks, stream); break;
+    case 32 * 16 + 1: launch_one<T, 32, 1>(p, blocks, stream); break;
+    case 32 * 16 + 2: launch_one<T, 32, 2>(p, blocks, stream); break;
+    case 32 * 16 + 4: launch_one<T, 32, 4>(p, blocks, stream); break;
+    case 128 * 16 + 1: launch_one<T, 128, 1>(p, blocks, stream); break;
+    case 128 * 16 + 2: launch_one<T, 128, 2>(p, blocks, stream); break;
+    case 256 * 16 + 1: launch_one<T, 256, 1>(p, blocks, stream); break;
+    case 256 * 16 + 2: launch_one<T, 256, 2>(p, blocks, stream); break;
+    case 256 * 16 + 3: launch_one<T, 256, 3>(p, blocks, stream); break;
+    case 256 * 16 + 4: launch_one<T, 256, 4>(p, blocks, stream); break;
+    case 512 * 16 + 1: launch_one<T, 512, 1>(p, blocks, stream); break;
+    case 512 * 16 + 4: launch_one<T, 512, 4>(p, blocks, stream); break;
+    case 1024 * 16 + 1: launch_one<T, 1024, 1>(p, blocks, stream); break;
+    case 1024 * 16 + 2: launch_one<T, 1024, 2>(p, blocks, stream); break;
+    case 1024 * 16 + 4: launch_one<T, 1024, 4>(p, blocks, stream); break;
+    default:
+      // 8 vectors a thread: only fp32 rows of more than 16384 get here
+      if constexpr (sizeof(T) == 4) launch_one<T, 1024, 8>(p, blocks, stream);
+      else return cudaErrorInvalidValue;
+  }
+  return cudaGetLastError();
+}
+
+int vec_elems(psrl_dtype_t t) { return t == PSRL_BF16 ? 8 : 4; }
+bool known(psrl_dtype_t t) { return t == PSRL_F32 || t == PSRL_BF16; }
+bool pitch_ok(int64_t pitch, int64_t least, int64_t unit) { return pitch >= least && pitch % unit == 0 && pitch <= (int64_t(1) << 40); }
+// a tensor that may be left out, with its pitch; in place of another one only with the same pitch
+bool tensor_ok(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool same_rows(const void* out, int64_t out_pitch, const void* in, int64_t in_pitch, int64_t rows) {
+  return !out || out != in || out_pitch == in_pitch || rows <= 1;
+}
+constexpr int64_t kMostRows = int64_t(1) << 32;
+
+psrl_status_t check(psrl_dtype_t dtype, int64_t rows, int32_t heads, int32_t dim, float eps) {
+  if (!known(dtype)) return PSRL_ERR_UNSUPPORTED;
+  if (rows < 0 || heads < 1 || heads > 65535 || rows > kMostRows || !(eps > 0.f) || !(eps <= FLT_MAX)) return PSRL_ERR_INVALID_ARG;
+  if (dim < 8 || dim % 8 || dim > kMaxDim) return PSRL_ERR_SHAPE;
+  return PSRL_OK;
+}
+
+psrl_status_t done(cudaError_t e) {
+  if (e == cudaSuccess) return PSRL_OK;
+  set_last_cuda_error(e);
+  return PSRL_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace psrl
+
+extern "C" {
+
+psrl_status_t psrl_rms_norm_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim, const void* x, int64_t x_pitch,
+                                const void* residual, int64_t residual_pitch, const void* weight, float eps, void* summed,
+                                int64_t summed_pitch, void* y, int64_t y_pitch, void* codes, int64_t codes_pitch, float* scales,
+                                void* stream) {
+  using namespace psrl;
+  psrl_status_t st = check(dtype, n_rows, n_heads, dim, eps);
+  if (st != PSRL_OK) return st;
+  const int64_t least = int64_t(n_heads) * dim, unit = vec_elems(dtype);
+  if (!pitch_ok(x_pitch, least, unit) || (residual && !pitch_ok(residual_pitch, least, unit)) || (residual && summed && !pitch_ok(summed_pitch, least, unit)) ||
+      (y && !pitch_ok(y_pitch, least, unit)) || (codes && !pitch_ok(codes_pitch, least, 16)))
+    return PSRL_ERR_SHAPE;
+  if (n_rows == 0) return PSRL_OK;
+  if (!residual) summed = nullptr;   // x itself is the stream
+  if (!x || !tensor_ok(x) || !tensor_ok(residual) || !tensor_ok(weight) || !tensor_ok(summed) || !tensor_ok(y) || !tensor_ok(codes) ||
+      (!codes) != (!scales) || (scales && !ptr_aligned(scales, 4)) || (y && y == summed) ||
+      !same_rows(summed, summed_pitch, x, x_pitch, n_rows) || !same_rows(summed, summed_pitch, residual, residual_pitch, n_rows) ||
+      !same_rows(y, y_pitch, x, x_pitch, n_rows) || !same_rows(y, y_pitch, residual, residual_pitch, n_rows))
+    return PSRL_ERR_INVALID_ARG;
+  if (!summed && !y && !codes) return PSRL_OK;
+  FwdParams p{x, residual, weight, summed, y, static_cast<uint8_t*>(codes), scales, x_pitch, residual_pitch, summed_pitch, y_pitch, codes_pitch,
+              n_rows * n_heads, n_heads, int32_t(dim / unit), 1.f / float(dim), eps, 1};
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return done(dtype == PSRL_BF16 ? launch<__nv_bfloat16>(p, s) : launch<float>(p, s));
+}
+
+psrl_status_t psrl_quantize_rows(psrl_dtype_t dtype, int64_t n_rows, int32_t dim, const void* x, int64_t x_pitch, void* codes,
+                                 int64_t codes_pitch, float* scales, void* stream) {
+  using namespace psrl;
+  psrl_status_t st = check(dtype, n_rows, 1, dim, 1.f);
+  if (st != PSRL_OK) return st;
+  const int64_t unit = vec_elems(dtype);
+  if (!pitch_ok(x_pitch, dim, unit) || !pitch_ok(codes_pitch, dim, 16)) return PSRL_ERR_SHAPE;
+  if (n_rows == 0) return PSRL_OK;
+  if (!ptr_aligned(x, 16) || !ptr_aligned(codes, 16) || !ptr_aligned(scales, 4)) return PSRL_ERR_INVALID_ARG;
+  FwdParams p{x, nullptr, nullptr, nullptr, nullptr, static_cast<uint8_t*>(codes), scales, x_pitch, 0, 0, 0, codes_pitch,
+              n_rows, 1, int32_t(dim / unit), 1.f / float(dim), 0.f, 0};
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return done(dtype == PSRL_BF16 ? launch<__nv_bfloat16>(p, s) : launch<float>(p, s));
+}
+
+size_t psrl_rms_norm_workspace_bytes(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim) {
+  using namespace psrl;
+  if (check(dtype, n_rows, n_heads, dim, 1.f) != PSRL_OK) return 0;
+  if (n_rows == 0) return kWsHeaderBytes;
+  const int64_t rows = n_rows * n_heads;
+  return kWsHeaderBytes + size_t(blocks_of(shape_of(dim / vec_elems(dtype), rows), rows)) * size_t(dim) * sizeof(float);
+}
+
+psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim, const void* summed, int64_t summed_pitch,
+                                const void* weight, float eps, const void* d_y, int64_t d_y_pitch, const void* d_summed,
+                                int64_t d_summed_pitch, void* d_x, int64_t d_x_pitch, void* d_weight, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  using namespace psrl;
+  psrl_status_t st = check(dtype, n_rows, n_heads, dim, eps);
+  if (st != PSRL_OK) return st;
+  const int64_t least = int64_t(n_heads) * dim, unit = vec_elems(dtype);
+  if (!pitch_ok(summed_pitch, least, unit) || !pitch_ok(d_y_pitch, least, unit) || (d_summed && !pitch_ok(d_summed_pitch, least, unit)) ||
+      (d_x && !pitch_ok(d_x_pitch, least, unit)))
+    return PSRL_ERR_SHAPE;
+  if (!ptr_aligned(workspace, 256) || (d_weight && (!weight || !tensor_ok(d_weight)))) return PSRL_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const size_t es = dtype == PSRL_BF16 ? 2 : 4;
+  if (n_rows == 0) {
+    cudaError_t e = workspace_bytes < kWsHeaderBytes ? cudaSuccess : cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+    if (workspace_bytes < kWsHeaderBytes) return PSRL_ERR_WORKSPACE;
+    if (e == cudaSuccess && d_weight) e = cudaMemsetAsync(d_weight, 0, size_t(dim) * es, s);
+    return done(e);
+  }
+  if (!summed || !d_y || !tensor_ok(summed) || !tensor_ok(weight) || !tensor_ok(d_y) || !tensor_ok(d_summed) || !tensor_ok(d_x) ||
+      !same_rows(d_x, d_x_pitch, summed, summed_pitch, n_rows) || !same_rows(d_x, d_x_pitch, d_y, d_y_pitch, n_rows) ||
+      !same_rows(d_x, d_x_pitch, d_summed, d_summed_pitch, n_rows))
+    return PSRL_ERR_INVALID_ARG;
+  if (workspace_bytes < (d_weight ? psrl_rms_norm_workspace_bytes(dtype, n_rows, n_heads, dim) : kWsHeaderBytes)) return PSRL_ERR_WORKSPACE;
+  float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kWsHeaderBytes);
+  BwdParams p{summed, weight, d_y, d_summed, d_x, d_weight ? part : nullptr, static_cast<int*>(workspace), summed_pitch, d_y_pitch, d_summed_pitch,
+              d_x_pitch, n_rows * n_heads, n_heads, int32_t(dim / unit), 1.f / float(dim), eps};
+  cudaError_t e = dtype == PSRL_BF16 ? launch<__nv_bfloat16>(p, s) : launch<float>(p, s);
+  if (e == cudaSuccess && d_weight) {
+    const int parts = int(blocks_of(shape_of(p.vecs, p.rows), p.rows));
+    const unsigned grid = unsigned((dim + 31) / 32);
+    if (dtype == PSRL_BF16) rms_weight_kernel<<<grid, 1024, 0, s>>>(part, parts, dim, static_cast<__nv_bfloat16*>(d_weight));
+    else rms_weight_kernel<<<grid, 1024, 0, s>>>(part, parts, dim, static_cast<float*>(d_weight));
+    e = cudaGetLastError();
+  }
+  return done(e);
+}
+
+}  // extern "C"
