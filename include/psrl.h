@@ -47,7 +47,7 @@ typedef enum {
   PSRL_ERR_INTERNAL = 11
 } psrl_status_t;
 
-typedef enum { PSRL_F32 = 0, PSRL_BF16 = 1 } psrl_dtype_t;
+typedef enum { PSRL_F32 = 0, PSRL_BF16 = 1, PSRL_E4M3 = 2 } psrl_dtype_t; /* E4M3: operands of psrl_linear_fwd only */
 
 /* Segment flags. */
 enum {
@@ -420,6 +420,45 @@ psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_he
                                 size_t workspace_bytes, void* stream);
 psrl_status_t psrl_quantize_rows(psrl_dtype_t dtype, int64_t n_rows, int32_t dim, const void* x, int64_t x_pitch, void* codes,
                                  int64_t codes_pitch, float* scales, void* stream);
+
+/*
+ * psrl_linear_fwd / _bwd - a layer's matrix products with what follows them (projections with bias, the output projection onto the
+ * residual stream, the gate of a gated MLP), and their gradients.
+ *   z = sum_k x[m, k] weight[n, k] + bias[n]        (E4M3: times x_scale[m] weight_scale[n] before the bias)
+ *   y = act(z) * mul + residual
+ * in fp32 from the products on, y and z rounded once.  Activations: NONE, RELU, SILU z / (1 + e^-z), GELU z (1 + erf(z / sqrt 2)) / 2,
+ * GELU_TANH z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2.
+ * Backward, at the z that the forward stored:
+ *   d_mul = d_y * act(z),   dz = d_y * mul * act'(z),   d_bias = sum over rows of dz,   d_x = dz weight,   d_weight = dz^T x
+ * (residual's gradient is d_y itself).  Sums in fp32; dz rounded to dtype as the products' operand; bitwise reproducible.
+ *   x        [n_rows, in_dim], weight [out_dim, in_dim] DEVICE of `dtype`, rows at a pitch in elements
+ *   x_scale [n_rows], weight_scale [out_dim] DEVICE fp32: with E4M3, and only then (psrl_rms_norm_fwd's and psrl_quantize_rows' outputs)
+ *   bias [out_dim], mul, residual, y, z [n_rows, out_dim] DEVICE of `dtype`, with E4M3 bf16; bias, mul, residual, z NULL: none
+ *   z        (backward) as the forward stored it; may be NULL where activation is NONE and d_mul is not wanted
+ *   d_y, d_x, d_weight, d_bias, d_mul  as their tensors; the outputs NULL: not wanted.  E4M3 has no backward
+ *   workspace  DEVICE, 256-byte aligned, of psrl_linear_workspace_bytes; holds the device status word.  Forward 256 bytes; backward dz
+ *              (n_rows rows of out_dim in whole 8s) and a number for each column and 64 rows, neither needed where there is no
+ *              activation, mul or d_bias that asks for it; F32: with few rows or columns the sums of parts of the depth, below 20 MB
+ * y and z may be mul or residual, d_mul may be d_y, mul or z (equal pitches); otherwise tensors are apart.  in_dim is a multiple of 8,
+ * out_dim any; pitches are multiples of 16 bytes and at least a row, pointers 16-byte aligned (scales 4).  Dimensions are at most 2^30.
+ * n_rows = 0 does nothing (backward: zeroes d_weight and d_bias).
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), WORKSPACE, CUDA.  Asynchronous; calls that may overlap on the GPU need distinct
+ * workspaces.
+ */
+typedef enum {
+  PSRL_ACT_NONE = 0, PSRL_ACT_RELU = 1, PSRL_ACT_SILU = 2, PSRL_ACT_GELU = 3, PSRL_ACT_GELU_TANH = 4
+} psrl_activation_t;
+size_t psrl_linear_workspace_bytes(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim, int32_t out_dim, int backward);
+psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim, int32_t out_dim, const void* x, int64_t x_pitch,
+                              const float* x_scale, const void* weight, int64_t weight_pitch, const float* weight_scale, const void* bias,
+                              psrl_activation_t activation, const void* mul, int64_t mul_pitch, const void* residual,
+                              int64_t residual_pitch, void* y, int64_t y_pitch, void* z, int64_t z_pitch, void* workspace,
+                              size_t workspace_bytes, void* stream);
+psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim, int32_t out_dim, const void* x, int64_t x_pitch,
+                              const void* weight, int64_t weight_pitch, const void* z, int64_t z_pitch, psrl_activation_t activation,
+                              const void* mul, int64_t mul_pitch, const void* d_y, int64_t d_y_pitch, void* d_x, int64_t d_x_pitch,
+                              void* d_weight, int64_t d_weight_pitch, void* d_bias, void* d_mul, int64_t d_mul_pitch, void* workspace,
+                              size_t workspace_bytes, void* stream);
 
 /*
  * psrl_plan_next_tokens - the targets of the tree's language-model loss.  A query row predicts the next token of its own

@@ -20,7 +20,7 @@ STATUS_NAMES = [
     "PSRL_ERR_UNSUPPORTED", "PSRL_ERR_POOL_FULL", "PSRL_ERR_WORKSPACE", "PSRL_ERR_HOST_OOM", "PSRL_ERR_CUDA",
     "PSRL_ERR_TIMEOUT", "PSRL_ERR_INTERNAL",
 ]
-PSRL_F32, PSRL_BF16 = 0, 1
+PSRL_F32, PSRL_BF16, PSRL_E4M3 = 0, 1, 2
 BWD_STATIC_SCRATCH_BYTES = 16 * 1024 * 1024 + 256   # PSRL_BWD_STATIC_SCRATCH_BYTES of include/psrl.h
 SEG_HAS_Q, SEG_SAMPLE_END = 1, 2
 
@@ -36,6 +36,7 @@ EXPORTS = [
     "psrl_rope_rows",
     "psrl_rope_create_axes", "psrl_rope_axes_qkv_fwd", "psrl_rope_axes_qkv_bwd", "psrl_rope_axes_rows",
     "psrl_rms_norm_fwd", "psrl_rms_norm_bwd", "psrl_rms_norm_workspace_bytes", "psrl_quantize_rows",
+    "psrl_linear_fwd", "psrl_linear_bwd", "psrl_linear_workspace_bytes",
     "psrl_plan_next_tokens", "psrl_token_logprob_workspace_bytes", "psrl_token_logprob_fwd", "psrl_token_logprob_bwd",
     "psrl_cache_compact", "psrl_kv_copy", "psrl_kv_move",
     "psrl_cost_sequence", "psrl_group_workloads", "psrl_place_groups", "psrl_microbatch_tokens",
@@ -220,6 +221,14 @@ def lib() -> C.CDLL:
     L.psrl_rms_norm_bwd.restype = C.c_int
     L.psrl_quantize_rows.argtypes = [C.c_int, _I64, C.c_int32, _VP, _I64, _VP, _I64, _VP, _VP]
     L.psrl_quantize_rows.restype = C.c_int
+    L.psrl_linear_workspace_bytes.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, C.c_int]
+    L.psrl_linear_workspace_bytes.restype = C.c_size_t
+    L.psrl_linear_fwd.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, _VP, _I64, _VP, _VP, _I64, _VP, _VP, C.c_int, _VP, _I64, _VP, _I64, _VP, _I64,
+                                  _VP, _I64, _VP, C.c_size_t, _VP]
+    L.psrl_linear_fwd.restype = C.c_int
+    L.psrl_linear_bwd.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, _VP, _I64, _VP, _I64, _VP, _I64, C.c_int, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64,
+                                  _VP, _VP, _I64, _VP, C.c_size_t, _VP]
+    L.psrl_linear_bwd.restype = C.c_int
     L.psrl_plan_next_tokens.argtypes = [_VP, C.POINTER(_I32P), C.POINTER(_I32P)]
     L.psrl_plan_next_tokens.restype = C.c_int
     L.psrl_token_logprob_workspace_bytes.argtypes = [C.c_int, _I64, C.c_int32, C.c_int32, _I64, C.c_int]
@@ -1093,6 +1102,134 @@ def psrl_quantize_rows(x, codes=None, scales=None, stream=None):
     scales = _floats(scales, x.shape[:1], keep, x.device, "scales")
     _launch("psrl_quantize_rows", dev, dt, rows, dim, x.data_ptr(), px, codes.data_ptr(), pc, scales.data_ptr(), raw)
     return codes, scales
+
+
+_ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+
+def _linear_args(x, weight, activation, others):
+    """(type, rows, in_dim, out_dim, device, the outputs' type) with what the two directions check alike."""
+    dt = _type_code(x)
+    if dt is None:
+        if x.dtype is not _codes_type():
+            raise TypeError(f"dtype {x.dtype} is none of float32, bfloat16, float8_e4m3fn")
+        dt = PSRL_E4M3
+    if weight.dtype is not x.dtype:
+        raise TypeError(f"weight is {weight.dtype}, x is {x.dtype}")
+    xs, ws = x.shape, weight.shape
+    if len(xs) != 2 or len(ws) != 2 or xs[1] != ws[1]:
+        raise ValueError("x must be [rows, in_dim], weight [out_dim, in_dim]")
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation {activation!r} unknown")
+    out = x.dtype
+    if dt == PSRL_E4M3:
+        import torch
+
+        out = torch.bfloat16
+    dev = _device_of(x, weight)
+    for name, t, shape in others:
+        if t is None:
+            continue
+        if t.dtype is not out or t.get_device() != dev or t.shape != shape:
+            raise ValueError(f"{name} must be {out} {tuple(shape)} on {x.device}")
+        if len(shape) == 1 and shape[0] > 1 and t.stride(0) != 1:
+            raise ValueError(f"{name} must be contiguous")
+    return dt, xs[0], xs[1], ws[0], dev, out
+
+
+def _operand_pitch(t, name: str) -> int:
+    """Row pitch of a matrix operand; a lone row has any that will do."""
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+
+
+def _matrix(t, rows: int, cols: int, dtype, keep, device):
+    """A [rows, cols] output, made if not given with rows that are whole 16-byte vectors apart, its address and row pitch."""
+    if t is None:
+        pitch = -(-cols // 8) * 8
+        t = _new(keep, (rows, pitch), dtype, device)
+        return (t if pitch == cols else t[:, :cols]), t.data_ptr(), pitch
+    return t, t.data_ptr(), _operand_pitch(t, "output")
+
+
+def _optional(t, name: str):
+    return (None, 0) if t is None else (t.data_ptr(), _operand_pitch(t, name))
+
+
+def psrl_linear_workspace_bytes(n_rows: int, in_dim: int, out_dim: int, backward: bool, dtype: str = "bf16") -> int:
+    return int(lib().psrl_linear_workspace_bytes({"f32": PSRL_F32, "e4m3": PSRL_E4M3}.get(dtype, PSRL_BF16), int(n_rows), int(in_dim), int(out_dim),
+                                                 int(bool(backward))))
+
+
+def psrl_linear_fwd(x, weight, bias=None, activation=None, mul=None, residual=None, x_scale=None, weight_scale=None, y=None, z=None,
+                    want_z: bool = False, stream=None, workspace=None):
+    """y = act(x weight^T + bias) * mul + residual: x [rows, in_dim], weight [out_dim, in_dim], both f32, both bf16, or both 8-bit codes
+    (float8_e4m3fn) with float32 x_scale [rows] and weight_scale [out_dim], the rest then bf16.  activation: None, "relu", "silu",
+    "gelu", "gelu_tanh".  Returns (y, z), z = x weight^T + bias with want_z (for the backward), else None.  y and z may be mul or
+    residual.  `workspace`: a Workspace of psrl_linear_workspace_bytes(), whose status() tells whether a wait inside the kernel gave
+    up; made if not given."""
+    m, n = x.shape[0], weight.shape[0]
+    dt, m, k, n, dev, out = _linear_args(x, weight, activation, (("bias", bias, (n,)), ("mul", mul, (m, n)), ("residual", residual, (m, n)), ("y", y, (m, n)),
+                                                                 ("z", z, (m, n))))
+    for name, t, count in (("x_scale", x_scale, m), ("weight_scale", weight_scale, n)):
+        if (t is not None) != (dt == PSRL_E4M3):
+            raise ValueError(f"{name}: 8-bit operands have scales, others none")
+        if t is not None:
+            _floats(t, (count,), None, x.device, name)
+    raw, keep = _stream_on(stream, dev)
+    a_mul, p_mul = _optional(mul, "mul")
+    a_res, p_res = _optional(residual, "residual")
+    px, pw = _operand_pitch(x, "x"), _operand_pitch(weight, "weight")
+    y, a_y, p_y = _matrix(y, m, n, out, keep, x.device)
+    if want_z:
+        z, a_z, p_z = _matrix(z, m, n, out, keep, x.device)
+    else:
+        z, a_z, p_z = None, None, 0
+    if workspace is None:
+        held = Workspace(lib().psrl_linear_workspace_bytes(dt, m, k, n, 0), x.device, keep, raw)
+        ws, wsb = held.ptr, held.nbytes
+    else:
+        ws, wsb = _use_workspace(workspace, raw, keep, dev)
+    _launch("psrl_linear_fwd", dev, dt, m, k, n, x.data_ptr(), px, None if x_scale is None else x_scale.data_ptr(), weight.data_ptr(), pw,
+            None if weight_scale is None else weight_scale.data_ptr(), None if bias is None else bias.data_ptr(), _ACTIVATIONS[activation],
+            a_mul, p_mul, a_res, p_res, a_y, p_y, a_z, p_z, ws, wsb, raw)
+    return y, z
+
+
+def psrl_linear_bwd(x, weight, d_y, z=None, activation=None, mul=None, d_x=None, d_weight=None, d_bias=None, d_mul=None, want_x: bool = True,
+                    want_weight: bool = True, want_bias: bool = False, want_mul: Optional[bool] = None, stream=None, workspace=None):
+    """Gradients of the above, f32 or bf16: (d_x, d_weight, d_bias, d_mul) given d_y and the forward's z (which may be None without an
+    activation where d_mul is not wanted); what is not wanted is None, d_mul is wanted where there is a mul.  The gradient of residual
+    is d_y.  `workspace` as above (backward True)."""
+    m, k, n = x.shape[0], x.shape[-1], weight.shape[0]
+    dt, m, k, n, dev, out = _linear_args(x, weight, activation, (("d_y", d_y, (m, n)), ("z", z, (m, n)), ("mul", mul, (m, n)), ("d_x", d_x, (m, k)),
+                                                                 ("d_weight", d_weight, (n, k)), ("d_bias", d_bias, (n,)), ("d_mul", d_mul, (m, n))))
+    if dt == PSRL_E4M3:
+        raise TypeError("8-bit operands have no backward")
+    if want_mul is None:
+        want_mul = mul is not None
+    elif want_mul and mul is None:
+        raise ValueError("d_mul without a mul")
+    raw, keep = _stream_on(stream, dev)
+    a_z, p_z = _optional(z, "z")
+    a_mul, p_mul = _optional(mul, "mul")
+    px, pw, pd = _operand_pitch(x, "x"), _operand_pitch(weight, "weight"), _operand_pitch(d_y, "d_y")
+    d_x, a_x, p_x = _matrix(d_x, m, k, out, keep, x.device) if want_x else (None, None, 0)
+    d_weight, a_w, p_w = _matrix(d_weight, n, k, out, keep, x.device) if want_weight else (None, None, 0)
+    d_mul, a_m, p_m = _matrix(d_mul, m, n, out, keep, x.device) if want_mul else (None, None, 0)
+    if not want_bias:
+        d_bias = None
+    elif d_bias is None:
+        d_bias = _new(keep, (n,), out, x.device)
+    if workspace is None:
+        held = Workspace(lib().psrl_linear_workspace_bytes(dt, m, k, n, 1), x.device, keep, raw)
+        ws, wsb = held.ptr, held.nbytes
+    else:
+        ws, wsb = _use_workspace(workspace, raw, keep, dev)
+    _launch("psrl_linear_bwd", dev, dt, m, k, n, x.data_ptr(), px, weight.data_ptr(), pw, a_z, p_z, _ACTIVATIONS[activation], a_mul, p_mul,
+            d_y.data_ptr(), pd, a_x, p_x, a_w, p_w, None if d_bias is None else d_bias.data_ptr(), a_m, p_m, ws, wsb, raw)
+    return d_x, d_weight, d_bias, d_mul
 
 
 def _flags_ptr(seg_flags):

@@ -1,0 +1,835 @@
+// Matrix products of a layer with what follows them in the same kernel, and their gradients.
+//
+//   z = sx[m] sw[n] sum_k x[m, k] w[n, k] + bias[n],   y = act(z) * mul + residual         (forward)
+//   dz = d_y * mul * act'(z),  d_mul = d_y * act(z),  d_bias = sum_m dz                     (one elementwise pass)
+//   d_x = dz w,  d_weight = dz^T x                                                          (one launch for both)
+//
+// The products run on one matrix kernel: tile 256 x 256 (or 128 wide) of a CTA pair (cta_group::2: each CTA holds 128 rows of A and
+// half of B's columns, so a 128-byte deep step brings 32 KB into each SM for 512 tensor cycles), 32 KB stages filled by TMA, two
+// accumulators in tensor memory so that the epilogue of one tile runs under the products of the next, persistent CTAs.
+// Operands lie K-major in the forward; in the gradients the weights, x and, for d_weight, dz lie with the other side contiguous
+// (MN-major), which the descriptors of shared memory take as they are: nothing is transposed in memory.
+// The epilogue's own operands (residual, mul) come through TMA into the buffers that its results leave from.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "../../include/psrl.h"
+#include "attn_bf16_common.cuh"
+#include "kernels.h"
+#include "linear_act.cuh"
+#include "linear_f32.cuh"
+#include "sm100_pair.cuh"
+#include "tma.h"
+
+namespace psrl {
+namespace {
+using namespace sm100;
+
+constexpr int kRowBytes = 128;                 // of an operand in a stage: 64 bf16 or 128 e4m3 deep
+constexpr int kOperandBytes = 128 * kRowBytes; // one CTA's share of A or B in a stage
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kOutBytes = 128 * 128;           // what an epilogue group loads or stores at a time: 128 rows of 128 bytes
+constexpr int kGroups = 2, kEpilogueWarps = 4 * kGroups, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + 1;
+constexpr int kGemmThreads = (kEpilogueWarps + 2) * 32;
+
+// kPlain: results leave through two buffers a group.  kFull: with mul, residual or z, three: one holds the residual and then y, one
+// mul and then z, and one is loaded ahead.
+enum Epilogue { kPlain, kFull };
+constexpr int stages(Epilogue e) { return e == kPlain ? 5 : 4; }
+constexpr int buffers(Epilogue e) { return e == kPlain ? 2 : 3; }
+constexpr size_t gemm_smem(Epilogue e) { return size_t(stages(e)) * kStageBytes + size_t(kGroups) * buffers(e) * kOutBytes + 1024; }
+
+struct Maps {
+  CUtensorMap a[2], b[2], out[2];   // of the products of the launch
+  CUtensorMap mul, residual, z;
+};
+// out [M, N] = A [M, depth] B [N, depth]^T
+struct Product {
+  int32_t M, N, steps;          // steps: of 128 bytes of depth (64 rows of an MN-major operand)
+  int32_t m_tiles, n_tiles, tile_n;
+  int32_t a_mn, b_mn;           // MN-major
+  int32_t group;                // row tiles that are walked together
+};
+struct Params {
+  Product product[2];           // the second one: fewer steps a tile, or empty
+  int32_t ratio;                // tiles of the second that cost one of the first
+  const __nv_bfloat16* bias;
+  const float *x_scale, *w_scale;
+  int32_t act, has_mul, has_residual, has_z;
+  int* status;
+};
+
+template <bool kFp8>
+__device__ __forceinline__ void mma_step(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (kFp8) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], da, db, %4, p;\n\t}" ::"r"(d),
+        "r"(a_lo), "r"(b_lo), "r"(kDescHi), "r"(idesc), "r"(accumulate)
+        : "memory");
+  } else {
+    mma_pair(d, a_lo, b_lo, idesc, accumulate);
+  }
+}
+// e4m3 x e4m3 (format 0 of both operands) -> fp32, both K-major
+__host__ __device__ constexpr uint32_t make_idesc_fp8(int M, int N) { return (1u << 4) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24); }
+
+// Tile `unit` of a product: groups of row tiles, inside a group the row tile moves fastest, so that the CTAs at work share column
+// tiles and a group's rows stay in the L2.
+__device__ __forceinline__ void tile_of(const Product& p, int unit, int& mt, int& nt) {
+  const int per = p.group * p.n_tiles;
+  const int g = unit / per, r = unit - g * per;
+  const int gm = min(p.group, p.m_tiles - g * p.group);
+  nt = r / gm;
+  mt = g * p.group + r - nt * gm;
+}
+
+// What a pair of CTAs does: pair c of C takes the tiles c, c + C, ... of the first product.  The first r pairs then have one more
+// than the others, who make up for it with the first tiles of the second; the rest of those go round.  No counter, no order
+// that could vary.
+struct Schedule {
+  int n_first, n_second, mine, ahead, light;
+  bool lighter;
+  __device__ __forceinline__ Schedule(const Params& p, int c, int C) {
+    n_first = p.product[0].m_tiles * p.product[0].n_tiles;
+    n_second = p.product[1].m_tiles * p.product[1].n_tiles;
+    const int q = n_first / C, r = n_first - q * C;
+    mine = q + (c < r ? 1 : 0);
+    light = C - r;
+    lighter = c >= r;
+    ahead = r > 0 ? min(p.ratio, n_second / light) : 0;
+  }
+  __device__ __forceinline__ bool get(const Params& p, int c, int C, int i, int& which, int& mt, int& nt) const {
+    if (i < mine) {
+      which = 0;
+      tile_of(p.product[0], c + i * C, mt, nt);
+      return true;
+    }
+    const int j = i - mine;
+    int at = ahead * light;
+    if (lighter && j < ahead) at = j * light + c - (C - light);
+    else at += (lighter ? j - ahead : j) * C + c;
+    if (at >= n_second) return false;
+    which = 1;
+    tile_of(p.product[1], at, mt, nt);
+    return true;
+  }
+};
+
+template <int kStages>
+struct __align__(8) Barriers {
+  uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], in[kGroups][3];
+};
+
+// The buffers of an epilogue group.  Use n of them is buffer n % count; thread 0 of the group sees to it that a buffer's last store
+// has been read out before it is loaded or written again.
+constexpr uint32_t kBarGroup = 1, kGroupThreads = 128;   // named barrier 1 + group
+
+__device__ __forceinline__ void put16(uint8_t* b, int row, int chunk, uint4 v) {
+  *reinterpret_cast<uint4*>(b + row * 128 + ((chunk ^ (row & 7)) << 4)) = v;
+}
+__device__ __forceinline__ uint4 get16(const uint8_t* b, int row, int chunk) {
+  return *reinterpret_cast<const uint4*>(b + row * 128 + ((chunk ^ (row & 7)) << 4));
+}
+
+// eight bf16 of a vector that ends at `n`, from column `col`; the same for all threads
+__device__ __forceinline__ void load_bias(const __nv_bfloat16* bias, int col, int n, float (&o)[8]) {
+  if (col + 8 <= n) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(bias + col));
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      o[2 * i] = __uint_as_float(w[i] << 16);
+      o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = col + i < n ? __bfloat162float(bias[col + i]) : 0.f;
+  }
+}
+
+template <bool kFp8, Epilogue kEpilogue>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
+linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  constexpr int kStages = stages(kEpilogue), kBuffers = buffers(kEpilogue);
+  constexpr int kDepth = kFp8 ? 128 : 64;
+  __shared__ Barriers<kStages> bar;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort, s_go[kGroups][2];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_rank();
+  const int cluster = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+
+  if (tid == 0) {
+    s_abort = 0;
+    for (int i = 0; i < kStages; ++i) { mbar_init(&bar.full[i], 1); mbar_init(&bar.empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar.acc_full[i], 1); mbar_init(&bar.acc_empty[i], 8); }   // four warps in either CTA
+    for (int g = 0; g < kGroups; ++g)
+      for (int i = 0; i < 3; ++i) mbar_init(&bar.in[g][i], 1);
+    fence_mbar_init();
+    tma_prefetch_desc(&maps.a[0]);
+    tma_prefetch_desc(&maps.b[0]);
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&s_tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();   // the peer's barriers exist before anything arrives on them
+  tc_fence_after();
+  previous_kernel_done();
+  if (blockIdx.x == 0 && tid == 0) *p.status = int(PSRL_OK);
+
+  const Schedule plan(p, cluster, n_clusters);
+  const uint32_t tmem = s_tmem;
+  volatile int* abortp = &s_abort;
+  int which, mt, nt;
+
+  if (warp == kTmaWarp) {
+    // ======================= TMA producer (both CTAs) =======================
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int i = 0; ok && plan.get(p, cluster, n_clusters, i, which, mt, nt); ++i) {
+        const Product& q = p.product[which];
+        const CUtensorMap *ma = &maps.a[which], *mb = &maps.b[which];
+        const int m0 = mt * 256 + int(rank) * 128, half = q.tile_n / 2, n0 = nt * q.tile_n + int(rank) * half;
+        const uint32_t stage_tx = 2 * (kOperandBytes + uint32_t(half) * kRowBytes);   // of both CTAs
+        for (int kb = 0; kb < q.steps; ++kb, ++it) {
+          const uint32_t s = it % kStages, round = it / kStages;
+          if (round > 0 && !mbar_wait(&bar.empty[s], (round + 1) & 1, abortp, p.status)) { ok = false; break; }
+          // the second CTA's copies count on the first one's barrier as well
+          if (rank == 0) mbar_expect_tx(&bar.full[s], stage_tx);
+          const uint32_t full = in_leader(&bar.full[s]);
+          uint8_t* sa = smem + s * kStageBytes;
+          uint8_t* sb = sa + kOperandBytes;
+          if (q.a_mn) {
+            tma_load_pair(sa, ma, full, m0, kb * kDepth);
+            tma_load_pair(sa + kOperandBytes / 2, ma, full, m0 + 64, kb * kDepth);
+          } else {
+            tma_load_pair(sa, ma, full, kb * kDepth, m0);
+          }
+          if (q.b_mn) {
+            tma_load_pair(sb, mb, full, n0, kb * kDepth);
+            if (half > 64) tma_load_pair(sb + kOperandBytes / 2, mb, full, n0 + 64, kb * kDepth);
+          } else {
+            tma_load_pair(sb, mb, full, kb * kDepth, n0);
+          }
+        }
+      }
+      // the last arrivals on the stages' barriers come from the pair's products: this CTA stays until they are here
+      for (uint32_t i = 0; i < kStages && ok; ++i) {
+        const uint32_t uses = it / kStages + (i < it % kStages ? 1 : 0);
+        if (uses > 0) ok = mbar_wait(&bar.empty[i], (uses + 1) & 1, abortp, p.status);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ======================= MMA issuer (first CTA of the pair) =======================
+    if (rank == 0) {
+      // An MN-major operand's 64-wide blocks are kLbo bytes apart and a 16-deep step is 16 rows of 128 bytes; K-major, a step is 32
+      // bytes (16 bf16 or 32 e4m3).
+      constexpr uint32_t kLbo = kOperandBytes / 2, kStepK = 32 >> 4, kStepMn = 2048 >> 4;
+      const bool elected = elect_one();
+      uint32_t it = 0, tile = 0;
+      bool ok = true;
+      for (int i = 0; ok && plan.get(p, cluster, n_clusters, i, which, mt, nt); ++i, ++tile) {
+        const Product& q = p.product[which];
+        const uint32_t idesc = kFp8 ? make_idesc_fp8(256, q.tile_n) : make_idesc(256, q.tile_n, q.a_mn, q.b_mn);
+        const uint32_t step_a = q.a_mn ? kStepMn : kStepK, lbo_a = q.a_mn ? kLbo : 0;
+        const uint32_t step_b = q.b_mn ? kStepMn : kStepK, lbo_b = q.b_mn ? kLbo : 0;
+        const uint32_t a = tile & 1, use = tile >> 1;
+        if (use > 0) ok = __all_sync(0xffffffffu, mbar_wait(&bar.acc_empty[a], (use + 1) & 1, abortp, p.status));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d = tmem + a * 256;
+        for (int kb = 0; kb < q.steps; ++kb, ++it) {
+          const uint32_t s = it % kStages;
+          if (!mbar_wait_all1(&bar.full[s], (it / kStages) & 1, abortp, p.status)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t sa = smem_u32(smem) + s * kStageBytes, sb = sa + kOperandBytes;
+          const uint32_t da = desc_lo(sa, lbo_a), db = desc_lo(sb, lbo_b);
+          if (elected) {
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) mma_step<kFp8>(d, da + k * step_a, db + k * step_b, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+            commit_pair(&bar.empty[s]);
+          }
+          __syncwarp();
+        }
+        if (ok && elected) commit_pair(&bar.acc_full[a]);
+        __syncwarp();
+      }
+    }
+  } else {
+    // ======================= epilogue: one thread per row, a group for every other tile =======================
+    const int group = warp >> 2, gt = tid & 127;
+    const uint32_t bar_id = kBarGroup + group;
+    const uint32_t lane_addr = tmem + (uint32_t(warp & 3) << 21) + group * 256;   // lane 32 * (warp % 4)
+    const uint32_t acc_empty = in_leader(&bar.acc_empty[group]);
+    uint8_t* buf = smem + kStages * kStageBytes + group * kBuffers * kOutBytes;
+    const bool has_second = kEpilogue == kFull && (p.has_mul || p.has_z);
+    const int per = has_second ? 2 : 1;          // buffers a chunk takes: residual -> y, mul -> z
+    uint32_t base = 0, go = 0;                   // uses of buffers before this tile; hand-overs between the group's warps
+    uint32_t phases = 0;                         // parity that the next load into each buffer completes
+    uint32_t tile = 0;
+    bool ok = true;
+    for (int i = 0; ok && plan.get(p, cluster, n_clusters, i, which, mt, nt); ++i, ++tile) {
+      if ((tile & 1) != uint32_t(group)) continue;
+      const Product& q = p.product[which];
+      const int row0 = mt * 256 + int(rank) * 128, n0 = nt * q.tile_n, n_end = min(n0 + q.tile_n, q.N);
+      const int chunks = row0 < q.M ? (n_end - n0 + 63) / 64 : 0;
+      int issued = 0;
+      // thread 0: loads into the buffers of uses up to `until` of this tile, which are free
+      auto issue = [&](int until) {
+        until = min(until, chunks * per);
+        for (; issued < until; ++issued) {
+          const bool second = per == 2 && (issued & 1);
+          if (kEpilogue == kPlain || !(second ? p.has_mul : p.has_residual)) continue;
+          const int b = int((base + issued) % kBuffers);
+          mbar_expect_tx(&bar.in[group][b], kOutBytes);
+          tma_load_2d(buf + b * kOutBytes, second ? &maps.mul : &maps.residual, &bar.in[group][b], n0 + issued / per * 64, row0);
+        }
+      };
+      if (kEpilogue == kFull && gt == 0) {
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        issue(kBuffers);
+      }
+      // one warp waits for its group: the four leave together if the wait gives up, so none is missed at their barrier
+      if ((warp & 3) == 0) {
+        ok = mbar_wait(&bar.acc_full[group], (tile >> 1) & 1, abortp, p.status);
+        if (lane == 0) s_go[group][go & 1] = ok;
+      }
+      named_sync(bar_id, kGroupThreads);
+      ok = s_go[group][go++ & 1];
+      if (!ok) break;
+      tc_fence_after();
+      const float sx = kFp8 && row0 + gt < q.M ? p.x_scale[row0 + gt] : 1.f;
+#pragma unroll 1
+      for (int c = 0; c < chunks; ++c) {
+        const int col = n0 + c * 64;
+        const uint32_t n = base + uint32_t(c * per);
+        uint32_t r[2][32];
+        tmem_ld32(lane_addr + c * 64, r[0]);
+        tmem_ld32(lane_addr + c * 64 + 32, r[1]);
+        if ((warp & 3) == 0) {
+          if (gt == 0) {
+            // the buffers of this chunk: free, and with their loads under way
+            if (kEpilogue == kPlain) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            else if (issued < (c + 1) * per) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            issue((c + 1) * per);
+          }
+          __syncwarp();
+          if (kEpilogue == kFull) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              if (u >= per || !(u ? p.has_mul : p.has_residual)) continue;
+              const int b = int((n + u) % kBuffers);
+              ok = ok && mbar_wait(&bar.in[group][b], (phases >> b) & 1, abortp, p.status);
+            }
+            ok = __all_sync(0xffffffffu, ok);
+            if (lane == 0) s_go[group][go & 1] = ok;
+          }
+        }
+        tmem_wait_ld();
+        named_sync(bar_id, kGroupThreads);
+        if (kEpilogue == kFull) {
+          ok = s_go[group][go++ & 1];
+          if (!ok) break;
+        }
+        uint8_t* first = buf + int(n % kBuffers) * kOutBytes;
+        uint8_t* second = buf + int((n + 1) % kBuffers) * kOutBytes;
+        if (kEpilogue == kFull) {
+          // complete already; this thread's own look at the barrier orders its reads behind the copies
+          if (p.has_residual) {
+            const int b = int(n % kBuffers);
+            mbar_wait(&bar.in[group][b], (phases >> b) & 1, abortp, p.status);
+            phases ^= 1u << b;
+          }
+          if (p.has_mul) {
+            const int b = int((n + 1) % kBuffers);
+            mbar_wait(&bar.in[group][b], (phases >> b) & 1, abortp, p.status);
+            phases ^= 1u << b;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[j / 4][j % 4 * 8 + e]);
+          const int at = col + j * 8;
+          if constexpr (kFp8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= sx * (at + e < q.N ? __ldg(p.w_scale + at + e) : 0.f);
+          }
+          if (p.bias) {
+            float b[8];
+            load_bias(p.bias, at, q.N, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += b[e];
+          }
+          if constexpr (kEpilogue == kFull) {
+            uint4 mul = make_uint4(0, 0, 0, 0);
+            if (p.has_mul) mul = get16(second, gt, j);
+            if (p.has_z)
+              put16(second, gt, j, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+            activate(v, p.act);
+            if (p.has_mul) {
+              const uint32_t w[4] = {mul.x, mul.y, mul.z, mul.w};
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] *= __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+            }
+            if (p.has_residual) {
+              const uint4 res = get16(first, gt, j);
+              const uint32_t w[4] = {res.x, res.y, res.z, res.w};
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+            }
+          } else {
+            activate(v, p.act);
+          }
+          put16(first, gt, j, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+        }
+        fence_proxy_async();
+        named_sync(bar_id, kGroupThreads);
+        if (gt == 0) {
+          tma_store_2d(&maps.out[which], first, col, row0);
+          if (kEpilogue == kFull && p.has_z) tma_store_2d(&maps.z, second, col, row0);
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          if (kEpilogue == kFull) {
+            // the stores before this chunk's have been read out: the buffers they left are loaded ahead
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            issue(c * per + kBuffers);
+          }
+        }
+      }
+      if (!ok) break;
+      base += uint32_t(chunks * per);
+      // the accumulator may be overwritten
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_leader(acc_empty);
+    }
+    if (gt == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+  // ---- teardown ----
+  __syncthreads();
+  if (s_abort) {
+    // a wait gave up: let copies and products in flight come to rest before the memory they use is given back
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  }
+  tc_fence_before();
+  cluster_sync();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------- elementwise backward
+
+// dz = d_y * mul * act'(z), d_mul = d_y * act(z), and sums over the rows of dz: a block takes 32 vectors of columns and 64 rows (more
+// where there are millions), and leaves its column sums for bias_kernel, which adds them in order.  Memory bound: every element once.
+constexpr int kDzRows = 64;
+template <class T> constexpr int kVec = 16 / int(sizeof(T));
+
+template <class T>
+struct DzParams {
+  const T *d_y, *mul, *z;
+  T *dz, *d_mul;               // NULL: not wanted
+  float* part;                 // [row blocks][N], or NULL
+  int64_t d_y_pitch, mul_pitch, z_pitch, dz_pitch, d_mul_pitch;
+  int32_t M, N, act, rows;     // rows of a block
+  int* status;
+};
+
+template <class T>
+__device__ __forceinline__ void load_vec(const T* at, int left, float (&o)[kVec<T>]) {
+  if (left >= kVec<T>) {
+    const uint4 v = *reinterpret_cast<const uint4*>(at);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        o[i] = __uint_as_float(w[i]);
+      } else {
+        o[2 * i] = __uint_as_float(w[i] << 16);
+        o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) o[i] = i < left ? float(at[i]) : 0.f;
+  }
+}
+template <class T>
+__device__ __forceinline__ void store_vec(T* at, int left, const float (&o)[kVec<T>]) {
+  if (left >= kVec<T>) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(o[i]);
+      else w[i] = pack_bf16(o[2 * i], o[2 * i + 1]);
+    }
+    *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i)
+      if (i < left) at[i] = T(o[i]);
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParams<T> p) {
+  constexpr int kE = kVec<T>;
+  next_kernel_may_start();
+  __shared__ float s_sum[8][32][kE + 1];
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const int64_t col = (int64_t(blockIdx.x) * 32 + tx) * kE;
+  const int left = int(p.N - col < kE ? p.N - col : kE);
+  float sum[kE] = {};
+  if (left > 0) {
+    const int64_t row0 = int64_t(blockIdx.y) * p.rows;
+#pragma unroll 2
+    for (int k = ty; k < p.rows; k += 8) {
+      const int64_t row = row0 + k;
+      if (row >= p.M) break;
+      float g[kE], m[kE], z[kE], d[kE];
+      load_vec(p.d_y + row * p.d_y_pitch + col, left, g);
+      if (p.mul) load_vec(p.mul + row * p.mul_pitch + col, left, m);
+      if (p.z) load_vec(p.z + row * p.z_pitch + col, left, z);
+      if (p.z) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          float value, slope;
+          act_and_slope(z[e], p.act, value, slope);
+          d[e] = g[e] * value;
+          if (p.mul) g[e] *= m[e];
+          g[e] *= slope;
+        }
+      } else if (p.mul) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) g[e] *= m[e];
+      }
+      if (p.d_mul) store_vec(p.d_mul + row * p.d_mul_pitch + col, left, d);
+      if (p.dz) store_vec(p.dz + row * p.dz_pitch + col, left, g);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) sum[e] += g[e];
+    }
+  }
+  if (!p.part) return;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) s_sum[ty][tx][e] = sum[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * kE; i += 256) {
+    const int64_t c = int64_t(blockIdx.x) * 32 * kE + i;
+    if (c >= p.N) break;
+    float s = 0.f;
+    for (int y = 0; y < 8; ++y) s += s_sum[y][i / kE][i % kE];
+    p.part[int64_t(blockIdx.y) * p.N + c] = s;
+  }
+}
+
+// d_bias from the blocks' sums: a block takes 32 columns, 32 threads share the parts of each, in a fixed order.
+template <class T>
+__global__ void __launch_bounds__(1024) bias_kernel(const float* __restrict__ part, int parts, int N, T* __restrict__ d_bias) {
+  previous_kernel_done();
+  next_kernel_may_start();
+  __shared__ float s[32][33];
+  const int c = threadIdx.x & 31, slice = threadIdx.x >> 5;
+  const int64_t col = int64_t(blockIdx.x) * 32 + c;
+  float sum = 0.f;
+  if (col < N)
+    for (int i = slice; i < parts; i += 32) sum += part[int64_t(i) * N + col];
+  s[slice][c] = sum;
+  __syncthreads();
+  sum = s[c][slice];   // thread (slice, c) now has part c of column `slice`
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (c == 0 && int64_t(blockIdx.x) * 32 + slice < N) d_bias[int64_t(blockIdx.x) * 32 + slice] = T(sum);
+}
+
+// ------------------------------------------------------------------------------------------------------------------- host
+
+int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t dz_rows(int64_t M) { return std::max<int64_t>(kDzRows, div_up(M, 65535)); }   // at most 65,535 blocks of rows
+
+// A kernel of a call; all but the first may start before the one before has ended (see previous_kernel_done).
+template <class... P, class... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, bool first, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = first ? 0 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
+template <bool kFp8, Epilogue kEpilogue>
+cudaError_t launch_gemm(const Maps& maps, const Params& p, bool first, cudaStream_t stream) {
+  static bool done[64] = {};
+  cudaError_t e = ensure_dynamic_smem(linear_kernel<kFp8, kEpilogue>, gemm_smem(kEpilogue), done);
+  if (e != cudaSuccess) return e;
+  int64_t tiles = 0;
+  for (const Product& q : p.product) tiles += int64_t(q.m_tiles) * q.n_tiles;
+  if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
+  const int clusters = static_cast<int>(std::min<int64_t>(tiles, resident_ctas() / 2));
+  return launch(linear_kernel<kFp8, kEpilogue>, dim3(2 * clusters), kGemmThreads, gemm_smem(kEpilogue), stream, first, maps, p);
+}
+
+Product product_of(int64_t M, int64_t N, int64_t depth, int64_t step, int tile_n, int a_mn, int b_mn, int64_t group_bytes) {
+  Product q{};
+  q.M = int32_t(M); q.N = int32_t(N); q.steps = int32_t(div_up(depth, step));
+  q.tile_n = tile_n;
+  q.m_tiles = int32_t(div_up(M, 256)); q.n_tiles = int32_t(div_up(N, tile_n));
+  q.a_mn = a_mn; q.b_mn = b_mn;
+  // even groups of at most group_bytes (a row tile is 256 rows of 128 bytes for each step)
+  const int64_t most = std::max<int64_t>(1, group_bytes / (int64_t(q.steps) * 256 * kRowBytes));
+  const int64_t groups = div_up(q.m_tiles, most);
+  q.group = int32_t(div_up(q.m_tiles, groups));
+  return q;
+}
+
+// Rounds of tiles that the pairs of CTAs make, in 256-wide ones; a 128-wide tile costs more than half of one.
+double rounds_of(int64_t M, int64_t N, int tile_n) {
+  const int64_t pairs = std::max(1, resident_ctas() / 2), tiles = div_up(M, 256) * div_up(N, tile_n);
+  return double(div_up(tiles, pairs)) * (tile_n == 256 ? 1.0 : 0.6);
+}
+int tile_of(int64_t M, int64_t N) { return rounds_of(M, N, 128) < rounds_of(M, N, 256) ? 128 : 256; }
+
+constexpr int64_t kGroupBytes = int64_t(36) << 20, kGradGroupBytes = int64_t(16) << 20;
+
+bool al16(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool opt16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool al4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+bool pitch16(int64_t pitch, int64_t cols, int64_t unit) { return pitch >= cols && pitch % unit == 0 && pitch <= (int64_t(1) << 36); }
+bool same_rows(const void* out, int64_t out_pitch, const void* in, int64_t in_pitch, int64_t rows) {
+  return !out || out != in || out_pitch == in_pitch || rows <= 1;
+}
+constexpr int64_t kMost = int64_t(1) << 30;
+// elements of 16 bytes
+int64_t unit_of(psrl_dtype_t t) { return t == PSRL_F32 ? 4 : t == PSRL_BF16 ? 8 : 16; }
+
+psrl_status_t cuda_failed(cudaError_t e) {
+  set_last_cuda_error(e);
+  return PSRL_ERR_CUDA;
+}
+
+psrl_status_t check(psrl_dtype_t t, int64_t M, int32_t K, int32_t N, psrl_activation_t act, const void* x, int64_t xp, const void* weight, int64_t wp) {
+  if (t != PSRL_F32 && t != PSRL_BF16 && t != PSRL_E4M3) return PSRL_ERR_UNSUPPORTED;
+  if (M < 0 || M > kMost || act < PSRL_ACT_NONE || act > PSRL_ACT_GELU_TANH) return PSRL_ERR_INVALID_ARG;
+  if (K < 8 || K % 8 || K > kMost || N < 1 || N > kMost || !pitch16(xp, K, unit_of(t)) || !pitch16(wp, K, unit_of(t))) return PSRL_ERR_SHAPE;
+  if (M > 0 && (!al16(x) || !al16(weight))) return PSRL_ERR_INVALID_ARG;
+  return PSRL_OK;
+}
+
+// Where the backward's workspace holds what: dz unless it is d_y itself, and the column sums' parts.
+struct Layout {
+  size_t dz = 0, part = 0, f32 = 0, total = 0;
+  int64_t dz_pitch = 0;
+};
+Layout layout(psrl_dtype_t t, int64_t M, int64_t K, int64_t N, bool with_dz, bool with_bias) {
+  Layout L;
+  size_t at = kWsHeaderBytes;
+  auto take = [&](size_t bytes) {
+    const size_t a = at;
+    at += (bytes + 255) / 256 * 256;
+    return a;
+  };
+  L.dz_pitch = round_up(N, 8);
+  if (with_dz) L.dz = take(size_t(M) * L.dz_pitch * (t == PSRL_F32 ? 4 : 2));
+  if (with_bias) L.part = take(size_t(div_up(M, dz_rows(M))) * N * sizeof(float));
+  if (t == PSRL_F32) L.f32 = take(std::max(f32_part_bytes(M, K, N), f32_part_bytes(N, K, M)));
+  L.total = at;
+  return L;
+}
+
+template <class T>
+cudaError_t run_dz(const DzParams<T>& p, T* d_bias, cudaStream_t s) {
+  const dim3 grid(unsigned(div_up(p.N, 32 * kVec<T>)), unsigned(div_up(p.M, p.rows)));
+  cudaError_t e = launch(dz_kernel<T>, grid, 256, 0, s, true, p);
+  if (e == cudaSuccess && d_bias)
+    e = launch(bias_kernel<T>, dim3(unsigned(div_up(p.N, 32))), 1024, 0, s, false, p.part, int(grid.y), p.N, d_bias);
+  return e;
+}
+
+}  // namespace
+}  // namespace psrl
+
+extern "C" {
+
+size_t psrl_linear_workspace_bytes(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim, int32_t out_dim, int backward) {
+  using namespace psrl;
+  if (n_rows < 0 || n_rows > kMost || in_dim < 1 || out_dim < 1) return 0;
+  if (n_rows == 0) return kWsHeaderBytes;
+  if (backward) return layout(dtype, n_rows, in_dim, out_dim, true, true).total;
+  return kWsHeaderBytes + (dtype == PSRL_F32 ? f32_part_bytes(n_rows, out_dim, in_dim) : 0);
+}
+
+psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim, int32_t out_dim, const void* x, int64_t x_pitch,
+                              const float* x_scale, const void* weight, int64_t weight_pitch, const float* weight_scale, const void* bias,
+                              psrl_activation_t activation, const void* mul, int64_t mul_pitch, const void* residual,
+                              int64_t residual_pitch, void* y, int64_t y_pitch, void* z, int64_t z_pitch, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  using namespace psrl;
+  psrl_status_t st = check(dtype, n_rows, in_dim, out_dim, activation, x, x_pitch, weight, weight_pitch);
+  if (st != PSRL_OK) return st;
+  const int64_t M = n_rows, N = out_dim, unit = dtype == PSRL_F32 ? 4 : 8;
+  const bool fp8 = dtype == PSRL_E4M3;
+  if ((mul && !pitch16(mul_pitch, N, unit)) || (residual && !pitch16(residual_pitch, N, unit)) || !pitch16(y_pitch, N, unit) || (z && !pitch16(z_pitch, N, unit)))
+    return PSRL_ERR_SHAPE;
+  if (!ptr_aligned(workspace, 256)) return PSRL_ERR_INVALID_ARG;
+  if (workspace_bytes < psrl_linear_workspace_bytes(dtype, n_rows, in_dim, out_dim, 0)) return PSRL_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (M == 0) {
+    const cudaError_t e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);   // otherwise the first kernel clears the status
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
+  if (!al16(y) || !opt16(bias) || !opt16(mul) || !opt16(residual) || !opt16(z) || (z && z == y) || fp8 != (x_scale != nullptr) || fp8 != (weight_scale != nullptr) ||
+      (fp8 && (!al4(x_scale) || !al4(weight_scale))))
+    return PSRL_ERR_INVALID_ARG;
+  for (const void* out : {static_cast<const void*>(y), static_cast<const void*>(z)}) {
+    const int64_t pitch = out == y ? y_pitch : z_pitch;
+    if (!same_rows(out, pitch, mul, mul_pitch, M) || !same_rows(out, pitch, residual, residual_pitch, M)) return PSRL_ERR_INVALID_ARG;
+  }
+  int* status = static_cast<int*>(workspace);
+  if (dtype == PSRL_F32) {
+    F32Params q{};
+    q.a = {static_cast<const float*>(x), x_pitch};
+    q.b = {static_cast<const float*>(weight), weight_pitch};
+    q.M = int32_t(M); q.N = int32_t(N); q.depth = in_dim; q.status = status;
+    q.e = {static_cast<const float*>(bias), static_cast<const float*>(mul), static_cast<const float*>(residual), static_cast<float*>(y), static_cast<float*>(z),
+           mul_pitch, residual_pitch, y_pitch, z_pitch, activation};
+    const cudaError_t e = f32_product<false, false>(q, reinterpret_cast<float*>(static_cast<char*>(workspace) + kWsHeaderBytes), s);
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
+  Maps maps{};
+  Params p{};
+  const int64_t step = fp8 ? 128 : 64;
+  p.product[0] = product_of(M, N, in_dim, step, tile_of(M, N), 0, 0, kGroupBytes);
+  const uint32_t half = uint32_t(p.product[0].tile_n / 2);
+  const bool full = mul || residual || z;
+  bool made = fp8 ? make_map_u8_2d(&maps.a[0], x, in_dim, M, x_pitch, 128) && make_map_u8_2d(&maps.b[0], weight, in_dim, N, weight_pitch, half)
+                  : make_map_bf16_2d(&maps.a[0], x, in_dim, M, x_pitch * 2, 128) && make_map_bf16_2d(&maps.b[0], weight, in_dim, N, weight_pitch * 2, half);
+  made = made && make_map_bf16_2d(&maps.out[0], y, N, M, y_pitch * 2, 128);
+  if (mul) made = made && make_map_bf16_2d(&maps.mul, mul, N, M, mul_pitch * 2, 128);
+  if (residual) made = made && make_map_bf16_2d(&maps.residual, residual, N, M, residual_pitch * 2, 128);
+  if (z) made = made && make_map_bf16_2d(&maps.z, z, N, M, z_pitch * 2, 128);
+  if (!made) return PSRL_ERR_CUDA;
+  p.bias = static_cast<const __nv_bfloat16*>(bias);
+  p.x_scale = x_scale; p.w_scale = weight_scale;
+  p.act = activation;
+  p.has_mul = mul != nullptr; p.has_residual = residual != nullptr; p.has_z = z != nullptr;
+  p.status = status;
+  const cudaError_t e = fp8 ? (full ? launch_gemm<true, kFull>(maps, p, true, s) : launch_gemm<true, kPlain>(maps, p, true, s))
+                            : (full ? launch_gemm<false, kFull>(maps, p, true, s) : launch_gemm<false, kPlain>(maps, p, true, s));
+  return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+}
+
+psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim, int32_t out_dim, const void* x, int64_t x_pitch,
+                              const void* weight, int64_t weight_pitch, const void* z, int64_t z_pitch, psrl_activation_t activation,
+                              const void* mul, int64_t mul_pitch, const void* d_y, int64_t d_y_pitch, void* d_x, int64_t d_x_pitch,
+                              void* d_weight, int64_t d_weight_pitch, void* d_bias, void* d_mul, int64_t d_mul_pitch, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  using namespace psrl;
+  psrl_status_t st = check(dtype, n_rows, in_dim, out_dim, activation, x, x_pitch, weight, weight_pitch);
+  if (st != PSRL_OK) return st;
+  if (dtype == PSRL_E4M3) return PSRL_ERR_UNSUPPORTED;
+  const int64_t M = n_rows, N = out_dim, K = in_dim, unit = unit_of(dtype);
+  const size_t es = dtype == PSRL_F32 ? 4 : 2;
+  if (!pitch16(d_y_pitch, N, unit) || (z && !pitch16(z_pitch, N, unit)) || (mul && !pitch16(mul_pitch, N, unit)) || (d_mul && !pitch16(d_mul_pitch, N, unit)) ||
+      (d_x && !pitch16(d_x_pitch, K, unit)) || (d_weight && !pitch16(d_weight_pitch, K, unit)))
+    return PSRL_ERR_SHAPE;
+  if (!ptr_aligned(workspace, 256) || !opt16(d_x) || !opt16(d_weight) || !opt16(d_bias)) return PSRL_ERR_INVALID_ARG;
+  const bool elementwise = activation != PSRL_ACT_NONE || mul;
+  Layout L;
+  L.total = kWsHeaderBytes;
+  if (M > 0) L = layout(dtype, M, K, N, elementwise, d_bias != nullptr);
+  if (workspace_bytes < L.total) return PSRL_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  char* ws = static_cast<char*>(workspace);
+  if (M == 0) {
+    e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+    if (e == cudaSuccess && d_weight) e = cudaMemset2DAsync(d_weight, size_t(d_weight_pitch) * es, 0, size_t(K) * es, size_t(N), s);
+    if (e == cudaSuccess && d_bias) e = cudaMemsetAsync(d_bias, 0, size_t(N) * es, s);
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
+  if (!al16(d_y) || !opt16(z) || !opt16(mul) || !opt16(d_mul) || (activation != PSRL_ACT_NONE && !z) || (d_mul && (!mul || !z)) ||
+      !same_rows(d_mul, d_mul_pitch, d_y, d_y_pitch, M) || !same_rows(d_mul, d_mul_pitch, mul, mul_pitch, M) || !same_rows(d_mul, d_mul_pitch, z, z_pitch, M))
+    return PSRL_ERR_INVALID_ARG;
+  int* status = static_cast<int*>(workspace);
+  bool first = true;
+  const void* dz = d_y;
+  int64_t dz_pitch = d_y_pitch;
+  if (elementwise || d_bias) {
+    if (elementwise && (d_x || d_weight)) { dz = ws + L.dz; dz_pitch = L.dz_pitch; }
+    auto run = [&](auto zero) {
+      using T = decltype(zero);
+      DzParams<T> q{};
+      q.d_y = static_cast<const T*>(d_y); q.d_y_pitch = d_y_pitch;
+      q.mul = static_cast<const T*>(mul); q.mul_pitch = mul_pitch;
+      q.z = activation != PSRL_ACT_NONE || d_mul ? static_cast<const T*>(z) : nullptr; q.z_pitch = z_pitch;
+      q.d_mul = static_cast<T*>(d_mul); q.d_mul_pitch = d_mul_pitch;
+      q.dz = dz == d_y ? nullptr : reinterpret_cast<T*>(ws + L.dz); q.dz_pitch = dz_pitch;
+      q.part = d_bias ? reinterpret_cast<float*>(ws + L.part) : nullptr;
+      q.M = int32_t(M); q.N = int32_t(N); q.act = activation; q.rows = int32_t(dz_rows(M)); q.status = status;
+      return run_dz(q, static_cast<T*>(d_bias), s);
+    };
+    e = dtype == PSRL_F32 ? run(float()) : run(__nv_bfloat16());
+    if (e != cudaSuccess) return cuda_failed(e);
+    first = false;
+  }
+  if (!d_x && !d_weight) {
+    if (first) e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
+  if (dtype == PSRL_F32) {
+    const F32Operand z_at{static_cast<const float*>(dz), dz_pitch}, x_at{static_cast<const float*>(x), x_pitch}, w_at{static_cast<const float*>(weight), weight_pitch};
+    float* part = reinterpret_cast<float*>(ws + L.f32);
+    auto params = [&](F32Operand a, F32Operand b, int64_t rows, int64_t depth, void* out, int64_t pitch) {
+      F32Params q{};
+      q.a = a; q.b = b;
+      q.M = int32_t(rows); q.N = int32_t(K); q.depth = int32_t(depth); q.status = status;
+      q.e.y = static_cast<float*>(out); q.e.y_pitch = pitch;
+      return q;
+    };
+    if (d_x) e = f32_product<false, true>(params(z_at, w_at, M, N, d_x, d_x_pitch), part, s);
+    if (e == cudaSuccess && d_weight) e = f32_product<true, true>(params(z_at, x_at, N, M, d_weight, d_weight_pitch), part, s);
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
+  // the deeper product first: its tiles cost more
+  const int tile_x = 256, tile_w = 256;
+  Product px = product_of(M, K, N, 64, tile_x, 0, 1, kGradGroupBytes), pw = product_of(N, K, M, 64, tile_w, 1, 1, kGradGroupBytes);
+  if (!d_x) px.m_tiles = 0;
+  if (!d_weight) pw.m_tiles = 0;
+  const int ix = !d_x || (d_weight && pw.steps > px.steps) ? 1 : 0, iw = 1 - ix;
+  Maps maps{};
+  Params p{};
+  p.product[ix] = px;
+  p.product[iw] = pw;
+  p.ratio = (p.product[0].steps + 6) / std::max(p.product[1].steps + 6, 1);
+  p.status = status;
+  bool made = true;
+  if (d_x)
+    made = make_map_bf16_2d(&maps.a[ix], dz, N, M, dz_pitch * 2, 128) && make_map_bf16_2d(&maps.b[ix], weight, K, N, weight_pitch * 2, 64) &&
+           make_map_bf16_2d(&maps.out[ix], d_x, K, M, d_x_pitch * 2, 128);
+  if (made && d_weight)
+    made = make_map_bf16_2d(&maps.a[iw], dz, N, M, dz_pitch * 2, 64) && make_map_bf16_2d(&maps.b[iw], x, K, M, x_pitch * 2, 64) &&
+           make_map_bf16_2d(&maps.out[iw], d_weight, K, N, d_weight_pitch * 2, 128);
+  if (!made) return PSRL_ERR_CUDA;
+  e = launch_gemm<false, kPlain>(maps, p, first, s);
+  return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+}
+
+}  // extern "C"

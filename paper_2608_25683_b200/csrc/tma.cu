@@ -94,5 +94,8 @@ bool make_map_f32_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t
                      uint32_t box_rows) {
   return make_map(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 32, base, cols, rows, pitch_bytes, box_rows);
 }
+bool make_map_u8_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes, uint32_t box_rows) {
+  return make_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 128, base, cols, rows, pitch_bytes, box_rows);
+}
 
 }  // namespace psrl

@@ -17,4 +17,7 @@ bool make_map_bf16_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_
 bool make_map_f32_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes,
                      uint32_t box_rows);
 
+// The same for 8-bit elements, boxes of box_rows x 128 columns.
+bool make_map_u8_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t pitch_bytes, uint32_t box_rows);
+
 }  // namespace psrl
