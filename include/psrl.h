@@ -400,7 +400,8 @@ psrl_status_t psrl_rope_axes_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, c
  *            d_summed NULL: none; summed (read only with a residual), y, codes, d_x NULL: not wanted
  *   weight, d_weight [dim] DEVICE of `dtype`; weight NULL: ones (d_weight must be NULL then); d_weight NULL: not wanted
  *   codes    [n_rows, n_heads, dim] DEVICE e4m3, codes_pitch a multiple of 16;  scales [n_rows * n_heads] DEVICE fp32, with codes
- *   workspace  DEVICE, 256-byte aligned, >= 256 bytes, with d_weight >= psrl_rms_norm_workspace_bytes; holds the device status word
+ *   workspace  DEVICE, 256-byte aligned, with d_weight >= psrl_rms_norm_workspace_bytes; holds the device status word.  Without d_weight
+ *            256 bytes, or NULL
  * An output may be one of the call's inputs (equal pitches); otherwise tensors are apart.  dim a multiple of 8, 8..32768;
  * pointers 16-byte aligned (scales 4), pitches a multiple of 16 bytes and at least a row; eps > 0.
  * n_rows = 0 does nothing (backward: zeroes d_weight).
@@ -438,7 +439,8 @@ psrl_status_t psrl_quantize_rows(psrl_dtype_t dtype, int64_t n_rows, int32_t dim
  *   d_y, d_x, d_weight, d_bias, d_mul  as their tensors; the outputs NULL: not wanted.  E4M3 has no backward
  *   workspace  DEVICE, 256-byte aligned, of psrl_linear_workspace_bytes; holds the device status word.  Forward 256 bytes; backward dz
  *              (n_rows rows of out_dim in whole 8s) and a number for each column and 64 rows, neither needed where there is no
- *              activation, mul or d_bias that asks for it; F32: with few rows or columns the sums of parts of the depth, below 20 MB
+ *              activation, mul or d_bias that asks for it; F32: with few rows or columns the sums of parts of the depth, below 20 MB.
+ *              NULL where 256 bytes would do: the status of the waits inside is then not kept
  * y and z may be mul or residual, d_mul may be d_y, mul or z (equal pitches); otherwise tensors are apart.  in_dim is a multiple of 8,
  * out_dim any; pitches are multiples of 16 bytes and at least a row, pointers 16-byte aligned (scales 4).  Dimensions are at most 2^30.
  * n_rows = 0 does nothing (backward: zeroes d_weight and d_bias).

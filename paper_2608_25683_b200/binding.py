@@ -581,6 +581,25 @@ def _cuda():
     return _torch_c
 
 
+_torch_module = None
+
+
+def _torch():
+    """torch, looked up once."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+
+        _torch_module = torch
+    return _torch_module
+
+
+def _scratch(nbytes: int, keep, device):
+    """(address, bytes, tensor that holds them until the call is on its stream) of a call's own workspace."""
+    buf = _new(keep, nbytes + 256, _torch().uint8, device)
+    return (buf.data_ptr() + 255) // 256 * 256, nbytes, buf
+
+
 _type_codes = None
 
 
@@ -955,58 +974,60 @@ def _stream_rows(t, shape, name: str, like=None) -> int:
     """Row pitch of a [rows, dim] or [rows, heads, dim] tensor of `shape`, of the type and on the device of `like`."""
     if t.shape != shape or (like is not None and (t.dtype is not like.dtype or t.get_device() != like.get_device())):
         raise ValueError(f"{name} must be {tuple(shape)}" + (f" of {like.dtype} on {like.device}" if like is not None else ""))
+    if t.is_contiguous():
+        return shape[1] if len(shape) == 2 else shape[1] * shape[2]
     if len(shape) == 2:
         return _matrix_pitch(t, name)
     return _rows_pitch(t, shape[0], shape[1], shape[2], name)
 
 
+def _like(t, keep):
+    """A contiguous tensor of t's shape, type and device, made for a call."""
+    return _torch().empty_like(t) if keep is None and t.is_contiguous() else _new(keep, t.shape, t.dtype, t.device)
+
+
 def _norm_args(x, weight):
-    """(type, rows, heads, dim) of the rows to be normed; weight fits them."""
+    """(type, rows, heads, dim, device) of the rows to be normed; weight fits them."""
     dt, shape = _type_code(x), x.shape
     if dt is None:
         raise TypeError(f"dtype {x.dtype} is neither float32 nor bfloat16")
-    if len(shape) not in (2, 3):
+    if len(shape) == 2:
+        (rows, dim), heads = shape, 1
+    elif len(shape) == 3:
+        rows, heads, dim = shape
+    else:
         raise ValueError("rows must be [rows, dim] or [rows, heads, dim]")
-    if weight is not None:
-        if weight.dtype is not x.dtype:
-            raise TypeError(f"weight is {weight.dtype}, the rows are {x.dtype}")
-        if weight.shape != shape[-1:] or not weight.is_contiguous():
-            raise ValueError(f"weight must be a contiguous vector of {shape[-1]}")
-    return dt, shape[0], shape[1] if len(shape) == 3 else 1, shape[-1]
+    if weight is None:
+        return dt, rows, heads, dim, _device_of(x)
+    if weight.dtype is not x.dtype:
+        raise TypeError(f"weight is {weight.dtype}, the rows are {x.dtype}")
+    if weight.shape != shape[-1:] or not weight.is_contiguous():
+        raise ValueError(f"weight must be a contiguous vector of {dim}")
+    return dt, rows, heads, dim, _device_of(x, weight)
 
 
-_e4m3 = None
-
-
-def _codes_type():
-    global _e4m3
-    if _e4m3 is None:
-        import torch
-
-        _e4m3 = torch.float8_e4m3fn
-    return _e4m3
-
-
-def _codes_rows(codes, shape, keep, device, name="codes"):
+def _codes_rows(codes, shape, keep, like, name="codes"):
     """(tensor of 8-bit codes of `shape`, row pitch), made if not given: rows 16 bytes or a multiple apart."""
     rows, least = shape[0], shape[1] if len(shape) == 2 else shape[1] * shape[2]
     pitch = -(-least // 16) * 16
     if codes is None:
-        codes = _new(keep, (rows, pitch) if pitch != least else shape, _codes_type(), device)
-        return (codes if pitch == least else codes[:, :least].unflatten(1, shape[1:]) if len(shape) == 3 else codes[:, :least]), pitch
-    if codes.dtype is not _codes_type() or codes.get_device() != device.index:
-        raise ValueError(f"{name} must be float8_e4m3fn on {device}")
+        if pitch == least:
+            if keep is None and like.is_contiguous():
+                return _torch().empty_like(like, dtype=_torch().float8_e4m3fn), pitch
+            return _new(keep, shape, _torch().float8_e4m3fn, like.device), pitch
+        codes = _new(keep, (rows, pitch), _torch().float8_e4m3fn, like.device)[:, :least]
+        return codes.unflatten(1, shape[1:]) if len(shape) == 3 else codes, pitch
+    if codes.dtype is not _torch().float8_e4m3fn or codes.get_device() != like.get_device():
+        raise ValueError(f"{name} must be float8_e4m3fn on {like.device}")
     at = _stream_rows(codes, shape, name)
     return codes, at if rows > 1 else pitch
 
 
 def _floats(t, shape, keep, device, name):
     """A contiguous float32 tensor of `shape`, made if not given."""
-    import torch
-
     if t is None:
-        return _new(keep, shape, torch.float32, device)
-    if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous() or t.get_device() != device.index:
+        return _new(keep, shape, _torch().float32, device)
+    if t.dtype is not _torch().float32 or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be contiguous float32 {tuple(shape)} on {device}")
     return t
 
@@ -1016,16 +1037,15 @@ def psrl_rms_norm_fwd(x, weight, eps: float = 1e-6, residual=None, y=None, summe
     """Root-mean-square norm of h = x + residual: x [rows, dim], or [rows, heads, dim] with a norm for each head (f32 or bf16, rows
     at any pitch), weight [dim] or None.  Returns (y, summed, codes, scales): summed = h where there is a residual, codes and scales
     the rows in 8 bits (float8_e4m3fn, a float32 scale for each) with want_codes; what is not wanted is None.  Outputs may be inputs."""
-    dt, rows, heads, dim = _norm_args(x, weight)
-    shape = x.shape
-    dev = _device_of(x) if weight is None else _device_of(x, weight)
+    dt, rows, heads, dim, dev = _norm_args(x, weight)
+    shape, least = x.shape, heads * dim
     raw, keep = _stream_on(stream, dev)
     px = _stream_rows(x, shape, "x")
     a_res, p_res, a_sum, p_sum, a_y, p_y, a_c, p_c, a_s = None, 0, None, 0, None, 0, None, 0, None
     if residual is not None:
         a_res, p_res = residual.data_ptr(), _stream_rows(residual, shape, "residual", x)
         if summed is None:
-            summed, p_sum = _new(keep, shape, x.dtype, x.device), heads * dim
+            summed, p_sum = _like(x, keep), least
         else:
             p_sum = _stream_rows(summed, shape, "summed", x)
         a_sum = summed.data_ptr()
@@ -1033,13 +1053,14 @@ def psrl_rms_norm_fwd(x, weight, eps: float = 1e-6, residual=None, y=None, summe
         raise ValueError("summed without a residual: x itself is the stream")
     if not want_y:
         y = None
-    elif y is None:
-        y, p_y = _new(keep, shape, x.dtype, x.device), heads * dim
-        a_y = y.data_ptr()
     else:
-        a_y, p_y = y.data_ptr(), _stream_rows(y, shape, "y", x)
+        if y is None:
+            y, p_y = _like(x, keep), least
+        else:
+            p_y = _stream_rows(y, shape, "y", x)
+        a_y = y.data_ptr()
     if want_codes:
-        codes, p_c = _codes_rows(codes, shape, keep, x.device)
+        codes, p_c = _codes_rows(codes, shape, keep, x)
         scales = _floats(scales, shape[:-1], keep, x.device, "scales")
         a_c, a_s = codes.data_ptr(), scales.data_ptr()
     else:
@@ -1058,9 +1079,8 @@ def psrl_rms_norm_bwd(summed, weight, d_y, eps: float = 1e-6, d_summed=None, d_x
     """Gradients of the above: (d_x, d_weight) given the rows h that were normed (the forward's `summed`, or its x), d_y and, with a
     residual, the gradient d_summed that the stream brings back; d_x is the gradient of x and of residual.  d_x may be d_y or
     d_summed.  `workspace`: a Workspace of psrl_rms_norm_workspace_bytes(); made if not given."""
-    dt, rows, heads, dim = _norm_args(summed, weight)
+    dt, rows, heads, dim, dev = _norm_args(summed, weight)
     shape = summed.shape
-    dev = _device_of(summed, d_y) if weight is None else _device_of(summed, d_y, weight)
     raw, keep = _stream_on(stream, dev)
     ph, pd = _stream_rows(summed, shape, "summed"), _stream_rows(d_y, shape, "d_y", summed)
     a_s, p_s, a_x, p_x = None, 0, None, 0
@@ -1070,19 +1090,20 @@ def psrl_rms_norm_bwd(summed, weight, d_y, eps: float = 1e-6, d_summed=None, d_x
         d_x = None
     else:
         if d_x is None:
-            d_x, p_x = _new(keep, shape, summed.dtype, summed.device), heads * dim
+            d_x, p_x = _like(summed, keep), heads * dim
         else:
             p_x = _stream_rows(d_x, shape, "d_x", summed)
         a_x = d_x.data_ptr()
     if not want_weight or weight is None:
         d_weight = None
     elif d_weight is None:
-        d_weight = _new(keep, weight.shape, weight.dtype, weight.device)
+        d_weight = _like(weight, keep)
     elif d_weight.dtype is not weight.dtype or d_weight.shape != weight.shape or not d_weight.is_contiguous() or d_weight.get_device() != dev:
         raise ValueError(f"d_weight must be a contiguous vector of {dim}, {weight.dtype} on {weight.device}")
     if workspace is None:
-        held = Workspace(lib().psrl_rms_norm_workspace_bytes(dt, rows, heads, dim), summed.device, keep, raw)
-        ws, wsb = held.ptr, held.nbytes
+        ws, wsb, held = None, 0, None
+        if d_weight is not None:
+            ws, wsb, held = _scratch((_lib or lib()).psrl_rms_norm_workspace_bytes(dt, rows, heads, dim), keep, summed.device)
     else:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
     _launch("psrl_rms_norm_bwd", dev, dt, rows, heads, dim, summed.data_ptr(), ph, None if weight is None else weight.data_ptr(), eps,
@@ -1092,13 +1113,12 @@ def psrl_rms_norm_bwd(summed, weight, d_y, eps: float = 1e-6, d_summed=None, d_x
 
 def psrl_quantize_rows(x, codes=None, scales=None, stream=None):
     """Rows x [rows, dim] (f32 or bf16) in 8 bits: (codes float8_e4m3fn [rows, dim], scales float32 [rows])."""
-    dt, rows, heads, dim = _norm_args(x, None)
+    dt, rows, heads, dim, dev = _norm_args(x, None)
     if x.dim() != 2:
         raise ValueError("x must be [rows, dim]")
-    dev = _device_of(x)
     raw, keep = _stream_on(stream, dev)
     px = _matrix_pitch(x, "x")
-    codes, pc = _codes_rows(codes, x.shape, keep, x.device)
+    codes, pc = _codes_rows(codes, x.shape, keep, x)
     scales = _floats(scales, x.shape[:1], keep, x.device, "scales")
     _launch("psrl_quantize_rows", dev, dt, rows, dim, x.data_ptr(), px, codes.data_ptr(), pc, scales.data_ptr(), raw)
     return codes, scales
@@ -1107,13 +1127,13 @@ def psrl_quantize_rows(x, codes=None, scales=None, stream=None):
 _ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 
 
-def _linear_args(x, weight, activation, others):
+def _linear_args(x, weight, activation):
     """(type, rows, in_dim, out_dim, device, the outputs' type) with what the two directions check alike."""
-    dt = _type_code(x)
+    dt, out = _type_code(x), x.dtype
     if dt is None:
-        if x.dtype is not _codes_type():
+        if out is not _torch().float8_e4m3fn:
             raise TypeError(f"dtype {x.dtype} is none of float32, bfloat16, float8_e4m3fn")
-        dt = PSRL_E4M3
+        dt, out = PSRL_E4M3, _torch().bfloat16
     if weight.dtype is not x.dtype:
         raise TypeError(f"weight is {weight.dtype}, x is {x.dtype}")
     xs, ws = x.shape, weight.shape
@@ -1121,40 +1141,48 @@ def _linear_args(x, weight, activation, others):
         raise ValueError("x must be [rows, in_dim], weight [out_dim, in_dim]")
     if activation not in _ACTIVATIONS:
         raise ValueError(f"activation {activation!r} unknown")
-    out = x.dtype
-    if dt == PSRL_E4M3:
-        import torch
-
-        out = torch.bfloat16
-    dev = _device_of(x, weight)
-    for name, t, shape in others:
-        if t is None:
-            continue
-        if t.dtype is not out or t.get_device() != dev or t.shape != shape:
-            raise ValueError(f"{name} must be {out} {tuple(shape)} on {x.device}")
-        if len(shape) == 1 and shape[0] > 1 and t.stride(0) != 1:
-            raise ValueError(f"{name} must be contiguous")
-    return dt, xs[0], xs[1], ws[0], dev, out
+    return dt, xs[0], xs[1], ws[0], _device_of(x, weight), out
 
 
 def _operand_pitch(t, name: str) -> int:
     """Row pitch of a matrix operand; a lone row has any that will do."""
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: the elements of a row must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16
+    rows, cols = t.shape
+    if rows > 1:
+        pitch, step = t.stride()
+        if step == 1 or cols == 1:
+            return pitch
+    elif cols == 1 or t.stride(1) == 1:
+        return -(-cols // 16) * 16
+    raise ValueError(f"{name}: the elements of a row must be contiguous")
 
 
-def _matrix(t, rows: int, cols: int, dtype, keep, device):
-    """A [rows, cols] output, made if not given with rows that are whole 16-byte vectors apart, its address and row pitch."""
+def _beside(t, rows: int, cols: int, dtype, dev: int, name: str):
+    """(address, row pitch) of a [rows, cols] matrix beside the operands, (None, 0) without one."""
     if t is None:
-        pitch = -(-cols // 8) * 8
-        t = _new(keep, (rows, pitch), dtype, device)
-        return (t if pitch == cols else t[:, :cols]), t.data_ptr(), pitch
-    return t, t.data_ptr(), _operand_pitch(t, "output")
+        return None, 0
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != (rows, cols):
+        raise ValueError(f"{name} must be {dtype} {(rows, cols)} on cuda:{dev}")
+    return t.data_ptr(), _operand_pitch(t, name)
 
 
-def _optional(t, name: str):
-    return (None, 0) if t is None else (t.data_ptr(), _operand_pitch(t, name))
+def _beside_vector(t, count: int, dtype, dev: int, name: str):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != (count,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} {(count,)} on cuda:{dev}")
+    return t.data_ptr()
+
+
+def _result(t, rows: int, cols: int, dtype, keep, like, name: str):
+    """A [rows, cols] output, made if not given with rows that are whole 16-byte vectors apart, its address and row pitch."""
+    if t is not None:
+        return (t, *_beside(t, rows, cols, dtype, like.get_device(), name))
+    pitch = -(-cols // 8) * 8
+    if keep is None and dtype is like.dtype:
+        t = like.new_empty((rows, pitch))
+    else:
+        t = _new(keep, (rows, pitch), dtype, like.device)
+    return (t if pitch == cols else t[:, :cols]), t.data_ptr(), pitch
 
 
 def psrl_linear_workspace_bytes(n_rows: int, in_dim: int, out_dim: int, backward: bool, dtype: str = "bf16") -> int:
@@ -1169,30 +1197,30 @@ def psrl_linear_fwd(x, weight, bias=None, activation=None, mul=None, residual=No
     "gelu", "gelu_tanh".  Returns (y, z), z = x weight^T + bias with want_z (for the backward), else None.  y and z may be mul or
     residual.  `workspace`: a Workspace of psrl_linear_workspace_bytes(), whose status() tells whether a wait inside the kernel gave
     up; made if not given."""
-    m, n = x.shape[0], weight.shape[0]
-    dt, m, k, n, dev, out = _linear_args(x, weight, activation, (("bias", bias, (n,)), ("mul", mul, (m, n)), ("residual", residual, (m, n)), ("y", y, (m, n)),
-                                                                 ("z", z, (m, n))))
-    for name, t, count in (("x_scale", x_scale, m), ("weight_scale", weight_scale, n)):
-        if (t is not None) != (dt == PSRL_E4M3):
-            raise ValueError(f"{name}: 8-bit operands have scales, others none")
-        if t is not None:
-            _floats(t, (count,), None, x.device, name)
+    dt, m, k, n, dev, out = _linear_args(x, weight, activation)
+    if dt == PSRL_E4M3:
+        if x_scale is None or weight_scale is None:
+            raise ValueError("8-bit operands come with x_scale and weight_scale")
+        a_xs = _beside_vector(x_scale, m, _torch().float32, dev, "x_scale")
+        a_ws = _beside_vector(weight_scale, n, _torch().float32, dev, "weight_scale")
+    elif x_scale is not None or weight_scale is not None:
+        raise ValueError("x_scale and weight_scale belong to 8-bit operands")
+    else:
+        a_xs = a_ws = None
     raw, keep = _stream_on(stream, dev)
-    a_mul, p_mul = _optional(mul, "mul")
-    a_res, p_res = _optional(residual, "residual")
+    a_mul, p_mul = _beside(mul, m, n, out, dev, "mul")
+    a_res, p_res = _beside(residual, m, n, out, dev, "residual")
+    a_bias = _beside_vector(bias, n, out, dev, "bias")
     px, pw = _operand_pitch(x, "x"), _operand_pitch(weight, "weight")
-    y, a_y, p_y = _matrix(y, m, n, out, keep, x.device)
-    if want_z:
-        z, a_z, p_z = _matrix(z, m, n, out, keep, x.device)
-    else:
-        z, a_z, p_z = None, None, 0
-    if workspace is None:
-        held = Workspace(lib().psrl_linear_workspace_bytes(dt, m, k, n, 0), x.device, keep, raw)
-        ws, wsb = held.ptr, held.nbytes
-    else:
+    y, a_y, p_y = _result(y, m, n, out, keep, x, "y")
+    z, a_z, p_z = _result(z, m, n, out, keep, x, "z") if want_z else (None, None, 0)
+    if workspace is not None:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
-    _launch("psrl_linear_fwd", dev, dt, m, k, n, x.data_ptr(), px, None if x_scale is None else x_scale.data_ptr(), weight.data_ptr(), pw,
-            None if weight_scale is None else weight_scale.data_ptr(), None if bias is None else bias.data_ptr(), _ACTIVATIONS[activation],
+    elif dt == PSRL_F32:
+        ws, wsb, held = _scratch((_lib or lib()).psrl_linear_workspace_bytes(dt, m, k, n, 0), keep, x.device)
+    else:
+        ws, wsb = None, 0
+    _launch("psrl_linear_fwd", dev, dt, m, k, n, x.data_ptr(), px, a_xs, weight.data_ptr(), pw, a_ws, a_bias, _ACTIVATIONS[activation],
             a_mul, p_mul, a_res, p_res, a_y, p_y, a_z, p_z, ws, wsb, raw)
     return y, z
 
@@ -1202,9 +1230,7 @@ def psrl_linear_bwd(x, weight, d_y, z=None, activation=None, mul=None, d_x=None,
     """Gradients of the above, f32 or bf16: (d_x, d_weight, d_bias, d_mul) given d_y and the forward's z (which may be None without an
     activation where d_mul is not wanted); what is not wanted is None, d_mul is wanted where there is a mul.  The gradient of residual
     is d_y.  `workspace` as above (backward True)."""
-    m, k, n = x.shape[0], x.shape[-1], weight.shape[0]
-    dt, m, k, n, dev, out = _linear_args(x, weight, activation, (("d_y", d_y, (m, n)), ("z", z, (m, n)), ("mul", mul, (m, n)), ("d_x", d_x, (m, k)),
-                                                                 ("d_weight", d_weight, (n, k)), ("d_bias", d_bias, (n,)), ("d_mul", d_mul, (m, n))))
+    dt, m, k, n, dev, out = _linear_args(x, weight, activation)
     if dt == PSRL_E4M3:
         raise TypeError("8-bit operands have no backward")
     if want_mul is None:
@@ -1212,23 +1238,26 @@ def psrl_linear_bwd(x, weight, d_y, z=None, activation=None, mul=None, d_x=None,
     elif want_mul and mul is None:
         raise ValueError("d_mul without a mul")
     raw, keep = _stream_on(stream, dev)
-    a_z, p_z = _optional(z, "z")
-    a_mul, p_mul = _optional(mul, "mul")
-    px, pw, pd = _operand_pitch(x, "x"), _operand_pitch(weight, "weight"), _operand_pitch(d_y, "d_y")
-    d_x, a_x, p_x = _matrix(d_x, m, k, out, keep, x.device) if want_x else (None, None, 0)
-    d_weight, a_w, p_w = _matrix(d_weight, n, k, out, keep, x.device) if want_weight else (None, None, 0)
-    d_mul, a_m, p_m = _matrix(d_mul, m, n, out, keep, x.device) if want_mul else (None, None, 0)
+    a_d, p_d = _beside(d_y, m, n, out, dev, "d_y")
+    a_z, p_z = _beside(z, m, n, out, dev, "z")
+    a_mul, p_mul = _beside(mul, m, n, out, dev, "mul")
+    px, pw = _operand_pitch(x, "x"), _operand_pitch(weight, "weight")
+    d_x, a_x, p_x = _result(d_x, m, k, out, keep, x, "d_x") if want_x else (None, None, 0)
+    d_weight, a_w, p_w = _result(d_weight, n, k, out, keep, x, "d_weight") if want_weight else (None, None, 0)
+    d_mul, a_m, p_m = _result(d_mul, m, n, out, keep, x, "d_mul") if want_mul else (None, None, 0)
     if not want_bias:
         d_bias = None
     elif d_bias is None:
-        d_bias = _new(keep, (n,), out, x.device)
-    if workspace is None:
-        held = Workspace(lib().psrl_linear_workspace_bytes(dt, m, k, n, 1), x.device, keep, raw)
-        ws, wsb = held.ptr, held.nbytes
-    else:
+        d_bias = x.new_empty((n,)) if keep is None else _new(keep, (n,), out, x.device)
+    a_bias = _beside_vector(d_bias, n, out, dev, "d_bias")
+    if workspace is not None:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
+    elif activation not in (None, "none") or mul is not None or want_bias or dt == PSRL_F32:
+        ws, wsb, held = _scratch((_lib or lib()).psrl_linear_workspace_bytes(dt, m, k, n, 1), keep, x.device)
+    else:
+        ws, wsb = None, 0
     _launch("psrl_linear_bwd", dev, dt, m, k, n, x.data_ptr(), px, weight.data_ptr(), pw, a_z, p_z, _ACTIVATIONS[activation], a_mul, p_mul,
-            d_y.data_ptr(), pd, a_x, p_x, a_w, p_w, None if d_bias is None else d_bias.data_ptr(), a_m, p_m, ws, wsb, raw)
+            a_d, p_d, a_x, p_x, a_w, p_w, a_bias, a_m, p_m, ws, wsb, raw)
     return d_x, d_weight, d_bias, d_mul
 
 

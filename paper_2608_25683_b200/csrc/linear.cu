@@ -183,7 +183,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
   cluster_sync();   // the peer's barriers exist before anything arrives on them
   tc_fence_after();
   previous_kernel_done();
-  if (blockIdx.x == 0 && tid == 0) *p.status = int(PSRL_OK);
+  if (p.status && blockIdx.x == 0 && tid == 0) *p.status = int(PSRL_OK);
 
   const Schedule plan(p, cluster, n_clusters);
   const uint32_t tmem = s_tmem;
@@ -429,6 +429,231 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
   }
 }
 
+// ------------------------------------------------------------------------------------------------------------- few rows
+
+// Few rows (the next tokens of rollouts): bound by the weights' bytes, which have to come in on all SMs at once.  The operands change
+// places: 128 columns of the result (rows of the weight) are the tile's rows, up to kFewRows rows of x its columns, so that the tensor
+// cores' work is no more than the rows need; and the depth is shared by a cluster of CTAs, which add their sums through one
+// another's shared memory in the order of their ranks: one launch, no sums in memory, no atomics.
+constexpr int kFewRows = 128;                  // rows of x in a tile at most
+constexpr int kFewThreads = 6 * 32, kFewTma = 4, kFewMma = 5;
+constexpr int kFewMaxStages = 12, kFewMaxSplit = 8;
+
+struct FewMaps {
+  CUtensorMap a, b;
+};
+struct FewParams {
+  int32_t rows, cols;          // of the result
+  int32_t steps, col_tiles, tile_rows;   // tile_rows: rows of x in a tile, a multiple of 16
+  int32_t a_mn;                // the weight lies with the result's columns contiguous (d_x)
+  int32_t stages, splits, tmem_cols;
+  const __nv_bfloat16 *bias, *mul, *residual;
+  const float *x_scale, *w_scale;
+  __nv_bfloat16 *y, *z;
+  int64_t mul_pitch, residual_pitch, y_pitch, z_pitch;
+  int32_t act;
+  int* status;
+};
+
+__device__ __forceinline__ float4 load_cluster(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+// four bf16 at a multiple of four columns, or the `left` ones that there are
+__device__ __forceinline__ void load4(const __nv_bfloat16* at, int left, float (&o)[4]) {
+  if (left >= 4) {
+    const uint2 v = *reinterpret_cast<const uint2*>(at);
+    o[0] = __uint_as_float(v.x << 16); o[1] = __uint_as_float(v.x & 0xffff0000u);
+    o[2] = __uint_as_float(v.y << 16); o[3] = __uint_as_float(v.y & 0xffff0000u);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = e < left ? __bfloat162float(at[e]) : 0.f;
+  }
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* at, int left, const float (&v)[4]) {
+  if (left >= 4) {
+    *reinterpret_cast<uint2*>(at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) at[e] = __float2bfloat16_rn(v[e]);
+  }
+}
+__device__ __forceinline__ uint32_t in_rank(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  return a;
+}
+template <bool kFp8>
+__device__ __forceinline__ void mma_few(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (kFp8) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n\t}" ::"r"(d),
+        "r"(a_lo), "r"(b_lo), "r"(kDescHi), "r"(idesc), "r"(accumulate)
+        : "memory");
+  } else {
+    mma_ss_lo(d, a_lo, b_lo, idesc, accumulate);
+  }
+}
+
+template <bool kFp8>
+__global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ FewParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  constexpr int kDepth = kFp8 ? 128 : 64;
+  __shared__ __align__(8) uint64_t full[kFewMaxStages], empty[kFewMaxStages], acc_full;
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = p.splits > 1 ? cluster_rank() : 0;
+  const int tile = int(blockIdx.x) / p.splits;
+  const int row_tile = tile / p.col_tiles, col0 = (tile - row_tile * p.col_tiles) * 128, row0 = row_tile * p.tile_rows;
+  const int kb0 = int(int64_t(p.steps) * rank / p.splits), kb1 = int(int64_t(p.steps) * (rank + 1) / p.splits);
+  const uint32_t b_bytes = uint32_t(p.tile_rows) * kRowBytes, stage_bytes = kOperandBytes + b_bytes;
+
+  if (threadIdx.x == 0) {
+    s_abort = 0;
+    for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
+    mbar_init(&acc_full, 1);
+    fence_mbar_init();
+  }
+  if (warp == kFewMma) {
+    tmem_alloc(&s_tmem, uint32_t(p.tmem_cols));
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  volatile int* abortp = &s_abort;
+  previous_kernel_done();
+  if (p.status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
+
+  if (warp == kFewTma) {
+    if (lane == 0) {
+      for (int kb = kb0, s = 0, round = 0; kb < kb1; ++kb) {
+        if (round > 0 && !mbar_wait(&empty[s], (round + 1) & 1, abortp, p.status)) break;
+        uint8_t* sa = smem + s * stage_bytes;
+        mbar_expect_tx(&full[s], stage_bytes);
+        if (p.a_mn) {
+          tma_load_2d(sa, &maps.a, &full[s], col0, kb * kDepth);
+          tma_load_2d(sa + kOperandBytes / 2, &maps.a, &full[s], col0 + 64, kb * kDepth);
+        } else {
+          tma_load_2d(sa, &maps.a, &full[s], kb * kDepth, col0);
+        }
+        tma_load_2d(sa + kOperandBytes, &maps.b, &full[s], kb * kDepth, row0);
+        if (++s == p.stages) { s = 0; ++round; }
+      }
+    }
+  } else if (warp == kFewMma) {
+    constexpr uint32_t kLbo = kOperandBytes / 2, kStepK = 32 >> 4, kStepMn = 2048 >> 4;
+    const bool elected = elect_one();
+    const uint32_t idesc = kFp8 ? make_idesc_fp8(128, p.tile_rows) : make_idesc(128, p.tile_rows, p.a_mn, 0);
+    const uint32_t step_a = p.a_mn ? kStepMn : kStepK, lbo_a = p.a_mn ? kLbo : 0;
+    bool ok = true;
+    for (int kb = kb0, s = 0, round = 0; kb < kb1; ++kb) {
+      if (!mbar_wait_all1(&full[s], round & 1, abortp, p.status)) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t sa = smem_u32(smem) + s * stage_bytes;
+      const uint32_t da = desc_lo(sa, lbo_a), db = desc_lo(sa + kOperandBytes, 0);
+      if (elected) {
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) mma_few<kFp8>(tmem, da + k * step_a, db + k * kStepK, idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+        mma_commit(&empty[s]);
+      }
+      __syncwarp();
+      if (++s == p.stages) { s = 0; ++round; }
+    }
+    if (ok && elected) mma_commit(&acc_full);
+    __syncwarp();
+    // all products are done before the stages' memory takes the sums (and before this CTA leaves)
+    if (ok) mbar_wait(&acc_full, 0, abortp, p.status);
+  } else {
+    mbar_wait(&acc_full, 0, abortp, p.status);
+    tc_fence_after();
+  }
+  __syncthreads();
+  const int rows = min(p.tile_rows, p.rows - row0);
+  float* sums = reinterpret_cast<float*>(smem);   // [tile_rows][128]
+  if (warp < 4) {
+    const uint32_t lane_addr = tmem + (uint32_t(warp) << 21);
+    for (int c0 = 0; c0 < rows; c0 += 16) {
+      uint32_t r[16];
+      tmem_ld16(lane_addr + c0, r);
+      tmem_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sums[(c0 + i) * 128 + threadIdx.x] = __uint_as_float(r[i]);
+    }
+  }
+  if (p.splits > 1) cluster_sync();
+  else __syncthreads();
+  // Row r belongs to rank r % splits: a warp takes two of the rank's rows at a time, a lane four columns of each.
+  const int col = col0 + lane * 4, left = p.cols - col;
+  if (left > 0 && !s_abort) {
+    float bias[4] = {}, scale[4] = {1.f, 1.f, 1.f, 1.f};
+    if (p.bias) load4(p.bias + col, left, bias);
+    if constexpr (kFp8) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) scale[e] = e < left ? p.w_scale[col + e] : 0.f;
+    }
+    constexpr int kRowsAtOnce = 2, kWarps = kFewThreads / 32;
+    for (int r0 = int(rank) + p.splits * warp; r0 < rows; r0 += p.splits * kWarps * kRowsAtOnce) {
+      float v[kRowsAtOnce][4], mul[kRowsAtOnce][4], res[kRowsAtOnce][4], sx[kRowsAtOnce];
+#pragma unroll
+      for (int i = 0; i < kRowsAtOnce; ++i) {
+        const int r = r0 + i * p.splits * kWarps;
+        if (r >= rows) break;
+        const int64_t row = row0 + r;
+        if (p.mul) load4(p.mul + row * p.mul_pitch + col, left, mul[i]);
+        if (p.residual) load4(p.residual + row * p.residual_pitch + col, left, res[i]);
+        if constexpr (kFp8) sx[i] = p.x_scale[row];
+        const uint32_t at = smem_u32(sums + r * 128 + lane * 4);
+        float4 part[kFewMaxSplit];
+#pragma unroll
+        for (int k = 0; k < kFewMaxSplit; ++k)
+          if (k < p.splits) part[k] = p.splits > 1 ? load_cluster(in_rank(at, uint32_t(k))) : *reinterpret_cast<const float4*>(sums + r * 128 + lane * 4);
+        v[i][0] = part[0].x; v[i][1] = part[0].y; v[i][2] = part[0].z; v[i][3] = part[0].w;
+#pragma unroll
+        for (int k = 1; k < kFewMaxSplit; ++k)
+          if (k < p.splits) { v[i][0] += part[k].x; v[i][1] += part[k].y; v[i][2] += part[k].z; v[i][3] += part[k].w; }
+      }
+#pragma unroll
+      for (int i = 0; i < kRowsAtOnce; ++i) {
+        const int r = r0 + i * p.splits * kWarps;
+        if (r >= rows) break;
+        const int64_t row = row0 + r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (kFp8) v[i][e] *= sx[i] * scale[e];
+          if (p.bias) v[i][e] += bias[e];
+        }
+        if (p.z) store4(p.z + row * p.z_pitch + col, left, v[i]);
+        activate(v[i], p.act);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (p.mul) v[i][e] *= mul[i][e];
+          if (p.residual) v[i][e] += res[i][e];
+        }
+        store4(p.y + row * p.y_pitch + col, left, v[i]);
+      }
+    }
+  }
+  if (p.splits > 1) cluster_sync();   // the others are done with this CTA's sums
+  tc_fence_before();
+  __syncthreads();
+  if (s_abort) {
+    // a wait gave up: let copies and products in flight come to rest before the memory they use is given back
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  }
+  if (warp == kFewMma) {
+    tc_fence_after();
+    tmem_dealloc(tmem, uint32_t(p.tmem_cols));
+  }
+}
+
 // ------------------------------------------------------------------------------------------------- elementwise backward
 
 // dz = d_y * mul * act'(z), d_mul = d_y * act(z), and sums over the rows of dz: a block takes 32 vectors of columns and 64 rows (more
@@ -607,6 +832,55 @@ double rounds_of(int64_t M, int64_t N, int tile_n) {
 }
 int tile_of(int64_t M, int64_t N) { return rounds_of(M, N, 128) < rounds_of(M, N, 256) ? 128 : 256; }
 
+// How a product of few rows is shared out: the CTAs of a cluster that split its depth, and stages of memory.
+struct FewShape {
+  int tile_rows, stages, splits;
+  int64_t col_tiles, row_tiles;
+  size_t smem;
+};
+FewShape few_shape(int64_t rows, int64_t cols, int64_t steps) {
+  FewShape f{};
+  f.row_tiles = div_up(rows, kFewRows);
+  f.tile_rows = int(round_up(div_up(rows, f.row_tiles), 16));
+  f.col_tiles = div_up(cols, 128);
+  const int64_t tiles = f.row_tiles * f.col_tiles, sms = resident_ctas();
+  const size_t stage = kOperandBytes + size_t(f.tile_rows) * kRowBytes;
+  // two CTAs an SM, so that one's loads run under the other's beginning and end
+  const size_t room = 111 * 1024;
+  f.stages = int(std::min<size_t>(kFewMaxStages, room / stage));
+  f.splits = 1;
+  while (f.splits < kFewMaxSplit && tiles * f.splits * 2 <= 2 * sms && steps / (f.splits * 2) >= 4) f.splits *= 2;
+  f.smem = std::max(size_t(f.stages) * stage, size_t(f.tile_rows) * 128 * sizeof(float)) + 1024;
+  return f;
+}
+bool few_better(int64_t rows, int64_t cols) { return rows <= kFewRows; }
+
+template <bool kFp8>
+cudaError_t launch_few(const FewMaps& maps, FewParams& p, const FewShape& f, bool first, cudaStream_t stream) {
+  static bool done[64] = {};
+  cudaError_t e = ensure_dynamic_smem(linear_few_kernel<kFp8>, 113 * 1024, done);
+  if (e != cudaSuccess) return e;
+  p.col_tiles = int32_t(f.col_tiles);
+  p.tile_rows = f.tile_rows; p.stages = f.stages; p.splits = f.splits;
+  p.tmem_cols = f.tile_rows <= 32 ? 32 : f.tile_rows <= 64 ? 64 : 128;
+  const int64_t blocks = f.row_tiles * f.col_tiles * f.splits;
+  if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(unsigned(blocks));
+  cfg.blockDim = dim3(kFewThreads);
+  cfg.dynamicSmemBytes = f.smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2]{};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(f.splits);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = first ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, linear_few_kernel<kFp8>, maps, p);
+}
+
 constexpr int64_t kGroupBytes = int64_t(36) << 20, kGradGroupBytes = int64_t(16) << 20;
 
 bool al16(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -688,10 +962,12 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
   const bool fp8 = dtype == PSRL_E4M3;
   if ((mul && !pitch16(mul_pitch, N, unit)) || (residual && !pitch16(residual_pitch, N, unit)) || !pitch16(y_pitch, N, unit) || (z && !pitch16(z_pitch, N, unit)))
     return PSRL_ERR_SHAPE;
-  if (!ptr_aligned(workspace, 256)) return PSRL_ERR_INVALID_ARG;
-  if (workspace_bytes < psrl_linear_workspace_bytes(dtype, n_rows, in_dim, out_dim, 0)) return PSRL_ERR_WORKSPACE;
+  const size_t need = psrl_linear_workspace_bytes(dtype, n_rows, in_dim, out_dim, 0);
+  if (workspace ? !ptr_aligned(workspace, 256) : need > kWsHeaderBytes) return PSRL_ERR_INVALID_ARG;
+  if (workspace && workspace_bytes < need) return PSRL_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (M == 0) {
+    if (!workspace) return PSRL_OK;
     const cudaError_t e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);   // otherwise the first kernel clears the status
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
@@ -713,9 +989,26 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     const cudaError_t e = f32_product<false, false>(q, reinterpret_cast<float*>(static_cast<char*>(workspace) + kWsHeaderBytes), s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
+  const int64_t step = fp8 ? 128 : 64;
+  using Bf = __nv_bfloat16;
+  if (few_better(M, N)) {
+    const FewShape f = few_shape(M, N, div_up(in_dim, step));
+    FewMaps maps;
+    const bool made = fp8 ? make_map_u8_2d(&maps.a, weight, in_dim, N, weight_pitch, 128) && make_map_u8_2d(&maps.b, x, in_dim, M, x_pitch, f.tile_rows)
+                          : make_map_bf16_2d(&maps.a, weight, in_dim, N, weight_pitch * 2, 128) && make_map_bf16_2d(&maps.b, x, in_dim, M, x_pitch * 2, f.tile_rows);
+    if (!made) return PSRL_ERR_CUDA;
+    FewParams q{};
+    q.rows = int32_t(M); q.cols = int32_t(N); q.steps = int32_t(div_up(in_dim, step));
+    q.bias = static_cast<const Bf*>(bias); q.mul = static_cast<const Bf*>(mul); q.residual = static_cast<const Bf*>(residual);
+    q.x_scale = x_scale; q.w_scale = weight_scale;
+    q.y = static_cast<Bf*>(y); q.z = static_cast<Bf*>(z);
+    q.mul_pitch = mul_pitch; q.residual_pitch = residual_pitch; q.y_pitch = y_pitch; q.z_pitch = z_pitch;
+    q.act = activation; q.status = status;
+    const cudaError_t e = fp8 ? launch_few<true>(maps, q, f, true, s) : launch_few<false>(maps, q, f, true, s);
+    return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
   Maps maps{};
   Params p{};
-  const int64_t step = fp8 ? 128 : 64;
   p.product[0] = product_of(M, N, in_dim, step, tile_of(M, N), 0, 0, kGroupBytes);
   const uint32_t half = uint32_t(p.product[0].tile_n / 2);
   const bool full = mul || residual || z;
@@ -750,17 +1043,18 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
   if (!pitch16(d_y_pitch, N, unit) || (z && !pitch16(z_pitch, N, unit)) || (mul && !pitch16(mul_pitch, N, unit)) || (d_mul && !pitch16(d_mul_pitch, N, unit)) ||
       (d_x && !pitch16(d_x_pitch, K, unit)) || (d_weight && !pitch16(d_weight_pitch, K, unit)))
     return PSRL_ERR_SHAPE;
-  if (!ptr_aligned(workspace, 256) || !opt16(d_x) || !opt16(d_weight) || !opt16(d_bias)) return PSRL_ERR_INVALID_ARG;
+  if (!opt16(d_x) || !opt16(d_weight) || !opt16(d_bias)) return PSRL_ERR_INVALID_ARG;
   const bool elementwise = activation != PSRL_ACT_NONE || mul;
   Layout L;
   L.total = kWsHeaderBytes;
   if (M > 0) L = layout(dtype, M, K, N, elementwise, d_bias != nullptr);
-  if (workspace_bytes < L.total) return PSRL_ERR_WORKSPACE;
+  if (workspace ? !ptr_aligned(workspace, 256) : L.total > kWsHeaderBytes) return PSRL_ERR_INVALID_ARG;
+  if (workspace && workspace_bytes < L.total) return PSRL_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   char* ws = static_cast<char*>(workspace);
   if (M == 0) {
-    e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+    if (workspace) e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
     if (e == cudaSuccess && d_weight) e = cudaMemset2DAsync(d_weight, size_t(d_weight_pitch) * es, 0, size_t(K) * es, size_t(N), s);
     if (e == cudaSuccess && d_bias) e = cudaMemsetAsync(d_bias, 0, size_t(N) * es, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
@@ -791,7 +1085,7 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     first = false;
   }
   if (!d_x && !d_weight) {
-    if (first) e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
+    if (first && workspace) e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
   if (dtype == PSRL_F32) {
@@ -807,6 +1101,19 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     if (d_x) e = f32_product<false, true>(params(z_at, w_at, M, N, d_x, d_x_pitch), part, s);
     if (e == cudaSuccess && d_weight) e = f32_product<true, true>(params(z_at, x_at, N, M, d_weight, d_weight_pitch), part, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
+  }
+  if (d_x && few_better(M, K)) {
+    const FewShape f = few_shape(M, K, div_up(N, 64));
+    FewMaps maps;
+    if (!make_map_bf16_2d(&maps.a, weight, K, N, weight_pitch * 2, 64) || !make_map_bf16_2d(&maps.b, dz, N, M, dz_pitch * 2, f.tile_rows)) return PSRL_ERR_CUDA;
+    FewParams q{};
+    q.rows = int32_t(M); q.cols = int32_t(K); q.steps = int32_t(div_up(N, 64)); q.a_mn = 1;
+    q.y = static_cast<__nv_bfloat16*>(d_x); q.y_pitch = d_x_pitch; q.status = status;
+    e = launch_few<false>(maps, q, f, first, s);
+    if (e != cudaSuccess) return cuda_failed(e);
+    if (!d_weight) return PSRL_OK;
+    first = false;
+    d_x = nullptr;
   }
   // the deeper product first: its tiles cost more
   const int tile_x = 256, tile_w = 256;

@@ -543,12 +543,13 @@ psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_he
   if (!pitch_ok(summed_pitch, least, unit) || !pitch_ok(d_y_pitch, least, unit) || (d_summed && !pitch_ok(d_summed_pitch, least, unit)) ||
       (d_x && !pitch_ok(d_x_pitch, least, unit)))
     return PSRL_ERR_SHAPE;
-  if (!ptr_aligned(workspace, 256) || (d_weight && (!weight || !tensor_ok(d_weight)))) return PSRL_ERR_INVALID_ARG;
+  const size_t need = d_weight ? psrl_rms_norm_workspace_bytes(dtype, n_rows, n_heads, dim) : kWsHeaderBytes;
+  if ((d_weight && (!weight || !tensor_ok(d_weight))) || (workspace ? !ptr_aligned(workspace, 256) : need > kWsHeaderBytes)) return PSRL_ERR_INVALID_ARG;
+  if (workspace && workspace_bytes < need) return PSRL_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const size_t es = dtype == PSRL_BF16 ? 2 : 4;
   if (n_rows == 0) {
-    cudaError_t e = workspace_bytes < kWsHeaderBytes ? cudaSuccess : cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
-    if (workspace_bytes < kWsHeaderBytes) return PSRL_ERR_WORKSPACE;
+    cudaError_t e = workspace ? cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s) : cudaSuccess;
     if (e == cudaSuccess && d_weight) e = cudaMemsetAsync(d_weight, 0, size_t(dim) * es, s);
     return done(e);
   }
@@ -556,7 +557,6 @@ psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_he
       !same_rows(d_x, d_x_pitch, summed, summed_pitch, n_rows) || !same_rows(d_x, d_x_pitch, d_y, d_y_pitch, n_rows) ||
       !same_rows(d_x, d_x_pitch, d_summed, d_summed_pitch, n_rows))
     return PSRL_ERR_INVALID_ARG;
-  if (workspace_bytes < (d_weight ? psrl_rms_norm_workspace_bytes(dtype, n_rows, n_heads, dim) : kWsHeaderBytes)) return PSRL_ERR_WORKSPACE;
   float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kWsHeaderBytes);
   BwdParams p{summed, weight, d_y, d_summed, d_x, d_weight ? part : nullptr, static_cast<int*>(workspace), summed_pitch, d_y_pitch, d_summed_pitch,
               d_x_pitch, n_rows * n_heads, n_heads, int32_t(dim / unit), 1.f / float(dim), eps};

@@ -52,19 +52,19 @@ def test_refusals(lib):
     for bad in (dict(dt=3), dict(dt=-1)):
         assert fwd(**bad) == "PSRL_ERR_UNSUPPORTED"
     for bad in (dict(m=-1), dict(m=2 ** 31), dict(act=5), dict(act=-1), dict(x=None), dict(x=p + 8), dict(w=None), dict(w=q + 2), dict(y=None), dict(y=r + 4),
-                dict(b=u + 8), dict(mul=u + 2, mp=24), dict(res=u + 2, rp=24), dict(z=u + 8, zp=24), dict(z=r, zp=24), dict(work=None), dict(work=t + 128),
+                dict(b=u + 8), dict(mul=u + 2, mp=24), dict(res=u + 2, rp=24), dict(z=u + 8, zp=24), dict(z=r, zp=24), dict(dt=0, m=2, k=4096, xp=4096, wp=4096, work=None), dict(work=t + 128),
                 dict(xs=u), dict(ws=u), dict(dt=2), dict(dt=2, xs=u), dict(dt=2, xs=u, ws=v + 2), dict(res=r, rp=32), dict(mul=r, mp=32), dict(mul=u, mp=24, z=u, zp=32)):
         assert fwd(**bad) == "PSRL_ERR_INVALID_ARG", bad
     for bad in (dict(k=60), dict(k=0), dict(k=4), dict(n=0), dict(n=-8), dict(xp=56), dict(xp=68), dict(wp=48), dict(yp=16), dict(yp=28), dict(mul=u, mp=16),
                 dict(res=u, rp=30), dict(z=u, zp=0), dict(dt=2, xs=u, ws=u, xp=72), dict(n=2 ** 31 - 1)):
         assert fwd(**bad) == "PSRL_ERR_SHAPE", bad
-    assert fwd(wb=255) == "PSRL_ERR_WORKSPACE"
+    assert fwd(wb=255) == "PSRL_ERR_WORKSPACE" and fwd(m=0, work=None, wb=0) == "PSRL_OK"
     bwd = lambda **k: name(L.psrl_linear_bwd(*{**dict(dt=1, m=2, k=64, n=24, x=p, xp=64, w=q, wp=64, z=None, zp=0, act=0, mul=None, mp=0, dy=r, dyp=24, dx=t, dxp=64,
                                                       dw=u, dwp=64, db=None, dm=None, dmp=0, work=v, wb=1 << 12, stream=None), **k}.values()))
     for bad in (dict(dt=2), dict(dt=7)):
         assert bwd(**bad) == "PSRL_ERR_UNSUPPORTED"
     for bad in (dict(act=2), dict(dm=r, dmp=24), dict(dm=r, dmp=24, mul=p, mp=24), dict(dm=r, dmp=24, z=p, zp=24), dict(dy=None), dict(dy=r + 4), dict(dx=t + 2),
-                dict(dw=u + 2), dict(db=u + 2), dict(z=p + 2, zp=24), dict(work=v + 4), dict(m=-1), dict(mul=p, mp=24, z=q, zp=24, dm=r, dmp=32)):
+                dict(dw=u + 2), dict(db=u + 2), dict(z=p + 2, zp=24), dict(work=v + 4), dict(work=None, db=p), dict(work=None, act=1, z=p, zp=24), dict(m=-1), dict(mul=p, mp=24, z=q, zp=24, dm=r, dmp=32)):
         assert bwd(**bad) == "PSRL_ERR_INVALID_ARG", bad
     for bad in (dict(dyp=20), dict(dxp=56), dict(dwp=60), dict(z=p, zp=8), dict(mul=p, mp=28), dict(k=12)):
         assert bwd(**bad) == "PSRL_ERR_SHAPE", bad

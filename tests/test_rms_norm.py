@@ -55,6 +55,7 @@ def test_refusals(lib):
     bwd = lambda **k: name(L.psrl_rms_norm_bwd(*{**dict(dt=0, n=2, heads=1, dim=64, h=p, hp=64, w=q, eps=1e-6, dy=r, dyp=64, ds=None, dsp=0, dx=t, dxp=64,
                                                         dw=q + 4096, ws=p + 32768, wsb=1 << 14, stream=None), **k}.values()))
     assert bwd(wsb=256 + 256 - 1) == bwd(wsb=0, dw=None) == bwd(n=0, wsb=255, dw=None) == "PSRL_ERR_WORKSPACE"
+    assert bwd(n=0, ws=None, wsb=0, dw=None) == "PSRL_OK"
     assert bwd(dt=5) == "PSRL_ERR_UNSUPPORTED"
     for bad in (dict(h=None), dict(dy=None), dict(ws=None), dict(ws=p + 32768 + 16), dict(w=None), dict(dw=q + 4098), dict(eps=0.0), dict(dx=r, dxp=72),
                 dict(dx=p, dxp=128), dict(ds=t, dsp=68)):
