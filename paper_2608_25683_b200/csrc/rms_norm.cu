@@ -104,9 +104,10 @@ __device__ __forceinline__ float join(float v, Op op, float* s) {
     constexpr int kWarps = kGroup / 32;
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = s[threadIdx.x & (kWarps - 1)];
+    v = (threadIdx.x & 31) < kWarps ? s[threadIdx.x & 31] : 0.f;   // sums and sizes: zero changes nothing
 #pragma unroll
-    for (int o = kWarps / 2; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int o = kWarps > 16 ? 16 : kWarps > 8 ? 8 : kWarps > 4 ? 4 : 2; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+    v = __shfl_sync(0xffffffffu, v, 0);
   }
   return v;
 }
@@ -121,12 +122,14 @@ __device__ __forceinline__ float2 join_sums(float2 v, float2* s) {
     constexpr int kWarps = kGroup / 32;
     if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = s[threadIdx.x & (kWarps - 1)];
+    v = (threadIdx.x & 31) < kWarps ? s[threadIdx.x & 31] : make_float2(0.f, 0.f);
 #pragma unroll
-    for (int o = kWarps / 2; o > 0; o >>= 1) {
+    for (int o = kWarps > 16 ? 16 : kWarps > 8 ? 8 : kWarps > 4 ? 4 : 2; o > 0; o >>= 1) {
       v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
       v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
     }
+    v.x = __shfl_sync(0xffffffffu, v.x, 0);
+    v.y = __shfl_sync(0xffffffffu, v.y, 0);
   }
   return v;
 }
@@ -136,7 +139,7 @@ __device__ __forceinline__ float2 join_sums(float2 v, float2* s) {
 constexpr float kSmall = 0x1p-80f;
 __device__ __forceinline__ bool too_large(float sum) { return !(sum <= FLT_MAX); }
 
-constexpr int threads_of(int group) { return group > 256 ? group : group > 32 ? group : 256; }
+constexpr int threads_of(int group) { return group > 32 ? group : 256; }
 
 // Row i of rows x heads, in vectors of the matrix at `pitch` elements a row.
 template <class T>
@@ -144,7 +147,19 @@ __device__ __forceinline__ int64_t vec_at(int64_t row, int head, int64_t pitch, 
   return row * (pitch / kElems<T>) + int64_t(head) * vecs;
 }
 
+// A row's vectors of one matrix, zeros where there are none.
 template <class T, int kGroup, int kVecs>
+__device__ __forceinline__ void load_row(uint4 (&v)[kVecs], const void* base, int64_t pitch, int64_t row, int head, int vecs, bool live) {
+  const uint4* at = static_cast<const uint4*>(base) + vec_at<T>(row, head, pitch, vecs);
+  const int lane = threadIdx.x % kGroup;
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    v[k] = make_uint4(0, 0, 0, 0);
+    if (live && lane + k * kGroup < vecs) v[k] = at[lane + k * kGroup];
+  }
+}
+
+template <class T, int kGroup, int kVecs, bool kCodes>
 __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __grid_constant__ FwdParams p) {
   constexpr int kE = kElems<T>, kPerBlock = threads_of(kGroup) / kGroup;
   __shared__ float s_sum[2][3][32];   // two rows in a row use two
@@ -157,26 +172,28 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __gri
     if (p.weight && v < p.vecs) w[k] = static_cast<const uint4*>(p.weight)[v];
   }
   int turn = 0;
+  const int64_t stride = int64_t(gridDim.x) * kPerBlock;
+  int64_t i = int64_t(blockIdx.x) * kPerBlock + group, row = 0;
+  int head = 0;
+  uint4 xv[kVecs], rv[kVecs];
+  auto load = [&](int64_t at) {
+    const bool live = at < p.rows;
+    row = p.heads == 1 ? at : at / p.heads;
+    head = p.heads == 1 ? 0 : int(at - row * p.heads);
+    load_row<T, kGroup, kVecs>(xv, p.x, p.x_pitch, row, head, p.vecs, live);
+    if (p.residual) load_row<T, kGroup, kVecs>(rv, p.residual, p.residual_pitch, row, head, p.vecs, live);
+  };
+  constexpr bool kAhead = kGroup < 1024;   // beyond that registers are short
+  if (kAhead) load(i);
   // all threads of a warp take part in its shuffles: a group without a row of its own goes along with the others
-  for (int64_t i0 = int64_t(blockIdx.x) * kPerBlock; i0 < p.rows; i0 += int64_t(gridDim.x) * kPerBlock, turn ^= 1) {
-    const int64_t i = i0 + group;
+  for (; i - group < p.rows; i += stride, turn ^= 1) {
+    if (!kAhead) load(i);
     const bool live = i < p.rows;
-    const int64_t row = p.heads == 1 ? i : i / p.heads;
-    const int head = p.heads == 1 ? 0 : int(i - row * p.heads);
-    const uint4* x = static_cast<const uint4*>(p.x) + vec_at<T>(row, head, p.x_pitch, p.vecs);
-    const uint4* res = static_cast<const uint4*>(p.residual) + vec_at<T>(row, head, p.residual_pitch, p.vecs);
-    uint4 xv[kVecs], rv[kVecs];
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int v = lane + k * kGroup;
-      xv[k] = rv[k] = make_uint4(0, 0, 0, 0);
-      if (live && v < p.vecs) {
-        xv[k] = x[v];
-        if (p.residual) rv[k] = res[v];
-      }
-    }
+    const int64_t this_row = row;
+    const int this_head = head;
+    uint4 hv[kVecs];
     if (p.residual) {
-      uint4* to = static_cast<uint4*>(p.summed) + vec_at<T>(row, head, p.summed_pitch, p.vecs);
+      uint4* to = static_cast<uint4*>(p.summed) + vec_at<T>(this_row, this_head, p.summed_pitch, p.vecs);
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
         float a[kE], b[kE];
@@ -184,18 +201,22 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __gri
         widen<T>(rv[k], b);
 #pragma unroll
         for (int e = 0; e < kE; ++e) a[e] += b[e];
-        xv[k] = narrow<T>(a);
+        hv[k] = narrow<T>(a);
         const int v = lane + k * kGroup;
-        if (p.summed && live && v < p.vecs) to[v] = xv[k];
+        if (p.summed && live && v < p.vecs) to[v] = hv[k];
       }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) hv[k] = xv[k];
     }
+    if (kAhead) load(i + stride);   // the next row is on its way while this one is summed and stored
     float r = 1.f;
     if (p.norm) {
       float sum = 0.f;
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
         float h[kE];
-        widen<T>(xv[k], h);
+        widen<T>(hv[k], h);
 #pragma unroll
         for (int e = 0; e < kE; ++e) sum = fmaf(h[e], h[e], sum);
       }
@@ -206,7 +227,7 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __gri
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) {
           float h[kE];
-          widen<T>(xv[k], h);
+          widen<T>(hv[k], h);
 #pragma unroll
           for (int e = 0; e < kE; ++e) small = fmaf(h[e] * kSmall, h[e] * kSmall, small);
         }
@@ -214,38 +235,45 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __gri
         if (too_large(sum)) r = rsqrtf(small * p.inv_dim) * kSmall;
       }
     }
-    uint4* y = static_cast<uint4*>(p.y) + vec_at<T>(row, head, p.y_pitch, p.vecs);
-    float amax = 0.f;
-    float o[kVecs][kE];
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
+    auto normed = [&](int k, float (&o)[kE]) {
       float g[kE];
-      widen<T>(xv[k], o[k]);
+      widen<T>(hv[k], o);
       widen<T>(w[k], g);
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
-        o[k][e] *= r;
-        if (p.weight) o[k][e] *= g[e];
+        o[e] *= r;
+        if (p.weight) o[e] *= g[e];
       }
+    };
+    uint4* y = static_cast<uint4*>(p.y) + vec_at<T>(this_row, this_head, p.y_pitch, p.vecs);
+    float amax = 0.f;
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      float o[kE];
+      normed(k, o);
       const int v = lane + k * kGroup;
       if (v < p.vecs) {
-        if (p.y && live) y[v] = narrow<T>(o[k]);
+        if (p.y && live) y[v] = narrow<T>(o);
+        if constexpr (kCodes) {
 #pragma unroll
-        for (int e = 0; e < kE; ++e) amax = max_nan(amax, fabsf(o[k][e]));
+          for (int e = 0; e < kE; ++e) amax = max_nan(amax, fabsf(o[e]));
+        }
       }
     }
-    if (p.codes) {
+    if constexpr (kCodes) {
       amax = join<kGroup>(amax, MaxNan(), s_sum[turn][2]);
       const float scale = max_nan(amax / kCodeMax, kLeastScale);
       const float inv = 1.f / scale;
-      uint8_t* c = p.codes + row * p.codes_pitch + int64_t(head) * p.vecs * kE;
+      uint8_t* c = p.codes + this_row * p.codes_pitch + int64_t(this_head) * p.vecs * kE;
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
+        float o[kE];
+        normed(k, o);
         uint32_t b[kE / 4];
 #pragma unroll
         for (int e = 0; e < kE; e += 4) {   // rounded to the nearest code, ties to even; what passes the largest by a rounding is held there
-          const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(o[k][e] * inv, o[k][e + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-          const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(o[k][e + 2] * inv, o[k][e + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+          const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(o[e] * inv, o[e + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+          const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(o[e + 2] * inv, o[e + 3] * inv), __NV_SATFINITE, __NV_E4M3);
           b[e / 4] = lo | hi << 16;
         }
         const int v = lane + k * kGroup;
@@ -277,25 +305,28 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __gri
     for (int e = 0; e < kE; ++e) dw[k][e] = 0.f;
   }
   int turn = 0;
-  for (int64_t i0 = int64_t(blockIdx.x) * kPerBlock; i0 < p.rows; i0 += int64_t(gridDim.x) * kPerBlock, turn ^= 1) {
-    const int64_t i = i0 + group;
+  constexpr bool kAhead = kVecs <= 2 && kGroup < 1024;   // beyond that registers are short
+  const int64_t stride = int64_t(gridDim.x) * kPerBlock;
+  int64_t i = int64_t(blockIdx.x) * kPerBlock + group, row = 0;
+  int head = 0;
+  uint4 next_h[kVecs], next_g[kVecs], next_s[kVecs];
+  auto load = [&](int64_t at) {
+    const bool live = at < p.rows;
+    row = p.heads == 1 ? at : at / p.heads;
+    head = p.heads == 1 ? 0 : int(at - row * p.heads);
+    load_row<T, kGroup, kVecs>(next_h, p.h, p.h_pitch, row, head, p.vecs, live);
+    load_row<T, kGroup, kVecs>(next_g, p.d_y, p.d_y_pitch, row, head, p.vecs, live);
+    load_row<T, kGroup, kVecs>(next_s, p.d_summed, p.d_summed_pitch, row, head, p.vecs, live && p.d_summed);
+  };
+  if (kAhead) load(i);
+  for (; i - group < p.rows; i += stride, turn ^= 1) {
+    if (!kAhead) load(i);
     const bool live = i < p.rows;
-    const int64_t row = p.heads == 1 ? i : i / p.heads;
-    const int head = p.heads == 1 ? 0 : int(i - row * p.heads);
-    const uint4* h = static_cast<const uint4*>(p.h) + vec_at<T>(row, head, p.h_pitch, p.vecs);
-    const uint4* dy = static_cast<const uint4*>(p.d_y) + vec_at<T>(row, head, p.d_y_pitch, p.vecs);
-    const uint4* ds = static_cast<const uint4*>(p.d_summed) + vec_at<T>(row, head, p.d_summed_pitch, p.vecs);
+    uint4* dx = static_cast<uint4*>(p.d_x) + vec_at<T>(row, head, p.d_x_pitch, p.vecs);
     uint4 hv[kVecs], gv[kVecs], sv[kVecs];
 #pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int v = lane + k * kGroup;
-      hv[k] = gv[k] = sv[k] = make_uint4(0, 0, 0, 0);
-      if (live && v < p.vecs) {
-        hv[k] = h[v];
-        gv[k] = dy[v];
-        if (p.d_summed) sv[k] = ds[v];
-      }
-    }
+    for (int k = 0; k < kVecs; ++k) { hv[k] = next_h[k]; gv[k] = next_g[k]; sv[k] = next_s[k]; }
+    if (kAhead) load(i + stride);   // the next row is on its way while this one is summed and stored
     auto sums = [&](float small) {
       float2 s = make_float2(0.f, 0.f);
 #pragma unroll
@@ -324,7 +355,6 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __gri
         r *= kSmall;
       }
     }
-    uint4* dx = static_cast<uint4*>(p.d_x) + vec_at<T>(row, head, p.d_x_pitch, p.vecs);
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       float a[kE], g[kE], c[kE], o[kE];
@@ -343,6 +373,7 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __gri
       if (p.d_x && live && v < p.vecs) dx[v] = narrow<T>(o);
     }
   }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (!p.part) return;
   float* part = p.part + int64_t(blockIdx.x) * p.vecs * kE;
   if constexpr (kGroup > 32) {
@@ -371,6 +402,7 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __gri
 // d_weight: the blocks' sums, added in a fixed order.  A block takes 32 columns, 32 threads share the parts of each.
 template <class T>
 __global__ void __launch_bounds__(1024) rms_weight_kernel(const float* __restrict__ part, int parts, int dim, T* __restrict__ d_weight) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");   // launched while the first kernel runs out
   __shared__ float s[32][33];
   const int c = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
   float sum = 0.f;
@@ -392,8 +424,9 @@ struct Shape {
   int group, vecs;
 };
 // Few vectors to a thread hide the latency of a row with many threads where rows are few; with many rows more vectors in flight
-// a thread and fewer barriers a byte are better.
-Shape shape_of(int vecs, int64_t rows) {
+// a thread and fewer barriers a byte are better.  The backward, with three loads and d_weight's sums to hold, takes two vectors a
+// thread, so that there are registers for the next row (8192 rows of 5120: three vectors and no row ahead 111 us).
+Shape shape_of(int vecs, int64_t rows, bool backward) {
   if (vecs <= 8) return {8, 1};
   if (vecs <= 16) return {16, 1};
   if (vecs <= 32) return {32, 1};
@@ -406,54 +439,99 @@ Shape shape_of(int vecs, int64_t rows) {
     return vecs <= 4096 ? Shape{1024, 4} : Shape{1024, 8};
   }
   if (vecs <= 64) return {32, 2};
-  if (vecs <= 128) return {32, 4};
-  if (vecs <= 256) return {128, 2};
-  if (vecs <= 512) return {256, 2};
-  if (vecs <= 768) return {256, 3};
-  if (vecs <= 1024) return {256, 4};
+  if (backward) {
+    if (vecs <= 128) return {128, 1};
+    if (vecs <= 256) return {128, 2};
+    if (vecs <= 384) return {192, 2};
+    if (vecs <= 512) return {256, 2};
+    if (vecs <= 640) return {320, 2};
+    if (vecs <= 768) return {384, 2};
+    if (vecs <= 1024) return {512, 2};
+  } else {
+    if (vecs <= 128) return {32, 4};
+    if (vecs <= 256) return {128, 2};
+    if (vecs <= 512) return {256, 2};
+    if (vecs <= 768) return {256, 3};
+    if (vecs <= 1024) return {256, 4};
+  }
   if (vecs <= 2048) return {512, 4};
   return vecs <= 4096 ? Shape{1024, 4} : Shape{1024, 8};
 }
 
-// Blocks of a launch: as many as the SMs hold at about 1024 threads each, and no more than there are rows for.
-int64_t blocks_of(const Shape& s, int64_t rows) {
-  const int threads = threads_of(s.group), per_block = threads / s.group;
-  return std::min<int64_t>(int64_t(resident_ctas()) * std::max(1, 1024 / threads), (rows + per_block - 1) / per_block);
+// Blocks of an SM in the backward, which the workspace goes by as each leaves a row of sums: as many as the registers hold.
+int bwd_per_sm(const Shape& s) { return std::max(1, (s.vecs == 1 ? 768 : 512) / threads_of(s.group)); }
+
+// Blocks of a launch: as many as the SMs hold, and no more than there are rows for.
+int64_t blocks_of(const Shape& s, int64_t rows, int per_sm) {
+  const int per_block = threads_of(s.group) / s.group;
+  return std::min<int64_t>(int64_t(resident_ctas()) * per_sm, (rows + per_block - 1) / per_block);
+}
+
+template <class Kernel>
+cudaError_t launch_fwd(Kernel kernel, const Shape& s, const FwdParams& p, cudaStream_t stream, int (&per_sm)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  int n = dev >= 0 && dev < 64 ? per_sm[dev] : 0;
+  if (n == 0) {
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads_of(s.group), 0);
+    if (e != cudaSuccess) return e;
+    n = std::max(1, n);
+    if (dev >= 0 && dev < 64) per_sm[dev] = n;
+  }
+  kernel<<<unsigned(blocks_of(s, p.rows, n)), threads_of(s.group), 0, stream>>>(p);
+  return cudaGetLastError();
 }
 
 template <class T, int kGroup, int kVecs, class P>
-void launch_one(const P& p, int64_t blocks, cudaStream_t stream) {
-  if constexpr (std::is_same_v<P, FwdParams>) rms_fwd_kernel<T, kGroup, kVecs><<<unsigned(blocks), threads_of(kGroup), 0, stream>>>(p);
-  else rms_bwd_kernel<T, kGroup, kVecs><<<unsigned(blocks), threads_of(kGroup), 0, stream>>>(p);
+cudaError_t launch_one(const P& p, cudaStream_t stream) {
+  const Shape s{kGroup, kVecs};
+  if constexpr (std::is_same_v<P, FwdParams>) {
+    static int per_sm[2][64] = {};
+    if (p.codes) return launch_fwd(rms_fwd_kernel<T, kGroup, kVecs, true>, s, p, stream, per_sm[0]);
+    return launch_fwd(rms_fwd_kernel<T, kGroup, kVecs, false>, s, p, stream, per_sm[1]);
+  } else {
+    rms_bwd_kernel<T, kGroup, kVecs><<<unsigned(blocks_of(s, p.rows, bwd_per_sm(s))), threads_of(kGroup), 0, stream>>>(p);
+    return cudaGetLastError();
+  }
 }
 
 template <class T, class P>
 cudaError_t launch(const P& p, cudaStream_t stream) {
-  const Shape s = shape_of(p.vecs, p.rows);
-  const int64_t blocks = blocks_of(s, p.rows);
+  constexpr bool kBackward = std::is_same_v<P, BwdParams>;
+  const Shape s = shape_of(p.vecs, p.rows, kBackward);
   switch (s.group * 16 + s.vecs) {
-    case 8 * 16 + 1: launch_one<T, 8, 1>(p, blocks, stream); break;
-    case 16 * 16 + 1: launch_one<T, 16, 1>(p, blocks, stream); break;
-    case 32 * 16 + 1: launch_one<T, 32, 1>(p, blocks, stream); break;
-    case 32 * 16 + 2: launch_one<T, 32, 2>(p, blocks, stream); break;
-    case 32 * 16 + 4: launch_one<T, 32, 4>(p, blocks, stream); break;
-    case 128 * 16 + 1: launch_one<T, 128, 1>(p, blocks, stream); break;
-    case 128 * 16 + 2: launch_one<T, 128, 2>(p, blocks, stream); break;
-    case 256 * 16 + 1: launch_one<T, 256, 1>(p, blocks, stream); break;
-    case 256 * 16 + 2: launch_one<T, 256, 2>(p, blocks, stream); break;
-    case 256 * 16 + 3: launch_one<T, 256, 3>(p, blocks, stream); break;
-    case 256 * 16 + 4: launch_one<T, 256, 4>(p, blocks, stream); break;
-    case 512 * 16 + 1: launch_one<T, 512, 1>(p, blocks, stream); break;
-    case 512 * 16 + 4: launch_one<T, 512, 4>(p, blocks, stream); break;
-    case 1024 * 16 + 1: launch_one<T, 1024, 1>(p, blocks, stream); break;
-    case 1024 * 16 + 2: launch_one<T, 1024, 2>(p, blocks, stream); break;
-    case 1024 * 16 + 4: launch_one<T, 1024, 4>(p, blocks, stream); break;
-    default:
-      // 8 vectors a thread: only fp32 rows of more than 16384 get here
-      if constexpr (sizeof(T) == 4) launch_one<T, 1024, 8>(p, blocks, stream);
-      else return cudaErrorInvalidValue;
+    case 8 * 16 + 1: return launch_one<T, 8, 1>(p, stream);
+    case 16 * 16 + 1: return launch_one<T, 16, 1>(p, stream);
+    case 32 * 16 + 1: return launch_one<T, 32, 1>(p, stream);
+    case 32 * 16 + 2: return launch_one<T, 32, 2>(p, stream);
+    case 128 * 16 + 1: return launch_one<T, 128, 1>(p, stream);
+    case 128 * 16 + 2: return launch_one<T, 128, 2>(p, stream);
+    case 256 * 16 + 1: return launch_one<T, 256, 1>(p, stream);
+    case 256 * 16 + 2: return launch_one<T, 256, 2>(p, stream);
+    case 512 * 16 + 1: return launch_one<T, 512, 1>(p, stream);
+    case 512 * 16 + 4: return launch_one<T, 512, 4>(p, stream);
+    case 1024 * 16 + 1: return launch_one<T, 1024, 1>(p, stream);
+    case 1024 * 16 + 2: return launch_one<T, 1024, 2>(p, stream);
+    case 1024 * 16 + 4: return launch_one<T, 1024, 4>(p, stream);
   }
-  return cudaGetLastError();
+  if constexpr (kBackward) {
+    switch (s.group) {
+      case 192: return launch_one<T, 192, 2>(p, stream);
+      case 320: return launch_one<T, 320, 2>(p, stream);
+      case 384: return launch_one<T, 384, 2>(p, stream);
+      case 512: return launch_one<T, 512, 2>(p, stream);
+    }
+  } else {
+    switch (s.group * 16 + s.vecs) {
+      case 32 * 16 + 4: return launch_one<T, 32, 4>(p, stream);
+      case 256 * 16 + 3: return launch_one<T, 256, 3>(p, stream);
+      case 256 * 16 + 4: return launch_one<T, 256, 4>(p, stream);
+    }
+  }
+  // 8 vectors a thread: only fp32 rows of more than 16384 get here
+  if constexpr (sizeof(T) == 4) return launch_one<T, 1024, 8>(p, stream);
+  else return cudaErrorInvalidValue;
 }
 
 int vec_elems(psrl_dtype_t t) { return t == PSRL_BF16 ? 8 : 4; }
@@ -529,7 +607,8 @@ size_t psrl_rms_norm_workspace_bytes(psrl_dtype_t dtype, int64_t n_rows, int32_t
   if (check(dtype, n_rows, n_heads, dim, 1.f) != PSRL_OK) return 0;
   if (n_rows == 0) return kWsHeaderBytes;
   const int64_t rows = n_rows * n_heads;
-  return kWsHeaderBytes + size_t(blocks_of(shape_of(dim / vec_elems(dtype), rows), rows)) * size_t(dim) * sizeof(float);
+  const Shape s = shape_of(dim / vec_elems(dtype), rows, true);
+  return kWsHeaderBytes + size_t(blocks_of(s, rows, bwd_per_sm(s))) * size_t(dim) * sizeof(float);
 }
 
 psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim, const void* summed, int64_t summed_pitch,
@@ -562,11 +641,21 @@ psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_he
               d_x_pitch, n_rows * n_heads, n_heads, int32_t(dim / unit), 1.f / float(dim), eps};
   cudaError_t e = dtype == PSRL_BF16 ? launch<__nv_bfloat16>(p, s) : launch<float>(p, s);
   if (e == cudaSuccess && d_weight) {
-    const int parts = int(blocks_of(shape_of(p.vecs, p.rows), p.rows));
+    const Shape shape = shape_of(p.vecs, p.rows, true);
+    const int parts = int(blocks_of(shape, p.rows, bwd_per_sm(shape)));
     const unsigned grid = unsigned((dim + 31) / 32);
-    if (dtype == PSRL_BF16) rms_weight_kernel<<<grid, 1024, 0, s>>>(part, parts, dim, static_cast<__nv_bfloat16*>(d_weight));
-    else rms_weight_kernel<<<grid, 1024, 0, s>>>(part, parts, dim, static_cast<float*>(d_weight));
-    e = cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(1024);
+    cfg.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const float* sums = part;
+    e = dtype == PSRL_BF16 ? cudaLaunchKernelEx(&cfg, rms_weight_kernel<__nv_bfloat16>, sums, parts, int(dim), static_cast<__nv_bfloat16*>(d_weight))
+                           : cudaLaunchKernelEx(&cfg, rms_weight_kernel<float>, sums, parts, int(dim), static_cast<float*>(d_weight));
   }
   return done(e);
 }
