@@ -30,8 +30,11 @@ constexpr int kRowBytes = 128;                 // of an operand in a stage: 64 b
 constexpr int kOperandBytes = 128 * kRowBytes; // one CTA's share of A or B in a stage
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kOutBytes = 128 * 128;           // what an epilogue group loads or stores at a time: 128 rows of 128 bytes
-constexpr int kGroups = 2, kEpilogueWarps = 4 * kGroups, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + 1;
-constexpr int kGemmThreads = (kEpilogueWarps + 2) * 32;
+// Four warps issue the copies: A and B, of even and of odd steps.  A look at a stage's barrier takes a thread up to 350 cycles while the
+// tensor cores use the shared memory, and a copy some 50, of the 512 that a step takes: one thread for all, 4 copies a step of the
+// gradients, left the tensor pipe busy for 67 % of 4096 x 4096 x 8192, one for each operand for 85 %.
+constexpr int kGroups = 2, kEpilogueWarps = 4 * kGroups, kTmaWarps = 4, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + kTmaWarps;
+constexpr int kGemmThreads = (kMmaWarp + 1) * 32;
 
 // kPlain: results leave through two buffers a group.  kFull: with mul, residual or z, three: one holds the residual and then y, one
 // mul and then z, and one is loaded ahead.
@@ -190,9 +193,11 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
   volatile int* abortp = &s_abort;
   int which, mt, nt;
 
-  if (warp == kTmaWarp) {
-    // ======================= TMA producer (both CTAs) =======================
+  if (warp >= kTmaWarp && warp < kTmaWarp + kTmaWarps) {
+    // ======================= TMA producers (both CTAs) =======================
     if (lane == 0) {
+      const bool of_a = (warp & 1) == 0;
+      const uint32_t odd = uint32_t(warp - kTmaWarp) >> 1;
       uint32_t it = 0;
       bool ok = true;
       for (int i = 0; ok && plan.get(p, cluster, n_clusters, i, which, mt, nt); ++i) {
@@ -201,24 +206,20 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
         const int m0 = mt * 256 + int(rank) * 128, half = q.tile_n / 2, n0 = nt * q.tile_n + int(rank) * half;
         const uint32_t stage_tx = 2 * (kOperandBytes + uint32_t(half) * kRowBytes);   // of both CTAs
         for (int kb = 0; kb < q.steps; ++kb, ++it) {
+          if ((it & 1) != odd) continue;
           const uint32_t s = it % kStages, round = it / kStages;
           if (round > 0 && !mbar_wait(&bar.empty[s], (round + 1) & 1, abortp, p.status)) { ok = false; break; }
-          // the second CTA's copies count on the first one's barrier as well
-          if (rank == 0) mbar_expect_tx(&bar.full[s], stage_tx);
+          // the second CTA's copies, and those of B, count on the first one's barrier as well, where they may be before this
+          if (of_a && rank == 0) mbar_expect_tx(&bar.full[s], stage_tx);
           const uint32_t full = in_leader(&bar.full[s]);
-          uint8_t* sa = smem + s * kStageBytes;
-          uint8_t* sb = sa + kOperandBytes;
-          if (q.a_mn) {
-            tma_load_pair(sa, ma, full, m0, kb * kDepth);
-            tma_load_pair(sa + kOperandBytes / 2, ma, full, m0 + 64, kb * kDepth);
+          uint8_t* to = smem + s * kStageBytes + (of_a ? 0 : kOperandBytes);
+          const CUtensorMap* map = of_a ? ma : mb;
+          const int at = of_a ? m0 : n0;
+          if (of_a ? q.a_mn : q.b_mn) {
+            tma_load_pair(to, map, full, at, kb * kDepth);
+            if (of_a || half > 64) tma_load_pair(to + kOperandBytes / 2, map, full, at + 64, kb * kDepth);
           } else {
-            tma_load_pair(sa, ma, full, kb * kDepth, m0);
-          }
-          if (q.b_mn) {
-            tma_load_pair(sb, mb, full, n0, kb * kDepth);
-            if (half > 64) tma_load_pair(sb + kOperandBytes / 2, mb, full, n0 + 64, kb * kDepth);
-          } else {
-            tma_load_pair(sb, mb, full, kb * kDepth, n0);
+            tma_load_pair(to, map, full, kb * kDepth, at);
           }
         }
       }
