@@ -30,10 +30,10 @@ constexpr int kRowBytes = 128;                 // of an operand in a stage: 64 b
 constexpr int kOperandBytes = 128 * kRowBytes; // one CTA's share of A or B in a stage
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kOutBytes = 128 * 128;           // what an epilogue group loads or stores at a time: 128 rows of 128 bytes
-// Four warps issue the copies: A and B, of even and of odd steps.  A look at a stage's barrier takes a thread up to 350 cycles while the
-// tensor cores use the shared memory, and a copy some 50, of the 512 that a step takes: one thread for all, 4 copies a step of the
-// gradients, left the tensor pipe busy for 67 % of 4096 x 4096 x 8192, one for each operand for 85 %.
-constexpr int kGroups = 2, kEpilogueWarps = 4 * kGroups, kTmaWarps = 4, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + kTmaWarps;
+// Three warps issue the copies, a step each in turn.  A look at a stage's barrier takes a thread up to 350 cycles while the tensor
+// cores use the shared memory, and a copy some 50, of the 512 that a step takes: one thread for all, 4 copies a step of the gradients, left
+// the tensor pipe busy for 67 % of 4096 x 4096 x 8192.  A 13th warp would cost each thread 40 registers, which the epilogue needs.
+constexpr int kGroups = 2, kEpilogueWarps = 4 * kGroups, kTmaWarps = 3, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + kTmaWarps;
 constexpr int kGemmThreads = (kMmaWarp + 1) * 32;
 
 // kPlain: results leave through two buffers a group.  kFull: with mul, residual or z, three: one holds the residual and then y, one
@@ -138,19 +138,34 @@ __device__ __forceinline__ uint4 get16(const uint8_t* b, int row, int chunk) {
 }
 
 // eight bf16 of a vector that ends at `n`, from column `col`; the same for all threads
-__device__ __forceinline__ void load_bias(const __nv_bfloat16* bias, int col, int n, float (&o)[8]) {
-  if (col + 8 <= n) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>(bias + col));
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ uint4 load_bias(const __nv_bfloat16* bias, int col, int n) {
+  if (col + 8 <= n) return __ldg(reinterpret_cast<const uint4*>(bias + col));
+  uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      o[2 * i] = __uint_as_float(w[i] << 16);
-      o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = col + i < n ? __bfloat162float(bias[col + i]) : 0.f;
+  for (int i = 0; i < 4; ++i) {
+    const float lo = col + 2 * i < n ? __bfloat162float(bias[col + 2 * i]) : 0.f, hi = col + 2 * i + 1 < n ? __bfloat162float(bias[col + 2 * i + 1]) : 0.f;
+    w[i] = pack_bf16(lo, hi);
   }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// four fp32 of such a vector
+__device__ __forceinline__ float4 load_scale(const float* scale, int col, int n) {
+  if (col + 4 <= n && (reinterpret_cast<uintptr_t>(scale) & 15) == 0) return __ldg(reinterpret_cast<const float4*>(scale + col));
+  float o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = col + i < n ? __ldg(scale + col + i) : 0.f;
+  return make_float4(o[0], o[1], o[2], o[3]);
+}
+__device__ __forceinline__ void widen8(const uint4& v, float (&o)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = __uint_as_float(w[i] << 16);
+    o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ uint4 narrow8(const float (&v)[8]) {
+  return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
 template <bool kFp8, Epilogue kEpilogue>
@@ -196,8 +211,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
   if (warp >= kTmaWarp && warp < kTmaWarp + kTmaWarps) {
     // ======================= TMA producers (both CTAs) =======================
     if (lane == 0) {
-      const bool of_a = (warp & 1) == 0;
-      const uint32_t odd = uint32_t(warp - kTmaWarp) >> 1;
+      uint32_t turn = uint32_t(kTmaWarps - (warp - kTmaWarp)) % kTmaWarps;   // 0: this warp's step
       uint32_t it = 0;
       bool ok = true;
       for (int i = 0; ok && plan.get(p, cluster, n_clusters, i, which, mt, nt); ++i) {
@@ -206,20 +220,27 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
         const int m0 = mt * 256 + int(rank) * 128, half = q.tile_n / 2, n0 = nt * q.tile_n + int(rank) * half;
         const uint32_t stage_tx = 2 * (kOperandBytes + uint32_t(half) * kRowBytes);   // of both CTAs
         for (int kb = 0; kb < q.steps; ++kb, ++it) {
-          if ((it & 1) != odd) continue;
+          const bool mine = turn == 0;
+          turn = turn + 1 == kTmaWarps ? 0 : turn + 1;
+          if (!mine) continue;
           const uint32_t s = it % kStages, round = it / kStages;
           if (round > 0 && !mbar_wait(&bar.empty[s], (round + 1) & 1, abortp, p.status)) { ok = false; break; }
-          // the second CTA's copies, and those of B, count on the first one's barrier as well, where they may be before this
-          if (of_a && rank == 0) mbar_expect_tx(&bar.full[s], stage_tx);
+          // the second CTA's copies count on the first one's barrier as well
+          if (rank == 0) mbar_expect_tx(&bar.full[s], stage_tx);
           const uint32_t full = in_leader(&bar.full[s]);
-          uint8_t* to = smem + s * kStageBytes + (of_a ? 0 : kOperandBytes);
-          const CUtensorMap* map = of_a ? ma : mb;
-          const int at = of_a ? m0 : n0;
-          if (of_a ? q.a_mn : q.b_mn) {
-            tma_load_pair(to, map, full, at, kb * kDepth);
-            if (of_a || half > 64) tma_load_pair(to + kOperandBytes / 2, map, full, at + 64, kb * kDepth);
+          uint8_t* sa = smem + s * kStageBytes;
+          uint8_t* sb = sa + kOperandBytes;
+          if (q.a_mn) {
+            tma_load_pair(sa, ma, full, m0, kb * kDepth);
+            tma_load_pair(sa + kOperandBytes / 2, ma, full, m0 + 64, kb * kDepth);
           } else {
-            tma_load_pair(to, map, full, kb * kDepth, at);
+            tma_load_pair(sa, ma, full, kb * kDepth, m0);
+          }
+          if (q.b_mn) {
+            tma_load_pair(sb, mb, full, n0, kb * kDepth);
+            if (half > 64) tma_load_pair(sb + kOperandBytes / 2, mb, full, n0 + 64, kb * kDepth);
+          } else {
+            tma_load_pair(sb, mb, full, kb * kDepth, n0);
           }
         }
       }
@@ -356,43 +377,55 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
             phases ^= 1u << b;
           }
         }
+// 32 columns at a time, all that they read first: an access to shared memory or L1 takes some 300 cycles beside the products, and one
+        // after the other, for 8 columns each, they made a chunk of 64 with bias 3300 cycles long and with mul, z and silu 6000
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float v[8];
+        for (int h = 0; h < 2; ++h) {
+          const int at = col + h * 32;
+          uint4 bias[4], mul[4], res[4];
+          float4 scale[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[j / 4][j % 4 * 8 + e]);
-          const int at = col + j * 8;
-          if constexpr (kFp8) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= sx * (at + e < q.N ? __ldg(p.w_scale + at + e) : 0.f);
-          }
-          if (p.bias) {
-            float b[8];
-            load_bias(p.bias, at, q.N, b);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += b[e];
-          }
-          if constexpr (kEpilogue == kFull) {
-            uint4 mul = make_uint4(0, 0, 0, 0);
-            if (p.has_mul) mul = get16(second, gt, j);
-            if (p.has_z)
-              put16(second, gt, j, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
-            activate(v, p.act);
-            if (p.has_mul) {
-              const uint32_t w[4] = {mul.x, mul.y, mul.z, mul.w};
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] *= __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+          for (int j = 0; j < 4; ++j) {
+            if (p.bias) bias[j] = load_bias(p.bias, at + j * 8, q.N);
+            if constexpr (kFp8) {
+              scale[2 * j] = load_scale(p.w_scale, at + j * 8, q.N);
+              scale[2 * j + 1] = load_scale(p.w_scale, at + j * 8 + 4, q.N);
             }
-            if (p.has_residual) {
-              const uint4 res = get16(first, gt, j);
-              const uint32_t w[4] = {res.x, res.y, res.z, res.w};
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+            if constexpr (kEpilogue == kFull) {
+              if (p.has_mul) mul[j] = get16(second, gt, h * 4 + j);
+              if (p.has_residual) res[j] = get16(first, gt, h * 4 + j);
             }
-          } else {
-            activate(v, p.act);
           }
-          put16(first, gt, j, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float v[8], o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[h][j * 8 + e]);
+            if constexpr (kFp8) {
+              const float4 a = scale[2 * j], b = scale[2 * j + 1];
+              const float s8[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] *= sx * s8[e];
+            }
+            if (p.bias) {
+              widen8(bias[j], o);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] += o[e];
+            }
+            if (kEpilogue == kFull && p.has_z) put16(second, gt, h * 4 + j, narrow8(v));
+            activate(v, p.act);
+            if (kEpilogue == kFull && p.has_mul) {
+              widen8(mul[j], o);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] *= o[e];
+            }
+            if (kEpilogue == kFull && p.has_residual) {
+              widen8(res[j], o);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] += o[e];
+            }
+            put16(first, gt, h * 4 + j, narrow8(v));
+          }
         }
         fence_proxy_async();
         named_sync(bar_id, kGroupThreads);
