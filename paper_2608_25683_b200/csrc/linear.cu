@@ -36,8 +36,8 @@ constexpr int kOutBytes = 128 * 128;           // what an epilogue group loads o
 constexpr int kGroups = 2, kEpilogueWarps = 4 * kGroups, kTmaWarps = 3, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + kTmaWarps;
 constexpr int kGemmThreads = (kMmaWarp + 1) * 32;
 
-// kPlain: results leave through two buffers a group.  kFull: with mul, residual or z, three: one holds the residual and then y, one
-// mul and then z, and one is loaded ahead.
+// kPlain: results leave through two buffers a group.  kFull: with mul, residual or z, three: one holds mul and then z, one the
+// residual and then y, and one is loaded ahead (mul's, where there are both).
 enum Epilogue { kPlain, kFull };
 constexpr int stages(Epilogue e) { return e == kPlain ? 5 : 4; }
 constexpr int buffers(Epilogue e) { return e == kPlain ? 2 : 3; }
@@ -156,15 +156,24 @@ __device__ __forceinline__ float4 load_scale(const float* scale, int col, int n)
   for (int i = 0; i < 4; ++i) o[i] = col + i < n ? __ldg(scale + col + i) : 0.f;
   return make_float4(o[0], o[1], o[2], o[3]);
 }
-__device__ __forceinline__ void widen8(const uint4& v, float (&o)[8]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// eight numbers and a vector of eight bf16
+__device__ __forceinline__ void add8(float* v, const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    o[2 * i] = __uint_as_float(w[i] << 16);
-    o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    v[2 * i] += __uint_as_float(w[i] << 16);
+    v[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ uint4 narrow8(const float (&v)[8]) {
+__device__ __forceinline__ void mul8(float* v, const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] *= __uint_as_float(w[i] << 16);
+    v[2 * i + 1] *= __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ uint4 narrow8(const float* v) {
   return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
@@ -294,7 +303,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
     const uint32_t acc_empty = in_leader(&bar.acc_empty[group]);
     uint8_t* buf = smem + kStages * kStageBytes + group * kBuffers * kOutBytes;
     const bool has_second = kEpilogue == kFull && (p.has_mul || p.has_z);
-    const int per = has_second ? 2 : 1;          // buffers a chunk takes: residual -> y, mul -> z
+    const int per = has_second ? 2 : 1;          // buffers a chunk takes: mul -> z if there is one of them, then residual -> y
     uint32_t base = 0, go = 0;                   // uses of buffers before this tile; hand-overs between the group's warps
     uint32_t phases = 0;                         // parity that the next load into each buffer completes
     uint32_t tile = 0;
@@ -309,11 +318,11 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
       auto issue = [&](int until) {
         until = min(until, chunks * per);
         for (; issued < until; ++issued) {
-          const bool second = per == 2 && (issued & 1);
-          if (kEpilogue == kPlain || !(second ? p.has_mul : p.has_residual)) continue;
+          const bool of_mul = per == 2 && !(issued & 1);
+          if (kEpilogue == kPlain || !(of_mul ? p.has_mul : p.has_residual)) continue;
           const int b = int((base + issued) % kBuffers);
           mbar_expect_tx(&bar.in[group][b], kOutBytes);
-          tma_load_2d(buf + b * kOutBytes, second ? &maps.mul : &maps.residual, &bar.in[group][b], n0 + issued / per * 64, row0);
+          tma_load_2d(buf + b * kOutBytes, of_mul ? &maps.mul : &maps.residual, &bar.in[group][b], n0 + issued / per * 64, row0);
         }
       };
       if (kEpilogue == kFull && gt == 0) {
@@ -348,7 +357,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
           if (kEpilogue == kFull) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              if (u >= per || !(u ? p.has_mul : p.has_residual)) continue;
+              if (u >= per || !(per == 2 && u == 0 ? p.has_mul : p.has_residual)) continue;
               const int b = int((n + u) % kBuffers);
               ok = ok && mbar_wait(&bar.in[group][b], (phases >> b) & 1, abortp, p.status);
             }
@@ -362,26 +371,30 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
           ok = s_go[group][go++ & 1];
           if (!ok) break;
         }
-        uint8_t* first = buf + int(n % kBuffers) * kOutBytes;
-        uint8_t* second = buf + int((n + 1) % kBuffers) * kOutBytes;
+        const int of_z = int(n % kBuffers), of_y = int((n + uint32_t(per) - 1) % kBuffers);
+        uint8_t* first = buf + of_y * kOutBytes;
+        uint8_t* second = buf + of_z * kOutBytes;   // with per == 2 only
         if (kEpilogue == kFull) {
           // complete already; this thread's own look at the barrier orders its reads behind the copies
-          if (p.has_residual) {
-            const int b = int(n % kBuffers);
-            mbar_wait(&bar.in[group][b], (phases >> b) & 1, abortp, p.status);
-            phases ^= 1u << b;
-          }
           if (p.has_mul) {
-            const int b = int((n + 1) % kBuffers);
-            mbar_wait(&bar.in[group][b], (phases >> b) & 1, abortp, p.status);
-            phases ^= 1u << b;
+            mbar_wait(&bar.in[group][of_z], (phases >> of_z) & 1, abortp, p.status);
+            phases ^= 1u << of_z;
+          }
+          if (p.has_residual) {
+            mbar_wait(&bar.in[group][of_y], (phases >> of_y) & 1, abortp, p.status);
+            phases ^= 1u << of_y;
           }
         }
-// 32 columns at a time, all that they read first: an access to shared memory or L1 takes some 300 cycles beside the products, and one
-        // after the other, for 8 columns each, they made a chunk of 64 with bias 3300 cycles long and with mul, z and silu 6000
+        // 32 columns at a time, all that they read first, and every choice once for all of them: with reads and branches for each 8 columns a
+        // chunk of 64 took 1300 cycles, with bias 2300 and with mul, z and silu 5900; so 620, 1550 and 5000
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = col + h * 32;
+          if (kEpilogue == kFull && h == 1 && gt == 0) {
+            // the stores of the chunks before this one have been read out by now: the buffers they left are loaded ahead
+            asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            issue(c * per + kBuffers);
+          }
           uint4 bias[4], mul[4], res[4];
           float4 scale[8];
 #pragma unroll
@@ -396,36 +409,35 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
               if (p.has_residual) res[j] = get16(first, gt, h * 4 + j);
             }
           }
+float v[32];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float v[8], o[8];
+          for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[h][e]);
+          if constexpr (kFp8) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[h][j * 8 + e]);
-            if constexpr (kFp8) {
-              const float4 a = scale[2 * j], b = scale[2 * j + 1];
-              const float s8[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] *= sx * s8[e];
+            for (int j = 0; j < 8; ++j) {
+              v[4 * j] *= sx * scale[j].x; v[4 * j + 1] *= sx * scale[j].y;
+              v[4 * j + 2] *= sx * scale[j].z; v[4 * j + 3] *= sx * scale[j].w;
             }
-            if (p.bias) {
-              widen8(bias[j], o);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] += o[e];
-            }
-            if (kEpilogue == kFull && p.has_z) put16(second, gt, h * 4 + j, narrow8(v));
-            activate(v, p.act);
-            if (kEpilogue == kFull && p.has_mul) {
-              widen8(mul[j], o);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] *= o[e];
-            }
-            if (kEpilogue == kFull && p.has_residual) {
-              widen8(res[j], o);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] += o[e];
-            }
-            put16(first, gt, h * 4 + j, narrow8(v));
           }
+          if (p.bias) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) add8(&v[j * 8], bias[j]);
+          }
+          if (kEpilogue == kFull && p.has_z) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) put16(second, gt, h * 4 + j, narrow8(&v[j * 8]));
+          }
+          activate(v, p.act);
+          if (kEpilogue == kFull && p.has_mul) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mul8(&v[j * 8], mul[j]);
+          }
+          if (kEpilogue == kFull && p.has_residual) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) add8(&v[j * 8], res[j]);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) put16(first, gt, h * 4 + j, narrow8(&v[j * 8]));
         }
         fence_proxy_async();
         named_sync(bar_id, kGroupThreads);
@@ -433,11 +445,6 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
           tma_store_2d(&maps.out[which], first, col, row0);
           if (kEpilogue == kFull && p.has_z) tma_store_2d(&maps.z, second, col, row0);
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          if (kEpilogue == kFull) {
-            // the stores before this chunk's have been read out: the buffers they left are loaded ahead
-            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-            issue(c * per + kBuffers);
-          }
         }
       }
       if (!ok) break;
