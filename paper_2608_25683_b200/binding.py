@@ -694,6 +694,8 @@ def _rows_pitch(t, rows: int, heads: int, d: int, name: str) -> int:
     """Row pitch in elements of a [rows, heads, d] tensor whose rows may be slices of a wider matrix."""
     if t.shape != (rows, heads, d):
         raise ValueError(f"{name} must be [{rows}, {heads}, {d}], got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return heads * d
     s = t.stride()
     if (s[2] != 1 and d > 1) or (s[1] != d and heads > 1):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
@@ -706,10 +708,14 @@ def _plan_device(plan, dev: int):
 
 
 def _rope_pools(plan, *pools):
-    for p in pools:
-        if p.dim() != 3 or p.shape != pools[0].shape or p.shape[0] != plan.n_kv_heads or p.shape[2] != plan.head_dim or not p.is_contiguous():
-            raise ValueError("pools must be contiguous [Hkv, capacity, d]")
-    return int(pools[0].shape[1])
+    shape = pools[0].shape
+    if len(shape) == 3 and shape[0] == plan.n_kv_heads and shape[2] == plan.head_dim:
+        for p in pools:
+            if p.shape != shape or not p.is_contiguous():
+                break
+        else:
+            return shape[1]
+    raise ValueError("pools must be contiguous [Hkv, capacity, d]")
 
 
 def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=None, stream=None):
@@ -736,16 +742,19 @@ def psrl_rope_axes_qkv_bwd(plan: Plan, rope: Rope, positions, d_q, dk_pool, dv_p
 
 def _axis_pitch(rope: Rope, positions, rows: int) -> int:
     """Elements between two axes' positions."""
-    if str(positions.dtype) != "torch.int32" or positions.shape != (rope.n_axes, rows) or (rows > 1 and positions.stride(1) != 1):
-        raise ValueError(f"positions must be int32 [{rope.n_axes}, {rows}], the rows of an axis contiguous")
-    return positions.stride(0) if rope.n_axes > 1 else rows
+    if positions.dtype is _torch().int32 and positions.shape == (rope.n_axes, rows):
+        if positions.is_contiguous():
+            return rows
+        if rows <= 1 or positions.stride(1) == 1:
+            return positions.stride(0) if rope.n_axes > 1 else rows
+    raise ValueError(f"positions must be int32 [{rope.n_axes}, {rows}], the rows of an axis contiguous")
 
 
 def _rope_qkv_fwd(name, plan, rope, positions, q, k, v, k_pool, v_pool, q_out, stream):
-    V, d = plan.view, plan.head_dim
+    V, d, hkv = plan.view, plan.head_dim, plan.n_kv_heads
     _check_dtype(plan, q, k, v, k_pool, v_pool)
     pq = _rows_pitch(q, V["T_q"], plan.n_q_heads, d, "q")
-    pk, pv = (_rows_pitch(t, V["T_q"], plan.n_kv_heads, d, n) for t, n in ((k, "k"), (v, "v")))
+    pk, pv = _rows_pitch(k, V["T_q"], hkv, d, "k"), _rows_pitch(v, V["T_q"], hkv, d, "v")
     cap = _rope_pools(plan, k_pool, v_pool)
     at = () if positions is None else (positions.data_ptr(), _axis_pitch(rope, positions, V["T_q"]))
     dev = _device_of(q, k, v, k_pool, v_pool, *(() if positions is None else (positions,)))
@@ -790,7 +799,7 @@ def _rope_qkv_bwd(name, plan, rope, positions, d_q, dk_pool, dv_pool, dq_out, dk
 
 def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stream=None):
     """Rotates x [rows, heads, head_dim] (f32 or bf16, rows at any pitch) at int32 `positions` [rows].  Returns y (y may be x)."""
-    if str(positions.dtype) != "torch.int32" or positions.shape != x.shape[:1] or not positions.is_contiguous():
+    if positions.dtype is not _torch().int32 or positions.shape != x.shape[:1] or not positions.is_contiguous():
         raise ValueError("positions must be contiguous int32 [rows]")
     return _rope_rows("psrl_rope_rows", rope, x, positions, (), y, inverse, stream)
 
@@ -812,11 +821,12 @@ def _rope_rows(name, rope, x, positions, axis_pitch, y, inverse, stream):
     dev = _device_of(x, positions)
     raw, keep = _stream_on(stream, dev)
     if y is None:
-        y = _new(keep, shape, x.dtype, x.device)
+        y, py = _like(x, keep), heads * rope.head_dim
     elif y.dtype is not x.dtype or y.get_device() != dev:
         raise ValueError("y must have x's type and device")
-    _launch(name, dev, rope._h, dt, x.data_ptr(), px, positions.data_ptr(), *axis_pitch, rows, heads, y.data_ptr(),
-            px if y is x else _rows_pitch(y, rows, heads, rope.head_dim, "y"), 1 if inverse else 0, raw)
+    else:
+        py = px if y is x else _rows_pitch(y, rows, heads, rope.head_dim, "y")
+    _launch(name, dev, rope._h, dt, x.data_ptr(), px, positions.data_ptr(), *axis_pitch, rows, heads, y.data_ptr(), py, 1 if inverse else 0, raw)
     return y
 
 
@@ -1026,6 +1036,8 @@ def _codes_rows(codes, shape, keep, like, name="codes"):
 def _floats(t, shape, keep, device, name):
     """A contiguous float32 tensor of `shape`, made if not given."""
     if t is None:
+        if keep is None:
+            return _torch().empty(shape, dtype=_torch().float32, device=device)
         return _new(keep, shape, _torch().float32, device)
     if t.dtype is not _torch().float32 or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be contiguous float32 {tuple(shape)} on {device}")
@@ -1387,11 +1399,9 @@ def psrl_launch_count(plan: Plan, backward: bool) -> int:
 
 
 def _check_dtype(plan: Plan, *tensors):
-    import torch
-
-    want = torch.float32 if plan.dtype == "f32" else torch.bfloat16
+    want = _torch().float32 if plan.dtype == "f32" else _torch().bfloat16
     for t in tensors:
-        if t.dtype != want:
+        if t.dtype is not want:
             raise TypeError(f"tensor dtype {t.dtype} does not match the plan's {want}")
         if not t.is_cuda:
             raise RuntimeError("tensors must live on a CUDA device: this library has no CPU path")
