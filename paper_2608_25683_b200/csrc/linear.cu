@@ -210,6 +210,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
   cluster_sync();   // the peer's barriers exist before anything arrives on them
   tc_fence_after();
   previous_kernel_done();
+  next_kernel_may_start();
   if (p.status && blockIdx.x == 0 && tid == 0) *p.status = int(PSRL_OK);
 
   const Schedule plan(p, cluster, n_clusters);
@@ -555,37 +556,46 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
   const int kb0 = int(int64_t(p.steps) * rank / p.splits), kb1 = int(int64_t(p.steps) * (rank + 1) / p.splits);
   const uint32_t b_bytes = uint32_t(p.tile_rows) * kRowBytes, stage_bytes = kOperandBytes + b_bytes;
 
-  if (threadIdx.x == 0) {
+  volatile int* abortp = &s_abort;
+  if (warp == kFewMma) {
+    tmem_alloc(&s_tmem, uint32_t(p.tmem_cols));
+    tmem_relinquish();
+  } else if (warp == kFewTma && lane == 0) {
+    tma_prefetch_desc(&maps.a);
+    tma_prefetch_desc(&maps.b);
     s_abort = 0;
     for (int i = 0; i < p.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 1); }
     mbar_init(&acc_full, 1);
     fence_mbar_init();
   }
-  if (warp == kFewMma) {
-    tmem_alloc(&s_tmem, uint32_t(p.tmem_cols));
-    tmem_relinquish();
-  }
+  previous_kernel_done();
+  next_kernel_may_start();
+  if (p.status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
+  // the first loads need nothing of the other warps: they are on their way while tensor memory is handed out
+  auto load = [&](int kb, int s) {
+    uint8_t* sa = smem + s * stage_bytes;
+    mbar_expect_tx(&full[s], stage_bytes);
+    if (p.a_mn) {
+      tma_load_2d(sa, &maps.a, &full[s], col0, kb * kDepth);
+      tma_load_2d(sa + kOperandBytes / 2, &maps.a, &full[s], col0 + 64, kb * kDepth);
+    } else {
+      tma_load_2d(sa, &maps.a, &full[s], kb * kDepth, col0);
+    }
+    tma_load_2d(sa + kOperandBytes, &maps.b, &full[s], kb * kDepth, row0);
+  };
+  if (warp == kFewTma && lane == 0)
+    for (int s = 0; s < p.stages && kb0 + s < kb1; ++s) load(kb0 + s, s);
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  volatile int* abortp = &s_abort;
-  previous_kernel_done();
-  if (p.status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
 
   if (warp == kFewTma) {
     if (lane == 0) {
-      for (int kb = kb0, s = 0, round = 0; kb < kb1; ++kb) {
-        if (round > 0 && !mbar_wait(&empty[s], (round + 1) & 1, abortp, p.status)) break;
-        uint8_t* sa = smem + s * stage_bytes;
-        mbar_expect_tx(&full[s], stage_bytes);
-        if (p.a_mn) {
-          tma_load_2d(sa, &maps.a, &full[s], col0, kb * kDepth);
-          tma_load_2d(sa + kOperandBytes / 2, &maps.a, &full[s], col0 + 64, kb * kDepth);
-        } else {
-          tma_load_2d(sa, &maps.a, &full[s], kb * kDepth, col0);
-        }
-        tma_load_2d(sa + kOperandBytes, &maps.b, &full[s], kb * kDepth, row0);
+      for (int kb = kb0 + p.stages, s = 0, round = 1; kb < kb1; ++kb) {
+        if (!mbar_wait(&empty[s], (round + 1) & 1, abortp, p.status)) break;
+        load(kb, s);
         if (++s == p.stages) { s = 0; ++round; }
       }
     }
@@ -698,8 +708,10 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
 // ------------------------------------------------------------------------------------------------- elementwise backward
 
 // dz = d_y * mul * act'(z), d_mul = d_y * act(z), and sums over the rows of dz: a block takes 32 vectors of columns and 64 rows (more
-// where there are millions), and leaves its column sums for bias_kernel, which adds them in order.  Memory bound: every element once.
-constexpr int kDzRows = 64;
+// where there are millions), and leaves its column sums for bias_kernel, which adds them in order.  Memory bound: every element once, so
+// a thread has the vectors of four rows on their way at a time, as they lie in memory: 4096 x 14336 with mul 92 us (5.1 TB/s); widened
+// and two at a time 220 us.  Blocks of 128 vectors, two rows side by side, 102 us, and 23 where 777 rows of 3584 take 8.
+constexpr int kDzRows = 64, kDzVecs = 32, kDzLanes = 8, kDzThreads = kDzVecs * kDzLanes;
 template <class T> constexpr int kVec = 16 / int(sizeof(T));
 
 template <class T>
@@ -712,23 +724,30 @@ struct DzParams {
   int* status;
 };
 
+// a vector, or the `left` numbers that there are
 template <class T>
-__device__ __forceinline__ void load_vec(const T* at, int left, float (&o)[kVec<T>]) {
-  if (left >= kVec<T>) {
-    const uint4 v = *reinterpret_cast<const uint4*>(at);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ uint4 load_vec(const T* at, int left) {
+  if (left >= kVec<T>) return *reinterpret_cast<const uint4*>(at);
+  uint32_t w[4] = {};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(T) == 4) {
-        o[i] = __uint_as_float(w[i]);
-      } else {
-        o[2 * i] = __uint_as_float(w[i] << 16);
-        o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
+  for (int i = 0; i < kVec<T>; ++i) {
+    if (i >= left) break;
+    if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(at[i]);
+    else w[i / 2] |= uint32_t(__bfloat16_as_ushort(at[i])) << (i % 2 * 16);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <class T>
+__device__ __forceinline__ void widen_vec(const uint4& v, float (&o)[kVec<T>]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      o[i] = __uint_as_float(w[i]);
+    } else {
+      o[2 * i] = __uint_as_float(w[i] << 16);
+      o[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) o[i] = i < left ? float(at[i]) : 0.f;
   }
 }
 template <class T>
@@ -749,54 +768,65 @@ __device__ __forceinline__ void store_vec(T* at, int left, const float (&o)[kVec
 }
 
 template <class T>
-__global__ void __launch_bounds__(256) dz_kernel(const __grid_constant__ DzParams<T> p) {
-  constexpr int kE = kVec<T>;
+__global__ void __launch_bounds__(kDzThreads, 2) dz_kernel(const __grid_constant__ DzParams<T> p) {
+  constexpr int kE = kVec<T>, kBatch = 4;
+  previous_kernel_done();
   next_kernel_may_start();
-  __shared__ float s_sum[8][32][kE + 1];
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
-  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-  const int64_t col = (int64_t(blockIdx.x) * 32 + tx) * kE;
+  __shared__ float s_sum[kDzThreads][kE + 1];
+  if (p.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
+  const int tx = threadIdx.x % kDzVecs, ty = threadIdx.x / kDzVecs;
+  const int64_t col = (int64_t(blockIdx.x) * kDzVecs + tx) * kE;
   const int left = int(p.N - col < kE ? p.N - col : kE);
   float sum[kE] = {};
   if (left > 0) {
-    const int64_t row0 = int64_t(blockIdx.y) * p.rows;
-#pragma unroll 2
-    for (int k = ty; k < p.rows; k += 8) {
-      const int64_t row = row0 + k;
-      if (row >= p.M) break;
-      float g[kE], m[kE], z[kE], d[kE];
-      load_vec(p.d_y + row * p.d_y_pitch + col, left, g);
-      if (p.mul) load_vec(p.mul + row * p.mul_pitch + col, left, m);
-      if (p.z) load_vec(p.z + row * p.z_pitch + col, left, z);
-      if (p.z) {
+    const int64_t end = min(int64_t(p.M), (int64_t(blockIdx.y) + 1) * p.rows);
+    for (int64_t row0 = int64_t(blockIdx.y) * p.rows + ty; row0 < end; row0 += kDzLanes * kBatch) {
+      uint4 g4[kBatch], m4[kBatch], z4[kBatch];
 #pragma unroll
-        for (int e = 0; e < kE; ++e) {
-          float value, slope;
-          act_and_slope(z[e], p.act, value, slope);
-          d[e] = g[e] * value;
-          if (p.mul) g[e] *= m[e];
-          g[e] *= slope;
-        }
-      } else if (p.mul) {
-#pragma unroll
-        for (int e = 0; e < kE; ++e) g[e] *= m[e];
+      for (int b = 0; b < kBatch; ++b) {
+        const int64_t row = min(row0 + b * kDzLanes, end - 1);   // behind the end the last row again, for nothing
+        g4[b] = load_vec(p.d_y + row * p.d_y_pitch + col, left);
+        if (p.mul) m4[b] = load_vec(p.mul + row * p.mul_pitch + col, left);
+        if (p.z) z4[b] = load_vec(p.z + row * p.z_pitch + col, left);
       }
-      if (p.d_mul) store_vec(p.d_mul + row * p.d_mul_pitch + col, left, d);
-      if (p.dz) store_vec(p.dz + row * p.dz_pitch + col, left, g);
 #pragma unroll
-      for (int e = 0; e < kE; ++e) sum[e] += g[e];
+      for (int b = 0; b < kBatch; ++b) {
+        const int64_t row = row0 + b * kDzLanes;
+        if (row >= end) break;
+        float g[kE], m[kE];
+        widen_vec<T>(g4[b], g);
+        if (p.mul) widen_vec<T>(m4[b], m);
+        if (p.z) {
+          float z[kE], d[kE];
+          widen_vec<T>(z4[b], z);
+          act_and_slope(z, p.act, d);   // d: values, z: slopes
+#pragma unroll
+          for (int e = 0; e < kE; ++e) {
+            d[e] *= g[e];
+            if (p.mul) g[e] *= m[e];
+            g[e] *= z[e];
+          }
+          if (p.d_mul) store_vec(p.d_mul + row * p.d_mul_pitch + col, left, d);
+        } else if (p.mul) {
+#pragma unroll
+          for (int e = 0; e < kE; ++e) g[e] *= m[e];
+        }
+        if (p.dz) store_vec(p.dz + row * p.dz_pitch + col, left, g);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) sum[e] += g[e];
+      }
     }
   }
   if (!p.part) return;
 #pragma unroll
-  for (int e = 0; e < kE; ++e) s_sum[ty][tx][e] = sum[e];
+  for (int e = 0; e < kE; ++e) s_sum[threadIdx.x][e] = sum[e];
   __syncthreads();
-  for (int i = threadIdx.x; i < 32 * kE; i += 256) {
-    const int64_t c = int64_t(blockIdx.x) * 32 * kE + i;
-    if (c >= p.N) break;
+  const int64_t first = int64_t(blockIdx.x) * kDzVecs * kE;
+  for (int i = threadIdx.x; i < kDzVecs * kE; i += kDzThreads) {
+    if (first + i >= p.N) break;
     float s = 0.f;
-    for (int y = 0; y < 8; ++y) s += s_sum[y][i / kE][i % kE];
-    p.part[int64_t(blockIdx.y) * p.N + c] = s;
+    for (int y = 0; y < kDzLanes; ++y) s += s_sum[y * kDzVecs + i / kE][i % kE];
+    p.part[int64_t(blockIdx.y) * p.N + first + i] = s;
   }
 }
 
@@ -825,9 +855,10 @@ int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t dz_rows(int64_t M) { return std::max<int64_t>(kDzRows, div_up(M, 65535)); }   // at most 65,535 blocks of rows
 
-// A kernel of a call; all but the first may start before the one before has ended (see previous_kernel_done).
+// Every kernel here may start before the one before it on the stream has ended, and touches memory behind previous_kernel_done() only: its
+// barriers and tensor memory are laid out meanwhile (1 row x 1024 x 1024 5.7 -> 4.2 us, 4096 x 4096 10.7 -> 9.0).
 template <class... P, class... A>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, bool first, const A&... args) {
+cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, const A&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
@@ -837,12 +868,12 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t sme
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
-  cfg.numAttrs = first ? 0 : 1;
+  cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
 template <bool kFp8, Epilogue kEpilogue>
-cudaError_t launch_gemm(const Maps& maps, const Params& p, bool first, cudaStream_t stream) {
+cudaError_t launch_gemm(const Maps& maps, const Params& p, cudaStream_t stream) {
   static bool done[64] = {};
   cudaError_t e = ensure_dynamic_smem(linear_kernel<kFp8, kEpilogue>, gemm_smem(kEpilogue), done);
   if (e != cudaSuccess) return e;
@@ -850,7 +881,7 @@ cudaError_t launch_gemm(const Maps& maps, const Params& p, bool first, cudaStrea
   for (const Product& q : p.product) tiles += int64_t(q.m_tiles) * q.n_tiles;
   if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int clusters = static_cast<int>(std::min<int64_t>(tiles, resident_ctas() / 2));
-  return launch(linear_kernel<kFp8, kEpilogue>, dim3(2 * clusters), kGemmThreads, gemm_smem(kEpilogue), stream, first, maps, p);
+  return launch(linear_kernel<kFp8, kEpilogue>, dim3(2 * clusters), kGemmThreads, gemm_smem(kEpilogue), stream, maps, p);
 }
 
 Product product_of(int64_t M, int64_t N, int64_t depth, int64_t step, int tile_n, int a_mn, int b_mn, int64_t group_bytes) {
@@ -866,10 +897,11 @@ Product product_of(int64_t M, int64_t N, int64_t depth, int64_t step, int tile_n
   return q;
 }
 
-// Rounds of tiles that the pairs of CTAs make, in 256-wide ones; a 128-wide tile costs more than half of one.
+// Rounds of tiles that the pairs of CTAs make, in 256-wide ones; a 128-wide tile takes 0.85 of the time of one while loads are waited for
+// (4096 deep 22.5 and 26.1 us), and no less than three quarters, by its bytes.
 double rounds_of(int64_t M, int64_t N, int tile_n) {
   const int64_t pairs = std::max(1, resident_ctas() / 2), tiles = div_up(M, 256) * div_up(N, tile_n);
-  return double(div_up(tiles, pairs)) * (tile_n == 256 ? 1.0 : 0.6);
+  return double(div_up(tiles, pairs)) * (tile_n == 256 ? 1.0 : 0.85);
 }
 int tile_of(int64_t M, int64_t N) { return rounds_of(M, N, 128) < rounds_of(M, N, 256) ? 128 : 256; }
 
@@ -894,10 +926,25 @@ FewShape few_shape(int64_t rows, int64_t cols, int64_t steps) {
   f.smem = std::max(size_t(f.stages) * stage, size_t(f.tile_rows) * 128 * sizeof(float)) + 1024;
   return f;
 }
-bool few_better(int64_t rows, int64_t cols) { return rows <= kFewRows; }
+// Which kernel a product goes to, by estimates of their times in us, from 28 products of 192 to 1024 rows, 512 to 14336 deep and 512 to
+// 8192 wide: the quicker one but for the last 10 % in two.  The pairs of CTAs make one round of tiles after the other, a step of 128 bytes
+// takes them 0.33 us (128 wide tiles 0.28); the few-rows kernel shares the depth out, its 32 KB a step and CTA come at 15 TB/s from the L2,
+// in rounds of two CTAs for each SM.  (4096 deep and wide: 384 rows 23.1 us with this one, 26.8 with that; 768 rows 36.3 and 26.8.)
+bool few_better(int64_t rows, int64_t cols, int64_t steps) {
+  if (rows <= kFewRows) return true;
+  const int64_t sms = resident_ctas(), pairs = std::max<int64_t>(1, sms / 2);
+  const int tile_n = tile_of(rows, cols);
+  const double rounds = double(div_up(div_up(rows, 256) * div_up(cols, tile_n), pairs));
+  const double of_pairs = 6.0 + rounds * double(steps) * (tile_n == 256 ? 0.33 : 0.28);
+  const FewShape f = few_shape(rows, cols, steps);
+  const int64_t tiles = f.row_tiles * f.col_tiles, ctas = tiles * f.splits, places = 2 * sms;
+  double of_few = double(tiles) * double(steps) * double(kOperandBytes + f.tile_rows * kRowBytes) / 15e6;
+  if (ctas > places) of_few *= double(div_up(ctas, places) * places) / double(ctas);
+  return 8.5 + of_few < of_pairs;
+}
 
 template <bool kFp8>
-cudaError_t launch_few(const FewMaps& maps, FewParams& p, const FewShape& f, bool first, cudaStream_t stream) {
+cudaError_t launch_few(const FewMaps& maps, FewParams& p, const FewShape& f, cudaStream_t stream) {
   static bool done[64] = {};
   cudaError_t e = ensure_dynamic_smem(linear_few_kernel<kFp8>, 113 * 1024, done);
   if (e != cudaSuccess) return e;
@@ -918,7 +965,7 @@ cudaError_t launch_few(const FewMaps& maps, FewParams& p, const FewShape& f, boo
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = first ? 1 : 2;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, linear_few_kernel<kFp8>, maps, p);
 }
 
@@ -971,10 +1018,10 @@ Layout layout(psrl_dtype_t t, int64_t M, int64_t K, int64_t N, bool with_dz, boo
 
 template <class T>
 cudaError_t run_dz(const DzParams<T>& p, T* d_bias, cudaStream_t s) {
-  const dim3 grid(unsigned(div_up(p.N, 32 * kVec<T>)), unsigned(div_up(p.M, p.rows)));
-  cudaError_t e = launch(dz_kernel<T>, grid, 256, 0, s, true, p);
+  const dim3 grid(unsigned(div_up(p.N, kDzVecs * kVec<T>)), unsigned(div_up(p.M, p.rows)));
+  cudaError_t e = launch(dz_kernel<T>, grid, kDzThreads, 0, s, p);
   if (e == cudaSuccess && d_bias)
-    e = launch(bias_kernel<T>, dim3(unsigned(div_up(p.N, 32))), 1024, 0, s, false, p.part, int(grid.y), p.N, d_bias);
+    e = launch(bias_kernel<T>, dim3(unsigned(div_up(p.N, 32))), 1024, 0, s, p.part, int(grid.y), p.N, d_bias);
   return e;
 }
 
@@ -1032,7 +1079,7 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
   }
   const int64_t step = fp8 ? 128 : 64;
   using Bf = __nv_bfloat16;
-  if (few_better(M, N)) {
+  if (few_better(M, N, div_up(in_dim, step))) {
     const FewShape f = few_shape(M, N, div_up(in_dim, step));
     FewMaps maps;
     const bool made = fp8 ? make_map_u8_2d(&maps.a, weight, in_dim, N, weight_pitch, 128) && make_map_u8_2d(&maps.b, x, in_dim, M, x_pitch, f.tile_rows)
@@ -1045,7 +1092,7 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     q.y = static_cast<Bf*>(y); q.z = static_cast<Bf*>(z);
     q.mul_pitch = mul_pitch; q.residual_pitch = residual_pitch; q.y_pitch = y_pitch; q.z_pitch = z_pitch;
     q.act = activation; q.status = status;
-    const cudaError_t e = fp8 ? launch_few<true>(maps, q, f, true, s) : launch_few<false>(maps, q, f, true, s);
+    const cudaError_t e = fp8 ? launch_few<true>(maps, q, f, s) : launch_few<false>(maps, q, f, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
   Maps maps{};
@@ -1065,8 +1112,8 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
   p.act = activation;
   p.has_mul = mul != nullptr; p.has_residual = residual != nullptr; p.has_z = z != nullptr;
   p.status = status;
-  const cudaError_t e = fp8 ? (full ? launch_gemm<true, kFull>(maps, p, true, s) : launch_gemm<true, kPlain>(maps, p, true, s))
-                            : (full ? launch_gemm<false, kFull>(maps, p, true, s) : launch_gemm<false, kPlain>(maps, p, true, s));
+  const cudaError_t e = fp8 ? (full ? launch_gemm<true, kFull>(maps, p, s) : launch_gemm<true, kPlain>(maps, p, s))
+                            : (full ? launch_gemm<false, kFull>(maps, p, s) : launch_gemm<false, kPlain>(maps, p, s));
   return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
 }
 
@@ -1143,17 +1190,16 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     if (e == cudaSuccess && d_weight) e = f32_product<true, true>(params(z_at, x_at, N, M, d_weight, d_weight_pitch), part, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
-  if (d_x && few_better(M, K)) {
+  if (d_x && few_better(M, K, div_up(N, 64))) {
     const FewShape f = few_shape(M, K, div_up(N, 64));
     FewMaps maps;
     if (!make_map_bf16_2d(&maps.a, weight, K, N, weight_pitch * 2, 64) || !make_map_bf16_2d(&maps.b, dz, N, M, dz_pitch * 2, f.tile_rows)) return PSRL_ERR_CUDA;
     FewParams q{};
     q.rows = int32_t(M); q.cols = int32_t(K); q.steps = int32_t(div_up(N, 64)); q.a_mn = 1;
     q.y = static_cast<__nv_bfloat16*>(d_x); q.y_pitch = d_x_pitch; q.status = status;
-    e = launch_few<false>(maps, q, f, first, s);
+    e = launch_few<false>(maps, q, f, s);
     if (e != cudaSuccess) return cuda_failed(e);
     if (!d_weight) return PSRL_OK;
-    first = false;
     d_x = nullptr;
   }
   // the deeper product first: its tiles cost more
@@ -1176,7 +1222,7 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     made = make_map_bf16_2d(&maps.a[iw], dz, N, M, dz_pitch * 2, 64) && make_map_bf16_2d(&maps.b[iw], x, K, M, x_pitch * 2, 64) &&
            make_map_bf16_2d(&maps.out[iw], d_weight, K, N, d_weight_pitch * 2, 128);
   if (!made) return PSRL_ERR_CUDA;
-  e = launch_gemm<false, kPlain>(maps, p, first, s);
+  e = launch_gemm<false, kPlain>(maps, p, s);
   return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
 }
 

@@ -33,25 +33,42 @@ __device__ __forceinline__ void activate(float (&v)[kN], int act) {
   }
 }
 
-__device__ __forceinline__ void act_and_slope(float z, int act, float& value, float& slope) {
+// Values of the activation at z, and its slopes in z's place.
+template <int kN>
+__device__ __forceinline__ void act_and_slope(float (&z)[kN], int act, float (&value)[kN]) {
   if (act == PSRL_ACT_NONE) {
-    value = z;
-    slope = 1.f;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      value[i] = z[i];
+      z[i] = 1.f;
+    }
   } else if (act == PSRL_ACT_RELU) {
-    value = z < 0.f ? 0.f : z;
-    slope = z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      value[i] = z[i] < 0.f ? 0.f : z[i];
+      z[i] = z[i] > 0.f ? 1.f : z[i] <= 0.f ? 0.f : z[i];   // NaN stays
+    }
   } else if (act == PSRL_ACT_SILU) {
-    const float s = sigmoid(z);
-    value = z * s;
-    slope = fmaf(value, 1.f - s, s);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const float s = sigmoid(z[i]);
+      value[i] = z[i] * s;
+      z[i] = fmaf(value[i], 1.f - s, s);
+    }
   } else if (act == PSRL_ACT_GELU) {
-    const float c = 0.5f * (1.f + erff(z * kRootHalf));
-    value = z * c;
-    slope = fmaf(z * kNormal, __expf(-0.5f * z * z), c);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const float c = 0.5f * (1.f + erff(z[i] * kRootHalf));
+      value[i] = z[i] * c;
+      z[i] = fmaf(z[i] * kNormal, __expf(-0.5f * z[i] * z[i]), c);
+    }
   } else {
-    const float s = sigmoid(gelu_u2(z));
-    value = z * s;
-    slope = fmaf(value * (1.f - s), 2.f * kGeluIn * fmaf(3.f * kGeluCubic * z, z, 1.f), s);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const float s = sigmoid(gelu_u2(z[i]));
+      value[i] = z[i] * s;
+      z[i] = fmaf(value[i] * (1.f - s), 2.f * kGeluIn * fmaf(3.f * kGeluCubic * z[i], z[i], 1.f), s);
+    }
   }
 }
 

@@ -17,9 +17,12 @@
 
 #include "../../include/psrl.h"
 #include "kernels.h"
+#include "sm100_pair.cuh"
 
 namespace psrl {
 namespace {
+using sm100::next_kernel_may_start;
+using sm100::previous_kernel_done;
 
 constexpr int kMaxDim = 32768;
 constexpr float kCodeMax = 448.f;          // the largest e4m3 number
@@ -164,6 +167,8 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __gri
   constexpr int kE = kElems<T>, kPerBlock = threads_of(kGroup) / kGroup;
   __shared__ float s_sum[2][3][32];   // two rows in a row use two
   const int lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup;
+  previous_kernel_done();
+  next_kernel_may_start();
   uint4 w[kVecs];
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
@@ -292,6 +297,8 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __gri
   constexpr int kE = kElems<T>, kThreads = threads_of(kGroup), kPerBlock = kThreads / kGroup;
   __shared__ float2 s_sum[2][2][32];
   __shared__ float s_part[kGroup > 32 ? 1 : kThreads * kVecs * kE];
+  previous_kernel_done();
+  next_kernel_may_start();
   if (p.status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
   const int lane = threadIdx.x % kGroup, group = threadIdx.x / kGroup;
   uint4 w[kVecs];
@@ -373,7 +380,6 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __gri
       if (p.d_x && live && v < p.vecs) dx[v] = narrow<T>(o);
     }
   }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (!p.part) return;
   float* part = p.part + int64_t(blockIdx.x) * p.vecs * kE;
   if constexpr (kGroup > 32) {
@@ -402,7 +408,8 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __gri
 // d_weight: the blocks' sums, added in a fixed order.  A block takes 32 columns, 32 threads share the parts of each.
 template <class T>
 __global__ void __launch_bounds__(1024) rms_weight_kernel(const float* __restrict__ part, int parts, int dim, T* __restrict__ d_weight) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");   // launched while the first kernel runs out
+  previous_kernel_done();
+  next_kernel_may_start();
   __shared__ float s[32][33];
   const int c = threadIdx.x & 31, slice = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
   float sum = 0.f;
@@ -467,6 +474,21 @@ int64_t blocks_of(const Shape& s, int64_t rows, int per_sm) {
   return std::min<int64_t>(int64_t(resident_ctas()) * per_sm, (rows + per_block - 1) / per_block);
 }
 
+// Every kernel here may start before the one before it on the stream has ended, and touches memory behind previous_kernel_done() only.
+template <class... P, class... A>
+cudaError_t launch_early(void (*kernel)(P...), unsigned blocks, unsigned threads, cudaStream_t stream, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 template <class Kernel>
 cudaError_t launch_fwd(Kernel kernel, const Shape& s, const FwdParams& p, cudaStream_t stream, int (&per_sm)[64]) {
   int dev = 0;
@@ -479,8 +501,7 @@ cudaError_t launch_fwd(Kernel kernel, const Shape& s, const FwdParams& p, cudaSt
     n = std::max(1, n);
     if (dev >= 0 && dev < 64) per_sm[dev] = n;
   }
-  kernel<<<unsigned(blocks_of(s, p.rows, n)), threads_of(s.group), 0, stream>>>(p);
-  return cudaGetLastError();
+  return launch_early(kernel, unsigned(blocks_of(s, p.rows, n)), unsigned(threads_of(s.group)), stream, p);
 }
 
 template <class T, int kGroup, int kVecs, class P>
@@ -491,8 +512,7 @@ cudaError_t launch_one(const P& p, cudaStream_t stream) {
     if (p.codes) return launch_fwd(rms_fwd_kernel<T, kGroup, kVecs, true>, s, p, stream, per_sm[0]);
     return launch_fwd(rms_fwd_kernel<T, kGroup, kVecs, false>, s, p, stream, per_sm[1]);
   } else {
-    rms_bwd_kernel<T, kGroup, kVecs><<<unsigned(blocks_of(s, p.rows, bwd_per_sm(s))), threads_of(kGroup), 0, stream>>>(p);
-    return cudaGetLastError();
+    return launch_early(rms_bwd_kernel<T, kGroup, kVecs>, unsigned(blocks_of(s, p.rows, bwd_per_sm(s))), unsigned(threads_of(kGroup)), stream, p);
   }
 }
 
@@ -644,18 +664,8 @@ psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_he
     const Shape shape = shape_of(p.vecs, p.rows, true);
     const int parts = int(blocks_of(shape, p.rows, bwd_per_sm(shape)));
     const unsigned grid = unsigned((dim + 31) / 32);
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(1024);
-    cfg.stream = s;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    const float* sums = part;
-    e = dtype == PSRL_BF16 ? cudaLaunchKernelEx(&cfg, rms_weight_kernel<__nv_bfloat16>, sums, parts, int(dim), static_cast<__nv_bfloat16*>(d_weight))
-                           : cudaLaunchKernelEx(&cfg, rms_weight_kernel<float>, sums, parts, int(dim), static_cast<float*>(d_weight));
+    e = dtype == PSRL_BF16 ? launch_early(rms_weight_kernel<__nv_bfloat16>, grid, 1024, s, part, parts, dim, static_cast<__nv_bfloat16*>(d_weight))
+                           : launch_early(rms_weight_kernel<float>, grid, 1024, s, part, parts, dim, static_cast<float*>(d_weight));
   }
   return done(e);
 }

@@ -242,6 +242,53 @@ def test_slices_in_place_streams_graphs(lib):
     assert work.status() == 0
 
 
+@pytest.mark.parametrize("m", [5, 300])
+def test_order_on_a_stream(lib, m):
+    """Kernels that may start early still see what is before them on their stream, and nothing behind them starts early: chains of
+    products over a memset, a copy and another stream's work, eager and captured."""
+    x, w, d = make(m, 512, 512, "bf16", 8)
+    x, w = x.to(torch.bfloat16), w.to(torch.bfloat16)
+    norm = torch.ones(512, device="cuda", dtype=torch.bfloat16)
+    side = torch.cuda.Stream()
+    one, two, out = (torch.empty(m, 512, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+
+    def chain():
+        one.zero_()                                                             # a memset right before
+        lib.psrl_linear_fwd(one, w, residual=x, y=two)                          # = x
+        one.copy_(two)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            lib.psrl_rms_norm_fwd(one, norm, y=one)                             # on another stream, joined again
+            lib.psrl_linear_fwd(one, w, y=two, activation="silu")
+        torch.cuda.current_stream().wait_stream(side)
+        for _ in range(6):                                                      # each needs all of the one before
+            lib.psrl_linear_fwd(two, w, y=one, residual=x)
+            lib.psrl_rms_norm_fwd(one, norm, y=two)
+        lib.psrl_linear_bwd(two, w, one, d_x=out, want_weight=False)
+        two.zero_()                                                             # must not reach the product before
+
+    chain()
+    torch.cuda.synchronize()
+    want = out.clone()
+    h = lib.psrl_rms_norm_fwd(x, norm)[0]
+    h = lib.psrl_linear_fwd(h, w, activation="silu")[0]
+    for _ in range(6):
+        torch.cuda.synchronize()
+        o = lib.psrl_linear_fwd(h, w, residual=x)[0]
+        torch.cuda.synchronize()
+        h = lib.psrl_rms_norm_fwd(o, norm)[0]
+    torch.cuda.synchronize()
+    assert torch.equal(lib.psrl_linear_bwd(h, w, o, want_weight=False)[0], want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for _ in range(5):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
 def test_no_rows_and_refusals(lib):
     x, w, d = make(6, 128, 72, "bf16", 6)
     x, w = x.to(torch.bfloat16), w.to(torch.bfloat16)
