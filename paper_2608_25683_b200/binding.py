@@ -6,6 +6,7 @@ if the library has not been built; there is no fallback of any kind.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -594,10 +595,19 @@ def _torch():
     return _torch_module
 
 
-def _scratch(nbytes: int, keep, device):
+def _scratch(nbytes: int, keep, like):
     """(address, bytes, tensor that holds them until the call is on its stream) of a call's own workspace."""
-    buf = _new(keep, nbytes + 256, _torch().uint8, device)
+    if keep is None:
+        buf = like.new_empty(((nbytes + 256) // like.element_size() + 1,))
+    else:
+        buf = _new(keep, nbytes + 256, _torch().uint8, like.device)
     return (buf.data_ptr() + 255) // 256 * 256, nbytes, buf
+
+
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(name: str, *args) -> int:
+    """What the library asks for a call of these sizes, asked once."""
+    return int(getattr(lib(), name)(*args))
 
 
 _type_codes = None
@@ -606,18 +616,19 @@ _type_codes = None
 def _type_code(t):
     """PSRL_F32, PSRL_BF16 or None."""
     global _type_codes
-    if _type_codes is None:
+    codes = _type_codes
+    if codes is None:
         import torch
 
-        _type_codes = {torch.float32: PSRL_F32, torch.bfloat16: PSRL_BF16}
-    return _type_codes.get(t.dtype)
+        codes = _type_codes = {torch.float32: PSRL_F32, torch.bfloat16: PSRL_BF16}
+    return codes.get(t.dtype)
 
 
 def _stream_on(stream, dev: int):
     """(raw stream handle of a call on device `dev`, torch stream to keep temporaries for or None).  Without a stream it is
     torch's current one of that device; the raw handle skips a Stream object, a third of a small call's host time."""
     if stream is None:
-        return _cuda()._cuda_getCurrentRawStream(dev), None
+        return (_torch_c or _cuda())._cuda_getCurrentRawStream(dev), None
     import torch
 
     if not hasattr(stream, "cuda_stream"):
@@ -641,7 +652,7 @@ def _new(stream, shape, dtype, device):
 def _launch(name: str, dev: int, *args):
     """One C call with the tensors' device as the current one: the library launches there."""
     fn = getattr(_lib or lib(), name)
-    if dev == _cuda()._cuda_getDevice():
+    if dev == (_torch_c or _cuda())._cuda_getDevice():
         st = fn(*args)
     else:
         import torch
@@ -993,7 +1004,9 @@ def _stream_rows(t, shape, name: str, like=None) -> int:
 
 def _like(t, keep):
     """A contiguous tensor of t's shape, type and device, made for a call."""
-    return _torch().empty_like(t) if keep is None and t.is_contiguous() else _new(keep, t.shape, t.dtype, t.device)
+    if keep is not None:
+        return _new(keep, t.shape, t.dtype, t.device)
+    return _torch().empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 def _norm_args(x, weight):
@@ -1007,13 +1020,15 @@ def _norm_args(x, weight):
         rows, heads, dim = shape
     else:
         raise ValueError("rows must be [rows, dim] or [rows, heads, dim]")
-    if weight is None:
-        return dt, rows, heads, dim, _device_of(x)
-    if weight.dtype is not x.dtype:
-        raise TypeError(f"weight is {weight.dtype}, the rows are {x.dtype}")
-    if weight.shape != shape[-1:] or not weight.is_contiguous():
-        raise ValueError(f"weight must be a contiguous vector of {dim}")
-    return dt, rows, heads, dim, _device_of(x, weight)
+    dev = x.get_device()
+    if dev < 0:
+        raise RuntimeError("tensors must live on a CUDA device: this library has no CPU path")
+    if weight is not None:
+        if weight.dtype is not x.dtype:
+            raise TypeError(f"weight is {weight.dtype}, the rows are {x.dtype}")
+        if weight.shape != (dim,) or weight.get_device() != dev or not weight.is_contiguous():
+            raise ValueError(f"weight must be a contiguous vector of {dim} on {x.device}")
+    return dt, rows, heads, dim, dev
 
 
 def _codes_rows(codes, shape, keep, like, name="codes"):
@@ -1023,7 +1038,8 @@ def _codes_rows(codes, shape, keep, like, name="codes"):
     if codes is None:
         if pitch == least:
             if keep is None and like.is_contiguous():
-                return _torch().empty_like(like, dtype=_torch().float8_e4m3fn), pitch
+                t = _torch()
+                return t.empty_like(like, dtype=t.float8_e4m3fn), pitch
             return _new(keep, shape, _torch().float8_e4m3fn, like.device), pitch
         codes = _new(keep, (rows, pitch), _torch().float8_e4m3fn, like.device)[:, :least]
         return codes.unflatten(1, shape[1:]) if len(shape) == 3 else codes, pitch
@@ -1036,8 +1052,6 @@ def _codes_rows(codes, shape, keep, like, name="codes"):
 def _floats(t, shape, keep, device, name):
     """A contiguous float32 tensor of `shape`, made if not given."""
     if t is None:
-        if keep is None:
-            return _torch().empty(shape, dtype=_torch().float32, device=device)
         return _new(keep, shape, _torch().float32, device)
     if t.dtype is not _torch().float32 or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be contiguous float32 {tuple(shape)} on {device}")
@@ -1102,7 +1116,7 @@ def psrl_rms_norm_bwd(summed, weight, d_y, eps: float = 1e-6, d_summed=None, d_x
         d_x = None
     else:
         if d_x is None:
-            d_x, p_x = _like(summed, keep), heads * dim
+            d_x, p_x = _like(d_y, keep), heads * dim
         else:
             p_x = _stream_rows(d_x, shape, "d_x", summed)
         a_x = d_x.data_ptr()
@@ -1115,7 +1129,7 @@ def psrl_rms_norm_bwd(summed, weight, d_y, eps: float = 1e-6, d_summed=None, d_x
     if workspace is None:
         ws, wsb, held = None, 0, None
         if d_weight is not None:
-            ws, wsb, held = _scratch((_lib or lib()).psrl_rms_norm_workspace_bytes(dt, rows, heads, dim), keep, summed.device)
+            ws, wsb, held = _scratch(_workspace_bytes("psrl_rms_norm_workspace_bytes", dt, rows, heads, dim), keep, summed)
     else:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
     _launch("psrl_rms_norm_bwd", dev, dt, rows, heads, dim, summed.data_ptr(), ph, None if weight is None else weight.data_ptr(), eps,
@@ -1159,13 +1173,10 @@ def _linear_args(x, weight, activation):
 def _operand_pitch(t, name: str) -> int:
     """Row pitch of a matrix operand; a lone row has any that will do."""
     rows, cols = t.shape
-    if rows > 1:
-        pitch, step = t.stride()
-        if step == 1 or cols == 1:
-            return pitch
-    elif cols == 1 or t.stride(1) == 1:
-        return -(-cols // 16) * 16
-    raise ValueError(f"{name}: the elements of a row must be contiguous")
+    pitch, step = t.stride()
+    if step != 1 and cols != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    return pitch if rows > 1 else -(-cols // 16) * 16
 
 
 def _beside(t, rows: int, cols: int, dtype, dev: int, name: str):
@@ -1190,6 +1201,9 @@ def _result(t, rows: int, cols: int, dtype, keep, like, name: str):
     if t is not None:
         return (t, *_beside(t, rows, cols, dtype, like.get_device(), name))
     pitch = -(-cols // 8) * 8
+    if keep is None and pitch == cols and like.shape == (rows, cols) and dtype is like.dtype and like.is_contiguous():
+        t = _torch().empty_like(like)
+        return t, t.data_ptr(), cols
     if keep is None and dtype is like.dtype:
         t = like.new_empty((rows, pitch))
     else:
@@ -1229,7 +1243,7 @@ def psrl_linear_fwd(x, weight, bias=None, activation=None, mul=None, residual=No
     if workspace is not None:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
     elif dt == PSRL_F32:
-        ws, wsb, held = _scratch((_lib or lib()).psrl_linear_workspace_bytes(dt, m, k, n, 0), keep, x.device)
+        ws, wsb, held = _scratch(_workspace_bytes("psrl_linear_workspace_bytes", dt, m, k, n, 0), keep, x)
     else:
         ws, wsb = None, 0
     _launch("psrl_linear_fwd", dev, dt, m, k, n, x.data_ptr(), px, a_xs, weight.data_ptr(), pw, a_ws, a_bias, _ACTIVATIONS[activation],
@@ -1255,17 +1269,17 @@ def psrl_linear_bwd(x, weight, d_y, z=None, activation=None, mul=None, d_x=None,
     a_mul, p_mul = _beside(mul, m, n, out, dev, "mul")
     px, pw = _operand_pitch(x, "x"), _operand_pitch(weight, "weight")
     d_x, a_x, p_x = _result(d_x, m, k, out, keep, x, "d_x") if want_x else (None, None, 0)
-    d_weight, a_w, p_w = _result(d_weight, n, k, out, keep, x, "d_weight") if want_weight else (None, None, 0)
-    d_mul, a_m, p_m = _result(d_mul, m, n, out, keep, x, "d_mul") if want_mul else (None, None, 0)
+    d_weight, a_w, p_w = _result(d_weight, n, k, out, keep, weight, "d_weight") if want_weight else (None, None, 0)
+    d_mul, a_m, p_m = _result(d_mul, m, n, out, keep, d_y, "d_mul") if want_mul else (None, None, 0)
     if not want_bias:
         d_bias = None
     elif d_bias is None:
-        d_bias = x.new_empty((n,)) if keep is None else _new(keep, (n,), out, x.device)
+        d_bias = d_y.new_empty((n,)) if keep is None else _new(keep, (n,), out, x.device)
     a_bias = _beside_vector(d_bias, n, out, dev, "d_bias")
     if workspace is not None:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
     elif activation not in (None, "none") or mul is not None or want_bias or dt == PSRL_F32:
-        ws, wsb, held = _scratch((_lib or lib()).psrl_linear_workspace_bytes(dt, m, k, n, 1), keep, x.device)
+        ws, wsb, held = _scratch(_workspace_bytes("psrl_linear_workspace_bytes", dt, m, k, n, 1), keep, x)
     else:
         ws, wsb = None, 0
     _launch("psrl_linear_bwd", dev, dt, m, k, n, x.data_ptr(), px, weight.data_ptr(), pw, a_z, p_z, _ACTIVATIONS[activation], a_mul, p_mul,
