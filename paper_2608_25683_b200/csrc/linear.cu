@@ -569,7 +569,6 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
     fence_mbar_init();
   }
   previous_kernel_done();
-  next_kernel_may_start();
   if (p.status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
   // the first loads need nothing of the other warps: they are on their way while tensor memory is handed out
   auto load = [&](int kb, int s) {
@@ -589,6 +588,7 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  next_kernel_may_start();   // not before this one has its tensor memory
   const uint32_t tmem = s_tmem;
 
   if (warp == kFewTma) {
@@ -926,21 +926,40 @@ FewShape few_shape(int64_t rows, int64_t cols, int64_t steps) {
   f.smem = std::max(size_t(f.stages) * stage, size_t(f.tile_rows) * 128 * sizeof(float)) + 1024;
   return f;
 }
-// Which kernel a product goes to, by estimates of their times in us, from 28 products of 192 to 1024 rows, 512 to 14336 deep and 512 to
-// 8192 wide: the quicker one but for the last 10 % in two.  The pairs of CTAs make one round of tiles after the other, a step of 128 bytes
-// takes them 0.33 us (128 wide tiles 0.28); the few-rows kernel shares the depth out, its 32 KB a step and CTA come at 15 TB/s from the L2,
-// in rounds of two CTAs for each SM.  (4096 deep and wide: 384 rows 23.1 us with this one, 26.8 with that; 768 rows 36.3 and 26.8.)
+// Estimates of times in us that decide which kernel a product goes to, from 28 products of 192 to 1024 rows, 512 to 14336 deep and 512 to
+// 8192 wide: they pick the quicker one but for the last 10 % in two.  The pairs of CTAs make one round of tiles after the other, a step of
+// 128 bytes takes them 0.33 us (128 wide tiles 0.28).  The few-rows kernel shares the depth out; its weights come at 5.5 TB/s from memory,
+// its 32 KB a step and CTA at 15 TB/s from the L2, in rounds of two CTAs for each SM.  (4096 deep and wide: 384 rows 23.1 us with this
+// one, 26.8 with that; 768 rows 36.3 and 26.8.)
+constexpr double kStepUs[2] = {0.28, 0.33};   // of a 128 wide tile, of a 256 wide one
+double few_time(int64_t rows, int64_t cols, int64_t steps) {
+  const FewShape f = few_shape(rows, cols, steps);
+  const int64_t tiles = f.row_tiles * f.col_tiles, ctas = tiles * f.splits, places = 2 * int64_t(resident_ctas());
+  double l2 = double(tiles) * double(steps) * double(kOperandBytes + f.tile_rows * kRowBytes) / 15e6;
+  if (ctas > places) l2 *= double(div_up(ctas, places) * places) / double(ctas);
+  return (rows <= kFewRows / 2 ? 5.0 : 8.5) + std::max(l2, double(cols) * double(steps) * kRowBytes / 5.5e6);
+}
 bool few_better(int64_t rows, int64_t cols, int64_t steps) {
   if (rows <= kFewRows) return true;
-  const int64_t sms = resident_ctas(), pairs = std::max<int64_t>(1, sms / 2);
   const int tile_n = tile_of(rows, cols);
-  const double rounds = double(div_up(div_up(rows, 256) * div_up(cols, tile_n), pairs));
-  const double of_pairs = 6.0 + rounds * double(steps) * (tile_n == 256 ? 0.33 : 0.28);
-  const FewShape f = few_shape(rows, cols, steps);
-  const int64_t tiles = f.row_tiles * f.col_tiles, ctas = tiles * f.splits, places = 2 * sms;
-  double of_few = double(tiles) * double(steps) * double(kOperandBytes + f.tile_rows * kRowBytes) / 15e6;
-  if (ctas > places) of_few *= double(div_up(ctas, places) * places) / double(ctas);
-  return 8.5 + of_few < of_pairs;
+  const int64_t pairs = std::max(1, resident_ctas() / 2);
+  return few_time(rows, cols, steps) < 6.0 + double(div_up(div_up(rows, 256) * div_up(cols, tile_n), pairs) * steps) * kStepUs[tile_n == 256];
+}
+// The gradients' products (rows 0: not that one) of `cols` columns: the tiles' width, and the time of both in one launch.
+struct GradShape {
+  int tile_n;
+  double time;
+};
+GradShape grad_shape(int64_t rows_x, int64_t steps_x, int64_t rows_w, int64_t steps_w, int64_t cols) {
+  const int64_t pairs = std::max(1, resident_ctas() / 2);
+  GradShape best{256, 1e30};
+  for (int tile_n : {256, 128}) {
+    const int64_t n = div_up(cols, tile_n), x = div_up(rows_x, 256) * n, w = div_up(rows_w, 256) * n;
+    const int64_t deepest = std::max(x ? steps_x : 0, w ? steps_w : 0);
+    const double time = 6.0 + std::max(double(deepest), double(x * steps_x + w * steps_w) / double(pairs) + 0.5 * double(deepest)) * kStepUs[tile_n == 256];
+    if (time < best.time) best = {tile_n, time};
+  }
+  return best;
 }
 
 template <bool kFp8>
@@ -1190,7 +1209,11 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     if (e == cudaSuccess && d_weight) e = f32_product<true, true>(params(z_at, x_at, N, M, d_weight, d_weight_pitch), part, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
-  if (d_x && few_better(M, K, div_up(N, 64))) {
+  // Both in one launch, or d_x shared out over its depth first, as the times of the few-rows kernel and of the pairs' rounds go; by the
+  // sizes alone, so that a gradient has the same bits whether or not the other is wanted.
+  const int64_t steps_x = div_up(N, 64), steps_w = div_up(M, 64);
+  const GradShape both = grad_shape(M, steps_x, N, steps_w, K), of_weight = grad_shape(0, 0, N, steps_w, K);
+  if (d_x && few_time(M, K, steps_x) + of_weight.time < both.time) {
     const FewShape f = few_shape(M, K, div_up(N, 64));
     FewMaps maps;
     if (!make_map_bf16_2d(&maps.a, weight, K, N, weight_pitch * 2, 64) || !make_map_bf16_2d(&maps.b, dz, N, M, dz_pitch * 2, f.tile_rows)) return PSRL_ERR_CUDA;
@@ -1203,8 +1226,8 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     d_x = nullptr;
   }
   // the deeper product first: its tiles cost more
-  const int tile_x = 256, tile_w = 256;
-  Product px = product_of(M, K, N, 64, tile_x, 0, 1, kGradGroupBytes), pw = product_of(N, K, M, 64, tile_w, 1, 1, kGradGroupBytes);
+  const int tile_n = d_x ? both.tile_n : of_weight.tile_n;
+  Product px = product_of(M, K, N, 64, tile_n, 0, 1, kGradGroupBytes), pw = product_of(N, K, M, 64, tile_n, 1, 1, kGradGroupBytes);
   if (!d_x) px.m_tiles = 0;
   if (!d_weight) pw.m_tiles = 0;
   const int ix = !d_x || (d_weight && pw.steps > px.steps) ? 1 : 0, iw = 1 - ix;

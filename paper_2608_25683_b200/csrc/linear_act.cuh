@@ -65,9 +65,9 @@ __device__ __forceinline__ void act_and_slope(float (&z)[kN], int act, float (&v
   } else {
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const float s = sigmoid(gelu_u2(z[i]));
+      const float s = sigmoid(gelu_u2(z[i])), near = fminf(fmaxf(z[i], -64.f), 64.f);   // beyond, 1 - s is nothing, and z^2 may be infinite
       value[i] = z[i] * s;
-      z[i] = fmaf(value[i] * (1.f - s), 2.f * kGeluIn * fmaf(3.f * kGeluCubic * z[i], z[i], 1.f), s);
+      z[i] = fmaf(value[i] * (1.f - s), 2.f * kGeluIn * fmaf(3.f * kGeluCubic * near, near, 1.f), s);
     }
   }
 }

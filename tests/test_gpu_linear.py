@@ -189,6 +189,12 @@ def test_values_that_are_not_numbers_stay_in_their_rows(lib):
     got = lib.psrl_linear_fwd(x, w, bias=d["bias"], activation="gelu", residual=d["residual"], mul=d["mul"])[0]
     rest = [i for i in range(300) if i not in (17, 200, 201)]
     assert torch.equal(got[rest], want[rest]) and torch.isnan(got[17]).all()
+    for act in ACTS:   # slopes far out: 0 on one side, 1 (or what the definition gives) on the other, for z of any size
+        z = torch.tensor([[-3e38, -1e20, -1e4, -200.0, 200.0, 1e4, 1e20, 3e38]], device="cuda", dtype=torch.bfloat16)
+        one = torch.ones_like(z)
+        dz = lib.psrl_linear_bwd(torch.zeros(1, 8, device="cuda", dtype=torch.bfloat16), torch.eye(8, device="cuda", dtype=torch.bfloat16), one, z=z, activation=act,
+                                 want_weight=False)[0]
+        assert dz.tolist() == [[0.0 if act else 1.0] * 4 + [1.0] * 4], (act, dz)
     for act in ACTS:   # large logits on both sides
         big = lib.psrl_linear_fwd((x[:16] * 1e4), w, activation=act)[0]
         z = to_np(x[:16] * 1e4) @ to_np(w).T
