@@ -582,6 +582,32 @@ def _cuda():
     return _torch_c
 
 
+_torch_calls = None
+
+
+def _calls():
+    """The module of csrc/torch_calls.cpp: the plain case of the calls below in one step (checks, outputs, C call).  It answers None
+    for any other case, which then takes the way through this file, and a status where the library refuses."""
+    global _torch_calls
+    if _torch_calls is None:
+        lib()
+        import torch  # noqa: F401  (its libraries)
+
+        try:
+            from . import _torch_calls as m
+        except ImportError as e:
+            raise RuntimeError(f"{_HERE}/_torch_calls.so cannot be loaded ({e}): build it with `python -m paper_2608_25683_b200.build`") from e
+        _torch_calls = m
+    return _torch_calls
+
+
+def _answer(r, name: str):
+    """The outputs, or the library's refusal."""
+    if type(r) is not tuple:
+        _check(r, name)
+    return r
+
+
 _torch_module = None
 
 
@@ -737,6 +763,11 @@ def psrl_rope_qkv_fwd(plan: Plan, rope: Rope, q, k, v, k_pool, v_pool, q_out=Non
 
 def psrl_rope_axes_qkv_fwd(plan: Plan, rope: Rope, positions, q, k, v, k_pool, v_pool, q_out=None, stream=None):
     """The same with int32 `positions` [axes, T_q] of the caller's own, a row for each axis of the rope."""
+    if stream is None and plan._dev is not None and plan._dev.get_device() == q.get_device():
+        r = (_torch_calls or _calls()).rope_axes_qkv_fwd(*_tree_args(plan, rope), positions, q, k, v, k_pool, v_pool, q_out)
+        if r is not None:
+            _answer(r, "psrl_rope_axes_qkv_fwd")
+            return r[0] if q_out is None else q_out
     return _rope_qkv_fwd("psrl_rope_axes_qkv_fwd", plan, rope, positions, q, k, v, k_pool, v_pool, q_out, stream)
 
 
@@ -748,7 +779,17 @@ def psrl_rope_qkv_bwd(plan: Plan, rope: Rope, d_q, dk_pool, dv_pool, dq_out=None
 
 def psrl_rope_axes_qkv_bwd(plan: Plan, rope: Rope, positions, d_q, dk_pool, dv_pool, dq_out=None, dk_out=None, dv_out=None, stream=None):
     """The same with int32 `positions` [axes, T_q], as in the forward."""
+    if stream is None and plan._dev is not None and plan._dev.get_device() == d_q.get_device():
+        r = (_torch_calls or _calls()).rope_axes_qkv_bwd(*_tree_args(plan, rope), positions, d_q, dk_pool, dv_pool, dq_out, dk_out, dv_out)
+        if r is not None:
+            return _answer(r, "psrl_rope_axes_qkv_bwd")
     return _rope_qkv_bwd("psrl_rope_axes_qkv_bwd", plan, rope, positions, d_q, dk_pool, dv_pool, dq_out, dk_out, dv_out, stream)
+
+
+def _tree_args(plan: Plan, rope: Rope):
+    """Handles and sizes as rope calls of csrc/torch_calls.cpp take them; None where there is no handle any more."""
+    return (plan._h.value, rope._h.value, rope.n_axes, PSRL_F32 if plan.dtype == "f32" else PSRL_BF16, plan.view["T_q"], plan.n_q_heads, plan.n_kv_heads,
+            plan.head_dim)
 
 
 def _axis_pitch(rope: Rope, positions, rows: int) -> int:
@@ -817,6 +858,10 @@ def psrl_rope_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stre
 
 def psrl_rope_axes_rows(rope: Rope, x, positions, y=None, inverse: bool = False, stream=None):
     """The same at `positions` [axes, rows], a row for each axis of the rope."""
+    if stream is None and y is None:
+        r = (_torch_calls or _calls()).rope_axes_rows(rope._h.value, rope.n_axes, rope.head_dim, x, positions, inverse)
+        if r is not None:
+            return _answer(r, "psrl_rope_axes_rows")[0]
     return _rope_rows("psrl_rope_axes_rows", rope, x, positions, (_axis_pitch(rope, positions, x.shape[0]),), y, inverse, stream)
 
 
@@ -1063,6 +1108,10 @@ def psrl_rms_norm_fwd(x, weight, eps: float = 1e-6, residual=None, y=None, summe
     """Root-mean-square norm of h = x + residual: x [rows, dim], or [rows, heads, dim] with a norm for each head (f32 or bf16, rows
     at any pitch), weight [dim] or None.  Returns (y, summed, codes, scales): summed = h where there is a residual, codes and scales
     the rows in 8 bits (float8_e4m3fn, a float32 scale for each) with want_codes; what is not wanted is None.  Outputs may be inputs."""
+    if stream is None and y is None and summed is None and codes is None and scales is None:
+        r = (_torch_calls or _calls()).rms_norm_fwd(x, weight, eps, residual, want_y, want_codes)
+        if r is not None:
+            return _answer(r, "psrl_rms_norm_fwd")
     dt, rows, heads, dim, dev = _norm_args(x, weight)
     shape, least = x.shape, heads * dim
     raw, keep = _stream_on(stream, dev)
@@ -1105,6 +1154,10 @@ def psrl_rms_norm_bwd(summed, weight, d_y, eps: float = 1e-6, d_summed=None, d_x
     """Gradients of the above: (d_x, d_weight) given the rows h that were normed (the forward's `summed`, or its x), d_y and, with a
     residual, the gradient d_summed that the stream brings back; d_x is the gradient of x and of residual.  d_x may be d_y or
     d_summed.  `workspace`: a Workspace of psrl_rms_norm_workspace_bytes(); made if not given."""
+    if stream is None and d_x is None and d_weight is None and workspace is None:
+        r = (_torch_calls or _calls()).rms_norm_bwd(summed, weight, d_y, eps, d_summed, want_x, want_weight)
+        if r is not None:
+            return _answer(r, "psrl_rms_norm_bwd")
     dt, rows, heads, dim, dev = _norm_args(summed, weight)
     shape = summed.shape
     raw, keep = _stream_on(stream, dev)
@@ -1223,6 +1276,10 @@ def psrl_linear_fwd(x, weight, bias=None, activation=None, mul=None, residual=No
     "gelu", "gelu_tanh".  Returns (y, z), z = x weight^T + bias with want_z (for the backward), else None.  y and z may be mul or
     residual.  `workspace`: a Workspace of psrl_linear_workspace_bytes(), whose status() tells whether a wait inside the kernel gave
     up; made if not given."""
+    if stream is None and y is None and z is None and workspace is None and activation in _ACTIVATIONS:
+        r = (_torch_calls or _calls()).linear_fwd(x, weight, bias, _ACTIVATIONS[activation], mul, residual, x_scale, weight_scale, want_z)
+        if r is not None:
+            return _answer(r, "psrl_linear_fwd")
     dt, m, k, n, dev, out = _linear_args(x, weight, activation)
     if dt == PSRL_E4M3:
         if x_scale is None or weight_scale is None:
@@ -1256,12 +1313,17 @@ def psrl_linear_bwd(x, weight, d_y, z=None, activation=None, mul=None, d_x=None,
     """Gradients of the above, f32 or bf16: (d_x, d_weight, d_bias, d_mul) given d_y and the forward's z (which may be None without an
     activation where d_mul is not wanted); what is not wanted is None, d_mul is wanted where there is a mul.  The gradient of residual
     is d_y.  `workspace` as above (backward True)."""
+    if want_mul is None:
+        want_mul = mul is not None
+    if (stream is None and d_x is None and d_weight is None and d_bias is None and d_mul is None and workspace is None and activation in _ACTIVATIONS
+            and (mul is not None or not want_mul)):
+        r = (_torch_calls or _calls()).linear_bwd(x, weight, d_y, z, _ACTIVATIONS[activation], mul, want_x, want_weight, want_bias, want_mul)
+        if r is not None:
+            return _answer(r, "psrl_linear_bwd")
     dt, m, k, n, dev, out = _linear_args(x, weight, activation)
     if dt == PSRL_E4M3:
         raise TypeError("8-bit operands have no backward")
-    if want_mul is None:
-        want_mul = mul is not None
-    elif want_mul and mul is None:
+    if want_mul and mul is None:
         raise ValueError("d_mul without a mul")
     raw, keep = _stream_on(stream, dev)
     a_d, p_d = _beside(d_y, m, n, out, dev, "d_y")

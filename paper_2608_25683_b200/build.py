@@ -1,13 +1,16 @@
-"""Builds libpsrl.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
+"""Builds libpsrl.so in-tree with nvcc for sm_100a (cross-compiles without a GPU), and the torch calls beside it."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpsrl.so")
+CALLS = os.path.join(HERE, "_torch_calls.so")   # a Python module: torch tensors to the library in one step
 SOURCES = ["plan.cpp", "cache.cpp", "sched.cpp", "api.cu", "attn_f32.cu", "attn_bf16_fwd.cu", "attn_bf16_bwd.cu", "attn_bf16_dq.cu", "attn_bf16_dkv.cu", "attn_bf16_merge.cu", "tma.cu", "bwd_static.cu", "kv_pack.cu", "rope.cu", "kv_move.cu", "logprob.cu", "rms_norm.cu", "linear.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -16,9 +19,9 @@ NVCC_FLAGS = [
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
     deps.append(os.path.join(HERE, "..", "include", "psrl.h"))
     deps.append(os.path.join(HERE, "..", "include", "psrl_cache.h"))
@@ -57,7 +60,20 @@ def build(force: bool = False, verbose: bool = False) -> str:
     tmp = LIB + ".tmp"
     subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", tmp, *objs, "-lcudart"])
     os.replace(tmp, LIB)
+    build_calls(nvcc)
     return LIB
+
+
+def build_calls(nvcc: str):
+    """csrc/torch_calls.cpp against the headers and libraries of the torch that is installed."""
+    torch_dir = list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+    cuda = os.path.join(os.path.dirname(os.path.dirname(nvcc)), "include")
+    include = [os.path.join(torch_dir, "include"), os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], cuda]
+    libs = ["-L" + os.path.join(torch_dir, "lib"), "-ltorch", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda", "-ltorch_python"]
+    tmp = CALLS + ".tmp"
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", *["-I" + i for i in include],
+                           os.path.join(CSRC, "torch_calls.cpp"), "-o", tmp, *libs, "-L" + HERE, "-l:libpsrl.so", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, CALLS)
 
 
 if __name__ == "__main__":

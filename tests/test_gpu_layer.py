@@ -172,3 +172,69 @@ def test_forward_with_8_bit_operands(lib):
     spread = float((f["y3"].double() @ w["head"].double().T).std(1).max())
     err = np.abs(to_np(lp) - ref_lp)
     assert err.max() <= 8 * 2.0 ** -4 * 4 * spread and np.sqrt((err ** 2).mean()) <= 8 * 2.0 ** -4 * spread
+
+
+def test_calls_in_one_step_are_the_calls(lib):
+    """The plain case of a call goes to the library in one step, any other through the wrapper (a stream given, a tensor's subclass, an
+    output given): the same bits, the same refusals."""
+    T = 70
+    plan = build_plan(lib, Workload("s", [-1, 0], [50, 20], [16], Hq, Hkv, D, "bf16"))
+    x, w, pos, _ = make(T, 4)
+    here = torch.cuda.current_stream()
+    rope = lib.Rope(D, base=BASE, sections=SECTIONS, order=ORDER)
+    same = lambda a, b: (a is None and b is None) or (a.shape == b.shape and a.dtype == b.dtype and torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8)))
+    class Sub(torch.Tensor):
+        pass
+    sub = x.as_subclass(Sub)
+    d = torch.randn(T, F, device="cuda").to(torch.bfloat16)
+    mul, z = d * 0.5, d * 0.25
+    wide = torch.randn(T, F + 24, device="cuda").to(torch.bfloat16)
+    codes, scales = lib.psrl_quantize_rows(x)
+    wc, ws = lib.psrl_quantize_rows(w["up"])
+    calls = [
+        (lib.psrl_rms_norm_fwd, (x, w["norm1"]), dict(eps=EPS, residual=x, want_codes=True)),
+        (lib.psrl_rms_norm_fwd, (wide[:, 8:8 + F], None), dict(want_y=0, want_codes=1)),
+        (lib.psrl_rms_norm_fwd, (x.view(T, 4, 128)[:, 1:3], w["q_norm"]), dict(want_codes=True)),
+        (lib.psrl_rms_norm_fwd, (x.view(-1, 8), None), dict(want_codes=True)),        # codes 16 bytes apart: not the plain case
+        (lib.psrl_rms_norm_bwd, (x, w["norm1"], x * 0.5), dict(eps=EPS, d_summed=x)),
+        (lib.psrl_rms_norm_bwd, (x, None, x * 0.5), dict()),
+        (lib.psrl_rms_norm_bwd, (x, w["norm1"], x * 0.5), dict(want_x=False)),
+        (lib.psrl_linear_fwd, (x, w["up"]), dict(mul=mul, residual=wide[:, 16:16 + F], activation="gelu", want_z=True)),
+        (lib.psrl_linear_fwd, (codes, wc), dict(x_scale=scales, weight_scale=ws)),
+        (lib.psrl_linear_fwd, (x, w["head"]), dict()),                                 # 701 columns
+        (lib.psrl_linear_fwd, (x.float(), w["head"].float()), dict(activation="silu")),
+        (lib.psrl_linear_bwd, (x, w["up"], d), dict(z=z, activation="silu", mul=mul, want_bias=True)),
+        (lib.psrl_linear_bwd, (x, w["up"], d), dict(want_x=False)),
+        (lib.psrl_linear_bwd, (x.float(), w["up"].float(), d.float()), dict(want_bias=True)),
+        (lib.psrl_linear_fwd, (x[:0], w["up"]), dict(want_z=True)),
+        (lib.psrl_rms_norm_fwd, (x[:0], w["norm1"]), dict(want_codes=True)),
+    ]
+    for f, args, kw in calls:
+        got, want = f(*args, **kw), f(*args, **kw, stream=here)
+        torch.cuda.synchronize()
+        assert len(got) == len(want) and all(same(a, b) for a, b in zip(got, want)), (f.__name__, kw)
+    assert all(same(a, b) for a, b in zip(lib.psrl_linear_fwd(sub, w["up"]), lib.psrl_linear_fwd(x, w["up"])))
+    q, k, v = (torch.randn(T, h, D, device="cuda").to(torch.bfloat16) for h in (Hq, Hkv, Hkv))
+    pools = lambda: [torch.zeros(Hkv, plan.oracle["pool_slots"], D, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    a, b = pools(), pools()
+    assert same(lib.psrl_rope_axes_qkv_fwd(plan, rope, pos, q, k, v, *a), lib.psrl_rope_axes_qkv_fwd(plan, rope, pos, q, k, v, *b, stream=here))
+    torch.cuda.synchronize()
+    assert same(a[0], b[0]) and same(a[1], b[1])
+    for got, want in zip(lib.psrl_rope_axes_qkv_bwd(plan, rope, pos, q, *a), lib.psrl_rope_axes_qkv_bwd(plan, rope, pos, q, *a, stream=here)):
+        torch.cuda.synchronize()
+        assert same(got, want)
+    got, want = lib.psrl_rope_axes_rows(rope, q, pos, inverse=1), lib.psrl_rope_axes_rows(rope, q, pos, inverse=True, stream=here)
+    torch.cuda.synchronize()
+    assert same(got, want)
+    # a plan of another type, one that is not uploaded, one that is closed
+    f32 = build_plan(lib, Workload("s", [-1, 0], [50, 20], [16], Hq, Hkv, D, "f32"))
+    with pytest.raises(TypeError):
+        lib.psrl_rope_axes_qkv_fwd(f32, rope, pos, q, k, v, *a)
+    fresh = lib.Plan([-1, 0], [50, 20], [16], Hq, Hkv, D, "bf16")
+    with pytest.raises(lib.PsrlError) as e:
+        lib.psrl_rope_axes_qkv_fwd(fresh, rope, pos, q, k, v, *a)
+    assert e.value.name == "PSRL_ERR_WORKSPACE"
+    fresh.upload().close()
+    with pytest.raises(lib.PsrlError) as e:
+        lib.psrl_rope_axes_qkv_fwd(fresh, rope, pos, q, k, v, *a)
+    assert e.value.name == "PSRL_ERR_INVALID_ARG"
