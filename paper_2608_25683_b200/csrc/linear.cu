@@ -855,23 +855,6 @@ int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t dz_rows(int64_t M) { return std::max<int64_t>(kDzRows, div_up(M, 65535)); }   // at most 65,535 blocks of rows
 
-// Every kernel here may start before the one before it on the stream has ended, and touches memory behind previous_kernel_done() only: its
-// barriers and tensor memory are laid out meanwhile (1 row x 1024 x 1024 5.7 -> 4.2 us, 4096 x 4096 10.7 -> 9.0).
-template <class... P, class... A>
-cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, const A&... args) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-}
-
 template <bool kFp8, Epilogue kEpilogue>
 cudaError_t launch_gemm(const Maps& maps, const Params& p, cudaStream_t stream) {
   static bool done[64] = {};

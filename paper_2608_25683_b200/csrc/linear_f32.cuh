@@ -6,10 +6,27 @@
 // parts' sums are added in order by a second kernel, with the epilogue.
 #pragma once
 #include "linear_act.cuh"
-#include "sm100.cuh"
+#include "sm100_pair.cuh"
 
 namespace psrl {
 namespace {
+
+// Every kernel here may start before the one before it on the stream has ended, and touches memory behind previous_kernel_done() only: its
+// barriers and tensor memory are laid out meanwhile (1 row x 1024 x 1024 5.7 -> 4.2 us, 4096 x 4096 10.7 -> 9.0).
+template <class... P, class... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
 
 struct F32Operand {
   const float* at;
@@ -23,39 +40,60 @@ struct F32Epilogue {
 };
 struct F32Params {
   F32Operand a, b;
-  int32_t M, N, depth, slice;   // depth of a part, a multiple of kF32Depth
-  float* part;                  // [parts][M][N], or NULL: the epilogue here
+  int32_t M, N, depth, slice;   // depth of a part, a multiple of 32
+  float* part;                  // [parts][M][part_pitch], or NULL: the epilogue here
+  int64_t part_pitch;           // N in whole fours
   int32_t m_tiles;
   F32Epilogue e;
   int* status;
 };
 
-constexpr int kF32Depth = 16;
+// Depth of a slice in shared memory: the small tile's few products would not cover the way of shorter ones from memory.
+constexpr int f32_depth(int tile) { return tile == 64 ? 32 : 16; }
 
-__device__ __forceinline__ void f32_finish(const F32Epilogue& e, int64_t m, int64_t n, float v) {
-  if (e.bias) v += e.bias[n];
-  if (e.z) {
-    // z may lie over mul or residual
-    const float mul = e.mul ? e.mul[m * e.mul_pitch + n] : 1.f, res = e.residual ? e.residual[m * e.residual_pitch + n] : 0.f;
-    e.z[m * e.z_pitch + n] = v;
-    float o[1] = {v};
-    activate(o, e.act);
-    if (e.mul) o[0] *= mul;
-    if (e.residual) o[0] += res;
-    e.y[m * e.y_pitch + n] = o[0];
-    return;
+// The epilogue of four numbers from a multiple of four columns, or of the `left` that there are.  z may lie over mul or residual, so
+// both are read first.
+__device__ __forceinline__ void f32_read(const float* at, int left, float (&o)[4]) {
+  if (left >= 4) {
+    const float4 v = *reinterpret_cast<const float4*>(at);
+    o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = i < left ? at[i] : 0.f;
   }
-  float o[1] = {v};
-  activate(o, e.act);
-  if (e.mul) o[0] *= e.mul[m * e.mul_pitch + n];
-  if (e.residual) o[0] += e.residual[m * e.residual_pitch + n];
-  e.y[m * e.y_pitch + n] = o[0];
+}
+__device__ __forceinline__ void f32_write(float* at, int left, const float (&o)[4]) {
+  if (left >= 4) {
+    *reinterpret_cast<float4*>(at) = make_float4(o[0], o[1], o[2], o[3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < left) at[i] = o[i];
+  }
+}
+__device__ __forceinline__ void f32_finish(const F32Epilogue& e, int64_t m, int64_t n, int left, float (&v)[4]) {
+  float mul[4], res[4], bias[4];
+  if (e.mul) f32_read(e.mul + m * e.mul_pitch + n, left, mul);
+  if (e.residual) f32_read(e.residual + m * e.residual_pitch + n, left, res);
+  if (e.bias) {
+    f32_read(e.bias + n, left, bias);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += bias[i];
+  }
+  if (e.z) f32_write(e.z + m * e.z_pitch + n, left, v);
+  activate(v, e.act);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (e.mul) v[i] *= mul[i];
+    if (e.residual) v[i] += res[i];
+  }
+  f32_write(e.y + m * e.y_pitch + n, left, v);
 }
 
-// A thread's vectors of a kTile x kF32Depth slice: along the depth (K-major) or along the tile.
+// A thread's vectors of a slice of kTile rows: along the depth (K-major) or along the tile.
 template <int kTile, bool kMn>
 struct F32Slice {
-  static constexpr int kVecs = kTile * kF32Depth / 4 / 256;
+  static constexpr int kF32Depth = f32_depth(kTile), kVecs = kTile * kF32Depth / 4 / 256;
   float4 v[kVecs];
 
   __device__ __forceinline__ static void place(int i, int& row, int& k) {
@@ -109,7 +147,9 @@ struct F32Slice {
 template <int kTile, bool kAMn, bool kBMn>
 __global__ void __launch_bounds__(256) linear_f32_kernel(const __grid_constant__ F32Params p) {
   using namespace sm100;
-  constexpr int kRuns = kTile / 64;
+  constexpr int kRuns = kTile / 64, kF32Depth = f32_depth(kTile);
+  previous_kernel_done();
+  next_kernel_may_start();
   __shared__ __align__(16) float sa[2][kF32Depth][kTile + 4], sb[2][kF32Depth][kTile + 4];
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
   const int mt = int(blockIdx.x) % p.m_tiles, nt = int(blockIdx.x) / p.m_tiles;
@@ -175,24 +215,28 @@ __global__ void __launch_bounds__(256) linear_f32_kernel(const __grid_constant__
         float v[4];
         split_f32x2(acc[r * 4 + i][c * 2], v[0], v[1]);
         split_f32x2(acc[r * 4 + i][c * 2 + 1], v[2], v[3]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (n + e >= p.N) continue;
-          if (p.part) p.part[(int64_t(blockIdx.y) * p.M + m) * p.N + n + e] = v[e];
-          else f32_finish(p.e, m, n + e, v[e]);
-        }
+        const int left = p.N - n;
+        if (left <= 0) continue;
+        if (p.part) f32_write(p.part + (int64_t(blockIdx.y) * p.M + m) * p.part_pitch + n, left, v);
+        else f32_finish(p.e, m, n, left, v);
       }
     }
 }
 
-// The parts' sums added in order, and the epilogue: one thread per number.
+// The parts' sums added in order, and the epilogue: one thread for four numbers.
 __global__ void __launch_bounds__(256) linear_f32_join_kernel(const float* __restrict__ part, int parts, int M, int N, const __grid_constant__ F32Epilogue e) {
-  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x, all = int64_t(M) * N;
+  sm100::previous_kernel_done();
+  sm100::next_kernel_may_start();
+  const int fours = (N + 3) / 4;
+  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x, all = int64_t(M) * fours;
   if (at >= all) return;
-  float v = 0.f;
-  for (int i = 0; i < parts; ++i) v += part[i * all + at];
-  const int64_t m = at / N;
-  f32_finish(e, m, at - m * N, v);
+  float v[4] = {};
+  for (int i = 0; i < parts; ++i) {
+    const float4 x = reinterpret_cast<const float4*>(part)[i * all + at];
+    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+  }
+  const int64_t m = at / fours, n = (at - m * fours) * 4;
+  f32_finish(e, m, n, int(N - n < 4 ? N - n : 4), v);
 }
 
 // The tile and the parts of the depth that a product is cut into.
@@ -204,17 +248,18 @@ inline F32Shape f32_shape(int64_t M, int64_t N, int64_t depth) {
   const int64_t sms = resident_ctas();
   F32Shape s{};
   auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-  s.tile = tiles(128) >= sms ? 128 : 64;
-  // two blocks for every SM, of at least eight slices each
-  const int64_t want = std::max<int64_t>(1, 2 * sms / tiles(s.tile)), most = std::max<int64_t>(1, depth / (8 * kF32Depth));
+  // 1000 x 2048 x 2048: large tiles 224 us, small ones 299; 253 x 1568 x 1202, the depth cut in seven, 41 and 81; 381 x 416 x 830 32 and 29
+  s.tile = tiles(128) >= sms || (depth >= 1024 && double(M) * double(N) * double(depth) >= 4e8) ? 128 : 64;
+  // two blocks for every SM, of at least 64 deep each
+  const int64_t want = std::max<int64_t>(1, 2 * sms / tiles(s.tile)), most = std::max<int64_t>(1, depth / 64);
   const int64_t parts = std::min(want, most);
-  s.slice = ((depth + parts - 1) / parts + kF32Depth - 1) / kF32Depth * kF32Depth;
+  s.slice = ((depth + parts - 1) / parts + 31) / 32 * 32;
   s.parts = int((depth + s.slice - 1) / s.slice);
   return s;
 }
 inline size_t f32_part_bytes(int64_t M, int64_t N, int64_t depth) {
   const F32Shape s = f32_shape(M, N, depth);
-  return s.parts > 1 ? size_t(s.parts) * M * N * sizeof(float) : 0;
+  return s.parts > 1 ? size_t(s.parts) * M * ((N + 3) / 4 * 4) * sizeof(float) : 0;
 }
 
 template <bool kAMn, bool kBMn>
@@ -222,17 +267,14 @@ cudaError_t f32_product(F32Params p, float* part, cudaStream_t stream) {
   const F32Shape s = f32_shape(p.M, p.N, p.depth);
   p.slice = int32_t(s.slice);
   p.part = s.parts > 1 ? part : nullptr;
+  p.part_pitch = (int64_t(p.N) + 3) / 4 * 4;
   p.m_tiles = (p.M + s.tile - 1) / s.tile;
   const int64_t tiles = int64_t(p.m_tiles) * ((p.N + s.tile - 1) / s.tile);
   if (tiles > INT32_MAX) return cudaErrorInvalidValue;
   const dim3 grid(static_cast<unsigned>(tiles), unsigned(s.parts));
-  if (s.tile == 128) linear_f32_kernel<128, kAMn, kBMn><<<grid, 256, 0, stream>>>(p);
-  else linear_f32_kernel<64, kAMn, kBMn><<<grid, 256, 0, stream>>>(p);
-  cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess && s.parts > 1) {
-    linear_f32_join_kernel<<<unsigned((int64_t(p.M) * p.N + 255) / 256), 256, 0, stream>>>(part, s.parts, p.M, p.N, p.e);
-    e = cudaGetLastError();
-  }
+  cudaError_t e = launch(s.tile == 128 ? linear_f32_kernel<128, kAMn, kBMn> : linear_f32_kernel<64, kAMn, kBMn>, grid, 256, 0, stream, p);
+  if (e == cudaSuccess && s.parts > 1)
+    e = launch(linear_f32_join_kernel, dim3(unsigned((int64_t(p.M) * (p.part_pitch / 4) + 255) / 256)), 256, 0, stream, part, s.parts, p.M, p.N, p.e);
   return e;
 }
 
