@@ -60,6 +60,7 @@ struct Params {
   const __nv_bfloat16* bias;
   const float *x_scale, *w_scale;
   int32_t act, has_mul, has_residual, has_z;
+  int32_t share;                // no pair has more than one tile
   int* status;
 };
 
@@ -298,9 +299,10 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
     }
   } else {
     // ======================= epilogue: one thread per row, a group for every other tile =======================
+    // Where no pair has a second tile, the groups share the one: every other 64 columns of it.
     const int group = warp >> 2, gt = tid & 127;
     const uint32_t bar_id = kBarGroup + group;
-    const uint32_t lane_addr = tmem + (uint32_t(warp & 3) << 21) + group * 256;   // lane 32 * (warp % 4)
+    const uint32_t lane_addr = tmem + (uint32_t(warp & 3) << 21) + (p.share ? 0 : group * 256);   // lane 32 * (warp % 4)
     const uint32_t acc_empty = in_leader(&bar.acc_empty[group]);
     uint8_t* buf = smem + kStages * kStageBytes + group * kBuffers * kOutBytes;
     const bool has_second = kEpilogue == kFull && (p.has_mul || p.has_z);
@@ -310,10 +312,11 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
     uint32_t tile = 0;
     bool ok = true;
     for (int i = 0; ok && plan.get(p, cluster, n_clusters, i, which, mt, nt); ++i, ++tile) {
-      if ((tile & 1) != uint32_t(group)) continue;
+      if (!p.share && (tile & 1) != uint32_t(group)) continue;
       const Product& q = p.product[which];
       const int row0 = mt * 256 + int(rank) * 128, n0 = nt * q.tile_n, n_end = min(n0 + q.tile_n, q.N);
-      const int chunks = row0 < q.M ? (n_end - n0 + 63) / 64 : 0;
+      const int chunk0 = p.share ? group : 0, stride = p.share ? 128 : 64;   // columns from one of this group's chunks to the next
+      const int all = row0 < q.M ? (n_end - n0 + 63) / 64 : 0, chunks = p.share ? (all + 1 - group) / 2 : all;
       int issued = 0;
       // thread 0: loads into the buffers of uses up to `until` of this tile, which are free
       auto issue = [&](int until) {
@@ -323,7 +326,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
           if (kEpilogue == kPlain || !(of_mul ? p.has_mul : p.has_residual)) continue;
           const int b = int((base + issued) % kBuffers);
           mbar_expect_tx(&bar.in[group][b], kOutBytes);
-          tma_load_2d(buf + b * kOutBytes, of_mul ? &maps.mul : &maps.residual, &bar.in[group][b], n0 + issued / per * 64, row0);
+          tma_load_2d(buf + b * kOutBytes, of_mul ? &maps.mul : &maps.residual, &bar.in[group][b], n0 + chunk0 * 64 + issued / per * stride, row0);
         }
       };
       if (kEpilogue == kFull && gt == 0) {
@@ -332,7 +335,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
       }
       // one warp waits for its group: the four leave together if the wait gives up, so none is missed at their barrier
       if ((warp & 3) == 0) {
-        ok = mbar_wait(&bar.acc_full[group], (tile >> 1) & 1, abortp, p.status);
+        ok = mbar_wait(&bar.acc_full[p.share ? 0 : group], (tile >> 1) & 1, abortp, p.status);
         if (lane == 0) s_go[group][go & 1] = ok;
       }
       named_sync(bar_id, kGroupThreads);
@@ -342,11 +345,11 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
       const float sx = kFp8 && row0 + gt < q.M ? p.x_scale[row0 + gt] : 1.f;
 #pragma unroll 1
       for (int c = 0; c < chunks; ++c) {
-        const int col = n0 + c * 64;
+        const int at_col = chunk0 * 64 + c * stride, col = n0 + at_col;
         const uint32_t n = base + uint32_t(c * per);
         uint32_t r[2][32];
-        tmem_ld32(lane_addr + c * 64, r[0]);
-        tmem_ld32(lane_addr + c * 64 + 32, r[1]);
+        tmem_ld32(lane_addr + at_col, r[0]);
+        tmem_ld32(lane_addr + at_col + 32, r[1]);
         if ((warp & 3) == 0) {
           if (gt == 0) {
             // the buffers of this chunk: free, and with their loads under way
@@ -856,7 +859,7 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t dz_rows(int64_t M) { return std::max<int64_t>(kDzRows, div_up(M, 65535)); }   // at most 65,535 blocks of rows
 
 template <bool kFp8, Epilogue kEpilogue>
-cudaError_t launch_gemm(const Maps& maps, const Params& p, cudaStream_t stream) {
+cudaError_t launch_gemm(const Maps& maps, Params& p, cudaStream_t stream) {
   static bool done[64] = {};
   cudaError_t e = ensure_dynamic_smem(linear_kernel<kFp8, kEpilogue>, gemm_smem(kEpilogue), done);
   if (e != cudaSuccess) return e;
@@ -864,6 +867,7 @@ cudaError_t launch_gemm(const Maps& maps, const Params& p, cudaStream_t stream) 
   for (const Product& q : p.product) tiles += int64_t(q.m_tiles) * q.n_tiles;
   if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int clusters = static_cast<int>(std::min<int64_t>(tiles, resident_ctas() / 2));
+  p.share = tiles <= clusters;
   return launch(linear_kernel<kFp8, kEpilogue>, dim3(2 * clusters), kGemmThreads, gemm_smem(kEpilogue), stream, maps, p);
 }
 
