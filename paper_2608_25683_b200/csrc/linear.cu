@@ -13,6 +13,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/psrl.h"
 #include "attn_bf16_common.cuh"
@@ -644,7 +645,7 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
   }
   if (p.splits > 1) cluster_sync();
   else __syncthreads();
-  // Row r belongs to rank r % splits: a warp takes two of the rank's rows at a time, a lane four columns of each.
+  // Row r belongs to rank r % splits: a warp takes several of the rank's rows at a time, a lane four columns of each.
   const int col = col0 + lane * 4, left = p.cols - col;
   if (left > 0 && !s_abort) {
     float bias[4] = {}, scale[4] = {1.f, 1.f, 1.f, 1.f};
@@ -653,47 +654,53 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
 #pragma unroll
       for (int e = 0; e < 4; ++e) scale[e] = e < left ? p.w_scale[col + e] : 0.f;
     }
-    constexpr int kRowsAtOnce = 2, kWarps = kFewThreads / 32;
-    for (int r0 = int(rank) + p.splits * warp; r0 < rows; r0 += p.splits * kWarps * kRowsAtOnce) {
-      float v[kRowsAtOnce][4], mul[kRowsAtOnce][4], res[kRowsAtOnce][4], sx[kRowsAtOnce];
+    // with many parts to add there are few rows for each rank, and the other way round
+    auto rows_of_rank = [&](auto rows_at_once, auto most_parts) {
+      constexpr int kRows = decltype(rows_at_once)::value, kParts = decltype(most_parts)::value, kWarps = kFewThreads / 32;
+      for (int r0 = int(rank) + p.splits * warp; r0 < rows; r0 += p.splits * kWarps * kRows) {
+        float v[kRows][4], mul[kRows][4], res[kRows][4];
+        [[maybe_unused]] float sx[kRows];
+        float4 part[kRows][kParts];
 #pragma unroll
-      for (int i = 0; i < kRowsAtOnce; ++i) {
-        const int r = r0 + i * p.splits * kWarps;
-        if (r >= rows) break;
-        const int64_t row = row0 + r;
-        if (p.mul) load4(p.mul + row * p.mul_pitch + col, left, mul[i]);
-        if (p.residual) load4(p.residual + row * p.residual_pitch + col, left, res[i]);
-        if constexpr (kFp8) sx[i] = p.x_scale[row];
-        const uint32_t at = smem_u32(sums + r * 128 + lane * 4);
-        float4 part[kFewMaxSplit];
+        for (int i = 0; i < kRows; ++i) {
+          const int r = r0 + i * p.splits * kWarps;
+          if (r >= rows) break;
+          const int64_t row = row0 + r;
+          if (p.mul) load4(p.mul + row * p.mul_pitch + col, left, mul[i]);
+          if (p.residual) load4(p.residual + row * p.residual_pitch + col, left, res[i]);
+          if constexpr (kFp8) sx[i] = p.x_scale[row];
+          const uint32_t at = smem_u32(sums + r * 128 + lane * 4);
 #pragma unroll
-        for (int k = 0; k < kFewMaxSplit; ++k)
-          if (k < p.splits) part[k] = p.splits > 1 ? load_cluster(in_rank(at, uint32_t(k))) : *reinterpret_cast<const float4*>(sums + r * 128 + lane * 4);
-        v[i][0] = part[0].x; v[i][1] = part[0].y; v[i][2] = part[0].z; v[i][3] = part[0].w;
-#pragma unroll
-        for (int k = 1; k < kFewMaxSplit; ++k)
-          if (k < p.splits) { v[i][0] += part[k].x; v[i][1] += part[k].y; v[i][2] += part[k].z; v[i][3] += part[k].w; }
-      }
-#pragma unroll
-      for (int i = 0; i < kRowsAtOnce; ++i) {
-        const int r = r0 + i * p.splits * kWarps;
-        if (r >= rows) break;
-        const int64_t row = row0 + r;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (kFp8) v[i][e] *= sx[i] * scale[e];
-          if (p.bias) v[i][e] += bias[e];
+          for (int k = 0; k < kParts; ++k)
+            if (k < p.splits) part[i][k] = p.splits > 1 ? load_cluster(in_rank(at, uint32_t(k))) : *reinterpret_cast<const float4*>(sums + r * 128 + lane * 4);
         }
-        if (p.z) store4(p.z + row * p.z_pitch + col, left, v[i]);
-        activate(v[i], p.act);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (p.mul) v[i][e] *= mul[i][e];
-          if (p.residual) v[i][e] += res[i][e];
+        for (int i = 0; i < kRows; ++i) {
+          const int r = r0 + i * p.splits * kWarps;
+          if (r >= rows) break;
+          const int64_t row = row0 + r;
+          v[i][0] = part[i][0].x; v[i][1] = part[i][0].y; v[i][2] = part[i][0].z; v[i][3] = part[i][0].w;
+#pragma unroll
+          for (int k = 1; k < kParts; ++k)
+            if (k < p.splits) { v[i][0] += part[i][k].x; v[i][1] += part[i][k].y; v[i][2] += part[i][k].z; v[i][3] += part[i][k].w; }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (kFp8) v[i][e] *= sx[i] * scale[e];
+            if (p.bias) v[i][e] += bias[e];
+          }
+          if (p.z) store4(p.z + row * p.z_pitch + col, left, v[i]);
+          activate(v[i], p.act);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (p.mul) v[i][e] *= mul[i][e];
+            if (p.residual) v[i][e] += res[i][e];
+          }
+          store4(p.y + row * p.y_pitch + col, left, v[i]);
         }
-        store4(p.y + row * p.y_pitch + col, left, v[i]);
       }
-    }
+    };
+    if (p.splits <= 2) rows_of_rank(std::integral_constant<int, 6>(), std::integral_constant<int, 2>());
+    else rows_of_rank(std::integral_constant<int, 2>(), std::integral_constant<int, kFewMaxSplit>());
   }
   if (p.splits > 1) cluster_sync();   // the others are done with this CTA's sums
   tc_fence_before();
@@ -904,12 +911,18 @@ FewShape few_shape(int64_t rows, int64_t cols, int64_t steps) {
   f.tile_rows = int(round_up(div_up(rows, f.row_tiles), 16));
   f.col_tiles = div_up(cols, 128);
   const int64_t tiles = f.row_tiles * f.col_tiles, sms = resident_ctas();
-  const size_t stage = kOperandBytes + size_t(f.tile_rows) * kRowBytes;
   // two CTAs an SM, so that one's loads run under the other's beginning and end
   const size_t room = 111 * 1024;
-  f.stages = int(std::min<size_t>(kFewMaxStages, room / stage));
+  f.stages = int(std::min<size_t>(kFewMaxStages, room / (kOperandBytes + size_t(f.tile_rows) * kRowBytes)));
   f.splits = 1;
   while (f.splits < kFewMaxSplit && tiles * f.splits * 2 <= 2 * sms && steps / (f.splits * 2) >= 4) f.splits *= 2;
+  // shallow and narrow products: rows in smaller tiles, for the epilogue's sake
+  while (f.tile_rows > 16 && f.row_tiles * f.col_tiles * f.splits * 2 <= sms) {
+    f.tile_rows = int(round_up(f.tile_rows / 2, 16));
+    f.row_tiles = div_up(rows, f.tile_rows);
+    f.stages = int(std::min<size_t>(kFewMaxStages, room / (kOperandBytes + size_t(f.tile_rows) * kRowBytes)));
+  }
+  const size_t stage = kOperandBytes + size_t(f.tile_rows) * kRowBytes;
   f.smem = std::max(size_t(f.stages) * stage, size_t(f.tile_rows) * 128 * sizeof(float)) + 1024;
   return f;
 }
