@@ -284,7 +284,9 @@ def flush_l2(device):
 def operators_leg(lib, r, w, V, device, pk, vocab=131072, most_rows=16384):
     """The steps around the attention on this workload's tree: rotary positions fused with the pools (both directions), a
     compaction that moves every slot behind the first sixteen, and the log-probabilities of the rows' next tokens with their
-    gradients over a vocabulary of `vocab` (at most `most_rows` rows, hidden width Hq * d)."""
+    gradients over a vocabulary of `vocab` (at most `most_rows` rows, hidden width Hq * d); and the rest of a layer: the norm onto the
+    residual stream and its gradients, rotary positions with three axes, Q, K and V in one product with bias in bf16 and in 8 bits, and
+    the gradients of that product (bf16 workloads only)."""
     import torch
 
     T, d, dt = V["T_q"], w.head_dim, r.k.dtype
@@ -320,6 +322,26 @@ def operators_leg(lib, r, w, V, device, pk, vocab=131072, most_rows=16384):
         tf = n * rows * h * vocab / (ms * 1e-3) / 1e12
         out[name] = {"ms": round(ms, 4), "rows": rows, "hidden": h, "vocab": vocab, "tflops": round(tf, 1),
                      "frac_of_bf16_peak": {"burst": round(tf / pk["bf16_tflops"], 4), "sustained": round(tf / pk["bf16_tflops_sustained"], 4)}}
+    del hidden, weight, grad
+    if dt != torch.bfloat16:
+        return out
+    x, res, gain = rnd(rows, h), rnd(rows, h), rnd(h)
+    y, summed, codes, scales = lib.psrl_rms_norm_fwd(x, gain, residual=res, want_codes=True)
+    hbm("rms_fwd", 8 * rows * h, lambda: lib.psrl_rms_norm_fwd(x, gain, residual=res))
+    hbm("rms_bwd", 8 * rows * h, lambda: lib.psrl_rms_norm_bwd(summed, gain, y, d_summed=res))
+    axes = lib.Rope(d, base=1000000.0, sections=[d // 2 - 2 * (d // 6), d // 6, d // 6], order="cyclic")
+    positions = torch.randint(0, 4096, (3, rows), device=device, dtype=torch.int32)
+    heads = x.view(rows, w.n_q_heads, d)
+    hbm("rope_axes_rows", 4 * rows * h, lambda: lib.psrl_rope_axes_rows(axes, heads, positions))
+    n = (w.n_q_heads + 2 * w.n_kv_heads) * d
+    qkv, bias = rnd(n, h) * (1.0 / np.sqrt(h)), rnd(n)
+    qkv8, qkv8_scale = lib.psrl_quantize_rows(qkv)
+    grad = rnd(rows, n)
+    for name, k, fn in (("linear_fwd", 2, lambda: lib.psrl_linear_fwd(y, qkv, bias=bias)),
+                        ("linear_fwd_8bit", 2, lambda: lib.psrl_linear_fwd(codes, qkv8, bias=bias, x_scale=scales, weight_scale=qkv8_scale)),
+                        ("linear_bwd", 4, lambda: lib.psrl_linear_bwd(y, qkv, grad, want_bias=True))):
+        ms = time_region(fn, 10, 2)
+        out[name] = {"ms": round(ms, 4), "rows": rows, "in": h, "out": n, "tflops": round(k * rows * h * n / (ms * 1e-3) / 1e12, 1)}
     return out
 
 
@@ -921,7 +943,8 @@ def main():
                     help="scale every segment length (tree shape and prefix match rate unchanged, cf. Sec. 7.5)")
     ap.add_argument("--pack", action="store_true", help="also time K/V scatter into the pools and the gather back")
     ap.add_argument("--operators", action="store_true",
-                    help="also time the steps around the attention: rotary positions with the pools, compacting the arena, token log-probabilities")
+                    help="also time the steps around the attention: rotary positions with the pools, compacting the arena, token log-probabilities, "
+                         "norms and products")
     ap.add_argument("--schedule", action="store_true",
                     help="also fit Eq. 1 to measured times and compare load-balanced with round-robin group placement")
     ap.add_argument("--microbatch", action="store_true",
