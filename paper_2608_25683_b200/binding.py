@@ -1,7 +1,8 @@
 """ctypes binding of libpsrl.so: same names as the C ABI, argument marshalling only.
 
 Every step of the path runs inside the library's kernels.  The binding raises
-if the library has not been built; there is no fallback of any kind.
+if the library has not been built; there is no fallback of any kind.  Calls
+whose kernels take a few microseconds have their plain case in csrc/torch_calls.cpp.
 """
 from __future__ import annotations
 
