@@ -408,7 +408,7 @@ psrl_status_t psrl_rope_axes_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, c
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), WORKSPACE, CUDA.  Asynchronous.
  *
  * psrl_quantize_rows - the 8-bit output alone, of rows as they are (a weight matrix, laid out once): codes = e4m3(x / scale),
- * scale = max(amax |x| / 448, 2^-126).
+ * scale = max(amax |x| / 448, 2^-126); a row that holds NaN or an infinity has NaN in all its codes and its scale.
  */
 psrl_status_t psrl_rms_norm_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim, const void* x, int64_t x_pitch,
                                 const void* residual, int64_t residual_pitch, const void* weight, float eps, void* summed,

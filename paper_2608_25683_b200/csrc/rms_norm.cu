@@ -12,6 +12,7 @@
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
 #include <float.h>
+#include <math_constants.h>
 
 #include <algorithm>
 
@@ -267,7 +268,7 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __gri
     }
     if constexpr (kCodes) {
       amax = join<kGroup>(amax, MaxNan(), s_sum[turn][2]);
-      const float scale = max_nan(amax / kCodeMax, kLeastScale);
+      const float scale = too_large(amax) ? CUDART_NAN_F : max_nan(amax / kCodeMax, kLeastScale);   // an infinity has no code
       const float inv = 1.f / scale;
       uint8_t* c = p.codes + this_row * p.codes_pitch + int64_t(this_head) * p.vecs * kE;
 #pragma unroll

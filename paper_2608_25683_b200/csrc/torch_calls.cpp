@@ -12,6 +12,7 @@
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <optional>
@@ -112,17 +113,12 @@ PyObject* answer(psrl_status_t st, const T&... out) {
 
 int code_of(at::ScalarType t) { return t == at::kFloat ? PSRL_F32 : t == at::kBFloat16 ? PSRL_BF16 : t == at::kFloat8_e4m3fn ? PSRL_E4M3 : -1; }
 
-// No C++ exception leaves a function: torch's allocator throws when memory is out.
+// No C++ exception leaves a function: they turn into torch's own Python errors (memory that is out among them).
 template <class F>
 PyObject* guarded(F f) {
-  try {
-    return f();
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-  } catch (...) {
-    PyErr_SetString(PyExc_RuntimeError, "a call failed in C++");
-  }
-  return nullptr;
+  HANDLE_TH_ERRORS
+  return f();
+  END_HANDLE_TH_ERRORS
 }
 
 bool int_of(PyObject* o, int64_t& v) {

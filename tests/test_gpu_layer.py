@@ -238,3 +238,7 @@ def test_calls_in_one_step_are_the_calls(lib):
     with pytest.raises(lib.PsrlError) as e:
         lib.psrl_rope_axes_qkv_fwd(fresh, rope, pos, q, k, v, *a)
     assert e.value.name == "PSRL_ERR_INVALID_ARG"
+    # memory that is out is torch's error
+    tall = torch.zeros(1 << 20, 8, device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(torch.OutOfMemoryError):
+        lib.psrl_linear_fwd(tall, tall)

@@ -145,6 +145,12 @@ def test_quantised_rows(lib, dtype, rows, dim):
     got = codes.float().double().cpu().numpy() * s[:, None]
     assert (np.abs(got - v) <= (2.0 ** -4 * np.abs(v) + 2.0 ** -10 * s[:, None]) * (1 + 2.0 ** -20)).all()
     assert np.abs(codes.float().cpu().numpy()).max(-1).min() == 448.0     # the largest number of a row has the largest code
+    bad = x.clone()
+    bad[0, dim - 1] = float("inf")
+    bad[-1, 0] = float("nan")
+    bc, bs = lib.psrl_quantize_rows(bad)
+    assert torch.isnan(bc[[0, -1]].float()).all() and torch.isnan(bs[[0, -1]]).all()
+    assert torch.equal(bc[1:-1].contiguous().view(torch.uint8), codes[1:-1].contiguous().view(torch.uint8)) and torch.equal(bs[1:-1], scales[1:-1])
     wide = torch.zeros(rows, -(-dim // 16) * 16 + 64, device="cuda").to(torch.float8_e4m3fn)
     lib.psrl_quantize_rows(x, codes=wide[:, 16:16 + dim])
     assert torch.equal(wide[:, 16:16 + dim].contiguous().view(torch.uint8), codes.contiguous().view(torch.uint8))
