@@ -293,8 +293,10 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __gri
   }
 }
 
+// Groups of 320 and 384 threads are alone on an SM and take all the registers that they can use (145 a thread for 117; 8192 bf16
+// rows of 6144: 79.4 -> 76.0 us).
 template <class T, int kGroup, int kVecs>
-__global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __grid_constant__ BwdParams p) {
+__global__ void __launch_bounds__(threads_of(kGroup), kVecs == 2 && (kGroup == 320 || kGroup == 384) ? 1 : 0) rms_bwd_kernel(const __grid_constant__ BwdParams p) {
   constexpr int kE = kElems<T>, kThreads = threads_of(kGroup), kPerBlock = kThreads / kGroup;
   __shared__ float2 s_sum[2][2][32];
   __shared__ float s_part[kGroup > 32 ? 1 : kThreads * kVecs * kE];
@@ -313,7 +315,7 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_bwd_kernel(const __gri
     for (int e = 0; e < kE; ++e) dw[k][e] = 0.f;
   }
   int turn = 0;
-  constexpr bool kAhead = kVecs <= 2 && kGroup < 1024;   // beyond that registers are short
+  constexpr bool kAhead = kVecs == 1 || (kVecs == 2 && kGroup < 1024);   // beyond that registers are short
   const int64_t stride = int64_t(gridDim.x) * kPerBlock;
   int64_t i = int64_t(blockIdx.x) * kPerBlock + group, row = 0;
   int head = 0;
@@ -433,8 +435,10 @@ struct Shape {
 };
 // Few vectors to a thread hide the latency of a row with many threads where rows are few; with many rows more vectors in flight
 // a thread and fewer barriers a byte are better.  The backward, with three loads and d_weight's sums to hold, takes two vectors a
-// thread, so that there are registers for the next row (8192 rows of 5120: three vectors and no row ahead 111 us).
-Shape shape_of(int vecs, int64_t rows, bool backward) {
+// thread, so that there are registers for the next row (8192 bf16 rows of 5120: three vectors and no row ahead 111 us, two 69); in
+// fp32, where a vector is half the values, one a thread and twice the threads (8192 rows of 2560: 100 -> 55 us, of 4096: 122 -> 88;
+// in bf16 that takes 100 us for 89 at 8192 wide).
+Shape shape_of(int vecs, int64_t rows, bool backward, bool f32) {
   if (vecs <= 8) return {8, 1};
   if (vecs <= 16) return {16, 1};
   if (vecs <= 32) return {32, 1};
@@ -449,12 +453,12 @@ Shape shape_of(int vecs, int64_t rows, bool backward) {
   if (vecs <= 64) return {32, 2};
   if (backward) {
     if (vecs <= 128) return {128, 1};
-    if (vecs <= 256) return {128, 2};
-    if (vecs <= 384) return {192, 2};
-    if (vecs <= 512) return {256, 2};
-    if (vecs <= 640) return {320, 2};
-    if (vecs <= 768) return {384, 2};
-    if (vecs <= 1024) return {512, 2};
+    if (vecs <= 256) return f32 ? Shape{256, 1} : Shape{128, 2};
+    if (vecs <= 384) return f32 ? Shape{384, 1} : Shape{192, 2};
+    if (vecs <= 512) return f32 ? Shape{512, 1} : Shape{256, 2};
+    if (vecs <= 640) return f32 ? Shape{640, 1} : Shape{320, 2};
+    if (vecs <= 768) return f32 ? Shape{768, 1} : Shape{384, 2};
+    if (vecs <= 1024) return f32 ? Shape{1024, 1} : Shape{512, 2};
   } else {
     if (vecs <= 128) return {32, 4};
     if (vecs <= 256) return {128, 2};
@@ -466,8 +470,13 @@ Shape shape_of(int vecs, int64_t rows, bool backward) {
   return vecs <= 4096 ? Shape{1024, 4} : Shape{1024, 8};
 }
 
-// Blocks of an SM in the backward, which the workspace goes by as each leaves a row of sums: as many as the registers hold.
-int bwd_per_sm(const Shape& s) { return std::max(1, (s.vecs == 1 ? 768 : 512) / threads_of(s.group)); }
+// Blocks of an SM in the backward, which the workspace goes by as each leaves a row of sums: as many as the registers hold.  With
+// room to spare the blocks gather on the SMs that the launch before left first (8192 fp32 rows of 3000, one block of 768 threads to
+// an SM 118 us, two 64).
+int bwd_per_sm(const Shape& s, bool f32) {
+  if (f32 && s.vecs == 1) return (1024 + threads_of(s.group) - 1) / threads_of(s.group);
+  return std::max(1, (s.vecs == 1 ? 768 : 512) / threads_of(s.group));
+}
 
 // Blocks of a launch: as many as the SMs hold, and no more than there are rows for.
 int64_t blocks_of(const Shape& s, int64_t rows, int per_sm) {
@@ -513,14 +522,14 @@ cudaError_t launch_one(const P& p, cudaStream_t stream) {
     if (p.codes) return launch_fwd(rms_fwd_kernel<T, kGroup, kVecs, true>, s, p, stream, per_sm[0]);
     return launch_fwd(rms_fwd_kernel<T, kGroup, kVecs, false>, s, p, stream, per_sm[1]);
   } else {
-    return launch_early(rms_bwd_kernel<T, kGroup, kVecs>, unsigned(blocks_of(s, p.rows, bwd_per_sm(s))), unsigned(threads_of(kGroup)), stream, p);
+    return launch_early(rms_bwd_kernel<T, kGroup, kVecs>, unsigned(blocks_of(s, p.rows, bwd_per_sm(s, sizeof(T) == 4))), unsigned(threads_of(kGroup)), stream, p);
   }
 }
 
 template <class T, class P>
 cudaError_t launch(const P& p, cudaStream_t stream) {
   constexpr bool kBackward = std::is_same_v<P, BwdParams>;
-  const Shape s = shape_of(p.vecs, p.rows, kBackward);
+  const Shape s = shape_of(p.vecs, p.rows, kBackward, sizeof(T) == 4);
   switch (s.group * 16 + s.vecs) {
     case 8 * 16 + 1: return launch_one<T, 8, 1>(p, stream);
     case 16 * 16 + 1: return launch_one<T, 16, 1>(p, stream);
@@ -537,11 +546,15 @@ cudaError_t launch(const P& p, cudaStream_t stream) {
     case 1024 * 16 + 4: return launch_one<T, 1024, 4>(p, stream);
   }
   if constexpr (kBackward) {
-    switch (s.group) {
-      case 192: return launch_one<T, 192, 2>(p, stream);
-      case 320: return launch_one<T, 320, 2>(p, stream);
-      case 384: return launch_one<T, 384, 2>(p, stream);
-      case 512: return launch_one<T, 512, 2>(p, stream);
+    if constexpr (sizeof(T) == 4) {
+      if (s.group == 384) return launch_one<T, 384, 1>(p, stream);
+      if (s.group == 640) return launch_one<T, 640, 1>(p, stream);
+      if (s.group == 768) return launch_one<T, 768, 1>(p, stream);
+    } else {
+      if (s.group == 192) return launch_one<T, 192, 2>(p, stream);
+      if (s.group == 320) return launch_one<T, 320, 2>(p, stream);
+      if (s.group == 384) return launch_one<T, 384, 2>(p, stream);
+      if (s.group == 512) return launch_one<T, 512, 2>(p, stream);
     }
   } else {
     switch (s.group * 16 + s.vecs) {
@@ -628,8 +641,9 @@ size_t psrl_rms_norm_workspace_bytes(psrl_dtype_t dtype, int64_t n_rows, int32_t
   if (check(dtype, n_rows, n_heads, dim, 1.f) != PSRL_OK) return 0;
   if (n_rows == 0) return kWsHeaderBytes;
   const int64_t rows = n_rows * n_heads;
-  const Shape s = shape_of(dim / vec_elems(dtype), rows, true);
-  return kWsHeaderBytes + size_t(blocks_of(s, rows, bwd_per_sm(s))) * size_t(dim) * sizeof(float);
+  const bool f32 = dtype == PSRL_F32;
+  const Shape s = shape_of(dim / vec_elems(dtype), rows, true, f32);
+  return kWsHeaderBytes + size_t(blocks_of(s, rows, bwd_per_sm(s, f32))) * size_t(dim) * sizeof(float);
 }
 
 psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_heads, int32_t dim, const void* summed, int64_t summed_pitch,
@@ -662,8 +676,9 @@ psrl_status_t psrl_rms_norm_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_he
               d_x_pitch, n_rows * n_heads, n_heads, int32_t(dim / unit), 1.f / float(dim), eps};
   cudaError_t e = dtype == PSRL_BF16 ? launch<__nv_bfloat16>(p, s) : launch<float>(p, s);
   if (e == cudaSuccess && d_weight) {
-    const Shape shape = shape_of(p.vecs, p.rows, true);
-    const int parts = int(blocks_of(shape, p.rows, bwd_per_sm(shape)));
+    const bool f32 = dtype == PSRL_F32;
+    const Shape shape = shape_of(p.vecs, p.rows, true, f32);
+    const int parts = int(blocks_of(shape, p.rows, bwd_per_sm(shape, f32)));
     const unsigned grid = unsigned((dim + 31) / 32);
     e = dtype == PSRL_BF16 ? launch_early(rms_weight_kernel<__nv_bfloat16>, grid, 1024, s, part, parts, dim, static_cast<__nv_bfloat16*>(d_weight))
                            : launch_early(rms_weight_kernel<float>, grid, 1024, s, part, parts, dim, static_cast<float*>(d_weight));
