@@ -437,7 +437,8 @@ struct Shape {
 // a thread and fewer barriers a byte are better.  The backward, with three loads and d_weight's sums to hold, takes two vectors a
 // thread, so that there are registers for the next row (8192 bf16 rows of 5120: three vectors and no row ahead 111 us, two 69); in
 // fp32, where a vector is half the values, one a thread and twice the threads (8192 rows of 2560: 100 -> 55 us, of 4096: 122 -> 88;
-// in bf16 that takes 100 us for 89 at 8192 wide).
+// in bf16 that takes 100 us for 89 at 8192 wide).  Longer rows have three vectors a thread or four, each as it comes (4096 bf16 rows of
+// 12288: three 85 us, four 122).
 Shape shape_of(int vecs, int64_t rows, bool backward, bool f32) {
   if (vecs <= 8) return {8, 1};
   if (vecs <= 16) return {16, 1};
@@ -459,6 +460,7 @@ Shape shape_of(int vecs, int64_t rows, bool backward, bool f32) {
     if (vecs <= 640) return f32 ? Shape{640, 1} : Shape{320, 2};
     if (vecs <= 768) return f32 ? Shape{768, 1} : Shape{384, 2};
     if (vecs <= 1024) return f32 ? Shape{1024, 1} : Shape{512, 2};
+    if (vecs <= 1536) return {512, 3};
   } else {
     if (vecs <= 128) return {32, 4};
     if (vecs <= 256) return {128, 2};
@@ -536,16 +538,19 @@ cudaError_t launch(const P& p, cudaStream_t stream) {
     case 32 * 16 + 1: return launch_one<T, 32, 1>(p, stream);
     case 32 * 16 + 2: return launch_one<T, 32, 2>(p, stream);
     case 128 * 16 + 1: return launch_one<T, 128, 1>(p, stream);
-    case 128 * 16 + 2: return launch_one<T, 128, 2>(p, stream);
     case 256 * 16 + 1: return launch_one<T, 256, 1>(p, stream);
-    case 256 * 16 + 2: return launch_one<T, 256, 2>(p, stream);
     case 512 * 16 + 1: return launch_one<T, 512, 1>(p, stream);
     case 512 * 16 + 4: return launch_one<T, 512, 4>(p, stream);
     case 1024 * 16 + 1: return launch_one<T, 1024, 1>(p, stream);
     case 1024 * 16 + 2: return launch_one<T, 1024, 2>(p, stream);
     case 1024 * 16 + 4: return launch_one<T, 1024, 4>(p, stream);
   }
+  if constexpr (!kBackward || sizeof(T) == 2) {
+    if (s.group * 16 + s.vecs == 128 * 16 + 2) return launch_one<T, 128, 2>(p, stream);
+    if (s.group * 16 + s.vecs == 256 * 16 + 2) return launch_one<T, 256, 2>(p, stream);
+  }
   if constexpr (kBackward) {
+    if (s.group == 512 && s.vecs == 3) return launch_one<T, 512, 3>(p, stream);
     if constexpr (sizeof(T) == 4) {
       if (s.group == 384) return launch_one<T, 384, 1>(p, stream);
       if (s.group == 640) return launch_one<T, 640, 1>(p, stream);

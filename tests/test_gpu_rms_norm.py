@@ -87,6 +87,18 @@ def test_rows(lib, dtype, dim, rows):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype,dim", [("f32", 1032), ("f32", 1504), ("f32", 2056), ("f32", 2560), ("f32", 2568), ("f32", 3000), ("bf16", 2056), ("bf16", 3000),
+                                       ("bf16", 4800), ("bf16", 5128), ("bf16", 6144), ("bf16", 9000), ("f32", 5000), ("f32", 6144)])
+def test_many_rows_of_sizes_between(lib, dtype, dim):
+    """Widths between powers of two, with more rows than the blocks take at once: groups of other sizes, some threads without a vector."""
+    rows = 1003
+    x, _, w, dy, ds = draw((rows, dim), dtype, dim)
+    check_fwd(lib.psrl_rms_norm_fwd(x, w, 1e-5, want_codes=True), to_np(x), w, 1e-5)
+    check_bwd(lib.psrl_rms_norm_bwd(x, w, dy, 1e-5, d_summed=ds), to_np(x), w, to_np(dy), 1e-5, to_np(ds))
+    a, b = (lib.psrl_rms_norm_bwd(x, w, dy, 1e-5) for _ in range(2))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,heads,dim", [(1, 1, 64), (5, 3, 64), (333, 7, 128), (1000, 40, 128), (257, 5, 80), (9, 2, 256), (40, 3, 1024)])
 def test_heads_of_a_projections_rows(lib, dtype, rows, heads, dim):
