@@ -141,7 +141,7 @@ __device__ __forceinline__ uint4 get16(const uint8_t* b, int row, int chunk) {
 
 // eight bf16 of a vector that ends at `n`, from column `col`; the same for all threads
 __device__ __forceinline__ uint4 load_bias(const __nv_bfloat16* bias, int col, int n) {
-  if (col + 8 <= n) return __ldg(reinterpret_cast<const uint4*>(bias + col));
+  if (col + 8 <= n) return *reinterpret_cast<const uint4*>(bias + col);
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -152,10 +152,10 @@ __device__ __forceinline__ uint4 load_bias(const __nv_bfloat16* bias, int col, i
 }
 // four fp32 of such a vector
 __device__ __forceinline__ float4 load_scale(const float* scale, int col, int n) {
-  if (col + 4 <= n && (reinterpret_cast<uintptr_t>(scale) & 15) == 0) return __ldg(reinterpret_cast<const float4*>(scale + col));
+  if (col + 4 <= n && (reinterpret_cast<uintptr_t>(scale) & 15) == 0) return *reinterpret_cast<const float4*>(scale + col);
   float o[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = col + i < n ? __ldg(scale + col + i) : 0.f;
+  for (int i = 0; i < 4; ++i) o[i] = col + i < n ? scale[col + i] : 0.f;
   return make_float4(o[0], o[1], o[2], o[3]);
 }
 // eight numbers and a vector of eight bf16
@@ -414,7 +414,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
               if (p.has_residual) res[j] = get16(first, gt, h * 4 + j);
             }
           }
-float v[32];
+          float v[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(r[h][e]);
           if constexpr (kFp8) {
@@ -842,7 +842,7 @@ __global__ void __launch_bounds__(kDzThreads, 2) dz_kernel(const __grid_constant
 
 // d_bias from the blocks' sums: a block takes 32 columns, 32 threads share the parts of each, in a fixed order.
 template <class T>
-__global__ void __launch_bounds__(1024) bias_kernel(const float* __restrict__ part, int parts, int N, T* __restrict__ d_bias) {
+__global__ void __launch_bounds__(1024) bias_kernel(const float* part, int parts, int N, T* d_bias) {
   previous_kernel_done();
   next_kernel_may_start();
   __shared__ float s[32][33];

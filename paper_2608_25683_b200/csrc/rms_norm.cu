@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(threads_of(kGroup), kVecs == 2 && (kGroup == 3
 
 // d_weight: the blocks' sums, added in a fixed order.  A block takes 32 columns, 32 threads share the parts of each.
 template <class T>
-__global__ void __launch_bounds__(1024) rms_weight_kernel(const float* __restrict__ part, int parts, int dim, T* __restrict__ d_weight) {
+__global__ void __launch_bounds__(1024) rms_weight_kernel(const float* part, int parts, int dim, T* d_weight) {
   previous_kernel_done();
   next_kernel_may_start();
   __shared__ float s[32][33];
@@ -486,7 +486,8 @@ int64_t blocks_of(const Shape& s, int64_t rows, int per_sm) {
   return std::min<int64_t>(int64_t(resident_ctas()) * per_sm, (rows + per_block - 1) / per_block);
 }
 
-// Every kernel here may start before the one before it on the stream has ended, and touches memory behind previous_kernel_done() only.
+// Every kernel here may start before the one before it on the stream has ended, and touches memory behind previous_kernel_done() only.  What it
+// reads may be written while it is here: no pointer is __restrict__, as the compiler may move loads through those in front of the wait.
 template <class... P, class... A>
 cudaError_t launch_early(void (*kernel)(P...), unsigned blocks, unsigned threads, cudaStream_t stream, const A&... args) {
   cudaLaunchConfig_t cfg{};
