@@ -313,13 +313,15 @@ struct Tree {
 };
 constexpr int kTreeArgs = 8;
 
+// [axes, rows], the rows of an axis contiguous: the elements from one axis to the next.  One row may be a slice as well as many: its axes
+// are then as far apart as those of the matrix that it was cut from.
 int64_t positions_of(Call& c, const Tensor* p, int64_t axes, int64_t rows) {
   if (!p || !c.ok) {
     c.ok = false;
     return 0;
   }
   if (p->dim() != 2 || p->size(0) != axes || p->size(1) != rows || (rows > 1 && p->stride(1) != 1)) c.ok = false;
-  return axes > 1 && rows > 1 ? p->stride(0) : rows;
+  return axes > 1 && !p->is_contiguous() ? p->stride(0) : rows;
 }
 
 // plan, rope, axes, type, T_q, Hq, Hkv, d, positions, q, k, v, k_pool, v_pool, q_out -> (q_out,)
