@@ -62,6 +62,7 @@ struct Params {
   const float *x_scale, *w_scale;
   int32_t act, has_mul, has_residual, has_z;
   int32_t share;                // no pair has more than one tile
+  int32_t clear;                // the call's first kernel: it clears the status, the later ones leave what those before them recorded
   int* status;
 };
 
@@ -213,7 +214,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
   tc_fence_after();
   previous_kernel_done();
   next_kernel_may_start();
-  if (p.status && blockIdx.x == 0 && tid == 0) *p.status = int(PSRL_OK);
+  if (p.clear && p.status && blockIdx.x == 0 && tid == 0) *p.status = int(PSRL_OK);
 
   const Schedule plan(p, cluster, n_clusters);
   const uint32_t tmem = s_tmem;
@@ -498,6 +499,7 @@ struct FewParams {
   __nv_bfloat16 *y, *z;
   int64_t mul_pitch, residual_pitch, y_pitch, z_pitch;
   int32_t act;
+  int32_t clear;               // as above
   int* status;
 };
 
@@ -573,7 +575,7 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
     fence_mbar_init();
   }
   previous_kernel_done();
-  if (p.status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
+  if (p.clear && p.status && blockIdx.x == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
   // the first loads need nothing of the other warps: they are on their way while tensor memory is handed out
   auto load = [&](int kb, int s) {
     uint8_t* sa = smem + s * stage_bytes;
@@ -1090,7 +1092,7 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     F32Params q{};
     q.a = {static_cast<const float*>(x), x_pitch};
     q.b = {static_cast<const float*>(weight), weight_pitch};
-    q.M = int32_t(M); q.N = int32_t(N); q.depth = in_dim; q.status = status;
+    q.M = int32_t(M); q.N = int32_t(N); q.depth = in_dim; q.clear = 1; q.status = status;
     q.e = {static_cast<const float*>(bias), static_cast<const float*>(mul), static_cast<const float*>(residual), static_cast<float*>(y), static_cast<float*>(z),
            mul_pitch, residual_pitch, y_pitch, z_pitch, activation};
     const cudaError_t e = f32_product<false, false>(q, reinterpret_cast<float*>(static_cast<char*>(workspace) + kWsHeaderBytes), s);
@@ -1110,7 +1112,7 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     q.x_scale = x_scale; q.w_scale = weight_scale;
     q.y = static_cast<Bf*>(y); q.z = static_cast<Bf*>(z);
     q.mul_pitch = mul_pitch; q.residual_pitch = residual_pitch; q.y_pitch = y_pitch; q.z_pitch = z_pitch;
-    q.act = activation; q.status = status;
+    q.act = activation; q.clear = 1; q.status = status;
     const cudaError_t e = fp8 ? launch_few<true>(maps, q, f, s) : launch_few<false>(maps, q, f, s);
     return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
   }
@@ -1130,7 +1132,7 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
   p.x_scale = x_scale; p.w_scale = weight_scale;
   p.act = activation;
   p.has_mul = mul != nullptr; p.has_residual = residual != nullptr; p.has_z = z != nullptr;
-  p.status = status;
+  p.clear = 1; p.status = status;
   const cudaError_t e = fp8 ? (full ? launch_gemm<true, kFull>(maps, p, s) : launch_gemm<true, kPlain>(maps, p, s))
                             : (full ? launch_gemm<false, kFull>(maps, p, s) : launch_gemm<false, kPlain>(maps, p, s));
   return e == cudaSuccess ? PSRL_OK : cuda_failed(e);
@@ -1170,7 +1172,7 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
       !same_rows(d_mul, d_mul_pitch, d_y, d_y_pitch, M) || !same_rows(d_mul, d_mul_pitch, mul, mul_pitch, M) || !same_rows(d_mul, d_mul_pitch, z, z_pitch, M))
     return PSRL_ERR_INVALID_ARG;
   int* status = static_cast<int*>(workspace);
-  bool first = true;
+  int32_t first = 1;   // no kernel of this call has been launched yet
   const void* dz = d_y;
   int64_t dz_pitch = d_y_pitch;
   if (elementwise || d_bias) {
@@ -1189,7 +1191,7 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     };
     e = dtype == PSRL_F32 ? run(float()) : run(__nv_bfloat16());
     if (e != cudaSuccess) return cuda_failed(e);
-    first = false;
+    first = 0;   // dz_kernel has cleared the status
   }
   if (!d_x && !d_weight) {
     if (first && workspace) e = cudaMemsetAsync(workspace, 0, kWsHeaderBytes, s);
@@ -1201,7 +1203,8 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     auto params = [&](F32Operand a, F32Operand b, int64_t rows, int64_t depth, void* out, int64_t pitch) {
       F32Params q{};
       q.a = a; q.b = b;
-      q.M = int32_t(rows); q.N = int32_t(K); q.depth = int32_t(depth); q.status = status;
+      q.M = int32_t(rows); q.N = int32_t(K); q.depth = int32_t(depth); q.clear = first; q.status = status;
+      first = 0;
       q.e.y = static_cast<float*>(out); q.e.y_pitch = pitch;
       return q;
     };
@@ -1219,7 +1222,8 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
     if (!make_map_bf16_2d(&maps.a, weight, K, N, weight_pitch * 2, 64) || !make_map_bf16_2d(&maps.b, dz, N, M, dz_pitch * 2, f.tile_rows)) return PSRL_ERR_CUDA;
     FewParams q{};
     q.rows = int32_t(M); q.cols = int32_t(K); q.steps = int32_t(div_up(N, 64)); q.a_mn = 1;
-    q.y = static_cast<__nv_bfloat16*>(d_x); q.y_pitch = d_x_pitch; q.status = status;
+    q.y = static_cast<__nv_bfloat16*>(d_x); q.y_pitch = d_x_pitch; q.clear = first; q.status = status;
+    first = 0;
     e = launch_few<false>(maps, q, f, s);
     if (e != cudaSuccess) return cuda_failed(e);
     if (!d_weight) return PSRL_OK;
@@ -1236,7 +1240,7 @@ psrl_status_t psrl_linear_bwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
   p.product[ix] = px;
   p.product[iw] = pw;
   p.ratio = (p.product[0].steps + 6) / std::max(p.product[1].steps + 6, 1);
-  p.status = status;
+  p.clear = first; p.status = status;
   bool made = true;
   if (d_x)
     made = make_map_bf16_2d(&maps.a[ix], dz, N, M, dz_pitch * 2, 128) && make_map_bf16_2d(&maps.b[ix], weight, K, N, weight_pitch * 2, 64) &&

@@ -47,6 +47,7 @@ struct F32Params {
   int64_t part_pitch;           // N in whole fours
   int32_t m_tiles;
   F32Epilogue e;
+  int32_t clear;                // the call's first kernel: it clears the status
   int* status;                  // NULL: a call without a workspace, whose depth is not cut
 };
 
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(256) linear_f32_kernel(const __grid_constant__
   previous_kernel_done();
   next_kernel_may_start();
   __shared__ __align__(16) float sa[2][kF32Depth][kTile + 4], sb[2][kF32Depth][kTile + 4];
-  if (p.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
+  if (p.clear && p.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.status = int(PSRL_OK);
   const int mt = int(blockIdx.x) % p.m_tiles, nt = int(blockIdx.x) / p.m_tiles;
   const int m0 = mt * kTile, n0 = nt * kTile;
   const int k0 = int(blockIdx.y) * p.slice, k_end = min(p.depth, k0 + p.slice);
