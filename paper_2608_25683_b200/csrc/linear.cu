@@ -433,7 +433,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
 #pragma unroll
             for (int j = 0; j < 4; ++j) put16(second, gt, h * 4 + j, narrow8(&v[j * 8]));
           }
-          activate(v, p.act);
+          activate<false>(v, p.act);
           if (kEpilogue == kFull && p.has_mul) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) mul8(&v[j * 8], mul[j]);
@@ -691,7 +691,7 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
             if (p.bias) v[i][e] += bias[e];
           }
           if (p.z) store4(p.z + row * p.z_pitch + col, left, v[i]);
-          activate(v[i], p.act);
+          activate<false>(v[i], p.act);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             if (p.mul) v[i][e] *= mul[i][e];
@@ -811,7 +811,7 @@ __global__ void __launch_bounds__(kDzThreads, 2) dz_kernel(const __grid_constant
         if (p.z) {
           float z[kE], d[kE];
           widen_vec<T>(z4[b], z);
-          act_and_slope(z, p.act, d);   // d: values, z: slopes
+          act_and_slope<sizeof(T) == 4>(z, p.act, d);   // d: values, z: slopes
 #pragma unroll
           for (int e = 0; e < kE; ++e) {
             d[e] *= g[e];

@@ -84,7 +84,7 @@ __device__ __forceinline__ void f32_finish(const F32Epilogue& e, int64_t m, int6
     for (int i = 0; i < 4; ++i) v[i] += bias[i];
   }
   if (e.z) f32_write(e.z + m * e.z_pitch + n, left, v);
-  activate(v, e.act);
+  activate<true>(v, e.act);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (e.mul) v[i] *= mul[i];
