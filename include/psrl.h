@@ -400,8 +400,8 @@ psrl_status_t psrl_rope_axes_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, c
  *            d_summed NULL: none; summed (read only with a residual), y, codes, d_x NULL: not wanted
  *   weight, d_weight [dim] DEVICE of `dtype`; weight NULL: ones (d_weight must be NULL then); d_weight NULL: not wanted
  *   codes    [n_rows, n_heads, dim] DEVICE e4m3, codes_pitch a multiple of 16;  scales [n_rows * n_heads] DEVICE fp32, with codes
- *   workspace  DEVICE, 256-byte aligned, with d_weight >= psrl_rms_norm_workspace_bytes; holds the device status word.  Without d_weight
- *            256 bytes, or NULL
+ *   workspace  DEVICE, 256-byte aligned, with d_weight >= psrl_rms_norm_workspace_bytes (asked with the call's device as the current one: it
+ *            goes by its SMs); holds the device status word.  Without d_weight 256 bytes, or NULL
  * An output may be one of the call's inputs (equal pitches); otherwise tensors are apart.  dim a multiple of 8, 8..32768;
  * pointers 16-byte aligned (scales 4), pitches a multiple of 16 bytes and at least a row; eps > 0.
  * n_rows = 0 does nothing (backward: zeroes d_weight).
@@ -440,7 +440,7 @@ psrl_status_t psrl_quantize_rows(psrl_dtype_t dtype, int64_t n_rows, int32_t dim
  *   workspace  DEVICE, 256-byte aligned, of psrl_linear_workspace_bytes; holds the device status word.  Forward 256 bytes; backward dz
  *              (n_rows rows of out_dim in whole 8s) and a number for each column and 64 rows, neither needed where there is no
  *              activation, mul or d_bias that asks for it; F32: with few rows or columns the sums of parts of the depth, below 20 MB.
- *              NULL where 256 bytes would do: the status of the waits inside is then not kept
+ *              NULL where 256 bytes would do: the status of the waits inside is then not kept.  The size is that for the current device
  * y and z may be mul or residual, d_mul may be d_y, mul or z (equal pitches); otherwise tensors are apart.  in_dim is a multiple of 8,
  * out_dim any; pitches are multiples of 16 bytes and at least a row, pointers 16-byte aligned (scales 4).  Dimensions are at most 2^30.
  * n_rows = 0 does nothing (backward: zeroes d_weight and d_bias).
@@ -493,7 +493,7 @@ psrl_status_t psrl_plan_next_tokens(const psrl_plan_t* plan, const int32_t** off
  *   scale    finite, not 0 (1 / temperature)
  *   logprob, d_logprob [n_targets], lse [n_rows] DEVICE fp32 (backward: as produced by the forward)
  *   d_hidden, d_weight  DEVICE of `dtype` as their tensors, fully overwritten; NULL: not wanted
- *   workspace  DEVICE, >= psrl_token_logprob_workspace_bytes, 256-byte aligned; holds the device status word.  Forward:
+ *   workspace  DEVICE, >= psrl_token_logprob_workspace_bytes (for the current device), 256-byte aligned; holds the device status word.  Forward:
  *              at most 16 bytes per row and 128 entries of the vocabulary (2 bytes where there are thousands of rows), and 8 MB;
  *              backward, with R = n_rows in whole 128s, at least 256: a piece of dz, 64 Mi numbers or 8192 per row of R if
  *              that is more; R rows of `hidden`; sums in fp32, R rows or 64 MB if that is more (bf16); 40 bytes per row and 24

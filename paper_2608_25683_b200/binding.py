@@ -632,9 +632,14 @@ def _scratch(nbytes: int, keep, like):
 
 
 @functools.lru_cache(maxsize=4096)
-def _workspace_bytes(name: str, *args) -> int:
-    """What the library asks for a call of these sizes, asked once."""
-    return int(getattr(lib(), name)(*args))
+def _workspace_bytes(name: str, dev: int, *args) -> int:
+    """What the library asks for a call of these sizes on device `dev`, asked once with that device as the current one: some sizes go by its
+    number of SMs."""
+    fn = getattr(lib(), name)
+    if dev == _cuda()._cuda_getDevice():
+        return int(fn(*args))
+    with _torch().cuda.device(dev):
+        return int(fn(*args))
 
 
 _type_codes = None
@@ -979,7 +984,7 @@ def _matrix_pitch(t, name: str) -> int:
 def _logprob_workspace(workspace, raw, keep, dt, n, h, v, m, backward, device):
     """(pointer, bytes, what holds the memory until the call is on its stream)"""
     if workspace is None:
-        workspace = Workspace(lib().psrl_token_logprob_workspace_bytes(dt, n, h, v, m, backward), device, keep, raw)
+        workspace = Workspace(_workspace_bytes("psrl_token_logprob_workspace_bytes", device.index, dt, n, h, v, m, int(backward)), device, keep, raw)
         return workspace.ptr, workspace.nbytes, workspace
     return (*_use_workspace(workspace, raw, keep, device.index), workspace)
 
@@ -1183,7 +1188,7 @@ def psrl_rms_norm_bwd(summed, weight, d_y, eps: float = 1e-6, d_summed=None, d_x
     if workspace is None:
         ws, wsb, held = None, 0, None
         if d_weight is not None:
-            ws, wsb, held = _scratch(_workspace_bytes("psrl_rms_norm_workspace_bytes", dt, rows, heads, dim), keep, summed)
+            ws, wsb, held = _scratch(_workspace_bytes("psrl_rms_norm_workspace_bytes", dev, dt, rows, heads, dim), keep, summed)
     else:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
     _launch("psrl_rms_norm_bwd", dev, dt, rows, heads, dim, summed.data_ptr(), ph, None if weight is None else weight.data_ptr(), eps,
@@ -1301,7 +1306,7 @@ def psrl_linear_fwd(x, weight, bias=None, activation=None, mul=None, residual=No
     if workspace is not None:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
     elif dt == PSRL_F32:
-        ws, wsb, held = _scratch(_workspace_bytes("psrl_linear_workspace_bytes", dt, m, k, n, 0), keep, x)
+        ws, wsb, held = _scratch(_workspace_bytes("psrl_linear_workspace_bytes", dev, dt, m, k, n, 0), keep, x)
     else:
         ws, wsb = None, 0
     _launch("psrl_linear_fwd", dev, dt, m, k, n, x.data_ptr(), px, a_xs, weight.data_ptr(), pw, a_ws, a_bias, _ACTIVATIONS[activation],
@@ -1342,7 +1347,7 @@ def psrl_linear_bwd(x, weight, d_y, z=None, activation=None, mul=None, d_x=None,
     if workspace is not None:
         ws, wsb = _use_workspace(workspace, raw, keep, dev)
     elif activation not in (None, "none") or mul is not None or want_bias or dt == PSRL_F32:
-        ws, wsb, held = _scratch(_workspace_bytes("psrl_linear_workspace_bytes", dt, m, k, n, 1), keep, x)
+        ws, wsb, held = _scratch(_workspace_bytes("psrl_linear_workspace_bytes", dev, dt, m, k, n, 1), keep, x)
     else:
         ws, wsb = None, 0
     _launch("psrl_linear_bwd", dev, dt, m, k, n, x.data_ptr(), px, weight.data_ptr(), pw, a_z, p_z, _ACTIVATIONS[activation], a_mul, p_mul,
