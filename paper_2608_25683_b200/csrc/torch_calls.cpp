@@ -2,6 +2,9 @@
 // step, where the same in Python takes as long as several such kernels (8 rows of 256, norm with residual and 8-bit output: 17.3 us
 // through ctypes, 3 us of them the launch).
 //
+// A launch can wait for room in the device's queue, and an allocation for the device, so both run without the interpreter's lock, as a call through
+// ctypes does: other threads go on meanwhile, those among them that the queue waits for.
+//
 // Each function serves the plain case of its wrapper in binding.py and nothing else: tensors of one device, which is the current one, of
 // the right types, on the current stream, with outputs and workspaces made here.  It answers None for any other, and the wrapper
 // goes its own way, with its own errors; a status other than PSRL_OK is answered as it is.
@@ -89,6 +92,16 @@ struct Call {
   void* stream() const { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(dev)).stream(); }
 };
 
+// f() without the interpreter's lock, which is taken again whichever way f ends.
+template <class F>
+psrl_status_t unlocked(F f) {
+  struct Lock {
+    PyThreadState* state = PyEval_SaveThread();
+    ~Lock() { PyEval_RestoreThread(state); }
+  } lock;
+  return f();
+}
+
 const void* at_of(const Tensor* t) { return t ? t->data_ptr() : nullptr; }
 PyObject* none() { Py_RETURN_NONE; }
 PyObject* wrap(const Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : none(); }
@@ -171,15 +184,17 @@ PyObject* rms_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const bool want_y = truth(a[4]), want_codes = truth(a[5]);
     if (!c.ok || (want_codes && least % 16)) return none();
     Tensor y, summed, codes, scales;
-    if (want_y) y = c.make(x->sizes(), c.type);
-    if (res) summed = c.make(x->sizes(), c.type);
-    if (want_codes) {
-      codes = c.make(x->sizes(), at::kFloat8_e4m3fn);
-      scales = c.make(x->sizes().slice(0, m.dims - 1), at::kFloat);
-    }
-    const psrl_status_t st = psrl_rms_norm_fwd(psrl_dtype_t(code_of(c.type)), m.rows, int32_t(m.heads), int32_t(m.dim), x->data_ptr(), px, at_of(res), pr, m.weight,
-                                               float(eps), res ? summed.data_ptr() : nullptr, least, want_y ? y.data_ptr() : nullptr, least,
-                                               want_codes ? codes.data_ptr() : nullptr, least, want_codes ? static_cast<float*>(scales.data_ptr()) : nullptr, c.stream());
+    const psrl_status_t st = unlocked([&] {
+      if (want_y) y = c.make(x->sizes(), c.type);
+      if (res) summed = c.make(x->sizes(), c.type);
+      if (want_codes) {
+        codes = c.make(x->sizes(), at::kFloat8_e4m3fn);
+        scales = c.make(x->sizes().slice(0, m.dims - 1), at::kFloat);
+      }
+      return psrl_rms_norm_fwd(psrl_dtype_t(code_of(c.type)), m.rows, int32_t(m.heads), int32_t(m.dim), x->data_ptr(), px, at_of(res), pr, m.weight, float(eps),
+                               res ? summed.data_ptr() : nullptr, least, want_y ? y.data_ptr() : nullptr, least, want_codes ? codes.data_ptr() : nullptr, least,
+                               want_codes ? static_cast<float*>(scales.data_ptr()) : nullptr, c.stream());
+    });
     return answer(st, y, summed, codes, scales);
   });
 }
@@ -198,16 +213,17 @@ PyObject* rms_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const bool want_x = truth(a[5]), want_w = truth(a[6]) && m.weight;
     const psrl_dtype_t t = psrl_dtype_t(code_of(c.type));
     Tensor dx, dw, ws;
-    size_t bytes = 0;
-    if (want_x) dx = c.make(h->sizes(), c.type);
-    if (want_w) {
-      dw = c.make({m.dim}, c.type);
-      bytes = psrl_rms_norm_workspace_bytes(t, m.rows, int32_t(m.heads), int32_t(m.dim));
-      ws = c.make({int64_t(bytes)}, at::kByte);
-    }
-    const psrl_status_t st = psrl_rms_norm_bwd(t, m.rows, int32_t(m.heads), int32_t(m.dim), h->data_ptr(), ph, m.weight, float(eps), dy->data_ptr(), pd, at_of(ds), ps,
-                                               want_x ? dx.data_ptr() : nullptr, m.heads * m.dim, want_w ? dw.data_ptr() : nullptr, want_w ? ws.data_ptr() : nullptr, bytes,
-                                               c.stream());
+    const psrl_status_t st = unlocked([&] {
+      size_t bytes = 0;
+      if (want_x) dx = c.make(h->sizes(), c.type);
+      if (want_w) {
+        dw = c.make({m.dim}, c.type);
+        bytes = psrl_rms_norm_workspace_bytes(t, m.rows, int32_t(m.heads), int32_t(m.dim));
+        ws = c.make({int64_t(bytes)}, at::kByte);
+      }
+      return psrl_rms_norm_bwd(t, m.rows, int32_t(m.heads), int32_t(m.dim), h->data_ptr(), ph, m.weight, float(eps), dy->data_ptr(), pd, at_of(ds), ps,
+                               want_x ? dx.data_ptr() : nullptr, m.heads * m.dim, want_w ? dw.data_ptr() : nullptr, want_w ? ws.data_ptr() : nullptr, bytes, c.stream());
+    });
     return answer(st, dx, dw);
   });
 }
@@ -251,17 +267,21 @@ PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t pm = c.matrix(mul, p.m, p.n), pr = c.matrix(res, p.m, p.n);
     if (!c.ok || codes != (a[6] != Py_None) || codes != (a[7] != Py_None)) return none();
     const psrl_dtype_t t = psrl_dtype_t(code_of(c.type));
-    int64_t py, pz = 0;
-    Tensor y = c.make_matrix(p.m, p.n, p.out, py), z, ws;
-    if (truth(a[8])) z = c.make_matrix(p.m, p.n, p.out, pz);
-    size_t bytes = 0;
-    if (t == PSRL_F32) {
-      bytes = psrl_linear_workspace_bytes(t, p.m, int32_t(p.k), int32_t(p.n), 0);
-      ws = c.make({int64_t(bytes)}, at::kByte);
-    }
-    const psrl_status_t st = psrl_linear_fwd(t, p.m, int32_t(p.k), int32_t(p.n), p.x->data_ptr(), p.px, static_cast<const float*>(sx), p.w->data_ptr(), p.pw,
-                                             static_cast<const float*>(sw), bias, psrl_activation_t(act), at_of(mul), pm, at_of(res), pr, y.data_ptr(), py,
-                                             z.defined() ? z.data_ptr() : nullptr, pz, bytes ? ws.data_ptr() : nullptr, bytes, c.stream());
+    const bool want_z = truth(a[8]);
+    Tensor y, z, ws;
+    const psrl_status_t st = unlocked([&] {
+      int64_t py, pz = 0;
+      y = c.make_matrix(p.m, p.n, p.out, py);
+      if (want_z) z = c.make_matrix(p.m, p.n, p.out, pz);
+      size_t bytes = 0;
+      if (t == PSRL_F32) {
+        bytes = psrl_linear_workspace_bytes(t, p.m, int32_t(p.k), int32_t(p.n), 0);
+        ws = c.make({int64_t(bytes)}, at::kByte);
+      }
+      return psrl_linear_fwd(t, p.m, int32_t(p.k), int32_t(p.n), p.x->data_ptr(), p.px, static_cast<const float*>(sx), p.w->data_ptr(), p.pw,
+                             static_cast<const float*>(sw), bias, psrl_activation_t(act), at_of(mul), pm, at_of(res), pr, y.data_ptr(), py,
+                             z.defined() ? z.data_ptr() : nullptr, pz, bytes ? ws.data_ptr() : nullptr, bytes, c.stream());
+    });
     return answer(st, y, z);
   });
 }
@@ -279,20 +299,22 @@ PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!c.ok || !dy) return none();
     const bool want_x = truth(a[6]), want_w = truth(a[7]), want_b = truth(a[8]), want_m = truth(a[9]);
     const psrl_dtype_t t = psrl_dtype_t(code_of(c.type));
-    int64_t px = 0, pw = 0, pq = 0;
     Tensor dx, dw, db, dm, ws;
-    if (want_x) dx = c.make_matrix(p.m, p.k, c.type, px);
-    if (want_w) dw = c.make_matrix(p.n, p.k, c.type, pw);
-    if (want_b) db = c.make({p.n}, c.type);
-    if (want_m) dm = c.make_matrix(p.m, p.n, c.type, pq);
-    size_t bytes = 0;
-    if (act != PSRL_ACT_NONE || mul || want_b || t == PSRL_F32) {
-      bytes = psrl_linear_workspace_bytes(t, p.m, int32_t(p.k), int32_t(p.n), 1);
-      ws = c.make({int64_t(bytes)}, at::kByte);
-    }
-    auto at_or = [](const Tensor& v) { return v.defined() ? v.data_ptr() : nullptr; };
-    const psrl_status_t st = psrl_linear_bwd(t, p.m, int32_t(p.k), int32_t(p.n), p.x->data_ptr(), p.px, p.w->data_ptr(), p.pw, at_of(z), pz, psrl_activation_t(act),
-                                             at_of(mul), pm, dy->data_ptr(), pd, at_or(dx), px, at_or(dw), pw, at_or(db), at_or(dm), pq, at_or(ws), bytes, c.stream());
+    const psrl_status_t st = unlocked([&] {
+      int64_t px = 0, pw = 0, pq = 0;
+      if (want_x) dx = c.make_matrix(p.m, p.k, c.type, px);
+      if (want_w) dw = c.make_matrix(p.n, p.k, c.type, pw);
+      if (want_b) db = c.make({p.n}, c.type);
+      if (want_m) dm = c.make_matrix(p.m, p.n, c.type, pq);
+      size_t bytes = 0;
+      if (act != PSRL_ACT_NONE || mul || want_b || t == PSRL_F32) {
+        bytes = psrl_linear_workspace_bytes(t, p.m, int32_t(p.k), int32_t(p.n), 1);
+        ws = c.make({int64_t(bytes)}, at::kByte);
+      }
+      auto at_or = [](const Tensor& v) { return v.defined() ? v.data_ptr() : nullptr; };
+      return psrl_linear_bwd(t, p.m, int32_t(p.k), int32_t(p.n), p.x->data_ptr(), p.px, p.w->data_ptr(), p.pw, at_of(z), pz, psrl_activation_t(act), at_of(mul), pm,
+                             dy->data_ptr(), pd, at_or(dx), px, at_or(dw), pw, at_or(db), at_or(dm), pq, at_or(ws), bytes, c.stream());
+    });
     return answer(st, dx, dw, db, dm);
   });
 }
@@ -341,9 +363,11 @@ PyObject* rope_axes_qkv_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t pq = c.rows(q, t.rows, t.hq, t.d, 3), pk = c.rows(k, t.rows, t.hkv, t.d, 3), pv = c.rows(v, t.rows, t.hkv, t.d, 3), pa = positions_of(c, pos, t.axes, t.rows);
     if (!c.ok) return none();
     Tensor made;
-    if (!out) made = c.make({t.rows, t.hq, t.d}, c.type);
-    const psrl_status_t st = psrl_rope_axes_qkv_fwd(t.plan, t.rope, static_cast<const int32_t*>(pos->data_ptr()), pa, q->data_ptr(), pq, k->data_ptr(), pk, v->data_ptr(), pv,
-                                                    out ? out->data_ptr() : made.data_ptr(), kp->data_ptr(), vp->data_ptr(), kp->size(1), c.stream());
+    const psrl_status_t st = unlocked([&] {
+      if (!out) made = c.make({t.rows, t.hq, t.d}, c.type);
+      return psrl_rope_axes_qkv_fwd(t.plan, t.rope, static_cast<const int32_t*>(pos->data_ptr()), pa, q->data_ptr(), pq, k->data_ptr(), pk, v->data_ptr(), pv,
+                                    out ? out->data_ptr() : made.data_ptr(), kp->data_ptr(), vp->data_ptr(), kp->size(1), c.stream());
+    });
     return answer(st, out ? *out : made);
   });
 }
@@ -369,13 +393,17 @@ PyObject* rope_axes_qkv_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int64_t pitch[3];
     for (int i = 0; i < 3; ++i) {
       const int64_t heads = i == 0 ? t.hq : t.hkv;
-      if (given[i]) out[i] = *given[i];
-      else out[i] = c.make({t.rows, heads, t.d}, c.type);
-      pitch[i] = c.rows(&out[i], t.rows, heads, t.d, 3);
+      pitch[i] = given[i] ? c.rows(given[i], t.rows, heads, t.d, 3) : heads * t.d;
     }
     if (!c.ok) return none();
-    const psrl_status_t st = psrl_rope_axes_qkv_bwd(t.plan, t.rope, static_cast<const int32_t*>(pos->data_ptr()), pa, q->data_ptr(), kp->data_ptr(), vp->data_ptr(), kp->size(1),
-                                                    out[0].data_ptr(), pitch[0], out[1].data_ptr(), pitch[1], out[2].data_ptr(), pitch[2], c.stream());
+    const psrl_status_t st = unlocked([&] {
+      for (int i = 0; i < 3; ++i) {
+        if (given[i]) out[i] = *given[i];
+        else out[i] = c.make({t.rows, i == 0 ? t.hq : t.hkv, t.d}, c.type);
+      }
+      return psrl_rope_axes_qkv_bwd(t.plan, t.rope, static_cast<const int32_t*>(pos->data_ptr()), pa, q->data_ptr(), kp->data_ptr(), vp->data_ptr(), kp->size(1),
+                                    out[0].data_ptr(), pitch[0], out[1].data_ptr(), pitch[1], out[2].data_ptr(), pitch[2], c.stream());
+    });
     return answer(st, out[0], out[1], out[2]);
   });
 }
@@ -392,9 +420,13 @@ PyObject* rope_axes_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor* pos = c.like(a[4], at::kInt);
     const int64_t px = c.rows(x, rows, heads, d, 3), pa = positions_of(c, pos, axes, rows);
     if (!c.ok || heads > INT32_MAX) return none();
-    Tensor y = c.make(x->sizes(), c.type);
-    const psrl_status_t st = psrl_rope_axes_rows(reinterpret_cast<const psrl_rope_t*>(r), psrl_dtype_t(code_of(c.type)), x->data_ptr(), px,
-                                                 static_cast<const int32_t*>(pos->data_ptr()), pa, rows, int32_t(heads), y.data_ptr(), heads * d, truth(a[5]) ? 1 : 0, c.stream());
+    const bool inverse = truth(a[5]);
+    Tensor y;
+    const psrl_status_t st = unlocked([&] {
+      y = c.make(x->sizes(), c.type);
+      return psrl_rope_axes_rows(reinterpret_cast<const psrl_rope_t*>(r), psrl_dtype_t(code_of(c.type)), x->data_ptr(), px, static_cast<const int32_t*>(pos->data_ptr()), pa,
+                                 rows, int32_t(heads), y.data_ptr(), heads * d, inverse ? 1 : 0, c.stream());
+    });
     return answer(st, y);
   });
 }
