@@ -138,9 +138,10 @@ __device__ __forceinline__ float2 join_sums(float2 v, float2* s) {
   return v;
 }
 
-// Squares of numbers beyond 2^56 may pass fp32's range: the sum is then made again of h 2^-80, whose squares do not, and whose
-// roundings are the same.  (eps is nothing beside such a row.  NaN and infinities come this way, too, and stay.)
-constexpr float kSmall = 0x1p-80f;
+// Squares of numbers beyond 2^56 may pass fp32's range: the sum is then made again of h 2^-110, whose squares do not, and whose
+// roundings are the same.  (eps is nothing beside such a row.  NaN and infinities come this way, too, and stay.)  So with the backward's sum of
+// g h, which may pass the range where its mean along the unit row does not: h 2^-110 keeps it in as long as no g h is beyond 2^220.
+constexpr float kSmall = 0x1p-110f;
 __device__ __forceinline__ bool too_large(float sum) { return !(sum <= FLT_MAX); }
 
 constexpr int threads_of(int group) { return group > 32 ? group : 256; }
@@ -293,10 +294,14 @@ __global__ void __launch_bounds__(threads_of(kGroup)) rms_fwd_kernel(const __gri
   }
 }
 
-// Groups of 320 and 384 threads are alone on an SM and take all the registers that they can use (145 a thread for 117; 8192 bf16
-// rows of 6144: 79.4 -> 76.0 us).
+// Groups of 320 and 384 threads with two vectors each are alone on an SM and take all the registers that they can use (145 a thread for 117; 8192
+// bf16 rows of 6144: 79.4 -> 76.0 us).  Groups of 384 to 768 with one vector, in fp32, take no more than leave room for bwd_per_sm() blocks.
+constexpr int least_blocks(int group, int vecs, bool f32) {
+  if (vecs == 2 && (group == 320 || group == 384)) return 1;
+  return f32 && vecs == 1 && group >= 384 && group <= 768 ? (1024 + group - 1) / group : 0;
+}
 template <class T, int kGroup, int kVecs>
-__global__ void __launch_bounds__(threads_of(kGroup), kVecs == 2 && (kGroup == 320 || kGroup == 384) ? 1 : 0) rms_bwd_kernel(const __grid_constant__ BwdParams p) {
+__global__ void __launch_bounds__(threads_of(kGroup), least_blocks(kGroup, kVecs, sizeof(T) == 4)) rms_bwd_kernel(const __grid_constant__ BwdParams p) {
   constexpr int kE = kElems<T>, kThreads = threads_of(kGroup), kPerBlock = kThreads / kGroup;
   __shared__ float2 s_sum[2][2][32];
   __shared__ float s_part[kGroup > 32 ? 1 : kThreads * kVecs * kE];
@@ -357,12 +362,13 @@ __global__ void __launch_bounds__(threads_of(kGroup), kVecs == 2 && (kGroup == 3
     };
     float2 s = join_sums<kGroup>(sums(1.f), s_sum[turn][0]);
     float r = rsqrtf(fmaf(s.x, p.inv_dim, p.eps)), along = s.y * p.inv_dim * r;   // mean of g times the unit row h r
-    if (kGroup > 32 ? too_large(s.x) : __any_sync(0xffffffffu, too_large(s.x))) {
+    const bool far = too_large(s.x), again = far || too_large(fabsf(s.y));
+    if (kGroup > 32 ? again : __any_sync(0xffffffffu, again)) {
       const float2 t = join_sums<kGroup>(sums(kSmall), s_sum[turn][1]);
-      if (too_large(s.x)) {
-        r = rsqrtf(t.x * p.inv_dim);
-        along = t.y * p.inv_dim * r;
-        r *= kSmall;
+      if (again) {
+        const float near = far ? rsqrtf(t.x * p.inv_dim) : r * (1.f / kSmall);
+        along = t.y * p.inv_dim * near;
+        if (far) r = near * kSmall;
       }
     }
 #pragma unroll
@@ -474,7 +480,7 @@ Shape shape_of(int vecs, int64_t rows, bool backward, bool f32) {
 
 // Blocks of an SM in the backward, which the workspace goes by as each leaves a row of sums: as many as the registers hold.  With
 // room to spare the blocks gather on the SMs that the launch before left first (8192 fp32 rows of 3000, one block of 768 threads to
-// an SM 118 us, two 64).
+// an SM 118 us, two 67).
 int bwd_per_sm(const Shape& s, bool f32) {
   if (f32 && s.vecs == 1) return (1024 + threads_of(s.group) - 1) / threads_of(s.group);
   return std::max(1, (s.vecs == 1 ? 768 : 512) / threads_of(s.group));
