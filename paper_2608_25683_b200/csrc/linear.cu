@@ -180,6 +180,10 @@ __device__ __forceinline__ uint4 narrow8(const float* v) {
   return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
+// Looks at the barrier of a tile's products before the wait for them gives up: a step takes 0.3 us, or 1.5 where all SMs wait for memory, a look with
+// its sleep some 0.1; the tile before may have to be waited for as well.  steps <= 2^24.
+__device__ __forceinline__ uint32_t looks(int steps) { return kSpinLimit + 64u * uint32_t(steps); }
+
 template <bool kFp8, Epilogue kEpilogue>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
@@ -337,7 +341,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
       }
       // one warp waits for its group: the four leave together if the wait gives up, so none is missed at their barrier
       if ((warp & 3) == 0) {
-        ok = mbar_wait(&bar.acc_full[p.share ? 0 : group], (tile >> 1) & 1, abortp, p.status);
+        ok = mbar_wait(&bar.acc_full[p.share ? 0 : group], (tile >> 1) & 1, abortp, p.status, looks(p.product[0].steps));   // the deeper one
         if (lane == 0) s_go[group][go & 1] = ok;
       }
       named_sync(bar_id, kGroupThreads);
@@ -629,7 +633,7 @@ __global__ void __launch_bounds__(kFewThreads) linear_few_kernel(const __grid_co
     // all products are done before the stages' memory takes the sums (and before this CTA leaves)
     if (ok) mbar_wait(&acc_full, 0, abortp, p.status);
   } else {
-    mbar_wait(&acc_full, 0, abortp, p.status);
+    mbar_wait(&acc_full, 0, abortp, p.status, looks(kb1 - kb0));
     tc_fence_after();
   }
   __syncthreads();

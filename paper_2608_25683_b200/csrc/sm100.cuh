@@ -45,11 +45,12 @@ __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
 // Bounded wait.  Every wait in the kernels goes through here: after
 // `kSpinLimit` polls it gives up, records PSRL_ERR_TIMEOUT (= 10) in the
 // device status word, raises the CTA-wide abort flag and returns false so the
-// caller can unwind to the common teardown (no trap, no endless loop).
+// caller can unwind to the common teardown (no trap, no endless loop).  A wait for work whose length goes by the call's sizes
+// has a limit that does, too.
 constexpr uint32_t kSpinLimit = 1u << 22;
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* s_abort,
-                                          int* g_status) {
-  for (uint32_t it = 0; it < kSpinLimit; ++it) {
+                                          int* g_status, uint32_t limit = kSpinLimit) {
+  for (uint32_t it = 0; it < limit; ++it) {
     if (mbar_test(bar, parity)) return true;
     if (it > 64) {
       __nanosleep(32);
