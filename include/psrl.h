@@ -402,7 +402,8 @@ psrl_status_t psrl_rope_axes_rows(const psrl_rope_t* rope, psrl_dtype_t dtype, c
  *   codes    [n_rows, n_heads, dim] DEVICE e4m3, codes_pitch a multiple of 16;  scales [n_rows * n_heads] DEVICE fp32, with codes
  *   workspace  DEVICE, 256-byte aligned, with d_weight >= psrl_rms_norm_workspace_bytes (asked with the call's device as the current one: it
  *            goes by its SMs); holds the device status word.  Without d_weight 256 bytes, or NULL
- * An output may be one of the call's inputs (equal pitches); otherwise tensors are apart.  dim a multiple of 8, 8..32768;
+ * An output may be one of the call's inputs (equal pitches; codes over x or residual: n_heads 1 and rows equally many bytes apart); otherwise
+ * tensors are apart, outputs from one another always.  dim a multiple of 8, 8..32768;
  * pointers 16-byte aligned (scales 4), pitches a multiple of 16 bytes and at least a row; eps > 0.
  * n_rows = 0 does nothing (backward: zeroes d_weight).
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (dtype), WORKSPACE, CUDA.  Asynchronous.

@@ -588,6 +588,11 @@ bool tensor_ok(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 bool same_rows(const void* out, int64_t out_pitch, const void* in, int64_t in_pitch, int64_t rows) {
   return !out || out != in || out_pitch == in_pitch || rows <= 1;
 }
+// A row's codes are fewer bytes than the row: over an input they have to lie at the beginning of the row that they are made of, which is read before
+// they are stored; those of a second head would lie over the first one's elements.
+bool codes_apart(const void* codes, int64_t codes_pitch, const void* in, int64_t in_pitch, psrl_dtype_t dtype, int64_t rows, int32_t heads) {
+  return !codes || codes != in || (heads == 1 && (rows <= 1 || codes_pitch == in_pitch * (dtype == PSRL_BF16 ? 2 : 4)));
+}
 constexpr int64_t kMostRows = int64_t(1) << 32;
 
 psrl_status_t check(psrl_dtype_t dtype, int64_t rows, int32_t heads, int32_t dim, float eps) {
@@ -622,7 +627,8 @@ psrl_status_t psrl_rms_norm_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t n_he
   if (n_rows == 0) return PSRL_OK;
   if (!residual) summed = nullptr;   // x itself is the stream
   if (!x || !tensor_ok(x) || !tensor_ok(residual) || !tensor_ok(weight) || !tensor_ok(summed) || !tensor_ok(y) || !tensor_ok(codes) ||
-      (!codes) != (!scales) || (scales && !ptr_aligned(scales, 4)) || (y && y == summed) ||
+      (!codes) != (!scales) || (scales && !ptr_aligned(scales, 4)) || (y && y == summed) || (codes && (codes == y || codes == summed)) ||
+      !codes_apart(codes, codes_pitch, x, x_pitch, dtype, n_rows, n_heads) || !codes_apart(codes, codes_pitch, residual, residual_pitch, dtype, n_rows, n_heads) ||
       !same_rows(summed, summed_pitch, x, x_pitch, n_rows) || !same_rows(summed, summed_pitch, residual, residual_pitch, n_rows) ||
       !same_rows(y, y_pitch, x, x_pitch, n_rows) || !same_rows(y, y_pitch, residual, residual_pitch, n_rows))
     return PSRL_ERR_INVALID_ARG;
@@ -641,7 +647,7 @@ psrl_status_t psrl_quantize_rows(psrl_dtype_t dtype, int64_t n_rows, int32_t dim
   const int64_t unit = vec_elems(dtype);
   if (!pitch_ok(x_pitch, dim, unit) || !pitch_ok(codes_pitch, dim, 16)) return PSRL_ERR_SHAPE;
   if (n_rows == 0) return PSRL_OK;
-  if (!ptr_aligned(x, 16) || !ptr_aligned(codes, 16) || !ptr_aligned(scales, 4)) return PSRL_ERR_INVALID_ARG;
+  if (!ptr_aligned(x, 16) || !ptr_aligned(codes, 16) || !ptr_aligned(scales, 4) || !codes_apart(codes, codes_pitch, x, x_pitch, dtype, n_rows, 1)) return PSRL_ERR_INVALID_ARG;
   FwdParams p{x, nullptr, nullptr, nullptr, nullptr, static_cast<uint8_t*>(codes), scales, x_pitch, 0, 0, 0, codes_pitch,
               n_rows, 1, int32_t(dim / unit), 1.f / float(dim), 0.f, 0};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
