@@ -879,6 +879,7 @@ def _rope_rows(name, rope, x, positions, axis_pitch, y, inverse, stream):
     if len(shape) != 3:
         raise ValueError("x must be [rows, heads, head_dim]")
     rows, heads, _ = shape
+    _int32(heads)
     px = _rows_pitch(x, rows, heads, rope.head_dim, "x")
     dev = _device_of(x, positions)
     raw, keep = _stream_on(stream, dev)
@@ -966,6 +967,7 @@ def _logprob_args(hidden, weight, targets, target_off, floats):
     if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1]:
         raise ValueError("hidden must be [rows, hidden_dim], weight [vocab, hidden_dim]")
     n, h = hidden.shape
+    _int32(h, weight.shape[0])
     for name, t, count in [("targets", targets, None), ("target_off", target_off, n + 1)]:
         if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (count and t.shape[0] != count)):
             raise ValueError(f"{name} must be a contiguous int32 vector" + (f" of {count}" if count else ""))
@@ -1042,6 +1044,13 @@ def psrl_token_logprob_bwd(hidden, weight, targets, logprob, lse, d_logprob, tar
     return tuple(out)
 
 
+def _int32(*sizes):
+    """Sizes that the library takes in 32 bits; ctypes would cut larger ones off without a word."""
+    for n in sizes:
+        if n > 0x7fffffff:
+            raise ValueError(f"{n} is beyond the library's dimensions")
+
+
 def _stream_rows(t, shape, name: str, like=None) -> int:
     """Row pitch of a [rows, dim] or [rows, heads, dim] tensor of `shape`, of the type and on the device of `like`."""
     if t.shape != shape or (like is not None and (t.dtype is not like.dtype or t.get_device() != like.get_device())):
@@ -1071,6 +1080,7 @@ def _norm_args(x, weight):
         rows, heads, dim = shape
     else:
         raise ValueError("rows must be [rows, dim] or [rows, heads, dim]")
+    _int32(heads, dim)
     dev = x.get_device()
     if dev < 0:
         raise RuntimeError("tensors must live on a CUDA device: this library has no CPU path")
@@ -1226,6 +1236,7 @@ def _linear_args(x, weight, activation):
         raise ValueError("x must be [rows, in_dim], weight [out_dim, in_dim]")
     if activation not in _ACTIVATIONS:
         raise ValueError(f"activation {activation!r} unknown")
+    _int32(xs[1], ws[0])
     return dt, xs[0], xs[1], ws[0], _device_of(x, weight), out
 
 
