@@ -150,7 +150,14 @@ bool double_of(PyObject* o, double& v) {
   }
   return true;
 }
-bool truth(PyObject* o) { return PyObject_IsTrue(o) == 1; }
+// what has no truth value is the wrapper's to refuse
+bool truth(Call& c, PyObject* o) {
+  const int t = PyObject_IsTrue(o);
+  if (t >= 0) return t == 1;
+  PyErr_Clear();
+  c.ok = false;
+  return false;
+}
 
 // The sizes of a norm: x [rows, dim] or [rows, heads, dim], f32 or bf16; weight [dim] or None.
 struct Norm {
@@ -181,7 +188,7 @@ PyObject* rms_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Norm m(c, x, a[1]);
     const Tensor* res = c.like(a[3], c.type);
     const int64_t px = c.rows(x, m.rows, m.heads, m.dim, m.dims), pr = c.rows(res, m.rows, m.heads, m.dim, m.dims), least = m.heads * m.dim;
-    const bool want_y = truth(a[4]), want_codes = truth(a[5]);
+    const bool want_y = truth(c, a[4]), want_codes = truth(c, a[5]);
     if (!c.ok || (want_codes && least % 16)) return none();
     Tensor y, summed, codes, scales;
     const psrl_status_t st = unlocked([&] {
@@ -209,8 +216,8 @@ PyObject* rms_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Norm m(c, h, a[1]);
     const Tensor *dy = c.like(a[2], c.type), *ds = c.like(a[4], c.type);
     const int64_t ph = c.rows(h, m.rows, m.heads, m.dim, m.dims), pd = c.rows(dy, m.rows, m.heads, m.dim, m.dims), ps = c.rows(ds, m.rows, m.heads, m.dim, m.dims);
+    const bool want_x = truth(c, a[5]), want_w = truth(c, a[6]) && m.weight;
     if (!c.ok || !dy) return none();
-    const bool want_x = truth(a[5]), want_w = truth(a[6]) && m.weight;
     const psrl_dtype_t t = psrl_dtype_t(code_of(c.type));
     Tensor dx, dw, ws;
     const psrl_status_t st = unlocked([&] {
@@ -265,9 +272,9 @@ PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const void* bias = c.vector(c.like(a[2], p.out), p.n);
     const void *sx = c.vector(c.like(a[6], at::kFloat), p.m), *sw = c.vector(c.like(a[7], at::kFloat), p.n);
     const int64_t pm = c.matrix(mul, p.m, p.n), pr = c.matrix(res, p.m, p.n);
+    const bool want_z = truth(c, a[8]);
     if (!c.ok || codes != (a[6] != Py_None) || codes != (a[7] != Py_None)) return none();
     const psrl_dtype_t t = psrl_dtype_t(code_of(c.type));
-    const bool want_z = truth(a[8]);
     Tensor y, z, ws;
     const psrl_status_t st = unlocked([&] {
       int64_t py, pz = 0;
@@ -296,8 +303,8 @@ PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!c.ok || c.type == at::kFloat8_e4m3fn) return none();
     const Tensor *dy = c.like(a[2], c.type), *z = c.like(a[3], c.type), *mul = c.like(a[5], c.type);
     const int64_t pd = c.matrix(dy, p.m, p.n), pz = c.matrix(z, p.m, p.n), pm = c.matrix(mul, p.m, p.n);
+    const bool want_x = truth(c, a[6]), want_w = truth(c, a[7]), want_b = truth(c, a[8]), want_m = truth(c, a[9]);
     if (!c.ok || !dy) return none();
-    const bool want_x = truth(a[6]), want_w = truth(a[7]), want_b = truth(a[8]), want_m = truth(a[9]);
     const psrl_dtype_t t = psrl_dtype_t(code_of(c.type));
     Tensor dx, dw, db, dm, ws;
     const psrl_status_t st = unlocked([&] {
@@ -419,8 +426,8 @@ PyObject* rope_axes_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t rows = x->size(0), heads = x->size(1);
     const Tensor* pos = c.like(a[4], at::kInt);
     const int64_t px = c.rows(x, rows, heads, d, 3), pa = positions_of(c, pos, axes, rows);
+    const bool inverse = truth(c, a[5]);
     if (!c.ok || heads > INT32_MAX) return none();
-    const bool inverse = truth(a[5]);
     Tensor y;
     const psrl_status_t st = unlocked([&] {
       y = c.make(x->sizes(), c.type);
