@@ -437,10 +437,10 @@ def psrl_tree_attn_bwd(plan: Plan, q, k_pool, v_pool, o, lse, d_o, softmax_scale
 
 
 class Workspace:
-    """Device memory for a call's temporaries and its status word, for psrl_kv_move and the token log-probabilities
-    (`workspace=`).  status() tells whether a wait inside the kernels gave up; without a workspace of one's own the
-    log-probabilities make one that is gone when the call returns, and its status with it.  Calls that may overlap on the GPU
-    need workspaces of their own."""
+    """Device memory for a call's temporaries and its status word, for psrl_kv_move, the token log-probabilities, products and the norms'
+    gradients (`workspace=`).  status() tells whether a wait inside the kernels gave up; without a workspace of one's own the
+    log-probabilities, products and norms make one that is gone when the call returns (or need none), and its status with it.  Calls that
+    may overlap on the GPU need workspaces of their own."""
 
     __slots__ = ("ptr", "nbytes", "_buf", "_home", "_raw")
 
@@ -1292,7 +1292,7 @@ def psrl_linear_fwd(x, weight, bias=None, activation=None, mul=None, residual=No
     (float8_e4m3fn) with float32 x_scale [rows] and weight_scale [out_dim], the rest then bf16.  activation: None, "relu", "silu",
     "gelu", "gelu_tanh".  Returns (y, z), z = x weight^T + bias with want_z (for the backward), else None.  y and z may be mul or
     residual.  `workspace`: a Workspace of psrl_linear_workspace_bytes(), whose status() tells whether a wait inside the kernel gave
-    up; made if not given."""
+    up; without one it cannot be asked."""
     if stream is None and y is None and z is None and workspace is None and activation in _ACTIVATIONS:
         r = (_torch_calls or _calls()).linear_fwd(x, weight, bias, _ACTIVATIONS[activation], mul, residual, x_scale, weight_scale, want_z)
         if r is not None:

@@ -10,6 +10,9 @@
 // Operands lie K-major in the forward; in the gradients the weights, x and, for d_weight, dz lie with the other side contiguous
 // (MN-major), which the descriptors of shared memory take as they are: nothing is transposed in memory.
 // The epilogue's own operands (residual, mul) come through TMA into the buffers that its results leave from.
+//
+// dz is rounded to bf16 before the gradients' products, as the tensor cores take their operands in pairs of a type: d_x and d_weight are 2.3e-3 from 64
+// bits in the 2-norm, of which 1.7e-3 are their own rounding.  A second bf16 part of it would double the products, which are the call's time.
 #include <cuda_bf16.h>
 
 #include <algorithm>
