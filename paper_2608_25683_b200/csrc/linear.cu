@@ -63,6 +63,8 @@ struct Params {
   int32_t ratio;                // tiles of the second that cost one of the first
   const __nv_bfloat16* bias;
   const float *x_scale, *w_scale;
+  __nv_bfloat16 *y, *z;         // of the first product, for the columns behind the last whole 16 bytes of a row
+  int64_t y_pitch, z_pitch;
   int32_t act, has_mul, has_residual, has_z;
   int32_t share;                // no pair has more than one tile
   int32_t clear;                // the call's first kernel: it clears the status, the later ones leave what those before them recorded
@@ -178,6 +180,13 @@ __device__ __forceinline__ void mul8(float* v, const uint4& x) {
     v[2 * i] *= __uint_as_float(w[i] << 16);
     v[2 * i + 1] *= __uint_as_float(w[i] & 0xffff0000u);
   }
+}
+// the first `count` of eight bf16
+__device__ __forceinline__ void store_few(__nv_bfloat16* at, const uint4& x, int count) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 7; ++i)
+    if (i < count) at[i] = __ushort_as_bfloat16(static_cast<unsigned short>(w[i / 2] >> (i % 2 * 16)));
 }
 __device__ __forceinline__ uint4 narrow8(const float* v) {
   return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
@@ -452,11 +461,19 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
 #pragma unroll
           for (int j = 0; j < 4; ++j) put16(first, gt, h * 4 + j, narrow8(&v[j * 8]));
         }
+        // A copy to memory ends with whole 16 bytes whatever the tensor's extent: what lies behind a row's last whole ones is stored by its thread.
+        const int whole = q.N & ~7;
+        if (whole < q.N && whole >= col && whole < col + 64 && row0 + gt < q.M) {
+          store_few(p.y + (row0 + gt) * p.y_pitch + whole, get16(first, gt, (whole - col) / 8), q.N - whole);
+          if (kEpilogue == kFull && p.has_z) store_few(p.z + (row0 + gt) * p.z_pitch + whole, get16(second, gt, (whole - col) / 8), q.N - whole);
+        }
         fence_proxy_async();
         named_sync(bar_id, kGroupThreads);
         if (gt == 0) {
-          tma_store_2d(&maps.out[which], first, col, row0);
-          if (kEpilogue == kFull && p.has_z) tma_store_2d(&maps.z, second, col, row0);
+          if (col < whole) {
+            tma_store_2d(&maps.out[which], first, col, row0);
+            if (kEpilogue == kFull && p.has_z) tma_store_2d(&maps.z, second, col, row0);
+          }
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
       }
@@ -1130,12 +1147,15 @@ psrl_status_t psrl_linear_fwd(psrl_dtype_t dtype, int64_t n_rows, int32_t in_dim
   const bool full = mul || residual || z;
   bool made = fp8 ? make_map_u8_2d(&maps.a[0], x, in_dim, M, x_pitch, 128) && make_map_u8_2d(&maps.b[0], weight, in_dim, N, weight_pitch, half)
                   : make_map_bf16_2d(&maps.a[0], x, in_dim, M, x_pitch * 2, 128) && make_map_bf16_2d(&maps.b[0], weight, in_dim, N, weight_pitch * 2, half);
-  made = made && make_map_bf16_2d(&maps.out[0], y, N, M, y_pitch * 2, 128);
+  const int64_t whole = N >= 8 ? N / 8 * 8 : N;   // columns that leave by copies; fewer than eight leave without
+  made = made && make_map_bf16_2d(&maps.out[0], y, whole, M, y_pitch * 2, 128);
   if (mul) made = made && make_map_bf16_2d(&maps.mul, mul, N, M, mul_pitch * 2, 128);
   if (residual) made = made && make_map_bf16_2d(&maps.residual, residual, N, M, residual_pitch * 2, 128);
-  if (z) made = made && make_map_bf16_2d(&maps.z, z, N, M, z_pitch * 2, 128);
+  if (z) made = made && make_map_bf16_2d(&maps.z, z, whole, M, z_pitch * 2, 128);
   if (!made) return PSRL_ERR_CUDA;
   p.bias = static_cast<const __nv_bfloat16*>(bias);
+  p.y = static_cast<__nv_bfloat16*>(y); p.y_pitch = y_pitch;
+  p.z = static_cast<__nv_bfloat16*>(z); p.z_pitch = z_pitch;
   p.x_scale = x_scale; p.w_scale = weight_scale;
   p.act = activation;
   p.has_mul = mul != nullptr; p.has_residual = residual != nullptr; p.has_z = z != nullptr;

@@ -52,7 +52,8 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
       "h"(uint16_t(3))
       : "memory");
 }
-// A box from shared memory to a tiled tensor map, or added to what is there (fp32).  Parts outside the tensor are dropped.
+// A box from shared memory to a tiled tensor map, or added to what is there (fp32).  Parts outside the tensor are dropped, but for what makes up
+// the last 16 bytes of its rows: extents that leave are whole 16 bytes.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* smem_src, int x, int y) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(reinterpret_cast<uint64_t>(m)),
                "r"(smem_u32(smem_src)), "r"(x), "r"(y)
