@@ -196,7 +196,8 @@ __device__ __forceinline__ uint4 narrow8(const float* v) {
 // its sleep some 0.1; the tile before may have to be waited for as well.  steps <= 2^24.
 __device__ __forceinline__ uint32_t looks(int steps) { return kSpinLimit + 64u * uint32_t(steps); }
 
-template <bool kFp8, Epilogue kEpilogue>
+// kRagged: a row of the result ends inside 16 bytes.  (In every call the columns behind its last whole ones would cost 1 to 2 % of a shallow product.)
+template <bool kFp8, Epilogue kEpilogue, bool kRagged>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
   extern __shared__ uint8_t smem_raw[];
@@ -333,6 +334,7 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
       if (!p.share && (tile & 1) != uint32_t(group)) continue;
       const Product& q = p.product[which];
       const int row0 = mt * 256 + int(rank) * 128, n0 = nt * q.tile_n, n_end = min(n0 + q.tile_n, q.N);
+      [[maybe_unused]] const int whole = q.N & ~7;
       const int chunk0 = p.share ? group : 0, stride = p.share ? 128 : 64;   // columns from one of this group's chunks to the next
       const int all = row0 < q.M ? (n_end - n0 + 63) / 64 : 0, chunks = p.share ? (all + 1 - group) / 2 : all;
       int issued = 0;
@@ -461,16 +463,10 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
 #pragma unroll
           for (int j = 0; j < 4; ++j) put16(first, gt, h * 4 + j, narrow8(&v[j * 8]));
         }
-        // A copy to memory ends with whole 16 bytes whatever the tensor's extent: what lies behind a row's last whole ones is stored by its thread.
-        const int whole = q.N & ~7;
-        if (whole < q.N && whole >= col && whole < col + 64 && row0 + gt < q.M) {
-          store_few(p.y + (row0 + gt) * p.y_pitch + whole, get16(first, gt, (whole - col) / 8), q.N - whole);
-          if (kEpilogue == kFull && p.has_z) store_few(p.z + (row0 + gt) * p.z_pitch + whole, get16(second, gt, (whole - col) / 8), q.N - whole);
-        }
         fence_proxy_async();
         named_sync(bar_id, kGroupThreads);
         if (gt == 0) {
-          if (col < whole) {
+          if (!kRagged || col < whole) {
             tma_store_2d(&maps.out[which], first, col, row0);
             if (kEpilogue == kFull && p.has_z) tma_store_2d(&maps.z, second, col, row0);
           }
@@ -478,6 +474,19 @@ linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params 
         }
       }
       if (!ok) break;
+      // A copy to memory ends with whole 16 bytes whatever the tensor's extent: what lies behind a row's last whole ones, in the last chunk
+      // of the last column tile, is stored by its thread.
+      if (kRagged && whole < n_end && chunks > 0) {
+        const int col = n0 + chunk0 * 64 + (chunks - 1) * stride;
+        const uint32_t n = base + uint32_t((chunks - 1) * per);
+        if (col <= whole && whole < col + 64) {
+          if (row0 + gt < q.M) {
+            store_few(p.y + (row0 + gt) * p.y_pitch + whole, get16(buf + int((n + uint32_t(per) - 1) % kBuffers) * kOutBytes, gt, (whole - col) / 8), q.N - whole);
+            if (kEpilogue == kFull && p.has_z) store_few(p.z + (row0 + gt) * p.z_pitch + whole, get16(buf + int(n % kBuffers) * kOutBytes, gt, (whole - col) / 8), q.N - whole);
+          }
+          named_sync(bar_id, kGroupThreads);   // before the buffers are loaded again
+        }
+      }
       base += uint32_t(chunks * per);
       // the accumulator may be overwritten
       tc_fence_before();
@@ -891,17 +900,22 @@ int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t dz_rows(int64_t M) { return std::max<int64_t>(kDzRows, div_up(M, 65535)); }   // at most 65,535 blocks of rows
 
+template <bool kFp8, Epilogue kEpilogue, bool kRagged>
+cudaError_t launch_gemm_as(const Maps& maps, const Params& p, int clusters, cudaStream_t stream) {
+  static bool done[64] = {};
+  const cudaError_t e = ensure_dynamic_smem(linear_kernel<kFp8, kEpilogue, kRagged>, gemm_smem(kEpilogue), done);
+  if (e != cudaSuccess) return e;
+  return launch(linear_kernel<kFp8, kEpilogue, kRagged>, dim3(2 * clusters), kGemmThreads, gemm_smem(kEpilogue), stream, maps, p);
+}
 template <bool kFp8, Epilogue kEpilogue>
 cudaError_t launch_gemm(const Maps& maps, Params& p, cudaStream_t stream) {
-  static bool done[64] = {};
-  cudaError_t e = ensure_dynamic_smem(linear_kernel<kFp8, kEpilogue>, gemm_smem(kEpilogue), done);
-  if (e != cudaSuccess) return e;
   int64_t tiles = 0;
   for (const Product& q : p.product) tiles += int64_t(q.m_tiles) * q.n_tiles;
   if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int clusters = static_cast<int>(std::min<int64_t>(tiles, resident_ctas() / 2));
   p.share = tiles <= clusters;
-  return launch(linear_kernel<kFp8, kEpilogue>, dim3(2 * clusters), kGemmThreads, gemm_smem(kEpilogue), stream, maps, p);
+  if (p.product[0].N % 8) return launch_gemm_as<kFp8, kEpilogue, true>(maps, p, clusters, stream);
+  return launch_gemm_as<kFp8, kEpilogue, false>(maps, p, clusters, stream);
 }
 
 Product product_of(int64_t M, int64_t N, int64_t depth, int64_t step, int tile_n, int a_mn, int b_mn, int64_t group_bytes) {
